@@ -564,6 +564,72 @@ acrl_status acrl_lmhead_stats_noalloc(const acrl_bf16* hidden, int64_t M, int64_
                                       float* lse, float* logp, float* entropy,
                                       int32_t* dev_flags, acrl_stream stream);
 
+/* ------------------------------------------------------------------------
+ * 8-bit matrices.  A rollout engine that runs in FP8, or a frozen reference
+ * policy beside the trained one, computes its linear layers on such matrices;
+ * the paper's discrepancy is what they differ by from BF16 (Sec. 5.1).
+ *
+ * An 8-bit matrix is its elements, uint8 [rows, ldq] (row-major, 16-byte
+ * aligned, ldq a multiple of 16), and its scales, uint8 [scale rows, lds]: byte
+ * s of block (r, c) stands for the factor 2^(s - 127), 255 for NaN.  A block
+ * is 128 columns of one row (ACRL_FP8_ROW: a scale row per row) or of 128 rows
+ * (ACRL_FP8_TILE: a scale row per 128 rows); the last ones may be shorter.
+ * lds >= ceil(columns / 128); a multiple of 4 lets the product read the scales
+ * of four blocks at once.
+ */
+typedef enum { ACRL_BF16 = 0, ACRL_F32 = 1 } acrl_dtype;
+typedef enum { ACRL_FP8_E4M3 = 0, ACRL_FP8_E5M2 = 1 } acrl_fp8_format;   /* e4m3fn (largest 448) and e5m2 (57344) */
+typedef enum { ACRL_FP8_ROW = 0, ACRL_FP8_TILE = 1 } acrl_fp8_block;
+
+/*
+ * acrl_fp8_quantize -- x, or its transpose, as an 8-bit matrix.  Per block, with
+ * a the largest absolute value: 2^e is the smallest power of two, e >= -127, with
+ * a <= MAX 2^e (e = 0 where a = 0), and every element is x 2^-e rounded to
+ * the nearest (ties to even) number of the format; x 2^-e itself is exact.
+ * A block with an infinity or a NaN is NaN throughout (elements 0x7f, scale 255),
+ * which the product carries into every output it touches, and raises NONFINITE.
+ *   x      device bf16 or float [R, ldx], C columns used; 16-byte aligned, ldx
+ *          a multiple of 8 (bf16) or 4 (float).
+ *   q      device uint8 [R, ldq], or [C, ldq] with `transpose` (blocks then run
+ *          along x's rows): what the gradient products contract over.
+ *   scale  device uint8, the scales of q.
+ * Columns of q and scale beyond the matrix are not written.
+ */
+acrl_status acrl_fp8_quantize(const void* x, acrl_dtype x_dtype, int64_t R, int64_t C, int64_t ldx,
+                              acrl_fp8_format format, acrl_fp8_block block, int32_t transpose,
+                              uint8_t* q, int64_t ldq, uint8_t* scale, int64_t lds,
+                              int32_t* dev_flags, acrl_stream stream);
+
+/*
+ * acrl_fp8_matmul -- out = A B^T on the tensor cores (A [M, K], B [N, K]), each
+ * product scaled by both of its blocks' factors, accumulated in fp32 and
+ * rounded once.  Either operand in either format and with either block.
+ *   out   device bf16 or float [M, ldo], 16-byte aligned, ldo >= N a multiple of
+ *         8; columns from N on are not written.
+ * The operands must be device memory of the current device, as for the LM head.
+ * K = 0 gives zeros.  Waits are time-bounded (ACRL_FLAG_TIMEOUT: the outputs are
+ * invalid).
+ */
+acrl_status acrl_fp8_matmul(const uint8_t* a, int64_t M, int64_t K, int64_t lda, acrl_fp8_format a_format,
+                            const uint8_t* a_scale, int64_t ldas, acrl_fp8_block a_block,
+                            const uint8_t* b, int64_t N, int64_t ldb, acrl_fp8_format b_format,
+                            const uint8_t* b_scale, int64_t ldbs, acrl_fp8_block b_block,
+                            void* out, acrl_dtype out_dtype, int64_t ldo, int32_t* dev_flags, acrl_stream stream);
+
+/*
+ * acrl_fp8_linear -- out = Q(x) W^T: acrl_fp8_quantize of the activations by
+ * rows, then acrl_fp8_matmul, in one call (one token or many).
+ *   x          device bf16 [M, ldx].
+ *   workspace  device, 16-byte aligned, of acrl_fp8_linear_workspace_bytes(M, K)
+ *              bytes: the quantised activations.
+ */
+int64_t     acrl_fp8_linear_workspace_bytes(int64_t M, int64_t K);
+acrl_status acrl_fp8_linear(const acrl_bf16* x, int64_t M, int64_t K, int64_t ldx, acrl_fp8_format x_format,
+                            const uint8_t* w, int64_t N, int64_t ldw, acrl_fp8_format w_format,
+                            const uint8_t* w_scale, int64_t ldws, acrl_fp8_block w_block,
+                            void* out, acrl_dtype out_dtype, int64_t ldo, void* workspace, int64_t workspace_bytes,
+                            int32_t* dev_flags, acrl_stream stream);
+
 /*
  * acrl_selftest_wait_timeout -- failure-detection self-test: one warp waits on
  * a shared-memory barrier that nothing arrives on, with the same bounded wait

@@ -25,6 +25,9 @@ MODE_NONE, MODE_TIS, MODE_MIS, MODE_ACRL, MODE_ACRL_CONTINUOUS, MODE_ACRL_FALLBA
 Y_GROUP, Y_SEQUENCE, Y_BATCH = 0, 1, 2
 AGG_SEQ_MEAN_TOKEN_MEAN, AGG_TOKEN_MEAN = 0, 1
 SINGLETON_MEAN0_STD1, SINGLETON_ZERO = 0, 1
+BF16, F32 = 0, 1
+FP8_E4M3, FP8_E5M2 = 0, 1
+FP8_ROW, FP8_TILE = 0, 1
 
 
 class Params(ctypes.Structure):
@@ -92,6 +95,13 @@ SIGNATURES = {
     "acrl_lmhead_merge": (c_i32, [c_p, c_p, c_i64, c_i64, c_i64, c_p, c_p, c_p, c_p, c_p, c_p, c_p]),
     "acrl_lmhead_stats_noalloc": (c_i32, [c_p, c_i64, c_i64, c_i64, c_p, c_i64, c_i64, c_p, c_i64, c_p, c_p, c_p,
                                           c_p, c_p, c_p, c_p]),
+    "acrl_fp8_quantize": (c_i32, [c_p, c_i32, c_i64, c_i64, c_i64, c_i32, c_i32, c_i32, c_p, c_i64, c_p, c_i64, c_p,
+                                  c_p]),
+    "acrl_fp8_matmul": (c_i32, [c_p, c_i64, c_i64, c_i64, c_i32, c_p, c_i64, c_i32, c_p, c_i64, c_i64, c_i32, c_p, c_i64,
+                                c_i32, c_p, c_i32, c_i64, c_p, c_p]),
+    "acrl_fp8_linear_workspace_bytes": (c_i64, [c_i64, c_i64]),
+    "acrl_fp8_linear": (c_i32, [c_p, c_i64, c_i64, c_i64, c_i32, c_p, c_i64, c_i64, c_i32, c_p, c_i64, c_i32, c_p, c_i32,
+                                c_i64, c_p, c_i64, c_p, c_p]),
     "acrl_read_flags": (c_i32, [c_p, ctypes.POINTER(c_i32), c_p]),
     "acrl_check_flags": (c_i32, [c_p, c_p]),
     "acrl_selftest_wait_timeout": (c_i32, [c_p, c_i64, c_p]),

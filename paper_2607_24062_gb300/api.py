@@ -431,6 +431,161 @@ def lmhead_stats_noalloc(hidden, weight, ids, mask=None, *, N=None, logits=None,
     return logits, lse, logp, entropy
 
 
+# ---------------------------------------------------------------------------
+# 8-bit matrices
+# ---------------------------------------------------------------------------
+
+_FP8 = {"e4m3": (_abi.FP8_E4M3, torch.float8_e4m3fn), "e5m2": (_abi.FP8_E5M2, torch.float8_e5m2)}
+_FP8_FORMAT = {dtype: code for code, dtype in _FP8.values()}
+_FP8_BLOCK = {"row": _abi.FP8_ROW, "tile": _abi.FP8_TILE}
+_OUT_DTYPE = {torch.bfloat16: _abi.BF16, torch.float32: _abi.F32}
+
+
+@dataclass
+class Fp8Tensor:
+    """An 8-bit matrix [rows, cols]: q (torch.float8_e4m3fn or float8_e5m2, rows at a stride of 16 bytes) and the
+    scales of its blocks, uint8 [rows or ceil(rows / 128), ceil(cols / 128)], byte s standing for 2^(s - 127)."""
+
+    q: torch.Tensor
+    scale: torch.Tensor
+
+    def __post_init__(self):
+        q, s = self.q, self.scale
+        if q.dtype not in _FP8_FORMAT or q.dim() != 2 or not q.is_cuda or (q.shape[1] > 1 and q.stride(1) != 1):
+            raise AcrlError("q: expected a 2-D float8_e4m3fn or float8_e5m2 CUDA tensor with unit column stride")
+        if s.dtype != torch.uint8 or s.dim() != 2 or not s.is_cuda or (s.shape[1] > 1 and s.stride(1) != 1):
+            raise AcrlError("scale: expected a 2-D uint8 CUDA tensor with unit column stride")
+        R, C = q.shape
+        if s.shape[1] < (C + 127) // 128 or s.shape[0] not in (R, (R + 127) // 128):
+            raise AcrlError(f"scale: shape {tuple(s.shape)} fits neither the rows nor the 128 x 128 tiles of "
+                            f"{tuple(q.shape)}")
+        # one row is one tile of one row: the same scales either way
+        self.block = "row" if s.shape[0] == R else "tile"
+
+    @property
+    def shape(self):
+        return self.q.shape
+
+    def values(self) -> torch.Tensor:
+        """The float32 matrix that the bytes stand for (for inspection)."""
+        R, C = self.q.shape
+        e = self.scale[:, : (C + 127) // 128].to(torch.int32)
+        s = torch.where(e > 0, e << 23, 1 << 22).view(torch.float32)    # 2^(s - 127); 2^-127 has no leading one
+        s = torch.where(e == 255, torch.nan, s)
+        if self.block == "tile":
+            s = s.repeat_interleave(128, 0)[:R]
+        return self.q.to(torch.float32) * s.repeat_interleave(128, 1)[:, :C]
+
+
+def _ld(t: torch.Tensor) -> int:
+    """The row stride of a matrix; where there is at most one row, or nothing in a row, any that a kernel accepts."""
+    return t.stride(0) if t.shape[0] > 1 and t.shape[1] > 0 else (t.shape[1] + 15) // 16 * 16
+
+
+def _fp8_args(t: Fp8Tensor, name: str):
+    if not isinstance(t, Fp8Tensor):
+        raise AcrlError(f"{name}: expected an Fp8Tensor")
+    lds = t.scale.stride(0) if t.scale.shape[0] > 1 and t.scale.shape[1] > 0 else t.scale.shape[1]
+    return _ptr(t.q), t.q.shape[0], _ld(t.q), _FP8_FORMAT[t.q.dtype], _ptr(t.scale), lds, _FP8_BLOCK[t.block]
+
+
+def _fp8_format(fmt: str) -> int:
+    if fmt not in _FP8:
+        raise AcrlError(f"fmt: {fmt!r}, expected one of {sorted(_FP8)}")
+    return _FP8[fmt][0]
+
+
+def fp8_quantize(x, *, block="row", fmt="e4m3", transpose=False, out: Fp8Tensor | None = None, flags=None,
+                 stream=None) -> Fp8Tensor:
+    """acrl_fp8_quantize: x (bf16 or float32 [R, C]) or its transpose as an 8-bit matrix with power-of-two scales per
+    128 columns of a row (block="row") or per 128 x 128 ("tile")."""
+    if not isinstance(x, torch.Tensor) or x.dtype not in _OUT_DTYPE or x.dim() != 2 or not x.is_cuda or \
+            (x.shape[1] > 1 and x.stride(1) != 1):
+        raise AcrlError("x: expected a 2-D bfloat16 or float32 CUDA tensor with unit column stride")
+    if block not in _FP8_BLOCK:
+        raise AcrlError(f"block: {block!r}, expected one of {sorted(_FP8_BLOCK)}")
+    code = _fp8_format(fmt)
+    R, C = x.shape
+    rows, cols = (C, R) if transpose else (R, C)
+    srows, kb = (rows if block == "row" else (rows + 127) // 128), (cols + 127) // 128
+    if out is None:
+        q = torch.empty((rows, (cols + 15) // 16 * 16), dtype=_FP8[fmt][1], device=x.device)[:, :cols]
+        out = Fp8Tensor(q, torch.empty((srows, (kb + 3) // 4 * 4), dtype=torch.uint8, device=x.device)[:, :kb])
+    elif tuple(out.q.shape) != (rows, cols) or out.q.dtype != _FP8[fmt][1] or out.scale.shape[0] != srows:
+        raise AcrlError(f"out: an 8-bit matrix of another shape, format or block than {(rows, cols)} {fmt} {block}")
+    flags = _flags(flags, x.device)
+    ptr, _, ldq, _, sptr, lds, _ = _fp8_args(out, "out")
+    _call("acrl_fp8_quantize", (x, out.q, out.scale, flags), stream, _ptr(x), _OUT_DTYPE[x.dtype], R, C, _ld(x), code,
+          _FP8_BLOCK[block], int(transpose), ptr, ldq, sptr, lds, _ptr(flags))
+    return out
+
+
+def _product_out(out, M: int, N: int, dtype, dev):
+    """(`out` as [M, N], its row stride)."""
+    if out is None:
+        out = torch.empty((M, (N + 7) // 8 * 8), dtype=dtype, device=dev)
+    if not isinstance(out, torch.Tensor) or out.dtype not in _OUT_DTYPE or out.dim() != 2 or not out.is_cuda or \
+            (out.shape[1] > 1 and out.stride(1) != 1) or out.shape[0] != M or out.shape[1] < N:
+        raise AcrlError(f"out: expected a bfloat16 or float32 CUDA matrix of {(M, N)} with unit column stride")
+    return out[:, :N], out.stride(0) if M > 1 and N > 0 else (N + 7) // 8 * 8
+
+
+def fp8_matmul(a: Fp8Tensor, b: Fp8Tensor, *, out_dtype=torch.bfloat16, out=None, flags=None, stream=None):
+    """acrl_fp8_matmul: a [M, K] times the transpose of b [N, K], as `out_dtype` [M, N]."""
+    aa, bb = _fp8_args(a, "a"), _fp8_args(b, "b")
+    M, N, K = a.shape[0], b.shape[0], a.shape[1]
+    if b.shape[1] != K:
+        raise AcrlError(f"a and b disagree on K: {K} and {b.shape[1]}")
+    if out_dtype not in _OUT_DTYPE:
+        raise AcrlError(f"out_dtype: {out_dtype}, expected bfloat16 or float32")
+    out, ldo = _product_out(out, M, N, out_dtype, a.q.device)
+    flags = _flags(flags, a.q.device)
+    _call("acrl_fp8_matmul", (a.q, a.scale, b.q, b.scale, out, flags), stream, aa[0], M, K, *aa[2:], bb[0], N, *bb[2:],
+          _ptr(out), _OUT_DTYPE[out.dtype], ldo, _ptr(flags))
+    return out
+
+
+def fp8_linear_workspace_bytes(M: int, K: int) -> int:
+    """acrl_fp8_linear_workspace_bytes."""
+    return int(lib().acrl_fp8_linear_workspace_bytes(M, K))
+
+
+def fp8_linear(x, weight: Fp8Tensor, *, fmt="e4m3", out_dtype=torch.bfloat16, out=None, workspace=None, flags=None,
+               stream=None):
+    """acrl_fp8_linear: x (bf16 [M, K]) quantised by rows, times the transpose of `weight` [N, K]; [M, N]."""
+    if not isinstance(x, torch.Tensor) or x.dtype != torch.bfloat16 or x.dim() != 2 or not x.is_cuda or \
+            (x.shape[1] > 1 and x.stride(1) != 1):
+        raise AcrlError("x: expected a 2-D bfloat16 CUDA tensor with unit column stride")
+    w = _fp8_args(weight, "weight")
+    M, K, N = x.shape[0], x.shape[1], weight.shape[0]
+    if weight.shape[1] != K:
+        raise AcrlError(f"x and weight disagree on K: {K} and {weight.shape[1]}")
+    if out_dtype not in _OUT_DTYPE:
+        raise AcrlError(f"out_dtype: {out_dtype}, expected bfloat16 or float32")
+    out, ldo = _product_out(out, M, N, out_dtype, x.device)
+    n = fp8_linear_workspace_bytes(M, K)
+    workspace = torch.empty(n, dtype=torch.uint8, device=x.device) if workspace is None else \
+        _need(workspace, torch.uint8, n, "workspace")
+    flags = _flags(flags, x.device)
+    _call("acrl_fp8_linear", (x, weight.q, weight.scale, out, workspace, flags), stream, _ptr(x), M, K, _ld(x),
+          _fp8_format(fmt), w[0], N, *w[2:], _ptr(out), _OUT_DTYPE[out.dtype], ldo, _ptr(workspace), workspace.numel(),
+          _ptr(flags))
+    return out
+
+
+def fp8_linear_backward(dy, x, weight_t: Fp8Tensor, *, fmt="e4m3", dx_dtype=torch.bfloat16, dw_dtype=torch.float32,
+                        flags=None, stream=None):
+    """The gradients of y = x W^T: dx = Q(dy) W and dw = Q(dy^T) Q(x^T)^T, products of 8-bit matrices over N and over
+    the rows.  dy [M, N] and x [M, K] bf16; `weight_t` is the 8-bit W^T [K, N] (fp8_quantize(w, block="tile",
+    transpose=True)); `fmt` is dy's format.  Returns (dx [M, K], dw [N, K])."""
+    flags = _flags(flags, dy.device)
+    kw = dict(flags=flags, stream=stream)
+    dx = fp8_matmul(fp8_quantize(dy, fmt=fmt, **kw), weight_t, out_dtype=dx_dtype, **kw)
+    dw = fp8_matmul(fp8_quantize(dy, fmt=fmt, transpose=True, **kw), fp8_quantize(x, transpose=True, **kw),
+                    out_dtype=dw_dtype, **kw)
+    return dx, dw
+
+
 def selftest_wait_timeout(flags, limit_ns: int, stream=None) -> None:
     """acrl_selftest_wait_timeout: a bounded wait on a barrier nothing arrives on."""
     _need(flags, torch.int32, 1, "flags")
@@ -533,6 +688,7 @@ def check_flags(flags, stream=None) -> None:
 __all__ = ["Params", "AcrlError", "token_stats", "seq_discrepancy", "grpo_advantage", "controller_init",
            "controller_step", "importance_weights", "step", "loss_grad_logits", "reduce_loss", "scale_grad",
            "read_flags", "check_flags", "read_state", "Discrepancy",
+           "Fp8Tensor", "fp8_quantize", "fp8_matmul", "fp8_linear", "fp8_linear_backward", "fp8_linear_workspace_bytes",
            "lmhead_logits_stats", "lmhead_merge", "lmhead_workspace_bytes", "lmhead_stats_noalloc", "save_state",
            "load_state", "controller_save", "controller_load", "selftest_wait_timeout",
            "host_pipeline_workspace_bytes", "host_pipeline_create", "host_pipeline_step", "host_pipeline_begin",

@@ -34,15 +34,12 @@
 // its TMEM.  The two CTAs meet at a cluster barrier after initialising their
 // barriers and again before either frees its TMEM or exits, so neither touches
 // a peer that has gone.
-#include <cuda.h>
-#include <cudaTypedefs.h>
-
-#include <initializer_list>
-
 #include "acrl_device.cuh"
 #include "acrl_host.h"
-#include "row_lse.cuh"
 #include "mbarrier.cuh"
+#include "row_lse.cuh"
+#include "tcgen05.cuh"
+#include "tma_host.h"
 
 namespace acrl {
 namespace {
@@ -107,10 +104,6 @@ static_assert(kBBytes >= kBM * kBK * 2, "the MMA's reads beyond the last A stage
 // PTX wrappers
 // ---------------------------------------------------------------------------
 
-__device__ __forceinline__ void remote_arrive(uint32_t cluster_addr) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
-}
-
 // Tile load into this CTA's shared memory whose completion is counted on the
 // barrier at `bar` (a shared::cluster address: either CTA of the pair).
 __device__ __forceinline__ void tma_load_pair(void* dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
@@ -119,19 +112,6 @@ __device__ __forceinline__ void tma_load_pair(void* dst, const CUtensorMap* map,
         "%3}], [%4];" ::"r"(smem_u32(dst)),
         "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
         : "memory");
-}
-
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-
-// Shared-memory matrix descriptor of a K-major bf16 tile written by TMA with
-// the 128-byte swizzle: rows of 128 bytes, 8-row groups 1024 bytes apart.
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr) {
-    uint64_t d = uint64_t((addr & 0x3FFFFu) >> 4);  // start address
-    d |= uint64_t(1024 >> 4) << 32;                  // stride between 8-row groups
-    d |= uint64_t(1) << 46;                          // descriptor version of tcgen05
-    d |= uint64_t(2) << 61;                          // 128-byte swizzle
-    return d;
 }
 
 __device__ __forceinline__ void mma_pair(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t accumulate) {
@@ -147,42 +127,6 @@ __device__ __forceinline__ void mma_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
-        "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(taddr));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-}
-
-__device__ __forceinline__ void st_shared16(uint32_t addr, const uint4& v) {
-    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
-                 : "memory");
-}
-
-// Make this thread's shared-memory writes visible to the TMA (async proxy).
-__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-
-__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, const void* src, int x, int y) {
-    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(
-                     reinterpret_cast<uint64_t>(map)),
-                 "r"(x), "r"(y), "r"(smem_u32(src))
-                 : "memory");
-    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-}
-
-// Wait until at most N of this thread's bulk stores still read shared memory.
-template <int N>
-__device__ __forceinline__ void bulk_wait_read() {
-    asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
-}
-
-__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
-
 // ---------------------------------------------------------------------------
 // tile schedule: bands of BAND row-tile pairs, all column tiles of a band in
 // turn; the pair of cluster c takes tiles c, c + clusters, ...
@@ -196,11 +140,6 @@ __device__ __forceinline__ void tile_coords(int t, int m_pairs, int n_tiles, int
     const int bm = min(BAND, m_pairs - band * BAND);
     mp = band * BAND + r % bm;
     n = r / bm;
-}
-
-__device__ __forceinline__ void give_up(volatile int32_t* abort, int32_t* flags) {
-    *abort = 1;
-    raise_flag(flags, ACRL_FLAG_TIMEOUT);
 }
 
 // ---------------------------------------------------------------------------
@@ -535,23 +474,6 @@ acrl_status launch_merge(const float4* partials, const acrl_bf16* logits, int64_
                   int(N), ldl, int((N + kBN - 1) / kBN), ids, mask, lse, logp, entropy, flags);
 }
 
-bool encode_map(CUtensorMap* map, const void* ptr, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t box_rows,
-                uint32_t box_cols, CUtensorMapSwizzle swizzle) {
-    void* fn = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q) != cudaSuccess ||
-        q != cudaDriverEntryPointSuccess || fn == nullptr)
-        return false;
-    auto encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
-    const cuuint64_t dims[2] = {cols, rows};
-    const cuuint64_t strides[1] = {ld * 2};
-    const cuuint32_t box[2] = {box_cols, box_rows};
-    const cuuint32_t estr[2] = {1, 1};
-    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(ptr), dims, strides, box, estr,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 // Tensor maps, shared-memory opt-in and the persistent launch (clusters of two
 // CTAs, one CTA per SM, fewer if there are fewer tiles).  Arguments, including
 // where the operands live, are checked by the callers.
@@ -561,9 +483,13 @@ acrl_status launch_ring(const acrl_bf16* hidden, int64_t M, int64_t K, int64_t l
     // the short ring's boxes have the tensor's rows, in eights
     const int a_rows = R::kARows == kBM ? kBM : int((M + 7) / 8 * 8);
     CUtensorMap tmA, tmB, tmC;
-    if (!encode_map(&tmA, hidden, uint64_t(M), uint64_t(K), uint64_t(ldh), a_rows, kBK, CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !encode_map(&tmB, weight, uint64_t(N), uint64_t(K), uint64_t(ldw), kHalfBN, kBK, CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !encode_map(&tmC, logits, uint64_t(M), uint64_t(N), uint64_t(ldl), 32, 32, CU_TENSOR_MAP_SWIZZLE_64B))
+    auto map = [](CUtensorMap* m, const acrl_bf16* p, uint64_t rows, uint64_t cols, int64_t ld, int box_rows, int box_cols,
+                  CUtensorMapSwizzle swizzle) {
+        return encode_map(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p, rows, cols, uint64_t(ld), box_rows, box_cols, swizzle);
+    };
+    if (!map(&tmA, hidden, uint64_t(M), uint64_t(K), ldh, a_rows, kBK, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !map(&tmB, weight, uint64_t(N), uint64_t(K), ldw, kHalfBN, kBK, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !map(&tmC, logits, uint64_t(M), uint64_t(N), ldl, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B))
         return ACRL_ERR_CUDA;
     auto* kernel = lmhead_kernel<R>;
     constexpr int smem = kSmemBytes<R>;
@@ -588,28 +514,6 @@ acrl_status launch_lmhead(const acrl_bf16* hidden, int64_t M, int64_t K, int64_t
                           int64_t ldw, acrl_bf16* logits, int64_t ldl, float4* partials, int32_t* flags, cudaStream_t s) {
     auto* run = M <= Ring16::kARows ? launch_ring<Ring16> : launch_ring<RingFull>;
     return run(hidden, M, K, ldh, weight, N, ldw, logits, ldl, partials, flags, s);
-}
-
-// True when every pointer is device memory of the current device: not managed
-// memory, not host memory and not a peer GPU's memory.  The GEMM's tensor maps
-// are encoded over these pointers, and its TMA copies must stay within this
-// GPU's own memory.  A failed query counts as "no" and leaves no error behind
-// for a later launch check.
-bool operands_on_current_device(std::initializer_list<const void*> ptrs) {
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return false;
-    }
-    for (const void* p : ptrs) {
-        cudaPointerAttributes a{};
-        if (cudaPointerGetAttributes(&a, p) != cudaSuccess) {
-            (void)cudaGetLastError();
-            return false;
-        }
-        if (a.type != cudaMemoryTypeDevice || a.device != dev) return false;
-    }
-    return true;
 }
 
 }  // namespace

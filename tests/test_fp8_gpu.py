@@ -1,0 +1,216 @@
+"""8-bit matrices and their products against the definitions in 64 bits."""
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+import paper_2607_24062_gb300 as acrl  # noqa: E402
+from paper_2607_24062_gb300 import api  # noqa: E402
+
+DEV = "cuda"
+FORMATS = {"e4m3": (448.0, 3, -6), "e5m2": (57344.0, 2, -14)}
+
+
+def _plain_quantize(x, block, fmt, transpose=False):
+    """(values of q, scales) of a float64 numpy matrix, from the definition."""
+    top, bits, low = FORMATS[fmt]
+    x = x.T if transpose else x
+    R, C = x.shape
+    h = 128 if block == "tile" else 1
+    q = np.zeros((R, C))
+    scale = np.zeros(((R + h - 1) // h, (C + 127) // 128))
+    for i in range(scale.shape[0]):
+        for j in range(scale.shape[1]):
+            at = (slice(i * h, (i + 1) * h), slice(j * 128, (j + 1) * 128))
+            b = x[at]
+            a = np.abs(b).max()
+            if not np.isfinite(a):
+                q[at], scale[i, j] = np.nan, np.nan
+                continue
+            e = -127
+            while a > top * 2.0 ** e:
+                e += 1
+            scale[i, j] = 2.0 ** e if a > 0 else 1.0
+            y = b / scale[i, j]
+            step = 2.0 ** (np.maximum(np.frexp(np.abs(y))[1] - 1, low) - bits)
+            q[at] = np.round(y / step) * step          # numpy rounds halves to even
+    return q, scale
+
+
+def _scales(t):
+    e = t.scale.cpu().numpy().astype(np.float64)
+    return np.where(e == 255, np.nan, 2.0 ** (e - 127))
+
+
+def _matrix(R, C, seed, dtype=torch.bfloat16, std=1.0, gap=0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    ld = (C + 7) // 8 * 8 + gap
+    x = torch.randn((R, ld), generator=g, device=DEV) * std * torch.exp2(torch.randint(-9, 9, (R, ld), generator=g, device=DEV) * 0.5)
+    return x.to(dtype)[:, :C]
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("block,transpose", [("row", False), ("row", True), ("tile", False), ("tile", True)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("R,C,gap", [(1, 1, 0), (1, 128, 8), (3, 129, 0), (130, 257, 16), (257, 1000, 8), (129, 17, 0)])
+def test_quantize(fmt, block, transpose, dtype, R, C, gap):
+    x = _matrix(R, C, 11 * R + C, dtype, gap=gap)
+    t = acrl.fp8_quantize(x, block=block, fmt=fmt, transpose=transpose)
+    q, s = _plain_quantize(x.double().cpu().numpy(), block, fmt, transpose)
+    assert np.array_equal(t.q.float().cpu().numpy().astype(np.float64), q)
+    assert np.array_equal(_scales(t), s)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+def test_quantize_extremes(fmt):
+    """Blocks of zeros, of subnormals, of the type's largest, at the edge of a scale, and with an infinity or a NaN."""
+    top = FORMATS[fmt][0]
+    x = torch.zeros((9, 256), device=DEV)
+    x[1, :128] = 1e-40
+    x[2, 5] = 3.3895e38
+    x[2, 6] = 1e-30
+    x[3, 7], x[3, 8] = top * 2.0 ** -20, -top * 2.0 ** -21
+    x[4, 7] = float(np.nextafter(np.float32(top * 2.0 ** -20), np.float32(np.inf)))
+    x[5, 9] = float("inf")
+    x[6, 9] = float("nan")
+    x[7, 130], x[7, 131] = -float("inf"), 1.0
+    x[8] = 2.0 ** -126
+    flags = api.new_flags()
+    t = acrl.fp8_quantize(x, fmt=fmt, flags=flags)
+    q, s = _plain_quantize(x.double().cpu().numpy(), "row", fmt)
+    assert np.array_equal(t.q.float().cpu().numpy().astype(np.float64), q, equal_nan=True)
+    assert np.array_equal(_scales(t), s, equal_nan=True)
+    assert acrl.read_flags(flags) == acrl.FLAG_NONFINITE
+    flags = api.new_flags()
+    acrl.fp8_quantize(x[:5], fmt=fmt, flags=flags)
+    assert acrl.read_flags(flags) == 0
+
+
+def test_quantize_writes_nothing_beyond_the_matrix():
+    x = _matrix(37, 100, 5)
+    q = torch.full((40, 112), 0x55, dtype=torch.uint8, device=DEV)
+    s = torch.full((40, 4), 0x55, dtype=torch.uint8, device=DEV)
+    acrl.fp8_quantize(x, out=acrl.Fp8Tensor(q[:37, :100].view(torch.float8_e4m3fn), s[:37, :1]))
+    assert bool((q[37:] == 0x55).all()) and bool((q[:, 100:] == 0x55).all())
+    assert bool((s[37:] == 0x55).all()) and bool((s[:, 1:] == 0x55).all())
+    qt = torch.full((101, 48), 0x55, dtype=torch.uint8, device=DEV)
+    st = torch.full((101, 4), 0x55, dtype=torch.uint8, device=DEV)
+    acrl.fp8_quantize(x, transpose=True, out=acrl.Fp8Tensor(qt[:100, :37].view(torch.float8_e4m3fn), st[:100, :1]))
+    assert bool((qt[100:] == 0x55).all()) and bool((qt[:, 37:] == 0x55).all())
+    assert bool((st[100:] == 0x55).all()) and bool((st[:, 1:] == 0x55).all())
+
+
+def _product(a, b):
+    """The exact product in float64 and the sum of the terms' absolute values."""
+    A, B = a.values().double().cpu().numpy(), b.values().double().cpu().numpy()
+    return A @ B.T, np.abs(A) @ np.abs(B).T
+
+
+def _check_product(out, a, b):
+    """fp32 sums of K terms: an error of at most 2^-24 max(4, sqrt(K)) sum |terms| before the one rounding to the output's
+    type, so the output lies between the roundings of the ends of that interval (rounding is monotone)."""
+    exact, size = _product(a, b)
+    off = 2.0 ** -24 * max(4.0, np.sqrt(a.shape[1])) * size + 1e-37
+    lo, hi = (torch.from_numpy(v).to(DEV).to(out.dtype) for v in (exact - off, exact + off))
+    bad = ~((out >= lo) & (out <= hi))
+    assert not bool(bad.any()), (int(bad.sum()), bad.nonzero()[:4], out[bad][:4], lo[bad][:4], hi[bad][:4])
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 130, 128), (5, 300, 129), (16, 257, 640), (17, 128, 1000), (64, 515, 513),
+                                   (128, 129, 300), (129, 16, 256), (200, 300, 520), (300, 257, 2047), (1000, 1111, 1280)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_matmul(M, N, K, dtype):
+    a = acrl.fp8_quantize(_matrix(M, K, 1))
+    b = acrl.fp8_quantize(_matrix(N, K, 2, std=0.02), block="tile")
+    _check_product(acrl.fp8_matmul(a, b, out_dtype=dtype), a, b)
+
+
+@pytest.mark.parametrize("fa,fb", [("e4m3", "e5m2"), ("e5m2", "e4m3"), ("e5m2", "e5m2")])
+@pytest.mark.parametrize("ba,bb", [("row", "row"), ("tile", "row"), ("tile", "tile")])
+@pytest.mark.parametrize("M,N,K", [(40, 200, 700), (333, 140, 900)])
+def test_matmul_formats_and_blocks(fa, fb, ba, bb, M, N, K):
+    a = acrl.fp8_quantize(_matrix(M, K, 3), fmt=fa, block=ba)
+    b = acrl.fp8_quantize(_matrix(N, K, 4), fmt=fb, block=bb)
+    _check_product(acrl.fp8_matmul(a, b, out_dtype=torch.float32), a, b)
+
+
+@pytest.mark.parametrize("M,N,K,gap", [(1, 1000, 520, 0), (7, 300, 1032, 8), (130, 513, 264, 16)])
+def test_linear_is_quantise_then_product(M, N, K, gap):
+    x = _matrix(M, K, 6, gap=gap)
+    w = acrl.fp8_quantize(_matrix(N, K, 7, std=0.02), block="tile")
+    got = acrl.fp8_linear(x, w)
+    assert torch.equal(got, acrl.fp8_matmul(acrl.fp8_quantize(x), w))
+    _check_product(got, acrl.fp8_quantize(x), w)
+
+
+def test_linear_backward():
+    M, N, K = 203, 328, 136
+    x, dy, w = _matrix(M, K, 8), _matrix(M, N, 9, std=1e-3), _matrix(N, K, 10, std=0.02)
+    wt = acrl.fp8_quantize(w, block="tile", transpose=True)
+    dx, dw = acrl.fp8_linear_backward(dy, x, wt)
+    _check_product(dx, acrl.fp8_quantize(dy), wt)
+    _check_product(dw, acrl.fp8_quantize(dy, transpose=True), acrl.fp8_quantize(x, transpose=True))
+    # the 8-bit weight is the same matrix either way round
+    assert torch.equal(wt.values().t(), acrl.fp8_quantize(w, block="tile").values())
+
+
+def test_nan_blocks_reach_what_they_touch():
+    x = _matrix(5, 300, 12)
+    x[2, 200] = float("nan")
+    w = acrl.fp8_quantize(_matrix(140, 300, 13), block="tile")
+    flags = api.new_flags()
+    out = acrl.fp8_linear(x, w, flags=flags)
+    assert acrl.read_flags(flags) == acrl.FLAG_NONFINITE
+    nan = out.isnan()
+    assert bool(nan[2].all()) and not bool(nan[[0, 1, 3, 4]].any())
+
+
+def test_products_of_nothing():
+    w = acrl.fp8_quantize(_matrix(20, 64, 1), block="tile")
+    assert acrl.fp8_linear(_matrix(3, 64, 2)[:0], w).shape == (0, 20)
+    x0 = torch.empty((3, 0), dtype=torch.bfloat16, device=DEV)
+    e = acrl.fp8_quantize(x0)
+    assert e.shape == (3, 0)
+    w0 = acrl.fp8_quantize(torch.empty((5, 0), dtype=torch.bfloat16, device=DEV))
+    assert bool((acrl.fp8_matmul(e, w0) == 0).all())
+
+
+def test_output_keeps_what_is_beyond_the_product():
+    a = acrl.fp8_quantize(_matrix(70, 256, 3))
+    for M in (3, 70):   # both ways round inside the kernel
+        am = acrl.Fp8Tensor(a.q[:M], a.scale[:M])
+        b = acrl.fp8_quantize(_matrix(37, 256, 4), block="tile")
+        big = torch.full((M + 2, 48), 7.0, dtype=torch.bfloat16, device=DEV)
+        out = acrl.fp8_matmul(am, b, out=big[:M])
+        _check_product(out, am, b)
+        assert bool((big[M:] == 7).all()) and bool((big[:, 37:] == 7).all())
+
+
+def test_other_stream():
+    x, w = _matrix(64, 512, 1), _matrix(700, 512, 2, std=0.02)
+    want = acrl.fp8_linear(x, acrl.fp8_quantize(w, block="tile"))
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    got = acrl.fp8_linear(x, acrl.fp8_quantize(w, block="tile", stream=s), stream=s)
+    s.synchronize()
+    assert torch.equal(got, want)
+
+
+def test_refusals():
+    x = _matrix(8, 64, 1)
+    w = acrl.fp8_quantize(x, block="tile")
+    for call in (lambda: acrl.fp8_quantize(x.half()), lambda: acrl.fp8_quantize(x.cpu()), lambda: acrl.fp8_quantize(x, fmt="e3m4"),
+                 lambda: acrl.fp8_quantize(x, block="column"), lambda: acrl.fp8_quantize(x.t()),
+                 lambda: acrl.fp8_quantize(torch.empty((4, 9), dtype=torch.bfloat16, device=DEV)),     # row stride of 9
+                 lambda: acrl.fp8_quantize(x, out=acrl.fp8_quantize(x, fmt="e5m2")),
+                 lambda: acrl.Fp8Tensor(x, w.scale), lambda: acrl.Fp8Tensor(w.q, w.scale.float()),
+                 lambda: acrl.Fp8Tensor(w.q, w.scale.repeat(3, 1)),
+                 lambda: acrl.fp8_matmul(w, acrl.fp8_quantize(_matrix(8, 72, 1))), lambda: acrl.fp8_matmul(w, x),
+                 lambda: acrl.fp8_matmul(w, w, out_dtype=torch.float16),
+                 lambda: acrl.fp8_matmul(w, w, out=torch.empty((8, 12), dtype=torch.bfloat16, device=DEV)),
+                 lambda: acrl.fp8_linear(x.float(), w), lambda: acrl.fp8_linear(x[:, :32], w),
+                 lambda: acrl.fp8_linear(x, w, workspace=torch.empty(8, dtype=torch.uint8, device=DEV))):
+        with pytest.raises(acrl.AcrlError):
+            call()
