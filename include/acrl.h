@@ -630,6 +630,99 @@ acrl_status acrl_fp8_linear(const acrl_bf16* x, int64_t M, int64_t K, int64_t ld
                             void* out, acrl_dtype out_dtype, int64_t ldo, void* workspace, int64_t workspace_bytes,
                             int32_t* dev_flags, acrl_stream stream);
 
+/* ------------------------------------------------------------------------
+ * Losses with a reference policy.
+ */
+
+/* The KL term: none; estimated from the log-prob d = logp - ref_logp of the sampled token; or summed over the
+ * vocabulary, p = softmax(logits) and q = softmax(ref_logits). */
+typedef enum {
+    ACRL_KL_NONE = 0,
+    ACRL_KL_K1 = 1,       /* d                                   */
+    ACRL_KL_K2 = 2,       /* d^2 / 2                             */
+    ACRL_KL_K3 = 3,       /* e^-d - 1 + d                        */
+    ACRL_KL_EXACT = 4,    /* sum_j p_j (log p_j - log q_j)       */
+    ACRL_KL_REVERSE = 5   /* sum_j q_j (log q_j - log p_j)       */
+} acrl_kl;
+
+/*
+ * acrl_policy_loss_grad_logits -- the log-prob, the clipped policy loss with a
+ * KL term and its gradient w.r.t. the logits, reading the logits (and the
+ * reference's) once.  With r_t = exp(logp_t - old_logp_t) (1 where old_logp is
+ * NULL) and c_t = coef_t:
+ *     token_loss_t = -c_t min(r_t, 1 + clip_high)                          c_t >= 0
+ *                    -c_t min(max(r_t, 1 - clip_low), dual_clip)           c_t <  0
+ *                    + kl_coef_t KL_t
+ *     grad[t, j]   = d token_loss_t / d logits[t, j]                       (bf16)
+ *     *loss        = sum_t token_loss_t
+ * As acrl_loss_grad_logits with clip_low = clip_high and dual_clip = 0, but the
+ * statistics need no call of their own: for updates whose coef is known before
+ * the logits are read (cached old log-probs, App. A).
+ *   logits, grad  device bf16 [T, ld]; columns of grad from V on are not written.
+ *   ids, mask  as for acrl_token_stats.  Masked rows: gradient row, logp, kl_out
+ *           and token_loss 0, logits not read; likewise an id outside [0, V), with
+ *           BAD_ID.
+ *   old_logp  device float [T] or NULL.
+ *   coef    device float [T] as for acrl_loss_grad_logits, or NULL for 0 (the KL
+ *           term alone: distillation).
+ *   clip_low in [0, 1), clip_high >= 0, dual_clip > 1 or 0 for none.
+ *   kl_coef device float [T] factor of the KL term per token (its mean over tokens
+ *           or responses is the caller's: acrl_controller_step's ent_coef has that
+ *           form), or NULL for 0 (KL is computed, not added).
+ *   ref_logits  device bf16 [T, ld_ref], EXACT and REVERSE only; no gradient.
+ *   ref_logp  device float [T], K1 to K3 only.
+ *   logp, token_loss  device float [T] outputs;  kl_out  device float [T] or NULL.
+ *   loss    device float [1] output.
+ *   dev_flags  device int32 word or NULL.
+ * A column at -infinity has probability 0 and adds nothing to the sums weighted by
+ * it.  A row whose log-prob, KL or ratio is not defined (a NaN; a +infinity; every
+ * column or the sampled one at -infinity; a KL that is infinite) raises
+ * NONFINITE; its logp and kl_out are NaN where they are undefined, and where coef
+ * or kl_coef is not 0 its token_loss and gradient row are NaN.  A row with both
+ * coefficients 0 has gradient and token_loss 0.
+ */
+acrl_status acrl_policy_loss_grad_logits(const acrl_bf16* logits, int64_t T, int64_t V, int64_t ld,
+                                         const int32_t* ids, const uint8_t* mask, const float* old_logp,
+                                         const float* coef, float clip_low, float clip_high, float dual_clip,
+                                         acrl_kl kl, const float* kl_coef, const acrl_bf16* ref_logits,
+                                         int64_t ld_ref, const float* ref_logp, acrl_bf16* grad, float* logp,
+                                         float* kl_out, float* token_loss, float* loss, int32_t* dev_flags,
+                                         acrl_stream stream);
+
+typedef enum {
+    ACRL_PREF_SIGMOID = 0,  /* (1 - s) log(1 + e^-h) + s log(1 + e^h), s = label_smoothing */
+    ACRL_PREF_HINGE = 1,    /* max(0, 1 - h)                                               */
+    ACRL_PREF_IPO = 2       /* ((h - 1/2) / beta)^2                                        */
+} acrl_preference_form;
+
+/*
+ * acrl_preference_loss -- a preference loss over pairs of responses to one
+ * prompt, and its gradient w.r.t. the tokens' log-probs.  Per response
+ *     D_i = sum_t m_t (logp_t - ref_logp_t)   (over n_i with length_norm)
+ * and per prompt over its pairs (i, j), R_i > R_j with n_i, n_j > 0,
+ *     h_ij = beta (D_i - D_j) - margin,   L_g = mean over the pairs of f(h_ij).
+ * Equal rewards make no pair.
+ *     *loss  = mean of L_g over the prompts with a pair (0 if there is none)
+ *     coef_t = -d loss / d logp_t   (0 where m_t = 0)
+ * so that acrl_loss_grad_logits with this coef (old_logp NULL) writes d loss / d logits.
+ *   logp    device float [T];  ref_logp  device float [T] or NULL for 0.
+ *   mask, seq_offsets, group_offsets, rewards  as for acrl_seq_discrepancy and
+ *           acrl_grpo_advantage, offsets that break the rules likewise (BAD_OFFSETS).
+ *   beta > 0;  label_smoothing in [0, 1/2), used by SIGMOID alone.
+ *   ratio   device float [S] output D_i (0 where n_i = 0).
+ *   coef    device float [T] output;  loss  device float [1] output.
+ *   workspace  device, 16-byte aligned, acrl_preference_workspace_bytes(S, Gn) bytes.
+ * A D_i that is not finite, or a NaN reward, raises NONFINITE; the former makes the
+ * loss and the coefficients of its prompt's pairs NaN.  Fixed order, fp64 sums.
+ */
+int64_t     acrl_preference_workspace_bytes(int32_t S, int32_t Gn);
+acrl_status acrl_preference_loss(const float* logp, const float* ref_logp, const uint8_t* mask, int64_t T,
+                                 const float* rewards, const int64_t* seq_offsets, int32_t S,
+                                 const int32_t* group_offsets, int32_t Gn, acrl_preference_form form, float beta,
+                                 float margin, float label_smoothing, int32_t length_norm, float* ratio,
+                                 float* coef, float* loss, void* workspace, int64_t workspace_bytes,
+                                 int32_t* dev_flags, acrl_stream stream);
+
 /*
  * acrl_selftest_wait_timeout -- failure-detection self-test: one warp waits on
  * a shared-memory barrier that nothing arrives on, with the same bounded wait

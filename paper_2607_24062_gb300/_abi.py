@@ -28,6 +28,8 @@ SINGLETON_MEAN0_STD1, SINGLETON_ZERO = 0, 1
 BF16, F32 = 0, 1
 FP8_E4M3, FP8_E5M2 = 0, 1
 FP8_ROW, FP8_TILE = 0, 1
+KL_NONE, KL_K1, KL_K2, KL_K3, KL_EXACT, KL_REVERSE = 0, 1, 2, 3, 4, 5
+PREF_SIGMOID, PREF_HINGE, PREF_IPO = 0, 1, 2
 
 
 class Params(ctypes.Structure):
@@ -102,6 +104,11 @@ SIGNATURES = {
     "acrl_fp8_linear_workspace_bytes": (c_i64, [c_i64, c_i64]),
     "acrl_fp8_linear": (c_i32, [c_p, c_i64, c_i64, c_i64, c_i32, c_p, c_i64, c_i64, c_i32, c_p, c_i64, c_i32, c_p, c_i32,
                                 c_i64, c_p, c_i64, c_p, c_p]),
+    "acrl_policy_loss_grad_logits": (c_i32, [c_p, c_i64, c_i64, c_i64, c_p, c_p, c_p, c_p, c_f32, c_f32, c_f32, c_i32,
+                                             c_p, c_p, c_i64, c_p, c_p, c_p, c_p, c_p, c_p, c_p, c_p]),
+    "acrl_preference_workspace_bytes": (c_i64, [c_i32, c_i32]),
+    "acrl_preference_loss": (c_i32, [c_p, c_p, c_p, c_i64, c_p, c_p, c_i32, c_p, c_i32, c_i32, c_f32, c_f32, c_f32, c_i32,
+                                     c_p, c_p, c_p, c_p, c_i64, c_p, c_p]),
     "acrl_read_flags": (c_i32, [c_p, ctypes.POINTER(c_i32), c_p]),
     "acrl_check_flags": (c_i32, [c_p, c_p]),
     "acrl_selftest_wait_timeout": (c_i32, [c_p, c_i64, c_p]),

@@ -586,6 +586,108 @@ def fp8_linear_backward(dy, x, weight_t: Fp8Tensor, *, fmt="e4m3", dx_dtype=torc
     return dx, dw
 
 
+# ---------------------------------------------------------------------------
+# losses with a reference policy
+# ---------------------------------------------------------------------------
+
+_KL = {None: _abi.KL_NONE, "k1": _abi.KL_K1, "k2": _abi.KL_K2, "k3": _abi.KL_K3, "exact": _abi.KL_EXACT,
+       "reverse": _abi.KL_REVERSE}
+_PREF = {"sigmoid": _abi.PREF_SIGMOID, "hinge": _abi.PREF_HINGE, "ipo": _abi.PREF_IPO}
+
+
+@dataclass
+class PolicyLoss:
+    grad: torch.Tensor          # bf16 [T, ld] dL/dlogits
+    logp: torch.Tensor          # float32 [T] log-prob of the sampled token
+    kl: torch.Tensor | None     # float32 [T] the KL term per token (None without one)
+    token_loss: torch.Tensor    # float32 [T]
+    loss: torch.Tensor          # float32 [1]
+
+
+def _vec(t, dtype, n, name, dev):
+    return torch.empty(n, dtype=dtype, device=dev) if t is None else _need(t, dtype, n, name)
+
+
+def policy_loss_grad_logits(logits, ids, mask, coef, *, V=None, old_logp=None, clip_low=0.2, clip_high=0.2, dual_clip=0.0,
+                            kl=None, kl_coef=None, ref_logits=None, ref_logp=None, grad=None, logp=None, kl_out=None,
+                            token_loss=None, loss=None, flags=None, stream=None) -> PolicyLoss:
+    """acrl_policy_loss_grad_logits.  `kl` is None, "exact" or "reverse" (with `ref_logits`, bf16 [T, ld_ref]), or "k1",
+    "k2" or "k3" (with `ref_logp`, float32 [T]); `kl_coef` float32 [T] its factor per token."""
+    T, ld = _rows(logits, "logits")
+    V = ld if V is None else V
+    dev = logits.device
+    if kl not in _KL:
+        raise AcrlError(f"kl: {kl!r}, expected one of {list(_KL)}")
+    full = kl in ("exact", "reverse")
+    if full != (ref_logits is not None) or (kl is not None and not full) != (ref_logp is not None):
+        raise AcrlError(f"kl={kl!r} takes " + ("ref_logits" if full else "neither ref_logits nor ref_logp" if kl is None
+                                                else "ref_logp") + " and no other")
+    ldr = 0
+    if full:
+        Tr, ldr = _rows(ref_logits, "ref_logits")
+        if Tr < T or ref_logits.shape[1] < V:
+            raise AcrlError(f"ref_logits: shape {tuple(ref_logits.shape)}, needs {(T, V)}")
+    _need(ids, torch.int32, T, "ids")
+    _opt(mask, torch.uint8, T, "mask")
+    for name, t in (("coef", coef), ("kl_coef", kl_coef), ("old_logp", old_logp), ("ref_logp", ref_logp)):
+        _opt(t, torch.float32, T, name)
+    if grad is None:
+        grad = torch.empty((T, ld), dtype=torch.bfloat16, device=dev)
+    elif grad.dtype != torch.bfloat16 or grad.dim() != 2 or grad.stride(0) != ld or grad.stride(1) != 1 or \
+            grad.shape[0] < T:
+        raise AcrlError("grad: expected a bf16 [T, ld] tensor with the logits' row stride")
+    f32 = torch.float32
+    logp, token_loss = _vec(logp, f32, T, "logp", dev), _vec(token_loss, f32, T, "token_loss", dev)
+    kl_out = None if kl is None else _vec(kl_out, f32, T, "kl_out", dev)
+    loss = _vec(loss, f32, 1, "loss", dev)
+    _opt(flags, torch.int32, 1, "flags")
+    _call("acrl_policy_loss_grad_logits",
+          (logits, ids, mask, old_logp, coef, kl_coef, ref_logits, ref_logp, grad, logp, kl_out, token_loss, loss, flags),
+          stream, _ptr(logits), T, V, ld, _ptr(ids), _ptr(mask), _ptr(old_logp), _ptr(coef), float(clip_low),
+          float(clip_high), float(dual_clip), _KL[kl], _ptr(kl_coef), _ptr(ref_logits), ldr, _ptr(ref_logp), _ptr(grad),
+          _ptr(logp), _ptr(kl_out), _ptr(token_loss), _ptr(loss), _ptr(flags))
+    return PolicyLoss(grad, logp, kl_out, token_loss, loss)
+
+
+@dataclass
+class Preference:
+    loss: torch.Tensor     # float32 [1]
+    coef: torch.Tensor     # float32 [T] -dL/dlogp
+    ratio: torch.Tensor    # float32 [S] log-ratio of each response
+
+
+def preference_workspace_bytes(S: int, Gn: int) -> int:
+    """acrl_preference_workspace_bytes."""
+    return int(lib().acrl_preference_workspace_bytes(S, Gn))
+
+
+def preference_loss(logp, ref_logp, mask, rewards, seq_offsets, group_offsets, *, beta=0.1, form="sigmoid", margin=0.0,
+                    label_smoothing=0.0, length_norm=False, ratio=None, coef=None, loss=None, workspace=None, flags=None,
+                    stream=None) -> Preference:
+    """acrl_preference_loss: pairs of a prompt's responses by their rewards; `form` "sigmoid", "hinge" or "ipo"."""
+    T, S, Gn = logp.numel(), seq_offsets.numel() - 1, group_offsets.numel() - 1
+    f32, dev = torch.float32, logp.device
+    if form not in _PREF:
+        raise AcrlError(f"form: {form!r}, expected one of {list(_PREF)}")
+    if S < 0 or Gn < 0:
+        raise AcrlError("seq_offsets / group_offsets: empty")
+    _need(logp, f32, T, "logp")
+    _opt(ref_logp, f32, T, "ref_logp")
+    _opt(mask, torch.uint8, T, "mask")
+    _need(rewards, f32, S, "rewards")
+    _need(seq_offsets, torch.int64, S + 1, "seq_offsets")
+    _need(group_offsets, torch.int32, Gn + 1, "group_offsets")
+    ratio, coef, loss = _vec(ratio, f32, S, "ratio", dev), _vec(coef, f32, T, "coef", dev), _vec(loss, f32, 1, "loss", dev)
+    workspace = _vec(workspace, torch.uint8, preference_workspace_bytes(S, Gn), "workspace", dev)
+    _opt(flags, torch.int32, 1, "flags")
+    _call("acrl_preference_loss",
+          (logp, ref_logp, mask, rewards, seq_offsets, group_offsets, ratio, coef, loss, workspace, flags), stream,
+          _ptr(logp), _ptr(ref_logp), _ptr(mask), T, _ptr(rewards), _ptr(seq_offsets), S, _ptr(group_offsets), Gn,
+          _PREF[form], float(beta), float(margin), float(label_smoothing), int(length_norm), _ptr(ratio), _ptr(coef),
+          _ptr(loss), _ptr(workspace), workspace.numel(), _ptr(flags))
+    return Preference(loss, coef, ratio)
+
+
 def selftest_wait_timeout(flags, limit_ns: int, stream=None) -> None:
     """acrl_selftest_wait_timeout: a bounded wait on a barrier nothing arrives on."""
     _need(flags, torch.int32, 1, "flags")
@@ -688,6 +790,7 @@ def check_flags(flags, stream=None) -> None:
 __all__ = ["Params", "AcrlError", "token_stats", "seq_discrepancy", "grpo_advantage", "controller_init",
            "controller_step", "importance_weights", "step", "loss_grad_logits", "reduce_loss", "scale_grad",
            "read_flags", "check_flags", "read_state", "Discrepancy",
+           "PolicyLoss", "policy_loss_grad_logits", "Preference", "preference_loss", "preference_workspace_bytes",
            "Fp8Tensor", "fp8_quantize", "fp8_matmul", "fp8_linear", "fp8_linear_backward", "fp8_linear_workspace_bytes",
            "lmhead_logits_stats", "lmhead_merge", "lmhead_workspace_bytes", "lmhead_stats_noalloc", "save_state",
            "load_state", "controller_save", "controller_load", "selftest_wait_timeout",

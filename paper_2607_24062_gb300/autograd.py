@@ -13,6 +13,11 @@ constants, as the paper's rho is built from theta_old.
 
 The returned gradient is a view of `step.grad`: it stays valid until the same
 step object runs again.
+
+The losses with a reference policy work alike: `policy_loss` (the clipped loss
+with a KL term) and `pairs_loss` (a PreferenceStep) write dL/dlogits in their
+forward.  `fp8_layer` is a linear layer on 8-bit matrices, whose backward makes
+both gradients on 8-bit matrices too.
 """
 
 from __future__ import annotations
@@ -22,7 +27,17 @@ from typing import Callable
 import torch
 
 from . import api
-from .pipeline import AcrlStep
+from .pipeline import AcrlStep, PreferenceStep
+
+
+def _scaled(g: torch.Tensor, grad_out: torch.Tensor) -> torch.Tensor:
+    """The forward's gradient, or a contiguous copy scaled by the incoming one where that is not 1."""
+    if float(grad_out) != 1.0:  # one scalar read; the common loss.backward() passes 1
+        if torch.is_grad_enabled() or grad_out.dtype != torch.float32 or grad_out.device != g.device:
+            g = g * grad_out.to(g.dtype)  # a graph of the backward itself, or no scalar the kernel reads
+        else:
+            g = api.scale_grad(g, grad_out, out=torch.empty(g.shape, dtype=g.dtype, device=g.device))
+    return g
 
 
 class _AcrlLoss(torch.autograd.Function):
@@ -35,13 +50,7 @@ class _AcrlLoss(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, grad_out):
-        g = ctx.step.grad[: ctx.rows, : ctx.cols]
-        if float(grad_out) != 1.0:  # one scalar read; the common loss.backward() passes 1
-            if torch.is_grad_enabled() or grad_out.dtype != torch.float32 or grad_out.device != g.device:
-                g = g * grad_out.to(g.dtype)  # a graph of the backward itself, or no scalar the kernel reads
-            else:
-                g = api.scale_grad(g, grad_out, out=torch.empty(g.shape, dtype=g.dtype, device=g.device))
-        return g, None, None, None, None, None, None, None, None
+        return _scaled(ctx.step.grad[: ctx.rows, : ctx.cols], grad_out), None, None, None, None, None, None, None, None
 
 
 def acrl_loss(step: AcrlStep, logits: torch.Tensor, ids, mask, logp_mu, rewards, seq_offsets, group_offsets,
@@ -52,3 +61,79 @@ def acrl_loss(step: AcrlStep, logits: torch.Tensor, ids, mask, logp_mu, rewards,
     if logits.shape != (step.T, step.V) or logits.stride(0) != step.ld:
         raise ValueError(f"logits: expected shape ({step.T}, {step.V}) with row stride {step.ld}")
     return _AcrlLoss.apply(logits, step, ids, mask, logp_mu, rewards, seq_offsets, group_offsets, exchange)
+
+
+class _PolicyLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, ids, mask, coef, kw):
+        out = api.policy_loss_grad_logits(logits.detach(), ids, mask, coef, **kw)
+        ctx.grad, ctx.shape = out.grad, logits.shape
+        return out.loss.reshape(()).clone()
+
+    @staticmethod
+    def backward(ctx, grad_out):
+        return _scaled(ctx.grad[: ctx.shape[0], : ctx.shape[1]], grad_out), None, None, None, None
+
+
+def policy_loss(logits: torch.Tensor, ids, mask, coef, **kw) -> torch.Tensor:
+    """The scalar loss of policy_loss_grad_logits (same arguments; fp32, 0-d) with dL/dlogits attached for autograd.
+    `logits` is bf16 [T, V] with a row stride that is a multiple of eight; outputs given by keyword (logp, kl_out,
+    token_loss) are filled."""
+    if kw.get("V") not in (None, logits.shape[1]):
+        raise ValueError("logits: pass the view [T, V] itself")
+    kw["V"] = logits.shape[1]
+    return _PolicyLoss.apply(logits, ids, mask, coef, kw)
+
+
+class _PairsLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, step, ids, mask, ref_logp, rewards, seq_offsets, group_offsets):
+        step.run(logits.detach(), ids, mask, ref_logp, rewards, seq_offsets, group_offsets)
+        ctx.step, ctx.shape = step, logits.shape
+        return step.loss.reshape(()).clone()
+
+    @staticmethod
+    def backward(ctx, grad_out):
+        g = _scaled(ctx.step.grad[: ctx.shape[0], : ctx.shape[1]], grad_out)
+        return g, None, None, None, None, None, None, None
+
+
+def pairs_loss(step: PreferenceStep, logits: torch.Tensor, ids, mask, ref_logp, rewards, seq_offsets,
+               group_offsets) -> torch.Tensor:
+    """A PreferenceStep's scalar loss (fp32, 0-d) with dL/dlogits attached for autograd; as acrl_loss, the gradient is a
+    view of `step.grad`."""
+    if logits.shape != (step.T, step.V) or logits.stride(0) != step.ld:
+        raise ValueError(f"logits: expected shape ({step.T}, {step.V}) with row stride {step.ld}")
+    return _PairsLoss.apply(logits, step, ids, mask, ref_logp, rewards, seq_offsets, group_offsets)
+
+
+def _rows_of_eight(x: torch.Tensor) -> torch.Tensor:
+    """x, or a copy of it whose rows start on 16 bytes."""
+    if x.stride(1) == 1 and x.stride(0) % 8 == 0 and x.stride(0) >= x.shape[1] and x.data_ptr() % 16 == 0:
+        return x
+    pad = torch.empty((x.shape[0], (x.shape[1] + 7) // 8 * 8), dtype=x.dtype, device=x.device)[:, : x.shape[1]]
+    return pad.copy_(x)
+
+
+class _Fp8Layer(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, grad_fmt):
+        w = _rows_of_eight(weight.detach())
+        x = _rows_of_eight(x.detach())
+        y = api.fp8_linear(x, api.fp8_quantize(w, block="tile"))
+        ctx.save_for_backward(x, w)
+        ctx.grad_fmt = grad_fmt
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, w = ctx.saved_tensors
+        dx, dw = api.fp8_linear_backward(_rows_of_eight(dy), x, api.fp8_quantize(w, block="tile", transpose=True),
+                                         fmt=ctx.grad_fmt, dw_dtype=torch.float32)
+        return dx, dw.to(w.dtype), None
+
+
+def fp8_layer(x: torch.Tensor, weight: torch.Tensor, grad_fmt: str = "e4m3") -> torch.Tensor:
+    """x [M, K] times the transpose of weight [N, K] (both bf16), computed on 8-bit matrices; the backward's two products
+    are on 8-bit matrices as well, the incoming gradient in `grad_fmt`."""
+    return _Fp8Layer.apply(x, weight, grad_fmt)

@@ -156,6 +156,22 @@ def test_linear_backward():
     assert torch.equal(wt.values().t(), acrl.fp8_quantize(w, block="tile").values())
 
 
+def test_layer_in_a_graph():
+    M, N, K = 33, 131, 72       # rows of N are no multiple of eight
+    x, w = _matrix(M, K, 8).contiguous().requires_grad_(), _matrix(N, K, 10, std=0.02).contiguous().requires_grad_()
+    y = acrl.fp8_layer(x, w)
+    assert torch.equal(y, acrl.fp8_linear(x.detach(), acrl.fp8_quantize(w.detach(), block="tile")))
+    dy = torch.randn((M, N), device=DEV).to(torch.bfloat16)
+    y.backward(dy)
+    wide = torch.zeros((M, 136), dtype=torch.bfloat16, device=DEV)
+    wide[:, :N] = dy
+    dx, dw = acrl.fp8_linear_backward(wide[:, :N], x.detach(), acrl.fp8_quantize(w.detach(), block="tile", transpose=True))
+    assert torch.equal(x.grad, dx) and torch.equal(w.grad, dw.to(torch.bfloat16))
+    # near the gradients of the product in full precision: two operands, each within 2^-4 of its elements (e4m3)
+    full = dy.double() @ w.detach().double()
+    assert bool(((x.grad - full).abs() <= 0.13 * (dy.double().abs() @ w.detach().double().abs())).all())
+
+
 def test_nan_blocks_reach_what_they_touch():
     x = _matrix(5, 300, 12)
     x[2, 200] = float("nan")

@@ -58,3 +58,27 @@ def test_linear(L):
                 dict(flags=None), dict(ldx=32), dict(ldw=40), dict(ldo=20), dict(fx=2), dict(fw=2), dict(bw=2), dict(M=-1)):
         assert _call(L.acrl_fp8_linear, ok, **bad) == E, bad
     assert _call(L.acrl_fp8_linear, ok, N=0) == OK
+
+
+def test_policy_loss(L):
+    ok = dict(z=FAKE, T=4, V=16, ld=16, ids=FAKE, mask=None, old=None, coef=FAKE, low=0.2, high=0.2, dual=0.0, kl=0,
+              kl_coef=None, x=None, ldx=0, ref=None, grad=FAKE, logp=FAKE, kl_out=None, tl=FAKE, loss=FAKE, flags=None,
+              stream=None)
+    for bad in (dict(z=None), dict(ids=None), dict(grad=None), dict(logp=None), dict(tl=None), dict(loss=None), dict(T=-1),
+                dict(V=0), dict(ld=8), dict(ld=20), dict(z=FAKE + 2), dict(grad=FAKE + 8), dict(low=-0.1), dict(low=1.0),
+                dict(high=-0.1), dict(high=float("nan")), dict(dual=1.0), dict(dual=-2.0), dict(kl=6), dict(kl=-1),
+                dict(kl_coef=FAKE), dict(kl_out=FAKE), dict(kl=1), dict(kl=3), dict(kl=4), dict(kl=4, x=FAKE),
+                dict(kl=4, x=FAKE, ldx=20), dict(kl=5, x=FAKE + 8, ldx=16), dict(V=(1 << 30) + 8, ld=(1 << 30) + 8)):
+        assert _call(L.acrl_policy_loss_grad_logits, ok, **bad) == E, bad
+
+
+def test_preference_loss(L):
+    assert L.acrl_preference_workspace_bytes(-1, 1) == -1 and L.acrl_preference_workspace_bytes(1, -1) == -1
+    n = L.acrl_preference_workspace_bytes(4, 2)
+    ok = dict(logp=FAKE, ref=None, mask=None, T=9, rewards=FAKE, so=FAKE, S=4, go=FAKE, Gn=2, form=0, beta=0.1, margin=0.0,
+              smooth=0.0, mean=0, ratio=FAKE, coef=FAKE, loss=FAKE, ws=FAKE, n=n, flags=None, stream=None)
+    for bad in (dict(logp=None), dict(rewards=None), dict(so=None), dict(go=None), dict(ratio=None), dict(coef=None),
+                dict(loss=None), dict(ws=None), dict(ws=FAKE + 8), dict(n=n - 1), dict(T=-1), dict(S=-1), dict(Gn=-1),
+                dict(Gn=0), dict(S=0), dict(form=3), dict(form=-1), dict(beta=0.0), dict(beta=float("inf")),
+                dict(margin=float("nan")), dict(smooth=0.5), dict(smooth=-0.1)):
+        assert _call(L.acrl_preference_loss, ok, **bad) == E, bad

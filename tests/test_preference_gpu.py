@@ -1,0 +1,189 @@
+"""The preference loss over the responses of a prompt against its definition in 64 bits."""
+
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+import paper_2607_24062_gb300 as acrl  # noqa: E402
+from paper_2607_24062_gb300 import api  # noqa: E402
+
+DEV = "cuda"
+
+
+def _batch(sizes, lengths, seed, masked=0.1, levels=3):
+    """Prompts of `sizes` responses with the given lengths (cycled)."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    S = sum(sizes)
+    n = [lengths[i % len(lengths)] for i in range(S)]
+    T = sum(n)
+    so = torch.tensor([0] + list(torch.tensor(n).cumsum(0)), dtype=torch.int64, device=DEV)
+    go = torch.tensor([0] + list(torch.tensor(sizes).cumsum(0)), dtype=torch.int32, device=DEV)
+    logp = -torch.rand(T, generator=g, device=DEV) * 3
+    return dict(logp=logp, ref=logp + 0.3 * torch.randn(T, generator=g, device=DEV),
+                mask=(torch.rand(T, generator=g, device=DEV) >= masked).to(torch.uint8),
+                rewards=torch.randint(0, levels, (S,), generator=g, device=DEV).float(), so=so, go=go)
+
+
+def _plain(b, beta=0.1, form="sigmoid", margin=0.0, label_smoothing=0.0, length_norm=False):
+    """Loss, D and dL/dlogp by autograd in float64."""
+    logp = b["logp"].double().cpu().requires_grad_()
+    ref = torch.zeros_like(logp) if b["ref"] is None else b["ref"].double().cpu()
+    mask = torch.ones(logp.numel(), dtype=torch.bool) if b["mask"] is None else b["mask"].bool().cpu()
+    so, go, R = b["so"].tolist(), b["go"].tolist(), b["rewards"].tolist()
+    D, n = [], []
+    for i in range(len(so) - 1):
+        m = mask[so[i]: so[i + 1]]
+        d = (logp - ref)[so[i]: so[i + 1]][m]
+        n.append(int(m.sum()))
+        D.append(d.sum() / (max(1, n[-1]) if length_norm else 1))
+    per = []
+    for g in range(len(go) - 1):
+        f = []
+        for i in range(go[g], go[g + 1]):
+            for j in range(go[g], go[g + 1]):
+                if R[i] > R[j] and n[i] and n[j]:
+                    h = beta * (D[i] - D[j]) - margin
+                    f.append((1 - label_smoothing) * torch.nn.functional.softplus(-h) +
+                             label_smoothing * torch.nn.functional.softplus(h) if form == "sigmoid" else
+                             torch.relu(1 - h) if form == "hinge" else ((h - 0.5) / beta) ** 2)
+        if f:
+            per.append(torch.stack(f).mean())
+    loss = torch.stack(per).mean() if per else (logp * 0).sum()
+    grad = torch.autograd.grad(loss, logp)[0]
+    return float(loss), torch.stack(D).detach() if D else torch.zeros(0), grad
+
+
+def _check(b, o, **kw):
+    """fp64 sums of fp32 log-probs, h and its functions in fp32: relative errors of a few 2^-24, h absolutely 2^-24 |h|."""
+    loss, D, grad = _plain(b, **kw)
+    assert torch.allclose(o.ratio.double().cpu(), D, rtol=2e-7, atol=1e-12)
+    assert abs(float(o.loss) - loss) <= 4e-6 * abs(loss) + 1e-12
+    got = o.coef.double().cpu()
+    assert bool(((got + grad).abs() <= 4e-6 * grad.abs() + 2e-6 * grad.abs().max()).all())
+    if b["mask"] is not None:
+        assert not bool(o.coef[b["mask"] == 0].any())
+
+
+def _run(b, **kw):
+    return acrl.preference_loss(b["logp"], b["ref"], b["mask"], b["rewards"], b["so"], b["go"], **kw)
+
+
+@pytest.mark.parametrize("form", ["sigmoid", "hinge", "ipo"])
+@pytest.mark.parametrize("length_norm", [False, True])
+@pytest.mark.parametrize("sizes,lengths", [([2], [1]), ([2, 2, 2], [5, 40]), ([1, 8, 3, 4], [0, 7, 300, 1025]),
+                                           ([130, 2], [3, 9, 1]), ([8] * 40, [17, 64, 2, 0, 90])])
+def test_preference(form, length_norm, sizes, lengths):
+    b = _batch(sizes, lengths, len(sizes) + lengths[-1])
+    kw = dict(form=form, length_norm=length_norm, beta=0.2 if form == "sigmoid" else 0.5)
+    flags = api.new_flags()
+    _check(b, _run(b, flags=flags, **kw), **kw)
+    assert acrl.read_flags(flags) == 0
+
+
+def test_options():
+    b = _batch([4, 6, 2], [9, 20], 3)
+    for kw in (dict(label_smoothing=0.2), dict(margin=0.7), dict(beta=3.0, margin=-0.2), dict(form="hinge", margin=0.3),
+               dict(form="ipo", margin=0.1, beta=0.05)):
+        _check(b, _run(b, **kw), **kw)
+    for part in ("mask", "ref"):
+        c = dict(b, **{part: None})
+        _check(c, _run(c))
+
+
+def test_no_pairs():
+    """Equal rewards, single responses and prompts whose other side is masked make no pair; they count for nothing."""
+    b = _batch([2, 1, 3, 2], [4, 6], 4, masked=0.0)
+    b["rewards"][:] = torch.tensor([1, 1, 0, 1, 0, 0, 1, 0.0], device=DEV)
+    b["mask"][int(b["so"][7]): int(b["so"][8])] = 0            # the last prompt's rejected answer has no valid token
+    _check(b, _run(b))
+    b["rewards"][:] = 0.5
+    o = _run(b)
+    assert float(o.loss) == 0 and not bool(o.coef.any())
+    b["mask"][:] = 0
+    b["rewards"][::2] = 1
+    o = _run(b)
+    assert float(o.loss) == 0 and not bool(o.coef.any()) and not bool(o.ratio.any())
+
+
+def test_far_apart():
+    """Log ratios of thousands: the sigmoid's tails, with no overflow."""
+    b = _batch([2, 2], [50], 5, masked=0.0)
+    b["ref"][: 50] -= 300.0
+    b["ref"][150:] -= 300.0
+    b["rewards"][:] = torch.tensor([1, 0, 1, 0.0], device=DEV)
+    _check(b, _run(b))
+
+
+def test_undefined():
+    b = _batch([2, 2], [5], 6, masked=0.0)
+    b["rewards"][:] = torch.tensor([1, 0, 0, 1.0], device=DEV)
+    b["logp"][2] = math.nan
+    flags = api.new_flags()
+    o = _run(b, flags=flags)
+    assert acrl.read_flags(flags) == acrl.FLAG_NONFINITE
+    assert bool(o.loss.isnan()) and bool(o.coef[:10].isnan().all()) and bool(o.coef[10:].isfinite().all())
+    b["mask"][2] = 0                                            # the same token masked
+    flags = api.new_flags()
+    _check(b, _run(b, flags=flags))
+    assert acrl.read_flags(flags) == 0
+    b["rewards"][1] = math.nan
+    flags = api.new_flags()
+    assert bool(_run(b, flags=flags).loss.isfinite())
+    assert acrl.read_flags(flags) == acrl.FLAG_NONFINITE
+
+
+def test_offsets_that_break_the_rules():
+    b = _batch([2, 2], [5], 7, masked=0.0)
+    for so, go in (([0, 5, 3, 15, 20], None), ([0, 5, 10, 15, 21], None), ([1, 5, 10, 15, 20], None), ([0, 5, 10, 15, 19], None),
+                   (None, [0, 3, 2]), (None, [0, 2, 5]), (None, [1, 2, 4]), (None, [0, 2, 3])):
+        c = dict(b)
+        if so:
+            c["so"] = torch.tensor(so, dtype=torch.int64, device=DEV)
+        if go:
+            c["go"] = torch.tensor(go, dtype=torch.int32, device=DEV)
+        flags = api.new_flags()
+        _run(c, flags=flags)
+        assert acrl.read_flags(flags) & acrl.FLAG_BAD_OFFSETS
+
+
+def test_step_from_logits():
+    sizes, lengths, V = [2, 3], [6, 11, 4], 777
+    b = _batch(sizes, lengths, 8)
+    T = b["logp"].numel()
+    g = torch.Generator(device=DEV).manual_seed(1)
+    z = (2 * torch.randn((T, 784), generator=g, device=DEV)).to(torch.bfloat16)
+    ids = torch.randint(0, V, (T,), generator=g, device=DEV, dtype=torch.int32)
+    x = z[:, :V].double().requires_grad_()
+    logp = torch.log_softmax(x, 1).gather(1, ids.long()[:, None])[:, 0]
+    step = acrl.PreferenceStep(T, V, 784, sum(sizes), len(sizes), beta=0.3)
+    step.run(z, ids, b["mask"], b["ref"], b["rewards"], b["so"], b["go"])
+    c = dict(b, logp=torch.where(b["mask"].bool(), logp.detach(), torch.zeros_like(logp)).float())
+    loss, D, grad = _plain(c, beta=0.3)
+    (logp * grad.to(DEV)).sum().backward()
+    # log-probs within 4e-6 + 2^-23 |logp|: up to 12 of them in a ratio, beta and the pairs' mean below 1
+    assert abs(float(step.loss) - loss) <= 1e-4 * abs(loss)
+    assert bool(((step.grad[:, :V].double() - x.grad).abs() <= 2.0 ** -8 * 1.02 * x.grad.abs() + 1e-5 * grad.abs().max()).all())
+    assert acrl.read_flags(step.flags) == 0
+    # and its scalar as an autograd node
+    y = z.clone().requires_grad_()
+    node = acrl.pairs_loss(step, y[:, :V], ids, b["mask"], b["ref"], b["rewards"], b["so"], b["go"])
+    (2.0 * node).backward()
+    assert torch.allclose(y.grad[:, :V].float(), 2.0 * step.grad[:, :V].float(), rtol=2.0 ** -8)
+
+
+def test_refusals():
+    b = _batch([2, 2], [5], 9)
+    for change in (dict(logp=b["logp"].double()), dict(ref=b["ref"][:3]), dict(mask=b["mask"].bool()),
+                   dict(rewards=b["rewards"][:2]), dict(so=b["so"].int()), dict(go=b["go"].long()), dict(so=b["so"][:0])):
+        with pytest.raises(acrl.AcrlError):
+            _run(dict(b, **change))
+    for kw in (dict(beta=0.0), dict(form="dpo"), dict(label_smoothing=0.6), dict(margin=math.inf), dict(coef=b["logp"][:1]),
+               dict(workspace=torch.empty(8, dtype=torch.uint8, device=DEV))):
+        with pytest.raises(acrl.AcrlError):
+            _run(b, **kw)
+    step = acrl.PreferenceStep(20, 64, 64, 4, 2)
+    with pytest.raises(acrl.AcrlError):
+        step.run(torch.zeros((19, 64), dtype=torch.bfloat16, device=DEV), None, None, None, b["rewards"], b["so"], b["go"])
