@@ -575,7 +575,8 @@ acrl_status acrl_lmhead_stats_noalloc(const acrl_bf16* hidden, int64_t M, int64_
  * is 128 columns of one row (ACRL_FP8_ROW: a scale row per row) or of 128 rows
  * (ACRL_FP8_TILE: a scale row per 128 rows); the last ones may be shorter.
  * lds >= ceil(columns / 128); a multiple of 4 lets the product read the scales
- * of four blocks at once.
+ * of four blocks at once.  dev_flags of these calls may be NULL: nothing is
+ * reported then.
  */
 typedef enum { ACRL_BF16 = 0, ACRL_F32 = 1 } acrl_dtype;
 typedef enum { ACRL_FP8_E4M3 = 0, ACRL_FP8_E5M2 = 1 } acrl_fp8_format;   /* e4m3fn (largest 448) and e5m2 (57344) */

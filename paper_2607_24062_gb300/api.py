@@ -23,17 +23,18 @@ def _ptr(t: torch.Tensor | None) -> int | None:
 
 def _one_device(tensors) -> torch.device:
     """The GPU every buffer of one call lives on (they must agree)."""
-    dev = None
+    first, index = None, -1
     for t in tensors:
         if t is None:
             continue
-        if dev is None:
-            dev = t.device
-        elif t.device != dev:
-            raise AcrlError(f"buffers on {dev} and {t.device}: every buffer of a call must be on one GPU")
-    if dev is None or dev.type != "cuda":
+        at = t.get_device()    # the index alone: comparing torch.device objects costs a short call several microseconds
+        if first is None:
+            first, index = t, at
+        elif at != index or (at < 0 and t.device != first.device):
+            raise AcrlError(f"buffers on {first.device} and {t.device}: every buffer of a call must be on one GPU")
+    if first is None or index < 0 or not first.is_cuda:
         raise AcrlError("expected CUDA tensors")
-    return dev
+    return first.device
 
 
 def _call(name: str, tensors, stream, *args) -> None:
@@ -43,13 +44,13 @@ def _call(name: str, tensors, stream, *args) -> None:
     if stream is not None and stream.device != dev:
         raise AcrlError(f"{name}: stream on {stream.device}, buffers on {dev}")
     fn = getattr(lib(), name)
-    if dev.index == torch.cuda.current_device():
-        s = torch.cuda.current_stream(dev) if stream is None else stream
-        check(fn(*args, s.cuda_stream), name)
+    index = dev.index
+    if index == torch._C._cuda_getDevice():
+        # the current stream's handle without a Stream object around it
+        check(fn(*args, torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream), name)
         return
     with torch.cuda.device(dev):
-        s = torch.cuda.current_stream(dev) if stream is None else stream
-        check(fn(*args, s.cuda_stream), name)
+        check(fn(*args, torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream), name)
 
 
 def _flags(flags, dev):
@@ -451,16 +452,22 @@ class Fp8Tensor:
 
     def __post_init__(self):
         q, s = self.q, self.scale
-        if q.dtype not in _FP8_FORMAT or q.dim() != 2 or not q.is_cuda or (q.shape[1] > 1 and q.stride(1) != 1):
-            raise AcrlError("q: expected a 2-D float8_e4m3fn or float8_e5m2 CUDA tensor with unit column stride")
-        if s.dtype != torch.uint8 or s.dim() != 2 or not s.is_cuda or (s.shape[1] > 1 and s.stride(1) != 1):
-            raise AcrlError("scale: expected a 2-D uint8 CUDA tensor with unit column stride")
-        R, C = q.shape
-        if s.shape[1] < (C + 127) // 128 or s.shape[0] not in (R, (R + 127) // 128):
-            raise AcrlError(f"scale: shape {tuple(s.shape)} fits neither the rows nor the 128 x 128 tiles of "
-                            f"{tuple(q.shape)}")
+        if q.dtype not in _FP8_FORMAT or q.dim() != 2 or not q.is_cuda:
+            raise AcrlError("q: expected a 2-D float8_e4m3fn or float8_e5m2 CUDA tensor")
+        if s.dtype != torch.uint8 or s.dim() != 2 or not s.is_cuda:
+            raise AcrlError("scale: expected a 2-D uint8 CUDA tensor")
+        (R, C), (SR, SC) = q.shape, s.shape
+        (ldq, cq), (lds, cs) = q.stride(), s.stride()
+        if (cq != 1 and C > 1) or (cs != 1 and SC > 1):
+            raise AcrlError("q and scale: expected unit column strides")
+        if SC < (C + 127) // 128 or (SR != R and SR != (R + 127) // 128):
+            raise AcrlError(f"scale: shape {(SR, SC)} fits neither the rows nor the 128 x 128 tiles of {(R, C)}")
         # one row is one tile of one row: the same scales either way
-        self.block = "row" if s.shape[0] == R else "tile"
+        self.block = "row" if SR == R else "tile"
+        # address, rows, row stride, format, scales' address, their row stride, block: as the library takes a matrix (of a
+        # single row, or with nothing in a row, the stride says nothing, and any that the library accepts will do)
+        self._args = (q.data_ptr(), R, ldq if R > 1 and C > 0 else (C + 15) // 16 * 16, _FP8_FORMAT[q.dtype],
+                      s.data_ptr(), lds if SR > 1 and SC > 0 else SC, _FP8_BLOCK[self.block])
 
     @property
     def shape(self):
@@ -485,14 +492,18 @@ def _ld(t: torch.Tensor) -> int:
 def _fp8_args(t: Fp8Tensor, name: str):
     if not isinstance(t, Fp8Tensor):
         raise AcrlError(f"{name}: expected an Fp8Tensor")
-    lds = t.scale.stride(0) if t.scale.shape[0] > 1 and t.scale.shape[1] > 0 else t.scale.shape[1]
-    return _ptr(t.q), t.q.shape[0], _ld(t.q), _FP8_FORMAT[t.q.dtype], _ptr(t.scale), lds, _FP8_BLOCK[t.block]
+    return t._args
 
 
 def _fp8_format(fmt: str) -> int:
     if fmt not in _FP8:
         raise AcrlError(f"fmt: {fmt!r}, expected one of {sorted(_FP8)}")
     return _FP8[fmt][0]
+
+
+def _padded(shape, to: int, dtype, dev) -> torch.Tensor:
+    """A new matrix with its rows at a stride that is a multiple of `to`."""
+    return torch.empty_strided(shape, ((shape[1] + to - 1) // to * to, 1), dtype=dtype, device=dev)
 
 
 def fp8_quantize(x, *, block="row", fmt="e4m3", transpose=False, out: Fp8Tensor | None = None, flags=None,
@@ -509,11 +520,11 @@ def fp8_quantize(x, *, block="row", fmt="e4m3", transpose=False, out: Fp8Tensor 
     rows, cols = (C, R) if transpose else (R, C)
     srows, kb = (rows if block == "row" else (rows + 127) // 128), (cols + 127) // 128
     if out is None:
-        q = torch.empty((rows, (cols + 15) // 16 * 16), dtype=_FP8[fmt][1], device=x.device)[:, :cols]
-        out = Fp8Tensor(q, torch.empty((srows, (kb + 3) // 4 * 4), dtype=torch.uint8, device=x.device)[:, :kb])
+        out = Fp8Tensor(_padded((rows, cols), 16, _FP8[fmt][1], x.device),
+                        _padded((srows, kb), 4, torch.uint8, x.device))
     elif tuple(out.q.shape) != (rows, cols) or out.q.dtype != _FP8[fmt][1] or out.scale.shape[0] != srows:
         raise AcrlError(f"out: an 8-bit matrix of another shape, format or block than {(rows, cols)} {fmt} {block}")
-    flags = _flags(flags, x.device)
+    _opt(flags, torch.int32, 1, "flags")
     ptr, _, ldq, _, sptr, lds, _ = _fp8_args(out, "out")
     _call("acrl_fp8_quantize", (x, out.q, out.scale, flags), stream, _ptr(x), _OUT_DTYPE[x.dtype], R, C, _ld(x), code,
           _FP8_BLOCK[block], int(transpose), ptr, ldq, sptr, lds, _ptr(flags))
@@ -523,7 +534,8 @@ def fp8_quantize(x, *, block="row", fmt="e4m3", transpose=False, out: Fp8Tensor 
 def _product_out(out, M: int, N: int, dtype, dev):
     """(`out` as [M, N], its row stride)."""
     if out is None:
-        out = torch.empty((M, (N + 7) // 8 * 8), dtype=dtype, device=dev)
+        ldo = (N + 7) // 8 * 8
+        return _padded((M, N), 8, dtype, dev), ldo
     if not isinstance(out, torch.Tensor) or out.dtype not in _OUT_DTYPE or out.dim() != 2 or not out.is_cuda or \
             (out.shape[1] > 1 and out.stride(1) != 1) or out.shape[0] != M or out.shape[1] < N:
         raise AcrlError(f"out: expected a bfloat16 or float32 CUDA matrix of {(M, N)} with unit column stride")
@@ -539,7 +551,7 @@ def fp8_matmul(a: Fp8Tensor, b: Fp8Tensor, *, out_dtype=torch.bfloat16, out=None
     if out_dtype not in _OUT_DTYPE:
         raise AcrlError(f"out_dtype: {out_dtype}, expected bfloat16 or float32")
     out, ldo = _product_out(out, M, N, out_dtype, a.q.device)
-    flags = _flags(flags, a.q.device)
+    _opt(flags, torch.int32, 1, "flags")
     _call("acrl_fp8_matmul", (a.q, a.scale, b.q, b.scale, out, flags), stream, aa[0], M, K, *aa[2:], bb[0], N, *bb[2:],
           _ptr(out), _OUT_DTYPE[out.dtype], ldo, _ptr(flags))
     return out
@@ -566,7 +578,7 @@ def fp8_linear(x, weight: Fp8Tensor, *, fmt="e4m3", out_dtype=torch.bfloat16, ou
     n = fp8_linear_workspace_bytes(M, K)
     workspace = torch.empty(n, dtype=torch.uint8, device=x.device) if workspace is None else \
         _need(workspace, torch.uint8, n, "workspace")
-    flags = _flags(flags, x.device)
+    _opt(flags, torch.int32, 1, "flags")
     _call("acrl_fp8_linear", (x, weight.q, weight.scale, out, workspace, flags), stream, _ptr(x), M, K, _ld(x),
           _fp8_format(fmt), w[0], N, *w[2:], _ptr(out), _OUT_DTYPE[out.dtype], ldo, _ptr(workspace), workspace.numel(),
           _ptr(flags))
@@ -578,7 +590,6 @@ def fp8_linear_backward(dy, x, weight_t: Fp8Tensor, *, fmt="e4m3", dx_dtype=torc
     """The gradients of y = x W^T: dx = Q(dy) W and dw = Q(dy^T) Q(x^T)^T, products of 8-bit matrices over N and over
     the rows.  dy [M, N] and x [M, K] bf16; `weight_t` is the 8-bit W^T [K, N] (fp8_quantize(w, block="tile",
     transpose=True)); `fmt` is dy's format.  Returns (dx [M, K], dw [N, K])."""
-    flags = _flags(flags, dy.device)
     kw = dict(flags=flags, stream=stream)
     dx = fp8_matmul(fp8_quantize(dy, fmt=fmt, **kw), weight_t, out_dtype=dx_dtype, **kw)
     dw = fp8_matmul(fp8_quantize(dy, fmt=fmt, transpose=True, **kw), fp8_quantize(x, transpose=True, **kw),

@@ -17,10 +17,23 @@
 //              memory (each warp its own quarter of the lanes: the MMA wants the
 //              32 lanes' words in every quarter);
 //   warps 6-9  the epilogue: accumulator rows out of tensor memory, rounded once,
-//              stored.
-// The operand whose rows become the MMA's 128 rows is "P", the other, whose rows
-// become its columns, is "Q".
+//              stored, while the MMAs fill the other accumulator.
+// The operand whose rows become the MMA's rows is "P", the other, whose rows
+// become its columns, is "Q".  Two ways:
+//
+// Pairs (many rows): two CTAs share a tile of 256 rows (cta_group::2), each staging
+//   its 128 rows of P and half of Q's, so that an SM loads 240 bytes per
+//   256 x 224 x 1 products where a CTA alone would load 352: the way from L2 into shared
+//   memory bounds the product.  The even CTA's thread issues the MMAs, which read
+//   both CTAs' shared memory and each CTA's own tensor memory (accumulator, the
+//   scales of its own rows and of all columns).  Persistent over the tiles.
+// Alone (few rows): P is the wide operand, the weight, and the few rows are the
+//   MMA's columns, so that nothing is computed or loaded for rows that are not there;
+//   HBM bounds it.  Where there are fewer tiles than SMs, a cluster shares a tile by
+//   columns of the sum (K) and adds its accumulators through distributed shared
+//   memory, in rank order.
 #include <algorithm>
+#include <atomic>
 
 #include "acrl_device.cuh"
 #include "acrl_host.h"
@@ -31,7 +44,7 @@
 namespace acrl {
 namespace {
 
-constexpr int kRows = 128;             // rows of P per tile
+constexpr int kRows = 128;             // rows of P per CTA and tile
 constexpr int kSlab = 128;             // columns of a slab: 128 bytes, one row of the 128-byte swizzle
 constexpr int kGroup = 4;              // slabs whose scales share a word
 constexpr int kThreads = 320;
@@ -40,21 +53,27 @@ constexpr uint32_t kTmemCols = 512;
 // Tensor memory: accumulators from column 0, scale slots of 16 columns at the end (P's words in the first four of
 // them, Q's, up to 256 rows, in the last eight).
 constexpr uint32_t kScaleCols = 16, kScaleBase = kTmemCols - kScaleSlots * kScaleCols;
-constexpr int kRingBytes = 216 * 1024;
+constexpr int kPairCols = int(kScaleBase) / 2;   // 224: two accumulators beside the scales
 
 struct Barriers {
-    uint64_t full[kMaxStages];      // the copies of a stage have landed
+    uint64_t full[kMaxStages];      // the copies of a stage have landed (pair: the even CTA's counts both CTAs')
     uint64_t empty[kMaxStages];     // the MMAs that read it are done
-    uint64_t sfull[kScaleSlots];    // the four warps have written a slot's scales
-    uint64_t sempty[kScaleSlots];   // the MMAs that read them are done
+    uint64_t sfull[kScaleSlots];    // the scale warps (pair: of both CTAs, on the even one) have written a slot
+    uint64_t sempty[kScaleSlots];   // the MMAs that read it are done
     uint64_t tfull[2];              // an accumulator is complete
-    uint64_t tempty[2];             // the epilogue has read it
+    uint64_t tempty[2];             // the epilogue warps (pair: of both CTAs, on the even one) have read it
     uint64_t mma_done;
     uint32_t tmem_base;
     int32_t abort;
 };
-constexpr int kSmemBytes = 1024 + kRingBytes + int(sizeof(Barriers));
-static_assert(kSmemBytes <= 227 * 1024, "shared memory per CTA");
+// Staging of the pair's output: two blocks of 32 x 32 per epilogue warp.
+template <typename T>
+constexpr int kOutBlock = 32 * 32 * int(sizeof(T));
+template <typename T, bool PAIR>
+constexpr int kStaging = PAIR ? 8 * kOutBlock<T> : 0;
+constexpr int kSmemBytes = 227 * 1024;
+template <typename T, bool PAIR>
+constexpr int kRingBytes = (kSmemBytes - 1024 - kStaging<T, PAIR> - int(sizeof(Barriers))) / 1024 * 1024;
 
 struct Operand {
     const uint8_t* scale;
@@ -67,10 +86,10 @@ struct Operand {
 struct Problem {
     Operand p, q;
     int slabs;             // ceil(K / 128)
-    int cols;              // columns of a tile (rows of Q), a multiple of 16, at most 256
+    int cols;              // columns of a tile (rows of Q): a multiple of 32 (pair) or 16
     int p_tiles, q_tiles;
     int stages;
-    int accs;              // 2 where two accumulators fit, else 1
+    int accs;              // accumulators
     uint32_t idesc;
     void* out;
     int64_t ldo;
@@ -79,27 +98,76 @@ struct Problem {
 
 // tcgen05.mma kind::mxf8f6f4 instruction descriptor: scale type E8M0 (bit 23), formats of A (bits 7-9) and B (10-12),
 // both K-major, N / 8 at bit 17, M / 128 at bit 27; the scale ids (A's at bit 29, B's at 4) are added per slab.
-constexpr uint32_t kIdescBase = (1u << 23) | (1u << 27);
+constexpr uint32_t kIdescBase = 1u << 23;
 
+template <bool PAIR>
 __device__ __forceinline__ void mma_scaled(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sa,
                                            uint32_t sb, uint32_t accumulate) {
-    asm volatile(
-        "{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
-        " tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n}\n" ::"r"(d),
-        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate));
+    if (PAIR)
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+            " tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n}\n" ::"r"(d),
+            "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate));
+    else
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+            " tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n}\n" ::"r"(d),
+            "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate));
 }
 
+// Arrive on this CTA's barrier, or on that of both CTAs of the pair, when this thread's MMAs so far have completed.
+template <bool PAIR>
 __device__ __forceinline__ void commit(uint64_t* bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+    if constexpr (PAIR) {
+#pragma unroll
+        for (uint32_t r = 0; r < 2; ++r)
+            asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(peer_addr(bar, r))
+                         : "memory");
+    } else {
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
+                     : "memory");
+    }
 }
 
-__device__ __forceinline__ void tma_load(void* dst, const CUtensorMap* map, uint64_t* bar, int x, int y) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
-            smem_u32(dst)),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(smem_u32(bar))
-        : "memory");
+// `bar`: a shared::cluster address.
+template <bool PAIR>
+__device__ __forceinline__ void tma_load(void* dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
+    if (PAIR)
+        asm volatile(
+            "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, "
+            "%3}], [%4];" ::"r"(smem_u32(dst)),
+            "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
+            : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
+                smem_u32(dst)),
+            "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
+            : "memory");
 }
+
+// What a CTA works on: pairs take tiles in turn, slab by slab; alone, a cluster of CTAs splits one tile's slabs.
+template <bool PAIR>
+struct Work {
+    int first, step;    // tiles
+    int lo, hi;         // slabs
+    __device__ Work(const Problem& pr, uint32_t rank) {
+        if (PAIR) {
+            first = int(blockIdx.x >> 1);
+            step = int(gridDim.x >> 1);
+            lo = 0;
+            hi = pr.slabs;
+        } else {
+            const int parts = int(cluster_size());
+            first = int(blockIdx.x) / parts;
+            step = int(gridDim.x) / parts;
+            // whole groups of slabs, so that a word of scales is one CTA's
+            const int groups = (pr.slabs + kGroup - 1) / kGroup, per = (groups + parts - 1) / parts * kGroup;
+            lo = min(pr.slabs, int(rank) * per);
+            hi = min(pr.slabs, lo + per);
+        }
+    }
+};
 
 // Tiles in bands of kBand row tiles, all column tiles of a band in turn, so that the tiles in flight share operands in L2.
 constexpr int kBand = 16;
@@ -111,27 +179,45 @@ __device__ __forceinline__ void tile_at(int t, const Problem& pr, int& tp, int& 
     tq = r / h;
 }
 
-__device__ void produce(const CUtensorMap* tmP, const CUtensorMap* tmQ, uint8_t* ring, Barriers* bars, const Problem& pr) {
+template <bool PAIR>
+__device__ void produce(const CUtensorMap* tmP, const CUtensorMap* tmQ, uint8_t* ring, Barriers* bars, const Problem& pr,
+                        uint32_t rank) {
     volatile int32_t* abort = &bars->abort;
-    const int bytes = (kRows + pr.cols) * kSlab;
+    const int q_rows = PAIR ? pr.cols / 2 : pr.cols, bytes = (kRows + q_rows) * kSlab;
+    const Work<PAIR> w(pr, rank);
     int stage = 0;
     uint32_t phase = 0;
     long issued = 0;
-    for (int t = blockIdx.x; t < pr.p_tiles * pr.q_tiles; t += gridDim.x) {
+    for (int t = w.first; t < pr.p_tiles * pr.q_tiles; t += w.step) {
         int tp, tq;
         tile_at(t, pr, tp, tq);
-        for (int kb = 0; kb < pr.slabs; ++kb) {
+        const int p0 = PAIR ? (2 * tp + int(rank)) * kRows : tp * kRows;
+        const int q0 = tq * pr.cols + (PAIR ? int(rank) * q_rows : 0);
+        for (int kb = w.lo; kb < w.hi; ++kb) {
             if (!mbar_try_wait(&bars->empty[stage], phase ^ 1u) && !wait_phase(&bars->empty[stage], phase ^ 1u, abort)) {
                 give_up(abort, pr.flags);
-                // the copies that were started land before the CTA can exit
-                for (long j = issued - 1; j >= 0 && j >= issued - pr.stages; --j)
-                    wait_phase(&bars->full[j % pr.stages], uint32_t((j / pr.stages) & 1), nullptr);
+                // the copies that were started land before the CTA can exit: the even CTA's barriers count both CTAs',
+                // the odd one gives its own time to land
+                if (!PAIR || rank == 0) {
+                    for (long j = issued - 1; j >= 0 && j >= issued - pr.stages; --j)
+                        wait_phase(&bars->full[j % pr.stages], uint32_t((j / pr.stages) & 1), nullptr);
+                } else {
+                    const uint64_t t0 = global_ns();
+                    while (global_ns() - t0 < 100000ull) {
+                    }
+                }
                 return;
             }
             uint8_t* s = ring + stage * bytes;
-            mbar_expect_tx(&bars->full[stage], bytes);
-            tma_load(s, tmP, &bars->full[stage], kb * kSlab, tp * kRows);
-            tma_load(s + kRows * kSlab, tmQ, &bars->full[stage], kb * kSlab, tq * pr.cols);
+            uint32_t bar = smem_u32(&bars->full[stage]);
+            if (PAIR) {
+                if (rank == 0) mbar_expect_tx(&bars->full[stage], 2 * bytes);
+                bar = peer_addr(&bars->full[stage], 0);
+            } else {
+                mbar_expect_tx(&bars->full[stage], bytes);
+            }
+            tma_load<PAIR>(s, tmP, bar, kb * kSlab, p0);
+            tma_load<PAIR>(s + kRows * kSlab, tmQ, bar, kb * kSlab, q0);
             ++issued;
             if (++stage == pr.stages) {
                 stage = 0;
@@ -141,21 +227,23 @@ __device__ void produce(const CUtensorMap* tmP, const CUtensorMap* tmQ, uint8_t*
     }
 }
 
-__device__ void issue_mmas(uint8_t* ring, Barriers* bars, uint32_t tmem, const Problem& pr) {
+template <bool PAIR>
+__device__ void issue_mmas(uint8_t* ring, Barriers* bars, uint32_t tmem, const Problem& pr, uint32_t rank) {
     volatile int32_t* abort = &bars->abort;
-    const int bytes = (kRows + pr.cols) * kSlab;
+    const int bytes = (kRows + (PAIR ? pr.cols / 2 : pr.cols)) * kSlab;
     const uint64_t pdesc0 = smem_desc(smem_u32(ring)), qdesc0 = smem_desc(smem_u32(ring + kRows * kSlab));
+    const Work<PAIR> w(pr, rank);
     int stage = 0, slot = 0, acc = 0;
     uint32_t phase = 0, sphase = 0, aphase = 0;
     bool ok = true;
-    for (int t = blockIdx.x; t < pr.p_tiles * pr.q_tiles && ok; t += gridDim.x) {
+    for (int t = w.first; t < pr.p_tiles * pr.q_tiles && ok; t += w.step) {
         if (!wait_phase(&bars->tempty[acc], aphase ^ 1u, abort)) {
             give_up(abort, pr.flags);
             break;
         }
         tc_fence_after();
         const uint32_t d = tmem + uint32_t(acc * pr.cols);
-        for (int kb = 0; kb < pr.slabs; ++kb) {
+        for (int kb = w.lo; kb < w.hi; ++kb) {
             const uint32_t id = uint32_t(kb % kGroup);
             if ((id == 0 && !wait_phase(&bars->sfull[slot], sphase, abort)) ||
                 (!mbar_try_wait(&bars->full[stage], phase) && !wait_phase(&bars->full[stage], phase, abort))) {
@@ -168,15 +256,15 @@ __device__ void issue_mmas(uint8_t* ring, Barriers* bars, uint32_t tmem, const P
             const uint32_t sc = tmem + kScaleBase + uint32_t(slot) * kScaleCols;
 #pragma unroll
             for (int k = 0; k < kSlab / 32; ++k)   // 32 columns = 32 bytes = 2 descriptor units
-                mma_scaled(d, pd + uint64_t(2 * k), qd + uint64_t(2 * k), pr.idesc | id << 29 | id << 4, sc, sc + 8,
-                           (kb | k) != 0);
-            commit(&bars->empty[stage]);
+                mma_scaled<PAIR>(d, pd + uint64_t(2 * k), qd + uint64_t(2 * k), pr.idesc | id << 29 | id << 4, sc, sc + 8,
+                                 kb > w.lo || k > 0);
+            commit<PAIR>(&bars->empty[stage]);
             if (++stage == pr.stages) {
                 stage = 0;
                 phase ^= 1u;
             }
-            if (id == kGroup - 1 || kb == pr.slabs - 1) {
-                commit(&bars->sempty[slot]);
+            if (id == kGroup - 1 || kb == w.hi - 1) {
+                commit<PAIR>(&bars->sempty[slot]);
                 if (++slot == kScaleSlots) {
                     slot = 0;
                     sphase ^= 1u;
@@ -184,13 +272,19 @@ __device__ void issue_mmas(uint8_t* ring, Barriers* bars, uint32_t tmem, const P
             }
         }
         if (!ok) break;
-        commit(&bars->tfull[acc]);
+        commit<PAIR>(&bars->tfull[acc]);
         if (++acc == pr.accs) {
             acc = 0;
             aphase ^= 1u;
         }
     }
-    commit(&bars->mma_done);   // every MMA has finished before the CTA moves on
+    // every MMA has finished before the CTA moves on
+    if (PAIR)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
+                         peer_addr(&bars->mma_done, 0))
+                     : "memory");
+    else
+        commit<false>(&bars->mma_done);
     wait_phase(&bars->mma_done, 0, nullptr);
 }
 
@@ -205,22 +299,24 @@ __device__ __forceinline__ uint32_t scale_word(const Operand& o, int row, int kb
     return w;
 }
 
-__device__ void write_scales(Barriers* bars, uint32_t tmem, const Problem& pr) {
+template <bool PAIR>
+__device__ void write_scales(Barriers* bars, uint32_t tmem, const Problem& pr, uint32_t rank) {
     volatile int32_t* abort = &bars->abort;
     const int lane = threadIdx.x & 31;
     const uint32_t lanes = uint32_t((threadIdx.x >> 5) & 3) << 21;   // this warp's quarter, 32 lanes each
+    const Work<PAIR> w(pr, rank);
     int slot = 0;
     uint32_t phase = 0;
-    for (int t = blockIdx.x; t < pr.p_tiles * pr.q_tiles; t += gridDim.x) {
+    for (int t = w.first; t < pr.p_tiles * pr.q_tiles; t += w.step) {
         int tp, tq;
         tile_at(t, pr, tp, tq);
-        const int p0 = tp * kRows + lane, q0 = tq * pr.cols + lane;
-        for (int kb = 0; kb < pr.slabs; kb += kGroup) {
-            uint32_t w[12];
+        const int p0 = (PAIR ? 2 * tp + int(rank) : tp) * kRows + lane, q0 = tq * pr.cols + lane;
+        for (int kb = w.lo; kb < w.hi; kb += kGroup) {
+            uint32_t v[12];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) w[c] = scale_word(pr.p, p0 + 32 * c, kb, pr.slabs);
+            for (int c = 0; c < 4; ++c) v[c] = scale_word(pr.p, p0 + 32 * c, kb, pr.slabs);
 #pragma unroll
-            for (int c = 0; c < 8; ++c) w[4 + c] = 32 * c < pr.cols ? scale_word(pr.q, q0 + 32 * c, kb, pr.slabs) : 0x7f7f7f7fu;
+            for (int c = 0; c < 8; ++c) v[4 + c] = 32 * c < pr.cols ? scale_word(pr.q, q0 + 32 * c, kb, pr.slabs) : 0x7f7f7f7fu;
             const bool free = wait_phase(&bars->sempty[slot], phase ^ 1u, abort);
             if (!__all_sync(0xffffffffu, free)) {
                 give_up(abort, pr.flags);
@@ -228,16 +324,21 @@ __device__ void write_scales(Barriers* bars, uint32_t tmem, const Problem& pr) {
             }
             tc_fence_after();
             const uint32_t at = tmem + lanes + kScaleBase + uint32_t(slot) * kScaleCols;
-            asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w[0]), "r"(w[1]),
-                         "r"(w[2]), "r"(w[3])
+            asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v[0]), "r"(v[1]),
+                         "r"(v[2]), "r"(v[3])
                          : "memory");
             asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(at + 8),
-                         "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]), "r"(w[8]), "r"(w[9]), "r"(w[10]), "r"(w[11])
+                         "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11])
                          : "memory");
             asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&bars->sfull[slot]);
+            if (lane == 0) {
+                if (PAIR)
+                    remote_arrive(peer_addr(&bars->sfull[slot], 0));
+                else
+                    mbar_arrive(&bars->sfull[slot]);
+            }
             if (++slot == kScaleSlots) {
                 slot = 0;
                 phase ^= 1u;
@@ -246,69 +347,126 @@ __device__ void write_scales(Barriers* bars, uint32_t tmem, const Problem& pr) {
     }
 }
 
-// 32 accumulators of one row of P, as columns q0 .. q0+31 of `out` row `row` (SWAP: as rows q0 .. of column `row`).
+// Accumulators of a pair's tile: each warp its 32 rows, 32 columns at a time, rounded, staged in shared memory and
+// stored by a TMA copy, which leaves out what is beyond the matrix.
 template <typename T>
-__device__ __forceinline__ T round_to(float v);
-template <>
-__device__ __forceinline__ float round_to<float>(float v) { return v; }
-template <>
-__device__ __forceinline__ acrl_bf16 round_to<acrl_bf16>(float v) { return acrl_bf16(pack_bf16x2(v, 0.f) & 0xffffu); }
-
-template <typename T, bool SWAP>
-__device__ __forceinline__ void store_chunk(T* out, int64_t ldo, int row, int q0, int n, const uint32_t (&r)[32]) {
-    if constexpr (SWAP) {
-#pragma unroll
-        for (int j = 0; j < 32; ++j)
-            if (j < n) out[int64_t(q0 + j) * ldo + row] = round_to<T>(__uint_as_float(r[j]));
-    } else {
-        T* p = out + int64_t(row) * ldo + q0;
-        if (n >= 32) {
-            uint4* v = reinterpret_cast<uint4*>(p);
-            if constexpr (sizeof(T) == 2) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        w[i] = pack_bf16x2(__uint_as_float(r[8 * j + 2 * i]), __uint_as_float(r[8 * j + 2 * i + 1]));
-                    v[j] = make_uint4(w[0], w[1], w[2], w[3]);
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = make_uint4(r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]);
-            }
-            return;
-        }
-#pragma unroll
-        for (int j = 0; j < 32; ++j)
-            if (j < n) p[j] = round_to<T>(__uint_as_float(r[j]));
-    }
-}
-
-template <typename T, bool SWAP>
-__device__ void epilogue(Barriers* bars, uint32_t tmem, const Problem& pr) {
+__device__ void pair_epilogue(Barriers* bars, uint32_t tmem, const CUtensorMap* tmO, uint8_t* staging, const Problem& pr,
+                              uint32_t rank) {
     volatile int32_t* abort = &bars->abort;
     const int lane = threadIdx.x & 31, quarter = (threadIdx.x >> 5) & 3;
-    int acc = 0;
+    uint8_t* blocks = staging + ((threadIdx.x >> 5) - 6) * 2 * kOutBlock<T>;
+    // row `lane` of a block, its 16-byte pieces permuted by the swizzle of the output's map: 64-byte rows in fours
+    // (bf16), 128-byte rows in eights (fp32)
+    constexpr int kPieces = 32 * int(sizeof(T)) / 16;
+    const uint32_t at = smem_u32(blocks) + uint32_t(lane * 32 * int(sizeof(T)));
+    const uint32_t swz = kPieces == 4 ? uint32_t((lane >> 1) & 3) : uint32_t(lane & 7);
+    int buf = 0, acc = 0;
     uint32_t phase = 0;
-    for (int t = blockIdx.x; t < pr.p_tiles * pr.q_tiles; t += gridDim.x) {
+    const Work<true> w(pr, rank);
+    for (int t = w.first; t < pr.p_tiles * pr.q_tiles; t += w.step) {
         int tp, tq;
         tile_at(t, pr, tp, tq);
         const bool ready = wait_phase(&bars->tfull[acc], phase, abort);
         if (!__all_sync(0xffffffffu, ready)) {
             give_up(abort, pr.flags);
-            return;
+            break;
         }
         tc_fence_after();
-        const int row = tp * kRows + quarter * 32 + lane;
+        const int row0 = (2 * tp + int(rank)) * kRows + quarter * 32;
 #pragma unroll 1
         for (int c = 0; c < pr.cols; c += 32) {
             uint32_t r[32];
             __syncwarp();
             tmem_ld32(tmem + uint32_t(acc * pr.cols + c) + (uint32_t(quarter * 32) << 16), r);
-            const int q0 = tq * pr.cols + c;
-            const int n = min(min(32, pr.cols - c), pr.q.rows - q0);
-            if (row < pr.p.rows && n > 0) store_chunk<T, SWAP>(static_cast<T*>(pr.out), pr.ldo, row, q0, n, r);
+            if (c + 32 == pr.cols) {   // read out: the even CTA's MMA thread may fill it again
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) remote_arrive(peer_addr(&bars->tempty[acc], 0));
+            }
+            const int col0 = tq * pr.cols + c;
+            if (row0 >= pr.p.rows || col0 >= pr.q.rows) continue;   // the same for the whole warp
+            if (lane == 0) bulk_wait_read<1>();                     // the store that last read this block is done
+            __syncwarp();
+            const uint32_t to = at + uint32_t(buf * kOutBlock<T>);
+#pragma unroll
+            for (int k = 0; k < kPieces; ++k) {
+                uint4 v;
+                if constexpr (sizeof(T) == 2)
+                    v = make_uint4(pack_bf16x2(__uint_as_float(r[8 * k]), __uint_as_float(r[8 * k + 1])),
+                                   pack_bf16x2(__uint_as_float(r[8 * k + 2]), __uint_as_float(r[8 * k + 3])),
+                                   pack_bf16x2(__uint_as_float(r[8 * k + 4]), __uint_as_float(r[8 * k + 5])),
+                                   pack_bf16x2(__uint_as_float(r[8 * k + 6]), __uint_as_float(r[8 * k + 7])));
+                else
+                    v = make_uint4(r[4 * k], r[4 * k + 1], r[4 * k + 2], r[4 * k + 3]);
+                st_shared16(to + ((uint32_t(k) ^ swz) << 4), v);
+            }
+            fence_async_shared();
+            __syncwarp();
+            if (lane == 0) tma_store_2d(tmO, blocks + buf * kOutBlock<T>, col0, row0);
+            buf ^= 1;
+        }
+        __syncwarp();
+        if (++acc == pr.accs) {
+            acc = 0;
+            phase ^= 1u;
+        }
+    }
+    if (lane == 0) bulk_wait_all();   // the blocks stay valid until every store has completed
+    __syncwarp();
+}
+
+template <typename T>
+__device__ __forceinline__ void store_one(T* p, float v);
+template <>
+__device__ __forceinline__ void store_one<float>(float* p, float v) { *p = v; }
+template <>
+__device__ __forceinline__ void store_one<acrl_bf16>(acrl_bf16* p, float v) { *p = acrl_bf16(pack_bf16x2(v, 0.f) & 0xffffu); }
+
+// A CTA alone: row r of P is column r of `out`, a column of the accumulator a row of it, so a warp stores 32 neighbours.
+// With a split sum the other ranks' accumulators wait in the first rank's shared memory (`parts`, [rank - 1][column][128]).
+template <typename T>
+__device__ bool alone_epilogue(Barriers* bars, uint32_t tmem, float* parts, const Problem& pr, uint32_t rank, int nct) {
+    const int lane = threadIdx.x & 31, quarter = (threadIdx.x >> 5) & 3;
+    const uint32_t lanes = uint32_t(quarter * 32) << 16;
+    const Work<false> w(pr, rank);
+    int acc = 0;
+    uint32_t phase = 0;
+    for (int t = w.first; t < pr.p_tiles * pr.q_tiles; t += w.step) {
+        int tp, tq;
+        tile_at(t, pr, tp, tq);
+        const bool ready = wait_phase(&bars->tfull[acc], phase, &bars->abort);
+        if (!__all_sync(0xffffffffu, ready)) {
+            give_up(&bars->abort, pr.flags);
+            return false;
+        }
+        tc_fence_after();
+        const int row = tp * kRows + quarter * 32 + lane;
+        T* out = static_cast<T*>(pr.out) + row;
+#pragma unroll 1
+        for (int c = 0; c < pr.cols; c += 16) {
+            uint32_t r[16];
+            __syncwarp();
+            asm volatile(
+                "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                  "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                : "r"(tmem + uint32_t(acc * pr.cols + c) + lanes));
+            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+            if (w.lo == w.hi)   // no slab left for this rank: nothing was accumulated
+#pragma unroll
+                for (int j = 0; j < 16; ++j) r[j] = 0u;
+            const int m0 = tq * pr.cols + c;
+            if (nct == 1) {
+                if (row < pr.p.rows)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (m0 + j < pr.q.rows) store_one(out + int64_t(m0 + j) * pr.ldo, __uint_as_float(r[j]));
+            } else if (rank > 0) {
+                const float* to = parts + ((int(rank) - 1) * pr.cols + c) * kRows + quarter * 32 + lane;
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(peer_addr(to + j * kRows, 0)), "r"(r[j]) : "memory");
+            }
         }
         tc_fence_before();
         __syncwarp();
@@ -318,28 +476,61 @@ __device__ void epilogue(Barriers* bars, uint32_t tmem, const Problem& pr) {
             phase ^= 1u;
         }
     }
+    return true;
 }
 
-template <typename T, bool SWAP>
+// The first rank's part of a split sum: its accumulator and the others', in rank order.
+template <typename T>
+__device__ void join(uint32_t tmem, const float* parts, const Problem& pr, int nct) {
+    const int lane = threadIdx.x & 31, quarter = (threadIdx.x >> 5) & 3;
+    int tp, tq;
+    tile_at(int(blockIdx.x) / nct, pr, tp, tq);
+    const int row = tp * kRows + quarter * 32 + lane;
+    T* out = static_cast<T*>(pr.out) + row;
+    tc_fence_after();
+#pragma unroll 1
+    for (int c = 0; c < pr.cols; c += 16) {
+        uint32_t r[16];
+        __syncwarp();
+        asm volatile(
+            "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+            : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+              "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+            : "r"(tmem + uint32_t(c) + (uint32_t(quarter * 32) << 16)));
+        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+        const int m0 = tq * pr.cols + c;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            float v = __uint_as_float(r[j]);
+            for (int k = 1; k < nct; ++k) v += parts[((k - 1) * pr.cols + c + j) * kRows + quarter * 32 + lane];
+            if (row < pr.p.rows && m0 + j < pr.q.rows) store_one(out + int64_t(m0 + j) * pr.ldo, v);
+        }
+    }
+}
+
+template <typename T, bool PAIR>
 __global__ void __launch_bounds__(kThreads, 1)
     fp8_matmul_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CUtensorMap tmQ,
-                      const __grid_constant__ Problem pr) {
+                      const __grid_constant__ CUtensorMap tmO, const __grid_constant__ Problem pr) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    Barriers* bars = reinterpret_cast<Barriers*>(ring + kRingBytes);
+    uint8_t* staging = ring + kRingBytes<T, PAIR>;
+    Barriers* bars = reinterpret_cast<Barriers*>(staging + kStaging<T, PAIR>);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    const int nct = int(cluster_size());
     if (threadIdx.x == 0) {
         for (int s = 0; s < kMaxStages; ++s) {
             mbar_init(&bars->full[s], 1);
             mbar_init(&bars->empty[s], 1);
         }
         for (int s = 0; s < kScaleSlots; ++s) {
-            mbar_init(&bars->sfull[s], 4);
+            mbar_init(&bars->sfull[s], PAIR ? 8 : 4);
             mbar_init(&bars->sempty[s], 1);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(&bars->tfull[b], 1);
-            mbar_init(&bars->tempty[b], 4);
+            mbar_init(&bars->tempty[b], PAIR ? 8 : 4);
         }
         mbar_init(&bars->mma_done, 1);
         bars->abort = 0;
@@ -349,30 +540,53 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     grid_begin();
     if (warp == 2) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)),
-                     "r"(kTmemCols)
-                     : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        if (PAIR) {   // one warp of each CTA of the pair, together
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)),
+                         "r"(kTmemCols)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)),
+                         "r"(kTmemCols)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
     }
     tc_fence_before();
     __syncthreads();
+    if (PAIR || nct > 1) cluster_sync();   // the others' barriers are initialised, and they run
     tc_fence_after();
     const uint32_t tmem = bars->tmem_base;
+    // the parts of a split sum wait in the ring's place, which no copy writes any more when they arrive (the ring of the
+    // first rank is still read by its own MMAs, so they go behind what it uses)
+    float* parts = reinterpret_cast<float*>(ring + pr.stages * (kRows + pr.cols) * kSlab);
+    bool ok = true;
     if (warp == 0) {
-        if (lane == 0) produce(&tmP, &tmQ, ring, bars, pr);
+        if (lane == 0) produce<PAIR>(&tmP, &tmQ, ring, bars, pr, rank);
     } else if (warp == 1) {
-        if (lane == 0) issue_mmas(ring, bars, tmem, pr);
+        if (lane == 0 && (!PAIR || rank == 0)) issue_mmas<PAIR>(ring, bars, tmem, pr, rank);
     } else if (warp < 6) {
-        write_scales(bars, tmem, pr);
+        write_scales<PAIR>(bars, tmem, pr, rank);
+    } else if constexpr (PAIR) {
+        pair_epilogue<T>(bars, tmem, &tmO, staging, pr, rank);
     } else {
-        epilogue<T, SWAP>(bars, tmem, pr);
+        ok = alone_epilogue<T>(bars, tmem, parts, pr, rank, nct);
     }
     __syncwarp();
     tc_fence_before();
     __syncthreads();
+    if (PAIR || nct > 1) cluster_sync();   // no CTA frees its TMEM or leaves while another may still touch it
+    if (!PAIR && nct > 1 && rank == 0 && warp >= 6 && ok) join<T>(tmem, parts, pr, nct);
+    if (!PAIR) {
+        tc_fence_before();
+        __syncthreads();
+    }
     if (warp == 2) {
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+        if (PAIR)
+            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+        else
+            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
     }
 }
 
@@ -396,47 +610,113 @@ Operand operand(const Matrix& m) {
                    (m.lds & 3) == 0 && (reinterpret_cast<uintptr_t>(m.scale) & 3) == 0};
 }
 
-// Tokens up to this many become the MMA's columns, so that a tile has no more of them than there are.
-constexpr int64_t kSwapRows = 128;
+// Rows up to this many become the MMA's columns.
+constexpr int64_t kAloneRows = 128;
+constexpr int kMaxSplit = 8;
 
-template <typename T>
-acrl_status launch_matmul(const Matrix& a, const Matrix& b, int64_t K, void* out, int64_t ldo, int32_t* flags,
-                          cudaStream_t s) {
-    const bool swap = a.rows <= kSwapRows;
-    const Matrix &p = swap ? b : a, &q = swap ? a : b;
-    Problem pr = {};
-    pr.p = operand(p);
-    pr.q = operand(q);
-    pr.slabs = int((K + kSlab - 1) / kSlab);
-    pr.cols = int(q.rows < 256 ? (q.rows + 15) / 16 * 16 : 256);
-    pr.p_tiles = int((p.rows + kRows - 1) / kRows);
-    pr.q_tiles = int((q.rows + pr.cols - 1) / pr.cols);
-    const int64_t total = int64_t(pr.p_tiles) * pr.q_tiles;
-    if (total > kMaxGrid) return ACRL_ERR_INVALID_ARG;
-    pr.stages = std::min(kMaxStages, kRingBytes / ((kRows + pr.cols) * kSlab));
-    pr.accs = 2 * pr.cols <= int(kScaleBase) ? 2 : 1;
-    pr.idesc = kIdescBase | uint32_t(p.format) << 7 | uint32_t(q.format) << 10 | uint32_t(pr.cols >> 3) << 17;
-    pr.out = out;
-    pr.ldo = ldo;
-    pr.flags = flags;
-    CUtensorMap tmP, tmQ;
+// How many CTA pairs of a kernel the current device holds at once: a property of the two, looked up once.
+template <typename K>
+int resident_pairs(K* kernel) {
+    constexpr int kDevices = 64;
+    static std::atomic<int> known[kDevices];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+    if (dev < kDevices)
+        if (const int n = known[dev].load(std::memory_order_relaxed)) return n;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2 * 1024, 1, 1);
+    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.dynamicSmemBytes = kSmemBytes;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 2;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return 0;
+    }
+    if (dev < kDevices) known[dev].store(n, std::memory_order_relaxed);
+    return n;
+}
+
+template <typename T, bool PAIR>
+acrl_status launch_kernel(const Matrix& p, const Matrix& q, int64_t K, Problem pr, int64_t grid, int cluster, cudaStream_t s) {
+    CUtensorMap tmP, tmQ, tmO;
     auto map = [&](CUtensorMap* m, const Matrix& x, int box_rows) {
         return encode_map(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, x.q, uint64_t(x.rows), uint64_t(K), uint64_t(x.ld), box_rows,
                           kSlab, CU_TENSOR_MAP_SWIZZLE_128B);
     };
-    if (!map(&tmP, p, kRows) || !map(&tmQ, q, pr.cols)) return ACRL_ERR_CUDA;
-    auto* kernel = swap ? fp8_matmul_kernel<T, true> : fp8_matmul_kernel<T, false>;
+    if (!map(&tmP, p, kRows) || !map(&tmQ, q, PAIR ? pr.cols / 2 : pr.cols)) return ACRL_ERR_CUDA;
+    constexpr bool bf16 = sizeof(T) == 2;
+    if (!PAIR)
+        tmO = tmP;   // not used
+    else if (!encode_map(&tmO, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, sizeof(T), pr.out,
+                         uint64_t(p.rows), uint64_t(q.rows), uint64_t(pr.ldo), 32, 32,
+                         bf16 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B))
+        return ACRL_ERR_CUDA;
+    auto* kernel = fp8_matmul_kernel<T, PAIR>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) != cudaSuccess)
         return launch_status();
+    if (PAIR) {   // no more than can be resident at once: they are persistent
+        const int most = resident_pairs(kernel);
+        if (most < 1) return ACRL_ERR_CUDA;
+        grid = std::min<int64_t>(grid, 2 * most);
+    }
+    return launch(kernel, grid, kThreads, kSmemBytes, cluster, s, tmP, tmQ, tmO, pr);
+}
+
+template <typename T>
+acrl_status launch_matmul(const Matrix& a, const Matrix& b, int64_t K, void* out, int64_t ldo, int32_t* flags,
+                          cudaStream_t s) {
     int dev = 0, sms = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
         return launch_status();
-    return launch(kernel, std::min<int64_t>(total, sms), kThreads, kSmemBytes, 0, s, tmP, tmQ, pr);
+    const bool alone = a.rows <= kAloneRows;
+    const Matrix &p = alone ? b : a, &q = alone ? a : b;
+    Problem pr = {};
+    pr.p = operand(p);
+    pr.q = operand(q);
+    pr.slabs = int((K + kSlab - 1) / kSlab);
+    pr.out = out;
+    pr.ldo = ldo;
+    pr.flags = flags;
+    pr.idesc = kIdescBase | uint32_t(p.format) << 7 | uint32_t(q.format) << 10;
+    if (alone) {
+        pr.cols = int((q.rows + 15) / 16 * 16);
+        pr.p_tiles = int((p.rows + kRows - 1) / kRows);
+        pr.q_tiles = 1;
+        pr.accs = 2;
+        const int bytes = (kRows + pr.cols) * kSlab;
+        // as many CTAs a tile as keep all SMs busy, each with four slabs or more
+        int split = 1;
+        while (split < kMaxSplit && 2 * split * pr.p_tiles <= sms && (pr.slabs + kGroup - 1) / kGroup >= 2 * split) split *= 2;
+        const int parts = (split - 1) * pr.cols * kRows * 4;
+        pr.stages = std::min(kMaxStages, (kRingBytes<T, false> - parts) / bytes);
+        while (pr.stages < 2) {   // never for up to 128 columns and eight parts of 64 KB less one
+            split /= 2;
+            pr.stages = std::min(kMaxStages, (kRingBytes<T, false> - (split - 1) * pr.cols * kRows * 4) / bytes);
+        }
+        pr.idesc |= uint32_t(pr.cols >> 3) << 17 | 1u << 27;
+        const int64_t grid = split > 1 ? int64_t(pr.p_tiles) * split : std::min(pr.p_tiles, sms);
+        return launch_kernel<T, false>(p, q, K, pr, grid, split, s);
+    }
+    pr.cols = kPairCols;
+    pr.p_tiles = int((p.rows + 2 * kRows - 1) / (2 * kRows));
+    pr.q_tiles = int((q.rows + pr.cols - 1) / pr.cols);
+    const int64_t total = int64_t(pr.p_tiles) * pr.q_tiles;
+    if (total > kMaxGrid / 2) return ACRL_ERR_INVALID_ARG;
+    pr.accs = 2;
+    pr.stages = std::min(kMaxStages, kRingBytes<T, true> / ((kRows + pr.cols / 2) * kSlab));
+    pr.idesc |= uint32_t(pr.cols >> 3) << 17 | 2u << 27;
+    return launch_kernel<T, true>(p, q, K, pr, 2 * total, 2, s);
 }
 
 acrl_status matmul(const Matrix& a, const Matrix& b, int64_t K, void* out, acrl_dtype out_dtype, int64_t ldo,
                    int32_t* flags, cudaStream_t s) {
-    if (K < 0 || K > kMaxGrid - 512 || !matrix_ok(a, K) || !matrix_ok(b, K) || !flags) return ACRL_ERR_INVALID_ARG;
+    if (K < 0 || K > kMaxGrid - 512 || !matrix_ok(a, K) || !matrix_ok(b, K)) return ACRL_ERR_INVALID_ARG;
     if ((out_dtype != ACRL_BF16 && out_dtype != ACRL_F32) || ldo < b.rows || (ldo & 7)) return ACRL_ERR_INVALID_ARG;
     if (a.rows == 0 || b.rows == 0) return ACRL_OK;
     if (!out || !aligned16(out)) return ACRL_ERR_INVALID_ARG;
@@ -446,7 +726,7 @@ acrl_status matmul(const Matrix& a, const Matrix& b, int64_t K, void* out, acrl_
                    ? ACRL_OK
                    : launch_status();
     if (!a.q || !b.q || !a.scale || !b.scale || !aligned16(a.q) || !aligned16(b.q)) return ACRL_ERR_INVALID_ARG;
-    if (!operands_on_current_device({a.q, b.q})) return ACRL_ERR_INVALID_ARG;
+    if (!operands_on_current_device({a.q, b.q, out})) return ACRL_ERR_INVALID_ARG;
     return out_dtype == ACRL_BF16 ? launch_matmul<acrl_bf16>(a, b, K, out, ldo, flags, s)
                                   : launch_matmul<float>(a, b, K, out, ldo, flags, s);
 }
@@ -483,7 +763,7 @@ extern "C" acrl_status acrl_fp8_linear(const acrl_bf16* x, int64_t M, int64_t K,
     const Matrix a{q, M, ldq, x_format, q + M * ldq, lds, ACRL_FP8_ROW};
     const Matrix b{w, N, ldw, w_format, w_scale, ldws, w_block};
     // the product's arguments are checked before anything is launched
-    if (!dev_flags || !matrix_ok(a, K) || !matrix_ok(b, K) || (out_dtype != ACRL_BF16 && out_dtype != ACRL_F32) || ldo < N ||
+    if (!matrix_ok(a, K) || !matrix_ok(b, K) || (out_dtype != ACRL_BF16 && out_dtype != ACRL_F32) || ldo < N ||
         (ldo & 7) || (M > 0 && N > 0 && (!out || !aligned16(out))) ||
         (M > 0 && N > 0 && K > 0 && (!w || !w_scale || !aligned16(w) || !operands_on_current_device({w, q}))))
         return ACRL_ERR_INVALID_ARG;

@@ -117,16 +117,22 @@ __global__ void __launch_bounds__(kRowThreads)
     const int team = threadIdx.x >> 4, l = threadIdx.x & 15;
     // a unit is kRowUnroll consecutive blocks of one row; a CTA's teams take consecutive units
     const int64_t unit = int64_t(blockIdx.x) * (kRowThreads / 16) + team;
-    const int64_t row = unit / chunks;
+    const int64_t row = unit >> 32 ? unit / chunks : int64_t(uint32_t(unit) / uint32_t(chunks));
     const int kb0 = int(unit - row * chunks) * kRowUnroll;
     const bool in = row < R;
     const T* xr = x + (in ? row : 0) * ldx;
     float f[kRowUnroll][8];
     uint32_t m[kRowUnroll];
+    // whole units without a test between their loads, so that all of them are in flight together
+    if (in && (kb0 + kRowUnroll) * 128 <= C) {
 #pragma unroll
-    for (int k = 0; k < kRowUnroll; ++k) {
-        const int c = (kb0 + k) * 128 + l * 8;
-        load8<T>(xr + c, in ? C - c : 0, f[k]);
+        for (int k = 0; k < kRowUnroll; ++k) load8<T>(xr + (kb0 + k) * 128 + l * 8, 8, f[k]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < kRowUnroll; ++k) {
+            const int c = (kb0 + k) * 128 + l * 8;
+            load8<T>(xr + c, in ? C - c : 0, f[k]);
+        }
     }
 #pragma unroll
     for (int k = 0; k < kRowUnroll; ++k) {
@@ -153,6 +159,35 @@ __global__ void __launch_bounds__(kRowThreads)
 // piece g of a column at g ^ (column / 8), so that neither side meets a bank twice.
 constexpr int kTileThreads = 256;
 
+// The tile's result, turned, in rows of 128 bytes.
+template <int FMT, bool TILE>
+__device__ __forceinline__ void turn_and_store(const float (&f)[8][8], const Scale* s, uint8_t* turned, uint8_t* q,
+                                               int64_t ldq, int64_t rb, int64_t cb, int64_t R, int64_t C) {
+    const int g = threadIdx.x >> 4, cl = threadIdx.x & 15;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float col[8] = {f[0][j], f[1][j], f[2][j], f[3][j], f[4][j], f[5][j], f[6][j], f[7][j]};
+        *reinterpret_cast<uint2*>(turned + (8 * cl + j) * 128 + 8 * (g ^ cl)) = pack8<FMT>(col, s[TILE ? 0 : j]);
+    }
+    __syncthreads();
+    // eight lanes a column of x (128 bytes of the result's row)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int c = k * 32 + (threadIdx.x >> 3), p = 2 * (threadIdx.x & 7);
+        const int64_t col = cb * 128 + c, row = rb * 128 + 8 * p;
+        if (col >= C || row >= R) continue;
+        const uint2 a = *reinterpret_cast<const uint2*>(turned + c * 128 + 8 * (p ^ (c >> 3)));
+        const uint2 b = *reinterpret_cast<const uint2*>(turned + c * 128 + 8 * ((p + 1) ^ (c >> 3)));
+        uint8_t* to = q + col * ldq + row;
+        if (row + 16 <= R) {
+            *reinterpret_cast<uint4*>(to) = make_uint4(a.x, a.y, b.x, b.y);
+        } else {
+            store8(to, a, int(R - row));
+            if (row + 8 < R) store8(to + 8, b, int(R - row - 8));
+        }
+    }
+}
+
 template <typename T, int FMT, bool TILE, bool TR>
 __global__ void __launch_bounds__(kTileThreads)
     quantize_tiles(const T* __restrict__ x, int64_t R, int64_t C, int64_t ldx, int col_blocks, uint8_t* __restrict__ q,
@@ -167,8 +202,13 @@ __global__ void __launch_bounds__(kTileThreads)
     const int64_t r0 = rb * 128 + 8 * g, c0 = cb * 128 + 8 * cl;
     const int nc = int(min(int64_t(8), C - c0));
     float f[8][8];
+    if (r0 + 8 <= R && nc == 8) {   // no test between the loads: all eight in flight
 #pragma unroll
-    for (int i = 0; i < 8; ++i) load8<T>(x + (r0 + i < R && nc > 0 ? (r0 + i) * ldx + c0 : 0), r0 + i < R ? nc : 0, f[i]);
+        for (int i = 0; i < 8; ++i) load8<T>(x + (r0 + i) * ldx + c0, 8, f[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) load8<T>(x + (r0 + i < R && nc > 0 ? (r0 + i) * ldx + c0 : 0), r0 + i < R ? nc : 0, f[i]);
+    }
     Scale s[TILE ? 1 : 8];
     if constexpr (TILE) {
         uint32_t m = 0;
@@ -210,29 +250,8 @@ __global__ void __launch_bounds__(kTileThreads)
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (r0 + i < R && nc > 0) store8(q + (r0 + i) * ldq + c0, pack8<FMT>(f[i], s[0]), nc);
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float col[8] = {f[0][j], f[1][j], f[2][j], f[3][j], f[4][j], f[5][j], f[6][j], f[7][j]};
-        *reinterpret_cast<uint2*>(turned + (8 * cl + j) * 128 + 8 * (g ^ cl)) = pack8<FMT>(col, s[TILE ? 0 : j]);
-    }
-    __syncthreads();
-    // eight lanes a column of x (128 bytes of the result's row)
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int c = k * 32 + (threadIdx.x >> 3), p = 2 * (threadIdx.x & 7);
-        const int64_t col = cb * 128 + c, row = rb * 128 + 8 * p;
-        if (col >= C || row >= R) continue;
-        const uint2 a = *reinterpret_cast<const uint2*>(turned + c * 128 + 8 * (p ^ (c >> 3)));
-        const uint2 b = *reinterpret_cast<const uint2*>(turned + c * 128 + 8 * ((p + 1) ^ (c >> 3)));
-        uint8_t* to = q + col * ldq + row;
-        if (row + 16 <= R) {
-            *reinterpret_cast<uint4*>(to) = make_uint4(a.x, a.y, b.x, b.y);
-        } else {
-            store8(to, a, int(R - row));
-            if (row + 8 < R) store8(to + 8, b, int(R - row - 8));
-        }
+    } else {
+        turn_and_store<FMT, TILE>(f, s, turned, q, ldq, rb, cb, R, C);
     }
 }
 
@@ -263,7 +282,7 @@ extern "C" acrl_status acrl_fp8_quantize(const void* x, acrl_dtype x_dtype, int6
                                          acrl_fp8_format format, acrl_fp8_block block, int32_t transpose, uint8_t* q,
                                          int64_t ldq, uint8_t* scale, int64_t lds, int32_t* dev_flags,
                                          acrl_stream stream) {
-    if (R < 0 || C < 0 || R > kMaxGrid || C > kMaxGrid || !dev_flags) return ACRL_ERR_INVALID_ARG;
+    if (R < 0 || C < 0 || R > kMaxGrid || C > kMaxGrid) return ACRL_ERR_INVALID_ARG;
     if (x_dtype != ACRL_BF16 && x_dtype != ACRL_F32) return ACRL_ERR_INVALID_ARG;
     if (format != ACRL_FP8_E4M3 && format != ACRL_FP8_E5M2) return ACRL_ERR_INVALID_ARG;
     if (block != ACRL_FP8_ROW && block != ACRL_FP8_TILE) return ACRL_ERR_INVALID_ARG;

@@ -119,7 +119,8 @@ def _check_product(out, a, b):
 
 
 @pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 130, 128), (5, 300, 129), (16, 257, 640), (17, 128, 1000), (64, 515, 513),
-                                   (128, 129, 300), (129, 16, 256), (200, 300, 520), (300, 257, 2047), (1000, 1111, 1280)])
+                                   (128, 129, 300), (3, 200, 4100), (128, 300, 2100), (100, 64, 9001), (2, 5000, 2600),
+                                   (129, 16, 256), (257, 500, 640), (513, 449, 384), (2100, 700, 130), (200, 300, 520), (300, 257, 2047), (1000, 1111, 1280)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_matmul(M, N, K, dtype):
     a = acrl.fp8_quantize(_matrix(M, K, 1))

@@ -26,7 +26,7 @@ def _call(fn, args, **changed):
 def test_quantize(L):
     ok = dict(x=FAKE, dtype=0, R=4, C=40, ldx=40, fmt=0, block=0, transpose=0, q=FAKE, ldq=48, scale=FAKE, lds=1,
               flags=FAKE, stream=None)
-    for bad in (dict(x=None), dict(q=None), dict(scale=None), dict(flags=None), dict(dtype=2), dict(fmt=2), dict(block=2),
+    for bad in (dict(x=None), dict(q=None), dict(scale=None), dict(dtype=2), dict(fmt=2), dict(block=2),
                 dict(R=-1), dict(C=-1), dict(ldx=32), dict(ldx=44), dict(ldq=32), dict(ldq=40), dict(lds=0),
                 dict(x=FAKE + 8), dict(q=FAKE + 8), dict(dtype=1, ldx=42), dict(C=200, ldx=200, ldq=208),
                 dict(transpose=1, R=200, ldq=208), dict(R=1 << 32)):
@@ -39,7 +39,7 @@ def test_matmul(L):
     ok = dict(a=FAKE, M=4, K=40, lda=48, fa=0, sa=FAKE, ldas=1, ba=0, b=FAKE, N=24, ldb=48, fb=0, sb=FAKE, ldbs=1, bb=1,
               out=FAKE, dtype=0, ldo=24, flags=FAKE, stream=None)
     # a host address (FAKE) is refused as well: every operand is device memory
-    for bad in ({}, dict(a=None), dict(sa=None), dict(b=None), dict(sb=None), dict(out=None), dict(flags=None), dict(M=-1),
+    for bad in ({}, dict(a=None), dict(sa=None), dict(b=None), dict(sb=None), dict(out=None), dict(M=-1),
                 dict(N=-1), dict(K=-1), dict(lda=32), dict(lda=40), dict(ldb=44), dict(ldas=0), dict(ldbs=0), dict(fa=2),
                 dict(fb=-1), dict(ba=2), dict(bb=2), dict(dtype=2), dict(ldo=16), dict(ldo=28), dict(out=FAKE + 8),
                 dict(a=FAKE + 8), dict(b=FAKE + 4), dict(M=1 << 31), dict(K=1 << 31, lda=1 << 32, ldb=1 << 32)):
@@ -55,7 +55,7 @@ def test_linear(L):
     ok = dict(x=FAKE, M=4, K=40, ldx=40, fx=0, w=FAKE, N=24, ldw=48, fw=0, sw=FAKE, ldws=1, bw=1, out=FAKE, dtype=0, ldo=24,
               ws=FAKE, n=n, flags=FAKE, stream=None)
     for bad in ({}, dict(x=None), dict(w=None), dict(sw=None), dict(out=None), dict(ws=None), dict(ws=FAKE + 8), dict(n=n - 1),
-                dict(flags=None), dict(ldx=32), dict(ldw=40), dict(ldo=20), dict(fx=2), dict(fw=2), dict(bw=2), dict(M=-1)):
+                dict(ldx=32), dict(ldw=40), dict(ldo=20), dict(fx=2), dict(fw=2), dict(bw=2), dict(M=-1)):
         assert _call(L.acrl_fp8_linear, ok, **bad) == E, bad
     assert _call(L.acrl_fp8_linear, ok, N=0) == OK
 
