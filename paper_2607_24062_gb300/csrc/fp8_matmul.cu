@@ -179,6 +179,22 @@ __device__ __forceinline__ void tile_at(int t, const Problem& pr, int& tp, int& 
     tq = r / h;
 }
 
+// One lane of a warp that is together.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t r;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(r));
+    return r != 0;
+}
+
+// A whole warp waits; the common case, a phase that has completed, without a call.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int32_t* abort) {
+    const bool ok = mbar_try_wait(bar, parity) || wait_phase(bar, parity, abort);
+    return __all_sync(0xffffffffu, ok);
+}
+
+// The producer's and the MMA warp's loops run in the whole warp, and one lane is elected for each batch of copies or MMAs:
+// stage, descriptors and coordinates are then the same for the warp and live in the uniform registers that those
+// instructions take.  Run by one lane of a diverged warp, the MMA loop took 900 cycles a slab, twice the MMAs' time.
 template <bool PAIR>
 __device__ void produce(const CUtensorMap* tmP, const CUtensorMap* tmQ, uint8_t* ring, Barriers* bars, const Problem& pr,
                         uint32_t rank) {
@@ -194,7 +210,7 @@ __device__ void produce(const CUtensorMap* tmP, const CUtensorMap* tmQ, uint8_t*
         const int p0 = PAIR ? (2 * tp + int(rank)) * kRows : tp * kRows;
         const int q0 = tq * pr.cols + (PAIR ? int(rank) * q_rows : 0);
         for (int kb = w.lo; kb < w.hi; ++kb) {
-            if (!mbar_try_wait(&bars->empty[stage], phase ^ 1u) && !wait_phase(&bars->empty[stage], phase ^ 1u, abort)) {
+            if (!warp_wait(&bars->empty[stage], phase ^ 1u, abort)) {
                 give_up(abort, pr.flags);
                 // the copies that were started land before the CTA can exit: the even CTA's barriers count both CTAs',
                 // the odd one gives its own time to land
@@ -209,15 +225,12 @@ __device__ void produce(const CUtensorMap* tmP, const CUtensorMap* tmQ, uint8_t*
                 return;
             }
             uint8_t* s = ring + stage * bytes;
-            uint32_t bar = smem_u32(&bars->full[stage]);
-            if (PAIR) {
-                if (rank == 0) mbar_expect_tx(&bars->full[stage], 2 * bytes);
-                bar = peer_addr(&bars->full[stage], 0);
-            } else {
-                mbar_expect_tx(&bars->full[stage], bytes);
+            const uint32_t bar = PAIR ? peer_addr(&bars->full[stage], 0) : smem_u32(&bars->full[stage]);
+            if (elect_one()) {
+                if (!PAIR || rank == 0) mbar_expect_tx(&bars->full[stage], (PAIR ? 2 : 1) * bytes);
+                tma_load<PAIR>(s, tmP, bar, kb * kSlab, p0);
+                tma_load<PAIR>(s + kRows * kSlab, tmQ, bar, kb * kSlab, q0);
             }
-            tma_load<PAIR>(s, tmP, bar, kb * kSlab, p0);
-            tma_load<PAIR>(s + kRows * kSlab, tmQ, bar, kb * kSlab, q0);
             ++issued;
             if (++stage == pr.stages) {
                 stage = 0;
@@ -230,120 +243,182 @@ __device__ void produce(const CUtensorMap* tmP, const CUtensorMap* tmQ, uint8_t*
 template <bool PAIR>
 __device__ void issue_mmas(uint8_t* ring, Barriers* bars, uint32_t tmem, const Problem& pr, uint32_t rank) {
     volatile int32_t* abort = &bars->abort;
-    const int bytes = (kRows + (PAIR ? pr.cols / 2 : pr.cols)) * kSlab;
+    const uint32_t units = uint32_t((kRows + (PAIR ? pr.cols / 2 : pr.cols)) * kSlab) >> 4;   // of a stage, in descriptors
     const uint64_t pdesc0 = smem_desc(smem_u32(ring)), qdesc0 = smem_desc(smem_u32(ring + kRows * kSlab));
     const Work<PAIR> w(pr, rank);
     int stage = 0, slot = 0, acc = 0;
     uint32_t phase = 0, sphase = 0, aphase = 0;
     bool ok = true;
     for (int t = w.first; t < pr.p_tiles * pr.q_tiles && ok; t += w.step) {
-        if (!wait_phase(&bars->tempty[acc], aphase ^ 1u, abort)) {
+        if (!warp_wait(&bars->tempty[acc], aphase ^ 1u, abort)) {
             give_up(abort, pr.flags);
             break;
         }
         tc_fence_after();
         const uint32_t d = tmem + uint32_t(acc * pr.cols);
-        for (int kb = w.lo; kb < w.hi; ++kb) {
-            const uint32_t id = uint32_t(kb % kGroup);
-            if ((id == 0 && !wait_phase(&bars->sfull[slot], sphase, abort)) ||
-                (!mbar_try_wait(&bars->full[stage], phase) && !wait_phase(&bars->full[stage], phase, abort))) {
-                give_up(abort, pr.flags);
-                ok = false;
-                break;
-            }
-            tc_fence_after();
-            const uint64_t pd = pdesc0 + uint64_t((stage * bytes) >> 4), qd = qdesc0 + uint64_t((stage * bytes) >> 4);
+        for (int kb = w.lo; kb < w.hi && ok; kb += kGroup) {
+            ok = warp_wait(&bars->sfull[slot], sphase, abort);
             const uint32_t sc = tmem + kScaleBase + uint32_t(slot) * kScaleCols;
 #pragma unroll
-            for (int k = 0; k < kSlab / 32; ++k)   // 32 columns = 32 bytes = 2 descriptor units
-                mma_scaled<PAIR>(d, pd + uint64_t(2 * k), qd + uint64_t(2 * k), pr.idesc | id << 29 | id << 4, sc, sc + 8,
-                                 kb > w.lo || k > 0);
-            commit<PAIR>(&bars->empty[stage]);
-            if (++stage == pr.stages) {
-                stage = 0;
-                phase ^= 1u;
-            }
-            if (id == kGroup - 1 || kb == w.hi - 1) {
-                commit<PAIR>(&bars->sempty[slot]);
-                if (++slot == kScaleSlots) {
-                    slot = 0;
-                    sphase ^= 1u;
+            for (int i = 0; i < kGroup; ++i) {     // the slab's scales are byte i of the group's words
+                if (kb + i >= w.hi || !ok) break;
+                ok = warp_wait(&bars->full[stage], phase, abort);
+                if (!ok) break;
+                tc_fence_after();
+                const uint64_t pd = pdesc0 + stage * units, qd = qdesc0 + stage * units;
+                const uint32_t more = kb + i > w.lo;
+                if (elect_one()) {
+#pragma unroll
+                    for (int k = 0; k < kSlab / 32; ++k)   // 32 columns = 32 bytes = 2 descriptor units
+                        mma_scaled<PAIR>(d, pd + uint64_t(2 * k), qd + uint64_t(2 * k), pr.idesc | uint32_t(i) << 29 | uint32_t(i) << 4,
+                                         sc, sc + 8, k > 0 ? 1u : more);
+                    commit<PAIR>(&bars->empty[stage]);
+                }
+                if (++stage == pr.stages) {
+                    stage = 0;
+                    phase ^= 1u;
                 }
             }
+            if (!ok) break;
+            if (elect_one()) commit<PAIR>(&bars->sempty[slot]);
+            if (++slot == kScaleSlots) {
+                slot = 0;
+                sphase ^= 1u;
+            }
         }
-        if (!ok) break;
-        commit<PAIR>(&bars->tfull[acc]);
+        if (!ok) {
+            give_up(abort, pr.flags);
+            break;
+        }
+        if (elect_one()) commit<PAIR>(&bars->tfull[acc]);
         if (++acc == pr.accs) {
             acc = 0;
             aphase ^= 1u;
         }
     }
     // every MMA has finished before the CTA moves on
-    if (PAIR)
-        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
-                         peer_addr(&bars->mma_done, 0))
-                     : "memory");
-    else
-        commit<false>(&bars->mma_done);
+    if (elect_one()) {
+        if (PAIR)
+            asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
+                             peer_addr(&bars->mma_done, 0))
+                         : "memory");
+        else
+            commit<false>(&bars->mma_done);
+    }
     wait_phase(&bars->mma_done, 0, nullptr);
+    __syncwarp();
 }
 
-// The scales of slabs kb .. kb+3 of one row, one a byte; 127 (2^0) beyond the matrix, where the operands are zeros.
-__device__ __forceinline__ uint32_t scale_word(const Operand& o, int row, int kb, int slabs) {
-    if (row >= o.rows) return 0x7f7f7f7fu;
-    const uint8_t* p = o.scale + int64_t(row >> o.shift) * o.lds + kb;
-    if (o.words && kb + kGroup <= slabs) return __ldg(reinterpret_cast<const uint32_t*>(p));
-    uint32_t w = 0;
+// The scales of slabs kb .. kb+3 of N rows 32 apart, one a byte.  Rows and slabs beyond the matrix take the last one's: what
+// they scale is zeros, or is not stored.  There is no test around a load, so that all of them are in flight together (a
+// test for each, and they came one after the other: 4,096 x 16,384 x 16,384 in 952 us, the tensor cores half idle).
+template <int N>
+__device__ __forceinline__ void scale_words(const Operand& o, int row, int kb, int slabs, uint32_t* v) {
+    const uint8_t* p[N];
 #pragma unroll
-    for (int i = 0; i < kGroup; ++i) w |= (kb + i < slabs ? uint32_t(__ldg(p + i)) : 127u) << (8 * i);
-    return w;
+    for (int c = 0; c < N; ++c) p[c] = o.scale + int64_t(min(row + 32 * c, o.rows - 1) >> o.shift) * o.lds;
+    if (o.words && kb + kGroup <= slabs) {
+#pragma unroll
+        for (int c = 0; c < N; ++c) v[c] = __ldg(reinterpret_cast<const uint32_t*>(p[c] + kb));
+        return;
+    }
+    uint32_t b[N][kGroup];
+#pragma unroll
+    for (int i = 0; i < kGroup; ++i) {
+        const int at = min(kb + i, slabs - 1);
+#pragma unroll
+        for (int c = 0; c < N; ++c) b[c][i] = __ldg(p[c] + at);
+    }
+#pragma unroll
+    for (int c = 0; c < N; ++c) v[c] = b[c][0] | b[c][1] << 8 | b[c][2] << 16 | b[c][3] << 24;
 }
 
+// The groups of slabs of a CTA's tiles, in the order that the MMAs take them.
+template <bool PAIR>
+struct Groups {
+    const Problem& pr;
+    const Work<PAIR> w;
+    const int lane;
+    const uint32_t rank;
+    int t, kb, p0, q0;
+    __device__ Groups(const Problem& problem, uint32_t r) : pr(problem), w(problem, r), lane(threadIdx.x & 31), rank(r) {
+        t = w.first;
+        kb = w.lo;
+        if (w.lo == w.hi) t = pr.p_tiles * pr.q_tiles;
+        place();
+    }
+    __device__ bool more() const { return t < pr.p_tiles * pr.q_tiles; }
+    __device__ void place() {
+        if (!more()) return;
+        int tp, tq;
+        tile_at(t, pr, tp, tq);
+        p0 = (PAIR ? 2 * tp + int(rank) : tp) * kRows + lane;
+        q0 = tq * pr.cols + lane;
+    }
+    // This lane's words of the group at hand, and on to the next.
+    __device__ bool take(uint32_t (&v)[12]) {
+        if (!more()) return false;
+        scale_words<4>(pr.p, p0, kb, pr.slabs, v);
+        scale_words<8>(pr.q, q0, kb, pr.slabs, v + 4);
+        kb += kGroup;
+        if (kb >= w.hi) {
+            kb = w.lo;
+            t += w.step;
+            place();
+        }
+        return true;
+    }
+};
+
+// Words are loaded two groups ahead of their use.
 template <bool PAIR>
 __device__ void write_scales(Barriers* bars, uint32_t tmem, const Problem& pr, uint32_t rank) {
     volatile int32_t* abort = &bars->abort;
     const int lane = threadIdx.x & 31;
     const uint32_t lanes = uint32_t((threadIdx.x >> 5) & 3) << 21;   // this warp's quarter, 32 lanes each
-    const Work<PAIR> w(pr, rank);
     int slot = 0;
     uint32_t phase = 0;
-    for (int t = w.first; t < pr.p_tiles * pr.q_tiles; t += w.step) {
-        int tp, tq;
-        tile_at(t, pr, tp, tq);
-        const int p0 = (PAIR ? 2 * tp + int(rank) : tp) * kRows + lane, q0 = tq * pr.cols + lane;
-        for (int kb = w.lo; kb < w.hi; kb += kGroup) {
-            uint32_t v[12];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) v[c] = scale_word(pr.p, p0 + 32 * c, kb, pr.slabs);
-#pragma unroll
-            for (int c = 0; c < 8; ++c) v[4 + c] = 32 * c < pr.cols ? scale_word(pr.q, q0 + 32 * c, kb, pr.slabs) : 0x7f7f7f7fu;
-            const bool free = wait_phase(&bars->sempty[slot], phase ^ 1u, abort);
-            if (!__all_sync(0xffffffffu, free)) {
-                give_up(abort, pr.flags);
-                return;
-            }
-            tc_fence_after();
-            const uint32_t at = tmem + lanes + kScaleBase + uint32_t(slot) * kScaleCols;
-            asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v[0]), "r"(v[1]),
-                         "r"(v[2]), "r"(v[3])
-                         : "memory");
-            asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(at + 8),
-                         "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11])
-                         : "memory");
-            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) {
-                if (PAIR)
-                    remote_arrive(peer_addr(&bars->sfull[slot], 0));
-                else
-                    mbar_arrive(&bars->sfull[slot]);
-            }
-            if (++slot == kScaleSlots) {
-                slot = 0;
-                phase ^= 1u;
-            }
+    auto write = [&](const uint32_t (&v)[12]) {
+        const bool free = wait_phase(&bars->sempty[slot], phase ^ 1u, abort);
+        if (!__all_sync(0xffffffffu, free)) {
+            give_up(abort, pr.flags);
+            return false;
         }
+        tc_fence_after();
+        const uint32_t at = tmem + lanes + kScaleBase + uint32_t(slot) * kScaleCols;
+        asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]),
+                     "r"(v[3])
+                     : "memory");
+        asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(at + 8), "r"(v[4]),
+                     "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11])
+                     : "memory");
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+            if (PAIR)
+                remote_arrive(peer_addr(&bars->sfull[slot], 0));
+            else
+                mbar_arrive(&bars->sfull[slot]);
+        }
+        if (++slot == kScaleSlots) {
+            slot = 0;
+            phase ^= 1u;
+        }
+        return true;
+    };
+    Groups<PAIR> g(pr, rank);
+    uint32_t a[12], b[12], c[12];
+    bool na = g.take(a), nb = g.take(b), nc = g.take(c);
+    while (na) {
+        if (!write(a)) return;
+        na = g.take(a);
+        if (!nb) return;
+        if (!write(b)) return;
+        nb = g.take(b);
+        if (!nc) return;
+        if (!write(c)) return;
+        nc = g.take(c);
     }
 }
 
@@ -562,9 +637,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     float* parts = reinterpret_cast<float*>(ring + pr.stages * (kRows + pr.cols) * kSlab);
     bool ok = true;
     if (warp == 0) {
-        if (lane == 0) produce<PAIR>(&tmP, &tmQ, ring, bars, pr, rank);
+        produce<PAIR>(&tmP, &tmQ, ring, bars, pr, rank);
     } else if (warp == 1) {
-        if (lane == 0 && (!PAIR || rank == 0)) issue_mmas<PAIR>(ring, bars, tmem, pr, rank);
+        if (!PAIR || rank == 0) issue_mmas<PAIR>(ring, bars, tmem, pr, rank);
     } else if (warp < 6) {
         write_scales<PAIR>(bars, tmem, pr, rank);
     } else if constexpr (PAIR) {
