@@ -52,6 +52,43 @@ acrl_status launch(void (*kernel)(P...), int64_t grid, int threads, size_t smem,
     return launch_status();
 }
 
+// How many clusters of `ctas` CTAs the current device holds at once: a property of the kernel, its shared memory and the
+// device, kept for the shapes asked for last.
+inline int64_t resident_clusters(const void* kernel, int threads, size_t smem, int ctas) {
+    struct Known {
+        const void* kernel;
+        size_t smem;
+        int dev, ctas, n;
+    };
+    static thread_local Known known[8] = {};
+    static thread_local int turn = 0;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return 0;
+    }
+    for (const Known& k : known)
+        if (k.kernel == kernel && k.smem == smem && k.dev == dev && k.ctas == ctas) return k.n;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(ctas) * 4096u, 1, 1);
+    cfg.blockDim = dim3(unsigned(threads), 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = unsigned(ctas);
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return 0;
+    }
+    known[turn] = Known{kernel, smem, dev, ctas, n};
+    turn = (turn + 1) % 8;
+    return n;
+}
+
 inline bool params_ok(const acrl_params* p) {
     if (!p) return false;
     if (!(p->gamma > 0.f) || !(p->C > 1.f) || !(p->clip_eps >= 0.f && p->clip_eps < 1.f)) return false;

@@ -33,7 +33,6 @@
 //   columns of the sum (K) and adds its accumulators through distributed shared
 //   memory, in rank order.
 #include <algorithm>
-#include <atomic>
 
 #include "acrl_device.cuh"
 #include "acrl_host.h"
@@ -591,7 +590,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t* staging = ring + kRingBytes<T, PAIR>;
     Barriers* bars = reinterpret_cast<Barriers*>(staging + kStaging<T, PAIR>);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5;
     const uint32_t rank = cluster_rank();
     const int nct = int(cluster_size());
     if (threadIdx.x == 0) {
@@ -689,34 +688,6 @@ Operand operand(const Matrix& m) {
 constexpr int64_t kAloneRows = 128;
 constexpr int kMaxSplit = 8;
 
-// How many CTA pairs of a kernel the current device holds at once: a property of the two, looked up once.
-template <typename K>
-int resident_pairs(K* kernel) {
-    constexpr int kDevices = 64;
-    static std::atomic<int> known[kDevices];
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
-    if (dev < kDevices)
-        if (const int n = known[dev].load(std::memory_order_relaxed)) return n;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(2 * 1024, 1, 1);
-    cfg.blockDim = dim3(kThreads, 1, 1);
-    cfg.dynamicSmemBytes = kSmemBytes;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = 2;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return 0;
-    }
-    if (dev < kDevices) known[dev].store(n, std::memory_order_relaxed);
-    return n;
-}
-
 template <typename T, bool PAIR>
 acrl_status launch_kernel(const Matrix& p, const Matrix& q, int64_t K, Problem pr, int64_t grid, int cluster, cudaStream_t s) {
     CUtensorMap tmP, tmQ, tmO;
@@ -736,7 +707,7 @@ acrl_status launch_kernel(const Matrix& p, const Matrix& q, int64_t K, Problem p
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) != cudaSuccess)
         return launch_status();
     if (PAIR) {   // no more than can be resident at once: they are persistent
-        const int most = resident_pairs(kernel);
+        const int64_t most = resident_clusters(reinterpret_cast<const void*>(kernel), kThreads, kSmemBytes, 2);
         if (most < 1) return ACRL_ERR_CUDA;
         grid = std::min<int64_t>(grid, 2 * most);
     }

@@ -46,8 +46,8 @@ __device__ __forceinline__ uint64_t global_ns() {
 // Wait for the completion of the phase of `bar` with parity `parity`.  Gives
 // up after kWaitNs, or early once another role has set *abort (unless abort
 // is null).
-__device__ __noinline__ bool wait_phase(uint64_t* bar, uint32_t parity, volatile int32_t* abort,
-                                        uint64_t limit_ns = kWaitNs) {
+__device__ __forceinline__ bool wait_phase_inline(uint64_t* bar, uint32_t parity, volatile int32_t* abort,
+                                                  uint64_t limit_ns = kWaitNs) {
     if (mbar_try_wait(bar, parity)) return true;
     const uint64_t t0 = global_ns();
     for (uint32_t i = 1;; ++i) {
@@ -57,6 +57,13 @@ __device__ __noinline__ bool wait_phase(uint64_t* bar, uint32_t parity, volatile
             if (global_ns() - t0 > limit_ns) return false;
         }
     }
+}
+
+// The same as a call, for the places where it is rare: few instructions there, but what is live across it is spilled where
+// it is more than a call preserves.
+__device__ __noinline__ bool wait_phase(uint64_t* bar, uint32_t parity, volatile int32_t* abort,
+                                        uint64_t limit_ns = kWaitNs) {
+    return wait_phase_inline(bar, parity, abort, limit_ns);
 }
 
 }  // namespace

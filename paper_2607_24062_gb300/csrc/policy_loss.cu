@@ -13,14 +13,18 @@
 //     k1 d,  k2 d^2 / 2,  k3 e^-d - 1 + d, whose slope in logp joins c.
 //
 // The gradient needs the sums of the whole row, so a row is swept twice; it is read
-// from memory once.  A cluster of CTAs shares a row: each copies its slice of
-// z (and x) into shared memory with bulk copies, folds the running maxima and
-// sums as the copies land, exchanges one partial state with the others through
-// distributed shared memory, and writes the gradient of its slice from what it
-// kept.  So HBM sees every operand once (2 bytes of z, 2 of x, 2 of the
-// gradient an element), which bounds it, with the SFU next (three
-// exponentials an element pair).  Several such CTAs share an SM, so that one
-// loads while another computes and a third stores.
+// from memory once.  Persistent CTAs, alone or as a cluster that shares each of its
+// rows, run four roles that work on different rows at the same time:
+//   warp 0       copies the CTA's slices of row after row into a ring of chunks in
+//                shared memory (bulk copies);
+//   warp 1       merges the states of a row's slices, works out its scalars and outputs;
+//   F warps      fold the running maxima and sums of a slice as its chunks land, and
+//                push the slice's state to every CTA of the cluster (distributed
+//                shared memory, counted on a barrier there);
+//   F warps      write the gradient of a slice from its chunks, and free them.
+// So loads, arithmetic, the exchange between CTAs and stores of neighbouring rows
+// overlap, and HBM sees every operand once: 2 bytes of z, 2 of x and 2 of the gradient an
+// element, which bounds it.
 #include <algorithm>
 #include <cmath>
 
@@ -32,9 +36,11 @@
 namespace acrl {
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
-constexpr int kMaxChunks = 8;
+constexpr int kMaxSlots = 32;      // chunks of a ring
+constexpr int kMaxAhead = 7;       // rows that may lie in a ring
+constexpr int kStates = 16;        // states of rows under way: a CTA's fold may be 2 kMaxAhead rows ahead of another's merge
+constexpr int kGrads = 4;          // rows between the merge and the writing warps
 
 enum Kind { kSampled, kExact, kReverse };   // which sums a row needs
 
@@ -42,8 +48,9 @@ struct PolicyArgs {
     const acrl_bf16 *z, *x;
     int64_t ldz, ldx;
     int V;
-    int keep;      // vectors of each operand that a CTA keeps
-    int chunk;     // vectors of a bulk copy
+    int64_t T;
+    int keep;      // vectors of each operand that a CTA keeps of a row
+    int slots;     // chunks of the ring
     const int32_t* ids;
     const uint8_t* mask;
     const float *coef, *kl_coef, *old_logp, *ref_logp;
@@ -63,11 +70,48 @@ struct State {
 
 __device__ __forceinline__ State empty_state() { return State{-INFINITY, kLowestU, 0.f, -INFINITY, kLowestU, 0.f, 0.f}; }
 
-__device__ __forceinline__ void unpack8(const uint4& v, float (&f)[8]) {
-    f[0] = bf16_lo(v.x); f[1] = bf16_hi(v.x);
-    f[2] = bf16_lo(v.y); f[3] = bf16_hi(v.y);
-    f[4] = bf16_lo(v.z); f[5] = bf16_hi(v.z);
-    f[6] = bf16_lo(v.w); f[7] = bf16_hi(v.w);
+// Two fp32 numbers in a register pair: sums, products and fused products of both in one instruction (issue bounds these
+// sweeps next to HBM; one number at a time took 36 instructions a column pair where this takes some 16).
+using Two = unsigned long long;
+
+__device__ __forceinline__ Two two(float lo, float hi) {
+    Two r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void split(Two a, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(a)); }
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+    Two r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ Two add2(Two a, Two b) {
+    Two r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ Two mul2(Two a, Two b) {
+    Two r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ Two ex2_2(Two a) {
+    float lo, hi;
+    split(a, lo, hi);
+    return two(ex2(lo), ex2(hi));
+}
+// d where the weight is not 0, 0 elsewhere.
+__device__ __forceinline__ Two where_weighted(Two w, Two d) {
+    float w0, w1, d0, d1;
+    split(w, w0, w1);
+    split(d, d0, d1);
+    return two(w0 > 0.f ? d0 : 0.f, w1 > 0.f ? d1 : 0.f);
+}
+__device__ __forceinline__ Two widen(uint32_t pair) { return two(bf16_lo(pair), bf16_hi(pair)); }
+__device__ __forceinline__ float sum_of(Two a) {
+    float lo, hi;
+    split(a, lo, hi);
+    return lo + hi;
 }
 
 __device__ __forceinline__ uint32_t max_pairs(const uint4& v) {
@@ -82,10 +126,9 @@ __device__ __forceinline__ float raise_max(float m, float& mx, float& U) {
     return f;
 }
 
-// Fold N vectors of each operand.  SAFE: a column of probability 0 adds nothing to the cross sum, whatever the
-// other side holds there (an infinite difference times 0 is NaN); without it such a row ends with a cross sum
-// that is not finite, and is folded again.
-template <Kind KIND, int N, bool SAFE>
+// Fold N vectors of each operand.  A column of probability 0 adds nothing to the cross sum, whatever the other side
+// holds there (an infinite difference times 0 would be NaN).
+template <Kind KIND, int N>
 __device__ __forceinline__ void fold(State& st, const uint4 (&z)[N], const uint4 (&x)[N]) {
     uint32_t pm = max_pairs(z[0]);
 #pragma unroll
@@ -107,28 +150,27 @@ __device__ __forceinline__ void fold(State& st, const uint4 (&z)[N], const uint4
             if (KIND == kReverse) st.cross *= f;
         }
     }
-    float sz[2] = {0.f, 0.f}, sx[2] = {0.f, 0.f}, cr[2] = {0.f, 0.f};
+    const Two l2e = two(kLog2e, kLog2e), nU = two(-st.U, -st.U), nW = two(-st.W, -st.W), minus = two(-1.f, -1.f);
+    Two sz = two(0.f, 0.f), sx = sz, cr = sz;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-        float a[8], b[8];
-        unpack8(z[k], a);
-        if (KIND != kSampled) unpack8(x[k], b);
+        const uint32_t zw[4] = {z[k].x, z[k].y, z[k].z, z[k].w}, xw[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float e = ex2(fmaf(a[j], kLog2e, -st.U));
-            sz[j & 1] += e;
+        for (int j = 0; j < 4; ++j) {
+            const Two a = widen(zw[j]), e = ex2_2(fma2(a, l2e, nU));
+            sz = add2(sz, e);
             if constexpr (KIND != kSampled) {
-                const float h = ex2(fmaf(b[j], kLog2e, -st.W));
-                sx[j & 1] += h;
-                const float w = KIND == kExact ? e : h, d = KIND == kExact ? a[j] - b[j] : b[j] - a[j];
-                cr[j & 1] = SAFE ? (w > 0.f ? fmaf(w, d, cr[j & 1]) : cr[j & 1]) : fmaf(w, d, cr[j & 1]);
+                const Two b = widen(xw[j]), h = ex2_2(fma2(b, l2e, nW));
+                sx = add2(sx, h);
+                const Two w = KIND == kExact ? e : h, d = KIND == kExact ? fma2(b, minus, a) : fma2(a, minus, b);
+                cr = fma2(w, where_weighted(w, d), cr);
             }
         }
     }
-    st.sz += sz[0] + sz[1];
+    st.sz += sum_of(sz);
     if (KIND != kSampled) {
-        st.sx += sx[0] + sx[1];
-        st.cross += cr[0] + cr[1];
+        st.sx += sum_of(sx);
+        st.cross += sum_of(cr);
     }
 }
 
@@ -182,17 +224,25 @@ __device__ __forceinline__ void bulk_in(void* dst, const void* src, uint32_t byt
         : "memory");
 }
 
-__device__ __forceinline__ void cluster_arrive() {
-    __syncwarp();
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void cluster_wait() {
-    __syncwarp();
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+// A state to CTA `rank` of the cluster, and an arrival on its barrier.
+__device__ __forceinline__ void push_state(const float4* slot, uint64_t* bar, uint32_t rank, const float4& a, const float4& b) {
+    const uint32_t to = peer_addr(slot, rank);
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to), "f"(a.x), "f"(a.y), "f"(a.z), "f"(a.w)
+                 : "memory");
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to + 16), "f"(b.x), "f"(b.y), "f"(b.z), "f"(b.w)
+                 : "memory");
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(peer_addr(bar, rank)) : "memory");
 }
 
-__device__ __forceinline__ void st_peer(const float* p, uint32_t rank, float v) {
-    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer_addr(p, rank)), "f"(v) : "memory");
+// A phase that other CTAs of the cluster complete: what they wrote before they arrived is visible after it.
+__device__ __forceinline__ bool try_wait_cluster(uint64_t* bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+    return ok != 0;
 }
 
 // What the gradient of a row's elements needs.
@@ -205,26 +255,35 @@ struct RowGrad {
     int a;
 };
 
-template <Kind KIND, bool SAFE>
-__device__ __forceinline__ float grad_at(float z, float x, const RowGrad& g) {
-    const float p = ex2(fmaf(z, kLog2e, -g.U));
-    if constexpr (KIND == kSampled) return p * g.c;
-    if constexpr (KIND == kReverse) return fmaf(p, g.c2, -g.k * ex2(fmaf(x, kLog2e, -g.W)));
-    const float v = p * fmaf(g.k, z - x, g.c2);
-    return SAFE ? (p > 0.f ? v : 0.f) : v;
+template <Kind KIND>
+__device__ __forceinline__ Two grad_two(Two z, Two x, const RowGrad& g) {
+    const Two l2e = two(kLog2e, kLog2e), p = ex2_2(fma2(z, l2e, two(-g.U, -g.U)));
+    if constexpr (KIND == kSampled) return mul2(p, two(g.c, g.c));
+    if constexpr (KIND == kReverse) {
+        const Two q = ex2_2(fma2(x, l2e, two(-g.W, -g.W)));
+        return fma2(p, two(g.c2, g.c2), mul2(q, two(-g.k, -g.k)));
+    }
+    const Two d = where_weighted(p, fma2(x, two(-1.f, -1.f), z));
+    return mul2(p, fma2(two(g.k, g.k), d, two(g.c2, g.c2)));
 }
 
-template <Kind KIND, bool SAFE>
+template <Kind KIND>
 __device__ __forceinline__ uint4 grad_vec8(const uint4& zv, const uint4& xv, const RowGrad& g, int rel) {
-    float a[8], b[8], o[8];
-    unpack8(zv, a);
-    if (KIND != kSampled) unpack8(xv, b);
+    const uint32_t zw[4] = {zv.x, zv.y, zv.z, zv.w}, xw[4] = {xv.x, xv.y, xv.z, xv.w};
+    uint32_t o[4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) o[j] = grad_at<KIND, SAFE>(a[j], KIND != kSampled ? b[j] : 0.f, g);
-    if (unsigned(rel) < 8u)
+    for (int j = 0; j < 4; ++j) {
+        float lo, hi;
+        split(grad_two<KIND>(widen(zw[j]), widen(xw[j]), g), lo, hi);
+        o[j] = pack_bf16x2(lo, hi);
+    }
+    if (unsigned(rel) < 8u) {
+        const uint32_t target = pack_bf16x2(g.target, g.target), half = rel & 1 ? 0xffff0000u : 0xffffu;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) o[j] = j == rel ? g.target : o[j];
-    return make_uint4(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]), pack_bf16x2(o[4], o[5]), pack_bf16x2(o[6], o[7]));
+        for (int j = 0; j < 4; ++j)
+            if (j == rel >> 1) o[j] = (o[j] & ~half) | (target & half);
+    }
+    return make_uint4(o[0], o[1], o[2], o[3]);
 }
 
 // A slice of a row: vectors [begin, end) of it, the first `kept` of them in shared memory; the last slice also has
@@ -234,165 +293,16 @@ struct Slice {
     bool last;
 };
 
-template <Kind KIND, bool SAFE>
-__device__ State sweep(const PolicyArgs& A, const acrl_bf16* zr, const acrl_bf16* xr, const uint4* sz, const uint4* sx,
-                       const Slice& sl, uint64_t* bars, bool& landed) {
-    State st = empty_state();
-    const int tid = threadIdx.x;
-    const uint4 *gz = reinterpret_cast<const uint4*>(zr) + sl.begin, *gx = reinterpret_cast<const uint4*>(xr) + sl.begin;
-    const int n = sl.end - sl.begin;
-    if (sl.last)
-        for (int j = (A.V & ~7) + tid; j < A.V; j += kThreads) {
-            // one column as a vector whose others are the lowest number of both operands: they add nothing
-            const uint32_t lowest = 0xff7fff7fu;
-            uint4 a[1] = {make_uint4(0xff7f0000u | zr[j], lowest, lowest, lowest)}, b[1] = {a[0]};
-            if (KIND != kSampled) b[0].x = 0xff7f0000u | xr[j];
-            fold<KIND, 1, SAFE>(st, a, b);
-        }
-    for (int v = sl.kept + tid; v < n; v += kThreads) {   // what is not kept: read again by the gradient
-        uint4 a[1] = {__ldg(gz + v)}, b[1] = {a[0]};
-        if (KIND != kSampled) b[0] = __ldg(gx + v);
-        fold<KIND, 1, SAFE>(st, a, b);
-    }
-    for (int c0 = 0, i = 0; c0 < sl.kept; c0 += A.chunk, ++i) {
-        if (!wait_phase(bars + i, 0, nullptr)) landed = false;
-        const int end = min(sl.kept, c0 + A.chunk);
-        int v = c0 + tid;
-        for (; v + kThreads < end; v += 2 * kThreads) {
-            const uint4 a[2] = {sz[v], sz[v + kThreads]};
-            uint4 b[2] = {a[0], a[1]};
-            if (KIND != kSampled) {
-                b[0] = sx[v];
-                b[1] = sx[v + kThreads];
-            }
-            fold<KIND, 2, SAFE>(st, a, b);
-        }
-        if (v < end) {
-            uint4 a[1] = {sz[v]}, b[1] = {a[0]};
-            if (KIND != kSampled) b[0] = sx[v];
-            fold<KIND, 1, SAFE>(st, a, b);
-        }
-    }
-    return st;
-}
+// What comes after a row's sums.
+enum { kWrite, kFillZero, kFillNaN };
 
-template <Kind KIND, bool SAFE>
-__device__ void write_grad(const PolicyArgs& A, const acrl_bf16* zr, const acrl_bf16* xr, acrl_bf16* gr, const uint4* sz,
-                           const uint4* sx, const Slice& sl, const RowGrad& g) {
-    const int tid = threadIdx.x;
-    const uint4 *gz = reinterpret_cast<const uint4*>(zr) + sl.begin, *gx = reinterpret_cast<const uint4*>(xr) + sl.begin;
-    uint4* out = reinterpret_cast<uint4*>(gr) + sl.begin;
-    const int n = sl.end - sl.begin, rel0 = g.a - (sl.begin << 3);
-    for (int v = tid; v < sl.kept; v += kThreads)
-        st_stream(out + v, grad_vec8<KIND, SAFE>(sz[v], KIND != kSampled ? sx[v] : sz[v], g, rel0 - (v << 3)));
-    for (int v = sl.kept + tid; v < n; v += kThreads) {
-        const uint4 a = __ldg(gz + v);
-        st_stream(out + v, grad_vec8<KIND, SAFE>(a, KIND != kSampled ? __ldg(gx + v) : a, g, rel0 - (v << 3)));
-    }
-    if (sl.last)
-        for (int j = (A.V & ~7) + tid; j < A.V; j += kThreads) {
-            const float v = grad_at<KIND, SAFE>(bf16_to_float(zr[j]), KIND != kSampled ? bf16_to_float(xr[j]) : 0.f, g);
-            gr[j] = acrl_bf16(pack_bf16x2(j == g.a ? g.target : v, 0.f) & 0xffffu);
-        }
-}
-
-__device__ __forceinline__ void fill_grad(const PolicyArgs& A, acrl_bf16* gr, const Slice& sl, uint32_t pair) {
-    uint4* out = reinterpret_cast<uint4*>(gr);
-    for (int v = sl.begin + threadIdx.x; v < sl.end; v += kThreads) st_stream(out + v, make_uint4(pair, pair, pair, pair));
-    if (sl.last)
-        for (int j = (A.V & ~7) + threadIdx.x; j < A.V; j += kThreads) gr[j] = acrl_bf16(pair & 0xffffu);
-}
-
+// The row's scalars from its merged state, in every lane of a warp; `writes`: this thread stores the row's outputs.
 template <Kind KIND>
-__global__ void __launch_bounds__(kThreads) policy_kernel(const __grid_constant__ PolicyArgs A) {
-    extern __shared__ __align__(16) uint4 kept[];
-    __shared__ uint64_t bars[kMaxChunks];
-    __shared__ float parts[2][kMaxCluster][8];     // per pass: the CTAs' states
-    __shared__ float warps[kWarps][8];
-    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-    const int nct = int(cluster_size()), rank = int(cluster_rank());
-    const int64_t t = int64_t(blockIdx.x) / nct;
-    grid_begin();
-    const int nvec = A.V >> 3, per = (nvec + nct - 1) / nct;
-    Slice sl;
-    sl.begin = min(nvec, rank * per);
-    sl.end = min(nvec, sl.begin + per);
-    sl.kept = min(sl.end - sl.begin, A.keep);
-    sl.last = rank == nct - 1;
-    acrl_bf16* gr = A.grad + t * A.ldg;
-    const bool first = rank == 0 && tid == 0;
-    const int a = A.ids[t];
-    const bool valid = !(A.mask && A.mask[t] == 0);
-    if (!valid || a < 0 || a >= A.V) {     // the same for the whole cluster
-        fill_grad(A, gr, sl, 0u);
-        if (first) {
-            A.logp[t] = A.token_loss[t] = 0.f;
-            if (A.kl_out) A.kl_out[t] = 0.f;
-            if (valid) raise_flag(A.flags, ACRL_FLAG_BAD_ID);
-        }
-        return;
-    }
-    const acrl_bf16 *zr = A.z + t * A.ldz, *xr = KIND == kSampled ? zr : A.x + t * A.ldx;
-    uint4 *sz = kept, *sx = kept + A.keep;
-    if (tid == 0) {
-        for (int i = 0; i < kMaxChunks; ++i) mbar_init(bars + i, 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        const uint64_t once = policy_evict_first();
-        for (int c0 = 0, i = 0; c0 < sl.kept; c0 += A.chunk, ++i) {
-            const uint32_t bytes = uint32_t(min(A.chunk, sl.kept - c0)) * 16u;
-            mbar_expect_tx(bars + i, (KIND == kSampled ? 1 : 2) * bytes);
-            bulk_in(sz + c0, reinterpret_cast<const uint4*>(zr) + sl.begin + c0, bytes, bars + i, once);
-            if (KIND != kSampled) bulk_in(sx + c0, reinterpret_cast<const uint4*>(xr) + sl.begin + c0, bytes, bars + i, once);
-        }
-    }
-    const float za = bf16_to_float(zr[a]), xa = KIND == kSampled ? 0.f : bf16_to_float(xr[a]);
-    const float c0 = A.coef ? A.coef[t] : 0.f, kc = A.kl_coef ? A.kl_coef[t] : 0.f;
-    const float old = A.old_logp ? A.old_logp[t] : 0.f, ref = A.ref_logp ? A.ref_logp[t] : 0.f;
-    __syncthreads();                        // the barriers are initialised
-    if (nct > 1) cluster_arrive();          // this CTA runs: its shared memory may be written
-    bool landed = true, safe = false;
-    State row;
-    for (int pass = 0;; ++pass) {
-        State st = pass == 0 ? sweep<KIND, false>(A, zr, xr, sz, sx, sl, bars, landed)
-                             : sweep<KIND, true>(A, zr, xr, sz, sx, sl, bars, landed);
-        st = meet<KIND, 32>(st);
-        if (pass > 0) __syncthreads();      // the warps have read the first pass's states
-        if (lane == 0) {
-            float* w = warps[wid];
-            w[0] = st.mz; w[1] = st.U; w[2] = st.sz; w[3] = st.mx; w[4] = st.W; w[5] = st.sx; w[6] = st.cross;
-        }
-        __syncthreads();
-        const float* w = warps[lane & (kWarps - 1)];
-        row = meet<KIND, kWarps>(State{w[0], w[1], w[2], w[3], w[4], w[5], w[6]});
-        if (nct > 1) {
-            if (pass == 0) cluster_wait();  // every CTA runs
-            if (wid == 0 && lane < nct) {   // lane r hands this CTA's state to CTA r
-                const float* mine = parts[pass][rank];
-                st_peer(mine + 0, lane, row.mz);
-                st_peer(mine + 1, lane, row.U);
-                st_peer(mine + 2, lane, row.sz);
-                st_peer(mine + 3, lane, row.mx);
-                st_peer(mine + 4, lane, row.W);
-                st_peer(mine + 5, lane, row.sx);
-                st_peer(mine + 6, lane, row.cross);
-            }
-            cluster_arrive();
-            cluster_wait();
-            const float* o = parts[pass][lane & (kMaxCluster - 1)];
-            const bool there = (lane & (kMaxCluster - 1)) < nct;
-            const State e = empty_state();
-            row = meet<KIND, kMaxCluster>(there ? State{o[0], o[1], o[2], o[3], o[4], o[5], o[6]} : e);
-        }
-        if (KIND == kSampled || pass > 0 || isfinite(row.cross) || !isfinite(row.sz) || !isfinite(row.sx)) break;
-        safe = true;
-    }
-    if (!landed) raise_flag(A.flags, ACRL_FLAG_TIMEOUT);
-
-    // the row's scalars, the same in every thread
+__device__ __forceinline__ int row_scalars(const PolicyArgs& A, int64_t t, const State& row, int a, float za, float xa,
+                                           float c0, float kc, float old, float ref, bool writes, RowGrad& g) {
     const float lz = kLn2 * (log2f(row.sz) - fmaf(row.mz, kLog2e, -row.U));      // lse_z - max z
     const float logp = (za - row.mz) - lz;
     float KL = 0.f, apart = 0.f, logq = 0.f;                                      // apart = lse_z - lse_x
-    RowGrad g;
     g.a = a;
     g.k = kc;
     g.U = row.U + log2f(row.sz);
@@ -433,17 +343,14 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(const __grid_constant_
     const bool defined = isfinite(logp) && isfinite(lz) && (KIND == kSampled || isfinite(KL));
     const bool carries = c0 != 0.f || kc != 0.f;
     const bool undefined = carries && (!defined || (c0 != 0.f && isnan(ratio)) || (kc != 0.f && !isfinite(KL)));
-    if (first) {
+    if (writes) {
         const float nan = __int_as_float(0x7fc00000);
         A.logp[t] = defined ? logp : nan;
         if (A.kl_out) A.kl_out[t] = defined ? KL : nan;
         A.token_loss[t] = undefined ? nan : loss;
         if (!defined || undefined) raise_flag(A.flags, ACRL_FLAG_NONFINITE);
     }
-    if (!carries || undefined) {
-        fill_grad(A, gr, sl, undefined ? 0x7fc07fc0u : 0u);
-        return;
-    }
+    if (!carries || undefined) return undefined ? kFillNaN : kFillZero;
     g.target = g.c * expm1f(logp);
     g.c2 = g.c;
     if (KIND == kExact) {
@@ -454,47 +361,347 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(const __grid_constant_
         g.c2 = g.c + kc;
         g.target = fmaf(kc, expf(logp) - expf(logq), g.target);
     }
-    if (safe)
-        write_grad<KIND, true>(A, zr, xr, gr, sz, sx, sl, g);
-    else
-        write_grad<KIND, false>(A, zr, xr, gr, sz, sx, sl, g);
+    return kWrite;
 }
 
-// Shared memory of a CTA's slice.  CTAs of up to kSliceBytes let several share an SM.
-constexpr int kSliceBytes = 40 * 1024, kMaxKeepBytes = 192 * 1024;
+template <int F>
+struct Shared {
+    uint64_t full[kMaxSlots];     // a chunk has landed
+    uint64_t empty[kMaxSlots];    // the F writing warps are done with it
+    uint64_t state[kStates];      // every CTA's state of a row is here
+    uint64_t ready[kGrads];       // a row's scalars are here
+    uint64_t taken[kGrads];       // the F writing warps have them
+    float4 states[kStates][kMaxCluster][2];
+    float4 parts[2][F][2];        // the folding warps' states, rows in turn
+    RowGrad grads[kGrads];
+    int what[kGrads];
+    int32_t abort;
+};
+
+__device__ __forceinline__ void put(float4* to, const State& s) {
+    to[0] = make_float4(s.mz, s.U, s.sz, s.mx);
+    to[1] = make_float4(s.W, s.sx, s.cross, 0.f);
+}
+__device__ __forceinline__ State get(const float4* from) {
+    const float4 a = from[0], b = from[1];
+    return State{a.x, a.y, a.z, a.w, b.x, b.y, b.z};
+}
+
+// Position in a ring.
+struct Ring {
+    int n, at = 0;
+    uint32_t phase = 0;
+    __device__ explicit Ring(int size) : n(size) {}
+    __device__ void next() {
+        if (++at == n) {
+            at = 0;
+            phase ^= 1u;
+        }
+    }
+};
+
+// A row's sampled column, or -1 for a row that is left out (masked, or an id outside the vocabulary).
+__device__ __forceinline__ int column_of(const PolicyArgs& A, int64_t t) {
+    if (t >= A.T) return -1;
+    const int a = A.ids[t];
+    return (A.mask && A.mask[t] == 0) || a < 0 || a >= A.V ? -1 : a;
+}
+
+template <Kind KIND, int F>
+struct Cta {
+    static constexpr int kLanes = 32 * F;          // of a role of F warps
+    static constexpr int kChunk = 2 * kLanes;      // vectors of a chunk
+    static constexpr int kOps = KIND == kSampled ? 1 : 2;
+    const PolicyArgs& A;
+    Shared<F>& sh;
+    uint4* ring;
+    Slice sl;
+    int chunks;            // of a row
+    int64_t first, step;   // rows
+    int rank, nct;
+
+    __device__ const uint4* z_of(int slot) const { return ring + slot * (kOps * kChunk); }
+    __device__ const uint4* x_of(int slot) const { return z_of(slot) + (kOps - 1) * kChunk; }
+    __device__ void fail() {
+        *static_cast<volatile int32_t*>(&sh.abort) = 1;
+        raise_flag(A.flags, ACRL_FLAG_TIMEOUT);
+    }
+    __device__ bool wait(uint64_t* bar, uint32_t parity) {
+        const bool ok = mbar_try_wait(bar, parity) || wait_phase_inline(bar, parity, &sh.abort);
+        if (__all_sync(0xffffffffu, ok)) return true;
+        fail();
+        return false;
+    }
+
+    __device__ void load() {   // one thread
+        const uint64_t once = policy_evict_first();
+        Ring r(A.slots);
+        int next = column_of(A, first);
+        for (int64_t t = first; t < A.T; t += step) {
+            const int a = next;
+            next = column_of(A, t + step);
+            if (a < 0) continue;
+            const uint4* zr = reinterpret_cast<const uint4*>(A.z + t * A.ldz) + sl.begin;
+            const uint4* xr = KIND == kSampled ? zr : reinterpret_cast<const uint4*>(A.x + t * A.ldx) + sl.begin;
+            for (int c = 0; c < chunks; ++c, r.next()) {
+                if (!mbar_try_wait(&sh.empty[r.at], r.phase ^ 1u) && !wait_phase_inline(&sh.empty[r.at], r.phase ^ 1u, &sh.abort)) {
+                    fail();
+                    const uint64_t t0 = global_ns();     // the copies that were started land before the CTA can leave
+                    while (global_ns() - t0 < 100000ull) {
+                    }
+                    return;
+                }
+                const uint32_t bytes = uint32_t(min(kChunk, sl.kept - c * kChunk)) * 16u;
+                mbar_expect_tx(&sh.full[r.at], kOps * bytes);
+                bulk_in(const_cast<uint4*>(z_of(r.at)), zr + c * kChunk, bytes, &sh.full[r.at], once);
+                if (KIND != kSampled) bulk_in(const_cast<uint4*>(x_of(r.at)), xr + c * kChunk, bytes, &sh.full[r.at], once);
+            }
+        }
+    }
+
+    __device__ void fold_rows(int warp) {
+        const int lane = threadIdx.x & 31, tid = warp * 32 + lane;
+        Ring r(A.slots), s(kStates);
+        int parity = 0, next = column_of(A, first);
+        for (int64_t t = first; t < A.T; t += step) {
+            const int a = next;
+            next = column_of(A, t + step);
+            if (a < 0) continue;
+            const acrl_bf16 *zr = A.z + t * A.ldz, *xr = KIND == kSampled ? zr : A.x + t * A.ldx;
+            // the columns beyond the whole vectors, one a lane, loaded first and folded last
+            const int j = (A.V & ~7) + tid;
+            const bool odd = sl.last && tid < (A.V & 7);
+            uint32_t zj = 0xff7fu, xj = 0xff7fu;
+            if (odd) {
+                zj = zr[j];
+                xj = KIND == kSampled ? zj : xr[j];
+            }
+            State st = empty_state();
+            for (int c = 0; c < chunks; ++c, r.next()) {
+                if (!wait(&sh.full[r.at], r.phase)) return;
+                const int n = min(kChunk, sl.kept - c * kChunk);
+                const uint4 *sz = z_of(r.at), *sx = x_of(r.at);
+                if (tid + kLanes < n) {
+                    const uint4 z[2] = {sz[tid], sz[tid + kLanes]}, x[2] = {sx[tid], sx[tid + kLanes]};
+                    fold<KIND, 2>(st, z, x);
+                } else if (tid < n) {
+                    const uint4 z[1] = {sz[tid]}, x[1] = {sx[tid]};
+                    fold<KIND, 1>(st, z, x);
+                }
+            }
+            // what is not kept, from L2 or HBM; the gradient reads it again
+            const uint4 *gz = reinterpret_cast<const uint4*>(zr) + sl.begin, *gx = reinterpret_cast<const uint4*>(xr) + sl.begin;
+            for (int v = sl.kept + tid; v < sl.end - sl.begin; v += kLanes) {
+                const uint4 z[1] = {__ldg(gz + v)};
+                if constexpr (KIND == kSampled) {
+                    fold<KIND, 1>(st, z, z);
+                } else {
+                    const uint4 x[1] = {__ldg(gx + v)};
+                    fold<KIND, 1>(st, z, x);
+                }
+            }
+            if (odd) {   // a vector whose other columns are both operands' lowest number: they add nothing
+                const uint32_t low = 0xff7fff7fu;
+                const uint4 z[1] = {make_uint4(0xff7f0000u | zj, low, low, low)}, x[1] = {make_uint4(0xff7f0000u | xj, low, low, low)};
+                fold<KIND, 1>(st, z, x);
+            }
+            __syncwarp();
+            st = meet<KIND, 32>(st);
+            if (F > 1) {
+                if (lane == 0) put(sh.parts[parity][warp], st);
+                asm volatile("bar.sync 1, %0;" ::"n"(kLanes) : "memory");
+                if (warp == 0) st = meet<KIND, F>(get(sh.parts[parity][lane & (F - 1)]));
+                parity ^= 1;
+            }
+            if (warp == 0 && nct > 1 && lane < nct)
+                push_state(sh.states[s.at][rank], &sh.state[s.at], lane, make_float4(st.mz, st.U, st.sz, st.mx),
+                           make_float4(st.W, st.sx, st.cross, 0.f));
+            if (warp == 0 && nct == 1 && lane == 0) {
+                put(sh.states[s.at][0], st);
+                mbar_arrive(&sh.state[s.at]);
+            }
+            __syncwarp();
+            s.next();
+        }
+    }
+
+    __device__ void merge_rows() {
+        const int lane = threadIdx.x & 31;
+        Ring s(kStates), g(kGrads);
+        for (int64_t t = first; t < A.T; t += step) {
+            const int a = column_of(A, t);
+            if (a < 0) {
+                if (rank == 0 && lane == 0) {
+                    A.logp[t] = A.token_loss[t] = 0.f;
+                    if (A.kl_out) A.kl_out[t] = 0.f;
+                    if (!A.mask || A.mask[t]) raise_flag(A.flags, ACRL_FLAG_BAD_ID);
+                }
+                continue;
+            }
+            const float za = bf16_to_float(A.z[t * A.ldz + a]), xa = KIND == kSampled ? 0.f : bf16_to_float(A.x[t * A.ldx + a]);
+            const float c0 = A.coef ? A.coef[t] : 0.f, kc = A.kl_coef ? A.kl_coef[t] : 0.f;
+            const float old = A.old_logp ? A.old_logp[t] : 0.f, ref = A.ref_logp ? A.ref_logp[t] : 0.f;
+            if (!wait(&sh.state[s.at], s.phase)) return;
+            if (nct > 1) try_wait_cluster(&sh.state[s.at], s.phase);   // completed: for what the other CTAs wrote
+            const int k = lane & (kMaxCluster - 1);
+            State row = k < nct ? get(sh.states[s.at][k]) : empty_state();
+            if (nct > 1) row = meet<KIND, kMaxCluster>(row);
+            else row = get(sh.states[s.at][0]);
+            RowGrad rg;
+            const int what = row_scalars<KIND>(A, t, row, a, za, xa, c0, kc, old, ref, rank == 0 && lane == 0, rg);
+            if (!wait(&sh.taken[g.at], g.phase ^ 1u)) return;
+            if (lane == 0) {
+                sh.grads[g.at] = rg;
+                sh.what[g.at] = what;
+                mbar_arrive(&sh.ready[g.at]);
+            }
+            __syncwarp();
+            s.next();
+            g.next();
+        }
+    }
+
+    __device__ void write_rows(int warp) {
+        const int lane = threadIdx.x & 31, tid = warp * 32 + lane;
+        Ring r(A.slots), g(kGrads);
+        int next = column_of(A, first);
+        for (int64_t t = first; t < A.T; t += step) {
+            const int a = next;
+            next = column_of(A, t + step);
+            acrl_bf16* gr = A.grad + t * A.ldg;
+            uint4* out = reinterpret_cast<uint4*>(gr) + sl.begin;
+            const int n = sl.end - sl.begin;
+            auto fill = [&](uint32_t pair) {
+                for (int v = tid; v < n; v += kLanes) st_stream(out + v, make_uint4(pair, pair, pair, pair));
+                if (sl.last && tid < (A.V & 7)) gr[(A.V & ~7) + tid] = acrl_bf16(pair & 0xffffu);
+            };
+            if (a < 0) {
+                fill(0u);
+                continue;
+            }
+            if (!wait(&sh.ready[g.at], g.phase)) return;
+            const RowGrad rg = sh.grads[g.at];
+            const int what = sh.what[g.at];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.taken[g.at]);
+            g.next();
+            const int rel0 = a - (sl.begin << 3);
+            if (what != kWrite) fill(what == kFillNaN ? 0x7fc07fc0u : 0u);
+            for (int c = 0; c < chunks; ++c, r.next()) {
+                if (what == kWrite) {
+                    if (!wait(&sh.full[r.at], r.phase)) return;   // long since: it makes the copy visible to this warp
+                    const uint4 *sz = z_of(r.at), *sx = x_of(r.at);
+                    const int end = min(kChunk, sl.kept - c * kChunk);
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const int v = tid + k * kLanes, at = c * kChunk + v;
+                        if (v < end) st_stream(out + at, grad_vec8<KIND>(sz[v], sx[v], rg, rel0 - (at << 3)));
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.empty[r.at]);
+            }
+            if (what != kWrite) continue;
+            const acrl_bf16 *zr = A.z + t * A.ldz, *xr = KIND == kSampled ? zr : A.x + t * A.ldx;
+            const uint4 *gz = reinterpret_cast<const uint4*>(zr) + sl.begin, *gx = reinterpret_cast<const uint4*>(xr) + sl.begin;
+            for (int v = sl.kept + tid; v < n; v += kLanes) {
+                const uint4 z = __ldg(gz + v);
+                uint4 x = z;
+                if constexpr (KIND != kSampled) x = __ldg(gx + v);
+                st_stream(out + v, grad_vec8<KIND>(z, x, rg, rel0 - (v << 3)));
+            }
+            if (sl.last && tid < (A.V & 7)) {
+                const int j = (A.V & ~7) + tid;
+                const float z = bf16_to_float(zr[j]), x = KIND == kSampled ? 0.f : bf16_to_float(xr[j]);
+                float v, none;
+                split(grad_two<KIND>(two(z, z), two(x, x), rg), v, none);
+                gr[j] = acrl_bf16(pack_bf16x2(j == a ? rg.target : v, 0.f) & 0xffffu);
+            }
+            __syncwarp();
+        }
+    }
+};
+
+template <int F>
+constexpr int kThreadsOf = (2 * F + 2) * 32;
+template <int F>
+constexpr int kPerSm = 8 / F;      // CTAs that share an SM
+
+template <Kind KIND, int F>
+__global__ void __launch_bounds__(kThreadsOf<F>, kPerSm<F>) policy_kernel(const __grid_constant__ PolicyArgs A) {
+    extern __shared__ __align__(16) uint4 ring[];
+    __shared__ __align__(16) Shared<F> sh;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int nct = int(cluster_size()), rank = int(cluster_rank());
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kMaxSlots; ++i) {
+            mbar_init(sh.full + i, 1);
+            mbar_init(sh.empty + i, F);
+        }
+        for (int i = 0; i < kStates; ++i) mbar_init(sh.state + i, uint32_t(nct));
+        for (int i = 0; i < kGrads; ++i) {
+            mbar_init(sh.ready + i, 1);
+            mbar_init(sh.taken + i, F);
+        }
+        sh.abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    grid_begin();
+    __syncthreads();
+    if (nct > 1) cluster_sync();   // every CTA's barriers are there before a state is pushed
+    const int nvec = A.V >> 3, per = (nvec + nct - 1) / nct;
+    Slice sl;
+    sl.begin = min(nvec, rank * per);
+    sl.end = min(nvec, sl.begin + per);
+    sl.kept = min(sl.end - sl.begin, A.keep);
+    sl.last = rank == nct - 1;
+    Cta<KIND, F> cta{A, sh, ring, sl, (sl.kept + Cta<KIND, F>::kChunk - 1) / Cta<KIND, F>::kChunk,
+                     int64_t(blockIdx.x) / nct, int64_t(gridDim.x) / nct, rank, nct};
+    if (warp == 0) {
+        if (lane == 0) cta.load();
+    } else if (warp == 1) {
+        cta.merge_rows();
+    } else if (warp < 2 + F) {
+        cta.fold_rows(warp - 2);
+    } else {
+        cta.write_rows(warp - 2 - F);
+    }
+    __syncwarp();
+    if (nct > 1) cluster_sync();   // no CTA leaves while another's state may still be on its way here
+}
+
+constexpr int kSmPerBytes = 227 * 1024;
+
+template <Kind KIND, int F>
+acrl_status launch_rows(PolicyArgs A, int ctas, cudaStream_t s) {
+    using C = Cta<KIND, F>;
+    constexpr int slot = C::kOps * C::kChunk * 16;
+    const int nvec = A.V >> 3, slice = (nvec + ctas - 1) / ctas;
+    const int room = kSmPerBytes / kPerSm<F> - 1024 - int(sizeof(Shared<F>));   // the system takes 1 KB of each CTA's
+    A.slots = std::min(kMaxSlots, room / slot);
+    // a slice keeps what leaves a quarter of the ring to the next row's
+    A.keep = std::min(slice, std::max(1, A.slots * 3 / 4) * C::kChunk);
+    const int chunks = std::max(1, (A.keep + C::kChunk - 1) / C::kChunk);
+    A.slots = std::min(A.slots, kMaxAhead * chunks);
+    const int smem = A.slots * slot;
+    auto* kernel = policy_kernel<KIND, F>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmPerBytes - 1024 - int(sizeof(Shared<F>))) !=
+        cudaSuccess)
+        return launch_status();
+    const int64_t most = resident_clusters(reinterpret_cast<const void*>(kernel), kThreadsOf<F>, smem, ctas);
+    if (most < 1) return ACRL_ERR_CUDA;
+    return launch(kernel, std::min(A.T, most) * ctas, kThreadsOf<F>, size_t(smem), ctas, s, A);
+}
 
 template <Kind KIND>
-acrl_status launch_policy(PolicyArgs A, int64_t T, cudaStream_t s) {
+acrl_status launch_policy(const PolicyArgs& A, cudaStream_t s) {
     constexpr int OPS = KIND == kSampled ? 1 : 2;
-    const int nvec = A.V >> 3;
+    const int bytes = (A.V >> 3) * 16 * OPS;
     int ctas = 1;
-    while (ctas < kMaxCluster && (nvec + ctas - 1) / ctas * 16 * OPS > kSliceBytes) ctas *= 2;
-    A.keep = std::min((nvec + ctas - 1) / ctas, kMaxKeepBytes / (16 * OPS));
-    constexpr int step = 2 * kThreads;
-    A.chunk = std::max(1, (A.keep + kMaxChunks * step - 1) / (kMaxChunks * step)) * step;
-    auto* kernel = policy_kernel<KIND>;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxKeepBytes) != cudaSuccess)
-        return launch_status();
-    const int64_t most = kMaxGrid / ctas;
-    for (int64_t t = 0; t < T; t += most) {      // a grid's limit
-        PolicyArgs B = A;
-        auto at = [t](auto* p, int64_t ld = 1) { return p ? p + t * ld : p; };
-        B.z = at(A.z, A.ldz);
-        B.x = at(A.x, A.ldx);
-        B.grad = at(A.grad, A.ldg);
-        B.ids = at(A.ids);
-        B.mask = at(A.mask);
-        B.coef = at(A.coef);
-        B.kl_coef = at(A.kl_coef);
-        B.old_logp = at(A.old_logp);
-        B.ref_logp = at(A.ref_logp);
-        B.logp = at(A.logp);
-        B.kl_out = at(A.kl_out);
-        B.token_loss = at(A.token_loss);
-        const acrl_status st = launch(kernel, std::min(most, T - t) * ctas, kThreads, size_t(A.keep) * 16 * OPS, ctas, s, B);
-        if (st != ACRL_OK) return st;
-    }
-    return ACRL_OK;
+    while (ctas < kMaxCluster && bytes / ctas > 80 * 1024) ctas *= 2;
+    if (bytes <= 12 * 1024) return launch_rows<KIND, 1>(A, 1, s);
+    if (bytes <= 24 * 1024) return launch_rows<KIND, 2>(A, 1, s);
+    return launch_rows<KIND, 4>(A, ctas, s);
 }
 
 }  // namespace
@@ -542,9 +749,10 @@ extern "C" acrl_status acrl_policy_loss_grad_logits(const acrl_bf16* logits, int
         A.kl_out = kl_out;
         A.token_loss = token_loss;
         A.flags = dev_flags;
-        const acrl_status st = kl == ACRL_KL_EXACT     ? launch_policy<kExact>(A, T, s)
-                               : kl == ACRL_KL_REVERSE ? launch_policy<kReverse>(A, T, s)
-                                                       : launch_policy<kSampled>(A, T, s);
+        A.T = T;
+        const acrl_status st = kl == ACRL_KL_EXACT     ? launch_policy<kExact>(A, s)
+                               : kl == ACRL_KL_REVERSE ? launch_policy<kReverse>(A, s)
+                                                       : launch_policy<kSampled>(A, s);
         if (st != ACRL_OK) return st;
     }
     return acrl_reduce_loss(token_loss, T, loss, stream);
