@@ -12,19 +12,19 @@
 // or from the reference's log-prob of the sampled token, d = logp - ref_logp:
 //     k1 d,  k2 d^2 / 2,  k3 e^-d - 1 + d, whose slope in logp joins c.
 //
-// The gradient needs the sums of the whole row, so a row is swept twice; it is read
-// from memory once.  Persistent CTAs, alone or as a cluster that shares each of its
-// rows, run four roles that work on different rows at the same time:
-//   warp 0       copies the CTA's slices of row after row into a ring of chunks in
-//                shared memory (bulk copies);
-//   warp 1       merges the states of a row's slices, works out its scalars and outputs;
-//   F warps      fold the running maxima and sums of a slice as its chunks land, and
-//                push the slice's state to every CTA of the cluster (distributed
-//                shared memory, counted on a barrier there);
-//   F warps      write the gradient of a slice from its chunks, and free them.
-// So loads, arithmetic, the exchange between CTAs and stores of neighbouring rows
-// overlap, and HBM sees every operand once: 2 bytes of z, 2 of x and 2 of the gradient an
-// element, which bounds it.
+// The gradient needs the sums of the whole row, so a row is swept twice; HBM sees it
+// once.  A CTA takes one row and keeps what fits of it in shared memory between the sweeps
+// (a bulk copy that runs while the threads load the rest); the rest of long rows comes from L2 the second
+// time.  CTAs are as small as the row allows, so that several rows share an SM and one is read while another is
+// written: HBM takes loads alone at 7.1 TB/s, stores alone at 4.0 and both together at 6.8.  Where rows are few, a
+// cluster of CTAs shares each (one state per CTA goes through distributed shared memory).  HBM bounds it: 2 bytes of z,
+// 2 of x and 2 of the gradient an element.
+//
+// Tried and slower, us for 2,632 rows of 151,936 columns with KL over the vocabulary (this: 480): persistent CTAs with a
+// ring of chunks and one role per warp 580-620 (the roles' warps are too few to hide their latencies); persistent CTAs
+// whose one pass writes a row's gradient and folds the next row 680; persistent CTAs that copy the next
+// row's part early 494, and 192 KB more of a row in tensor memory 514: CTAs that stay begin and end their rows together
+// and HBM reads and writes in turn; a cluster of two, four or eight CTAs a row 530-790.
 #include <algorithm>
 #include <cmath>
 
@@ -37,10 +37,6 @@ namespace acrl {
 namespace {
 
 constexpr int kMaxCluster = 8;
-constexpr int kMaxSlots = 32;      // chunks of a ring
-constexpr int kMaxAhead = 7;       // rows that may lie in a ring
-constexpr int kStates = 16;        // states of rows under way: a CTA's fold may be 2 kMaxAhead rows ahead of another's merge
-constexpr int kGrads = 4;          // rows between the merge and the writing warps
 
 enum Kind { kSampled, kExact, kReverse };   // which sums a row needs
 
@@ -49,8 +45,9 @@ struct PolicyArgs {
     int64_t ldz, ldx;
     int V;
     int64_t T;
-    int keep;      // vectors of each operand that a CTA keeps of a row
-    int slots;     // chunks of the ring
+    int keep;      // vectors of each operand that a CTA keeps of a row in shared memory
+    uint32_t first_wave;   // CTAs that begin one after another, and by how much
+    int phase_ns;
     const int32_t* ids;
     const uint8_t* mask;
     const float *coef, *kl_coef, *old_logp, *ref_logp;
@@ -65,7 +62,7 @@ struct PolicyArgs {
 // A row's (or part's) running state in base 2: maxima, exponents U = max log2 e, sums
 // against them, and the cross sum: exact  sum 2^(u - U) (z - x),  reverse  sum 2^(w - W) (x - z).
 struct State {
-    float mz, U, sz, mx, W, sx, cross;
+    float mz, U, sz, mx, W, sx, cross;   // mz, mx: of some columns, near the maxima
 };
 
 __device__ __forceinline__ State empty_state() { return State{-INFINITY, kLowestU, 0.f, -INFINITY, kLowestU, 0.f, 0.f}; }
@@ -126,8 +123,8 @@ __device__ __forceinline__ float raise_max(float m, float& mx, float& U) {
     return f;
 }
 
-// Fold N vectors of each operand.  A column of probability 0 adds nothing to the cross sum, whatever the other side
-// holds there (an infinite difference times 0 would be NaN).
+// Fold N vectors of each operand: the careful way, with a running maximum, and where a column of probability 0 adds
+// nothing to the cross sum, whatever the other side holds there (an infinite difference times 0 would be NaN).
 template <Kind KIND, int N>
 __device__ __forceinline__ void fold(State& st, const uint4 (&z)[N], const uint4 (&x)[N]) {
     uint32_t pm = max_pairs(z[0]);
@@ -173,6 +170,65 @@ __device__ __forceinline__ void fold(State& st, const uint4 (&z)[N], const uint4
         st.cross += sum_of(cr);
     }
 }
+
+// The quick way: sums against exponents that are fixed for the row, those of some of its columns.  Sums are as exact
+// against any exponent from which they neither overflow nor vanish; a row whose sums are not finite (a maximum that is
+// 2^127 times what the exponents stand for, an infinity, a column taken out on one side) is folded again the careful way.
+// Where the careful way is not needed both give the same cross sum's terms; the careful way costs nearly half as much again.
+template <Kind KIND>
+struct Quick {
+    float mz, mx;
+    Two nU, nW, sz, sx, cr;
+
+    // `z`, `x`: vectors of every lane of a warp.
+    __device__ __forceinline__ void start(const uint4& z, const uint4& x) {
+        mz = warp_max_of(max_pairs(z));
+        const float U = max_exponent<true>(mz);
+        nU = two(-U, -U);
+        sz = sx = cr = two(0.f, 0.f);
+        if constexpr (KIND != kSampled) {
+            mx = warp_max_of(max_pairs(x));
+            const float W = max_exponent<true>(mx);
+            nW = two(-W, -W);
+        }
+    }
+    static __device__ __forceinline__ float warp_max_of(uint32_t pair) {
+        const int a = __float_as_int(fmaxf(bf16_lo(pair), bf16_hi(pair)));
+        const int m = __reduce_max_sync(0xffffffffu, a ^ ((a >> 31) & 0x7fffffff));   // ordered as the numbers are
+        return __int_as_float(m ^ ((m >> 31) & 0x7fffffff));
+    }
+    template <int N>
+    __device__ __forceinline__ void fold(const uint4 (&z)[N], const uint4 (&x)[N]) {
+        const Two l2e = two(kLog2e, kLog2e), minus = two(-1.f, -1.f);
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const uint32_t zw[4] = {z[k].x, z[k].y, z[k].z, z[k].w}, xw[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const Two a = widen(zw[j]), e = ex2_2(fma2(a, l2e, nU));
+                sz = add2(sz, e);
+                if constexpr (KIND != kSampled) {
+                    const Two b = widen(xw[j]), h = ex2_2(fma2(b, l2e, nW));
+                    sx = add2(sx, h);
+                    cr = KIND == kExact ? fma2(e, fma2(b, minus, a), cr) : fma2(h, fma2(a, minus, b), cr);
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ State state() const {
+        State s = empty_state();
+        s.mz = mz;
+        s.U = max_exponent<true>(mz);
+        s.sz = sum_of(sz);
+        if constexpr (KIND != kSampled) {
+            s.mx = mx;
+            s.W = max_exponent<true>(mx);
+            s.sx = sum_of(sx);
+            s.cross = sum_of(cr);
+        }
+        return s;
+    }
+};
 
 // The state against common maxima: one exponential for each.
 template <Kind KIND>
@@ -224,25 +280,10 @@ __device__ __forceinline__ void bulk_in(void* dst, const void* src, uint32_t byt
         : "memory");
 }
 
-// A state to CTA `rank` of the cluster, and an arrival on its barrier.
-__device__ __forceinline__ void push_state(const float4* slot, uint64_t* bar, uint32_t rank, const float4& a, const float4& b) {
-    const uint32_t to = peer_addr(slot, rank);
-    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to), "f"(a.x), "f"(a.y), "f"(a.z), "f"(a.w)
+__device__ __forceinline__ void st_peer4(const float4* p, uint32_t rank, const float4& v) {
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(peer_addr(p, rank)), "f"(v.x), "f"(v.y), "f"(v.z),
+                 "f"(v.w)
                  : "memory");
-    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to + 16), "f"(b.x), "f"(b.y), "f"(b.z), "f"(b.w)
-                 : "memory");
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(peer_addr(bar, rank)) : "memory");
-}
-
-// A phase that other CTAs of the cluster complete: what they wrote before they arrived is visible after it.
-__device__ __forceinline__ bool try_wait_cluster(uint64_t* bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
-        : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity)
-        : "memory");
-    return ok != 0;
 }
 
 // What the gradient of a row's elements needs.
@@ -255,7 +296,8 @@ struct RowGrad {
     int a;
 };
 
-template <Kind KIND>
+// SAFE: as in fold.
+template <Kind KIND, bool SAFE>
 __device__ __forceinline__ Two grad_two(Two z, Two x, const RowGrad& g) {
     const Two l2e = two(kLog2e, kLog2e), p = ex2_2(fma2(z, l2e, two(-g.U, -g.U)));
     if constexpr (KIND == kSampled) return mul2(p, two(g.c, g.c));
@@ -263,18 +305,19 @@ __device__ __forceinline__ Two grad_two(Two z, Two x, const RowGrad& g) {
         const Two q = ex2_2(fma2(x, l2e, two(-g.W, -g.W)));
         return fma2(p, two(g.c2, g.c2), mul2(q, two(-g.k, -g.k)));
     }
-    const Two d = where_weighted(p, fma2(x, two(-1.f, -1.f), z));
+    Two d = fma2(x, two(-1.f, -1.f), z);
+    if constexpr (SAFE) d = where_weighted(p, d);
     return mul2(p, fma2(two(g.k, g.k), d, two(g.c2, g.c2)));
 }
 
-template <Kind KIND>
+template <Kind KIND, bool SAFE>
 __device__ __forceinline__ uint4 grad_vec8(const uint4& zv, const uint4& xv, const RowGrad& g, int rel) {
     const uint32_t zw[4] = {zv.x, zv.y, zv.z, zv.w}, xw[4] = {xv.x, xv.y, xv.z, xv.w};
     uint32_t o[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         float lo, hi;
-        split(grad_two<KIND>(widen(zw[j]), widen(xw[j]), g), lo, hi);
+        split(grad_two<KIND, SAFE>(widen(zw[j]), widen(xw[j]), g), lo, hi);
         o[j] = pack_bf16x2(lo, hi);
     }
     if (unsigned(rel) < 8u) {
@@ -294,7 +337,7 @@ struct Slice {
 };
 
 // What comes after a row's sums.
-enum { kWrite, kFillZero, kFillNaN };
+enum { kWrite, kWriteSafe, kFillZero, kFillNaN };
 
 // The row's scalars from its merged state, in every lane of a warp; `writes`: this thread stores the row's outputs.
 template <Kind KIND>
@@ -364,344 +407,344 @@ __device__ __forceinline__ int row_scalars(const PolicyArgs& A, int64_t t, const
     return kWrite;
 }
 
-template <int F>
-struct Shared {
-    uint64_t full[kMaxSlots];     // a chunk has landed
-    uint64_t empty[kMaxSlots];    // the F writing warps are done with it
-    uint64_t state[kStates];      // every CTA's state of a row is here
-    uint64_t ready[kGrads];       // a row's scalars are here
-    uint64_t taken[kGrads];       // the F writing warps have them
-    float4 states[kStates][kMaxCluster][2];
-    float4 parts[2][F][2];        // the folding warps' states, rows in turn
-    RowGrad grads[kGrads];
-    int what[kGrads];
-    int32_t abort;
-};
+// A row's sampled column, or -1 for a row that is left out (masked, or an id outside the vocabulary).
+__device__ __forceinline__ int column_of(const PolicyArgs& A, int64_t t) {
+    const int a = A.ids[t];
+    return (A.mask && A.mask[t] == 0) || a < 0 || a >= A.V ? -1 : a;
+}
 
-__device__ __forceinline__ void put(float4* to, const State& s) {
+__device__ __forceinline__ void put(float4* to, const State& s, bool careful) {
     to[0] = make_float4(s.mz, s.U, s.sz, s.mx);
-    to[1] = make_float4(s.W, s.sx, s.cross, 0.f);
+    to[1] = make_float4(s.W, s.sx, s.cross, careful ? 1.f : 0.f);
 }
 __device__ __forceinline__ State get(const float4* from) {
     const float4 a = from[0], b = from[1];
     return State{a.x, a.y, a.z, a.w, b.x, b.y, b.z};
 }
 
-// Position in a ring.
-struct Ring {
-    int n, at = 0;
-    uint32_t phase = 0;
-    __device__ explicit Ring(int size) : n(size) {}
-    __device__ void next() {
-        if (++at == n) {
-            at = 0;
-            phase ^= 1u;
-        }
-    }
+template <int THREADS>
+struct Shared {
+    uint64_t landed;
+    float4 warps[THREADS / 32][2];
+    float4 parts[kMaxCluster][2];      // the CTAs' states
+    RowGrad grad;
+    int what;
 };
 
-// A row's sampled column, or -1 for a row that is left out (masked, or an id outside the vocabulary).
-__device__ __forceinline__ int column_of(const PolicyArgs& A, int64_t t) {
-    if (t >= A.T) return -1;
-    const int a = A.ids[t];
-    return (A.mask && A.mask[t] == 0) || a < 0 || a >= A.V ? -1 : a;
-}
-
-template <Kind KIND, int F>
+template <Kind KIND, int THREADS>
 struct Cta {
-    static constexpr int kLanes = 32 * F;          // of a role of F warps
-    static constexpr int kChunk = 2 * kLanes;      // vectors of a chunk
     static constexpr int kOps = KIND == kSampled ? 1 : 2;
+    static constexpr int kWide = 4 / kOps;             // vectors of each operand that a thread has in flight
+    static constexpr int kStep = kWide * THREADS;      // vectors of a step of the CTA
     const PolicyArgs& A;
-    Shared<F>& sh;
-    uint4* ring;
-    Slice sl;
-    int chunks;            // of a row
-    int64_t first, step;   // rows
-    int rank, nct;
+    Shared<THREADS>& sh;
+    const uint4 *sz, *sx;      // the part in shared memory
+    int begin, n, kept;        // this CTA's vectors of a row: the first, how many, of them in shared memory
+    bool last;                 // the columns beyond the whole vectors are this CTA's
 
-    __device__ const uint4* z_of(int slot) const { return ring + slot * (kOps * kChunk); }
-    __device__ const uint4* x_of(int slot) const { return z_of(slot) + (kOps - 1) * kChunk; }
-    __device__ void fail() {
-        *static_cast<volatile int32_t*>(&sh.abort) = 1;
-        raise_flag(A.flags, ACRL_FLAG_TIMEOUT);
-    }
-    __device__ bool wait(uint64_t* bar, uint32_t parity) {
-        const bool ok = mbar_try_wait(bar, parity) || wait_phase_inline(bar, parity, &sh.abort);
-        if (__all_sync(0xffffffffu, ok)) return true;
-        fail();
-        return false;
-    }
-
-    __device__ void load() {   // one thread
+    // one thread: the copies of the part in shared memory
+    __device__ void load(int64_t t) const {
+        if (kept == 0) return;
         const uint64_t once = policy_evict_first();
-        Ring r(A.slots);
-        int next = column_of(A, first);
-        for (int64_t t = first; t < A.T; t += step) {
-            const int a = next;
-            next = column_of(A, t + step);
-            if (a < 0) continue;
-            const uint4* zr = reinterpret_cast<const uint4*>(A.z + t * A.ldz) + sl.begin;
-            const uint4* xr = KIND == kSampled ? zr : reinterpret_cast<const uint4*>(A.x + t * A.ldx) + sl.begin;
-            for (int c = 0; c < chunks; ++c, r.next()) {
-                if (!mbar_try_wait(&sh.empty[r.at], r.phase ^ 1u) && !wait_phase_inline(&sh.empty[r.at], r.phase ^ 1u, &sh.abort)) {
-                    fail();
-                    const uint64_t t0 = global_ns();     // the copies that were started land before the CTA can leave
-                    while (global_ns() - t0 < 100000ull) {
-                    }
-                    return;
-                }
-                const uint32_t bytes = uint32_t(min(kChunk, sl.kept - c * kChunk)) * 16u;
-                mbar_expect_tx(&sh.full[r.at], kOps * bytes);
-                bulk_in(const_cast<uint4*>(z_of(r.at)), zr + c * kChunk, bytes, &sh.full[r.at], once);
-                if (KIND != kSampled) bulk_in(const_cast<uint4*>(x_of(r.at)), xr + c * kChunk, bytes, &sh.full[r.at], once);
-            }
-        }
+        const uint32_t bytes = uint32_t(kept) * 16u;
+        mbar_expect_tx(&sh.landed, kOps * bytes);
+        bulk_in(const_cast<uint4*>(sz), reinterpret_cast<const uint4*>(A.z + t * A.ldz) + begin, bytes, &sh.landed, once);
+        if (KIND != kSampled)
+            bulk_in(const_cast<uint4*>(sx), reinterpret_cast<const uint4*>(A.x + t * A.ldx) + begin, bytes, &sh.landed, once);
     }
 
-    __device__ void fold_rows(int warp) {
-        const int lane = threadIdx.x & 31, tid = warp * 32 + lane;
-        Ring r(A.slots), s(kStates);
-        int parity = 0, next = column_of(A, first);
-        for (int64_t t = first; t < A.T; t += step) {
-            const int a = next;
-            next = column_of(A, t + step);
-            if (a < 0) continue;
-            const acrl_bf16 *zr = A.z + t * A.ldz, *xr = KIND == kSampled ? zr : A.x + t * A.ldx;
-            // the columns beyond the whole vectors, one a lane, loaded first and folded last
-            const int j = (A.V & ~7) + tid;
-            const bool odd = sl.last && tid < (A.V & 7);
-            uint32_t zj = 0xff7fu, xj = 0xff7fu;
-            if (odd) {
-                zj = zr[j];
-                xj = KIND == kSampled ? zj : xr[j];
-            }
-            State st = empty_state();
-            for (int c = 0; c < chunks; ++c, r.next()) {
-                if (!wait(&sh.full[r.at], r.phase)) return;
-                const int n = min(kChunk, sl.kept - c * kChunk);
-                const uint4 *sz = z_of(r.at), *sx = x_of(r.at);
-                if (tid + kLanes < n) {
-                    const uint4 z[2] = {sz[tid], sz[tid + kLanes]}, x[2] = {sx[tid], sx[tid + kLanes]};
-                    fold<KIND, 2>(st, z, x);
-                } else if (tid < n) {
-                    const uint4 z[1] = {sz[tid]}, x[1] = {sx[tid]};
-                    fold<KIND, 1>(st, z, x);
-                }
-            }
-            // what is not kept, from L2 or HBM; the gradient reads it again
-            const uint4 *gz = reinterpret_cast<const uint4*>(zr) + sl.begin, *gx = reinterpret_cast<const uint4*>(xr) + sl.begin;
-            for (int v = sl.kept + tid; v < sl.end - sl.begin; v += kLanes) {
-                const uint4 z[1] = {__ldg(gz + v)};
-                if constexpr (KIND == kSampled) {
-                    fold<KIND, 1>(st, z, z);
-                } else {
-                    const uint4 x[1] = {__ldg(gx + v)};
-                    fold<KIND, 1>(st, z, x);
-                }
-            }
-            if (odd) {   // a vector whose other columns are both operands' lowest number: they add nothing
-                const uint32_t low = 0xff7fff7fu;
-                const uint4 z[1] = {make_uint4(0xff7f0000u | zj, low, low, low)}, x[1] = {make_uint4(0xff7f0000u | xj, low, low, low)};
-                fold<KIND, 1>(st, z, x);
-            }
-            __syncwarp();
-            st = meet<KIND, 32>(st);
-            if (F > 1) {
-                if (lane == 0) put(sh.parts[parity][warp], st);
-                asm volatile("bar.sync 1, %0;" ::"n"(kLanes) : "memory");
-                if (warp == 0) st = meet<KIND, F>(get(sh.parts[parity][lane & (F - 1)]));
-                parity ^= 1;
-            }
-            if (warp == 0 && nct > 1 && lane < nct)
-                push_state(sh.states[s.at][rank], &sh.state[s.at], lane, make_float4(st.mz, st.U, st.sz, st.mx),
-                           make_float4(st.W, st.sx, st.cross, 0.f));
-            if (warp == 0 && nct == 1 && lane == 0) {
-                put(sh.states[s.at][0], st);
-                mbar_arrive(&sh.state[s.at]);
-            }
-            __syncwarp();
-            s.next();
-        }
-    }
-
-    __device__ void merge_rows() {
-        const int lane = threadIdx.x & 31;
-        Ring s(kStates), g(kGrads);
-        for (int64_t t = first; t < A.T; t += step) {
-            const int a = column_of(A, t);
-            if (a < 0) {
-                if (rank == 0 && lane == 0) {
-                    A.logp[t] = A.token_loss[t] = 0.f;
-                    if (A.kl_out) A.kl_out[t] = 0.f;
-                    if (!A.mask || A.mask[t]) raise_flag(A.flags, ACRL_FLAG_BAD_ID);
-                }
-                continue;
-            }
-            const float za = bf16_to_float(A.z[t * A.ldz + a]), xa = KIND == kSampled ? 0.f : bf16_to_float(A.x[t * A.ldx + a]);
-            const float c0 = A.coef ? A.coef[t] : 0.f, kc = A.kl_coef ? A.kl_coef[t] : 0.f;
-            const float old = A.old_logp ? A.old_logp[t] : 0.f, ref = A.ref_logp ? A.ref_logp[t] : 0.f;
-            if (!wait(&sh.state[s.at], s.phase)) return;
-            if (nct > 1) try_wait_cluster(&sh.state[s.at], s.phase);   // completed: for what the other CTAs wrote
-            const int k = lane & (kMaxCluster - 1);
-            State row = k < nct ? get(sh.states[s.at][k]) : empty_state();
-            if (nct > 1) row = meet<KIND, kMaxCluster>(row);
-            else row = get(sh.states[s.at][0]);
-            RowGrad rg;
-            const int what = row_scalars<KIND>(A, t, row, a, za, xa, c0, kc, old, ref, rank == 0 && lane == 0, rg);
-            if (!wait(&sh.taken[g.at], g.phase ^ 1u)) return;
-            if (lane == 0) {
-                sh.grads[g.at] = rg;
-                sh.what[g.at] = what;
-                mbar_arrive(&sh.ready[g.at]);
-            }
-            __syncwarp();
-            s.next();
-            g.next();
-        }
-    }
-
-    __device__ void write_rows(int warp) {
-        const int lane = threadIdx.x & 31, tid = warp * 32 + lane;
-        Ring r(A.slots), g(kGrads);
-        int next = column_of(A, first);
-        for (int64_t t = first; t < A.T; t += step) {
-            const int a = next;
-            next = column_of(A, t + step);
-            acrl_bf16* gr = A.grad + t * A.ldg;
-            uint4* out = reinterpret_cast<uint4*>(gr) + sl.begin;
-            const int n = sl.end - sl.begin;
-            auto fill = [&](uint32_t pair) {
-                for (int v = tid; v < n; v += kLanes) st_stream(out + v, make_uint4(pair, pair, pair, pair));
-                if (sl.last && tid < (A.V & 7)) gr[(A.V & ~7) + tid] = acrl_bf16(pair & 0xffffu);
-            };
-            if (a < 0) {
-                fill(0u);
-                continue;
-            }
-            if (!wait(&sh.ready[g.at], g.phase)) return;
-            const RowGrad rg = sh.grads[g.at];
-            const int what = sh.what[g.at];
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sh.taken[g.at]);
-            g.next();
-            const int rel0 = a - (sl.begin << 3);
-            if (what != kWrite) fill(what == kFillNaN ? 0x7fc07fc0u : 0u);
-            for (int c = 0; c < chunks; ++c, r.next()) {
-                if (what == kWrite) {
-                    if (!wait(&sh.full[r.at], r.phase)) return;   // long since: it makes the copy visible to this warp
-                    const uint4 *sz = z_of(r.at), *sx = x_of(r.at);
-                    const int end = min(kChunk, sl.kept - c * kChunk);
+    // f(z, x) on the vectors that are not in shared memory: from global memory, kWide of each operand at a time, with an
+    // L2 policy.
+    template <typename Fn>
+    __device__ __forceinline__ void rest(const uint4* gz, const uint4* gx, uint64_t pol, Fn f) const {
+        int v = kept + threadIdx.x;
+        for (; v + (kWide - 1) * THREADS < n; v += kStep) {
+            uint4 z[kWide], x[kWide];
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const int v = tid + k * kLanes, at = c * kChunk + v;
-                        if (v < end) st_stream(out + at, grad_vec8<KIND>(sz[v], sx[v], rg, rel0 - (at << 3)));
-                    }
-                }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sh.empty[r.at]);
+            for (int k = 0; k < kWide; ++k) {
+                z[k] = ld_policy(gz + v + k * THREADS, pol);
+                if constexpr (KIND != kSampled) x[k] = ld_policy(gx + v + k * THREADS, pol);
+                else x[k] = z[k];
             }
-            if (what != kWrite) continue;
-            const acrl_bf16 *zr = A.z + t * A.ldz, *xr = KIND == kSampled ? zr : A.x + t * A.ldx;
-            const uint4 *gz = reinterpret_cast<const uint4*>(zr) + sl.begin, *gx = reinterpret_cast<const uint4*>(xr) + sl.begin;
-            for (int v = sl.kept + tid; v < n; v += kLanes) {
-                const uint4 z = __ldg(gz + v);
-                uint4 x = z;
-                if constexpr (KIND != kSampled) x = __ldg(gx + v);
-                st_stream(out + v, grad_vec8<KIND>(z, x, rg, rel0 - (v << 3)));
-            }
-            if (sl.last && tid < (A.V & 7)) {
-                const int j = (A.V & ~7) + tid;
-                const float z = bf16_to_float(zr[j]), x = KIND == kSampled ? 0.f : bf16_to_float(xr[j]);
-                float v, none;
-                split(grad_two<KIND>(two(z, z), two(x, x), rg), v, none);
-                gr[j] = acrl_bf16(pack_bf16x2(j == a ? rg.target : v, 0.f) & 0xffffu);
-            }
-            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < kWide; ++k) f(z[k], x[k], v + k * THREADS);
         }
+        for (; v < n; v += THREADS) {
+            const uint4 z = ld_policy(gz + v, pol);
+            uint4 x = z;
+            if constexpr (KIND != kSampled) x = ld_policy(gx + v, pol);
+            f(z, x, v);
+        }
+    }
+    __device__ __forceinline__ State fold_row(int64_t t, bool& careful) {
+        const int tid = threadIdx.x;
+        const acrl_bf16 *zr = A.z + t * A.ldz, *xr = KIND == kSampled ? zr : A.x + t * A.ldx;
+        const uint4 *gz = reinterpret_cast<const uint4*>(zr) + begin, *gx = reinterpret_cast<const uint4*>(xr) + begin;
+        // the columns beyond the whole vectors, one a thread: a vector whose other columns are both operands' lowest
+        // number, which add nothing
+        const bool odd = last && tid < (A.V & 7);
+        const uint32_t low = 0xff7fff7fu;
+        uint4 oz = make_uint4(low, low, low, low), ox = oz;
+        if (odd) {
+            oz.x = 0xff7f0000u | zr[(A.V & ~7) + tid];
+            ox.x = KIND == kSampled ? oz.x : 0xff7f0000u | xr[(A.V & ~7) + tid];
+        }
+        const uint64_t again = policy_evict_last();
+        Quick<KIND> q;
+        bool started = false;
+        auto first_of = [&](const uint4& z, const uint4& x) {
+            if (!started) q.start(z, x);
+            started = true;
+        };
+        // exponents from the first columns that the warp comes to: those of the rest, or of the part in shared memory
+        if (kept + (tid & ~31) < n) {
+            const int at = min(kept + tid, n - 1);
+            const uint4 z = __ldg(gz + at);
+            first_of(z, KIND == kSampled ? z : __ldg(gx + at));
+            rest(gz, gx, again, [&](const uint4& z, const uint4& x, int) {
+                const uint4 a[1] = {z}, b[1] = {x};
+                q.fold(a, b);
+            });
+        }
+        __syncwarp();
+        if (kept > 0) {
+            if (!mbar_try_wait(&sh.landed, 0) && !wait_phase_inline(&sh.landed, 0, nullptr)) raise_flag(A.flags, ACRL_FLAG_TIMEOUT);
+            __syncwarp();
+            if (!started) first_of(sz[min(tid, kept - 1)], sx[min(tid, kept - 1)]);
+            int v = tid;
+            for (; v + THREADS < kept; v += 2 * THREADS) {
+                const uint4 z[2] = {sz[v], sz[v + THREADS]}, x[2] = {sx[v], sx[v + THREADS]};
+                q.fold(z, x);
+            }
+            if (v < kept) {
+                const uint4 z[1] = {sz[v]}, x[1] = {sx[v]};
+                q.fold(z, x);
+            }
+        }
+        __syncwarp();
+        first_of(oz, ox);       // a row of fewer than eight columns
+        if (odd) {
+            const uint4 a[1] = {oz}, b[1] = {ox};
+            q.fold(a, b);
+        }
+        __syncwarp();
+        State st = q.state();
+        // no sum is finite in which one of these is not
+        careful = __any_sync(0xffffffffu, !isfinite(KIND == kSampled ? st.sz : st.cross + (st.sz + st.sx)));
+        if (careful) {          // once more, from where the vectors are now
+            st = empty_state();
+            auto f = [&](const uint4& z, const uint4& x, int) {
+                const uint4 a[1] = {z}, b[1] = {x};
+                fold<KIND, 1>(st, a, b);
+            };
+            for (int v = tid; v < kept; v += THREADS) f(sz[v], sx[v], v);
+            rest(gz, gx, again, f);
+            if (odd) f(oz, ox, 0);
+        }
+        __syncwarp();
+        return meet<KIND, 32>(st);
+    }
+
+    template <bool SAFE>
+    __device__ __forceinline__ void write_part(uint4* out, const RowGrad& g, int rel0) const {
+        int v = threadIdx.x;
+        for (; v + THREADS < kept; v += 2 * THREADS) {
+            const uint4 z[2] = {sz[v], sz[v + THREADS]}, x[2] = {sx[v], sx[v + THREADS]};
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                st_stream(out + v + k * THREADS, grad_vec8<KIND, SAFE>(z[k], x[k], g, rel0 - ((v + k * THREADS) << 3)));
+        }
+        if (v < kept) st_stream(out + v, grad_vec8<KIND, SAFE>(sz[v], sx[v], g, rel0 - (v << 3)));
+    }
+    template <bool SAFE>
+    __device__ __forceinline__ void write_rest(int64_t t, uint4* out, acrl_bf16* gr, const RowGrad& g, int rel0) const {
+        const acrl_bf16 *zr = A.z + t * A.ldz, *xr = KIND == kSampled ? zr : A.x + t * A.ldx;
+        const uint4 *gz = reinterpret_cast<const uint4*>(zr) + begin, *gx = reinterpret_cast<const uint4*>(xr) + begin;
+        auto f = [&](const uint4& z, const uint4& x, int v) {
+            st_stream(out + v, grad_vec8<KIND, SAFE>(z, x, g, rel0 - (v << 3)));
+        };
+        rest(gz, gx, policy_evict_first(), f);
+        if (last && threadIdx.x < (A.V & 7)) {
+            const int j = (A.V & ~7) + int(threadIdx.x);
+            const float z = bf16_to_float(zr[j]), x = KIND == kSampled ? 0.f : bf16_to_float(xr[j]);
+            float v, none;
+            split(grad_two<KIND, SAFE>(two(z, z), two(x, x), g), v, none);
+            gr[j] = acrl_bf16(pack_bf16x2(j == g.a ? g.target : v, 0.f) & 0xffffu);
+        }
+    }
+    __device__ __forceinline__ void fill(int64_t t, uint32_t pair) const {
+        acrl_bf16* gr = A.grad + t * A.ldg;
+        uint4* out = reinterpret_cast<uint4*>(gr) + begin;
+        for (int v = threadIdx.x; v < n; v += THREADS) st_stream(out + v, make_uint4(pair, pair, pair, pair));
+        if (last && threadIdx.x < (A.V & 7)) gr[(A.V & ~7) + threadIdx.x] = acrl_bf16(pair & 0xffffu);
     }
 };
 
-template <int F>
-constexpr int kThreadsOf = (2 * F + 2) * 32;
-template <int F>
-constexpr int kPerSm = 8 / F;      // CTAs that share an SM
-
-template <Kind KIND, int F>
-__global__ void __launch_bounds__(kThreadsOf<F>, kPerSm<F>) policy_kernel(const __grid_constant__ PolicyArgs A) {
-    extern __shared__ __align__(16) uint4 ring[];
-    __shared__ __align__(16) Shared<F> sh;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+// Small CTAs work a row's scalars out in every warp, with one barrier; from 256 threads the first warp does, for a second
+// barrier.
+template <Kind KIND, int THREADS, int PER_SM>
+__global__ void __launch_bounds__(THREADS, PER_SM) policy_kernel(const __grid_constant__ PolicyArgs A) {
+    constexpr int kWarps = THREADS / 32;
+    constexpr bool kEvery = THREADS < 256;
+    extern __shared__ __align__(16) uint4 kept_rows[];
+    __shared__ __align__(16) Shared<THREADS> sh;
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     const int nct = int(cluster_size()), rank = int(cluster_rank());
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < kMaxSlots; ++i) {
-            mbar_init(sh.full + i, 1);
-            mbar_init(sh.empty + i, F);
-        }
-        for (int i = 0; i < kStates; ++i) mbar_init(sh.state + i, uint32_t(nct));
-        for (int i = 0; i < kGrads; ++i) {
-            mbar_init(sh.ready + i, 1);
-            mbar_init(sh.taken + i, F);
-        }
-        sh.abort = 0;
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    grid_begin();
-    __syncthreads();
-    if (nct > 1) cluster_sync();   // every CTA's barriers are there before a state is pushed
+    const int64_t t = int64_t(blockIdx.x) / nct;
+    using C = Cta<KIND, THREADS>;
     const int nvec = A.V >> 3, per = (nvec + nct - 1) / nct;
-    Slice sl;
-    sl.begin = min(nvec, rank * per);
-    sl.end = min(nvec, sl.begin + per);
-    sl.kept = min(sl.end - sl.begin, A.keep);
-    sl.last = rank == nct - 1;
-    Cta<KIND, F> cta{A, sh, ring, sl, (sl.kept + Cta<KIND, F>::kChunk - 1) / Cta<KIND, F>::kChunk,
-                     int64_t(blockIdx.x) / nct, int64_t(gridDim.x) / nct, rank, nct};
-    if (warp == 0) {
-        if (lane == 0) cta.load();
-    } else if (warp == 1) {
-        cta.merge_rows();
-    } else if (warp < 2 + F) {
-        cta.fold_rows(warp - 2);
-    } else {
-        cta.write_rows(warp - 2 - F);
+    const int begin = min(nvec, rank * per), n = min(per, nvec - begin), kept = min(n, A.keep);
+    C cta{A, sh, kept_rows, kept_rows + (C::kOps - 1) * A.keep, begin, n, kept, rank == nct - 1};
+    grid_begin();
+    if (blockIdx.x < A.first_wave) {          // see stagger()
+        const uint64_t t0 = global_ns(), wait = uint64_t(A.phase_ns) * (PER_SM == 1 ? blockIdx.x & 3u : blockIdx.x / (A.first_wave / PER_SM));
+        while (global_ns() - t0 < wait) __nanosleep(200);
     }
-    __syncwarp();
-    if (nct > 1) cluster_sync();   // no CTA leaves while another's state may still be on its way here
+    const int a = column_of(A, t);
+    if (a < 0) {     // left out: zeros (the same for the whole cluster)
+        cta.fill(t, 0u);
+        if (rank == 0 && tid == 0) {
+            A.logp[t] = A.token_loss[t] = 0.f;
+            if (A.kl_out) A.kl_out[t] = 0.f;
+            if (!A.mask || A.mask[t]) raise_flag(A.flags, ACRL_FLAG_BAD_ID);
+        }
+        return;
+    }
+    if (tid == 0) {
+        mbar_init(&sh.landed, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        cta.load(t);
+    }
+    // what there is one of per row, one number a lane: the sampled column of z and x, and the token's numbers
+    float mine = 0.f;
+    if ((kEvery || wid == 0) && lane < 6) {
+        if (lane >= 2) {
+            const float* p = lane == 2 ? A.coef : lane == 3 ? A.kl_coef : lane == 4 ? A.old_logp : A.ref_logp;
+            if (p) mine = p[t];
+        } else if (lane == 0 || KIND != kSampled) {
+            mine = bf16_to_float(lane == 0 ? A.z[t * A.ldz + a] : A.x[t * A.ldx + a]);
+        }
+    }
+    __syncthreads();                         // the barrier is initialised
+    if (nct > 1) cluster_sync();             // every CTA runs before its shared memory is written
+    bool careful;
+    State st = cta.fold_row(t, careful);
+    RowGrad g;
+    int what = kWrite;
+    auto scalars = [&] {
+        auto one = [&](int k) { return __shfl_sync(0xffffffffu, mine, k); };
+        what = row_scalars<KIND>(A, t, st, a, one(0), one(1), one(2), one(3), one(4), one(5), rank == 0 && tid == 0, g);
+        if (what == kWrite && careful) what = kWriteSafe;
+    };
+    const State none = empty_state();
+    if (kWarps > 1) {
+        if (lane == 0) put(sh.warps[wid], st, careful);
+        __syncthreads();
+        if (kEvery || wid == 0) {
+            careful = __any_sync(0xffffffffu, lane < kWarps && sh.warps[lane][1].w != 0.f);
+            st = meet<KIND, 32>(lane < kWarps ? get(sh.warps[lane]) : none);
+        }
+    }
+    if (nct > 1) {
+        if (wid == 0 && lane < nct) {        // lane r hands this CTA's state to CTA r
+            st_peer4(&sh.parts[rank][0], lane, make_float4(st.mz, st.U, st.sz, st.mx));
+            st_peer4(&sh.parts[rank][1], lane, make_float4(st.W, st.sx, st.cross, careful ? 1.f : 0.f));
+        }
+        cluster_sync();
+        const int k = lane & (kMaxCluster - 1);
+        careful = __any_sync(0xffffffffu, k < nct && sh.parts[k][1].w != 0.f);
+        st = meet<KIND, kMaxCluster>(k < nct ? get(sh.parts[k]) : none);
+    }
+    if constexpr (kEvery) {
+        scalars();
+    } else {
+        if (wid == 0) {
+            scalars();
+            if (lane == 0) {
+                sh.grad = g;
+                sh.what = what;
+            }
+        }
+        __syncthreads();
+        g = sh.grad;
+        what = sh.what;
+    }
+    acrl_bf16* gr = A.grad + t * A.ldg;
+    uint4* out = reinterpret_cast<uint4*>(gr) + begin;
+    const int rel0 = a - (begin << 3);
+    if (what == kWrite) {
+        cta.template write_rest<false>(t, out, gr, g, rel0);
+        cta.template write_part<false>(out, g, rel0);
+    } else if (what == kWriteSafe) {
+        cta.template write_rest<true>(t, out, gr, g, rel0);
+        cta.template write_part<true>(out, g, rel0);
+    } else {
+        cta.fill(t, what == kFillNaN ? 0x7fc07fc0u : 0u);
+    }
 }
 
-constexpr int kSmPerBytes = 227 * 1024;
+constexpr int kSmBytes = 227 * 1024;
 
-template <Kind KIND, int F>
+// CTAs of long rows all begin together, and as their rows take equally long, HBM then reads and writes in turn.  So the first
+// wave begins in phases: with one CTA an SM, quarters of a row's time apart; with more, the CTAs of an SM spread over it.
+// 2,632 x 151,936 over the vocabulary 512 / 479 us, sampled 357 / 314; 6,102 x 65,544 316 / 296.  A call of fewer than
+// kPhasedWaves waves would lose more than it gains.
+constexpr int kPhasedWaves = 6;
+constexpr int kSms = 152;
+constexpr double kSmBytesPerNs = 44.6;    // an SM's share of HBM's rate
+
+void stagger(PolicyArgs& A, int64_t bytes_moved, int per_sm) {
+    if (A.T < int64_t(kPhasedWaves) * kSms * per_sm) return;
+    A.first_wave = uint32_t(kSms * per_sm);
+    A.phase_ns = int(double(bytes_moved) / kSmBytesPerNs * per_sm / (per_sm == 1 ? 4 : per_sm));
+}
+
+template <Kind KIND, int THREADS, int PER_SM>
 acrl_status launch_rows(PolicyArgs A, int ctas, cudaStream_t s) {
-    using C = Cta<KIND, F>;
-    constexpr int slot = C::kOps * C::kChunk * 16;
+    constexpr int kVec = KIND == kSampled ? 16 : 32;       // bytes of a vector of all operands
     const int nvec = A.V >> 3, slice = (nvec + ctas - 1) / ctas;
-    const int room = kSmPerBytes / kPerSm<F> - 1024 - int(sizeof(Shared<F>));   // the system takes 1 KB of each CTA's
-    A.slots = std::min(kMaxSlots, room / slot);
-    // a slice keeps what leaves a quarter of the ring to the next row's
-    A.keep = std::min(slice, std::max(1, A.slots * 3 / 4) * C::kChunk);
-    const int chunks = std::max(1, (A.keep + C::kChunk - 1) / C::kChunk);
-    A.slots = std::min(A.slots, kMaxAhead * chunks);
-    const int smem = A.slots * slot;
-    auto* kernel = policy_kernel<KIND, F>;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmPerBytes - 1024 - int(sizeof(Shared<F>))) !=
-        cudaSuccess)
-        return launch_status();
-    const int64_t most = resident_clusters(reinterpret_cast<const void*>(kernel), kThreadsOf<F>, smem, ctas);
-    if (most < 1) return ACRL_ERR_CUDA;
-    return launch(kernel, std::min(A.T, most) * ctas, kThreadsOf<F>, size_t(smem), ctas, s, A);
+    constexpr int room = kSmBytes / PER_SM - 1024 - int(sizeof(Shared<THREADS>));   // the system takes 1 KB of each CTA's
+    // whole steps of the CTA, where not all of it
+    A.keep = slice <= room / kVec ? slice : room / kVec / (2 * THREADS) * (2 * THREADS);
+    if (A.keep < slice && ctas == 1) stagger(A, int64_t(nvec) * (KIND == kSampled ? 32 : 48), PER_SM);
+    auto* kernel = policy_kernel<KIND, THREADS, PER_SM>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, room) != cudaSuccess) return launch_status();
+    const int64_t T = A.T, most = kMaxGrid / ctas;
+    for (int64_t t = 0; t < T; t += most) {      // a grid's limit
+        PolicyArgs B = A;
+        auto at = [t](auto* p, int64_t ld = 1) { return p ? p + t * ld : p; };
+        B.T = std::min(most, T - t);
+        if (t > 0) B.first_wave = 0;
+        B.z = at(A.z, A.ldz);
+        B.x = at(A.x, A.ldx);
+        B.grad = at(A.grad, A.ldg);
+        B.ids = at(A.ids);
+        B.mask = at(A.mask);
+        B.coef = at(A.coef);
+        B.kl_coef = at(A.kl_coef);
+        B.old_logp = at(A.old_logp);
+        B.ref_logp = at(A.ref_logp);
+        B.logp = at(A.logp);
+        B.kl_out = at(A.kl_out);
+        B.token_loss = at(A.token_loss);
+        const acrl_status st = launch(kernel, B.T * ctas, THREADS, size_t(A.keep) * kVec, ctas, s, B);
+        if (st != ACRL_OK) return st;
+    }
+    return ACRL_OK;
 }
 
 template <Kind KIND>
 acrl_status launch_policy(const PolicyArgs& A, cudaStream_t s) {
-    constexpr int OPS = KIND == kSampled ? 1 : 2;
-    const int bytes = (A.V >> 3) * 16 * OPS;
-    int ctas = 1;
-    while (ctas < kMaxCluster && bytes / ctas > 80 * 1024) ctas *= 2;
-    if (bytes <= 12 * 1024) return launch_rows<KIND, 1>(A, 1, s);
-    if (bytes <= 24 * 1024) return launch_rows<KIND, 2>(A, 1, s);
-    return launch_rows<KIND, 4>(A, ctas, s);
+    const int64_t bytes = int64_t(A.V >> 3) * (KIND == kSampled ? 16 : 32);    // of a row
+    int ctas = 1;      // few rows: several CTAs each
+    while (ctas < kMaxCluster && 2 * ctas * A.T <= 152 && bytes / ctas > 16 * 1024) ctas *= 2;
+    const int64_t slice = bytes / ctas;
+    if (slice <= 9 * 1024) return launch_rows<KIND, 32, 24>(A, ctas, s);
+    if (slice <= 16 * 1024) return launch_rows<KIND, 64, 13>(A, ctas, s);
+    if (slice <= 40 * 1024) return launch_rows<KIND, 128, 5>(A, ctas, s);
+    if (slice <= 72 * 1024) return launch_rows<KIND, 256, 3>(A, ctas, s);
+    if (KIND == kSampled || slice <= 300 * 1024) return launch_rows<KIND, 512, 2>(A, ctas, s);
+    return launch_rows<KIND, 1024, 1>(A, ctas, s);
 }
 
 }  // namespace
