@@ -575,13 +575,14 @@ def fp8_linear(x, weight: Fp8Tensor, *, fmt="e4m3", out_dtype=torch.bfloat16, ou
     if out_dtype not in _OUT_DTYPE:
         raise AcrlError(f"out_dtype: {out_dtype}, expected bfloat16 or float32")
     out, ldo = _product_out(out, M, N, out_dtype, x.device)
-    n = fp8_linear_workspace_bytes(M, K)
-    workspace = torch.empty(n, dtype=torch.uint8, device=x.device) if workspace is None else \
+    n = lib().acrl_fp8_linear_workspace_bytes(M, K)
+    if workspace is not None:
         _need(workspace, torch.uint8, n, "workspace")
+    elif n > 0:
+        workspace = torch.empty(n, dtype=torch.uint8, device=x.device)
     _opt(flags, torch.int32, 1, "flags")
-    _call("acrl_fp8_linear", (x, weight.q, weight.scale, out, workspace, flags), stream, _ptr(x), M, K, _ld(x),
-          _fp8_format(fmt), w[0], N, *w[2:], _ptr(out), _OUT_DTYPE[out.dtype], ldo, _ptr(workspace), workspace.numel(),
-          _ptr(flags))
+    _call("acrl_fp8_linear", (x, weight.q, weight.scale, out, workspace, flags), stream, x.data_ptr(), M, K, _ld(x),
+          _fp8_format(fmt), w[0], N, *w[2:], out.data_ptr(), _OUT_DTYPE[out.dtype], ldo, _ptr(workspace), n, _ptr(flags))
     return out
 
 

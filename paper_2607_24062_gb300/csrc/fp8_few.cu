@@ -1,0 +1,251 @@
+// Products of a few rows (a token or four) with an 8-bit matrix: every byte of the matrix is used a few times only,
+// so HBM bounds them, and at the sizes of one layer the latency of a launch.  No tensor cores: their pipeline's start and end
+// (tensor memory, barriers, the split of the sum) takes longer than these products (1 x 4,096 x 4,096: 15 us against
+// 5).  A warp takes kW rows of the matrix at a time: each lane loads 16 bytes of each, 512 columns a step, converts them
+// to fp32 through half precision (exact for both formats) and multiplies them with the few rows, which lie in
+// shared memory as fp32 values of their own scales; the 16 products' sum takes the block's scale.  Then the lanes' sums
+// meet in a fixed order.  The few rows may come as bf16 activations: every CTA then quantises them itself (8 KB a row of
+// 4,096 columns, from L2), while its first loads of the matrix are under way.
+#include <cuda_fp16.h>
+
+#include "fp8.cuh"
+
+namespace acrl {
+namespace {
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kStep = 512;                      // columns of a warp's step
+constexpr int kMostBytes = 64 * 1024;           // of the few rows in shared memory
+
+int64_t few_cols(int64_t K) { return (K + kStep - 1) / kStep * kStep; }
+
+struct FewArgs {
+    Matrix a, b;
+    const acrl_bf16* x;
+    int64_t ldx, ldo;
+    int K, cols;      // columns, and those that the steps cover
+    void* out;
+    int32_t* flags;
+};
+
+// 2^(s - 127) of a scale byte; NaN for 255.
+__device__ __forceinline__ float factor_of(uint32_t s) {
+    return s == 255u ? __int_as_float(0x7fc00000) : __uint_as_float(s ? s << 23 : 1u << 22);
+}
+
+// Four 8-bit numbers of a word to fp32.
+template <int FMT>
+__device__ __forceinline__ void widen4(uint32_t w, float* f) {
+    uint32_t lo, hi;
+    if (FMT == ACRL_FP8_E4M3) {
+        asm("{\n .reg .b16 a, b;\n mov.b32 {a, b}, %2;\n cvt.rn.f16x2.e4m3x2 %0, a;\n cvt.rn.f16x2.e4m3x2 %1, b;\n}\n"
+            : "=r"(lo), "=r"(hi)
+            : "r"(w));
+    } else {
+        asm("{\n .reg .b16 a, b;\n mov.b32 {a, b}, %2;\n cvt.rn.f16x2.e5m2x2 %0, a;\n cvt.rn.f16x2.e5m2x2 %1, b;\n}\n"
+            : "=r"(lo), "=r"(hi)
+            : "r"(w));
+    }
+    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&lo)), b = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+    f[0] = a.x;
+    f[1] = a.y;
+    f[2] = b.x;
+    f[3] = b.y;
+}
+
+template <int FMT>
+__device__ __forceinline__ void widen16(const uint4& v, float (&f)[16]) {
+    widen4<FMT>(v.x, f);
+    widen4<FMT>(v.y, f + 4);
+    widen4<FMT>(v.z, f + 8);
+    widen4<FMT>(v.w, f + 12);
+}
+
+// 16 bytes of a row, zeros beyond its end.
+__device__ __forceinline__ uint4 load16(const uint8_t* row, int c, int K) {
+    if (c + 16 <= K) return ld_stream(reinterpret_cast<const uint4*>(row + c));
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    uint8_t* b = reinterpret_cast<uint8_t*>(&v);
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+        if (c + j < K) b[j] = row[c + j];
+    return v;
+}
+
+// The few rows as fp32 values of [cols], zeros beyond K: sixteen lanes a block of 128 columns.
+template <int FMT>
+__device__ __forceinline__ void quantise_into(const FewArgs& A, float* xs) {
+    const int blocks = A.cols / 128, l = threadIdx.x & 15;
+    for (int u = threadIdx.x >> 4; u < int(A.a.rows) * blocks; u += kThreads / 16) {   // whole half-warps
+        const int m = u / blocks, c = (u - m * blocks) * 128 + l * 8;
+        float f[8];
+        load8<acrl_bf16>(A.x + m * A.ldx + min(c, A.K), max(0, A.K - c), f);
+        uint32_t top = max8(f);
+        const uint32_t mask = 0xffffu << (threadIdx.x & 16);
+#pragma unroll
+        for (int d = 8; d >= 1; d >>= 1) top = max(top, __shfl_xor_sync(mask, top, d));
+        const Scale s = block_scale<FMT>(top);
+        if (s.byte == 255u && l == 0 && blockIdx.x == 0) raise_flag(A.flags, ACRL_FLAG_NONFINITE);
+        const uint2 q = pack8<FMT>(f, s);
+        const float by = factor_of(s.byte);
+        float w[8];
+        widen4<FMT>(q.x, w);
+        widen4<FMT>(q.y, w + 4);
+        float4* to = reinterpret_cast<float4*>(xs + m * A.cols + c);
+        to[0] = make_float4(w[0] * by, w[1] * by, w[2] * by, w[3] * by);
+        to[1] = make_float4(w[4] * by, w[5] * by, w[6] * by, w[7] * by);
+    }
+}
+
+template <int FMT>
+__device__ __forceinline__ void widen_into(const FewArgs& A, float* xs) {
+    const int pieces = A.cols / 16;
+    for (int u = threadIdx.x; u < int(A.a.rows) * pieces; u += kThreads) {
+        const int m = u / pieces, c = (u - m * pieces) * 16;
+        float w[16];
+        widen16<FMT>(load16(A.a.q + m * A.a.ld, c, A.K), w);
+        const float by = c < A.K ? factor_of(A.a.scale[(A.a.block == ACRL_FP8_TILE ? 0 : m) * A.a.lds + (c >> 7)]) : 0.f;
+        float4* to = reinterpret_cast<float4*>(xs + m * A.cols + c);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) to[j] = make_float4(w[4 * j] * by, w[4 * j + 1] * by, w[4 * j + 2] * by, w[4 * j + 3] * by);
+    }
+}
+
+template <int FMT, int M, int W>
+__device__ __forceinline__ void dot_step(const FewArgs& A, const float* xs, const uint4 (&v)[W], const float (&by)[W], int c,
+                                         float (&acc)[W][M]) {
+    float part[W][M];
+#pragma unroll
+    for (int r = 0; r < W; ++r)
+#pragma unroll
+        for (int m = 0; m < M; ++m) part[r][m] = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        float w[W][4];
+#pragma unroll
+        for (int r = 0; r < W; ++r) widen4<FMT>(j == 0 ? v[r].x : j == 1 ? v[r].y : j == 2 ? v[r].z : v[r].w, w[r]);
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            const float4 x = *reinterpret_cast<const float4*>(xs + m * A.cols + c + 4 * j);
+#pragma unroll
+            for (int r = 0; r < W; ++r)
+                part[r][m] = fmaf(w[r][3], x.w, fmaf(w[r][2], x.z, fmaf(w[r][1], x.y, fmaf(w[r][0], x.x, part[r][m]))));
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < W; ++r)
+#pragma unroll
+        for (int m = 0; m < M; ++m) acc[r][m] = fmaf(part[r][m], by[r], acc[r][m]);
+}
+
+// W rows of the matrix a warp, one after the other grid stride.
+template <typename T, int FMT, int M, int W>
+__global__ void __launch_bounds__(kThreads, 2) few_kernel(const __grid_constant__ FewArgs A) {
+    extern __shared__ __align__(16) float xs[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int N = int(A.b.rows), shift = A.b.block == ACRL_FP8_TILE ? 7 : 0;
+    grid_begin();
+    auto load = [&](int n0, int c, uint4 (&v)[W], float (&by)[W]) {
+#pragma unroll
+        for (int r = 0; r < W; ++r) {
+            const int n = min(n0 + r, N - 1);
+            v[r] = load16(A.b.q + n * A.b.ld, min(c, A.K), A.K);
+            by[r] = c < A.K ? factor_of(__ldg(A.b.scale + int64_t(n >> shift) * A.b.lds + (c >> 7))) : 0.f;
+        }
+    };
+    int n0 = (int(blockIdx.x) * kWarps + warp) * W;
+    uint4 v[W];
+    float by[W];
+    if (n0 < N) load(n0, lane * 16, v, by);   // under way while the few rows are made
+    if (A.x) {
+        if (A.a.format == ACRL_FP8_E4M3) quantise_into<ACRL_FP8_E4M3>(A, xs);
+        else quantise_into<ACRL_FP8_E5M2>(A, xs);
+    } else {
+        if (A.a.format == ACRL_FP8_E4M3) widen_into<ACRL_FP8_E4M3>(A, xs);
+        else widen_into<ACRL_FP8_E5M2>(A, xs);
+    }
+    __syncthreads();
+    for (; n0 < N; n0 += int(gridDim.x) * kWarps * W) {
+        float acc[W][M];
+#pragma unroll
+        for (int r = 0; r < W; ++r)
+#pragma unroll
+            for (int m = 0; m < M; ++m) acc[r][m] = 0.f;
+        const int next_n = n0 + int(gridDim.x) * kWarps * W;
+        for (int c = lane * 16; c < A.cols; c += kStep) {
+            uint4 nv[W];
+            float nby[W];
+            // the next step's loads before this one's sums: of these rows, or the first of the warp's next ones
+            if (c + kStep < A.cols) load(n0, c + kStep, nv, nby);
+            else if (next_n < N) load(next_n, lane * 16, nv, nby);
+            dot_step<FMT, M, W>(A, xs, v, by, c, acc);
+#pragma unroll
+            for (int r = 0; r < W; ++r) {
+                v[r] = nv[r];
+                by[r] = nby[r];
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < W; ++r)
+#pragma unroll
+            for (int m = 0; m < M; ++m) {
+                const float sum = warp_sum(acc[r][m]);
+                if (lane == 0 && n0 + r < N) {
+                    if constexpr (sizeof(T) == 2)
+                        static_cast<acrl_bf16*>(A.out)[m * A.ldo + n0 + r] = acrl_bf16(pack_bf16x2(sum, 0.f) & 0xffffu);
+                    else
+                        static_cast<float*>(A.out)[m * A.ldo + n0 + r] = sum;
+                }
+            }
+    }
+}
+
+template <typename T, int FMT, int M>
+acrl_status launch_few(const FewArgs& A, cudaStream_t s) {
+    auto run = [&](auto* kernel, int W) {
+        const size_t smem = size_t(M) * A.cols * 4;
+        if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostBytes) != cudaSuccess)
+            return launch_status();
+        const int64_t tasks = (A.b.rows + W * kWarps - 1) / (W * kWarps);
+        return launch(kernel, std::min<int64_t>(tasks, 152 * 2), kThreads, smem, 0, s, A);
+    };
+    // two rows a warp, where there are enough four (half the reads of the few rows, as far as registers go)
+    if constexpr (M <= 2)
+        if (A.b.rows >= 16384) return run(few_kernel<T, FMT, M, 4>, 4);
+    return run(few_kernel<T, FMT, M, 2>, 2);
+}
+
+template <typename T, int FMT>
+acrl_status launch_rows_of(const FewArgs& A, cudaStream_t s) {
+    switch (A.a.rows) {
+        case 1: return launch_few<T, FMT, 1>(A, s);
+        case 2: return launch_few<T, FMT, 2>(A, s);
+        case 3: return launch_few<T, FMT, 3>(A, s);
+        default: return launch_few<T, FMT, 4>(A, s);
+    }
+}
+
+}  // namespace
+
+bool few_rows(int64_t M, int64_t K) { return M <= kFewRows && M * few_cols(K) * 4 <= kMostBytes; }
+
+acrl_status matmul_few(const Matrix& a, const acrl_bf16* x, int64_t ldx, const Matrix& b, int64_t K, void* out, acrl_dtype out_dtype,
+                       int64_t ldo, int32_t* flags, cudaStream_t s) {
+    if (!few_rows(a.rows, K)) return kFewNot;
+    const int64_t cols = few_cols(K);
+    FewArgs A = {};
+    A.a = a;
+    A.b = b;
+    A.x = x;
+    A.ldx = ldx;
+    A.ldo = ldo;
+    A.K = int(K);
+    A.cols = int(cols);
+    A.out = out;
+    A.flags = flags;
+    const bool bf16 = out_dtype == ACRL_BF16;
+    if (b.format == ACRL_FP8_E4M3) return bf16 ? launch_rows_of<acrl_bf16, 0>(A, s) : launch_rows_of<float, 0>(A, s);
+    return bf16 ? launch_rows_of<acrl_bf16, 1>(A, s) : launch_rows_of<float, 1>(A, s);
+}
+
+}  // namespace acrl

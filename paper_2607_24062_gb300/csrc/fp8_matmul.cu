@@ -36,6 +36,7 @@
 
 #include "acrl_device.cuh"
 #include "acrl_host.h"
+#include "fp8.cuh"
 #include "mbarrier.cuh"
 #include "tcgen05.cuh"
 #include "tma_host.h"
@@ -664,21 +665,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
 }
 
-struct Matrix {   // one operand of a product, as the entry points take it
-    const uint8_t* q;
-    int64_t rows, ld;
-    acrl_fp8_format format;
-    const uint8_t* scale;
-    int64_t lds;
-    acrl_fp8_block block;
-};
-
-bool matrix_ok(const Matrix& m, int64_t K) {
-    if (m.rows < 0 || m.rows > kMaxGrid - 256 || m.ld < K || (m.ld & 15) || m.lds < (K + 127) / 128) return false;
-    if (m.format != ACRL_FP8_E4M3 && m.format != ACRL_FP8_E5M2) return false;
-    return m.block == ACRL_FP8_ROW || m.block == ACRL_FP8_TILE;
-}
-
 Operand operand(const Matrix& m) {
     return Operand{m.scale, m.lds, int(m.rows), m.block == ACRL_FP8_TILE ? 7 : 0,
                    (m.lds & 3) == 0 && (reinterpret_cast<uintptr_t>(m.scale) & 3) == 0};
@@ -760,21 +746,32 @@ acrl_status launch_matmul(const Matrix& a, const Matrix& b, int64_t K, void* out
     return launch_kernel<T, true>(p, q, K, pr, 2 * total, 2, s);
 }
 
+// Checked operands of one row or more each.
+acrl_status product(const Matrix& a, const Matrix& b, int64_t K, void* out, acrl_dtype out_dtype, int64_t ldo, int32_t* flags,
+                    cudaStream_t s) {
+    if (K == 0) {   // an empty sum
+        const size_t size = out_dtype == ACRL_BF16 ? 2 : 4;
+        return cudaMemset2DAsync(out, size_t(ldo) * size, 0, size_t(b.rows) * size, size_t(a.rows), s) == cudaSuccess
+                   ? ACRL_OK
+                   : launch_status();
+    }
+    return out_dtype == ACRL_BF16 ? launch_matmul<acrl_bf16>(a, b, K, out, ldo, flags, s)
+                                  : launch_matmul<float>(a, b, K, out, ldo, flags, s);
+}
+
 acrl_status matmul(const Matrix& a, const Matrix& b, int64_t K, void* out, acrl_dtype out_dtype, int64_t ldo,
                    int32_t* flags, cudaStream_t s) {
     if (K < 0 || K > kMaxGrid - 512 || !matrix_ok(a, K) || !matrix_ok(b, K)) return ACRL_ERR_INVALID_ARG;
     if ((out_dtype != ACRL_BF16 && out_dtype != ACRL_F32) || ldo < b.rows || (ldo & 7)) return ACRL_ERR_INVALID_ARG;
     if (a.rows == 0 || b.rows == 0) return ACRL_OK;
     if (!out || !aligned16(out)) return ACRL_ERR_INVALID_ARG;
-    if (K == 0)   // an empty sum
-        return cudaMemset2DAsync(out, size_t(ldo) * (out_dtype == ACRL_BF16 ? 2 : 4), 0,
-                                 size_t(b.rows) * (out_dtype == ACRL_BF16 ? 2 : 4), size_t(a.rows), s) == cudaSuccess
-                   ? ACRL_OK
-                   : launch_status();
-    if (!a.q || !b.q || !a.scale || !b.scale || !aligned16(a.q) || !aligned16(b.q)) return ACRL_ERR_INVALID_ARG;
-    if (!operands_on_current_device({a.q, b.q, out})) return ACRL_ERR_INVALID_ARG;
-    return out_dtype == ACRL_BF16 ? launch_matmul<acrl_bf16>(a, b, K, out, ldo, flags, s)
-                                  : launch_matmul<float>(a, b, K, out, ldo, flags, s);
+    if (K > 0) {
+        if (!a.q || !b.q || !a.scale || !b.scale || !aligned16(a.q) || !aligned16(b.q)) return ACRL_ERR_INVALID_ARG;
+        const acrl_status few = matmul_few(a, nullptr, 0, b, K, out, out_dtype, ldo, flags, s);
+        if (few != kFewNot) return few;
+        if (!operands_on_current_device({a.q, b.q, out})) return ACRL_ERR_INVALID_ARG;
+    }
+    return product(a, b, K, out, out_dtype, ldo, flags, s);
 }
 
 }  // namespace
@@ -791,10 +788,10 @@ extern "C" acrl_status acrl_fp8_matmul(const uint8_t* a, int64_t M, int64_t K, i
                   out, out_dtype, ldo, dev_flags, reinterpret_cast<cudaStream_t>(stream));
 }
 
-// Rows of quantised activations at a stride of 16 bytes, then their scales at one of four.
+// Rows of quantised activations at a stride of 16 bytes, then their scales at one of four; a few rows need none.
 extern "C" int64_t acrl_fp8_linear_workspace_bytes(int64_t M, int64_t K) {
     if (M < 0 || K < 0) return -1;
-    return M * ((K + 15) / 16 * 16 + ((K + 127) / 128 + 3) / 4 * 4);
+    return few_rows(M, K) ? 0 : M * ((K + 15) / 16 * 16 + ((K + 127) / 128 + 3) / 4 * 4);
 }
 
 extern "C" acrl_status acrl_fp8_linear(const acrl_bf16* x, int64_t M, int64_t K, int64_t ldx, acrl_fp8_format x_format,
@@ -804,18 +801,24 @@ extern "C" acrl_status acrl_fp8_linear(const acrl_bf16* x, int64_t M, int64_t K,
                                        int32_t* dev_flags, acrl_stream stream) {
     if (M < 0 || K < 0 || workspace_bytes < acrl_fp8_linear_workspace_bytes(M, K)) return ACRL_ERR_INVALID_ARG;
     const int64_t ldq = (K + 15) / 16 * 16, lds = ((K + 127) / 128 + 3) / 4 * 4;
-    if (M > 0 && K > 0 && (!workspace || !aligned16(workspace))) return ACRL_ERR_INVALID_ARG;
+    if (workspace_bytes < 0 || (!few_rows(M, K) && K > 0 && (!workspace || !aligned16(workspace)))) return ACRL_ERR_INVALID_ARG;
     uint8_t* q = static_cast<uint8_t*>(workspace);
     const Matrix a{q, M, ldq, x_format, q + M * ldq, lds, ACRL_FP8_ROW};
     const Matrix b{w, N, ldw, w_format, w_scale, ldws, w_block};
     // the product's arguments are checked before anything is launched
-    if (!matrix_ok(a, K) || !matrix_ok(b, K) || (out_dtype != ACRL_BF16 && out_dtype != ACRL_F32) || ldo < N ||
-        (ldo & 7) || (M > 0 && N > 0 && (!out || !aligned16(out))) ||
-        (M > 0 && N > 0 && K > 0 && (!w || !w_scale || !aligned16(w) || !operands_on_current_device({w, q}))))
+    if (!matrix_ok(a, K) || !matrix_ok(b, K) || (out_dtype != ACRL_BF16 && out_dtype != ACRL_F32) || ldo < N || (ldo & 7) ||
+        ldx < K || (ldx & 7))
         return ACRL_ERR_INVALID_ARG;
     if (M == 0 || N == 0) return ACRL_OK;
+    if (!out || !aligned16(out) || (K > 0 && (!x || !w || !w_scale || !aligned16(x) || !aligned16(w)))) return ACRL_ERR_INVALID_ARG;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    if (K > 0) {
+        const acrl_status few = matmul_few(a, x, ldx, b, K, out, out_dtype, ldo, dev_flags, s);
+        if (few != kFewNot) return few;
+        if (!operands_on_current_device({w, q, out})) return ACRL_ERR_INVALID_ARG;
+    }
     const acrl_status st = acrl_fp8_quantize(x, ACRL_BF16, M, K, ldx, x_format, ACRL_FP8_ROW, 0, q, ldq, q + M * ldq, lds,
                                              dev_flags, stream);
     if (st != ACRL_OK) return st;
-    return matmul(a, b, K, out, out_dtype, ldo, dev_flags, reinterpret_cast<cudaStream_t>(stream));
+    return product(a, b, K, out, out_dtype, ldo, dev_flags, s);
 }

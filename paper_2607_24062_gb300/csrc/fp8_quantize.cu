@@ -13,86 +13,10 @@
 // bytes at a time.
 #include "acrl_device.cuh"
 #include "acrl_host.h"
+#include "fp8.cuh"
 
 namespace acrl {
 namespace {
-
-constexpr int kTopExp[2] = {8, 15};        // of 448 and 57344, by acrl_fp8_format
-
-// 8 consecutive elements of a row in registers, as fp32 bit patterns.
-template <typename T>
-__device__ __forceinline__ void load8(const T* __restrict__ p, int n, float (&f)[8]);
-
-template <>
-__device__ __forceinline__ void load8<acrl_bf16>(const acrl_bf16* __restrict__ p, int n, float (&f)[8]) {
-    if (n >= 8) {
-        const uint4 v = ld_stream(reinterpret_cast<const uint4*>(p));
-        f[0] = bf16_lo(v.x); f[1] = bf16_hi(v.x);
-        f[2] = bf16_lo(v.y); f[3] = bf16_hi(v.y);
-        f[4] = bf16_lo(v.z); f[5] = bf16_hi(v.z);
-        f[6] = bf16_lo(v.w); f[7] = bf16_hi(v.w);
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = j < n ? bf16_to_float(p[j]) : 0.f;
-}
-
-template <>
-__device__ __forceinline__ void load8<float>(const float* __restrict__ p, int n, float (&f)[8]) {
-    if (n >= 8) {
-        const uint4 a = ld_stream(reinterpret_cast<const uint4*>(p)), b = ld_stream(reinterpret_cast<const uint4*>(p) + 1);
-        f[0] = __uint_as_float(a.x); f[1] = __uint_as_float(a.y); f[2] = __uint_as_float(a.z); f[3] = __uint_as_float(a.w);
-        f[4] = __uint_as_float(b.x); f[5] = __uint_as_float(b.y); f[6] = __uint_as_float(b.z); f[7] = __uint_as_float(b.w);
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = j < n ? p[j] : 0.f;
-}
-
-// Bits of |f|: they order as unsigned integers, with an infinity and then NaN above every number.
-__device__ __forceinline__ uint32_t abs_bits(float f) { return __float_as_uint(f) & 0x7fffffffu; }
-
-__device__ __forceinline__ uint32_t max8(const float (&f)[8]) {
-    uint32_t m = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) m = max(m, abs_bits(f[j]));
-    return m;
-}
-
-// A block's scale from the bits of its maximum: the stored byte, and the factor 2^-e.
-struct Scale {
-    uint32_t byte;   // e + 127; 255 (NaN) for a block with an infinity or a NaN
-    float inv;
-};
-
-template <int FMT>
-__device__ __forceinline__ Scale block_scale(uint32_t m) {
-    if (m == 0u) return Scale{127u, 1.f};
-    if (m >= 0x7f800000u) return Scale{255u, 0.f};
-    // a below 2^-126 is stored without its leading one; its e is below -127 whatever its bits, and is raised to that
-    const int e = max(int(m >> 23) - 127 - kTopExp[FMT] + ((m & 0x7fffffu) > 0x600000u ? 1 : 0), -127);
-    return Scale{uint32_t(e + 127), __uint_as_float(uint32_t(127 - e) << 23)};
-}
-
-// Two fp32 to a pair of 8-bit numbers, `lo` in the low byte.
-template <int FMT>
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-    uint16_t r;
-    if (FMT == ACRL_FP8_E4M3)
-        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
-    else
-        asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-
-template <int FMT>
-__device__ __forceinline__ uint2 pack8(const float (&f)[8], const Scale& s) {
-    if (s.byte == 255u) return make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu);   // NaN in both formats
-    uint2 o;
-    o.x = pack2<FMT>(f[0] * s.inv, f[1] * s.inv) | pack2<FMT>(f[2] * s.inv, f[3] * s.inv) << 16;
-    o.y = pack2<FMT>(f[4] * s.inv, f[5] * s.inv) | pack2<FMT>(f[6] * s.inv, f[7] * s.inv) << 16;
-    return o;
-}
 
 // The first n (of 8) bytes; p is 8-byte aligned.
 __device__ __forceinline__ void store8(uint8_t* p, const uint2& v, int n) {

@@ -137,7 +137,8 @@ def test_matmul_formats_and_blocks(fa, fb, ba, bb, M, N, K):
     _check_product(acrl.fp8_matmul(a, b, out_dtype=torch.float32), a, b)
 
 
-@pytest.mark.parametrize("M,N,K,gap", [(1, 1000, 520, 0), (7, 300, 1032, 8), (130, 513, 264, 16)])
+@pytest.mark.parametrize("M,N,K,gap", [(1, 1000, 520, 0), (1, 1, 1, 7), (2, 17000, 136, 0), (3, 301, 4104, 8), (4, 77, 1000, 0),
+                                       (4, 40, 4104, 0), (7, 300, 1032, 8), (130, 513, 264, 16)])
 def test_linear_is_quantise_then_product(M, N, K, gap):
     x = _matrix(M, K, 6, gap=gap)
     w = acrl.fp8_quantize(_matrix(N, K, 7, std=0.02), block="tile")
@@ -174,14 +175,19 @@ def test_layer_in_a_graph():
 
 
 def test_nan_blocks_reach_what_they_touch():
-    x = _matrix(5, 300, 12)
-    x[2, 200] = float("nan")
-    w = acrl.fp8_quantize(_matrix(140, 300, 13), block="tile")
-    flags = api.new_flags()
-    out = acrl.fp8_linear(x, w, flags=flags)
-    assert acrl.read_flags(flags) == acrl.FLAG_NONFINITE
-    nan = out.isnan()
-    assert bool(nan[2].all()) and not bool(nan[[0, 1, 3, 4]].any())
+    for M in (4, 5):
+        x = _matrix(M, 300, 12)
+        x[2, 200] = float("nan")
+        w = acrl.fp8_quantize(_matrix(140, 300, 13), block="tile")
+        flags = api.new_flags()
+        out = acrl.fp8_linear(x, w, flags=flags)
+        assert acrl.read_flags(flags) == acrl.FLAG_NONFINITE
+        nan = out.isnan()
+        assert bool(nan[2].all()) and not bool(nan[[0, 1, 3]].any())
+        bad = _matrix(140, 300, 13)
+        bad[130, 5] = float("inf")
+        out = acrl.fp8_linear(_matrix(M, 300, 12), acrl.fp8_quantize(bad, block="tile"))
+        assert bool(out[:, 128:].isnan().all()) and not bool(out[:, :128].isnan().any())
 
 
 def test_products_of_nothing():

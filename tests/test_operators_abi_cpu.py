@@ -36,7 +36,7 @@ def test_quantize(L):
 
 
 def test_matmul(L):
-    ok = dict(a=FAKE, M=4, K=40, lda=48, fa=0, sa=FAKE, ldas=1, ba=0, b=FAKE, N=24, ldb=48, fb=0, sb=FAKE, ldbs=1, bb=1,
+    ok = dict(a=FAKE, M=5, K=40, lda=48, fa=0, sa=FAKE, ldas=1, ba=0, b=FAKE, N=24, ldb=48, fb=0, sb=FAKE, ldbs=1, bb=1,
               out=FAKE, dtype=0, ldo=24, flags=FAKE, stream=None)
     # a host address (FAKE) is refused as well: every operand is device memory
     for bad in ({}, dict(a=None), dict(sa=None), dict(b=None), dict(sb=None), dict(out=None), dict(M=-1),
@@ -50,12 +50,14 @@ def test_matmul(L):
 
 def test_linear(L):
     assert L.acrl_fp8_linear_workspace_bytes(-1, 4) == -1 and L.acrl_fp8_linear_workspace_bytes(4, -1) == -1
-    n = L.acrl_fp8_linear_workspace_bytes(4, 40)
-    assert n >= 4 * (48 + 1)
-    ok = dict(x=FAKE, M=4, K=40, ldx=40, fx=0, w=FAKE, N=24, ldw=48, fw=0, sw=FAKE, ldws=1, bw=1, out=FAKE, dtype=0, ldo=24,
+    assert L.acrl_fp8_linear_workspace_bytes(1, 4096) == 0   # a few rows are quantised in the product's kernel
+    n = L.acrl_fp8_linear_workspace_bytes(5, 40)
+    assert n >= 5 * (48 + 1)
+    ok = dict(x=FAKE, M=5, K=40, ldx=40, fx=0, w=FAKE, N=24, ldw=48, fw=0, sw=FAKE, ldws=1, bw=1, out=FAKE, dtype=0, ldo=24,
               ws=FAKE, n=n, flags=FAKE, stream=None)
     for bad in ({}, dict(x=None), dict(w=None), dict(sw=None), dict(out=None), dict(ws=None), dict(ws=FAKE + 8), dict(n=n - 1),
-                dict(ldx=32), dict(ldw=40), dict(ldo=20), dict(fx=2), dict(fw=2), dict(bw=2), dict(M=-1)):
+                dict(ldx=32), dict(ldw=40), dict(ldo=20), dict(fx=2), dict(fw=2), dict(bw=2), dict(M=-1), dict(M=1, n=0, ws=None, x=None),
+                dict(M=1, n=0, ws=None, ldx=44)):
         assert _call(L.acrl_fp8_linear, ok, **bad) == E, bad
     assert _call(L.acrl_fp8_linear, ok, N=0) == OK
 
