@@ -608,7 +608,7 @@ acrl_status acrl_fp8_quantize(const void* x, acrl_dtype x_dtype, int64_t R, int6
  *   out   device bf16 or float [M, ldo], 16-byte aligned, ldo >= N a multiple of
  *         8; columns from N on are not written.
  * The operands must be device memory of the current device, as for the LM head
- * (up to four rows of A: any memory the device reads).  K = 0 gives zeros.  Waits are time-bounded (ACRL_FLAG_TIMEOUT: the outputs are
+ * (one row of A: any memory the device reads).  K = 0 gives zeros.  Waits are time-bounded (ACRL_FLAG_TIMEOUT: the outputs are
  * invalid).
  */
 acrl_status acrl_fp8_matmul(const uint8_t* a, int64_t M, int64_t K, int64_t lda, acrl_fp8_format a_format,
@@ -621,16 +621,36 @@ acrl_status acrl_fp8_matmul(const uint8_t* a, int64_t M, int64_t K, int64_t lda,
  * acrl_fp8_linear -- out = Q(x) W^T: acrl_fp8_quantize of the activations by
  * rows, then acrl_fp8_matmul, in one call (one token or many).
  *   x          device bf16 [M, ldx].
- *   workspace  device, 16-byte aligned, of acrl_fp8_linear_workspace_bytes(M, K)
- *              bytes: the quantised activations (0 bytes, and NULL, for a few
- *              rows, which the product's kernel quantises itself).
+ *   workspace  device, 16-byte aligned, of acrl_fp8_linear_workspace_bytes
+ *              (M, N, K) bytes: the quantised activations (0 bytes, and NULL, for
+ *              one row, which the product's kernel quantises itself).
  */
-int64_t     acrl_fp8_linear_workspace_bytes(int64_t M, int64_t K);
+int64_t     acrl_fp8_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
 acrl_status acrl_fp8_linear(const acrl_bf16* x, int64_t M, int64_t K, int64_t ldx, acrl_fp8_format x_format,
                             const uint8_t* w, int64_t N, int64_t ldw, acrl_fp8_format w_format,
                             const uint8_t* w_scale, int64_t ldws, acrl_fp8_block w_block,
                             void* out, acrl_dtype out_dtype, int64_t ldo, void* workspace, int64_t workspace_bytes,
                             int32_t* dev_flags, acrl_stream stream);
+
+/*
+ * acrl_fp8_linear_backward -- the gradients of y = x W^T on 8-bit matrices:
+ *     dx = Q(dy) W            (contracted over W's rows, N)
+ *     dw = Q(dy^T) Q(x^T)^T   (contracted over the rows of x, M)
+ * with dy and x quantised by rows of 128 along the contraction; dy is read once.
+ *   dy         device bf16 [M, lddy];  x  device bf16 [M, ldx].
+ *   wt         the 8-bit transpose of W, [K, ldwt] (acrl_fp8_quantize with `transpose`).
+ *   dx         device bf16 or float [M, lddx];  dw  device bf16 or float [N, lddw]:
+ *              row strides at least K and multiples of 8.
+ *   workspace  device, 16-byte aligned, acrl_fp8_linear_backward_workspace_bytes
+ *              (M, N, K) bytes: the three quantised matrices.
+ */
+int64_t     acrl_fp8_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K);
+acrl_status acrl_fp8_linear_backward(const acrl_bf16* dy, int64_t M, int64_t N, int64_t lddy, acrl_fp8_format dy_format,
+                                     const acrl_bf16* x, int64_t K, int64_t ldx, acrl_fp8_format x_format,
+                                     const uint8_t* wt, int64_t ldwt, acrl_fp8_format w_format,
+                                     const uint8_t* wt_scale, int64_t ldwts, acrl_fp8_block w_block,
+                                     void* dx, acrl_dtype dx_dtype, int64_t lddx, void* dw, acrl_dtype dw_dtype, int64_t lddw,
+                                     void* workspace, int64_t workspace_bytes, int32_t* dev_flags, acrl_stream stream);
 
 /* ------------------------------------------------------------------------
  * Losses with a reference policy.

@@ -101,9 +101,12 @@ SIGNATURES = {
                                   c_p]),
     "acrl_fp8_matmul": (c_i32, [c_p, c_i64, c_i64, c_i64, c_i32, c_p, c_i64, c_i32, c_p, c_i64, c_i64, c_i32, c_p, c_i64,
                                 c_i32, c_p, c_i32, c_i64, c_p, c_p]),
-    "acrl_fp8_linear_workspace_bytes": (c_i64, [c_i64, c_i64]),
+    "acrl_fp8_linear_workspace_bytes": (c_i64, [c_i64, c_i64, c_i64]),
     "acrl_fp8_linear": (c_i32, [c_p, c_i64, c_i64, c_i64, c_i32, c_p, c_i64, c_i64, c_i32, c_p, c_i64, c_i32, c_p, c_i32,
                                 c_i64, c_p, c_i64, c_p, c_p]),
+    "acrl_fp8_linear_backward_workspace_bytes": (c_i64, [c_i64, c_i64, c_i64]),
+    "acrl_fp8_linear_backward": (c_i32, [c_p, c_i64, c_i64, c_i64, c_i32, c_p, c_i64, c_i64, c_i32, c_p, c_i64, c_i32, c_p,
+                                         c_i64, c_i32, c_p, c_i32, c_i64, c_p, c_i32, c_i64, c_p, c_i64, c_p, c_p]),
     "acrl_policy_loss_grad_logits": (c_i32, [c_p, c_i64, c_i64, c_i64, c_p, c_p, c_p, c_p, c_f32, c_f32, c_f32, c_i32,
                                              c_p, c_p, c_i64, c_p, c_p, c_p, c_p, c_p, c_p, c_p, c_p]),
     "acrl_preference_workspace_bytes": (c_i64, [c_i32, c_i32]),

@@ -557,25 +557,23 @@ def fp8_matmul(a: Fp8Tensor, b: Fp8Tensor, *, out_dtype=torch.bfloat16, out=None
     return out
 
 
-def fp8_linear_workspace_bytes(M: int, K: int) -> int:
+def fp8_linear_workspace_bytes(M: int, N: int, K: int) -> int:
     """acrl_fp8_linear_workspace_bytes."""
-    return int(lib().acrl_fp8_linear_workspace_bytes(M, K))
+    return int(lib().acrl_fp8_linear_workspace_bytes(M, N, K))
 
 
 def fp8_linear(x, weight: Fp8Tensor, *, fmt="e4m3", out_dtype=torch.bfloat16, out=None, workspace=None, flags=None,
                stream=None):
     """acrl_fp8_linear: x (bf16 [M, K]) quantised by rows, times the transpose of `weight` [N, K]; [M, N]."""
-    if not isinstance(x, torch.Tensor) or x.dtype != torch.bfloat16 or x.dim() != 2 or not x.is_cuda or \
-            (x.shape[1] > 1 and x.stride(1) != 1):
-        raise AcrlError("x: expected a 2-D bfloat16 CUDA tensor with unit column stride")
+    M, K = _bf16_rows(x, "x")
     w = _fp8_args(weight, "weight")
-    M, K, N = x.shape[0], x.shape[1], weight.shape[0]
+    N = w[1]
     if weight.shape[1] != K:
         raise AcrlError(f"x and weight disagree on K: {K} and {weight.shape[1]}")
     if out_dtype not in _OUT_DTYPE:
         raise AcrlError(f"out_dtype: {out_dtype}, expected bfloat16 or float32")
     out, ldo = _product_out(out, M, N, out_dtype, x.device)
-    n = lib().acrl_fp8_linear_workspace_bytes(M, K)
+    n = lib().acrl_fp8_linear_workspace_bytes(M, N, K)
     if workspace is not None:
         _need(workspace, torch.uint8, n, "workspace")
     elif n > 0:
@@ -586,15 +584,39 @@ def fp8_linear(x, weight: Fp8Tensor, *, fmt="e4m3", out_dtype=torch.bfloat16, ou
     return out
 
 
-def fp8_linear_backward(dy, x, weight_t: Fp8Tensor, *, fmt="e4m3", dx_dtype=torch.bfloat16, dw_dtype=torch.float32,
-                        flags=None, stream=None):
-    """The gradients of y = x W^T: dx = Q(dy) W and dw = Q(dy^T) Q(x^T)^T, products of 8-bit matrices over N and over
-    the rows.  dy [M, N] and x [M, K] bf16; `weight_t` is the 8-bit W^T [K, N] (fp8_quantize(w, block="tile",
-    transpose=True)); `fmt` is dy's format.  Returns (dx [M, K], dw [N, K])."""
-    kw = dict(flags=flags, stream=stream)
-    dx = fp8_matmul(fp8_quantize(dy, fmt=fmt, **kw), weight_t, out_dtype=dx_dtype, **kw)
-    dw = fp8_matmul(fp8_quantize(dy, fmt=fmt, transpose=True, **kw), fp8_quantize(x, transpose=True, **kw),
-                    out_dtype=dw_dtype, **kw)
+def fp8_linear_backward_workspace_bytes(M: int, N: int, K: int) -> int:
+    """acrl_fp8_linear_backward_workspace_bytes."""
+    return int(lib().acrl_fp8_linear_backward_workspace_bytes(M, N, K))
+
+
+def _bf16_rows(x, name: str):
+    if not isinstance(x, torch.Tensor) or x.dtype != torch.bfloat16 or x.dim() != 2 or not x.is_cuda or \
+            (x.shape[1] > 1 and x.stride(1) != 1):
+        raise AcrlError(f"{name}: expected a 2-D bfloat16 CUDA tensor with unit column stride")
+    return x.shape
+
+
+def fp8_linear_backward(dy, x, weight_t: Fp8Tensor, *, fmt="e4m3", x_fmt="e4m3", dx_dtype=torch.bfloat16,
+                        dw_dtype=torch.float32, dx=None, dw=None, workspace=None, flags=None, stream=None):
+    """acrl_fp8_linear_backward, the gradients of y = x W^T: dx = Q(dy) W and dw = Q(dy^T) Q(x^T)^T, products of 8-bit
+    matrices over N and over the rows.  dy [M, N] and x [M, K] bf16; `weight_t` is the 8-bit W^T [K, N]
+    (fp8_quantize(w, block="tile", transpose=True)); `fmt` and `x_fmt` are dy's and x's formats.  Returns (dx [M, K],
+    dw [N, K])."""
+    (M, N), (Mx, K) = _bf16_rows(dy, "dy"), _bf16_rows(x, "x")
+    w = _fp8_args(weight_t, "weight_t")
+    if Mx != M or tuple(weight_t.shape) != (K, N):
+        raise AcrlError(f"dy {(M, N)}, x {(Mx, K)} and weight_t {tuple(weight_t.shape)} do not belong together")
+    if dx_dtype not in _OUT_DTYPE or dw_dtype not in _OUT_DTYPE:
+        raise AcrlError("dx_dtype, dw_dtype: expected bfloat16 or float32")
+    dx, lddx = _product_out(dx, M, K, dx_dtype, dy.device)
+    dw, lddw = _product_out(dw, N, K, dw_dtype, dy.device)
+    n = lib().acrl_fp8_linear_backward_workspace_bytes(M, N, K)
+    workspace = torch.empty(n, dtype=torch.uint8, device=dy.device) if workspace is None else \
+        _need(workspace, torch.uint8, n, "workspace")
+    _opt(flags, torch.int32, 1, "flags")
+    _call("acrl_fp8_linear_backward", (dy, x, weight_t.q, weight_t.scale, dx, dw, workspace, flags), stream, dy.data_ptr(), M, N,
+          _ld(dy), _fp8_format(fmt), x.data_ptr(), K, _ld(x), _fp8_format(x_fmt), w[0], *w[2:], dx.data_ptr(),
+          _OUT_DTYPE[dx.dtype], lddx, dw.data_ptr(), _OUT_DTYPE[dw.dtype], lddw, workspace.data_ptr(), n, _ptr(flags))
     return dx, dw
 
 
@@ -804,6 +826,7 @@ __all__ = ["Params", "AcrlError", "token_stats", "seq_discrepancy", "grpo_advant
            "read_flags", "check_flags", "read_state", "Discrepancy",
            "PolicyLoss", "policy_loss_grad_logits", "Preference", "preference_loss", "preference_workspace_bytes",
            "Fp8Tensor", "fp8_quantize", "fp8_matmul", "fp8_linear", "fp8_linear_backward", "fp8_linear_workspace_bytes",
+           "fp8_linear_backward_workspace_bytes",
            "lmhead_logits_stats", "lmhead_merge", "lmhead_workspace_bytes", "lmhead_stats_noalloc", "save_state",
            "load_state", "controller_save", "controller_load", "selftest_wait_timeout",
            "host_pipeline_workspace_bytes", "host_pipeline_create", "host_pipeline_step", "host_pipeline_begin",

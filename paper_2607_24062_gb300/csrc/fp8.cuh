@@ -24,13 +24,17 @@ inline bool matrix_ok(const Matrix& m, int64_t K) {
     return m.block == ACRL_FP8_ROW || m.block == ACRL_FP8_TILE;
 }
 
-// out = A B^T of up to kFewRows rows of A, in fp8_few.cu: `a`, or bf16 activations `x` quantised in the kernel.  kFewNot: these
-// sizes are not its.
-constexpr int kFewRows = 4;
-bool few_rows(int64_t M, int64_t K);
+// out = A B^T of one row of A and a matrix of moderate size, in fp8_few.cu: `a`, or bf16 activations `x` quantised in the kernel.
+// kFewNot: these sizes are not its.
 constexpr acrl_status kFewNot = ACRL_ERR_NOT_IMPLEMENTED;
+bool few_rows(int64_t M, int64_t N, int64_t K);
 acrl_status matmul_few(const Matrix& a, const acrl_bf16* x, int64_t ldx, const Matrix& b, int64_t K, void* out, acrl_dtype out_dtype,
                        int64_t ldo, int32_t* flags, cudaStream_t s);
+
+// x by rows and the transpose of x by rows (acrl_fp8_quantize twice), x read once; checked arguments.
+acrl_status quantize_both(const acrl_bf16* x, int64_t R, int64_t C, int64_t ldx, acrl_fp8_format format, uint8_t* q, int64_t ldq,
+                          uint8_t* scale, int64_t lds, uint8_t* qt, int64_t ldqt, uint8_t* scale_t, int64_t ldst,
+                          int32_t* flags, cudaStream_t s);
 
 namespace {
 
@@ -79,13 +83,13 @@ __device__ __forceinline__ uint32_t max8(const float (&f)[8]) {
 // A block's scale from the bits of its maximum: the stored byte, and the factor 2^-e.
 struct Scale {
     uint32_t byte;   // e + 127; 255 (NaN) for a block with an infinity or a NaN
-    float inv;
+    float inv;       // NaN for such a block: every element becomes one
 };
 
 template <int FMT>
 __device__ __forceinline__ Scale block_scale(uint32_t m) {
     if (m == 0u) return Scale{127u, 1.f};
-    if (m >= 0x7f800000u) return Scale{255u, 0.f};
+    if (m >= 0x7f800000u) return Scale{255u, __int_as_float(0x7fc00000)};
     // a below 2^-126 is stored without its leading one; its e is below -127 whatever its bits, and is raised to that
     const int e = max(int(m >> 23) - 127 - kTopExp[FMT] + ((m & 0x7fffffu) > 0x600000u ? 1 : 0), -127);
     return Scale{uint32_t(e + 127), __uint_as_float(uint32_t(127 - e) << 23)};
@@ -103,11 +107,10 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 }
 
 template <int FMT>
-__device__ __forceinline__ uint2 pack8(const float (&f)[8], const Scale& s) {
-    if (s.byte == 255u) return make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu);   // NaN in both formats
+__device__ __forceinline__ uint2 pack8(const float (&f)[8], float inv) {
     uint2 o;
-    o.x = pack2<FMT>(f[0] * s.inv, f[1] * s.inv) | pack2<FMT>(f[2] * s.inv, f[3] * s.inv) << 16;
-    o.y = pack2<FMT>(f[4] * s.inv, f[5] * s.inv) | pack2<FMT>(f[6] * s.inv, f[7] * s.inv) << 16;
+    o.x = pack2<FMT>(f[0] * inv, f[1] * inv) | pack2<FMT>(f[2] * inv, f[3] * inv) << 16;
+    o.y = pack2<FMT>(f[4] * inv, f[5] * inv) | pack2<FMT>(f[6] * inv, f[7] * inv) << 16;
     return o;
 }
 

@@ -1,10 +1,10 @@
-// Products of a few rows (a token or four) with an 8-bit matrix: every byte of the matrix is used a few times only,
-// so HBM bounds them, and at the sizes of one layer the latency of a launch.  No tensor cores: their pipeline's start and end
-// (tensor memory, barriers, the split of the sum) takes longer than these products (1 x 4,096 x 4,096: 15 us against
-// 5).  A warp takes kW rows of the matrix at a time: each lane loads 16 bytes of each, 512 columns a step, converts them
-// to fp32 through half precision (exact for both formats) and multiplies them with the few rows, which lie in
-// shared memory as fp32 values of their own scales; the 16 products' sum takes the block's scale.  Then the lanes' sums
-// meet in a fixed order.  The few rows may come as bf16 activations: every CTA then quantises them itself (8 KB a row of
+// The product of one row, a token, with an 8-bit matrix: every byte of the matrix is used once, so HBM bounds it, and
+// at the sizes of one layer the latency of a launch.  No tensor cores: their pipeline's start and end (tensor memory,
+// barriers, the split of the sum) and the launch that quantises the row take longer than this product (1 x 4,096 x 4,096: 18
+// us against 10, and 25 against 15 as a call).  A warp takes kW rows of the matrix at a time: each lane loads 16 bytes of each,
+// 512 columns a step, two steps ahead, converts them to fp32 through half precision (exact for both formats) and multiplies
+// them with the row, which lies in shared memory as fp32 values of its own scales; the 16 products' sum takes the block's scale.
+// Then the lanes' sums meet in a fixed order.  The row may come as bf16 activations: every CTA then quantises it itself (8 KB for
 // 4,096 columns, from L2), while its first loads of the matrix are under way.
 #include <cuda_fp16.h>
 
@@ -15,9 +15,11 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kStep = 512;                      // columns of a warp's step
-constexpr int kMostBytes = 64 * 1024;           // of the few rows in shared memory
+constexpr int kW = 2;                           // rows of the matrix a warp takes at a time
+constexpr int kMostBytes = 64 * 1024;           // of the row in shared memory
+constexpr int64_t kFewBytes = 128 << 20;
 
-int64_t few_cols(int64_t K) { return (K + kStep - 1) / kStep * kStep; }
+int64_t few_cols(int64_t K) { return (K + 2 * kStep - 1) / (2 * kStep) * (2 * kStep); }
 
 struct FewArgs {
     Matrix a, b;
@@ -72,7 +74,7 @@ __device__ __forceinline__ uint4 load16(const uint8_t* row, int c, int K) {
     return v;
 }
 
-// The few rows as fp32 values of [cols], zeros beyond K: sixteen lanes a block of 128 columns.
+// The row as fp32 values, zeros beyond K: sixteen lanes a block of 128 columns.
 template <int FMT>
 __device__ __forceinline__ void quantise_into(const FewArgs& A, float* xs) {
     const int blocks = A.cols / 128, l = threadIdx.x & 15;
@@ -86,7 +88,7 @@ __device__ __forceinline__ void quantise_into(const FewArgs& A, float* xs) {
         for (int d = 8; d >= 1; d >>= 1) top = max(top, __shfl_xor_sync(mask, top, d));
         const Scale s = block_scale<FMT>(top);
         if (s.byte == 255u && l == 0 && blockIdx.x == 0) raise_flag(A.flags, ACRL_FLAG_NONFINITE);
-        const uint2 q = pack8<FMT>(f, s);
+        const uint2 q = pack8<FMT>(f, s.inv);
         const float by = factor_of(s.byte);
         float w[8];
         widen4<FMT>(q.x, w);
@@ -111,52 +113,44 @@ __device__ __forceinline__ void widen_into(const FewArgs& A, float* xs) {
     }
 }
 
-template <int FMT, int M, int W>
-__device__ __forceinline__ void dot_step(const FewArgs& A, const float* xs, const uint4 (&v)[W], const float (&by)[W], int c,
-                                         float (&acc)[W][M]) {
-    float part[W][M];
-#pragma unroll
-    for (int r = 0; r < W; ++r)
-#pragma unroll
-        for (int m = 0; m < M; ++m) part[r][m] = 0.f;
+template <int FMT>
+__device__ __forceinline__ void dot_step(const float* xs, const uint4 (&v)[kW], const float (&by)[kW], float (&acc)[kW]) {
+    float part[kW] = {};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        float w[W][4];
+        const float4 x = *reinterpret_cast<const float4*>(xs + 4 * j);
 #pragma unroll
-        for (int r = 0; r < W; ++r) widen4<FMT>(j == 0 ? v[r].x : j == 1 ? v[r].y : j == 2 ? v[r].z : v[r].w, w[r]);
-#pragma unroll
-        for (int m = 0; m < M; ++m) {
-            const float4 x = *reinterpret_cast<const float4*>(xs + m * A.cols + c + 4 * j);
-#pragma unroll
-            for (int r = 0; r < W; ++r)
-                part[r][m] = fmaf(w[r][3], x.w, fmaf(w[r][2], x.z, fmaf(w[r][1], x.y, fmaf(w[r][0], x.x, part[r][m]))));
+        for (int r = 0; r < kW; ++r) {
+            float w[4];
+            widen4<FMT>(j == 0 ? v[r].x : j == 1 ? v[r].y : j == 2 ? v[r].z : v[r].w, w);
+            part[r] = fmaf(w[3], x.w, fmaf(w[2], x.z, fmaf(w[1], x.y, fmaf(w[0], x.x, part[r]))));
         }
     }
 #pragma unroll
-    for (int r = 0; r < W; ++r)
-#pragma unroll
-        for (int m = 0; m < M; ++m) acc[r][m] = fmaf(part[r][m], by[r], acc[r][m]);
+    for (int r = 0; r < kW; ++r) acc[r] = fmaf(part[r], by[r], acc[r]);
 }
 
-// W rows of the matrix a warp, one after the other grid stride.
-template <typename T, int FMT, int M, int W>
+template <typename T, int FMT>
 __global__ void __launch_bounds__(kThreads, 2) few_kernel(const __grid_constant__ FewArgs A) {
     extern __shared__ __align__(16) float xs[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int N = int(A.b.rows), shift = A.b.block == ACRL_FP8_TILE ? 7 : 0;
+    const int N = int(A.b.rows), shift = A.b.block == ACRL_FP8_TILE ? 7 : 0, step = int(gridDim.x) * kWarps * kW;
     grid_begin();
-    auto load = [&](int n0, int c, uint4 (&v)[W], float (&by)[W]) {
+    auto load = [&](int n0, int c, uint4 (&v)[kW], float (&by)[kW]) {
 #pragma unroll
-        for (int r = 0; r < W; ++r) {
+        for (int r = 0; r < kW; ++r) {
             const int n = min(n0 + r, N - 1);
             v[r] = load16(A.b.q + n * A.b.ld, min(c, A.K), A.K);
             by[r] = c < A.K ? factor_of(__ldg(A.b.scale + int64_t(n >> shift) * A.b.lds + (c >> 7))) : 0.f;
         }
     };
-    int n0 = (int(blockIdx.x) * kWarps + warp) * W;
-    uint4 v[W];
-    float by[W];
-    if (n0 < N) load(n0, lane * 16, v, by);   // under way while the few rows are made
+    int n0 = (int(blockIdx.x) * kWarps + warp) * kW;
+    uint4 v[2][kW];
+    float by[2][kW];
+    if (n0 < N) {   // under way while the row is made
+        load(n0, lane * 16, v[0], by[0]);
+        load(n0, lane * 16 + kStep, v[1], by[1]);
+    }
     if (A.x) {
         if (A.a.format == ACRL_FP8_E4M3) quantise_into<ACRL_FP8_E4M3>(A, xs);
         else quantise_into<ACRL_FP8_E5M2>(A, xs);
@@ -165,73 +159,50 @@ __global__ void __launch_bounds__(kThreads, 2) few_kernel(const __grid_constant_
         else widen_into<ACRL_FP8_E5M2>(A, xs);
     }
     __syncthreads();
-    for (; n0 < N; n0 += int(gridDim.x) * kWarps * W) {
-        float acc[W][M];
+    for (; n0 < N; n0 += step) {
+        float acc[kW] = {};
+        // two steps in flight: those to come of these rows, then the first ones of the warp's next
+        for (int c = lane * 16; c < A.cols; c += 2 * kStep) {
 #pragma unroll
-        for (int r = 0; r < W; ++r)
-#pragma unroll
-            for (int m = 0; m < M; ++m) acc[r][m] = 0.f;
-        const int next_n = n0 + int(gridDim.x) * kWarps * W;
-        for (int c = lane * 16; c < A.cols; c += kStep) {
-            uint4 nv[W];
-            float nby[W];
-            // the next step's loads before this one's sums: of these rows, or the first of the warp's next ones
-            if (c + kStep < A.cols) load(n0, c + kStep, nv, nby);
-            else if (next_n < N) load(next_n, lane * 16, nv, nby);
-            dot_step<FMT, M, W>(A, xs, v, by, c, acc);
-#pragma unroll
-            for (int r = 0; r < W; ++r) {
-                v[r] = nv[r];
-                by[r] = nby[r];
+            for (int k = 0; k < 2; ++k) {
+                const int at = c + k * kStep, ahead = at + 2 * kStep;
+                dot_step<FMT>(xs + at, v[k], by[k], acc);
+                if (ahead < A.cols) load(n0, ahead, v[k], by[k]);
+                else if (n0 + step < N) load(n0 + step, lane * 16 + k * kStep, v[k], by[k]);
             }
         }
 #pragma unroll
-        for (int r = 0; r < W; ++r)
-#pragma unroll
-            for (int m = 0; m < M; ++m) {
-                const float sum = warp_sum(acc[r][m]);
-                if (lane == 0 && n0 + r < N) {
-                    if constexpr (sizeof(T) == 2)
-                        static_cast<acrl_bf16*>(A.out)[m * A.ldo + n0 + r] = acrl_bf16(pack_bf16x2(sum, 0.f) & 0xffffu);
-                    else
-                        static_cast<float*>(A.out)[m * A.ldo + n0 + r] = sum;
-                }
+        for (int r = 0; r < kW; ++r) {
+            const float sum = warp_sum(acc[r]);
+            if (lane == 0 && n0 + r < N) {
+                if constexpr (sizeof(T) == 2)
+                    static_cast<acrl_bf16*>(A.out)[n0 + r] = acrl_bf16(pack_bf16x2(sum, 0.f) & 0xffffu);
+                else
+                    static_cast<float*>(A.out)[n0 + r] = sum;
             }
+        }
     }
-}
-
-template <typename T, int FMT, int M>
-acrl_status launch_few(const FewArgs& A, cudaStream_t s) {
-    auto run = [&](auto* kernel, int W) {
-        const size_t smem = size_t(M) * A.cols * 4;
-        if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostBytes) != cudaSuccess)
-            return launch_status();
-        const int64_t tasks = (A.b.rows + W * kWarps - 1) / (W * kWarps);
-        return launch(kernel, std::min<int64_t>(tasks, 152 * 2), kThreads, smem, 0, s, A);
-    };
-    // two rows a warp, where there are enough four (half the reads of the few rows, as far as registers go)
-    if constexpr (M <= 2)
-        if (A.b.rows >= 16384) return run(few_kernel<T, FMT, M, 4>, 4);
-    return run(few_kernel<T, FMT, M, 2>, 2);
 }
 
 template <typename T, int FMT>
-acrl_status launch_rows_of(const FewArgs& A, cudaStream_t s) {
-    switch (A.a.rows) {
-        case 1: return launch_few<T, FMT, 1>(A, s);
-        case 2: return launch_few<T, FMT, 2>(A, s);
-        case 3: return launch_few<T, FMT, 3>(A, s);
-        default: return launch_few<T, FMT, 4>(A, s);
-    }
+acrl_status launch_few(const FewArgs& A, cudaStream_t s) {
+    const size_t smem = size_t(A.cols) * 4;
+    auto* kernel = few_kernel<T, FMT>;
+    if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostBytes) != cudaSuccess)
+        return launch_status();
+    const int64_t tasks = (A.b.rows + kW * kWarps - 1) / (kW * kWarps);
+    return launch(kernel, std::min<int64_t>(tasks, 152 * 2), kThreads, smem, 0, s, A);
 }
 
 }  // namespace
 
-bool few_rows(int64_t M, int64_t K) { return M <= kFewRows && M * few_cols(K) * 4 <= kMostBytes; }
+// Matrices of up to kFewBytes only: beyond, the latency is a small part, and the tensor cores' path streams a matrix faster
+// (1 x 4,096 x 151,936: 100 us against 142).
+bool few_rows(int64_t M, int64_t N, int64_t K) { return M == 1 && K > 0 && N * K <= kFewBytes && few_cols(K) * 4 <= kMostBytes; }
 
 acrl_status matmul_few(const Matrix& a, const acrl_bf16* x, int64_t ldx, const Matrix& b, int64_t K, void* out, acrl_dtype out_dtype,
                        int64_t ldo, int32_t* flags, cudaStream_t s) {
-    if (!few_rows(a.rows, K)) return kFewNot;
+    if (!few_rows(a.rows, b.rows, K)) return kFewNot;
     const int64_t cols = few_cols(K);
     FewArgs A = {};
     A.a = a;
@@ -244,8 +215,8 @@ acrl_status matmul_few(const Matrix& a, const acrl_bf16* x, int64_t ldx, const M
     A.out = out;
     A.flags = flags;
     const bool bf16 = out_dtype == ACRL_BF16;
-    if (b.format == ACRL_FP8_E4M3) return bf16 ? launch_rows_of<acrl_bf16, 0>(A, s) : launch_rows_of<float, 0>(A, s);
-    return bf16 ? launch_rows_of<acrl_bf16, 1>(A, s) : launch_rows_of<float, 1>(A, s);
+    if (b.format == ACRL_FP8_E4M3) return bf16 ? launch_few<acrl_bf16, 0>(A, s) : launch_few<float, 0>(A, s);
+    return bf16 ? launch_few<acrl_bf16, 1>(A, s) : launch_few<float, 1>(A, s);
 }
 
 }  // namespace acrl

@@ -422,6 +422,13 @@ __device__ void write_scales(Barriers* bars, uint32_t tmem, const Problem& pr, u
     }
 }
 
+template <typename T>
+__device__ __forceinline__ void store_one(T* p, float v);
+template <>
+__device__ __forceinline__ void store_one<float>(float* p, float v) { *p = v; }
+template <>
+__device__ __forceinline__ void store_one<acrl_bf16>(acrl_bf16* p, float v) { *p = acrl_bf16(pack_bf16x2(v, 0.f) & 0xffffu); }
+
 // Accumulators of a pair's tile: each warp its 32 rows, 32 columns at a time, rounded, staged in shared memory and
 // stored by a TMA copy, which leaves out what is beyond the matrix.
 template <typename T>
@@ -460,6 +467,15 @@ __device__ void pair_epilogue(Barriers* bars, uint32_t tmem, const CUtensorMap* 
             }
             const int col0 = tq * pr.cols + c;
             if (row0 >= pr.p.rows || col0 >= pr.q.rows) continue;   // the same for the whole warp
+            if (col0 + 32 > pr.q.rows && (pr.q.rows * int(sizeof(T)) & 15) != 0) {
+                // a TMA store leaves columns out in 16-byte pieces: here the last ones would write beyond the matrix
+                T* out = static_cast<T*>(pr.out) + int64_t(row0 + lane) * pr.ldo + col0;
+                if (row0 + lane < pr.p.rows)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (col0 + j < pr.q.rows) store_one(out + j, __uint_as_float(r[j]));
+                continue;
+            }
             if (lane == 0) bulk_wait_read<1>();                     // the store that last read this block is done
             __syncwarp();
             const uint32_t to = at + uint32_t(buf * kOutBlock<T>);
@@ -489,13 +505,6 @@ __device__ void pair_epilogue(Barriers* bars, uint32_t tmem, const CUtensorMap* 
     if (lane == 0) bulk_wait_all();   // the blocks stay valid until every store has completed
     __syncwarp();
 }
-
-template <typename T>
-__device__ __forceinline__ void store_one(T* p, float v);
-template <>
-__device__ __forceinline__ void store_one<float>(float* p, float v) { *p = v; }
-template <>
-__device__ __forceinline__ void store_one<acrl_bf16>(acrl_bf16* p, float v) { *p = acrl_bf16(pack_bf16x2(v, 0.f) & 0xffffu); }
 
 // A CTA alone: row r of P is column r of `out`, a column of the accumulator a row of it, so a warp stores 32 neighbours.
 // With a split sum the other ranks' accumulators wait in the first rank's shared memory (`parts`, [rank - 1][column][128]).
@@ -670,8 +679,9 @@ Operand operand(const Matrix& m) {
                    (m.lds & 3) == 0 && (reinterpret_cast<uintptr_t>(m.scale) & 3) == 0};
 }
 
-// Rows up to this many become the MMA's columns.
-constexpr int64_t kAloneRows = 128;
+// Rows up to this many become the MMA's columns: with fewer tiles than SMs, where the sum is split and its parts go
+// through shared memory, kSplitRows (64 x 4,096 x 4,096: 27 us, as pairs 18; 16: 18).
+constexpr int64_t kAloneRows = 128, kSplitRows = 32;
 constexpr int kMaxSplit = 8;
 
 template <typename T, bool PAIR>
@@ -706,7 +716,7 @@ acrl_status launch_matmul(const Matrix& a, const Matrix& b, int64_t K, void* out
     int dev = 0, sms = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
         return launch_status();
-    const bool alone = a.rows <= kAloneRows;
+    const bool alone = a.rows <= kSplitRows || (a.rows <= kAloneRows && b.rows >= int64_t(kRows) * sms);
     const Matrix &p = alone ? b : a, &q = alone ? a : b;
     Problem pr = {};
     pr.p = operand(p);
@@ -735,10 +745,21 @@ acrl_status launch_matmul(const Matrix& a, const Matrix& b, int64_t K, void* out
         const int64_t grid = split > 1 ? int64_t(pr.p_tiles) * split : std::min(pr.p_tiles, sms);
         return launch_kernel<T, false>(p, q, K, pr, grid, split, s);
     }
-    pr.cols = kPairCols;
     pr.p_tiles = int((p.rows + 2 * kRows - 1) / (2 * kRows));
+    // Columns of a tile: the loads of a slab, 128 rows of P and half the columns a CTA, take longest, and all pairs run whole
+    // rounds of tiles; so the least rounds x (128 + columns / 2), wide tiles first.  2,507 x 2,048 x 8,200 (100 tiles of 224
+    // columns or 130 of 160 for 76 pairs) 58 / 52 us.
+    int64_t total = 0, least = 0;
+    for (int cols = kPairCols; cols >= 96; cols -= 32) {
+        const int64_t tiles = int64_t(pr.p_tiles) * ((q.rows + cols - 1) / cols);
+        const int64_t cost = (tiles + sms / 2 - 1) / (sms / 2) * (128 + cols / 2);
+        if (least == 0 || cost < least) {
+            least = cost;
+            total = tiles;
+            pr.cols = cols;
+        }
+    }
     pr.q_tiles = int((q.rows + pr.cols - 1) / pr.cols);
-    const int64_t total = int64_t(pr.p_tiles) * pr.q_tiles;
     if (total > kMaxGrid / 2) return ACRL_ERR_INVALID_ARG;
     pr.accs = 2;
     pr.stages = std::min(kMaxStages, kRingBytes<T, true> / ((kRows + pr.cols / 2) * kSlab));
@@ -755,6 +776,8 @@ acrl_status product(const Matrix& a, const Matrix& b, int64_t K, void* out, acrl
                    ? ACRL_OK
                    : launch_status();
     }
+    const acrl_status few = matmul_few(a, nullptr, 0, b, K, out, out_dtype, ldo, flags, s);
+    if (few != kFewNot) return few;
     return out_dtype == ACRL_BF16 ? launch_matmul<acrl_bf16>(a, b, K, out, ldo, flags, s)
                                   : launch_matmul<float>(a, b, K, out, ldo, flags, s);
 }
@@ -767,9 +790,7 @@ acrl_status matmul(const Matrix& a, const Matrix& b, int64_t K, void* out, acrl_
     if (!out || !aligned16(out)) return ACRL_ERR_INVALID_ARG;
     if (K > 0) {
         if (!a.q || !b.q || !a.scale || !b.scale || !aligned16(a.q) || !aligned16(b.q)) return ACRL_ERR_INVALID_ARG;
-        const acrl_status few = matmul_few(a, nullptr, 0, b, K, out, out_dtype, ldo, flags, s);
-        if (few != kFewNot) return few;
-        if (!operands_on_current_device({a.q, b.q, out})) return ACRL_ERR_INVALID_ARG;
+        if (!few_rows(a.rows, b.rows, K) && !operands_on_current_device({a.q, b.q, out})) return ACRL_ERR_INVALID_ARG;
     }
     return product(a, b, K, out, out_dtype, ldo, flags, s);
 }
@@ -788,10 +809,11 @@ extern "C" acrl_status acrl_fp8_matmul(const uint8_t* a, int64_t M, int64_t K, i
                   out, out_dtype, ldo, dev_flags, reinterpret_cast<cudaStream_t>(stream));
 }
 
-// Rows of quantised activations at a stride of 16 bytes, then their scales at one of four; a few rows need none.
-extern "C" int64_t acrl_fp8_linear_workspace_bytes(int64_t M, int64_t K) {
-    if (M < 0 || K < 0) return -1;
-    return few_rows(M, K) ? 0 : M * ((K + 15) / 16 * 16 + ((K + 127) / 128 + 3) / 4 * 4);
+// Rows of quantised activations at a stride of 16 bytes, then their scales at one of four; none where the product's
+// kernel quantises a row itself.
+extern "C" int64_t acrl_fp8_linear_workspace_bytes(int64_t M, int64_t N, int64_t K) {
+    if (M < 0 || N < 0 || K < 0) return -1;
+    return few_rows(M, N, K) ? 0 : M * ((K + 15) / 16 * 16 + ((K + 127) / 128 + 3) / 4 * 4);
 }
 
 extern "C" acrl_status acrl_fp8_linear(const acrl_bf16* x, int64_t M, int64_t K, int64_t ldx, acrl_fp8_format x_format,
@@ -799,9 +821,9 @@ extern "C" acrl_status acrl_fp8_linear(const acrl_bf16* x, int64_t M, int64_t K,
                                        const uint8_t* w_scale, int64_t ldws, acrl_fp8_block w_block, void* out,
                                        acrl_dtype out_dtype, int64_t ldo, void* workspace, int64_t workspace_bytes,
                                        int32_t* dev_flags, acrl_stream stream) {
-    if (M < 0 || K < 0 || workspace_bytes < acrl_fp8_linear_workspace_bytes(M, K)) return ACRL_ERR_INVALID_ARG;
+    if (M < 0 || N < 0 || K < 0 || workspace_bytes < acrl_fp8_linear_workspace_bytes(M, N, K)) return ACRL_ERR_INVALID_ARG;
     const int64_t ldq = (K + 15) / 16 * 16, lds = ((K + 127) / 128 + 3) / 4 * 4;
-    if (workspace_bytes < 0 || (!few_rows(M, K) && K > 0 && (!workspace || !aligned16(workspace)))) return ACRL_ERR_INVALID_ARG;
+    if (workspace_bytes < 0 || (M > 0 && N > 0 && K > 0 && !few_rows(M, N, K) && (!workspace || !aligned16(workspace)))) return ACRL_ERR_INVALID_ARG;
     uint8_t* q = static_cast<uint8_t*>(workspace);
     const Matrix a{q, M, ldq, x_format, q + M * ldq, lds, ACRL_FP8_ROW};
     const Matrix b{w, N, ldw, w_format, w_scale, ldws, w_block};
@@ -821,4 +843,74 @@ extern "C" acrl_status acrl_fp8_linear(const acrl_bf16* x, int64_t M, int64_t K,
                                              dev_flags, stream);
     if (st != ACRL_OK) return st;
     return product(a, b, K, out, out_dtype, ldo, dev_flags, s);
+}
+
+namespace acrl {
+namespace {
+
+// The backward's workspace: dy by rows, dy's transpose, x's transpose, each its elements and then its scales.
+struct Part {
+    int64_t rows, ldq, lds, at;   // at: of the elements; the scales follow
+    int64_t end() const { return (at + rows * (ldq + lds) + 15) / 16 * 16; }
+};
+
+struct BackwardParts {
+    Part dy, dyt, xt;
+    BackwardParts(int64_t M, int64_t N, int64_t K) {
+        auto part = [](int64_t rows, int64_t cols, int64_t at) {
+            return Part{rows, (cols + 15) / 16 * 16, ((cols + 127) / 128 + 3) / 4 * 4, at};
+        };
+        dy = part(M, N, 0);
+        dyt = part(N, M, dy.end());
+        xt = part(K, M, dyt.end());
+    }
+};
+
+Matrix matrix_of(uint8_t* base, const Part& p, acrl_fp8_format format) {
+    return Matrix{base + p.at, p.rows, p.ldq, format, base + p.at + p.rows * p.ldq, p.lds, ACRL_FP8_ROW};
+}
+
+}  // namespace
+}  // namespace acrl
+
+extern "C" int64_t acrl_fp8_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K) {
+    return M < 0 || N < 0 || K < 0 ? -1 : BackwardParts(M, N, K).xt.end();
+}
+
+extern "C" acrl_status acrl_fp8_linear_backward(const acrl_bf16* dy, int64_t M, int64_t N, int64_t lddy,
+                                                acrl_fp8_format dy_format, const acrl_bf16* x, int64_t K, int64_t ldx,
+                                                acrl_fp8_format x_format, const uint8_t* wt, int64_t ldwt,
+                                                acrl_fp8_format w_format, const uint8_t* wt_scale, int64_t ldwts,
+                                                acrl_fp8_block w_block, void* dx, acrl_dtype dx_dtype, int64_t lddx, void* dw,
+                                                acrl_dtype dw_dtype, int64_t lddw, void* workspace, int64_t workspace_bytes,
+                                                int32_t* dev_flags, acrl_stream stream) {
+    if (M < 0 || N < 0 || K < 0 || M > kMaxGrid / 2 || N > kMaxGrid / 2 || K > kMaxGrid / 2) return ACRL_ERR_INVALID_ARG;
+    const BackwardParts parts(M, N, K);
+    const Matrix w{wt, K, ldwt, w_format, wt_scale, ldwts, w_block};
+    auto format_ok = [](acrl_fp8_format f) { return f == ACRL_FP8_E4M3 || f == ACRL_FP8_E5M2; };
+    auto dtype_ok = [](acrl_dtype d) { return d == ACRL_BF16 || d == ACRL_F32; };
+    if (!format_ok(dy_format) || !format_ok(x_format) || !matrix_ok(w, N) || !dtype_ok(dx_dtype) || !dtype_ok(dw_dtype))
+        return ACRL_ERR_INVALID_ARG;
+    if (lddy < N || (lddy & 7) || ldx < K || (ldx & 7) || lddx < K || (lddx & 7) || lddw < K || (lddw & 7)) return ACRL_ERR_INVALID_ARG;
+    if (workspace_bytes < parts.xt.end()) return ACRL_ERR_INVALID_ARG;
+    if (K == 0 || (M == 0 && N == 0)) return ACRL_OK;
+    if ((M > 0 && (!dx || !aligned16(dx) || !x || !aligned16(x))) || (N > 0 && (!dw || !aligned16(dw) || !wt || !wt_scale || !aligned16(wt))))
+        return ACRL_ERR_INVALID_ARG;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    uint8_t* base = static_cast<uint8_t*>(workspace);
+    const Matrix a = matrix_of(base, parts.dy, dy_format), at = matrix_of(base, parts.dyt, dy_format),
+                 xt = matrix_of(base, parts.xt, x_format);
+    if (M == 0) return product(at, xt, 0, dw, dw_dtype, lddw, dev_flags, s);     // empty sums
+    if (N == 0) return product(a, w, 0, dx, dx_dtype, lddx, dev_flags, s);
+    if (!dy || !aligned16(dy) || !workspace || !aligned16(workspace) || !operands_on_current_device({wt, base, dx, dw}))
+        return ACRL_ERR_INVALID_ARG;
+    acrl_status st = quantize_both(dy, M, N, lddy, dy_format, base + parts.dy.at, parts.dy.ldq, const_cast<uint8_t*>(a.scale),
+                                   parts.dy.lds, base + parts.dyt.at, parts.dyt.ldq, const_cast<uint8_t*>(at.scale), parts.dyt.lds,
+                                   dev_flags, s);
+    if (st == ACRL_OK)
+        st = acrl_fp8_quantize(x, ACRL_BF16, M, K, ldx, x_format, ACRL_FP8_ROW, 1, base + parts.xt.at, parts.xt.ldq,
+                               const_cast<uint8_t*>(xt.scale), parts.xt.lds, dev_flags, stream);
+    if (st == ACRL_OK) st = product(a, w, N, dx, dx_dtype, lddx, dev_flags, s);
+    if (st == ACRL_OK) st = product(at, xt, M, dw, dw_dtype, lddw, dev_flags, s);
+    return st;
 }

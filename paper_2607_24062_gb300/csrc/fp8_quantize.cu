@@ -18,6 +18,31 @@
 namespace acrl {
 namespace {
 
+// Eight elements as they were loaded: a bf16 tile's registers are half of what its fp32 numbers would take.
+template <typename T>
+struct Eight;
+template <>
+struct Eight<acrl_bf16> {
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const acrl_bf16* p, int n) {
+        if (n >= 8) {
+            const uint4 v = ld_stream(reinterpret_cast<const uint4*>(p));
+            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            w[j] = (2 * j < n ? uint32_t(p[2 * j]) : 0u) | (2 * j + 1 < n ? uint32_t(p[2 * j + 1]) << 16 : 0u);
+    }
+    __device__ __forceinline__ float at(int j) const { return j & 1 ? bf16_hi(w[j >> 1]) : bf16_lo(w[j >> 1]); }
+};
+template <>
+struct Eight<float> {
+    float f[8];
+    __device__ __forceinline__ void load(const float* p, int n) { load8<float>(p, n, f); }
+    __device__ __forceinline__ float at(int j) const { return f[j]; }
+};
+
 // The first n (of 8) bytes; p is 8-byte aligned.
 __device__ __forceinline__ void store8(uint8_t* p, const uint2& v, int n) {
     if (n >= 8) {
@@ -74,130 +99,174 @@ __global__ void __launch_bounds__(kRowThreads)
             scale[row * lds + kb] = uint8_t(s.byte);
             if (s.byte == 255u) raise_flag(flags, ACRL_FLAG_NONFINITE);
         }
-        if (c < C) store8(q + row * ldq + c, pack8<FMT>(f[k], s), C - c);
+        if (c < C) store8(q + row * ldq + c, pack8<FMT>(f[k], s.inv), C - c);
     }
 }
 
-// 128 x 128 elements of x a CTA: a thread holds eight consecutive rows of eight columns.  TILE: one scale, else (the
-// transpose of x, by rows) one per column.  TR: the result is the transpose, turned in shared memory: 8-byte pieces,
-// piece g of a column at g ^ (column / 8), so that neither side meets a bank twice.
-constexpr int kTileThreads = 256;
+// 128 x 128 elements of x a CTA, loaded once into registers: eight consecutive rows of eight columns a thread for what is stored as
+// it is (151,936 x 4,096 in 284 us, with four rows in twice the threads 357), four for what is turned (the transpose of 5,003 x
+// 2,056 in 15 us, with eight 18.7).  What is made of them:
+//   kTile    one scale, the elements as they are          kTileT  one scale, the transpose
+//   kRowT    a scale per column, the transpose            kBoth   a scale per row, the elements as they are, and kRowT's
+// The transpose is turned in shared memory: 8-byte pieces, piece p of a column at p ^ (column / 8), so that neither side meets a
+// bank twice; a thread writes half a piece.
+enum Make { kTile, kTileT, kRowT, kBoth };
+template <Make MAKE>
+constexpr int kTileRows = MAKE == kTile ? 8 : 4;
+template <Make MAKE>
+constexpr int kTileThreads = 2048 / kTileRows<MAKE>;
 
-// The tile's result, turned, in rows of 128 bytes.
-template <int FMT, bool TILE>
-__device__ __forceinline__ void turn_and_store(const float (&f)[8][8], const Scale* s, uint8_t* turned, uint8_t* q,
-                                               int64_t ldq, int64_t rb, int64_t cb, int64_t R, int64_t C) {
-    const int g = threadIdx.x >> 4, cl = threadIdx.x & 15;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float col[8] = {f[0][j], f[1][j], f[2][j], f[3][j], f[4][j], f[5][j], f[6][j], f[7][j]};
-        *reinterpret_cast<uint2*>(turned + (8 * cl + j) * 128 + 8 * (g ^ cl)) = pack8<FMT>(col, s[TILE ? 0 : j]);
-    }
-    __syncthreads();
-    // eight lanes a column of x (128 bytes of the result's row)
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int c = k * 32 + (threadIdx.x >> 3), p = 2 * (threadIdx.x & 7);
-        const int64_t col = cb * 128 + c, row = rb * 128 + 8 * p;
-        if (col >= C || row >= R) continue;
-        const uint2 a = *reinterpret_cast<const uint2*>(turned + c * 128 + 8 * (p ^ (c >> 3)));
-        const uint2 b = *reinterpret_cast<const uint2*>(turned + c * 128 + 8 * ((p + 1) ^ (c >> 3)));
-        uint8_t* to = q + col * ldq + row;
-        if (row + 16 <= R) {
-            *reinterpret_cast<uint4*>(to) = make_uint4(a.x, a.y, b.x, b.y);
-        } else {
-            store8(to, a, int(R - row));
-            if (row + 8 < R) store8(to + 8, b, int(R - row - 8));
-        }
-    }
-}
+struct Quantised {
+    uint8_t* q;
+    int64_t ldq;
+    uint8_t* scale;
+    int64_t lds;
+};
 
-template <typename T, int FMT, bool TILE, bool TR>
-__global__ void __launch_bounds__(kTileThreads)
-    quantize_tiles(const T* __restrict__ x, int64_t R, int64_t C, int64_t ldx, int col_blocks, uint8_t* __restrict__ q,
-                   int64_t ldq, uint8_t* __restrict__ scale, int64_t lds, int32_t* flags) {
-    static_assert(TILE || TR, "rows as they are have a kernel of their own");
-    __shared__ uint32_t sh_max[TILE ? 8 : 8 * 128];
-    __shared__ __align__(16) uint8_t turned[TR ? 128 * 128 : 16];
-    grid_begin();
-    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-    const int g = threadIdx.x >> 4, cl = threadIdx.x & 15;        // rows 8 g .., columns 8 cl ..
-    const int64_t rb = blockIdx.x / col_blocks, cb = blockIdx.x % col_blocks;
-    const int64_t r0 = rb * 128 + 8 * g, c0 = cb * 128 + 8 * cl;
+template <typename T, int FMT, Make MAKE>
+__global__ void __launch_bounds__(kTileThreads<MAKE>, MAKE == kTile ? 3 : 2)
+    quantize_tiles(const T* __restrict__ x, int64_t R, int64_t C, int64_t ldx, int col_blocks, Quantised as, Quantised turned,
+                   int32_t* flags) {
+    constexpr int U = kTileRows<MAKE>, kThreads = kTileThreads<MAKE>;
+    __shared__ uint32_t top[128];                       // of each column (or, of the tile, in the first)
+    __shared__ __align__(16) uint8_t turn[MAKE == kTile ? 16 : 128 * 128];
+    const int lane = threadIdx.x & 31;
+    const int g = threadIdx.x >> 4, cl = threadIdx.x & 15;        // rows U g .., columns 8 cl ..
+    const int64_t rb = blockIdx.x / col_blocks, cb = blockIdx.x - rb * col_blocks;
+    const int64_t r0 = rb * 128 + U * g, c0 = cb * 128 + 8 * cl;
     const int nc = int(min(int64_t(8), C - c0));
-    float f[8][8];
-    if (r0 + 8 <= R && nc == 8) {   // no test between the loads: all eight in flight
+    if (threadIdx.x < 128) top[threadIdx.x] = 0u;
+    grid_begin();
+    Eight<T> f[U];
+    if (r0 + U <= R && nc == 8) {   // no test between the loads: all in flight
 #pragma unroll
-        for (int i = 0; i < 8; ++i) load8<T>(x + (r0 + i) * ldx + c0, 8, f[i]);
+        for (int i = 0; i < U; ++i) f[i].load(x + (r0 + i) * ldx + c0, 8);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) load8<T>(x + (r0 + i < R && nc > 0 ? (r0 + i) * ldx + c0 : 0), r0 + i < R ? nc : 0, f[i]);
+        for (int i = 0; i < U; ++i) f[i].load(x + (r0 + i < R && nc > 0 ? (r0 + i) * ldx + c0 : 0), r0 + i < R ? nc : 0);
     }
-    Scale s[TILE ? 1 : 8];
-    if constexpr (TILE) {
+    auto max_of = [&](int i) {
         uint32_t m = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) m = max(m, max8(f[i]));
-        m = __reduce_max_sync(0xffffffffu, m);
-        if (lane == 0) sh_max[wid] = m;
-        __syncthreads();
+        for (int j = 0; j < 8; ++j) m = max(m, abs_bits(f[i].at(j)));
+        return m;
+    };
+    auto store_as = [&](int i, float inv) {
+        float v[8];
 #pragma unroll
-        for (int w = 0; w < 8; ++w) m = max(m, sh_max[w]);
-        s[0] = block_scale<FMT>(m);
+        for (int j = 0; j < 8; ++j) v[j] = f[i].at(j);
+        if (r0 + i < R && nc > 0) store8(as.q + (r0 + i) * as.ldq + c0, pack8<FMT>(v, inv), nc);
+    };
+    if constexpr (MAKE == kBoth) {   // sixteen lanes hold a row's 128 columns
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            uint32_t m = max_of(i);
+#pragma unroll
+            for (int d = 8; d >= 1; d >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, d));
+            const Scale s = block_scale<FMT>(m);
+            if (cl == 0 && r0 + i < R) as.scale[(r0 + i) * as.lds + cb] = uint8_t(s.byte);
+            store_as(i, s.inv);
+        }
+    }
+    __syncthreads();
+    float inv[MAKE == kTile || MAKE == kTileT ? 1 : 8];
+    if constexpr (MAKE == kTile || MAKE == kTileT) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < U; ++i) m = max(m, max_of(i));
+        m = __reduce_max_sync(0xffffffffu, m);
+        if (lane == 0) atomicMax(top, m);
+        __syncthreads();
+        const Scale s = block_scale<FMT>(top[0]);
+        inv[0] = s.inv;
         if (threadIdx.x == 0) {
-            scale[TR ? cb * lds + rb : rb * lds + cb] = uint8_t(s[0].byte);
-            if (s[0].byte == 255u) raise_flag(flags, ACRL_FLAG_NONFINITE);
+            if (MAKE == kTileT) turned.scale[cb * turned.lds + rb] = uint8_t(s.byte);
+            else as.scale[rb * as.lds + cb] = uint8_t(s.byte);
+            if (s.byte == 255u) raise_flag(flags, ACRL_FLAG_NONFINITE);
         }
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             uint32_t m = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) m = max(m, abs_bits(f[i][j]));
+            for (int i = 0; i < U; ++i) m = max(m, abs_bits(f[i].at(j)));
             m = max(m, __shfl_xor_sync(0xffffffffu, m, 16));
-            if (lane < 16) sh_max[wid * 128 + 8 * cl + j] = m;
+            if (lane < 16) atomicMax(top + 8 * cl + j, m);
         }
         __syncthreads();
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            uint32_t m = 0;
-#pragma unroll
-            for (int w = 0; w < 8; ++w) m = max(m, sh_max[w * 128 + 8 * cl + j]);
-            s[j] = block_scale<FMT>(m);
-            if (g == 0 && c0 + j < C) {
-                scale[(c0 + j) * lds + rb] = uint8_t(s[j].byte);
-                if (s[j].byte == 255u) raise_flag(flags, ACRL_FLAG_NONFINITE);
+        for (int j = 0; j < 8; ++j) inv[j] = block_scale<FMT>(top[8 * cl + j]).inv;
+        if (threadIdx.x < 128) {
+            const int64_t c = cb * 128 + threadIdx.x;
+            const Scale mine = block_scale<FMT>(top[threadIdx.x]);
+            if (c < C) {
+                turned.scale[c * turned.lds + rb] = uint8_t(mine.byte);
+                if (mine.byte == 255u) raise_flag(flags, ACRL_FLAG_NONFINITE);
             }
         }
     }
-    if constexpr (!TR) {
+    if constexpr (MAKE == kTile) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (r0 + i < R && nc > 0) store8(q + (r0 + i) * ldq + c0, pack8<FMT>(f[i], s[0]), nc);
+        for (int i = 0; i < U; ++i) store_as(i, inv[0]);
     } else {
-        turn_and_store<FMT, TILE>(f, s, turned, q, ldq, rb, cb, R, C);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float by = inv[MAKE == kTileT ? 0 : j];
+            const uint32_t w = pack2<FMT>(f[0].at(j) * by, f[1].at(j) * by) | pack2<FMT>(f[2].at(j) * by, f[3].at(j) * by) << 16;
+            *reinterpret_cast<uint32_t*>(turn + (8 * cl + j) * 128 + 8 * ((g >> 1) ^ cl) + 4 * (g & 1)) = w;
+        }
+        __syncthreads();
+        // eight lanes a column of x (128 bytes of the result's row)
+#pragma unroll
+        for (int k = 0; k < 128 / (kThreads / 8); ++k) {
+            const int c = k * (kThreads / 8) + (threadIdx.x >> 3), p = 2 * (threadIdx.x & 7);
+            const int64_t col = cb * 128 + c, row = rb * 128 + 8 * p;
+            if (col >= C || row >= R) continue;
+            const uint2 a = *reinterpret_cast<const uint2*>(turn + c * 128 + 8 * (p ^ (c >> 3)));
+            const uint2 b = *reinterpret_cast<const uint2*>(turn + c * 128 + 8 * ((p + 1) ^ (c >> 3)));
+            uint8_t* to = turned.q + col * turned.ldq + row;
+            if (row + 16 <= R) {
+                *reinterpret_cast<uint4*>(to) = make_uint4(a.x, a.y, b.x, b.y);
+            } else {
+                store8(to, a, int(R - row));
+                if (row + 8 < R) store8(to + 8, b, int(R - row - 8));
+            }
+        }
     }
+}
+
+template <typename T, int FMT, Make MAKE>
+acrl_status launch_tiles(const T* x, int64_t R, int64_t C, int64_t ldx, const Quantised& as, const Quantised& turned,
+                         int32_t* flags, cudaStream_t s) {
+    const int64_t cb = (C + 127) / 128, grid = (R + 127) / 128 * cb;
+    if (grid > kMaxGrid) return ACRL_ERR_INVALID_ARG;
+    return launch(quantize_tiles<T, FMT, MAKE>, grid, kTileThreads<MAKE>, 0, 0, s, x, R, C, ldx, int(cb), as, turned, flags);
 }
 
 template <typename T, int FMT>
-acrl_status launch_quantize(const T* x, int64_t R, int64_t C, int64_t ldx, bool tile, bool transpose, uint8_t* q,
-                            int64_t ldq, uint8_t* scale, int64_t lds, int32_t* flags, cudaStream_t s) {
-    if (!tile && !transpose) {
-        const int KB = int((C + 127) / 128), chunks = (KB + kRowUnroll - 1) / kRowUnroll;
-        const int64_t units = R * chunks, grid = (units + kRowThreads / 16 - 1) / (kRowThreads / 16);
-        if (grid > kMaxGrid) return ACRL_ERR_INVALID_ARG;
-        return launch(quantize_rows<T, FMT>, grid, kRowThreads, 0, 0, s, x, R, int(C), ldx, KB, chunks, q, ldq, scale, lds,
-                      flags);
-    }
-    const int64_t cb = (C + 127) / 128, grid = (R + 127) / 128 * cb;
+acrl_status launch_quantize(const T* x, int64_t R, int64_t C, int64_t ldx, bool tile, bool transpose, const Quantised& out,
+                            int32_t* flags, cudaStream_t s) {
+    if (transpose)
+        return tile ? launch_tiles<T, FMT, kTileT>(x, R, C, ldx, out, out, flags, s)
+                    : launch_tiles<T, FMT, kRowT>(x, R, C, ldx, out, out, flags, s);
+    if (tile) return launch_tiles<T, FMT, kTile>(x, R, C, ldx, out, out, flags, s);
+    const int KB = int((C + 127) / 128), chunks = (KB + kRowUnroll - 1) / kRowUnroll;
+    const int64_t units = R * chunks, grid = (units + kRowThreads / 16 - 1) / (kRowThreads / 16);
     if (grid > kMaxGrid) return ACRL_ERR_INVALID_ARG;
-    auto* kernel = !transpose ? quantize_tiles<T, FMT, true, false>
-                   : tile     ? quantize_tiles<T, FMT, true, true>
-                              : quantize_tiles<T, FMT, false, true>;
-    return launch(kernel, grid, kTileThreads, 0, 0, s, x, R, C, ldx, int(cb), q, ldq, scale, lds, flags);
+    return launch(quantize_rows<T, FMT>, grid, kRowThreads, 0, 0, s, x, R, int(C), ldx, KB, chunks, out.q, out.ldq, out.scale,
+                  out.lds, flags);
 }
 
 }  // namespace
+
+acrl_status quantize_both(const acrl_bf16* x, int64_t R, int64_t C, int64_t ldx, acrl_fp8_format format, uint8_t* q, int64_t ldq,
+                          uint8_t* scale, int64_t lds, uint8_t* qt, int64_t ldqt, uint8_t* scale_t, int64_t ldst,
+                          int32_t* flags, cudaStream_t s) {
+    const Quantised as{q, ldq, scale, lds}, turned{qt, ldqt, scale_t, ldst};
+    return format == ACRL_FP8_E4M3 ? launch_tiles<acrl_bf16, 0, kBoth>(x, R, C, ldx, as, turned, flags, s)
+                                   : launch_tiles<acrl_bf16, 1, kBoth>(x, R, C, ldx, as, turned, flags, s);
+}
+
 }  // namespace acrl
 
 using namespace acrl;
@@ -216,13 +285,14 @@ extern "C" acrl_status acrl_fp8_quantize(const void* x, acrl_dtype x_dtype, int6
     if (R == 0 || C == 0) return ACRL_OK;
     if (!x || !q || !scale || !aligned16(x) || !aligned16(q)) return ACRL_ERR_INVALID_ARG;
     const bool tile = block == ACRL_FP8_TILE, tr = transpose != 0;
+    const Quantised out{q, ldq, scale, lds};
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     if (x_dtype == ACRL_BF16) {
         auto* p = static_cast<const acrl_bf16*>(x);
-        return format == ACRL_FP8_E4M3 ? launch_quantize<acrl_bf16, 0>(p, R, C, ldx, tile, tr, q, ldq, scale, lds, dev_flags, s)
-                                       : launch_quantize<acrl_bf16, 1>(p, R, C, ldx, tile, tr, q, ldq, scale, lds, dev_flags, s);
+        return format == ACRL_FP8_E4M3 ? launch_quantize<acrl_bf16, 0>(p, R, C, ldx, tile, tr, out, dev_flags, s)
+                                       : launch_quantize<acrl_bf16, 1>(p, R, C, ldx, tile, tr, out, dev_flags, s);
     }
     auto* p = static_cast<const float*>(x);
-    return format == ACRL_FP8_E4M3 ? launch_quantize<float, 0>(p, R, C, ldx, tile, tr, q, ldq, scale, lds, dev_flags, s)
-                                   : launch_quantize<float, 1>(p, R, C, ldx, tile, tr, q, ldq, scale, lds, dev_flags, s);
+    return format == ACRL_FP8_E4M3 ? launch_quantize<float, 0>(p, R, C, ldx, tile, tr, out, dev_flags, s)
+                                   : launch_quantize<float, 1>(p, R, C, ldx, tile, tr, out, dev_flags, s);
 }

@@ -147,15 +147,26 @@ def test_linear_is_quantise_then_product(M, N, K, gap):
     _check_product(got, acrl.fp8_quantize(x), w)
 
 
-def test_linear_backward():
-    M, N, K = 203, 328, 136
-    x, dy, w = _matrix(M, K, 8), _matrix(M, N, 9, std=1e-3), _matrix(N, K, 10, std=0.02)
+@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (3, 130, 257), (129, 100, 40), (203, 328, 136), (600, 70, 1000)])
+@pytest.mark.parametrize("fmt,x_fmt", [("e4m3", "e4m3"), ("e5m2", "e4m3"), ("e4m3", "e5m2")])
+def test_linear_backward(M, N, K, fmt, x_fmt):
+    x, dy, w = _matrix(M, K, 8, gap=8), _matrix(M, N, 9, std=1e-3), _matrix(N, K, 10, std=0.02)
     wt = acrl.fp8_quantize(w, block="tile", transpose=True)
-    dx, dw = acrl.fp8_linear_backward(dy, x, wt)
-    _check_product(dx, acrl.fp8_quantize(dy), wt)
-    _check_product(dw, acrl.fp8_quantize(dy, transpose=True), acrl.fp8_quantize(x, transpose=True))
+    dx, dw = acrl.fp8_linear_backward(dy, x, wt, fmt=fmt, x_fmt=x_fmt)
+    # the products of what fp8_quantize makes, to the last bit
+    assert torch.equal(dx, acrl.fp8_matmul(acrl.fp8_quantize(dy, fmt=fmt), wt))
+    _check_product(dx, acrl.fp8_quantize(dy, fmt=fmt), wt)
+    a, b = acrl.fp8_quantize(dy, fmt=fmt, transpose=True), acrl.fp8_quantize(x, fmt=x_fmt, transpose=True)
+    assert torch.equal(dw, acrl.fp8_matmul(a, b, out_dtype=torch.float32))
+    _check_product(dw, a, b)
     # the 8-bit weight is the same matrix either way round
     assert torch.equal(wt.values().t(), acrl.fp8_quantize(w, block="tile").values())
+
+
+def test_linear_backward_of_nothing():
+    wt = acrl.fp8_quantize(_matrix(30, 20, 1), block="tile", transpose=True)
+    dx, dw = acrl.fp8_linear_backward(_matrix(3, 30, 2)[:0], _matrix(3, 20, 3)[:0], wt)
+    assert dx.shape == (0, 20) and dw.shape == (30, 20) and not bool(dw.any())
 
 
 def test_layer_in_a_graph():
@@ -201,14 +212,16 @@ def test_products_of_nothing():
 
 
 def test_output_keeps_what_is_beyond_the_product():
-    a = acrl.fp8_quantize(_matrix(70, 256, 3))
-    for M in (3, 70):   # both ways round inside the kernel
-        am = acrl.Fp8Tensor(a.q[:M], a.scale[:M])
-        b = acrl.fp8_quantize(_matrix(37, 256, 4), block="tile")
-        big = torch.full((M + 2, 48), 7.0, dtype=torch.bfloat16, device=DEV)
-        out = acrl.fp8_matmul(am, b, out=big[:M])
-        _check_product(out, am, b)
-        assert bool((big[M:] == 7).all()) and bool((big[:, 37:] == 7).all())
+    a = acrl.fp8_quantize(_matrix(300, 256, 3))
+    for M in (1, 3, 70, 300):   # one row; both ways round inside the kernel
+        for N in (37, 36, 250):
+            for dtype in (torch.bfloat16, torch.float32):
+                am = acrl.Fp8Tensor(a.q[:M], a.scale[:M])
+                b = acrl.fp8_quantize(_matrix(N, 256, 4), block="tile")
+                big = torch.full((M + 2, 264), 7.0, dtype=dtype, device=DEV)
+                out = acrl.fp8_matmul(am, b, out=big[:M])
+                _check_product(out, am, b)
+                assert bool((big[M:] == 7).all()) and bool((big[:, N:] == 7).all())
 
 
 def test_other_stream():
@@ -233,6 +246,7 @@ def test_refusals():
                  lambda: acrl.fp8_matmul(w, acrl.fp8_quantize(_matrix(8, 72, 1))), lambda: acrl.fp8_matmul(w, x),
                  lambda: acrl.fp8_matmul(w, w, out_dtype=torch.float16),
                  lambda: acrl.fp8_matmul(w, w, out=torch.empty((8, 12), dtype=torch.bfloat16, device=DEV)),
+                 lambda: acrl.fp8_linear_backward(x, x, w), lambda: acrl.fp8_linear_backward(x.float(), x, w),
                  lambda: acrl.fp8_linear(x.float(), w), lambda: acrl.fp8_linear(x[:, :32], w),
                  lambda: acrl.fp8_linear(x, w, workspace=torch.empty(8, dtype=torch.uint8, device=DEV))):
         with pytest.raises(acrl.AcrlError):

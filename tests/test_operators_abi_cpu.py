@@ -49,9 +49,9 @@ def test_matmul(L):
 
 
 def test_linear(L):
-    assert L.acrl_fp8_linear_workspace_bytes(-1, 4) == -1 and L.acrl_fp8_linear_workspace_bytes(4, -1) == -1
-    assert L.acrl_fp8_linear_workspace_bytes(1, 4096) == 0   # a few rows are quantised in the product's kernel
-    n = L.acrl_fp8_linear_workspace_bytes(5, 40)
+    assert L.acrl_fp8_linear_workspace_bytes(-1, 4, 4) == -1 and L.acrl_fp8_linear_workspace_bytes(4, 4, -1) == -1
+    assert L.acrl_fp8_linear_workspace_bytes(1, 4096, 4096) == 0   # one row is quantised in the product's kernel
+    n = L.acrl_fp8_linear_workspace_bytes(5, 24, 40)
     assert n >= 5 * (48 + 1)
     ok = dict(x=FAKE, M=5, K=40, ldx=40, fx=0, w=FAKE, N=24, ldw=48, fw=0, sw=FAKE, ldws=1, bw=1, out=FAKE, dtype=0, ldo=24,
               ws=FAKE, n=n, flags=FAKE, stream=None)
@@ -60,6 +60,19 @@ def test_linear(L):
                 dict(M=1, n=0, ws=None, ldx=44)):
         assert _call(L.acrl_fp8_linear, ok, **bad) == E, bad
     assert _call(L.acrl_fp8_linear, ok, N=0) == OK
+
+
+def test_linear_backward(L):
+    assert L.acrl_fp8_linear_backward_workspace_bytes(-1, 1, 1) == -1
+    n = L.acrl_fp8_linear_backward_workspace_bytes(5, 24, 40)
+    assert n >= 5 * 24 + 24 * 5 + 40 * 5
+    ok = dict(dy=FAKE, M=5, N=24, lddy=24, fy=0, x=FAKE, K=40, ldx=40, fx=0, wt=FAKE, ldwt=32, fw=0, swt=FAKE, ldwts=1, bw=1,
+              dx=FAKE, tx=0, lddx=40, dw=FAKE, tw=1, lddw=40, ws=FAKE, n=n, flags=None, stream=None)
+    for bad in ({}, dict(dy=None), dict(x=None), dict(wt=None), dict(swt=None), dict(dx=None), dict(dw=None), dict(ws=None),
+                dict(n=n - 1), dict(M=-1), dict(N=-1), dict(K=-1), dict(lddy=20), dict(ldx=36), dict(ldwt=24), dict(lddx=32),
+                dict(lddw=44), dict(fy=2), dict(fx=2), dict(fw=2), dict(bw=2), dict(tx=2), dict(tw=-1), dict(dy=FAKE + 2),
+                dict(x=FAKE + 8), dict(dx=FAKE + 4), dict(ws=FAKE + 8)):
+        assert _call(L.acrl_fp8_linear_backward, ok, **bad) == E, bad
 
 
 def test_policy_loss(L):
