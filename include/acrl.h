@@ -746,6 +746,24 @@ acrl_status acrl_preference_loss(const float* logp, const float* ref_logp, const
                                  int32_t* dev_flags, acrl_stream stream);
 
 /*
+ * acrl_preference_step -- a preference step from the logits, in one call: lse and
+ * log-probs of the rows, acrl_preference_loss on them, and acrl_loss_grad_logits
+ * with its coef, which writes d loss / d logits.  Arguments, outputs and flags are
+ * theirs (dev_flags is required); lse and logp, device float [T], are those of
+ * acrl_token_stats, from sums without a bias that a response's tokens would add up.
+ *   workspace  device, 16-byte aligned, acrl_preference_step_workspace_bytes(T, S,
+ *              Gn) bytes.
+ */
+int64_t     acrl_preference_step_workspace_bytes(int64_t T, int32_t S, int32_t Gn);
+acrl_status acrl_preference_step(const acrl_bf16* logits, int64_t T, int64_t V, int64_t ld, const int32_t* ids,
+                                 const uint8_t* mask, const float* ref_logp, const float* rewards,
+                                 const int64_t* seq_offsets, int32_t S, const int32_t* group_offsets, int32_t Gn,
+                                 acrl_preference_form form, float beta, float margin, float label_smoothing,
+                                 int32_t length_norm, float* lse, float* logp, float* ratio, float* coef,
+                                 acrl_bf16* grad, float* loss, void* workspace, int64_t workspace_bytes,
+                                 int32_t* dev_flags, acrl_stream stream);
+
+/*
  * acrl_selftest_wait_timeout -- failure-detection self-test: one warp waits on
  * a shared-memory barrier that nothing arrives on, with the same bounded wait
  * that guards every pipeline wait of acrl_lmhead_logits_stats; after

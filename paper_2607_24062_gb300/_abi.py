@@ -112,6 +112,9 @@ SIGNATURES = {
     "acrl_preference_workspace_bytes": (c_i64, [c_i32, c_i32]),
     "acrl_preference_loss": (c_i32, [c_p, c_p, c_p, c_i64, c_p, c_p, c_i32, c_p, c_i32, c_i32, c_f32, c_f32, c_f32, c_i32,
                                      c_p, c_p, c_p, c_p, c_i64, c_p, c_p]),
+    "acrl_preference_step_workspace_bytes": (c_i64, [c_i64, c_i32, c_i32]),
+    "acrl_preference_step": (c_i32, [c_p, c_i64, c_i64, c_i64, c_p, c_p, c_p, c_p, c_p, c_i32, c_p, c_i32, c_i32, c_f32, c_f32,
+                                     c_f32, c_i32, c_p, c_p, c_p, c_p, c_p, c_p, c_p, c_i64, c_p, c_p]),
     "acrl_read_flags": (c_i32, [c_p, ctypes.POINTER(c_i32), c_p]),
     "acrl_check_flags": (c_i32, [c_p, c_p]),
     "acrl_selftest_wait_timeout": (c_i32, [c_p, c_i64, c_p]),

@@ -37,20 +37,36 @@ def _one_device(tensors) -> torch.device:
     return first.device
 
 
+_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
+_ENTRY = {}    # the library's functions by name, as looked up
+
+
 def _call(name: str, tensors, stream, *args) -> None:
     """Call entry point `name` with `args` followed by the stream, on the GPU
     that holds `tensors` (the stream defaults to that GPU's current stream)."""
-    dev = _one_device(tensors)
-    if stream is not None and stream.device != dev:
-        raise AcrlError(f"{name}: stream on {stream.device}, buffers on {dev}")
-    fn = getattr(lib(), name)
-    index = dev.index
-    if index == torch._C._cuda_getDevice():
+    index = -1
+    for t in tensors:
+        if t is not None:
+            at = t.get_device()
+            if at != index:
+                if index >= 0 or at < 0 or not t.is_cuda:
+                    _one_device(tensors)    # says what is wrong
+                index = at
+    if index < 0:
+        _one_device(tensors)
+    if stream is not None and stream.device.index != index:
+        raise AcrlError(f"{name}: stream on {stream.device}, buffers on cuda:{index}")
+    fn = _ENTRY.get(name)
+    if fn is None:
+        fn = _ENTRY[name] = getattr(lib(), name)
+    if index == _current_device():
         # the current stream's handle without a Stream object around it
-        check(fn(*args, torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream), name)
-        return
-    with torch.cuda.device(dev):
-        check(fn(*args, torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream), name)
+        st = fn(*args, torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream)
+    else:
+        with torch.cuda.device(index):
+            st = fn(*args, torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream)
+    if st:
+        check(st, name)
 
 
 def _flags(flags, dev):
@@ -58,6 +74,9 @@ def _flags(flags, dev):
 
 
 def _need(t: torch.Tensor, dtype, n: int | None, name: str):
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.is_contiguous() and \
+            (n is None or t.numel() >= n):
+        return t
     if not isinstance(t, torch.Tensor):
         raise AcrlError(f"{name}: expected a torch tensor")
     if t.dtype != dtype:
@@ -510,24 +529,28 @@ def fp8_quantize(x, *, block="row", fmt="e4m3", transpose=False, out: Fp8Tensor 
                  stream=None) -> Fp8Tensor:
     """acrl_fp8_quantize: x (bf16 or float32 [R, C]) or its transpose as an 8-bit matrix with power-of-two scales per
     128 columns of a row (block="row") or per 128 x 128 ("tile")."""
-    if not isinstance(x, torch.Tensor) or x.dtype not in _OUT_DTYPE or x.dim() != 2 or not x.is_cuda or \
-            (x.shape[1] > 1 and x.stride(1) != 1):
-        raise AcrlError("x: expected a 2-D bfloat16 or float32 CUDA tensor with unit column stride")
-    if block not in _FP8_BLOCK:
-        raise AcrlError(f"block: {block!r}, expected one of {sorted(_FP8_BLOCK)}")
-    code = _fp8_format(fmt)
-    R, C = x.shape
+    if not isinstance(x, torch.Tensor) or x.dim() != 2 or not x.is_cuda:
+        raise AcrlError("x: expected a 2-D CUDA tensor")
+    xt = _OUT_DTYPE.get(x.dtype)
+    (R, C), (ldx, cs) = x.shape, x.stride()
+    if xt is None or (cs != 1 and C > 1):
+        raise AcrlError("x: expected bfloat16 or float32 with unit column stride")
+    kind = _FP8_BLOCK.get(block)
+    if kind is None or fmt not in _FP8:
+        raise AcrlError(f"block {block!r}, fmt {fmt!r}: expected one of {sorted(_FP8_BLOCK)} and one of {sorted(_FP8)}")
+    code, dtype = _FP8[fmt]
     rows, cols = (C, R) if transpose else (R, C)
-    srows, kb = (rows if block == "row" else (rows + 127) // 128), (cols + 127) // 128
+    srows, kb = (rows if kind == _abi.FP8_ROW else (rows + 127) // 128), (cols + 127) // 128
     if out is None:
-        out = Fp8Tensor(_padded((rows, cols), 16, _FP8[fmt][1], x.device),
-                        _padded((srows, kb), 4, torch.uint8, x.device))
-    elif tuple(out.q.shape) != (rows, cols) or out.q.dtype != _FP8[fmt][1] or out.scale.shape[0] != srows:
+        out = Fp8Tensor(_padded((rows, cols), 16, dtype, x.device), _padded((srows, kb), 4, torch.uint8, x.device))
+    elif tuple(out.q.shape) != (rows, cols) or out.q.dtype != dtype or out.scale.shape[0] != srows:
         raise AcrlError(f"out: an 8-bit matrix of another shape, format or block than {(rows, cols)} {fmt} {block}")
-    _opt(flags, torch.int32, 1, "flags")
-    ptr, _, ldq, _, sptr, lds, _ = _fp8_args(out, "out")
-    _call("acrl_fp8_quantize", (x, out.q, out.scale, flags), stream, _ptr(x), _OUT_DTYPE[x.dtype], R, C, _ld(x), code,
-          _FP8_BLOCK[block], int(transpose), ptr, ldq, sptr, lds, _ptr(flags))
+    if flags is not None:
+        _need(flags, torch.int32, 1, "flags")
+    ptr, _, ldq, _, sptr, lds, _ = out._args
+    _call("acrl_fp8_quantize", (x, out.q, out.scale, flags), stream, x.data_ptr(), xt, R, C,
+          ldx if R > 1 and C > 0 else (C + 15) // 16 * 16, code, kind, 1 if transpose else 0, ptr, ldq, sptr, lds,
+          None if flags is None else flags.data_ptr())
     return out
 
 
@@ -662,24 +685,41 @@ def policy_loss_grad_logits(logits, ids, mask, coef, *, V=None, old_logp=None, c
         if Tr < T or ref_logits.shape[1] < V:
             raise AcrlError(f"ref_logits: shape {tuple(ref_logits.shape)}, needs {(T, V)}")
     _need(ids, torch.int32, T, "ids")
-    _opt(mask, torch.uint8, T, "mask")
-    for name, t in (("coef", coef), ("kl_coef", kl_coef), ("old_logp", old_logp), ("ref_logp", ref_logp)):
-        _opt(t, torch.float32, T, name)
+    f32 = torch.float32
+    if mask is not None:
+        _need(mask, torch.uint8, T, "mask")
+    if coef is not None:
+        _need(coef, f32, T, "coef")
+    if kl_coef is not None:
+        _need(kl_coef, f32, T, "kl_coef")
+    if old_logp is not None:
+        _need(old_logp, f32, T, "old_logp")
+    if ref_logp is not None:
+        _need(ref_logp, f32, T, "ref_logp")
     if grad is None:
         grad = torch.empty((T, ld), dtype=torch.bfloat16, device=dev)
     elif grad.dtype != torch.bfloat16 or grad.dim() != 2 or grad.stride(0) != ld or grad.stride(1) != 1 or \
             grad.shape[0] < T:
         raise AcrlError("grad: expected a bf16 [T, ld] tensor with the logits' row stride")
-    f32 = torch.float32
-    logp, token_loss = _vec(logp, f32, T, "logp", dev), _vec(token_loss, f32, T, "token_loss", dev)
-    kl_out = None if kl is None else _vec(kl_out, f32, T, "kl_out", dev)
+    if logp is None and token_loss is None and kl_out is None:   # one allocation for the three
+        three = torch.empty((3, (T + 3) // 4 * 4), dtype=f32, device=dev)   # each on 16 bytes
+        logp, token_loss, kl_out = (three if T % 4 == 0 else three[:, :T]).unbind(0)
+    else:
+        logp, token_loss = _vec(logp, f32, T, "logp", dev), _vec(token_loss, f32, T, "token_loss", dev)
+        kl_out = None if kl is None else _vec(kl_out, f32, T, "kl_out", dev)
+    if kl is None:
+        kl_out = None
     loss = _vec(loss, f32, 1, "loss", dev)
-    _opt(flags, torch.int32, 1, "flags")
+    if flags is not None:
+        _need(flags, torch.int32, 1, "flags")
     _call("acrl_policy_loss_grad_logits",
           (logits, ids, mask, old_logp, coef, kl_coef, ref_logits, ref_logp, grad, logp, kl_out, token_loss, loss, flags),
-          stream, _ptr(logits), T, V, ld, _ptr(ids), _ptr(mask), _ptr(old_logp), _ptr(coef), float(clip_low),
-          float(clip_high), float(dual_clip), _KL[kl], _ptr(kl_coef), _ptr(ref_logits), ldr, _ptr(ref_logp), _ptr(grad),
-          _ptr(logp), _ptr(kl_out), _ptr(token_loss), _ptr(loss), _ptr(flags))
+          stream, logits.data_ptr(), T, V, ld, ids.data_ptr(), None if mask is None else mask.data_ptr(),
+          None if old_logp is None else old_logp.data_ptr(), None if coef is None else coef.data_ptr(), clip_low, clip_high,
+          dual_clip, _KL[kl], None if kl_coef is None else kl_coef.data_ptr(),
+          None if ref_logits is None else ref_logits.data_ptr(), ldr, None if ref_logp is None else ref_logp.data_ptr(),
+          grad.data_ptr(), logp.data_ptr(), None if kl_out is None else kl_out.data_ptr(), token_loss.data_ptr(),
+          loss.data_ptr(), None if flags is None else flags.data_ptr())
     return PolicyLoss(grad, logp, kl_out, token_loss, loss)
 
 
@@ -712,14 +752,54 @@ def preference_loss(logp, ref_logp, mask, rewards, seq_offsets, group_offsets, *
     _need(seq_offsets, torch.int64, S + 1, "seq_offsets")
     _need(group_offsets, torch.int32, Gn + 1, "group_offsets")
     ratio, coef, loss = _vec(ratio, f32, S, "ratio", dev), _vec(coef, f32, T, "coef", dev), _vec(loss, f32, 1, "loss", dev)
-    workspace = _vec(workspace, torch.uint8, preference_workspace_bytes(S, Gn), "workspace", dev)
-    _opt(flags, torch.int32, 1, "flags")
+    n = lib().acrl_preference_workspace_bytes(S, Gn)
+    workspace = _vec(workspace, torch.uint8, n, "workspace", dev)
+    if flags is not None:
+        _need(flags, torch.int32, 1, "flags")
     _call("acrl_preference_loss",
           (logp, ref_logp, mask, rewards, seq_offsets, group_offsets, ratio, coef, loss, workspace, flags), stream,
-          _ptr(logp), _ptr(ref_logp), _ptr(mask), T, _ptr(rewards), _ptr(seq_offsets), S, _ptr(group_offsets), Gn,
-          _PREF[form], float(beta), float(margin), float(label_smoothing), int(length_norm), _ptr(ratio), _ptr(coef),
-          _ptr(loss), _ptr(workspace), workspace.numel(), _ptr(flags))
+          logp.data_ptr(), None if ref_logp is None else ref_logp.data_ptr(), None if mask is None else mask.data_ptr(), T,
+          rewards.data_ptr(), seq_offsets.data_ptr(), S, group_offsets.data_ptr(), Gn, _PREF[form], beta, margin,
+          label_smoothing, int(length_norm), ratio.data_ptr(), coef.data_ptr(), loss.data_ptr(), workspace.data_ptr(), n,
+          None if flags is None else flags.data_ptr())
     return Preference(loss, coef, ratio)
+
+
+def preference_step_workspace_bytes(T: int, S: int, Gn: int) -> int:
+    """acrl_preference_step_workspace_bytes."""
+    return int(lib().acrl_preference_step_workspace_bytes(T, S, Gn))
+
+
+def preference_step(logits, ids, mask, ref_logp, rewards, seq_offsets, group_offsets, *, V, lse, logp, ratio, coef, grad, loss,
+                    workspace, flags, beta=0.1, form="sigmoid", margin=0.0, label_smoothing=0.0, length_norm=False,
+                    stream=None) -> None:
+    """acrl_preference_step, into the caller's buffers."""
+    T, ld = _rows(logits, "logits")
+    S, Gn = seq_offsets.numel() - 1, group_offsets.numel() - 1
+    f32 = torch.float32
+    if form not in _PREF:
+        raise AcrlError(f"form: {form!r}, expected one of {list(_PREF)}")
+    _need(ids, torch.int32, T, "ids")
+    if mask is not None:
+        _need(mask, torch.uint8, T, "mask")
+    if ref_logp is not None:
+        _need(ref_logp, f32, T, "ref_logp")
+    _need(rewards, f32, S, "rewards")
+    _need(seq_offsets, torch.int64, S + 1, "seq_offsets")
+    _need(group_offsets, torch.int32, Gn + 1, "group_offsets")
+    for name, t, n in (("lse", lse, T), ("logp", logp, T), ("ratio", ratio, S), ("coef", coef, T), ("loss", loss, 1)):
+        _need(t, f32, n, name)
+    if grad.dtype != torch.bfloat16 or grad.dim() != 2 or grad.stride(0) != ld or grad.stride(1) != 1 or grad.shape[0] < T:
+        raise AcrlError("grad: expected a bf16 [T, ld] tensor with the logits' row stride")
+    _need(flags, torch.int32, 1, "flags")
+    _need(workspace, torch.uint8, None, "workspace")
+    _call("acrl_preference_step", (logits, ids, mask, ref_logp, rewards, seq_offsets, group_offsets, lse, logp, ratio, coef, grad,
+                                   loss, workspace, flags), stream,
+          logits.data_ptr(), T, V, ld, ids.data_ptr(), None if mask is None else mask.data_ptr(),
+          None if ref_logp is None else ref_logp.data_ptr(), rewards.data_ptr(), seq_offsets.data_ptr(), S,
+          group_offsets.data_ptr(), Gn, _PREF[form], beta, margin, label_smoothing, int(length_norm), lse.data_ptr(),
+          logp.data_ptr(), ratio.data_ptr(), coef.data_ptr(), grad.data_ptr(), loss.data_ptr(), workspace.data_ptr(),
+          workspace.numel(), flags.data_ptr())
 
 
 def selftest_wait_timeout(flags, limit_ns: int, stream=None) -> None:
@@ -825,6 +905,7 @@ __all__ = ["Params", "AcrlError", "token_stats", "seq_discrepancy", "grpo_advant
            "controller_step", "importance_weights", "step", "loss_grad_logits", "reduce_loss", "scale_grad",
            "read_flags", "check_flags", "read_state", "Discrepancy",
            "PolicyLoss", "policy_loss_grad_logits", "Preference", "preference_loss", "preference_workspace_bytes",
+           "preference_step", "preference_step_workspace_bytes",
            "Fp8Tensor", "fp8_quantize", "fp8_matmul", "fp8_linear", "fp8_linear_backward", "fp8_linear_workspace_bytes",
            "fp8_linear_backward_workspace_bytes",
            "lmhead_logits_stats", "lmhead_merge", "lmhead_workspace_bytes", "lmhead_stats_noalloc", "save_state",

@@ -31,6 +31,7 @@
 #include "acrl_device.cuh"
 #include "acrl_host.h"
 #include "mbarrier.cuh"
+#include "row_logp.h"
 #include "row_lse.cuh"
 
 namespace acrl {
@@ -353,7 +354,9 @@ __device__ __forceinline__ int row_scalars(const PolicyArgs& A, int64_t t, const
     float slope = 0.f;                                                            // of the sampled estimators, in logp
     if constexpr (KIND != kSampled) {
         const float lx = kLn2 * (log2f(row.sx) - fmaf(row.mx, kLog2e, -row.W));
-        apart = (row.mz - row.mx) + (lz - lx);
+        // the logarithm of the sums' ratio, not the difference of two logarithms whose roundings KL would carry whole
+        const float diff = row.sz - row.sx, ratio = fabsf(diff) < 0.5f * row.sx ? log1pf(diff / row.sx) : logf(row.sz / row.sx);
+        apart = (row.mz - row.mx) + (ratio - kLn2 * (fmaf(row.mz, kLog2e, -row.U) - fmaf(row.mx, kLog2e, -row.W)));
         logq = (xa - row.mx) - lx;
         KL = KIND == kExact ? row.cross / row.sz - apart : row.cross / row.sx + apart;
         g.W = row.W + log2f(row.sx);
@@ -683,6 +686,43 @@ __global__ void __launch_bounds__(THREADS, PER_SM) policy_kernel(const __grid_co
     }
 }
 
+// The statistics alone: lse and the sampled token's log-prob, one row a CTA, nothing kept.  Sums against fixed exponents leave
+// the log-probs without a bias, which a sum over a response's tokens would carry: their mean error over rows of 151,936
+// columns is 1e-8 (5e-7 rms), that of an online log-softmax whose sums are rescaled at every new maximum 1.4e-7.
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_kernel(const __grid_constant__ PolicyArgs A, float* __restrict__ lse) {
+    constexpr int kWarps = THREADS / 32;
+    __shared__ __align__(16) Shared<THREADS> sh;
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+    const int64_t t = blockIdx.x;
+    Cta<kSampled, THREADS> cta{A, sh, nullptr, nullptr, 0, A.V >> 3, 0, true};
+    grid_begin();
+    const bool masked = A.mask && A.mask[t] == 0;
+    if (masked) {
+        if (tid == 0) lse[t] = A.logp[t] = 0.f;
+        return;
+    }
+    const int a = A.ids[t];
+    const bool in = a >= 0 && a < A.V;
+    const float za = in && tid == 0 ? bf16_to_float(A.z[t * A.ldz + a]) : 0.f;
+    bool careful;
+    State st = cta.fold_row(t, careful);
+    if (kWarps > 1) {
+        if (lane == 0) put(sh.warps[wid], st, careful);
+        __syncthreads();
+        if (wid != 0) return;
+        const State none = empty_state();
+        st = meet<kSampled, 32>(lane < kWarps ? get(sh.warps[lane]) : none);
+    }
+    if (tid != 0) return;
+    const float lz = kLn2 * (log2f(st.sz) - fmaf(st.mz, kLog2e, -st.U)), l = st.mz + lz, lp = in ? (za - st.mz) - lz : 0.f;
+    if (!in) raise_flag(A.flags, ACRL_FLAG_BAD_ID);
+    const bool fine = isfinite(l) && isfinite(lp);
+    if (!fine) raise_flag(A.flags, ACRL_FLAG_NONFINITE);
+    lse[t] = fine ? l : __int_as_float(0x7fc00000);
+    A.logp[t] = fine ? lp : __int_as_float(0x7fc00000);
+}
+
 constexpr int kSmBytes = 227 * 1024;
 
 // CTAs of long rows all begin together, and as their rows take equally long, HBM then reads and writes in turn.  So the first
@@ -748,6 +788,26 @@ acrl_status launch_policy(const PolicyArgs& A, cudaStream_t s) {
 }
 
 }  // namespace
+
+acrl_status row_logp(const acrl_bf16* logits, int64_t T, int64_t V, int64_t ld, const int32_t* ids, const uint8_t* mask, float* lse,
+                     float* logp, int32_t* flags, cudaStream_t s) {
+    PolicyArgs A = {};
+    A.V = int(V);
+    A.ldz = ld;
+    A.flags = flags;
+    for (int64_t t = 0; t < T; t += kMaxGrid) {
+        A.z = logits + t * ld;
+        A.ids = ids + t;
+        A.mask = mask ? mask + t : nullptr;
+        A.logp = logp + t;
+        A.T = std::min(kMaxGrid, T - t);
+        auto run = [&](auto* kernel, int threads) { return launch(kernel, A.T, threads, 0, 0, s, A, lse + t); };
+        const acrl_status st = V <= 4096 ? run(logp_kernel<32>, 32) : V <= 16384 ? run(logp_kernel<64>, 64) : V <= 65536 ? run(logp_kernel<128>, 128) : run(logp_kernel<256>, 256);
+        if (st != ACRL_OK) return st;
+    }
+    return ACRL_OK;
+}
+
 }  // namespace acrl
 
 using namespace acrl;

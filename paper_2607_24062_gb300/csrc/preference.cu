@@ -14,6 +14,7 @@
 
 #include "acrl_device.cuh"
 #include "acrl_host.h"
+#include "row_logp.h"
 
 namespace acrl {
 namespace {
@@ -59,11 +60,24 @@ __global__ void __launch_bounds__(kRespThreads)
     }
     double sum = 0.0;
     int n = 0;
-    for (int64_t t = lo + threadIdx.x; t < hi; t += kRespThreads)
-        if (!mask || mask[t]) {
-            sum += double(logp[t]) - (ref ? double(ref[t]) : 0.0);
-            ++n;
+    // four tokens a thread in flight; differences and sums in fp64 (with fp32 differences a sum near 0 had lost three digits)
+    for (int64_t t0 = lo + threadIdx.x; t0 < hi; t0 += 4 * kRespThreads) {
+        bool in[4];
+        float a[4], b[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int64_t t = t0 + k * kRespThreads;
+            in[k] = t < hi && !(mask && mask[t] == 0);
+            a[k] = t < hi ? logp[t] : 0.f;
+            b[k] = t < hi && ref ? ref[t] : 0.f;
         }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (in[k]) {
+                sum += double(a[k]) - double(b[k]);
+                ++n;
+            }
+    }
     sum = warp_sum(sum);
     n = __reduce_add_sync(0xffffffffu, n);
     if (lane == 0) {
@@ -105,6 +119,8 @@ __global__ void __launch_bounds__(kPairThreads)
     constexpr int NW = kPairThreads / 32;
     __shared__ double sums[NW];
     __shared__ long long pairs[NW];
+    __shared__ float their_reward[kPairThreads];
+    __shared__ double their_ratio[kPairThreads];
     const int g = blockIdx.x, lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
     grid_begin();
     int lo = go[g], hi = go[g + 1];
@@ -112,20 +128,29 @@ __global__ void __launch_bounds__(kPairThreads)
     if (!ok) lo = hi = 0;
     if ((g == 0 && go[0] != 0) || (g == Gn - 1 && go[Gn] != S)) ok = false;
     if (!ok && threadIdx.x == 0) raise_flag(flags, ACRL_FLAG_BAD_OFFSETS);
-    auto valid = [&](int i) { return w.count[i] > 0; };
     long long n = 0;
     double loss = 0.0;
-    for (int i = lo + int(threadIdx.x); i < hi; i += kPairThreads) {
-        const float Ri = rewards[i];
-        if (isnan(Ri)) raise_flag(flags, ACRL_FLAG_NONFINITE);
-        double slope = 0.0;
-        if (valid(i)) {
-            const double Di = w.ratio[i];
-            for (int j = lo; j < hi; ++j) {
-                const float Rj = rewards[j];
-                if (!(Ri > Rj || Rj > Ri) || !valid(j)) continue;
+    // pairs with the responses [j0, j1) of the prompt, which lie in shared memory; kPairThreads of them at a time
+    for (int j0 = lo; j0 < hi; j0 += kPairThreads) {
+        const int j1 = min(hi, j0 + kPairThreads), mine = j0 + int(threadIdx.x);
+        __syncthreads();
+        if (mine < j1) {
+            const float R = rewards[mine];
+            if (isnan(R)) raise_flag(flags, ACRL_FLAG_NONFINITE);
+            their_reward[threadIdx.x] = w.count[mine] > 0 ? R : __int_as_float(0x7fc00000);   // NaN: no pair
+            their_ratio[threadIdx.x] = w.ratio[mine];
+        }
+        __syncthreads();
+        for (int i = lo + int(threadIdx.x); i < hi; i += kPairThreads) {
+            const bool here = i >= j0 && i < j1;
+            const float Ri = here ? their_reward[i - j0] : w.count[i] > 0 ? rewards[i] : __int_as_float(0x7fc00000);
+            const double Di = here ? their_ratio[i - j0] : w.ratio[i];
+            double slope = j0 == lo ? 0.0 : w.slope[i];
+            for (int j = 0; j < j1 - j0; ++j) {
+                const float Rj = their_reward[j];
+                if (!(Ri > Rj || Rj > Ri)) continue;
                 const bool wins = Ri > Rj;
-                const double d = Di - w.ratio[j];
+                const double d = Di - their_ratio[j];
                 const float2 v = pair_loss(f, float(double(f.beta) * (wins ? d : -d) - double(f.margin)));
                 if (wins) {
                     loss += v.x;
@@ -135,8 +160,8 @@ __global__ void __launch_bounds__(kPairThreads)
                     slope -= v.y;
                 }
             }
+            w.slope[i] = slope;
         }
-        w.slope[i] = slope;
     }
     loss = warp_sum(loss);
     n = warp_sum(n);
@@ -185,12 +210,26 @@ __global__ void __launch_bounds__(kRespThreads)
     int64_t lo, hi;
     if (!range_of(so, i, T, lo, hi)) return;
     const float c = Q > 0 ? float(-w.slope[i] / Q) : 0.f;
+#pragma unroll 4
     for (int64_t t = lo + threadIdx.x; t < hi; t += kRespThreads) coef[t] = !mask || mask[t] ? c : 0.f;
 }
 
 constexpr int64_t kPrefHead = 16;
 
 int64_t work_bytes(int64_t S, int64_t Gn) { return kPrefHead + 8 * (2 * S + Gn) + 4 * S; }
+
+bool pairs_ok(const float* logp, int64_t T, const float* rewards, const int64_t* seq_offsets, int32_t S, const int32_t* group_offsets,
+              int32_t Gn, acrl_preference_form form, float beta, float margin, float label_smoothing, const float* ratio,
+              const float* coef, const float* loss) {
+    if (T < 0 || S < 0 || Gn < 0 || S == 0x7fffffff || !loss) return false;
+    if (form < ACRL_PREF_SIGMOID || form > ACRL_PREF_IPO) return false;
+    if (!(beta > 0.f) || !std::isfinite(beta) || !std::isfinite(margin)) return false;
+    if (!(label_smoothing >= 0.f && label_smoothing < 0.5f)) return false;
+    if (T > 0 && (!logp || !coef)) return false;
+    if (S > 0 && (!rewards || !seq_offsets || !ratio)) return false;
+    if (Gn > 0 && !group_offsets) return false;
+    return !((S == 0 && T > 0) || (Gn == 0 && S > 0));   // offsets that cannot cover
+}
 
 }  // namespace
 }  // namespace acrl
@@ -207,15 +246,9 @@ extern "C" acrl_status acrl_preference_loss(const float* logp, const float* ref_
                                             float margin, float label_smoothing, int32_t length_norm, float* ratio,
                                             float* coef, float* loss, void* workspace, int64_t workspace_bytes,
                                             int32_t* dev_flags, acrl_stream stream) {
-    if (T < 0 || S < 0 || Gn < 0 || S == 0x7fffffff || !loss) return ACRL_ERR_INVALID_ARG;
-    if (form < ACRL_PREF_SIGMOID || form > ACRL_PREF_IPO) return ACRL_ERR_INVALID_ARG;
-    if (!(beta > 0.f) || !std::isfinite(beta) || !std::isfinite(margin)) return ACRL_ERR_INVALID_ARG;
-    if (!(label_smoothing >= 0.f && label_smoothing < 0.5f)) return ACRL_ERR_INVALID_ARG;
+    if (!pairs_ok(logp, T, rewards, seq_offsets, S, group_offsets, Gn, form, beta, margin, label_smoothing, ratio, coef, loss))
+        return ACRL_ERR_INVALID_ARG;
     if (!workspace || !aligned16(workspace) || workspace_bytes < work_bytes(S, Gn)) return ACRL_ERR_INVALID_ARG;
-    if (T > 0 && (!logp || !coef)) return ACRL_ERR_INVALID_ARG;
-    if (S > 0 && (!rewards || !seq_offsets || !ratio)) return ACRL_ERR_INVALID_ARG;
-    if (Gn > 0 && !group_offsets) return ACRL_ERR_INVALID_ARG;
-    if ((S == 0 && T > 0) || (Gn == 0 && S > 0)) return ACRL_ERR_INVALID_ARG;   // offsets that cannot cover
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     char* p = static_cast<char*>(workspace);
     PrefWork w;
@@ -233,4 +266,37 @@ extern "C" acrl_status acrl_preference_loss(const float* logp, const float* ref_
     st = launch(pref_pairs, Gn, kPairThreads, 0, 0, s, rewards, group_offsets, Gn, S, f, w, dev_flags);
     if (st != ACRL_OK) return st;
     return launch(pref_tokens, int64_t(S) + 1, kRespThreads, 0, 0, s, mask, T, seq_offsets, S, Gn, w, coef, loss);
+}
+
+// The step's workspace: that of the pairs, then the gradient call's own sums, which nothing reads.
+static int64_t step_bytes(int64_t T, int64_t S, int64_t Gn) { return (work_bytes(S, Gn) + 15) / 16 * 16 + 16 + 4 * T; }
+
+extern "C" int64_t acrl_preference_step_workspace_bytes(int64_t T, int32_t S, int32_t Gn) {
+    return T < 0 || S < 0 || Gn < 0 ? -1 : step_bytes(T, S, Gn);
+}
+
+extern "C" acrl_status acrl_preference_step(const acrl_bf16* logits, int64_t T, int64_t V, int64_t ld, const int32_t* ids,
+                                            const uint8_t* mask, const float* ref_logp, const float* rewards,
+                                            const int64_t* seq_offsets, int32_t S, const int32_t* group_offsets, int32_t Gn,
+                                            acrl_preference_form form, float beta, float margin, float label_smoothing,
+                                            int32_t length_norm, float* lse, float* logp, float* ratio, float* coef,
+                                            acrl_bf16* grad, float* loss, void* workspace, int64_t workspace_bytes,
+                                            int32_t* dev_flags, acrl_stream stream) {
+    if (T < 0 || V < 1 || V > kMaxVocab || ld < V || (ld & 7) != 0 || S < 0 || Gn < 0) return ACRL_ERR_INVALID_ARG;
+    if (!dev_flags || !workspace || !aligned16(workspace) || workspace_bytes < step_bytes(T, S, Gn)) return ACRL_ERR_INVALID_ARG;
+    if (T > 0 && (!logits || !aligned16(logits) || !ids || !lse || !logp || !coef || !grad || !aligned16(grad)))
+        return ACRL_ERR_INVALID_ARG;
+    const int64_t head = (work_bytes(S, Gn) + 15) / 16 * 16;
+    if (!pairs_ok(logp, T, rewards, seq_offsets, S, group_offsets, Gn, form, beta, margin, label_smoothing, ratio, coef, loss))
+        return ACRL_ERR_INVALID_ARG;
+    if (T > 0) {
+        const acrl_status st = row_logp(logits, T, V, ld, ids, mask, lse, logp, dev_flags, reinterpret_cast<cudaStream_t>(stream));
+        if (st != ACRL_OK) return st;
+    }
+    acrl_status st = acrl_preference_loss(logp, ref_logp, mask, T, rewards, seq_offsets, S, group_offsets, Gn, form, beta, margin,
+                                          label_smoothing, length_norm, ratio, coef, loss, workspace, head, dev_flags, stream);
+    if (st != ACRL_OK || T == 0) return st;
+    float* scratch = reinterpret_cast<float*>(static_cast<char*>(workspace) + head);
+    return acrl_loss_grad_logits(logits, T, V, ld, ids, mask, lse, nullptr, coef, nullptr, nullptr, 0.f, grad, scratch + 4, scratch,
+                                 dev_flags, stream);
 }

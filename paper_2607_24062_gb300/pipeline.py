@@ -216,38 +216,34 @@ def _host(t, dtype, n, name):
 
 
 class PreferenceStep:
-    """A preference step over a batch of responses: statistics of the logits, the pairs of each prompt and dL/dlogits,
-    the calls in order on one stream, with every buffer allocated once.
+    """A preference step over a batch of responses: log-probs of the logits, the pairs of each prompt and dL/dlogits in one
+    call, with every buffer allocated once.
 
         step = PreferenceStep(T, V, ld, S, Gn, beta=0.1)
         step.run(logits, ids, mask, ref_logp, rewards, seq_offsets, group_offsets)
-        step.grad, step.loss, step.ratio, step.coef
+        step.grad, step.loss, step.ratio, step.coef, step.logp
 
     The responses of a prompt are paired by their rewards, so that a batch sampled for a policy loss serves as it is;
     a chosen and a rejected answer are a prompt of two with rewards 1 and 0.  Keywords are preference_loss's."""
 
-    def __init__(self, T: int, V: int, ld: int, S: int, Gn: int, *, device="cuda", grad=None, **loss_kw):
+    def __init__(self, T: int, V: int, ld: int, S: int, Gn: int, *, device="cuda", grad=None, beta=0.1, form="sigmoid",
+                 margin=0.0, label_smoothing=0.0, length_norm=False):
         dev = torch.device(device)
         f32 = dict(dtype=torch.float32, device=dev)
         self.T, self.V, self.ld, self.S, self.Gn = T, V, ld, S, Gn
-        self.loss_kw = loss_kw
-        self.lse, self.logp, self.entropy, self.coef, self._surrogate = (torch.empty(T, **f32) for _ in range(5))
-        self.ratio = torch.empty(S, **f32)
-        self.loss, self._surrogate_sum = torch.empty(1, **f32), torch.empty(1, **f32)
+        self.loss_kw = dict(beta=beta, form=form, margin=margin, label_smoothing=label_smoothing, length_norm=length_norm)
+        self.lse, self.logp, self.coef = (torch.empty(T, **f32) for _ in range(3))
+        self.ratio, self.loss = torch.empty(S, **f32), torch.empty(1, **f32)
         self.grad = torch.empty((T, ld), dtype=torch.bfloat16, device=dev) if grad is None else grad
-        self.workspace = torch.empty(api.preference_workspace_bytes(S, Gn), dtype=torch.uint8, device=dev)
+        self.workspace = torch.empty(api.preference_step_workspace_bytes(T, S, Gn), dtype=torch.uint8, device=dev)
         self.flags = api.new_flags(dev)
 
     def run(self, logits, ids, mask, ref_logp, rewards, seq_offsets, group_offsets, stream=None):
         if logits.shape[0] != self.T or seq_offsets.numel() != self.S + 1 or group_offsets.numel() != self.Gn + 1:
             raise AcrlError(f"expected {self.T} rows, {self.S} responses and {self.Gn} prompts")
-        api.token_stats(logits, ids, mask, V=self.V, lse=self.lse, logp=self.logp, entropy=self.entropy, flags=self.flags,
-                        stream=stream)
-        api.preference_loss(self.logp, ref_logp, mask, rewards, seq_offsets, group_offsets, ratio=self.ratio,
-                            coef=self.coef, loss=self.loss, workspace=self.workspace, flags=self.flags, stream=stream,
-                            **self.loss_kw)
-        api.loss_grad_logits(logits, ids, mask, self.lse, None, self.coef, 0.0, V=self.V, grad=self.grad,
-                             token_loss=self._surrogate, loss=self._surrogate_sum, flags=self.flags, stream=stream)
+        api.preference_step(logits, ids, mask, ref_logp, rewards, seq_offsets, group_offsets, V=self.V, lse=self.lse,
+                            logp=self.logp, ratio=self.ratio, coef=self.coef, grad=self.grad, loss=self.loss,
+                            workspace=self.workspace, flags=self.flags, stream=stream, **self.loss_kw)
 
 
 class HostPipeline:

@@ -97,3 +97,16 @@ def test_preference_loss(L):
                 dict(Gn=0), dict(S=0), dict(form=3), dict(form=-1), dict(beta=0.0), dict(beta=float("inf")),
                 dict(margin=float("nan")), dict(smooth=0.5), dict(smooth=-0.1)):
         assert _call(L.acrl_preference_loss, ok, **bad) == E, bad
+
+
+def test_preference_step(L):
+    assert L.acrl_preference_step_workspace_bytes(-1, 1, 1) == -1
+    n = L.acrl_preference_step_workspace_bytes(9, 4, 2)
+    ok = dict(z=FAKE, T=9, V=16, ld=16, ids=FAKE, mask=None, ref=None, rewards=FAKE, so=FAKE, S=4, go=FAKE, Gn=2, form=0,
+              beta=0.1, margin=0.0, smooth=0.0, mean=0, lse=FAKE, logp=FAKE, ratio=FAKE, coef=FAKE, grad=FAKE, loss=FAKE,
+              ws=FAKE, n=n, flags=FAKE, stream=None)
+    for bad in (dict(z=None), dict(ids=None), dict(rewards=None), dict(so=None), dict(go=None), dict(lse=None), dict(logp=None),
+                dict(ratio=None), dict(coef=None), dict(grad=None), dict(loss=None), dict(ws=None), dict(flags=None),
+                dict(n=n - 1), dict(ws=FAKE + 4), dict(z=FAKE + 2), dict(grad=FAKE + 8), dict(T=-1), dict(V=0), dict(ld=8),
+                dict(ld=20), dict(S=-1), dict(S=0), dict(Gn=0), dict(form=3), dict(beta=-1.0), dict(smooth=0.5)):
+        assert _call(L.acrl_preference_step, ok, **bad) == E, bad

@@ -174,6 +174,55 @@ def test_step_from_logits():
     assert torch.allclose(y.grad[:, :V].float(), 2.0 * step.grad[:, :V].float(), rtol=2.0 ** -8)
 
 
+@pytest.mark.parametrize("V,gap", [(1, 0), (7, 8), (64, 0), (4096, 0), (5003, 8), (20011, 0), (70001, 0), (151936, 0)])
+def test_log_probs_of_the_step(V, gap):
+    """lse and logp of the step's rows: fp32 sums (4e-6 + 2e-7 of the number, as for the policy loss), masked rows and bad ids,
+    undefined rows; and no bias that a response's tokens would add up."""
+    T = 96 if V < 60000 else 40
+    g = torch.Generator(device=DEV).manual_seed(V)
+    ld = (V + 7) // 8 * 8 + gap
+    z = (2 * torch.randn((T, ld), generator=g, device=DEV)).to(torch.bfloat16)
+    ids = torch.randint(0, V, (T,), generator=g, device=DEV, dtype=torch.int32)
+    mask = torch.ones(T, dtype=torch.uint8, device=DEV)
+    mask[::5] = 0
+    z[5] = math.nan                                 # masked: not looked at
+    ids[1] = V
+    z[2, 0] = math.nan
+    z[3, :V] = -math.inf
+    if V > 1:
+        z[4, V - 1] = -math.inf                     # a column taken out
+        ids[4] = 0
+        z[6, :V] = -3.3895313892515355e38           # all but one
+        z[6, 0], ids[6] = 1.0, 0
+    step = acrl.PreferenceStep(T, V, ld, 2, 1)
+    so, go = torch.tensor([0, T // 2, T], device=DEV), torch.tensor([0, 2], dtype=torch.int32, device=DEV)
+    step.run(z, ids, mask, None, torch.tensor([1.0, 0.0], device=DEV), so, go)
+    assert acrl.read_flags(step.flags) == acrl.FLAG_BAD_ID | acrl.FLAG_NONFINITE
+    lse = torch.logsumexp(z[:, :V].double(), 1)
+    lp = z[:, :V].gather(1, ids.clamp(max=V - 1).long()[:, None])[:, 0].double() - lse
+    live = mask.bool()
+    assert not bool(step.logp[~live].any()) and not bool(step.lse[~live].any()) and float(step.logp[1]) == 0
+    assert bool(step.logp[[2, 3]].isnan().all()) and bool(step.lse[[2, 3]].isnan().all())
+    live[[1, 2, 3]] = False
+    for got, want in ((step.lse, lse), (step.logp, lp)):
+        assert bool(((got - want).abs() <= 4e-6 + 2e-7 * want.abs())[live].all())
+
+
+def test_sums_of_many_tokens():
+    """The log ratio of 1,500 tokens against a reference that is the policy itself, rounded to fp32: what is left are the
+    log-probs' own errors.  Each is below 4e-6 + 2e-7 |logp| in size and their signs mix; a bias of 1e-7 would make 1.5e-4."""
+    T, V = 1500, 32000
+    g = torch.Generator(device=DEV).manual_seed(4)
+    z = (2 * torch.randn((T, V), generator=g, device=DEV)).to(torch.bfloat16)
+    ids = torch.randint(0, V, (T,), generator=g, device=DEV, dtype=torch.int32)
+    lp = torch.log_softmax(z.double(), 1).gather(1, ids.long()[:, None])[:, 0]
+    step = acrl.PreferenceStep(T, V, V, 1, 1)
+    step.run(z, ids, None, lp.float(), torch.ones(1, device=DEV), torch.tensor([0, T], device=DEV),
+             torch.tensor([0, 1], dtype=torch.int32, device=DEV))
+    # 6 standard deviations of 1,500 errors of 1e-6 (fp32's spacing at 16), the reference's own rounding among them
+    assert abs(float(step.ratio)) <= 6 * 1e-6 * math.sqrt(T) / 2
+
+
 def test_refusals():
     b = _batch([2, 2], [5], 9)
     for change in (dict(logp=b["logp"].double()), dict(ref=b["ref"][:3]), dict(mask=b["mask"].bool()),
