@@ -522,7 +522,9 @@ def _fp8_format(fmt: str) -> int:
 
 def _padded(shape, to: int, dtype, dev) -> torch.Tensor:
     """A new matrix with its rows at a stride that is a multiple of `to`."""
-    return torch.empty_strided(shape, ((shape[1] + to - 1) // to * to, 1), dtype=dtype, device=dev)
+    ld = (shape[1] + to - 1) // to * to
+    x = torch.empty((shape[0], ld), dtype=dtype, device=dev)
+    return x if ld == shape[1] else x[:, : shape[1]]
 
 
 def fp8_quantize(x, *, block="row", fmt="e4m3", transpose=False, out: Fp8Tensor | None = None, flags=None,

@@ -246,6 +246,27 @@ class PreferenceStep:
                             workspace=self.workspace, flags=self.flags, stream=stream, **self.loss_kw)
 
 
+class Fp8Head:
+    """An LM head whose weights are held as 8-bit tiles, quantised once: a frozen reference policy's, or the numerics of
+    an engine that serves in FP8.
+
+        ref = Fp8Head(weight)                       # bf16 [V, K]
+        policy_loss_grad_logits(..., kl="exact", ref_logits=ref.logits(hidden))
+        preference.run(..., ref_logp=ref.logp(hidden, ids, mask), ...)"""
+
+    def __init__(self, weight: torch.Tensor, fmt="e4m3"):
+        self.weight = api.fp8_quantize(weight, block="tile", fmt=fmt)
+
+    def logits(self, hidden, *, out=None, workspace=None, flags=None, stream=None):
+        """bf16 [T, V] logits of hidden (bf16 [T, K]), quantised by rows; the row stride is V rounded up to 8."""
+        return api.fp8_linear(hidden, self.weight, out=out, workspace=workspace, flags=flags, stream=stream)
+
+    def logp(self, hidden, ids, mask=None, *, out=None, flags=None, stream=None):
+        """float32 [T] log-probs of the sampled tokens (0 where masked)."""
+        z = self.logits(hidden, out=out, flags=flags, stream=stream)
+        return api.token_stats(z, ids, mask, V=z.shape[1], flags=flags, stream=stream)[1]
+
+
 class HostPipeline:
     """acrl_host_pipeline_*: the whole on-policy pass for batches whose inputs
     and outputs are host tensors (page-locked for the copies to overlap),
