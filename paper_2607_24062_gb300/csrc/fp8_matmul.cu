@@ -26,7 +26,9 @@
 //   256 x 224 x 1 products where a CTA alone would load 352: the way from L2 into shared
 //   memory bounds the product.  The even CTA's thread issues the MMAs, which read
 //   both CTAs' shared memory and each CTA's own tensor memory (accumulator, the
-//   scales of its own rows and of all columns).  Persistent over the tiles.
+//   scales of its own rows and of all columns).  Persistent over the tiles.  Where there
+//   are tiles enough, or K is long, a tile has 320 to 448 columns: 176 bytes for as many products,
+//   in two parts of one accumulator, each drained by the epilogue while the other's MMAs run.
 // Alone (few rows): P is the wide operand, the weight, and the few rows are the
 //   MMA's columns, so that nothing is computed or loaded for rows that are not there;
 //   HBM bounds it.  Where there are fewer tiles than SMs, a cluster shares a tile by
@@ -47,13 +49,30 @@ namespace {
 constexpr int kRows = 128;             // rows of P per CTA and tile
 constexpr int kSlab = 128;             // columns of a slab: 128 bytes, one row of the 128-byte swizzle
 constexpr int kGroup = 4;              // slabs whose scales share a word
-constexpr int kThreads = 320;
 constexpr int kMaxStages = 12, kScaleSlots = 4;
 constexpr uint32_t kTmemCols = 512;
 // Tensor memory: accumulators from column 0, scale slots of 16 columns at the end (P's words in the first four of
 // them, Q's, up to 256 rows, in the last eight).
 constexpr uint32_t kScaleCols = 16, kScaleBase = kTmemCols - kScaleSlots * kScaleCols;
 constexpr int kPairCols = int(kScaleBase) / 2;   // 224: two accumulators beside the scales
+
+// How a tile is made: kAlone and kPair as above; kWide, a pair's tile of up to 448 columns in two parts, the first of 256
+// (the most columns of an MMA), with two slots of scales of twice the width.
+enum Mode { kAlone, kPair, kWide };
+constexpr int kPart = 256;
+template <int MODE>
+constexpr int kSlots = MODE == kWide ? 2 : kScaleSlots;
+template <int MODE>
+constexpr int kSlotCols = (kTmemCols - kScaleBase) / kSlots<MODE>;
+// Epilogue warps: four, or eight that share the columns of a wide tile, whose drain the next tile's MMAs wait for.
+template <int MODE>
+constexpr int kDrain = MODE == kWide ? 8 : 4;
+template <int MODE>
+constexpr int kThreads = (6 + kDrain<MODE>) * 32;
+
+// A CTA of a wide tile holds half of the columns in one piece, 32 h of them, and an MMA takes equal shares of both CTAs':
+// where the j-th 32 columns of the accumulator are in the tile.
+__device__ __forceinline__ int wide_chunk(int j, int h) { return j < 4 ? j : j < 8 ? h + j - 4 : j < 4 + h ? j - 4 : j; }
 
 struct Barriers {
     uint64_t full[kMaxStages];      // the copies of a stage have landed (pair: the even CTA's counts both CTAs')
@@ -66,14 +85,16 @@ struct Barriers {
     uint32_t tmem_base;
     int32_t abort;
 };
-// Staging of the pair's output: two blocks of 32 x 32 per epilogue warp.
+// Staging of the pair's output: blocks of 32 x 32, two per epilogue warp, one of fp32 where there are eight warps.
 template <typename T>
 constexpr int kOutBlock = 32 * 32 * int(sizeof(T));
-template <typename T, bool PAIR>
-constexpr int kStaging = PAIR ? 8 * kOutBlock<T> : 0;
+template <typename T, int MODE>
+constexpr int kBlocks = MODE == kWide && sizeof(T) == 4 ? 1 : 2;   // a warp's blocks
+template <typename T, int MODE>
+constexpr int kStaging = MODE == kAlone ? 0 : kDrain<MODE> * kBlocks<T, MODE> * kOutBlock<T>;
 constexpr int kSmemBytes = 227 * 1024;
-template <typename T, bool PAIR>
-constexpr int kRingBytes = (kSmemBytes - 1024 - kStaging<T, PAIR> - int(sizeof(Barriers))) / 1024 * 1024;
+template <typename T, int MODE>
+constexpr int kRingBytes = (kSmemBytes - 1024 - kStaging<T, MODE> - int(sizeof(Barriers))) / 1024 * 1024;
 
 struct Operand {
     const uint8_t* scale;
@@ -90,7 +111,7 @@ struct Problem {
     int p_tiles, q_tiles;
     int stages;
     int accs;              // accumulators
-    uint32_t idesc;
+    uint32_t idesc, idesc2;   // idesc2: of a wide tile's second part
     void* out;
     int64_t ldo;
     int32_t* flags;
@@ -240,8 +261,9 @@ __device__ void produce(const CUtensorMap* tmP, const CUtensorMap* tmQ, uint8_t*
     }
 }
 
-template <bool PAIR>
+template <int MODE>
 __device__ void issue_mmas(uint8_t* ring, Barriers* bars, uint32_t tmem, const Problem& pr, uint32_t rank) {
+    constexpr bool PAIR = MODE != kAlone;
     volatile int32_t* abort = &bars->abort;
     const uint32_t units = uint32_t((kRows + (PAIR ? pr.cols / 2 : pr.cols)) * kSlab) >> 4;   // of a stage, in descriptors
     const uint64_t pdesc0 = smem_desc(smem_u32(ring)), qdesc0 = smem_desc(smem_u32(ring + kRows * kSlab));
@@ -258,7 +280,7 @@ __device__ void issue_mmas(uint8_t* ring, Barriers* bars, uint32_t tmem, const P
         const uint32_t d = tmem + uint32_t(acc * pr.cols);
         for (int kb = w.lo; kb < w.hi && ok; kb += kGroup) {
             ok = warp_wait(&bars->sfull[slot], sphase, abort);
-            const uint32_t sc = tmem + kScaleBase + uint32_t(slot) * kScaleCols;
+            const uint32_t sc = tmem + kScaleBase + uint32_t(slot) * kSlotCols<MODE>;
 #pragma unroll
             for (int i = 0; i < kGroup; ++i) {     // the slab's scales are byte i of the group's words
                 if (kb + i >= w.hi || !ok) break;
@@ -266,12 +288,28 @@ __device__ void issue_mmas(uint8_t* ring, Barriers* bars, uint32_t tmem, const P
                 if (!ok) break;
                 tc_fence_after();
                 const uint64_t pd = pdesc0 + stage * units, qd = qdesc0 + stage * units;
-                const uint32_t more = kb + i > w.lo;
-                if (elect_one()) {
+                const uint32_t more = kb + i > w.lo, id = uint32_t(i) << 29 | uint32_t(i) << 4;
+                auto mmas = [&](uint32_t to, uint64_t q, uint32_t idesc, uint32_t sq) {
 #pragma unroll
                     for (int k = 0; k < kSlab / 32; ++k)   // 32 columns = 32 bytes = 2 descriptor units
-                        mma_scaled<PAIR>(d, pd + uint64_t(2 * k), qd + uint64_t(2 * k), pr.idesc | uint32_t(i) << 29 | uint32_t(i) << 4,
-                                         sc, sc + 8, k > 0 ? 1u : more);
+                        mma_scaled<PAIR>(to, pd + uint64_t(2 * k), q + uint64_t(2 * k), idesc | id, sc, sq, k > 0 ? 1u : more);
+                };
+                if constexpr (MODE == kWide) {
+                    if (elect_one()) {
+                        mmas(d, qd, pr.idesc, sc + 8);
+                        if (kb + i + 1 == w.hi) commit<true>(&bars->tfull[0]);
+                    }
+                    if (more == 0) {
+                        ok = warp_wait(&bars->tempty[1], aphase ^ 1u, abort);
+                        if (!ok) break;
+                        tc_fence_after();
+                    }
+                    if (elect_one()) {
+                        mmas(d + kPart, qd + (kPart / 2 * kSlab >> 4), pr.idesc2, sc + 16);
+                        commit<true>(&bars->empty[stage]);
+                    }
+                } else if (elect_one()) {
+                    mmas(d, qd, pr.idesc, sc + 8);
                     commit<PAIR>(&bars->empty[stage]);
                 }
                 if (++stage == pr.stages) {
@@ -281,7 +319,7 @@ __device__ void issue_mmas(uint8_t* ring, Barriers* bars, uint32_t tmem, const P
             }
             if (!ok) break;
             if (elect_one()) commit<PAIR>(&bars->sempty[slot]);
-            if (++slot == kScaleSlots) {
+            if (++slot == kSlots<MODE>) {
                 slot = 0;
                 sphase ^= 1u;
             }
@@ -290,8 +328,10 @@ __device__ void issue_mmas(uint8_t* ring, Barriers* bars, uint32_t tmem, const P
             give_up(abort, pr.flags);
             break;
         }
-        if (elect_one()) commit<PAIR>(&bars->tfull[acc]);
-        if (++acc == pr.accs) {
+        if (elect_one()) commit<PAIR>(&bars->tfull[MODE == kWide ? 1 : acc]);
+        if (MODE == kWide) {
+            aphase ^= 1u;
+        } else if (++acc == pr.accs) {
             acc = 0;
             aphase ^= 1u;
         }
@@ -312,11 +352,13 @@ __device__ void issue_mmas(uint8_t* ring, Barriers* bars, uint32_t tmem, const P
 // The scales of slabs kb .. kb+3 of N rows 32 apart, one a byte.  Rows and slabs beyond the matrix take the last one's: what
 // they scale is zeros, or is not stored.  There is no test around a load, so that all of them are in flight together (a
 // test for each, and they came one after the other: 4,096 x 16,384 x 16,384 in 952 us, the tensor cores half idle).
+// `h`: the order of a wide tile, from its word `j0`; 0 for the matrix's.
 template <int N>
-__device__ __forceinline__ void scale_words(const Operand& o, int row, int kb, int slabs, uint32_t* v) {
+__device__ __forceinline__ void scale_words(const Operand& o, int row, int kb, int slabs, int h, int j0, uint32_t* v) {
     const uint8_t* p[N];
 #pragma unroll
-    for (int c = 0; c < N; ++c) p[c] = o.scale + int64_t(min(row + 32 * c, o.rows - 1) >> o.shift) * o.lds;
+    for (int c = 0; c < N; ++c)
+        p[c] = o.scale + int64_t(min(row + 32 * (h > 0 ? wide_chunk(j0 + c, h) : c), o.rows - 1) >> o.shift) * o.lds;
     if (o.words && kb + kGroup <= slabs) {
 #pragma unroll
         for (int c = 0; c < N; ++c) v[c] = __ldg(reinterpret_cast<const uint32_t*>(p[c] + kb));
@@ -334,8 +376,10 @@ __device__ __forceinline__ void scale_words(const Operand& o, int row, int kb, i
 }
 
 // The groups of slabs of a CTA's tiles, in the order that the MMAs take them.
-template <bool PAIR>
+template <int MODE>
 struct Groups {
+    static constexpr bool PAIR = MODE != kAlone;
+    static constexpr int kQ = MODE == kWide ? 16 : 8, kWords = 4 + kQ;
     const Problem& pr;
     const Work<PAIR> w;
     const int lane;
@@ -356,10 +400,11 @@ struct Groups {
         q0 = tq * pr.cols + lane;
     }
     // This lane's words of the group at hand, and on to the next.
-    __device__ bool take(uint32_t (&v)[12]) {
+    __device__ bool take(uint32_t (&v)[kWords]) {
         if (!more()) return false;
-        scale_words<4>(pr.p, p0, kb, pr.slabs, v);
-        scale_words<8>(pr.q, q0, kb, pr.slabs, v + 4);
+        scale_words<4>(pr.p, p0, kb, pr.slabs, 0, 0, v);
+#pragma unroll
+        for (int j = 0; j < kQ; j += 8) scale_words<8>(pr.q, q0, kb, pr.slabs, MODE == kWide ? pr.cols / 64 : 0, j, v + 4 + j);
         kb += kGroup;
         if (kb >= w.hi) {
             kb = w.lo;
@@ -370,28 +415,33 @@ struct Groups {
     }
 };
 
-// Words are loaded two groups ahead of their use.
-template <bool PAIR>
+// Words are loaded two groups ahead of their use (wide tiles, of longer groups: one).
+template <int MODE>
 __device__ void write_scales(Barriers* bars, uint32_t tmem, const Problem& pr, uint32_t rank) {
+    constexpr bool PAIR = MODE != kAlone;
+    constexpr int kWords = Groups<MODE>::kWords;
     volatile int32_t* abort = &bars->abort;
     const int lane = threadIdx.x & 31;
     const uint32_t lanes = uint32_t((threadIdx.x >> 5) & 3) << 21;   // this warp's quarter, 32 lanes each
     int slot = 0;
     uint32_t phase = 0;
-    auto write = [&](const uint32_t (&v)[12]) {
+    auto write = [&](const uint32_t (&v)[kWords]) {
         const bool free = wait_phase(&bars->sempty[slot], phase ^ 1u, abort);
         if (!__all_sync(0xffffffffu, free)) {
             give_up(abort, pr.flags);
             return false;
         }
         tc_fence_after();
-        const uint32_t at = tmem + lanes + kScaleBase + uint32_t(slot) * kScaleCols;
+        const uint32_t at = tmem + lanes + kScaleBase + uint32_t(slot) * kSlotCols<MODE>;
         asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]),
                      "r"(v[3])
                      : "memory");
-        asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(at + 8), "r"(v[4]),
-                     "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11])
-                     : "memory");
+#pragma unroll
+        for (int c = 4; c < kWords; c += 8)
+            asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(at + 4 + c),
+                         "r"(v[c]), "r"(v[c + 1]), "r"(v[c + 2]), "r"(v[c + 3]), "r"(v[c + 4]), "r"(v[c + 5]), "r"(v[c + 6]),
+                         "r"(v[c + 7])
+                         : "memory");
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         tc_fence_before();
         __syncwarp();
@@ -401,42 +451,49 @@ __device__ void write_scales(Barriers* bars, uint32_t tmem, const Problem& pr, u
             else
                 mbar_arrive(&bars->sfull[slot]);
         }
-        if (++slot == kScaleSlots) {
+        if (++slot == kSlots<MODE>) {
             slot = 0;
             phase ^= 1u;
         }
         return true;
     };
-    Groups<PAIR> g(pr, rank);
-    uint32_t a[12], b[12], c[12];
-    bool na = g.take(a), nb = g.take(b), nc = g.take(c);
-    while (na) {
-        if (!write(a)) return;
-        na = g.take(a);
-        if (!nb) return;
-        if (!write(b)) return;
-        nb = g.take(b);
-        if (!nc) return;
-        if (!write(c)) return;
-        nc = g.take(c);
+    Groups<MODE> g(pr, rank);
+    uint32_t a[kWords], b[kWords];
+    bool na = g.take(a), nb = g.take(b);
+    if constexpr (MODE == kWide) {
+        while (na) {
+            if (!write(a)) return;
+            na = g.take(a);
+            if (!nb || !write(b)) return;
+            nb = g.take(b);
+        }
+    } else {
+        uint32_t c[kWords];
+        bool nc = g.take(c);
+        while (na) {
+            if (!write(a)) return;
+            na = g.take(a);
+            if (!nb || !write(b)) return;
+            nb = g.take(b);
+            if (!nc || !write(c)) return;
+            nc = g.take(c);
+        }
     }
 }
 
-template <typename T>
-__device__ __forceinline__ void store_one(T* p, float v);
-template <>
-__device__ __forceinline__ void store_one<float>(float* p, float v) { *p = v; }
-template <>
-__device__ __forceinline__ void store_one<acrl_bf16>(acrl_bf16* p, float v) { *p = acrl_bf16(pack_bf16x2(v, 0.f) & 0xffffu); }
+__device__ __forceinline__ void store_one(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store_one(acrl_bf16* p, float v) { *p = acrl_bf16(pack_bf16x2(v, 0.f) & 0xffffu); }
 
 // Accumulators of a pair's tile: each warp its 32 rows, 32 columns at a time, rounded, staged in shared memory and
 // stored by a TMA copy, which leaves out what is beyond the matrix.
-template <typename T>
+template <typename T, int MODE>
 __device__ void pair_epilogue(Barriers* bars, uint32_t tmem, const CUtensorMap* tmO, uint8_t* staging, const Problem& pr,
                               uint32_t rank) {
     volatile int32_t* abort = &bars->abort;
     const int lane = threadIdx.x & 31, quarter = (threadIdx.x >> 5) & 3;
-    uint8_t* blocks = staging + ((threadIdx.x >> 5) - 6) * 2 * kOutBlock<T>;
+    constexpr int kBuf = kBlocks<T, MODE>, kStep = 32 * (kDrain<MODE> / 4);   // the warps of a quarter take chunks in turn
+    const int first = 32 * (((threadIdx.x >> 5) - 6) >> 2);
+    uint8_t* blocks = staging + ((threadIdx.x >> 5) - 6) * kBuf * kOutBlock<T>;
     // row `lane` of a block, its 16-byte pieces permuted by the swizzle of the output's map: 64-byte rows in fours
     // (bf16), 128-byte rows in eights (fp32)
     constexpr int kPieces = 32 * int(sizeof(T)) / 16;
@@ -448,56 +505,66 @@ __device__ void pair_epilogue(Barriers* bars, uint32_t tmem, const CUtensorMap* 
     for (int t = w.first; t < pr.p_tiles * pr.q_tiles; t += w.step) {
         int tp, tq;
         tile_at(t, pr, tp, tq);
-        const bool ready = wait_phase(&bars->tfull[acc], phase, abort);
-        if (!__all_sync(0xffffffffu, ready)) {
+        const int row0 = (2 * tp + int(rank)) * kRows + quarter * 32;
+        bool ready = true;
+#pragma unroll 1
+        for (int part = 0; part < (MODE == kWide ? 2 : 1); ++part) {
+            const int a = MODE == kWide ? part : acc;
+            const int c0 = part * kPart + first, end = MODE == kWide && part == 0 ? kPart : pr.cols;
+            ready = wait_phase(&bars->tfull[a], phase, abort);
+            ready = __all_sync(0xffffffffu, ready);
+            if (!ready) break;
+            tc_fence_after();
+#pragma unroll 1
+            for (int c = c0; c < end; c += kStep) {
+                uint32_t r[32];
+                __syncwarp();
+                tmem_ld32(tmem + uint32_t((MODE == kWide ? 0 : acc * pr.cols) + c) + (uint32_t(quarter * 32) << 16), r);
+                if (c + kStep >= end) {   // read out: the even CTA's MMA warp may fill it again
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) remote_arrive(peer_addr(&bars->tempty[a], 0));
+                }
+                const int col0 = tq * pr.cols + (MODE == kWide ? 32 * wide_chunk(c / 32, pr.cols / 64) : c);
+                if (row0 >= pr.p.rows || col0 >= pr.q.rows) continue;   // the same for the whole warp
+                if (col0 + 32 > pr.q.rows && (pr.q.rows * int(sizeof(T)) & 15) != 0) {
+                    // a TMA store leaves columns out in 16-byte pieces: here the last ones would write beyond the matrix
+                    T* out = static_cast<T*>(pr.out) + int64_t(row0 + lane) * pr.ldo + col0;
+                    if (row0 + lane < pr.p.rows)
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (col0 + j < pr.q.rows) store_one(out + j, __uint_as_float(r[j]));
+                    continue;
+                }
+                if (lane == 0) bulk_wait_read<kBuf - 1>();              // the store that last read this block is done
+                __syncwarp();
+                const uint32_t to = at + uint32_t(buf * kOutBlock<T>);
+#pragma unroll
+                for (int k = 0; k < kPieces; ++k) {
+                    uint4 v;
+                    if constexpr (sizeof(T) == 2)
+                        v = make_uint4(pack_bf16x2(__uint_as_float(r[8 * k]), __uint_as_float(r[8 * k + 1])),
+                                       pack_bf16x2(__uint_as_float(r[8 * k + 2]), __uint_as_float(r[8 * k + 3])),
+                                       pack_bf16x2(__uint_as_float(r[8 * k + 4]), __uint_as_float(r[8 * k + 5])),
+                                       pack_bf16x2(__uint_as_float(r[8 * k + 6]), __uint_as_float(r[8 * k + 7])));
+                    else
+                        v = make_uint4(r[4 * k], r[4 * k + 1], r[4 * k + 2], r[4 * k + 3]);
+                    st_shared16(to + ((uint32_t(k) ^ swz) << 4), v);
+                }
+                fence_async_shared();
+                __syncwarp();
+                if (lane == 0) tma_store_2d(tmO, blocks + buf * kOutBlock<T>, col0, row0);
+                if (kBuf > 1) buf ^= 1;
+            }
+            __syncwarp();
+        }
+        if (!ready) {
             give_up(abort, pr.flags);
             break;
         }
-        tc_fence_after();
-        const int row0 = (2 * tp + int(rank)) * kRows + quarter * 32;
-#pragma unroll 1
-        for (int c = 0; c < pr.cols; c += 32) {
-            uint32_t r[32];
-            __syncwarp();
-            tmem_ld32(tmem + uint32_t(acc * pr.cols + c) + (uint32_t(quarter * 32) << 16), r);
-            if (c + 32 == pr.cols) {   // read out: the even CTA's MMA thread may fill it again
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) remote_arrive(peer_addr(&bars->tempty[acc], 0));
-            }
-            const int col0 = tq * pr.cols + c;
-            if (row0 >= pr.p.rows || col0 >= pr.q.rows) continue;   // the same for the whole warp
-            if (col0 + 32 > pr.q.rows && (pr.q.rows * int(sizeof(T)) & 15) != 0) {
-                // a TMA store leaves columns out in 16-byte pieces: here the last ones would write beyond the matrix
-                T* out = static_cast<T*>(pr.out) + int64_t(row0 + lane) * pr.ldo + col0;
-                if (row0 + lane < pr.p.rows)
-#pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (col0 + j < pr.q.rows) store_one(out + j, __uint_as_float(r[j]));
-                continue;
-            }
-            if (lane == 0) bulk_wait_read<1>();                     // the store that last read this block is done
-            __syncwarp();
-            const uint32_t to = at + uint32_t(buf * kOutBlock<T>);
-#pragma unroll
-            for (int k = 0; k < kPieces; ++k) {
-                uint4 v;
-                if constexpr (sizeof(T) == 2)
-                    v = make_uint4(pack_bf16x2(__uint_as_float(r[8 * k]), __uint_as_float(r[8 * k + 1])),
-                                   pack_bf16x2(__uint_as_float(r[8 * k + 2]), __uint_as_float(r[8 * k + 3])),
-                                   pack_bf16x2(__uint_as_float(r[8 * k + 4]), __uint_as_float(r[8 * k + 5])),
-                                   pack_bf16x2(__uint_as_float(r[8 * k + 6]), __uint_as_float(r[8 * k + 7])));
-                else
-                    v = make_uint4(r[4 * k], r[4 * k + 1], r[4 * k + 2], r[4 * k + 3]);
-                st_shared16(to + ((uint32_t(k) ^ swz) << 4), v);
-            }
-            fence_async_shared();
-            __syncwarp();
-            if (lane == 0) tma_store_2d(tmO, blocks + buf * kOutBlock<T>, col0, row0);
-            buf ^= 1;
-        }
-        __syncwarp();
-        if (++acc == pr.accs) {
+        if (MODE == kWide) {
+            phase ^= 1u;
+        } else if (++acc == pr.accs) {
             acc = 0;
             phase ^= 1u;
         }
@@ -592,14 +659,15 @@ __device__ void join(uint32_t tmem, const float* parts, const Problem& pr, int n
     }
 }
 
-template <typename T, bool PAIR>
-__global__ void __launch_bounds__(kThreads, 1)
+template <typename T, int MODE>
+__global__ void __launch_bounds__(kThreads<MODE>, 1)
     fp8_matmul_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CUtensorMap tmQ,
                       const __grid_constant__ CUtensorMap tmO, const __grid_constant__ Problem pr) {
+    constexpr bool PAIR = MODE != kAlone;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    uint8_t* staging = ring + kRingBytes<T, PAIR>;
-    Barriers* bars = reinterpret_cast<Barriers*>(staging + kStaging<T, PAIR>);
+    uint8_t* staging = ring + kRingBytes<T, MODE>;
+    Barriers* bars = reinterpret_cast<Barriers*>(staging + kStaging<T, MODE>);
     const int warp = threadIdx.x >> 5;
     const uint32_t rank = cluster_rank();
     const int nct = int(cluster_size());
@@ -614,7 +682,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(&bars->tfull[b], 1);
-            mbar_init(&bars->tempty[b], PAIR ? 8 : 4);
+            mbar_init(&bars->tempty[b], (PAIR ? 2 : 1) * kDrain<MODE>);
         }
         mbar_init(&bars->mma_done, 1);
         bars->abort = 0;
@@ -648,11 +716,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (warp == 0) {
         produce<PAIR>(&tmP, &tmQ, ring, bars, pr, rank);
     } else if (warp == 1) {
-        if (!PAIR || rank == 0) issue_mmas<PAIR>(ring, bars, tmem, pr, rank);
+        if (!PAIR || rank == 0) issue_mmas<MODE>(ring, bars, tmem, pr, rank);
     } else if (warp < 6) {
-        write_scales<PAIR>(bars, tmem, pr, rank);
+        write_scales<MODE>(bars, tmem, pr, rank);
     } else if constexpr (PAIR) {
-        pair_epilogue<T>(bars, tmem, &tmO, staging, pr, rank);
+        pair_epilogue<T, MODE>(bars, tmem, &tmO, staging, pr, rank);
     } else {
         ok = alone_epilogue<T>(bars, tmem, parts, pr, rank, nct);
     }
@@ -684,8 +752,9 @@ Operand operand(const Matrix& m) {
 constexpr int64_t kAloneRows = 128, kSplitRows = 32;
 constexpr int kMaxSplit = 8;
 
-template <typename T, bool PAIR>
+template <typename T, int MODE>
 acrl_status launch_kernel(const Matrix& p, const Matrix& q, int64_t K, Problem pr, int64_t grid, int cluster, cudaStream_t s) {
+    constexpr bool PAIR = MODE != kAlone;
     CUtensorMap tmP, tmQ, tmO;
     auto map = [&](CUtensorMap* m, const Matrix& x, int box_rows) {
         return encode_map(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, x.q, uint64_t(x.rows), uint64_t(K), uint64_t(x.ld), box_rows,
@@ -699,15 +768,15 @@ acrl_status launch_kernel(const Matrix& p, const Matrix& q, int64_t K, Problem p
                          uint64_t(p.rows), uint64_t(q.rows), uint64_t(pr.ldo), 32, 32,
                          bf16 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B))
         return ACRL_ERR_CUDA;
-    auto* kernel = fp8_matmul_kernel<T, PAIR>;
+    auto* kernel = fp8_matmul_kernel<T, MODE>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) != cudaSuccess)
         return launch_status();
     if (PAIR) {   // no more than can be resident at once: they are persistent
-        const int64_t most = resident_clusters(reinterpret_cast<const void*>(kernel), kThreads, kSmemBytes, 2);
+        const int64_t most = resident_clusters(reinterpret_cast<const void*>(kernel), kThreads<MODE>, kSmemBytes, 2);
         if (most < 1) return ACRL_ERR_CUDA;
         grid = std::min<int64_t>(grid, 2 * most);
     }
-    return launch(kernel, grid, kThreads, kSmemBytes, cluster, s, tmP, tmQ, tmO, pr);
+    return launch(kernel, grid, kThreads<MODE>, kSmemBytes, cluster, s, tmP, tmQ, tmO, pr);
 }
 
 template <typename T>
@@ -736,35 +805,41 @@ acrl_status launch_matmul(const Matrix& a, const Matrix& b, int64_t K, void* out
         int split = 1;
         while (split < kMaxSplit && 2 * split * pr.p_tiles <= sms && (pr.slabs + kGroup - 1) / kGroup >= 2 * split) split *= 2;
         const int parts = (split - 1) * pr.cols * kRows * 4;
-        pr.stages = std::min(kMaxStages, (kRingBytes<T, false> - parts) / bytes);
+        pr.stages = std::min(kMaxStages, (kRingBytes<T, kAlone> - parts) / bytes);
         while (pr.stages < 2) {   // never for up to 128 columns and eight parts of 64 KB less one
             split /= 2;
-            pr.stages = std::min(kMaxStages, (kRingBytes<T, false> - (split - 1) * pr.cols * kRows * 4) / bytes);
+            pr.stages = std::min(kMaxStages, (kRingBytes<T, kAlone> - (split - 1) * pr.cols * kRows * 4) / bytes);
         }
         pr.idesc |= uint32_t(pr.cols >> 3) << 17 | 1u << 27;
         const int64_t grid = split > 1 ? int64_t(pr.p_tiles) * split : std::min(pr.p_tiles, sms);
-        return launch_kernel<T, false>(p, q, K, pr, grid, split, s);
+        return launch_kernel<T, kAlone>(p, q, K, pr, grid, split, s);
     }
     pr.p_tiles = int((p.rows + 2 * kRows - 1) / (2 * kRows));
-    // Columns of a tile: the loads of a slab, 128 rows of P and half the columns a CTA, take longest, and all pairs run whole
-    // rounds of tiles; so the least rounds x (128 + columns / 2), wide tiles first.  2,507 x 2,048 x 8,200 (100 tiles of 224
-    // columns or 130 of 160 for 76 pairs) 58 / 52 us.
+    // Columns of a tile: the loads of a slab, 128 rows of P and half the columns a CTA, take longest (1.5 ns for one of them),
+    // a wide tile's MMAs also wait for the drain of the one before, and all pairs run whole rounds of tiles.  224 / 320 / 448
+    // columns: 4,096 x 4,096 x 4,096 (76 pairs: 4, 3 and 3 rounds) 52 / 56 / 63 us, 2,504 x 2,048 x 8,200 (2, 1 and 1) 61 / 44 / 47,
+    // 8,192 x 8,192 x 1,024 (16, 11 and 8) 65 / 77 / 69, 4,096 x 151,936 x 4,096 (143, 101 and 72) 1,680 / 1,660 / 1,510.
+    // Narrow ones where the last round would be short: 1,500 x 6,000 x 1,024 of 192 / 224: 18.1 / 18.7 us.
+    constexpr int64_t kTileCost = 300, kWideCost = 2000;
     int64_t total = 0, least = 0;
-    for (int cols = kPairCols; cols >= 96; cols -= 32) {
+    for (int cols = 2 * kPairCols; cols >= 96; cols -= cols > kPart ? 64 : 32) {
         const int64_t tiles = int64_t(pr.p_tiles) * ((q.rows + cols - 1) / cols);
-        const int64_t cost = (tiles + sms / 2 - 1) / (sms / 2) * (128 + cols / 2);
+        const int64_t cost = (tiles + sms / 2 - 1) / (sms / 2) * (pr.slabs * (128 + cols / 2) + (cols > kPart ? kWideCost : kTileCost));
         if (least == 0 || cost < least) {
             least = cost;
             total = tiles;
             pr.cols = cols;
         }
+        if (cols == kPart + 64) cols = kPairCols + 32;   // two accumulators of 256 do not fit
     }
     pr.q_tiles = int((q.rows + pr.cols - 1) / pr.cols);
     if (total > kMaxGrid / 2) return ACRL_ERR_INVALID_ARG;
+    const bool wide = pr.cols > kPart;
     pr.accs = 2;
-    pr.stages = std::min(kMaxStages, kRingBytes<T, true> / ((kRows + pr.cols / 2) * kSlab));
-    pr.idesc |= uint32_t(pr.cols >> 3) << 17 | 2u << 27;
-    return launch_kernel<T, true>(p, q, K, pr, 2 * total, 2, s);
+    pr.stages = std::min(kMaxStages, (wide ? kRingBytes<T, kWide> : kRingBytes<T, kPair>) / ((kRows + pr.cols / 2) * kSlab));
+    pr.idesc2 = pr.idesc | uint32_t((pr.cols - kPart) >> 3) << 17 | 2u << 27;
+    pr.idesc |= uint32_t(std::min(pr.cols, kPart) >> 3) << 17 | 2u << 27;
+    return wide ? launch_kernel<T, kWide>(p, q, K, pr, 2 * total, 2, s) : launch_kernel<T, kPair>(p, q, K, pr, 2 * total, 2, s);
 }
 
 // Checked operands of one row or more each.

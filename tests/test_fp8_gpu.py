@@ -128,6 +128,17 @@ def test_matmul(M, N, K, dtype):
     _check_product(acrl.fp8_matmul(a, b, out_dtype=dtype), a, b)
 
 
+@pytest.mark.parametrize("M,N,K", [(2500, 2001, 1500), (517, 8203, 1500), (260, 33003, 1300), (513, 24001, 1700)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_matmul_of_many_columns(M, N, K, dtype):
+    """Tiles of more columns than an instruction's, once and several times over; nothing beyond the matrix is written."""
+    a = acrl.fp8_quantize(_matrix(M, K, 31))
+    b = acrl.fp8_quantize(_matrix(N, K, 32, std=0.02))
+    out = torch.full((M + 1, (N + 7) // 8 * 8), 7.0, dtype=dtype, device=DEV)
+    _check_product(acrl.fp8_matmul(a, b, out=out[:M]), a, b)
+    assert bool((out[M:] == 7.0).all()) and bool((out[:, N:] == 7.0).all())
+
+
 @pytest.mark.parametrize("fa,fb", [("e4m3", "e5m2"), ("e5m2", "e4m3"), ("e5m2", "e5m2")])
 @pytest.mark.parametrize("ba,bb", [("row", "row"), ("tile", "row"), ("tile", "tile")])
 @pytest.mark.parametrize("M,N,K", [(40, 200, 700), (333, 140, 900)])
