@@ -521,7 +521,7 @@ def _fp8_format(fmt: str) -> int:
 
 
 def _padded(shape, to: int, dtype, dev) -> torch.Tensor:
-    """A new matrix with its rows at a stride that is a multiple of `to`."""
+    """A new matrix with its rows, the last one too, at a stride that is a multiple of `to`."""
     ld = (shape[1] + to - 1) // to * to
     x = torch.empty((shape[0], ld), dtype=dtype, device=dev)
     return x if ld == shape[1] else x[:, : shape[1]]
@@ -544,7 +544,9 @@ def fp8_quantize(x, *, block="row", fmt="e4m3", transpose=False, out: Fp8Tensor 
     rows, cols = (C, R) if transpose else (R, C)
     srows, kb = (rows if kind == _abi.FP8_ROW else (rows + 127) // 128), (cols + 127) // 128
     if out is None:
-        out = Fp8Tensor(_padded((rows, cols), 16, dtype, x.device), _padded((srows, kb), 4, torch.uint8, x.device))
+        ldq, lds = (cols + 15) // 16 * 16, (kb + 3) // 4 * 4
+        out = Fp8Tensor(torch.empty_strided((rows, cols), (ldq, 1), dtype=dtype, device=x.device),
+                        torch.empty_strided((srows, kb), (lds, 1), dtype=torch.uint8, device=x.device))
     elif tuple(out.q.shape) != (rows, cols) or out.q.dtype != dtype or out.scale.shape[0] != srows:
         raise AcrlError(f"out: an 8-bit matrix of another shape, format or block than {(rows, cols)} {fmt} {block}")
     if flags is not None:
@@ -703,14 +705,8 @@ def policy_loss_grad_logits(logits, ids, mask, coef, *, V=None, old_logp=None, c
     elif grad.dtype != torch.bfloat16 or grad.dim() != 2 or grad.stride(0) != ld or grad.stride(1) != 1 or \
             grad.shape[0] < T:
         raise AcrlError("grad: expected a bf16 [T, ld] tensor with the logits' row stride")
-    if logp is None and token_loss is None and kl_out is None:   # one allocation for the three
-        three = torch.empty((3, (T + 3) // 4 * 4), dtype=f32, device=dev)   # each on 16 bytes
-        logp, token_loss, kl_out = (three if T % 4 == 0 else three[:, :T]).unbind(0)
-    else:
-        logp, token_loss = _vec(logp, f32, T, "logp", dev), _vec(token_loss, f32, T, "token_loss", dev)
-        kl_out = None if kl is None else _vec(kl_out, f32, T, "kl_out", dev)
-    if kl is None:
-        kl_out = None
+    logp, token_loss = _vec(logp, f32, T, "logp", dev), _vec(token_loss, f32, T, "token_loss", dev)
+    kl_out = None if kl is None else _vec(kl_out, f32, T, "kl_out", dev)
     loss = _vec(loss, f32, 1, "loss", dev)
     if flags is not None:
         _need(flags, torch.int32, 1, "flags")

@@ -60,13 +60,38 @@ struct PolicyArgs {
     int32_t* flags;
 };
 
-// A row's (or part's) running state in base 2: maxima, exponents U = max log2 e, sums
+// A row's (or part's) running state in base 2: maxima, exponents U = max log2 e as whole numbers, sums
 // against them, and the cross sum: exact  sum 2^(u - U) (z - x),  reverse  sum 2^(w - W) (x - z).
+// `off` = sx - sz where U = W: KL of two close distributions needs the logarithm of the sums' ratio to better than the
+// sums' own roundings, and the difference, summed by itself from the lanes on, is rounded at its own size.
 struct State {
-    float mz, U, sz, mx, W, sx, cross;   // mz, mx: of some columns, near the maxima
+    float mz, U, sz, mx, W, sx, cross, off;   // mz, mx: of some columns, near the maxima
 };
 
-__device__ __forceinline__ State empty_state() { return State{-INFINITY, kLowestU, 0.f, -INFINITY, kLowestU, 0.f, 0.f}; }
+__device__ __forceinline__ State empty_state() { return State{-INFINITY, kLowestU, 0.f, -INFINITY, kLowestU, 0.f, 0.f, 0.f}; }
+
+// log2 e less its nearest fp32 number: left out, it would tilt every log-prob by 1.3e-8 of the logits' weighted mean, which
+// a sum over a response's tokens carries.  (With KL over the vocabulary nothing sums them, and p's and q's tilts cancel.)
+constexpr float kLog2eLow = 1.92596303e-8f;
+
+// Whole numbers: sums are brought from one to another without a rounding.
+__device__ __forceinline__ float exponent_of(float m) { return rintf(max_exponent<true>(m)); }
+// That of the reference's columns: the policy's where they are near.
+__device__ __forceinline__ float exponent_beside(float mx, float U) {
+    const float W = exponent_of(mx);
+    return fabsf(W - U) <= 16.f ? U : W;
+}
+
+// z - log(2^U s).  U log 2 in two parts, the first of 15 bits, so that z less it is exact for every bf16 z of ordinary size
+// and one rounding at the result's size is left.  Beyond, by differences of the logits, which are as coarse as units there.
+__device__ __forceinline__ float less_log(float z, float m, float U, float s) {
+    constexpr float kHi = 22713.f / 32768.f, kLo = 1.42860682e-6f;   // log 2 = kHi + kLo
+    const int bits = __float_as_int(s), e = (bits - 0x3f400000) >> 23;   // s = 2^e f, 3/4 <= f < 3/2
+    const bool normal = s > 1e-37f && s < 3e38f;                         // else (0, infinite, NaN): its own logarithm
+    const float f = normal ? __int_as_float(bits - e * (1 << 23)) : s, n = normal ? U + float(e) : U;
+    const float l = kLn2 * log2f(f);
+    return fabsf(U) < 1e6f ? fmaf(-n, kHi, z) - fmaf(n, kLo, l) : (z - m) - (l + kLn2 * (n - U - fmaf(m, kLog2e, -U)));
+}
 
 // Two fp32 numbers in a register pair: sums, products and fused products of both in one instruction (issue bounds these
 // sweeps next to HBM; one number at a time took 36 instructions a column pair where this takes some 16).
@@ -118,7 +143,7 @@ __device__ __forceinline__ uint32_t max_pairs(const uint4& v) {
 
 // A new running maximum m of one operand: its exponent, and the factor that brings sums to it.
 __device__ __forceinline__ float raise_max(float m, float& mx, float& U) {
-    const float Un = max_exponent<true>(m), f = ex2(U - Un);
+    const float Un = exponent_of(m), f = ex2(U - Un);
     U = Un;
     mx = m;
     return f;
@@ -184,12 +209,12 @@ struct Quick {
     // `z`, `x`: vectors of every lane of a warp.
     __device__ __forceinline__ void start(const uint4& z, const uint4& x) {
         mz = warp_max_of(max_pairs(z));
-        const float U = max_exponent<true>(mz);
+        const float U = exponent_of(mz);
         nU = two(-U, -U);
         sz = sx = cr = two(0.f, 0.f);
         if constexpr (KIND != kSampled) {
             mx = warp_max_of(max_pairs(x));
-            const float W = max_exponent<true>(mx);
+            const float W = exponent_beside(mx, U);
             nW = two(-W, -W);
         }
     }
@@ -200,13 +225,13 @@ struct Quick {
     }
     template <int N>
     __device__ __forceinline__ void fold(const uint4 (&z)[N], const uint4 (&x)[N]) {
-        const Two l2e = two(kLog2e, kLog2e), minus = two(-1.f, -1.f);
+        const Two l2e = two(kLog2e, kLog2e), low = two(kLog2eLow, kLog2eLow), minus = two(-1.f, -1.f);
 #pragma unroll
         for (int k = 0; k < N; ++k) {
             const uint32_t zw[4] = {z[k].x, z[k].y, z[k].z, z[k].w}, xw[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const Two a = widen(zw[j]), e = ex2_2(fma2(a, l2e, nU));
+                const Two a = widen(zw[j]), u = fma2(a, l2e, nU), e = ex2_2(KIND == kSampled ? fma2(a, low, u) : u);
                 sz = add2(sz, e);
                 if constexpr (KIND != kSampled) {
                     const Two b = widen(xw[j]), h = ex2_2(fma2(b, l2e, nW));
@@ -219,13 +244,14 @@ struct Quick {
     __device__ __forceinline__ State state() const {
         State s = empty_state();
         s.mz = mz;
-        s.U = max_exponent<true>(mz);
+        s.U = exponent_of(mz);
         s.sz = sum_of(sz);
         if constexpr (KIND != kSampled) {
             s.mx = mx;
-            s.W = max_exponent<true>(mx);
+            s.W = exponent_beside(mx, s.U);
             s.sx = sum_of(sx);
             s.cross = sum_of(cr);
+            s.off = s.sx - s.sz;
         }
         return s;
     }
@@ -236,18 +262,19 @@ template <Kind KIND>
 __device__ __forceinline__ State bring(const State& s, float mz, float mx) {
     State r;
     r.mz = mz;
-    r.U = max_exponent<true>(mz);
+    r.U = exponent_of(mz);
     const float f = ex2(s.U - r.U);
     r.sz = s.sz * f;
     if constexpr (KIND == kSampled) {
         r.mx = mx;
-        r.W = r.sx = r.cross = 0.f;
+        r.W = r.sx = r.cross = r.off = 0.f;
     } else {
         r.mx = mx;
-        r.W = max_exponent<true>(mx);
+        r.W = exponent_beside(mx, r.U);
         const float g = ex2(s.W - r.W);
         r.sx = s.sx * g;
         r.cross = s.cross * (KIND == kExact ? f : g);
+        r.off = s.U == s.W && f == g ? s.off * f : r.sx - r.sz;
     }
     return r;
 }
@@ -268,6 +295,7 @@ __device__ __forceinline__ State meet(State s) {
         if (KIND != kSampled) {
             s.sx += __shfl_xor_sync(0xffffffffu, s.sx, m);
             s.cross += __shfl_xor_sync(0xffffffffu, s.cross, m);
+            s.off += __shfl_xor_sync(0xffffffffu, s.off, m);
         }
     }
     return s;
@@ -344,8 +372,8 @@ enum { kWrite, kWriteSafe, kFillZero, kFillNaN };
 template <Kind KIND>
 __device__ __forceinline__ int row_scalars(const PolicyArgs& A, int64_t t, const State& row, int a, float za, float xa,
                                            float c0, float kc, float old, float ref, bool writes, RowGrad& g) {
-    const float lz = kLn2 * (log2f(row.sz) - fmaf(row.mz, kLog2e, -row.U));      // lse_z - max z
-    const float logp = (za - row.mz) - lz;
+    const bool sums = row.sz > 0.f && isfinite(row.sz) && isfinite(row.mz);
+    const float logp = less_log(za, row.mz, row.U, row.sz);
     float KL = 0.f, apart = 0.f, logq = 0.f;                                      // apart = lse_z - lse_x
     g.a = a;
     g.k = kc;
@@ -353,11 +381,12 @@ __device__ __forceinline__ int row_scalars(const PolicyArgs& A, int64_t t, const
     g.W = 0.f;
     float slope = 0.f;                                                            // of the sampled estimators, in logp
     if constexpr (KIND != kSampled) {
-        const float lx = kLn2 * (log2f(row.sx) - fmaf(row.mx, kLog2e, -row.W));
-        // the logarithm of the sums' ratio, not the difference of two logarithms whose roundings KL would carry whole
-        const float diff = row.sz - row.sx, ratio = fabsf(diff) < 0.5f * row.sx ? log1pf(diff / row.sx) : logf(row.sz / row.sx);
-        apart = (row.mz - row.mx) + (ratio - kLn2 * (fmaf(row.mz, kLog2e, -row.U) - fmaf(row.mx, kLog2e, -row.W)));
-        logq = (xa - row.mx) - lx;
+        const float off = isfinite(row.off) ? row.off : row.sx - row.sz;
+        const float ratio = row.U == row.W && fabsf(off) < 0.5f * row.sx ? log1pf(-off / row.sx) : kLn2 * log2f(row.sz / row.sx);
+        apart = fabsf(row.U) < 1e6f && fabsf(row.W) < 1e6f
+                    ? fmaf(row.U - row.W, kLn2, ratio)
+                    : (row.mz - row.mx) + (ratio - kLn2 * (fmaf(row.mz, kLog2e, -row.U) - fmaf(row.mx, kLog2e, -row.W)));
+        logq = less_log(xa, row.mx, row.W, row.sx);
         KL = KIND == kExact ? row.cross / row.sz - apart : row.cross / row.sx + apart;
         g.W = row.W + log2f(row.sx);
     } else {
@@ -386,7 +415,7 @@ __device__ __forceinline__ int row_scalars(const PolicyArgs& A, int64_t t, const
     }
     if (kc != 0.f && KIND == kSampled) g.c -= kc * slope;
     const float loss = kc != 0.f ? fmaf(kc, KL, surrogate) : surrogate;
-    const bool defined = isfinite(logp) && isfinite(lz) && (KIND == kSampled || isfinite(KL));
+    const bool defined = isfinite(logp) && sums && (KIND == kSampled || isfinite(KL));
     const bool carries = c0 != 0.f || kc != 0.f;
     const bool undefined = carries && (!defined || (c0 != 0.f && isnan(ratio)) || (kc != 0.f && !isfinite(KL)));
     if (writes) {
@@ -416,13 +445,14 @@ __device__ __forceinline__ int column_of(const PolicyArgs& A, int64_t t) {
     return (A.mask && A.mask[t] == 0) || a < 0 || a >= A.V ? -1 : a;
 }
 
+__device__ __forceinline__ bool was_careful(const float4* from) { return !isfinite(from[1].w); }
 __device__ __forceinline__ void put(float4* to, const State& s, bool careful) {
     to[0] = make_float4(s.mz, s.U, s.sz, s.mx);
-    to[1] = make_float4(s.W, s.sx, s.cross, careful ? 1.f : 0.f);
+    to[1] = make_float4(s.W, s.sx, s.cross, careful ? INFINITY : s.off);   // finite where not careful
 }
 __device__ __forceinline__ State get(const float4* from) {
     const float4 a = from[0], b = from[1];
-    return State{a.x, a.y, a.z, a.w, b.x, b.y, b.z};
+    return State{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 }
 
 template <int THREADS>
@@ -545,6 +575,7 @@ struct Cta {
             if (odd) f(oz, ox, 0);
         }
         __syncwarp();
+        if (careful) st.off = st.sx - st.sz;
         return meet<KIND, 32>(st);
     }
 
@@ -644,18 +675,18 @@ __global__ void __launch_bounds__(THREADS, PER_SM) policy_kernel(const __grid_co
         if (lane == 0) put(sh.warps[wid], st, careful);
         __syncthreads();
         if (kEvery || wid == 0) {
-            careful = __any_sync(0xffffffffu, lane < kWarps && sh.warps[lane][1].w != 0.f);
+            careful = __any_sync(0xffffffffu, lane < kWarps && was_careful(sh.warps[lane]));
             st = meet<KIND, 32>(lane < kWarps ? get(sh.warps[lane]) : none);
         }
     }
     if (nct > 1) {
         if (wid == 0 && lane < nct) {        // lane r hands this CTA's state to CTA r
             st_peer4(&sh.parts[rank][0], lane, make_float4(st.mz, st.U, st.sz, st.mx));
-            st_peer4(&sh.parts[rank][1], lane, make_float4(st.W, st.sx, st.cross, careful ? 1.f : 0.f));
+            st_peer4(&sh.parts[rank][1], lane, make_float4(st.W, st.sx, st.cross, careful ? INFINITY : st.off));
         }
         cluster_sync();
         const int k = lane & (kMaxCluster - 1);
-        careful = __any_sync(0xffffffffu, k < nct && sh.parts[k][1].w != 0.f);
+        careful = __any_sync(0xffffffffu, k < nct && was_careful(sh.parts[k]));
         st = meet<KIND, kMaxCluster>(k < nct ? get(sh.parts[k]) : none);
     }
     if constexpr (kEvery) {
@@ -687,8 +718,9 @@ __global__ void __launch_bounds__(THREADS, PER_SM) policy_kernel(const __grid_co
 }
 
 // The statistics alone: lse and the sampled token's log-prob, one row a CTA, nothing kept.  Sums against fixed exponents leave
-// the log-probs without a bias, which a sum over a response's tokens would carry: their mean error over rows of 151,936
-// columns is 1e-8 (5e-7 rms), that of an online log-softmax whose sums are rescaled at every new maximum 1.4e-7.
+// the log-probs without a bias, which a sum over a response's tokens would carry: their mean error over 1,000 rows of 151,936
+// columns is 4e-8 (3.6e-7 rms, fp32's spacing at 8 to 16 being 9.5e-7), that of an online log-softmax whose sums are rescaled
+// at every new maximum 1.4e-7.
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_kernel(const __grid_constant__ PolicyArgs A, float* __restrict__ lse) {
     constexpr int kWarps = THREADS / 32;
@@ -715,7 +747,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_kernel(const __g
         st = meet<kSampled, 32>(lane < kWarps ? get(sh.warps[lane]) : none);
     }
     if (tid != 0) return;
-    const float lz = kLn2 * (log2f(st.sz) - fmaf(st.mz, kLog2e, -st.U)), l = st.mz + lz, lp = in ? (za - st.mz) - lz : 0.f;
+    const float l = -less_log(0.f, st.mz, st.U, st.sz), lp = in ? less_log(za, st.mz, st.U, st.sz) : 0.f;
     if (!in) raise_flag(A.flags, ACRL_FLAG_BAD_ID);
     const bool fine = isfinite(l) && isfinite(lp);
     if (!fine) raise_flag(A.flags, ACRL_FLAG_NONFINITE);
