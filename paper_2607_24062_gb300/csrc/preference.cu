@@ -42,6 +42,13 @@ __device__ __forceinline__ bool range_of(const int64_t* so, int i, int64_t T, in
     return lo >= 0 && lo <= hi && hi <= T;
 }
 
+// a + b = s + e exactly (Knuth 1969), where nothing overflows.
+__device__ __forceinline__ void two_sum(float a, float b, float& s, float& e) {
+    const float t = __fadd_rn(a, b), bb = __fsub_rn(t, a);
+    e = __fadd_rn(__fsub_rn(a, __fsub_rn(t, bb)), __fsub_rn(b, bb));
+    s = t;
+}
+
 __global__ void __launch_bounds__(kRespThreads)
     pref_responses(const float* __restrict__ logp, const float* __restrict__ ref, const uint8_t* __restrict__ mask, int64_t T,
                    const int64_t* __restrict__ so, int S, int mean, PrefWork w, float* __restrict__ ratio, int32_t* flags) {
@@ -58,9 +65,10 @@ __global__ void __launch_bounds__(kRespThreads)
         if (!ok) raise_flag(flags, ACRL_FLAG_BAD_OFFSETS);
         if (i == 0) *w.prompts = 0;
     }
-    double sum = 0.0;
+    // Differences and sums exactly, in two fp32 numbers a thread, then in fp64 (with rounded differences a sum near 0 had lost three
+    // digits; with fp64 a token, 2 a cycle and SM, the kernel took 14 us at 512 x 2,048).  Four tokens a thread in flight.
+    float high = 0.f, low = 0.f;
     int n = 0;
-    // four tokens a thread in flight; differences and sums in fp64 (with fp32 differences a sum near 0 had lost three digits)
     for (int64_t t0 = lo + threadIdx.x; t0 < hi; t0 += 4 * kRespThreads) {
         bool in[4];
         float a[4], b[4];
@@ -74,11 +82,16 @@ __global__ void __launch_bounds__(kRespThreads)
 #pragma unroll
         for (int k = 0; k < 4; ++k)
             if (in[k]) {
-                sum += double(a[k]) - double(b[k]);
+                float d, e;
+                two_sum(a[k], -b[k], d, e);
+                low += e;
+                two_sum(high, d, high, e);
+                low += e;
                 ++n;
             }
     }
-    sum = warp_sum(sum);
+    // an infinite or undefined sum is that of the high parts
+    double sum = warp_sum(isfinite(high) ? double(high) + double(low) : double(high));
     n = __reduce_add_sync(0xffffffffu, n);
     if (lane == 0) {
         sums[wid] = sum;
@@ -130,6 +143,11 @@ __global__ void __launch_bounds__(kPairThreads)
     if (!ok && threadIdx.x == 0) raise_flag(flags, ACRL_FLAG_BAD_OFFSETS);
     long long n = 0;
     double loss = 0.0;
+    // as many lanes a response as there are threads for (whole powers of two up to a warp), its pairs in turn
+    int each = 1;
+    while (each < 32 && 2 * each * (hi - lo) <= kPairThreads) each *= 2;
+    const int part = int(threadIdx.x) & (each - 1), first = lo + int(threadIdx.x) / each;
+    const uint32_t together = (each == 32 ? 0xffffffffu : (1u << each) - 1u) << (lane & ~(each - 1));
     // pairs with the responses [j0, j1) of the prompt, which lie in shared memory; kPairThreads of them at a time
     for (int j0 = lo; j0 < hi; j0 += kPairThreads) {
         const int j1 = min(hi, j0 + kPairThreads), mine = j0 + int(threadIdx.x);
@@ -141,12 +159,12 @@ __global__ void __launch_bounds__(kPairThreads)
             their_ratio[threadIdx.x] = w.ratio[mine];
         }
         __syncthreads();
-        for (int i = lo + int(threadIdx.x); i < hi; i += kPairThreads) {
+        for (int i = first; i < hi; i += kPairThreads / each) {
             const bool here = i >= j0 && i < j1;
             const float Ri = here ? their_reward[i - j0] : w.count[i] > 0 ? rewards[i] : __int_as_float(0x7fc00000);
             const double Di = here ? their_ratio[i - j0] : w.ratio[i];
-            double slope = j0 == lo ? 0.0 : w.slope[i];
-            for (int j = 0; j < j1 - j0; ++j) {
+            double slope = 0.0;
+            for (int j = part; j < j1 - j0; j += each) {
                 const float Rj = their_reward[j];
                 if (!(Ri > Rj || Rj > Ri)) continue;
                 const bool wins = Ri > Rj;
@@ -160,7 +178,8 @@ __global__ void __launch_bounds__(kPairThreads)
                     slope -= v.y;
                 }
             }
-            w.slope[i] = slope;
+            for (int m = each / 2; m >= 1; m >>= 1) slope += __shfl_xor_sync(together, slope, m);
+            if (part == 0) w.slope[i] = j0 == lo ? slope : w.slope[i] + slope;
         }
     }
     loss = warp_sum(loss);
@@ -209,7 +228,9 @@ __global__ void __launch_bounds__(kRespThreads)
     }
     int64_t lo, hi;
     if (!range_of(so, i, T, lo, hi)) return;
-    const float c = Q > 0 ? float(-w.slope[i] / Q) : 0.f;
+    float c = 0.f;                    // one fp64 division a warp: one a thread took 4 us at 512 x 2,048
+    if ((threadIdx.x & 31) == 0 && Q > 0) c = float(-w.slope[i] / Q);
+    c = __shfl_sync(0xffffffffu, c, 0);
 #pragma unroll 4
     for (int64_t t = lo + threadIdx.x; t < hi; t += kRespThreads) coef[t] = !mask || mask[t] ? c : 0.f;
 }
