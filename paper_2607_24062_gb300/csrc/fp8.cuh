@@ -95,22 +95,24 @@ __device__ __forceinline__ Scale block_scale(uint32_t m) {
     return Scale{uint32_t(e + 127), __uint_as_float(uint32_t(127 - e) << 23)};
 }
 
-// Two fp32 to a pair of 8-bit numbers, `lo` in the low byte.
+// Two fp32 numbers times a power of two to a pair of 8-bit numbers, `lo` in the low byte.
 template <int FMT>
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+__device__ __forceinline__ uint32_t pack2(float lo, float hi, float inv) {
     uint16_t r;
     if (FMT == ACRL_FP8_E4M3)
-        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+        asm("{\n .reg .b64 v, s;\n .reg .f32 a, b;\n mov.b64 v, {%1, %2};\n mov.b64 s, {%3, %3};\n mul.rn.f32x2 v, v, s;\n"
+            " mov.b64 {a, b}, v;\n cvt.rn.satfinite.e4m3x2.f32 %0, b, a;\n}" : "=h"(r) : "f"(lo), "f"(hi), "f"(inv));
     else
-        asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+        asm("{\n .reg .b64 v, s;\n .reg .f32 a, b;\n mov.b64 v, {%1, %2};\n mov.b64 s, {%3, %3};\n mul.rn.f32x2 v, v, s;\n"
+            " mov.b64 {a, b}, v;\n cvt.rn.satfinite.e5m2x2.f32 %0, b, a;\n}" : "=h"(r) : "f"(lo), "f"(hi), "f"(inv));
     return r;
 }
 
 template <int FMT>
 __device__ __forceinline__ uint2 pack8(const float (&f)[8], float inv) {
     uint2 o;
-    o.x = pack2<FMT>(f[0] * inv, f[1] * inv) | pack2<FMT>(f[2] * inv, f[3] * inv) << 16;
-    o.y = pack2<FMT>(f[4] * inv, f[5] * inv) | pack2<FMT>(f[6] * inv, f[7] * inv) << 16;
+    o.x = pack2<FMT>(f[0], f[1], inv) | pack2<FMT>(f[2], f[3], inv) << 16;
+    o.y = pack2<FMT>(f[4], f[5], inv) | pack2<FMT>(f[6], f[7], inv) << 16;
     return o;
 }
 

@@ -18,11 +18,20 @@
 namespace acrl {
 namespace {
 
+// Maxima are found in the bits of |x|, which order as unsigned integers: of bf16 two in a word (one instruction for both; as fp32
+// numbers one at a time, 2,507 x 8,200 both ways took 27 us, the ALUs more than half busy), of fp32 one.
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
 // Eight elements as they were loaded: a bf16 tile's registers are half of what its fp32 numbers would take.
 template <typename T>
 struct Eight;
 template <>
 struct Eight<acrl_bf16> {
+    static constexpr int kKeys = 4;       // words of the elements' keys
     uint32_t w[4];
     __device__ __forceinline__ void load(const acrl_bf16* p, int n) {
         if (n >= 8) {
@@ -35,13 +44,75 @@ struct Eight<acrl_bf16> {
             w[j] = (2 * j < n ? uint32_t(p[2 * j]) : 0u) | (2 * j + 1 < n ? uint32_t(p[2 * j + 1]) << 16 : 0u);
     }
     __device__ __forceinline__ float at(int j) const { return j & 1 ? bf16_hi(w[j >> 1]) : bf16_lo(w[j >> 1]); }
+    __device__ __forceinline__ uint32_t key(int k) const { return w[k] & 0x7fff7fffu; }
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return max_u16x2(a, b); }
+    // The keys' maximum as bits of an fp32 number.
+    static __device__ __forceinline__ uint32_t most(const uint32_t (&k)[4]) {
+        const uint32_t m = larger(larger(k[0], k[1]), larger(k[2], k[3]));
+        return max(m << 16, m & 0xffff0000u);
+    }
 };
 template <>
 struct Eight<float> {
+    static constexpr int kKeys = 8;
     float f[8];
     __device__ __forceinline__ void load(const float* p, int n) { load8<float>(p, n, f); }
     __device__ __forceinline__ float at(int j) const { return f[j]; }
+    __device__ __forceinline__ uint32_t key(int k) const { return abs_bits(f[k]); }
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return max(a, b); }
+    static __device__ __forceinline__ uint32_t most(const uint32_t (&k)[8]) {
+        return max(max(max(k[0], k[1]), max(k[2], k[3])), max(max(k[4], k[5]), max(k[6], k[7])));
+    }
 };
+
+// The largest of the eights of sixteen lanes, U of them, as bits of fp32 in every lane; bf16's go through the lanes in pairs.
+template <typename T, int U>
+__device__ __forceinline__ void most_of_sixteen(const Eight<T> (&f)[U], uint32_t (&m)[U]) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        uint32_t k[Eight<T>::kKeys];
+#pragma unroll
+        for (int j = 0; j < Eight<T>::kKeys; ++j) k[j] = f[i].key(j);
+        m[i] = Eight<T>::most(k);
+    }
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int i = 0; i < U; i += 2) {
+            uint32_t v = m[i] >> 16 | m[i + 1];
+#pragma unroll
+            for (int d = 8; d >= 1; d >>= 1) v = max_u16x2(v, __shfl_xor_sync(0xffffffffu, v, d));
+            m[i] = v << 16;
+            m[i + 1] = v & 0xffff0000u;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+#pragma unroll
+            for (int d = 8; d >= 1; d >>= 1) m[i] = max(m[i], __shfl_xor_sync(0xffffffffu, m[i], d));
+    }
+}
+
+// The scales of U (a power of two) maxima that sixteen lanes share: each lane works one out, that of m[lane % U], which it
+// returns, and `inv` has all.
+template <int FMT, int U>
+__device__ __forceinline__ Scale scales_of(const uint32_t (&m)[U], float (&inv)[U]) {
+    const int lane = threadIdx.x & 31;
+    uint32_t mine = m[0];
+#pragma unroll
+    for (int i = 1; i < U; ++i) mine = (lane & (U - 1)) == i ? m[i] : mine;
+    const Scale s = block_scale<FMT>(mine);
+#pragma unroll
+    for (int i = 0; i < U; ++i) inv[i] = __shfl_sync(0xffffffffu, s.inv, (lane & 16) + i);
+    return s;
+}
+
+template <int FMT, typename T>
+__device__ __forceinline__ uint2 pack8(const Eight<T>& f, float inv) {
+    uint2 o;
+    o.x = pack2<FMT>(f.at(0), f.at(1), inv) | pack2<FMT>(f.at(2), f.at(3), inv) << 16;
+    o.y = pack2<FMT>(f.at(4), f.at(5), inv) | pack2<FMT>(f.at(6), f.at(7), inv) << 16;
+    return o;
+}
 
 // The first n (of 8) bytes; p is 8-byte aligned.
 __device__ __forceinline__ void store8(uint8_t* p, const uint2& v, int n) {
@@ -70,36 +141,31 @@ __global__ void __launch_bounds__(kRowThreads)
     const int kb0 = int(unit - row * chunks) * kRowUnroll;
     const bool in = row < R;
     const T* xr = x + (in ? row : 0) * ldx;
-    float f[kRowUnroll][8];
-    uint32_t m[kRowUnroll];
+    Eight<T> f[kRowUnroll];
     // whole units without a test between their loads, so that all of them are in flight together
     if (in && (kb0 + kRowUnroll) * 128 <= C) {
 #pragma unroll
-        for (int k = 0; k < kRowUnroll; ++k) load8<T>(xr + (kb0 + k) * 128 + l * 8, 8, f[k]);
+        for (int k = 0; k < kRowUnroll; ++k) f[k].load(xr + (kb0 + k) * 128 + l * 8, 8);
     } else {
 #pragma unroll
         for (int k = 0; k < kRowUnroll; ++k) {
             const int c = (kb0 + k) * 128 + l * 8;
-            load8<T>(xr + c, in ? C - c : 0, f[k]);
+            f[k].load(xr + c, in ? C - c : 0);
         }
     }
-#pragma unroll
-    for (int k = 0; k < kRowUnroll; ++k) {
-        m[k] = max8(f[k]);
-#pragma unroll
-        for (int d = 8; d >= 1; d >>= 1) m[k] = max(m[k], __shfl_xor_sync(0xffffffffu, m[k], d));
-    }
+    uint32_t m[kRowUnroll];
+    float inv[kRowUnroll];
+    most_of_sixteen<T, kRowUnroll>(f, m);
+    const Scale s = scales_of<FMT, kRowUnroll>(m, inv);
     if (!in) return;
+    if (l < kRowUnroll && kb0 + l < KB) {
+        scale[row * lds + kb0 + l] = uint8_t(s.byte);
+        if (s.byte == 255u) raise_flag(flags, ACRL_FLAG_NONFINITE);
+    }
 #pragma unroll
     for (int k = 0; k < kRowUnroll; ++k) {
-        const int kb = kb0 + k, c = kb * 128 + l * 8;
-        if (kb >= KB) break;
-        const Scale s = block_scale<FMT>(m[k]);
-        if (l == 0) {
-            scale[row * lds + kb] = uint8_t(s.byte);
-            if (s.byte == 255u) raise_flag(flags, ACRL_FLAG_NONFINITE);
-        }
-        if (c < C) store8(q + row * ldq + c, pack8<FMT>(f[k], s.inv), C - c);
+        const int c = (kb0 + k) * 128 + l * 8;
+        if (c < C) store8(q + row * ldq + c, pack8<FMT>(f[k], inv[k]), C - c);
     }
 }
 
@@ -128,14 +194,16 @@ __global__ void __launch_bounds__(kTileThreads<MAKE>, MAKE == kTile ? 3 : 2)
     quantize_tiles(const T* __restrict__ x, int64_t R, int64_t C, int64_t ldx, int col_blocks, Quantised as, Quantised turned,
                    int32_t* flags) {
     constexpr int U = kTileRows<MAKE>, kThreads = kTileThreads<MAKE>;
-    __shared__ uint32_t top[128];                       // of each column (or, of the tile, in the first)
+    constexpr int kWarps = kThreads / 32, kKeys = Eight<T>::kKeys;
+    constexpr bool kOne = MAKE == kTile || MAKE == kTileT;
+    __shared__ uint32_t top[kWarps];                    // kOne: the warps' maxima
+    __shared__ __align__(16) float inverse[kOne ? 4 : 128];   // else each column's 2^-e
     __shared__ __align__(16) uint8_t turn[MAKE == kTile ? 16 : 128 * 128];
     const int lane = threadIdx.x & 31;
     const int g = threadIdx.x >> 4, cl = threadIdx.x & 15;        // rows U g .., columns 8 cl ..
     const int64_t rb = blockIdx.x / col_blocks, cb = blockIdx.x - rb * col_blocks;
     const int64_t r0 = rb * 128 + U * g, c0 = cb * 128 + 8 * cl;
     const int nc = int(min(int64_t(8), C - c0));
-    if (threadIdx.x < 128) top[threadIdx.x] = 0u;
     grid_begin();
     Eight<T> f[U];
     if (r0 + U <= R && nc == 8) {   // no test between the loads: all in flight
@@ -145,39 +213,31 @@ __global__ void __launch_bounds__(kTileThreads<MAKE>, MAKE == kTile ? 3 : 2)
 #pragma unroll
         for (int i = 0; i < U; ++i) f[i].load(x + (r0 + i < R && nc > 0 ? (r0 + i) * ldx + c0 : 0), r0 + i < R ? nc : 0);
     }
-    auto max_of = [&](int i) {
-        uint32_t m = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) m = max(m, abs_bits(f[i].at(j)));
-        return m;
-    };
     auto store_as = [&](int i, float inv) {
-        float v[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = f[i].at(j);
-        if (r0 + i < R && nc > 0) store8(as.q + (r0 + i) * as.ldq + c0, pack8<FMT>(v, inv), nc);
+        if (r0 + i < R && nc > 0) store8(as.q + (r0 + i) * as.ldq + c0, pack8<FMT>(f[i], inv), nc);
     };
     if constexpr (MAKE == kBoth) {   // sixteen lanes hold a row's 128 columns
+        uint32_t m[U];
+        float inv[U];
+        most_of_sixteen<T, U>(f, m);
+        const Scale s = scales_of<FMT, U>(m, inv);
+        if (cl < U && r0 + cl < R) as.scale[(r0 + cl) * as.lds + cb] = uint8_t(s.byte);
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            uint32_t m = max_of(i);
-#pragma unroll
-            for (int d = 8; d >= 1; d >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, d));
-            const Scale s = block_scale<FMT>(m);
-            if (cl == 0 && r0 + i < R) as.scale[(r0 + i) * as.lds + cb] = uint8_t(s.byte);
-            store_as(i, s.inv);
-        }
+        for (int i = 0; i < U; ++i) store_as(i, inv[i]);
     }
-    __syncthreads();
-    float inv[MAKE == kTile || MAKE == kTileT ? 1 : 8];
-    if constexpr (MAKE == kTile || MAKE == kTileT) {
-        uint32_t m = 0;
+    uint32_t k[kKeys];               // the largest of this thread's rows
 #pragma unroll
-        for (int i = 0; i < U; ++i) m = max(m, max_of(i));
-        m = __reduce_max_sync(0xffffffffu, m);
-        if (lane == 0) atomicMax(top, m);
+    for (int j = 0; j < kKeys; ++j) {
+        k[j] = f[0].key(j);
+#pragma unroll
+        for (int i = 1; i < U; ++i) k[j] = Eight<T>::larger(k[j], f[i].key(j));
+    }
+    float inv[kOne ? 1 : 8];
+    if constexpr (kOne) {
+        const uint32_t m = __reduce_max_sync(0xffffffffu, Eight<T>::most(k));
+        if (lane == 0) top[threadIdx.x >> 5] = m;
         __syncthreads();
-        const Scale s = block_scale<FMT>(top[0]);
+        const Scale s = block_scale<FMT>(__reduce_max_sync(0xffffffffu, lane < kWarps ? top[lane] : 0u));
         inv[0] = s.inv;
         if (threadIdx.x == 0) {
             if (MAKE == kTileT) turned.scale[cb * turned.lds + rb] = uint8_t(s.byte);
@@ -185,25 +245,33 @@ __global__ void __launch_bounds__(kTileThreads<MAKE>, MAKE == kTile ? 3 : 2)
             if (s.byte == 255u) raise_flag(flags, ACRL_FLAG_NONFINITE);
         }
     } else {
+        // each warp's maxima of the columns, where the turned elements will be; then a thread a column
+        uint32_t* parts = reinterpret_cast<uint32_t*>(turn);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            uint32_t m = 0;
-#pragma unroll
-            for (int i = 0; i < U; ++i) m = max(m, abs_bits(f[i].at(j)));
-            m = max(m, __shfl_xor_sync(0xffffffffu, m, 16));
-            if (lane < 16) atomicMax(top + 8 * cl + j, m);
+        for (int j = 0; j < kKeys; ++j) {
+            k[j] = Eight<T>::larger(k[j], __shfl_xor_sync(0xffffffffu, k[j], 16));
+            if (lane < 16) parts[((threadIdx.x >> 5) * kKeys + j) * 16 + cl] = k[j];
         }
         __syncthreads();
-#pragma unroll
-        for (int j = 0; j < 8; ++j) inv[j] = block_scale<FMT>(top[8 * cl + j]).inv;
         if (threadIdx.x < 128) {
-            const int64_t c = cb * 128 + threadIdx.x;
-            const Scale mine = block_scale<FMT>(top[threadIdx.x]);
+            // thread t: column 8 (t % 16) + t / 16
+            const int l = threadIdx.x & 15, j = threadIdx.x >> 4, word = j * kKeys / 8;
+            uint32_t most = 0u;
+#pragma unroll
+            for (int i = 0; i < kWarps; ++i) most = Eight<T>::larger(most, parts[(i * kKeys + word) * 16 + l]);
+            if (kKeys == 4) most = j & 1 ? most & 0xffff0000u : most << 16;
+            const Scale mine = block_scale<FMT>(most);
+            inverse[8 * l + j] = mine.inv;
+            const int64_t c = cb * 128 + 8 * l + j;
             if (c < C) {
                 turned.scale[c * turned.lds + rb] = uint8_t(mine.byte);
                 if (mine.byte == 255u) raise_flag(flags, ACRL_FLAG_NONFINITE);
             }
         }
+        __syncthreads();
+        const float4 a = *reinterpret_cast<const float4*>(inverse + 8 * cl), b = *reinterpret_cast<const float4*>(inverse + 8 * cl + 4);
+        inv[0] = a.x; inv[1] = a.y; inv[2] = a.z; inv[3] = a.w;
+        inv[4] = b.x; inv[5] = b.y; inv[6] = b.z; inv[7] = b.w;
     }
     if constexpr (MAKE == kTile) {
 #pragma unroll
@@ -212,7 +280,7 @@ __global__ void __launch_bounds__(kTileThreads<MAKE>, MAKE == kTile ? 3 : 2)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const float by = inv[MAKE == kTileT ? 0 : j];
-            const uint32_t w = pack2<FMT>(f[0].at(j) * by, f[1].at(j) * by) | pack2<FMT>(f[2].at(j) * by, f[3].at(j) * by) << 16;
+            const uint32_t w = pack2<FMT>(f[0].at(j), f[1].at(j), by) | pack2<FMT>(f[2].at(j), f[3].at(j), by) << 16;
             *reinterpret_cast<uint32_t*>(turn + (8 * cl + j) * 128 + 8 * ((g >> 1) ^ cl) + 4 * (g & 1)) = w;
         }
         __syncthreads();
