@@ -607,8 +607,8 @@ acrl_status acrl_fp8_quantize(const void* x, acrl_dtype x_dtype, int64_t R, int6
  * rounded once.  Either operand in either format and with either block.
  *   out   device bf16 or float [M, ldo], 16-byte aligned, ldo >= N a multiple of
  *         8; columns from N on are not written.
- * The operands must be device memory of the current device, as for the LM head
- * (one row of A: any memory the device reads).  K = 0 gives zeros.  Waits are time-bounded (ACRL_FLAG_TIMEOUT: the outputs are
+ * The operands must be device memory of the current device, as for the LM head.
+ * K = 0 gives zeros.  Waits are time-bounded (ACRL_FLAG_TIMEOUT: the outputs are
  * invalid).
  */
 acrl_status acrl_fp8_matmul(const uint8_t* a, int64_t M, int64_t K, int64_t lda, acrl_fp8_format a_format,
@@ -623,7 +623,7 @@ acrl_status acrl_fp8_matmul(const uint8_t* a, int64_t M, int64_t K, int64_t lda,
  *   x          device bf16 [M, ldx].
  *   workspace  device, 16-byte aligned, of acrl_fp8_linear_workspace_bytes
  *              (M, N, K) bytes: the quantised activations (0 bytes, and NULL, for
- *              one row, which the product's kernel quantises itself).
+ *              one row and a small weight, where the product's kernel quantises it).
  */
 int64_t     acrl_fp8_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
 acrl_status acrl_fp8_linear(const acrl_bf16* x, int64_t M, int64_t K, int64_t ldx, acrl_fp8_format x_format,

@@ -1,7 +1,8 @@
 // The product of one row, a token, with an 8-bit matrix: every byte of the matrix is used once, so HBM bounds it, and
 // at the sizes of one layer the latency of a launch.  No tensor cores: their pipeline's start and end (tensor memory,
-// barriers, the split of the sum) and the launch that quantises the row take longer than this product (1 x 4,096 x 4,096: 18
-// us against 10, and 25 against 15 as a call).  A warp takes kW rows of the matrix at a time: each lane loads 16 bytes of each,
+// barriers, the split of the sum) and the launch that quantises the row take longer than a small product: 1,024 x 1,024 3.3 us
+// against 6.6, 4,096 x 4,096 9.3 against 9.1, and 16 against 25 as a call; from there on the tensor cores' way is faster (8,192 x
+// 4,096 14.7 against 11.5).  A warp takes kW rows of the matrix at a time: each lane loads 16 bytes of each,
 // 512 columns a step, two steps ahead, converts them to fp32 through half precision (exact for both formats) and multiplies
 // them with the row, which lies in shared memory as fp32 values of its own scales; the 16 products' sum takes the block's scale.
 // Then the lanes' sums meet in a fixed order.  The row may come as bf16 activations: every CTA then quantises it itself (8 KB for
@@ -17,7 +18,7 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kStep = 512;                      // columns of a warp's step
 constexpr int kW = 2;                           // rows of the matrix a warp takes at a time
 constexpr int kMostBytes = 64 * 1024;           // of the row in shared memory
-constexpr int64_t kFewBytes = 128 << 20;
+constexpr int64_t kFewBytes = 16 << 20;
 
 int64_t few_cols(int64_t K) { return (K + 2 * kStep - 1) / (2 * kStep) * (2 * kStep); }
 

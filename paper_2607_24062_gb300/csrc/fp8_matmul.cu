@@ -50,6 +50,7 @@ constexpr int kRows = 128;             // rows of P per CTA and tile
 constexpr int kSlab = 128;             // columns of a slab: 128 bytes, one row of the 128-byte swizzle
 constexpr int kGroup = 4;              // slabs whose scales share a word
 constexpr int kMaxStages = 12, kScaleSlots = 4;
+constexpr int kMaxSplit = 8;           // CTAs that share a tile's sum; 16 columns are eight's shares
 constexpr uint32_t kTmemCols = 512;
 // Tensor memory: accumulators from column 0, scale slots of 16 columns at the end (P's words in the first four of
 // them, Q's, up to 256 rows, in the last eight).
@@ -574,7 +575,8 @@ __device__ void pair_epilogue(Barriers* bars, uint32_t tmem, const CUtensorMap* 
 }
 
 // A CTA alone: row r of P is column r of `out`, a column of the accumulator a row of it, so a warp stores 32 neighbours.
-// With a split sum the other ranks' accumulators wait in the first rank's shared memory (`parts`, [rank - 1][column][128]).
+// With a split sum each rank adds up a share of the columns: every rank's accumulators of it wait in its shared memory (`parts`,
+// [rank][column of the share][128]; one rank for all took 5 us more for 16 rows of 4,096 x 4,096, 15 more for 64).
 template <typename T>
 __device__ bool alone_epilogue(Barriers* bars, uint32_t tmem, float* parts, const Problem& pr, uint32_t rank, int nct) {
     const int lane = threadIdx.x & 31, quarter = (threadIdx.x >> 5) & 3;
@@ -612,11 +614,15 @@ __device__ bool alone_epilogue(Barriers* bars, uint32_t tmem, float* parts, cons
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
                         if (m0 + j < pr.q.rows) store_one(out + int64_t(m0 + j) * pr.ldo, __uint_as_float(r[j]));
-            } else if (rank > 0) {
-                const float* to = parts + ((int(rank) - 1) * pr.cols + c) * kRows + quarter * 32 + lane;
+            } else {
+                const int per = pr.cols / nct;      // of the share: a power of two of ranks divides the columns
+                const float* to = parts + int(rank) * per * kRows + quarter * 32 + lane;
 #pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(peer_addr(to + j * kRows, 0)), "r"(r[j]) : "memory");
+                for (int j = 0; j < 16; ++j) {
+                    const int owner = (c + j) / per, at = c + j - owner * per;
+                    asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(peer_addr(to + at * kRows, uint32_t(owner))), "r"(r[j])
+                                 : "memory");
+                }
             }
         }
         tc_fence_before();
@@ -630,32 +636,21 @@ __device__ bool alone_epilogue(Barriers* bars, uint32_t tmem, float* parts, cons
     return true;
 }
 
-// The first rank's part of a split sum: its accumulator and the others', in rank order.
+// A rank's share of a split sum: the ranks' accumulators in their order.
 template <typename T>
-__device__ void join(uint32_t tmem, const float* parts, const Problem& pr, int nct) {
-    const int lane = threadIdx.x & 31, quarter = (threadIdx.x >> 5) & 3;
+__device__ void join(const float* parts, const Problem& pr, uint32_t rank, int nct) {
+    const int at = int(threadIdx.x) & (kRows - 1), per = pr.cols / nct;   // four warps, a row of P a thread
     int tp, tq;
     tile_at(int(blockIdx.x) / nct, pr, tp, tq);
-    const int row = tp * kRows + quarter * 32 + lane;
+    const int row = tp * kRows + at, m0 = tq * pr.cols + int(rank) * per;
+    if (row >= pr.p.rows) return;
     T* out = static_cast<T*>(pr.out) + row;
-    tc_fence_after();
-#pragma unroll 1
-    for (int c = 0; c < pr.cols; c += 16) {
-        uint32_t r[16];
-        __syncwarp();
-        asm volatile(
-            "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-            : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-              "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-            : "r"(tmem + uint32_t(c) + (uint32_t(quarter * 32) << 16)));
-        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-        const int m0 = tq * pr.cols + c;
+    for (int j = 0; j < per && m0 + j < pr.q.rows; ++j) {
+        float v = 0.f;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            float v = __uint_as_float(r[j]);
-            for (int k = 1; k < nct; ++k) v += parts[((k - 1) * pr.cols + c + j) * kRows + quarter * 32 + lane];
-            if (row < pr.p.rows && m0 + j < pr.q.rows) store_one(out + int64_t(m0 + j) * pr.ldo, v);
-        }
+        for (int k = 0; k < kMaxSplit; ++k)
+            if (k < nct) v += parts[(k * per + j) * kRows + at];
+        store_one(out + int64_t(m0 + j) * pr.ldo, v);
     }
 }
 
@@ -709,8 +704,7 @@ __global__ void __launch_bounds__(kThreads<MODE>, 1)
     if (PAIR || nct > 1) cluster_sync();   // the others' barriers are initialised, and they run
     tc_fence_after();
     const uint32_t tmem = bars->tmem_base;
-    // the parts of a split sum wait in the ring's place, which no copy writes any more when they arrive (the ring of the
-    // first rank is still read by its own MMAs, so they go behind what it uses)
+    // the parts of a split sum, behind the stages
     float* parts = reinterpret_cast<float*>(ring + pr.stages * (kRows + pr.cols) * kSlab);
     bool ok = true;
     if (warp == 0) {
@@ -728,11 +722,7 @@ __global__ void __launch_bounds__(kThreads<MODE>, 1)
     tc_fence_before();
     __syncthreads();
     if (PAIR || nct > 1) cluster_sync();   // no CTA frees its TMEM or leaves while another may still touch it
-    if (!PAIR && nct > 1 && rank == 0 && warp >= 6 && ok) join<T>(tmem, parts, pr, nct);
-    if (!PAIR) {
-        tc_fence_before();
-        __syncthreads();
-    }
+    if (!PAIR && nct > 1 && warp >= 6 && ok) join<T>(parts, pr, rank, nct);
     if (warp == 2) {
         tc_fence_after();
         if (PAIR)
@@ -747,10 +737,13 @@ Operand operand(const Matrix& m) {
                    (m.lds & 3) == 0 && (reinterpret_cast<uintptr_t>(m.scale) & 3) == 0};
 }
 
-// Rows up to this many become the MMA's columns: with fewer tiles than SMs, where the sum is split and its parts go
-// through shared memory, kSplitRows (64 x 4,096 x 4,096: 27 us, as pairs 18; 16: 18).
-constexpr int64_t kAloneRows = 128, kSplitRows = 32;
-constexpr int kMaxSplit = 8;
+// Rows up to kAloneRows become the MMA's columns, where the weight has tiles for more than half of the SMs; with fewer tiles
+// the sum is split, at a price that grows with the rows, and the rows are up to kSplitRows, or kSplitRowsASlab for each slab of
+// the sum.  us, alone / as pairs, for 16, 64 and 128 rows:
+//     16,384 x 4,096  14.4 / 24.0  15.7 / 20.5  18.0 / 20.9        4,096 x 4,096   7.8 / 18.7  10.1 / 17.1  13.2 / 17.3
+//    151,936 x 4,096  99.9 / 121   99.1 / 122    102 / 128         1,024 x 2,048   5.4 / 9.3    7.7 / 9.5   10.7 / 9.7
+//      9,800 x 1,024   5.6 / 8.9    7.1 / 8.8    9.2 / 8.4         4,096 x 1,024   6.0 / 7.9    9.0 / 7.7   13.2 / 7.4
+constexpr int64_t kAloneRows = 128, kSplitRows = 32, kSplitRowsASlab = 6;
 
 template <typename T, int MODE>
 acrl_status launch_kernel(const Matrix& p, const Matrix& q, int64_t K, Problem pr, int64_t grid, int cluster, cudaStream_t s) {
@@ -785,12 +778,13 @@ acrl_status launch_matmul(const Matrix& a, const Matrix& b, int64_t K, void* out
     int dev = 0, sms = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
         return launch_status();
-    const bool alone = a.rows <= kSplitRows || (a.rows <= kAloneRows && b.rows >= int64_t(kRows) * sms);
+    const int64_t slabs = (K + kSlab - 1) / kSlab, tiles = (b.rows + kRows - 1) / kRows;
+    const bool alone = a.rows <= (2 * tiles > sms ? kAloneRows : std::min(kAloneRows, std::max(kSplitRows, kSplitRowsASlab * slabs)));
     const Matrix &p = alone ? b : a, &q = alone ? a : b;
     Problem pr = {};
     pr.p = operand(p);
     pr.q = operand(q);
-    pr.slabs = int((K + kSlab - 1) / kSlab);
+    pr.slabs = int(slabs);
     pr.out = out;
     pr.ldo = ldo;
     pr.flags = flags;
@@ -804,12 +798,8 @@ acrl_status launch_matmul(const Matrix& a, const Matrix& b, int64_t K, void* out
         // as many CTAs a tile as keep all SMs busy, each with four slabs or more
         int split = 1;
         while (split < kMaxSplit && 2 * split * pr.p_tiles <= sms && (pr.slabs + kGroup - 1) / kGroup >= 2 * split) split *= 2;
-        const int parts = (split - 1) * pr.cols * kRows * 4;
-        pr.stages = std::min(kMaxStages, (kRingBytes<T, kAlone> - parts) / bytes);
-        while (pr.stages < 2) {   // never for up to 128 columns and eight parts of 64 KB less one
-            split /= 2;
-            pr.stages = std::min(kMaxStages, (kRingBytes<T, kAlone> - (split - 1) * pr.cols * kRows * 4) / bytes);
-        }
+        const int parts = split > 1 ? pr.cols * kRows * 4 : 0;
+        pr.stages = std::min(kMaxStages, (kRingBytes<T, kAlone> - parts) / bytes);   // 128 columns: 5
         pr.idesc |= uint32_t(pr.cols >> 3) << 17 | 1u << 27;
         const int64_t grid = split > 1 ? int64_t(pr.p_tiles) * split : std::min(pr.p_tiles, sms);
         return launch_kernel<T, kAlone>(p, q, K, pr, grid, split, s);

@@ -808,14 +808,30 @@ acrl_status launch_rows(PolicyArgs A, int ctas, cudaStream_t s) {
 template <Kind KIND>
 acrl_status launch_policy(const PolicyArgs& A, cudaStream_t s) {
     const int64_t bytes = int64_t(A.V >> 3) * (KIND == kSampled ? 16 : 32);    // of a row
-    int ctas = 1;      // few rows: several CTAs each
-    while (ctas < kMaxCluster && 2 * ctas * A.T <= 152 && bytes / ctas > 16 * 1024) ctas *= 2;
+    // Few rows: several CTAs each, of 16 KB or more.  V = 151,936 over the vocabulary, 1 / 2 / 4 / 8 CTAs a row: 19 rows
+    // 27.3 / 19.1 / 15.1 / 15.4 us, 76 rows 27.9 / 21.2 / 29.0 / 31.0, 152 rows 33.5 / 35.7 / 50.9 / 55.9.
+    int ctas = 1;
+    while (ctas < kMaxCluster && 2 * ctas * A.T <= kSms && bytes / ctas > 16 * 1024) ctas *= 2;
+    // Threads by the row's bytes: few enough that rows share an SM, enough that a row's latency shows little.  600 MB of each
+    // operand over the vocabulary (from log-probs), us:
+    //     row      32         64         128        256        512        1,024
+    //      9 KB    185 (210)  226 (213)
+    //     11 KB    202 (225)  200 (203)  330 (282)
+    //     18 KB    190 (286)  178 (206)  232 (220)
+    //     24 KB               182 (247)  193 (203)  276 (278)
+    //     44 KB               189 (301)  169 (213)  197 (222)
+    //     52 KB                          197 (244)  185 (213)  244 (260)
+    //     72 KB                          180 (254)  168 (207)  210 (232)
+    //     90 KB                                     192 (236)  190 (217)
+    //    310 KB                                     277 (380)  181 (256)  222 (302)
+    //    350 KB                                     256 (386)  215 (284)  211 (313)
+    //    600 KB                                     310 (497)  250 (349)  191 (343)
     const int64_t slice = bytes / ctas;
-    if (slice <= 9 * 1024) return launch_rows<KIND, 32, 24>(A, ctas, s);
-    if (slice <= 16 * 1024) return launch_rows<KIND, 64, 13>(A, ctas, s);
-    if (slice <= 40 * 1024) return launch_rows<KIND, 128, 5>(A, ctas, s);
-    if (slice <= 72 * 1024) return launch_rows<KIND, 256, 3>(A, ctas, s);
-    if (KIND == kSampled || slice <= 300 * 1024) return launch_rows<KIND, 512, 2>(A, ctas, s);
+    if (slice <= 10 * 1024) return launch_rows<KIND, 32, 24>(A, ctas, s);
+    if (slice <= 20 * 1024) return launch_rows<KIND, 64, 13>(A, ctas, s);
+    if (slice <= 48 * 1024) return launch_rows<KIND, 128, 5>(A, ctas, s);
+    if (slice <= 84 * 1024) return launch_rows<KIND, 256, 3>(A, ctas, s);
+    if (KIND == kSampled || slice <= 340 * 1024) return launch_rows<KIND, 512, 2>(A, ctas, s);
     return launch_rows<KIND, 1024, 1>(A, ctas, s);
 }
 
@@ -834,7 +850,9 @@ acrl_status row_logp(const acrl_bf16* logits, int64_t T, int64_t V, int64_t ld, 
         A.logp = logp + t;
         A.T = std::min(kMaxGrid, T - t);
         auto run = [&](auto* kernel, int threads) { return launch(kernel, A.T, threads, 0, 0, s, A, lse + t); };
-        const acrl_status st = V <= 4096 ? run(logp_kernel<32>, 32) : V <= 16384 ? run(logp_kernel<64>, 64) : V <= 65536 ? run(logp_kernel<128>, 128) : run(logp_kernel<256>, 256);
+        // with the pairs and the gradient, 32 / 128 / 256 threads a row: 48,828 x 4,096 218 / 271 / 375 us, 12,207 x 16,384
+        // 208 / 204 / 214, 1,316 x 151,936 212 / 212 / 204
+        const acrl_status st = V <= 8192 ? run(logp_kernel<32>, 32) : V <= 65536 ? run(logp_kernel<128>, 128) : run(logp_kernel<256>, 256);
         if (st != ACRL_OK) return st;
     }
     return ACRL_OK;
