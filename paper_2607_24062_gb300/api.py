@@ -461,7 +461,7 @@ _FP8_BLOCK = {"row": _abi.FP8_ROW, "tile": _abi.FP8_TILE}
 _OUT_DTYPE = {torch.bfloat16: _abi.BF16, torch.float32: _abi.F32}
 
 
-@dataclass
+@dataclass(frozen=True)
 class Fp8Tensor:
     """An 8-bit matrix [rows, cols]: q (torch.float8_e4m3fn or float8_e5m2, rows at a stride of 16 bytes) and the
     scales of its blocks, uint8 [rows or ceil(rows / 128), ceil(cols / 128)], byte s standing for 2^(s - 127)."""
@@ -482,11 +482,27 @@ class Fp8Tensor:
         if SC < (C + 127) // 128 or (SR != R and SR != (R + 127) // 128):
             raise AcrlError(f"scale: shape {(SR, SC)} fits neither the rows nor the 128 x 128 tiles of {(R, C)}")
         # one row is one tile of one row: the same scales either way
-        self.block = "row" if SR == R else "tile"
-        # address, rows, row stride, format, scales' address, their row stride, block: as the library takes a matrix (of a
-        # single row, or with nothing in a row, the stride says nothing, and any that the library accepts will do)
-        self._args = (q.data_ptr(), R, ldq if R > 1 and C > 0 else (C + 15) // 16 * 16, _FP8_FORMAT[q.dtype],
-                      s.data_ptr(), lds if SR > 1 and SC > 0 else SC, _FP8_BLOCK[self.block])
+        block = "row" if SR == R else "tile"
+        # of a single row, or with nothing in a row, the stride says nothing, and any that the library accepts will do
+        self._known(block, R, ldq if R > 1 and C > 0 else (C + 15) // 16 * 16, _FP8_FORMAT[q.dtype],
+                    lds if SR > 1 and SC > 0 else SC)
+
+    def _known(self, block: str, rows: int, ldq: int, code: int, lds: int) -> None:
+        self.__dict__.update(block=block, _layout=(rows, ldq, code, lds, _FP8_BLOCK[block]))
+
+    @property
+    def _args(self):
+        """Address, rows, row stride, format, scales' address, their row stride, block: as the library takes a matrix."""
+        rows, ldq, code, lds, block = self._layout
+        return self.q.data_ptr(), rows, ldq, code, self.scale.data_ptr(), lds, block
+
+    @classmethod
+    def _made(cls, q, scale, *known):
+        """One whose parts need no check."""
+        t = object.__new__(cls)
+        t.__dict__.update(q=q, scale=scale)
+        t._known(*known)
+        return t
 
     @property
     def shape(self):
@@ -545,8 +561,9 @@ def fp8_quantize(x, *, block="row", fmt="e4m3", transpose=False, out: Fp8Tensor 
     srows, kb = (rows if kind == _abi.FP8_ROW else (rows + 127) // 128), (cols + 127) // 128
     if out is None:
         ldq, lds = (cols + 15) // 16 * 16, (kb + 3) // 4 * 4
-        out = Fp8Tensor(torch.empty_strided((rows, cols), (ldq, 1), dtype=dtype, device=x.device),
-                        torch.empty_strided((srows, kb), (lds, 1), dtype=torch.uint8, device=x.device))
+        out = Fp8Tensor._made(torch.empty_strided((rows, cols), (ldq, 1), dtype=dtype, device=x.device),
+                              torch.empty_strided((srows, kb), (lds, 1), dtype=torch.uint8, device=x.device),
+                              "row" if srows == rows else "tile", rows, ldq, code, lds)
     elif tuple(out.q.shape) != (rows, cols) or out.q.dtype != dtype or out.scale.shape[0] != srows:
         raise AcrlError(f"out: an 8-bit matrix of another shape, format or block than {(rows, cols)} {fmt} {block}")
     if flags is not None:
