@@ -110,11 +110,20 @@ struct Problem {
     int slabs;             // ceil(K / 128)
     int cols;              // columns of a tile (rows of Q): a multiple of 32 (pair) or 16
     int p_tiles, q_tiles;
-    int stages;
-    int accs;              // accumulators
     uint32_t idesc, idesc2;   // idesc2: of a wide tile's second part
     void* out;
     int64_t ldo;
+    bool f32;              // the output's type, where a launch has both
+};
+
+// One launch: one problem, or two whose tiles share the pairs.
+template <int N>
+struct Launch {
+    CUtensorMap p[N], q[N], o[N];
+    Problem pr[N];
+    int stages, stage_bytes;
+    int acc_cols;          // of an accumulator
+    int more_first, most_else, extra;   // N == 2: tiles of the second problem, see Tiles
     int32_t* flags;
 };
 
@@ -168,27 +177,52 @@ __device__ __forceinline__ void tma_load(void* dst, const CUtensorMap* map, uint
             : "memory");
 }
 
-// What a CTA works on: pairs take tiles in turn, slab by slab; alone, a cluster of CTAs splits one tile's slabs.
-template <bool PAIR>
-struct Work {
-    int first, step;    // tiles
-    int lo, hi;         // slabs
-    __device__ Work(const Problem& pr, uint32_t rank) {
-        if (PAIR) {
-            first = int(blockIdx.x >> 1);
+// What a CTA works on.  Pairs take tiles in turn, all slabs of each; of two problems the first one's, and then consecutive tiles of
+// the second, as many as even out what the first left unequal (share_out): `more_first` for a pair that has one tile more of
+// the first, `most_else` or one more for the others.  Alone, a cluster of CTAs splits one tile's slabs.
+template <int MODE, int N>
+struct Tiles {
+    int tile, step, count;
+    int second, end;       // N == 2: the second problem's tiles
+    int which = 0;
+    int lo = 0, hi;        // slabs
+    __device__ Tiles(const Launch<N>& L, uint32_t rank) {
+        count = L.pr[0].p_tiles * L.pr[0].q_tiles;
+        hi = L.pr[0].slabs;
+        second = end = 0;
+        if (MODE != kAlone) {
+            tile = int(blockIdx.x >> 1);
             step = int(gridDim.x >> 1);
-            lo = 0;
-            hi = pr.slabs;
+            if (N == 2) {
+                const int full = count % step, i = tile - full;   // pairs below `full` have a tile more of the first problem
+                second = i < 0 ? tile * L.more_first : full * L.more_first + i * L.most_else + min(i, L.extra);
+                end = second + (i < 0 ? L.more_first : L.most_else + (i < L.extra ? 1 : 0));
+            }
         } else {
             const int parts = int(cluster_size());
-            first = int(blockIdx.x) / parts;
+            tile = int(blockIdx.x) / parts;
             step = int(gridDim.x) / parts;
             // whole groups of slabs, so that a word of scales is one CTA's
-            const int groups = (pr.slabs + kGroup - 1) / kGroup, per = (groups + parts - 1) / parts * kGroup;
-            lo = min(pr.slabs, int(rank) * per);
-            hi = min(pr.slabs, lo + per);
+            const int groups = (hi + kGroup - 1) / kGroup, per = (groups + parts - 1) / parts * kGroup, slabs = hi;
+            lo = min(slabs, int(rank) * per);
+            hi = min(slabs, lo + per);
+        }
+        turn(L);
+    }
+    __device__ __forceinline__ void turn(const Launch<N>& L) {
+        if (N == 2 && which == 0 && tile >= count) {
+            which = 1;
+            tile = second;
+            count = end;
+            hi = L.pr[N - 1].slabs;
         }
     }
+    __device__ __forceinline__ bool more() const { return tile < count; }
+    __device__ __forceinline__ void next(const Launch<N>& L) {
+        tile += which ? 1 : step;
+        turn(L);
+    }
+    __device__ __forceinline__ const Problem& problem(const Launch<N>& L) const { return L.pr[N == 2 ? which : 0]; }
 };
 
 // Tiles in bands of kBand row tiles, all column tiles of a band in turn, so that the tiles in flight share operands in L2.
@@ -217,28 +251,29 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volati
 // The producer's and the MMA warp's loops run in the whole warp, and one lane is elected for each batch of copies or MMAs:
 // stage, descriptors and coordinates are then the same for the warp and live in the uniform registers that those
 // instructions take.  Run by one lane of a diverged warp, the MMA loop took 900 cycles a slab, twice the MMAs' time.
-template <bool PAIR>
-__device__ void produce(const CUtensorMap* tmP, const CUtensorMap* tmQ, uint8_t* ring, Barriers* bars, const Problem& pr,
-                        uint32_t rank) {
+template <int MODE, int N>
+__device__ void produce(const Launch<N>& L, uint8_t* ring, Barriers* bars, uint32_t rank) {
+    constexpr bool PAIR = MODE != kAlone;
     volatile int32_t* abort = &bars->abort;
-    const int q_rows = PAIR ? pr.cols / 2 : pr.cols, bytes = (kRows + q_rows) * kSlab;
-    const Work<PAIR> w(pr, rank);
     int stage = 0;
     uint32_t phase = 0;
     long issued = 0;
-    for (int t = w.first; t < pr.p_tiles * pr.q_tiles; t += w.step) {
+    for (Tiles<MODE, N> w(L, rank); w.more(); w.next(L)) {
+        const Problem& pr = w.problem(L);
+        const CUtensorMap *tmP = &L.p[N == 2 ? w.which : 0], *tmQ = &L.q[N == 2 ? w.which : 0];
+        const int q_rows = PAIR ? pr.cols / 2 : pr.cols, bytes = (kRows + q_rows) * kSlab;
         int tp, tq;
-        tile_at(t, pr, tp, tq);
+        tile_at(w.tile, pr, tp, tq);
         const int p0 = PAIR ? (2 * tp + int(rank)) * kRows : tp * kRows;
         const int q0 = tq * pr.cols + (PAIR ? int(rank) * q_rows : 0);
         for (int kb = w.lo; kb < w.hi; ++kb) {
             if (!warp_wait(&bars->empty[stage], phase ^ 1u, abort)) {
-                give_up(abort, pr.flags);
+                give_up(abort, L.flags);
                 // the copies that were started land before the CTA can exit: the even CTA's barriers count both CTAs',
                 // the odd one gives its own time to land
                 if (!PAIR || rank == 0) {
-                    for (long j = issued - 1; j >= 0 && j >= issued - pr.stages; --j)
-                        wait_phase(&bars->full[j % pr.stages], uint32_t((j / pr.stages) & 1), nullptr);
+                    for (long j = issued - 1; j >= 0 && j >= issued - L.stages; --j)
+                        wait_phase(&bars->full[j % L.stages], uint32_t((j / L.stages) & 1), nullptr);
                 } else {
                     const uint64_t t0 = global_ns();
                     while (global_ns() - t0 < 100000ull) {
@@ -246,7 +281,7 @@ __device__ void produce(const CUtensorMap* tmP, const CUtensorMap* tmQ, uint8_t*
                 }
                 return;
             }
-            uint8_t* s = ring + stage * bytes;
+            uint8_t* s = ring + stage * L.stage_bytes;
             const uint32_t bar = PAIR ? peer_addr(&bars->full[stage], 0) : smem_u32(&bars->full[stage]);
             if (elect_one()) {
                 if (!PAIR || rank == 0) mbar_expect_tx(&bars->full[stage], (PAIR ? 2 : 1) * bytes);
@@ -254,7 +289,7 @@ __device__ void produce(const CUtensorMap* tmP, const CUtensorMap* tmQ, uint8_t*
                 tma_load<PAIR>(s + kRows * kSlab, tmQ, bar, kb * kSlab, q0);
             }
             ++issued;
-            if (++stage == pr.stages) {
+            if (++stage == L.stages) {
                 stage = 0;
                 phase ^= 1u;
             }
@@ -262,23 +297,23 @@ __device__ void produce(const CUtensorMap* tmP, const CUtensorMap* tmQ, uint8_t*
     }
 }
 
-template <int MODE>
-__device__ void issue_mmas(uint8_t* ring, Barriers* bars, uint32_t tmem, const Problem& pr, uint32_t rank) {
+template <int MODE, int N>
+__device__ void issue_mmas(const Launch<N>& L, uint8_t* ring, Barriers* bars, uint32_t tmem, uint32_t rank) {
     constexpr bool PAIR = MODE != kAlone;
     volatile int32_t* abort = &bars->abort;
-    const uint32_t units = uint32_t((kRows + (PAIR ? pr.cols / 2 : pr.cols)) * kSlab) >> 4;   // of a stage, in descriptors
+    const uint32_t units = uint32_t(L.stage_bytes) >> 4;   // of a stage, in descriptors
     const uint64_t pdesc0 = smem_desc(smem_u32(ring)), qdesc0 = smem_desc(smem_u32(ring + kRows * kSlab));
-    const Work<PAIR> w(pr, rank);
     int stage = 0, slot = 0, acc = 0;
     uint32_t phase = 0, sphase = 0, aphase = 0;
     bool ok = true;
-    for (int t = w.first; t < pr.p_tiles * pr.q_tiles && ok; t += w.step) {
+    for (Tiles<MODE, N> w(L, rank); w.more() && ok; w.next(L)) {
+        const Problem& pr = w.problem(L);
         if (!warp_wait(&bars->tempty[acc], aphase ^ 1u, abort)) {
-            give_up(abort, pr.flags);
+            give_up(abort, L.flags);
             break;
         }
         tc_fence_after();
-        const uint32_t d = tmem + uint32_t(acc * pr.cols);
+        const uint32_t d = tmem + uint32_t(acc * L.acc_cols);
         for (int kb = w.lo; kb < w.hi && ok; kb += kGroup) {
             ok = warp_wait(&bars->sfull[slot], sphase, abort);
             const uint32_t sc = tmem + kScaleBase + uint32_t(slot) * kSlotCols<MODE>;
@@ -313,7 +348,7 @@ __device__ void issue_mmas(uint8_t* ring, Barriers* bars, uint32_t tmem, const P
                     mmas(d, qd, pr.idesc, sc + 8);
                     commit<PAIR>(&bars->empty[stage]);
                 }
-                if (++stage == pr.stages) {
+                if (++stage == L.stages) {
                     stage = 0;
                     phase ^= 1u;
                 }
@@ -326,13 +361,13 @@ __device__ void issue_mmas(uint8_t* ring, Barriers* bars, uint32_t tmem, const P
             }
         }
         if (!ok) {
-            give_up(abort, pr.flags);
+            give_up(abort, L.flags);
             break;
         }
         if (elect_one()) commit<PAIR>(&bars->tfull[MODE == kWide ? 1 : acc]);
         if (MODE == kWide) {
             aphase ^= 1u;
-        } else if (++acc == pr.accs) {
+        } else if (++acc == 2) {
             acc = 0;
             aphase ^= 1u;
         }
@@ -377,39 +412,39 @@ __device__ __forceinline__ void scale_words(const Operand& o, int row, int kb, i
 }
 
 // The groups of slabs of a CTA's tiles, in the order that the MMAs take them.
-template <int MODE>
+template <int MODE, int N>
 struct Groups {
     static constexpr bool PAIR = MODE != kAlone;
     static constexpr int kQ = MODE == kWide ? 16 : 8, kWords = 4 + kQ;
-    const Problem& pr;
-    const Work<PAIR> w;
+    const Launch<N>& L;
+    Tiles<MODE, N> w;
     const int lane;
     const uint32_t rank;
-    int t, kb, p0, q0;
-    __device__ Groups(const Problem& problem, uint32_t r) : pr(problem), w(problem, r), lane(threadIdx.x & 31), rank(r) {
-        t = w.first;
+    int kb, p0, q0;
+    __device__ Groups(const Launch<N>& l, uint32_t r) : L(l), w(l, r), lane(threadIdx.x & 31), rank(r) {
         kb = w.lo;
-        if (w.lo == w.hi) t = pr.p_tiles * pr.q_tiles;
+        if (w.lo == w.hi) w.tile = w.count;
         place();
     }
-    __device__ bool more() const { return t < pr.p_tiles * pr.q_tiles; }
     __device__ void place() {
-        if (!more()) return;
+        if (!w.more()) return;
+        const Problem& pr = w.problem(L);
         int tp, tq;
-        tile_at(t, pr, tp, tq);
+        tile_at(w.tile, pr, tp, tq);
         p0 = (PAIR ? 2 * tp + int(rank) : tp) * kRows + lane;
         q0 = tq * pr.cols + lane;
     }
     // This lane's words of the group at hand, and on to the next.
     __device__ bool take(uint32_t (&v)[kWords]) {
-        if (!more()) return false;
+        if (!w.more()) return false;
+        const Problem& pr = w.problem(L);
         scale_words<4>(pr.p, p0, kb, pr.slabs, 0, 0, v);
 #pragma unroll
         for (int j = 0; j < kQ; j += 8) scale_words<8>(pr.q, q0, kb, pr.slabs, MODE == kWide ? pr.cols / 64 : 0, j, v + 4 + j);
         kb += kGroup;
         if (kb >= w.hi) {
+            w.next(L);
             kb = w.lo;
-            t += w.step;
             place();
         }
         return true;
@@ -417,10 +452,10 @@ struct Groups {
 };
 
 // Words are loaded two groups ahead of their use (wide tiles, of longer groups: one).
-template <int MODE>
-__device__ void write_scales(Barriers* bars, uint32_t tmem, const Problem& pr, uint32_t rank) {
+template <int MODE, int N>
+__device__ void write_scales(const Launch<N>& L, Barriers* bars, uint32_t tmem, uint32_t rank) {
     constexpr bool PAIR = MODE != kAlone;
-    constexpr int kWords = Groups<MODE>::kWords;
+    constexpr int kWords = Groups<MODE, N>::kWords;
     volatile int32_t* abort = &bars->abort;
     const int lane = threadIdx.x & 31;
     const uint32_t lanes = uint32_t((threadIdx.x >> 5) & 3) << 21;   // this warp's quarter, 32 lanes each
@@ -429,7 +464,7 @@ __device__ void write_scales(Barriers* bars, uint32_t tmem, const Problem& pr, u
     auto write = [&](const uint32_t (&v)[kWords]) {
         const bool free = wait_phase(&bars->sempty[slot], phase ^ 1u, abort);
         if (!__all_sync(0xffffffffu, free)) {
-            give_up(abort, pr.flags);
+            give_up(abort, L.flags);
             return false;
         }
         tc_fence_after();
@@ -458,7 +493,7 @@ __device__ void write_scales(Barriers* bars, uint32_t tmem, const Problem& pr, u
         }
         return true;
     };
-    Groups<MODE> g(pr, rank);
+    Groups<MODE, N> g(L, rank);
     uint32_t a[kWords], b[kWords];
     bool na = g.take(a), nb = g.take(b);
     if constexpr (MODE == kWide) {
@@ -487,25 +522,59 @@ __device__ __forceinline__ void store_one(acrl_bf16* p, float v) { *p = acrl_bf1
 
 // Accumulators of a pair's tile: each warp its 32 rows, 32 columns at a time, rounded, staged in shared memory and
 // stored by a TMA copy, which leaves out what is beyond the matrix.
-template <typename T, int MODE>
-__device__ void pair_epilogue(Barriers* bars, uint32_t tmem, const CUtensorMap* tmO, uint8_t* staging, const Problem& pr,
-                              uint32_t rank) {
+// T: the outputs' type, of two problems the larger (Problem::f32 says which each has).
+template <typename T, int MODE, int N>
+__device__ void pair_epilogue(const Launch<N>& L, Barriers* bars, uint32_t tmem, uint8_t* staging, uint32_t rank) {
     volatile int32_t* abort = &bars->abort;
     const int lane = threadIdx.x & 31, quarter = (threadIdx.x >> 5) & 3;
     constexpr int kBuf = kBlocks<T, MODE>, kStep = 32 * (kDrain<MODE> / 4);   // the warps of a quarter take chunks in turn
     const int first = 32 * (((threadIdx.x >> 5) - 6) >> 2);
     uint8_t* blocks = staging + ((threadIdx.x >> 5) - 6) * kBuf * kOutBlock<T>;
-    // row `lane` of a block, its 16-byte pieces permuted by the swizzle of the output's map: 64-byte rows in fours
-    // (bf16), 128-byte rows in eights (fp32)
-    constexpr int kPieces = 32 * int(sizeof(T)) / 16;
-    const uint32_t at = smem_u32(blocks) + uint32_t(lane * 32 * int(sizeof(T)));
-    const uint32_t swz = kPieces == 4 ? uint32_t((lane >> 1) & 3) : uint32_t(lane & 7);
     int buf = 0, acc = 0;
     uint32_t phase = 0;
-    const Work<true> w(pr, rank);
-    for (int t = w.first; t < pr.p_tiles * pr.q_tiles; t += w.step) {
+    // 32 columns of this warp's rows to `out`, rounded to U
+    auto store = [&](auto type, const Problem& pr, const CUtensorMap* tmO, const uint32_t (&r)[32], int row0, int col0) {
+        using U = decltype(type);
+        if (row0 >= pr.p.rows || col0 >= pr.q.rows) return;   // the same for the whole warp
+        if (col0 + 32 > pr.q.rows && (pr.q.rows * int(sizeof(U)) & 15) != 0) {
+            // a TMA store leaves columns out in 16-byte pieces: here the last ones would write beyond the matrix
+            U* out = static_cast<U*>(pr.out) + int64_t(row0 + lane) * pr.ldo + col0;
+            if (row0 + lane < pr.p.rows)
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (col0 + j < pr.q.rows) store_one(out + j, __uint_as_float(r[j]));
+            return;
+        }
+        if (lane == 0) bulk_wait_read<kBuf - 1>();              // the store that last read this block is done
+        __syncwarp();
+        // row `lane` of a block, its 16-byte pieces permuted by the swizzle of the output's map: 64-byte rows in fours
+        // (bf16), 128-byte rows in eights (fp32)
+        constexpr int kPieces = 32 * int(sizeof(U)) / 16;
+        const uint32_t swz = kPieces == 4 ? uint32_t((lane >> 1) & 3) : uint32_t(lane & 7);
+        uint8_t* block = blocks + buf * kOutBlock<T>;
+        const uint32_t to = smem_u32(block) + uint32_t(lane * 32 * int(sizeof(U)));
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) {
+            uint4 v;
+            if constexpr (sizeof(U) == 2)
+                v = make_uint4(pack_bf16x2(__uint_as_float(r[8 * k]), __uint_as_float(r[8 * k + 1])),
+                               pack_bf16x2(__uint_as_float(r[8 * k + 2]), __uint_as_float(r[8 * k + 3])),
+                               pack_bf16x2(__uint_as_float(r[8 * k + 4]), __uint_as_float(r[8 * k + 5])),
+                               pack_bf16x2(__uint_as_float(r[8 * k + 6]), __uint_as_float(r[8 * k + 7])));
+            else
+                v = make_uint4(r[4 * k], r[4 * k + 1], r[4 * k + 2], r[4 * k + 3]);
+            st_shared16(to + ((uint32_t(k) ^ swz) << 4), v);
+        }
+        fence_async_shared();
+        __syncwarp();
+        if (lane == 0) tma_store_2d(tmO, block, col0, row0);
+        if (kBuf > 1) buf ^= 1;
+    };
+    for (Tiles<MODE, N> w(L, rank); w.more(); w.next(L)) {
+        const Problem& pr = w.problem(L);
+        const CUtensorMap* tmO = &L.o[N == 2 ? w.which : 0];
         int tp, tq;
-        tile_at(t, pr, tp, tq);
+        tile_at(w.tile, pr, tp, tq);
         const int row0 = (2 * tp + int(rank)) * kRows + quarter * 32;
         bool ready = true;
 #pragma unroll 1
@@ -520,52 +589,27 @@ __device__ void pair_epilogue(Barriers* bars, uint32_t tmem, const CUtensorMap* 
             for (int c = c0; c < end; c += kStep) {
                 uint32_t r[32];
                 __syncwarp();
-                tmem_ld32(tmem + uint32_t((MODE == kWide ? 0 : acc * pr.cols) + c) + (uint32_t(quarter * 32) << 16), r);
+                tmem_ld32(tmem + uint32_t((MODE == kWide ? 0 : acc * L.acc_cols) + c) + (uint32_t(quarter * 32) << 16), r);
                 if (c + kStep >= end) {   // read out: the even CTA's MMA warp may fill it again
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) remote_arrive(peer_addr(&bars->tempty[a], 0));
                 }
                 const int col0 = tq * pr.cols + (MODE == kWide ? 32 * wide_chunk(c / 32, pr.cols / 64) : c);
-                if (row0 >= pr.p.rows || col0 >= pr.q.rows) continue;   // the same for the whole warp
-                if (col0 + 32 > pr.q.rows && (pr.q.rows * int(sizeof(T)) & 15) != 0) {
-                    // a TMA store leaves columns out in 16-byte pieces: here the last ones would write beyond the matrix
-                    T* out = static_cast<T*>(pr.out) + int64_t(row0 + lane) * pr.ldo + col0;
-                    if (row0 + lane < pr.p.rows)
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (col0 + j < pr.q.rows) store_one(out + j, __uint_as_float(r[j]));
-                    continue;
-                }
-                if (lane == 0) bulk_wait_read<kBuf - 1>();              // the store that last read this block is done
-                __syncwarp();
-                const uint32_t to = at + uint32_t(buf * kOutBlock<T>);
-#pragma unroll
-                for (int k = 0; k < kPieces; ++k) {
-                    uint4 v;
-                    if constexpr (sizeof(T) == 2)
-                        v = make_uint4(pack_bf16x2(__uint_as_float(r[8 * k]), __uint_as_float(r[8 * k + 1])),
-                                       pack_bf16x2(__uint_as_float(r[8 * k + 2]), __uint_as_float(r[8 * k + 3])),
-                                       pack_bf16x2(__uint_as_float(r[8 * k + 4]), __uint_as_float(r[8 * k + 5])),
-                                       pack_bf16x2(__uint_as_float(r[8 * k + 6]), __uint_as_float(r[8 * k + 7])));
-                    else
-                        v = make_uint4(r[4 * k], r[4 * k + 1], r[4 * k + 2], r[4 * k + 3]);
-                    st_shared16(to + ((uint32_t(k) ^ swz) << 4), v);
-                }
-                fence_async_shared();
-                __syncwarp();
-                if (lane == 0) tma_store_2d(tmO, blocks + buf * kOutBlock<T>, col0, row0);
-                if (kBuf > 1) buf ^= 1;
+                if (N == 2 && !pr.f32)
+                    store(acrl_bf16{}, pr, tmO, r, row0, col0);
+                else
+                    store(T{}, pr, tmO, r, row0, col0);
             }
             __syncwarp();
         }
         if (!ready) {
-            give_up(abort, pr.flags);
+            give_up(abort, L.flags);
             break;
         }
         if (MODE == kWide) {
             phase ^= 1u;
-        } else if (++acc == pr.accs) {
+        } else if (++acc == 2) {
             acc = 0;
             phase ^= 1u;
         }
@@ -578,18 +622,18 @@ __device__ void pair_epilogue(Barriers* bars, uint32_t tmem, const CUtensorMap* 
 // With a split sum each rank adds up a share of the columns: every rank's accumulators of it wait in its shared memory (`parts`,
 // [rank][column of the share][128]; one rank for all took 5 us more for 16 rows of 4,096 x 4,096, 15 more for 64).
 template <typename T>
-__device__ bool alone_epilogue(Barriers* bars, uint32_t tmem, float* parts, const Problem& pr, uint32_t rank, int nct) {
+__device__ bool alone_epilogue(const Launch<1>& L, Barriers* bars, uint32_t tmem, float* parts, uint32_t rank, int nct) {
+    const Problem& pr = L.pr[0];
     const int lane = threadIdx.x & 31, quarter = (threadIdx.x >> 5) & 3;
     const uint32_t lanes = uint32_t(quarter * 32) << 16;
-    const Work<false> w(pr, rank);
     int acc = 0;
     uint32_t phase = 0;
-    for (int t = w.first; t < pr.p_tiles * pr.q_tiles; t += w.step) {
+    for (Tiles<kAlone, 1> w(L, rank); w.more(); w.next(L)) {
         int tp, tq;
-        tile_at(t, pr, tp, tq);
+        tile_at(w.tile, pr, tp, tq);
         const bool ready = wait_phase(&bars->tfull[acc], phase, &bars->abort);
         if (!__all_sync(0xffffffffu, ready)) {
-            give_up(&bars->abort, pr.flags);
+            give_up(&bars->abort, L.flags);
             return false;
         }
         tc_fence_after();
@@ -603,7 +647,7 @@ __device__ bool alone_epilogue(Barriers* bars, uint32_t tmem, float* parts, cons
                 "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-                : "r"(tmem + uint32_t(acc * pr.cols + c) + lanes));
+                : "r"(tmem + uint32_t(acc * L.acc_cols + c) + lanes));
             asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
             if (w.lo == w.hi)   // no slab left for this rank: nothing was accumulated
 #pragma unroll
@@ -628,7 +672,7 @@ __device__ bool alone_epilogue(Barriers* bars, uint32_t tmem, float* parts, cons
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&bars->tempty[acc]);
-        if (++acc == pr.accs) {
+        if (++acc == 2) {
             acc = 0;
             phase ^= 1u;
         }
@@ -654,10 +698,8 @@ __device__ void join(const float* parts, const Problem& pr, uint32_t rank, int n
     }
 }
 
-template <typename T, int MODE>
-__global__ void __launch_bounds__(kThreads<MODE>, 1)
-    fp8_matmul_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CUtensorMap tmQ,
-                      const __grid_constant__ CUtensorMap tmO, const __grid_constant__ Problem pr) {
+template <typename T, int MODE, int N>
+__global__ void __launch_bounds__(kThreads<MODE>, 1) fp8_matmul_kernel(const __grid_constant__ Launch<N> L) {
     constexpr bool PAIR = MODE != kAlone;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -682,8 +724,8 @@ __global__ void __launch_bounds__(kThreads<MODE>, 1)
         mbar_init(&bars->mma_done, 1);
         bars->abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmP)) : "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmQ)) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&L.p[0])) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&L.q[0])) : "memory");
     }
     grid_begin();
     if (warp == 2) {
@@ -705,24 +747,26 @@ __global__ void __launch_bounds__(kThreads<MODE>, 1)
     tc_fence_after();
     const uint32_t tmem = bars->tmem_base;
     // the parts of a split sum, behind the stages
-    float* parts = reinterpret_cast<float*>(ring + pr.stages * (kRows + pr.cols) * kSlab);
+    float* parts = reinterpret_cast<float*>(ring + L.stages * L.stage_bytes);
     bool ok = true;
     if (warp == 0) {
-        produce<PAIR>(&tmP, &tmQ, ring, bars, pr, rank);
+        produce<MODE, N>(L, ring, bars, rank);
     } else if (warp == 1) {
-        if (!PAIR || rank == 0) issue_mmas<MODE>(ring, bars, tmem, pr, rank);
+        if (!PAIR || rank == 0) issue_mmas<MODE, N>(L, ring, bars, tmem, rank);
     } else if (warp < 6) {
-        write_scales<MODE>(bars, tmem, pr, rank);
+        write_scales<MODE, N>(L, bars, tmem, rank);
     } else if constexpr (PAIR) {
-        pair_epilogue<T, MODE>(bars, tmem, &tmO, staging, pr, rank);
+        pair_epilogue<T, MODE, N>(L, bars, tmem, staging, rank);
     } else {
-        ok = alone_epilogue<T>(bars, tmem, parts, pr, rank, nct);
+        ok = alone_epilogue<T>(L, bars, tmem, parts, rank, nct);
     }
     __syncwarp();
     tc_fence_before();
     __syncthreads();
     if (PAIR || nct > 1) cluster_sync();   // no CTA frees its TMEM or leaves while another may still touch it
-    if (!PAIR && nct > 1 && warp >= 6 && ok) join<T>(parts, pr, rank, nct);
+    if constexpr (!PAIR) {
+        if (nct > 1 && warp >= 6 && ok) join<T>(parts, L.pr[0], rank, nct);
+    }
     if (warp == 2) {
         tc_fence_after();
         if (PAIR)
@@ -745,91 +789,148 @@ Operand operand(const Matrix& m) {
 //      9,800 x 1,024   5.6 / 8.9    7.1 / 8.8    9.2 / 8.4         4,096 x 1,024   6.0 / 7.9    9.0 / 7.7   13.2 / 7.4
 constexpr int64_t kAloneRows = 128, kSplitRows = 32, kSplitRowsASlab = 6;
 
-template <typename T, int MODE>
-acrl_status launch_kernel(const Matrix& p, const Matrix& q, int64_t K, Problem pr, int64_t grid, int cluster, cudaStream_t s) {
-    constexpr bool PAIR = MODE != kAlone;
-    CUtensorMap tmP, tmQ, tmO;
+// The tensor maps of a problem: P's rows and Q's, and the output's for a pair's stores.
+template <int MODE>
+bool maps_of(const Matrix& p, const Matrix& q, int64_t K, const Problem& pr, CUtensorMap* tmP, CUtensorMap* tmQ, CUtensorMap* tmO) {
     auto map = [&](CUtensorMap* m, const Matrix& x, int box_rows) {
         return encode_map(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, x.q, uint64_t(x.rows), uint64_t(K), uint64_t(x.ld), box_rows,
                           kSlab, CU_TENSOR_MAP_SWIZZLE_128B);
     };
-    if (!map(&tmP, p, kRows) || !map(&tmQ, q, PAIR ? pr.cols / 2 : pr.cols)) return ACRL_ERR_CUDA;
-    constexpr bool bf16 = sizeof(T) == 2;
-    if (!PAIR)
-        tmO = tmP;   // not used
-    else if (!encode_map(&tmO, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, sizeof(T), pr.out,
-                         uint64_t(p.rows), uint64_t(q.rows), uint64_t(pr.ldo), 32, 32,
-                         bf16 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B))
-        return ACRL_ERR_CUDA;
-    auto* kernel = fp8_matmul_kernel<T, MODE>;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) != cudaSuccess)
-        return launch_status();
-    if (PAIR) {   // no more than can be resident at once: they are persistent
-        const int64_t most = resident_clusters(reinterpret_cast<const void*>(kernel), kThreads<MODE>, kSmemBytes, 2);
-        if (most < 1) return ACRL_ERR_CUDA;
-        grid = std::min<int64_t>(grid, 2 * most);
+    if (!map(tmP, p, kRows) || !map(tmQ, q, MODE == kAlone ? pr.cols : pr.cols / 2)) return false;
+    if (MODE == kAlone) {
+        *tmO = *tmP;   // not used
+        return true;
     }
-    return launch(kernel, grid, kThreads<MODE>, kSmemBytes, cluster, s, tmP, tmQ, tmO, pr);
+    return encode_map(tmO, pr.f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, pr.f32 ? 4 : 2, pr.out,
+                      uint64_t(p.rows), uint64_t(q.rows), uint64_t(pr.ldo), 32, 32,
+                      pr.f32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
+}
+
+// Allows the kernel its shared memory; the pairs of CTAs that can be resident at once.
+template <typename T, int MODE, int N>
+int64_t resident_pairs() {
+    auto* kernel = fp8_matmul_kernel<T, MODE, N>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return 0;
+    }
+    return MODE == kAlone ? kMaxGrid : resident_clusters(reinterpret_cast<const void*>(kernel), kThreads<MODE>, kSmemBytes, 2);
+}
+
+// `grid`: of pairs' launches twice the tiles, of which as many run as can be resident at once: they are persistent.
+template <typename T, int MODE, int N>
+acrl_status launch_kernel(const Launch<N>& L, int64_t grid, int cluster, cudaStream_t s) {
+    const int64_t most = resident_pairs<T, MODE, N>();
+    if (most < 1) return ACRL_ERR_CUDA;
+    if (MODE != kAlone) grid = std::min<int64_t>(grid, 2 * most);
+    return launch(fp8_matmul_kernel<T, MODE, N>, grid, kThreads<MODE>, kSmemBytes, cluster, s, L);
+}
+
+template <typename T, int MODE>
+acrl_status launch_one(const Matrix& p, const Matrix& q, int64_t K, const Problem& pr, int stage_bytes, int stages, int64_t grid,
+                       int cluster, int32_t* flags, cudaStream_t s) {
+    Launch<1> L = {};
+    L.pr[0] = pr;
+    L.stages = std::min(kMaxStages, stages);
+    L.stage_bytes = stage_bytes;
+    L.acc_cols = pr.cols;
+    L.flags = flags;
+    if (!maps_of<MODE>(p, q, K, pr, &L.p[0], &L.q[0], &L.o[0])) return ACRL_ERR_CUDA;
+    return launch_kernel<T, MODE, 1>(L, grid, cluster, s);
+}
+
+// out = A B^T, as a problem of pairs or alone.
+Problem problem_of(const Matrix& p, const Matrix& q, int64_t K, void* out, int64_t ldo, bool f32) {
+    Problem pr = {};
+    pr.p = operand(p);
+    pr.q = operand(q);
+    pr.slabs = int((K + kSlab - 1) / kSlab);
+    pr.out = out;
+    pr.ldo = ldo;
+    pr.f32 = f32;
+    pr.idesc = kIdescBase | uint32_t(p.format) << 7 | uint32_t(q.format) << 10;
+    return pr;
+}
+
+// Whether A's rows become the MMA's columns.
+bool rows_alone(int64_t rows, int64_t cols, int64_t K, int sms) {
+    const int64_t slabs = (K + kSlab - 1) / kSlab, tiles = (cols + kRows - 1) / kRows;
+    return rows <= (2 * tiles > sms ? kAloneRows : std::min(kAloneRows, std::max(kSplitRows, kSplitRowsASlab * slabs)));
+}
+
+// The cost of a pair's tile, in loads of one of a slab's rows (1.5 ns): the loads of a slab, 128 rows of P and half the
+// columns a CTA, take longest; a wide tile's MMAs also wait for the drain of the one before, and an fp32 output's stores take
+// their share of the way to L2 (8,200 x 2,048 x 2,504 in tiles of 224 columns 9.4 us a tile, 7.5 as bf16).
+int64_t tile_cost(const Problem& pr) {
+    constexpr int64_t kTileCost = 300, kWideCost = 2000;
+    return int64_t(pr.slabs) * (128 + pr.cols / 2) + (pr.cols > kPart ? kWideCost : kTileCost) + (pr.f32 ? 5 * pr.cols : 0);
+}
+
+// Sets a pair's tiles to `cols` columns.
+void cut(Problem& pr, int cols) {
+    pr.cols = cols;
+    pr.p_tiles = (pr.p.rows + 2 * kRows - 1) / (2 * kRows);
+    pr.q_tiles = (pr.q.rows + cols - 1) / cols;
+}
+void describe(Problem& pr) {
+    pr.idesc2 = pr.idesc | uint32_t((pr.cols - kPart) >> 3) << 17 | 2u << 27;
+    pr.idesc |= uint32_t(std::min(pr.cols, kPart) >> 3) << 17 | 2u << 27;
+}
+int64_t tiles_of(const Problem& pr) { return int64_t(pr.p_tiles) * pr.q_tiles; }
+
+// Columns of a pair's tile: all pairs run whole rounds of tiles, so the least rounds x cost.  224 / 320 / 448
+// columns: 4,096 x 4,096 x 4,096 (76 pairs: 4, 3 and 3 rounds) 52 / 56 / 63 us, 2,504 x 2,048 x 8,200 (2, 1 and 1) 61 / 44 / 47,
+// 8,192 x 8,192 x 1,024 (16, 11 and 8) 65 / 77 / 69, 4,096 x 151,936 x 4,096 (143, 101 and 72) 1,680 / 1,660 / 1,510.
+// Narrow ones where the last round would be short: 1,500 x 6,000 x 1,024 of 192 / 224: 18.1 / 18.7 us.
+int64_t cut_best(Problem& pr, int pairs) {
+    int64_t least = 0;
+    int best = 0;
+    for (int cols = 2 * kPairCols; cols >= 96; cols -= cols > kPart ? 64 : 32) {
+        cut(pr, cols);
+        const int64_t cost = (tiles_of(pr) + pairs - 1) / pairs * tile_cost(pr);
+        if (least == 0 || cost < least) {
+            least = cost;
+            best = cols;
+        }
+        if (cols == kPart + 64) cols = kPairCols + 32;   // two accumulators of 256 do not fit
+    }
+    cut(pr, best);
+    return least;
+}
+
+bool sms_of_device(int& sms) {
+    int dev = 0;
+    return cudaGetDevice(&dev) == cudaSuccess && cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess;
 }
 
 template <typename T>
 acrl_status launch_matmul(const Matrix& a, const Matrix& b, int64_t K, void* out, int64_t ldo, int32_t* flags,
                           cudaStream_t s) {
-    int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-        return launch_status();
-    const int64_t slabs = (K + kSlab - 1) / kSlab, tiles = (b.rows + kRows - 1) / kRows;
-    const bool alone = a.rows <= (2 * tiles > sms ? kAloneRows : std::min(kAloneRows, std::max(kSplitRows, kSplitRowsASlab * slabs)));
+    int sms = 0;
+    if (!sms_of_device(sms)) return launch_status();
+    const bool alone = rows_alone(a.rows, b.rows, K, sms);
     const Matrix &p = alone ? b : a, &q = alone ? a : b;
-    Problem pr = {};
-    pr.p = operand(p);
-    pr.q = operand(q);
-    pr.slabs = int(slabs);
-    pr.out = out;
-    pr.ldo = ldo;
-    pr.flags = flags;
-    pr.idesc = kIdescBase | uint32_t(p.format) << 7 | uint32_t(q.format) << 10;
+    Problem pr = problem_of(p, q, K, out, ldo, sizeof(T) == 4);
     if (alone) {
         pr.cols = int((q.rows + 15) / 16 * 16);
         pr.p_tiles = int((p.rows + kRows - 1) / kRows);
         pr.q_tiles = 1;
-        pr.accs = 2;
+        pr.idesc |= uint32_t(pr.cols >> 3) << 17 | 1u << 27;
         const int bytes = (kRows + pr.cols) * kSlab;
         // as many CTAs a tile as keep all SMs busy, each with four slabs or more
         int split = 1;
         while (split < kMaxSplit && 2 * split * pr.p_tiles <= sms && (pr.slabs + kGroup - 1) / kGroup >= 2 * split) split *= 2;
         const int parts = split > 1 ? pr.cols * kRows * 4 : 0;
-        pr.stages = std::min(kMaxStages, (kRingBytes<T, kAlone> - parts) / bytes);   // 128 columns: 5
-        pr.idesc |= uint32_t(pr.cols >> 3) << 17 | 1u << 27;
         const int64_t grid = split > 1 ? int64_t(pr.p_tiles) * split : std::min(pr.p_tiles, sms);
-        return launch_kernel<T, kAlone>(p, q, K, pr, grid, split, s);
+        return launch_one<T, kAlone>(p, q, K, pr, bytes, (kRingBytes<T, kAlone> - parts) / bytes, grid, split, flags, s);
     }
-    pr.p_tiles = int((p.rows + 2 * kRows - 1) / (2 * kRows));
-    // Columns of a tile: the loads of a slab, 128 rows of P and half the columns a CTA, take longest (1.5 ns for one of them),
-    // a wide tile's MMAs also wait for the drain of the one before, and all pairs run whole rounds of tiles.  224 / 320 / 448
-    // columns: 4,096 x 4,096 x 4,096 (76 pairs: 4, 3 and 3 rounds) 52 / 56 / 63 us, 2,504 x 2,048 x 8,200 (2, 1 and 1) 61 / 44 / 47,
-    // 8,192 x 8,192 x 1,024 (16, 11 and 8) 65 / 77 / 69, 4,096 x 151,936 x 4,096 (143, 101 and 72) 1,680 / 1,660 / 1,510.
-    // Narrow ones where the last round would be short: 1,500 x 6,000 x 1,024 of 192 / 224: 18.1 / 18.7 us.
-    constexpr int64_t kTileCost = 300, kWideCost = 2000;
-    int64_t total = 0, least = 0;
-    for (int cols = 2 * kPairCols; cols >= 96; cols -= cols > kPart ? 64 : 32) {
-        const int64_t tiles = int64_t(pr.p_tiles) * ((q.rows + cols - 1) / cols);
-        const int64_t cost = (tiles + sms / 2 - 1) / (sms / 2) * (pr.slabs * (128 + cols / 2) + (cols > kPart ? kWideCost : kTileCost));
-        if (least == 0 || cost < least) {
-            least = cost;
-            total = tiles;
-            pr.cols = cols;
-        }
-        if (cols == kPart + 64) cols = kPairCols + 32;   // two accumulators of 256 do not fit
-    }
-    pr.q_tiles = int((q.rows + pr.cols - 1) / pr.cols);
-    if (total > kMaxGrid / 2) return ACRL_ERR_INVALID_ARG;
-    const bool wide = pr.cols > kPart;
-    pr.accs = 2;
-    pr.stages = std::min(kMaxStages, (wide ? kRingBytes<T, kWide> : kRingBytes<T, kPair>) / ((kRows + pr.cols / 2) * kSlab));
-    pr.idesc2 = pr.idesc | uint32_t((pr.cols - kPart) >> 3) << 17 | 2u << 27;
-    pr.idesc |= uint32_t(std::min(pr.cols, kPart) >> 3) << 17 | 2u << 27;
-    return wide ? launch_kernel<T, kWide>(p, q, K, pr, 2 * total, 2, s) : launch_kernel<T, kPair>(p, q, K, pr, 2 * total, 2, s);
+    cut_best(pr, sms / 2);
+    if (tiles_of(pr) > kMaxGrid / 2) return ACRL_ERR_INVALID_ARG;
+    describe(pr);
+    const int bytes = (kRows + pr.cols / 2) * kSlab;
+    return pr.cols > kPart
+               ? launch_one<T, kWide>(p, q, K, pr, bytes, kRingBytes<T, kWide> / bytes, 2 * tiles_of(pr), 2, flags, s)
+               : launch_one<T, kPair>(p, q, K, pr, bytes, kRingBytes<T, kPair> / bytes, 2 * tiles_of(pr), 2, flags, s);
 }
 
 // Checked operands of one row or more each.
@@ -858,6 +959,84 @@ acrl_status matmul(const Matrix& a, const Matrix& b, int64_t K, void* out, acrl_
         if (!few_rows(a.rows, b.rows, K) && !operands_on_current_device({a.q, b.q, out})) return ACRL_ERR_INVALID_ARG;
     }
     return product(a, b, K, out, out_dtype, ldo, flags, s);
+}
+
+// Two products at once: their tiles share the pairs, so that a part-filled last round of one is filled by the other, and one
+// launch's start and end are saved.  Both gradients with their quantisation, together / apart, us, by rows, K and N: 200 x 1,024 x
+// 1,024 14 / 20, 1,024 x 1,024 x 4,096 26 / 37, 1,500 x 1,536 x 6,000 48 / 64, 4,096 x 4,096 x 4,096 135 / 146; narrow tiles only, so
+// the largest stay apart (4,096 x 4,096 x 16,384 502 / 473).
+struct Product {
+    const Matrix &a, &b;
+    int64_t K;
+    void* out;
+    acrl_dtype type;
+    int64_t ldo;
+};
+
+// How the second problem's n1 tiles of cost c1 are shared out among the pairs when n0 of cost c0 were taken in turn; the time
+// of the busiest pair.
+int64_t share_out(int64_t n0, int64_t c0, int64_t n1, int64_t c1, int64_t pairs, Launch<2>& L) {
+    const int64_t full = n0 % pairs, each = n0 / pairs, others = pairs - full;
+    const int64_t even = ((n0 * c0 + n1 * c1) / pairs - (each + 1) * c0) / c1;    // for a pair with one more of the first
+    int64_t least = 0;
+    for (int64_t m = std::max<int64_t>(0, even); m <= std::max<int64_t>(0, even) + 1; ++m) {
+        if (full * m > n1) break;
+        const int64_t left = n1 - full * m, some = left / others, extra = left % others;
+        const int64_t time = std::max(full > 0 ? (each + 1) * c0 + m * c1 : 0, each * c0 + (some + (extra > 0)) * c1);
+        if (least > 0 && time >= least) continue;
+        least = time;
+        L.more_first = int(m);
+        L.most_else = int(some);
+        L.extra = int(extra);
+    }
+    return least > 0 ? least : kMaxGrid * kMaxGrid / 4;
+}
+
+acrl_status two_products(const Product& x, const Product& y, int32_t* flags, cudaStream_t s) {
+    constexpr int64_t kLaunchCost = 3000;   // of a launch's start and end, 4.5 us
+    int sms = 0;
+    if (!sms_of_device(sms)) return launch_status();
+    auto pairs_work = [&](const Product& p) { return !few_rows(p.a.rows, p.b.rows, p.K) && !rows_alone(p.a.rows, p.b.rows, p.K, sms); };
+    if (x.K > 0 && y.K > 0 && pairs_work(x) && pairs_work(y)) {
+        const int64_t resident = resident_pairs<float, kPair, 2>();
+        Launch<2> L = {};
+        const Product* of[2] = {&x, &y};
+        Problem pr[2];
+        int64_t apart = kLaunchCost, cost[2];
+        for (int i = 0; i < 2; ++i) {
+            const Product& p = *of[i];
+            pr[i] = problem_of(p.a, p.b, p.K, p.out, p.ldo, p.type == ACRL_F32);
+            apart += cut_best(pr[i], sms / 2);
+            int best = 0;
+            for (int cols = kPairCols; cols >= 96; cols -= 32) {   // the least work: there are no rounds to fill
+                cut(pr[i], cols);
+                const int64_t c = tiles_of(pr[i]) * tile_cost(pr[i]);
+                if (best == 0 || c < cost[i]) {
+                    cost[i] = c;
+                    best = cols;
+                }
+            }
+            cut(pr[i], best);
+            cost[i] = tile_cost(pr[i]);
+            describe(pr[i]);
+        }
+        const int first = cost[0] >= cost[1] ? 0 : 1;              // the longer tiles
+        const int64_t n0 = tiles_of(pr[first]), n1 = tiles_of(pr[1 - first]), pairs = std::min(resident, n0 + n1);
+        if (pairs > 0 && n0 + n1 <= kMaxGrid / 2 && share_out(n0, cost[first], n1, cost[1 - first], pairs, L) < apart) {
+            for (int i = 0; i < 2; ++i) {
+                const int k = i == 0 ? first : 1 - first;
+                L.pr[i] = pr[k];
+                L.stage_bytes = std::max(L.stage_bytes, (kRows + pr[k].cols / 2) * kSlab);
+                if (!maps_of<kPair>(of[k]->a, of[k]->b, of[k]->K, pr[k], &L.p[i], &L.q[i], &L.o[i])) return ACRL_ERR_CUDA;
+            }
+            L.stages = std::min(kMaxStages, kRingBytes<float, kPair> / L.stage_bytes);
+            L.acc_cols = kPairCols;
+            L.flags = flags;
+            return launch_kernel<float, kPair, 2>(L, 2 * pairs, 2, s);
+        }
+    }
+    const acrl_status st = product(x.a, x.b, x.K, x.out, x.type, x.ldo, flags, s);
+    return st != ACRL_OK ? st : product(y.a, y.b, y.K, y.out, y.type, y.ldo, flags, s);
 }
 
 }  // namespace
@@ -975,7 +1154,6 @@ extern "C" acrl_status acrl_fp8_linear_backward(const acrl_bf16* dy, int64_t M, 
     if (st == ACRL_OK)
         st = acrl_fp8_quantize(x, ACRL_BF16, M, K, ldx, x_format, ACRL_FP8_ROW, 1, base + parts.xt.at, parts.xt.ldq,
                                const_cast<uint8_t*>(xt.scale), parts.xt.lds, dev_flags, stream);
-    if (st == ACRL_OK) st = product(a, w, N, dx, dx_dtype, lddx, dev_flags, s);
-    if (st == ACRL_OK) st = product(at, xt, M, dw, dw_dtype, lddw, dev_flags, s);
+    if (st == ACRL_OK) st = two_products({a, w, N, dx, dx_dtype, lddx}, {at, xt, M, dw, dw_dtype, lddw}, dev_flags, s);
     return st;
 }

@@ -262,3 +262,19 @@ def test_refusals():
                  lambda: acrl.fp8_linear(x, w, workspace=torch.empty(8, dtype=torch.uint8, device=DEV))):
         with pytest.raises(acrl.AcrlError):
             call()
+
+
+@pytest.mark.parametrize("M,N,K", [(200, 300, 520), (515, 1030, 264), (1300, 264, 2056), (131, 20000, 136), (3000, 520, 520)])
+@pytest.mark.parametrize("dx_dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("dw_dtype", [torch.bfloat16, torch.float32])
+def test_both_gradients_are_the_products(M, N, K, dx_dtype, dw_dtype):
+    """The two gradients of one call, bit for bit those of two calls on the quantised matrices; nothing beyond them is written."""
+    dy, x, w = _matrix(M, N, 41), _matrix(M, K, 42), _matrix(N, K, 43, std=0.02)
+    wt = acrl.fp8_quantize(w, block="tile", transpose=True)
+    dx, dw = torch.full((M + 1, K), 3.0, dtype=dx_dtype, device=DEV), torch.full((N + 1, K), 3.0, dtype=dw_dtype, device=DEV)
+    acrl.fp8_linear_backward(dy, x, wt, fmt="e5m2", dx_dtype=dx_dtype, dw_dtype=dw_dtype, dx=dx[:M], dw=dw[:N])
+    by_rows = acrl.fp8_quantize(dy, fmt="e5m2")
+    turned, xt = acrl.fp8_quantize(dy, fmt="e5m2", transpose=True), acrl.fp8_quantize(x, transpose=True)
+    assert torch.equal(dx[:M], acrl.fp8_matmul(by_rows, wt, out_dtype=dx_dtype))
+    assert torch.equal(dw[:N], acrl.fp8_matmul(turned, xt, out_dtype=dw_dtype))
+    assert bool((dx[M:] == 3.0).all()) and bool((dw[N:] == 3.0).all())
