@@ -69,6 +69,15 @@ def _call(name: str, tensors, stream, *args) -> None:
         check(st, name)
 
 
+def _on_stream(f, name: str, t, stream, *args, **kw):
+    """f(*args, **kw) with `stream` the current one: what it allocates then belongs to the stream that uses it.  (Memory of
+    the current stream could still be in use there, or be handed out again while `stream` has yet to read it.)"""
+    if stream.device.index != t.get_device():
+        raise AcrlError(f"{name}: stream on {stream.device}, buffers on {t.device}")
+    with torch.cuda.stream(stream):
+        return f(*args, **kw)
+
+
 def _flags(flags, dev):
     return new_flags(dev) if flags is None else _need(flags, torch.int32, 1, "flags")
 
@@ -549,6 +558,9 @@ def fp8_quantize(x, *, block="row", fmt="e4m3", transpose=False, out: Fp8Tensor 
     128 columns of a row (block="row") or per 128 x 128 ("tile")."""
     if not isinstance(x, torch.Tensor) or x.dim() != 2 or not x.is_cuda:
         raise AcrlError("x: expected a 2-D CUDA tensor")
+    if stream is not None:
+        return _on_stream(fp8_quantize, "acrl_fp8_quantize", x, stream, x, block=block, fmt=fmt, transpose=transpose, out=out,
+                          flags=flags)
     xt = _OUT_DTYPE.get(x.dtype)
     (R, C), (ldx, cs) = x.shape, x.stride()
     if xt is None or (cs != 1 and C > 1):
@@ -569,7 +581,7 @@ def fp8_quantize(x, *, block="row", fmt="e4m3", transpose=False, out: Fp8Tensor 
     if flags is not None:
         _need(flags, torch.int32, 1, "flags")
     ptr, _, ldq, _, sptr, lds, _ = out._args
-    _call("acrl_fp8_quantize", (x, out.q, out.scale, flags), stream, x.data_ptr(), xt, R, C,
+    _call("acrl_fp8_quantize", (x, out.q, out.scale, flags), None, x.data_ptr(), xt, R, C,
           ldx if R > 1 and C > 0 else (C + 15) // 16 * 16, code, kind, 1 if transpose else 0, ptr, ldq, sptr, lds,
           None if flags is None else flags.data_ptr())
     return out
@@ -583,12 +595,14 @@ def _product_out(out, M: int, N: int, dtype, dev):
     if not isinstance(out, torch.Tensor) or out.dtype not in _OUT_DTYPE or out.dim() != 2 or not out.is_cuda or \
             (out.shape[1] > 1 and out.stride(1) != 1) or out.shape[0] != M or out.shape[1] < N:
         raise AcrlError(f"out: expected a bfloat16 or float32 CUDA matrix of {(M, N)} with unit column stride")
-    return out[:, :N], out.stride(0) if M > 1 and N > 0 else (N + 7) // 8 * 8
+    return out if out.shape[1] == N else out[:, :N], out.stride(0) if M > 1 and N > 0 else (N + 7) // 8 * 8
 
 
 def fp8_matmul(a: Fp8Tensor, b: Fp8Tensor, *, out_dtype=torch.bfloat16, out=None, flags=None, stream=None):
     """acrl_fp8_matmul: a [M, K] times the transpose of b [N, K], as `out_dtype` [M, N]."""
     aa, bb = _fp8_args(a, "a"), _fp8_args(b, "b")
+    if stream is not None:
+        return _on_stream(fp8_matmul, "acrl_fp8_matmul", a.q, stream, a, b, out_dtype=out_dtype, out=out, flags=flags)
     M, N, K = a.shape[0], b.shape[0], a.shape[1]
     if b.shape[1] != K:
         raise AcrlError(f"a and b disagree on K: {K} and {b.shape[1]}")
@@ -596,7 +610,7 @@ def fp8_matmul(a: Fp8Tensor, b: Fp8Tensor, *, out_dtype=torch.bfloat16, out=None
         raise AcrlError(f"out_dtype: {out_dtype}, expected bfloat16 or float32")
     out, ldo = _product_out(out, M, N, out_dtype, a.q.device)
     _opt(flags, torch.int32, 1, "flags")
-    _call("acrl_fp8_matmul", (a.q, a.scale, b.q, b.scale, out, flags), stream, aa[0], M, K, *aa[2:], bb[0], N, *bb[2:],
+    _call("acrl_fp8_matmul", (a.q, a.scale, b.q, b.scale, out, flags), None, aa[0], M, K, *aa[2:], bb[0], N, *bb[2:],
           _ptr(out), _OUT_DTYPE[out.dtype], ldo, _ptr(flags))
     return out
 
@@ -611,6 +625,9 @@ def fp8_linear(x, weight: Fp8Tensor, *, fmt="e4m3", out_dtype=torch.bfloat16, ou
     """acrl_fp8_linear: x (bf16 [M, K]) quantised by rows, times the transpose of `weight` [N, K]; [M, N]."""
     M, K = _bf16_rows(x, "x")
     w = _fp8_args(weight, "weight")
+    if stream is not None:
+        return _on_stream(fp8_linear, "acrl_fp8_linear", x, stream, x, weight, fmt=fmt, out_dtype=out_dtype, out=out,
+                          workspace=workspace, flags=flags)
     N = w[1]
     if weight.shape[1] != K:
         raise AcrlError(f"x and weight disagree on K: {K} and {weight.shape[1]}")
@@ -623,7 +640,7 @@ def fp8_linear(x, weight: Fp8Tensor, *, fmt="e4m3", out_dtype=torch.bfloat16, ou
     elif n > 0:
         workspace = torch.empty(n, dtype=torch.uint8, device=x.device)
     _opt(flags, torch.int32, 1, "flags")
-    _call("acrl_fp8_linear", (x, weight.q, weight.scale, out, workspace, flags), stream, x.data_ptr(), M, K, _ld(x),
+    _call("acrl_fp8_linear", (x, weight.q, weight.scale, out, workspace, flags), None, x.data_ptr(), M, K, _ld(x),
           _fp8_format(fmt), w[0], N, *w[2:], out.data_ptr(), _OUT_DTYPE[out.dtype], ldo, _ptr(workspace), n, _ptr(flags))
     return out
 
@@ -648,6 +665,9 @@ def fp8_linear_backward(dy, x, weight_t: Fp8Tensor, *, fmt="e4m3", x_fmt="e4m3",
     dw [N, K])."""
     (M, N), (Mx, K) = _bf16_rows(dy, "dy"), _bf16_rows(x, "x")
     w = _fp8_args(weight_t, "weight_t")
+    if stream is not None:
+        return _on_stream(fp8_linear_backward, "acrl_fp8_linear_backward", dy, stream, dy, x, weight_t, fmt=fmt, x_fmt=x_fmt,
+                          dx_dtype=dx_dtype, dw_dtype=dw_dtype, dx=dx, dw=dw, workspace=workspace, flags=flags)
     if Mx != M or tuple(weight_t.shape) != (K, N):
         raise AcrlError(f"dy {(M, N)}, x {(Mx, K)} and weight_t {tuple(weight_t.shape)} do not belong together")
     if dx_dtype not in _OUT_DTYPE or dw_dtype not in _OUT_DTYPE:
@@ -658,7 +678,7 @@ def fp8_linear_backward(dy, x, weight_t: Fp8Tensor, *, fmt="e4m3", x_fmt="e4m3",
     workspace = torch.empty(n, dtype=torch.uint8, device=dy.device) if workspace is None else \
         _need(workspace, torch.uint8, n, "workspace")
     _opt(flags, torch.int32, 1, "flags")
-    _call("acrl_fp8_linear_backward", (dy, x, weight_t.q, weight_t.scale, dx, dw, workspace, flags), stream, dy.data_ptr(), M, N,
+    _call("acrl_fp8_linear_backward", (dy, x, weight_t.q, weight_t.scale, dx, dw, workspace, flags), None, dy.data_ptr(), M, N,
           _ld(dy), _fp8_format(fmt), x.data_ptr(), K, _ld(x), _fp8_format(x_fmt), w[0], *w[2:], dx.data_ptr(),
           _OUT_DTYPE[dx.dtype], lddx, dw.data_ptr(), _OUT_DTYPE[dw.dtype], lddw, workspace.data_ptr(), n, _ptr(flags))
     return dx, dw
@@ -692,6 +712,11 @@ def policy_loss_grad_logits(logits, ids, mask, coef, *, V=None, old_logp=None, c
     """acrl_policy_loss_grad_logits.  `kl` is None, "exact" or "reverse" (with `ref_logits`, bf16 [T, ld_ref]), or "k1",
     "k2" or "k3" (with `ref_logp`, float32 [T]); `kl_coef` float32 [T] its factor per token."""
     T, ld = _rows(logits, "logits")
+    if stream is not None:
+        return _on_stream(policy_loss_grad_logits, "acrl_policy_loss_grad_logits", logits, stream, logits, ids, mask, coef, V=V,
+                          old_logp=old_logp, clip_low=clip_low, clip_high=clip_high, dual_clip=dual_clip, kl=kl,
+                          kl_coef=kl_coef, ref_logits=ref_logits, ref_logp=ref_logp, grad=grad, logp=logp, kl_out=kl_out,
+                          token_loss=token_loss, loss=loss, flags=flags)
     V = ld if V is None else V
     dev = logits.device
     if kl not in _KL:
@@ -729,7 +754,7 @@ def policy_loss_grad_logits(logits, ids, mask, coef, *, V=None, old_logp=None, c
         _need(flags, torch.int32, 1, "flags")
     _call("acrl_policy_loss_grad_logits",
           (logits, ids, mask, old_logp, coef, kl_coef, ref_logits, ref_logp, grad, logp, kl_out, token_loss, loss, flags),
-          stream, logits.data_ptr(), T, V, ld, ids.data_ptr(), None if mask is None else mask.data_ptr(),
+          None, logits.data_ptr(), T, V, ld, ids.data_ptr(), None if mask is None else mask.data_ptr(),
           None if old_logp is None else old_logp.data_ptr(), None if coef is None else coef.data_ptr(), clip_low, clip_high,
           dual_clip, _KL[kl], None if kl_coef is None else kl_coef.data_ptr(),
           None if ref_logits is None else ref_logits.data_ptr(), ldr, None if ref_logp is None else ref_logp.data_ptr(),
@@ -756,6 +781,10 @@ def preference_loss(logp, ref_logp, mask, rewards, seq_offsets, group_offsets, *
     """acrl_preference_loss: pairs of a prompt's responses by their rewards; `form` "sigmoid", "hinge" or "ipo"."""
     T, S, Gn = logp.numel(), seq_offsets.numel() - 1, group_offsets.numel() - 1
     f32, dev = torch.float32, logp.device
+    if stream is not None:
+        return _on_stream(preference_loss, "acrl_preference_loss", logp, stream, logp, ref_logp, mask, rewards, seq_offsets,
+                          group_offsets, beta=beta, form=form, margin=margin, label_smoothing=label_smoothing,
+                          length_norm=length_norm, ratio=ratio, coef=coef, loss=loss, workspace=workspace, flags=flags)
     if form not in _PREF:
         raise AcrlError(f"form: {form!r}, expected one of {list(_PREF)}")
     if S < 0 or Gn < 0:
@@ -772,7 +801,7 @@ def preference_loss(logp, ref_logp, mask, rewards, seq_offsets, group_offsets, *
     if flags is not None:
         _need(flags, torch.int32, 1, "flags")
     _call("acrl_preference_loss",
-          (logp, ref_logp, mask, rewards, seq_offsets, group_offsets, ratio, coef, loss, workspace, flags), stream,
+          (logp, ref_logp, mask, rewards, seq_offsets, group_offsets, ratio, coef, loss, workspace, flags), None,
           logp.data_ptr(), None if ref_logp is None else ref_logp.data_ptr(), None if mask is None else mask.data_ptr(), T,
           rewards.data_ptr(), seq_offsets.data_ptr(), S, group_offsets.data_ptr(), Gn, _PREF[form], beta, margin,
           label_smoothing, int(length_norm), ratio.data_ptr(), coef.data_ptr(), loss.data_ptr(), workspace.data_ptr(), n,

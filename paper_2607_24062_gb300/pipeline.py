@@ -263,8 +263,11 @@ class Fp8Head:
 
     def logp(self, hidden, ids, mask=None, *, out=None, flags=None, stream=None):
         """float32 [T] log-probs of the sampled tokens (0 where masked)."""
-        z = self.logits(hidden, out=out, flags=flags, stream=stream)
-        return api.token_stats(z, ids, mask, V=z.shape[1], flags=flags, stream=stream)[1]
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.logp(hidden, ids, mask, out=out, flags=flags)
+        z = self.logits(hidden, out=out, flags=flags)
+        return api.token_stats(z, ids, mask, V=z.shape[1], flags=flags)[1]
 
 
 class HostPipeline:

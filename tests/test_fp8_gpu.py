@@ -278,3 +278,26 @@ def test_both_gradients_are_the_products(M, N, K, dx_dtype, dw_dtype):
     assert torch.equal(dx[:M], acrl.fp8_matmul(by_rows, wt, out_dtype=dx_dtype))
     assert torch.equal(dw[:N], acrl.fp8_matmul(turned, xt, out_dtype=dw_dtype))
     assert bool((dx[M:] == 3.0).all()) and bool((dw[N:] == 3.0).all())
+
+
+def test_what_a_call_allocates_belongs_to_its_stream():
+    """Memory that the current stream has freed but still writes is not what a call on another stream works in."""
+    x, dy = _matrix(300, 1000, 51), _matrix(300, 520, 52)
+    w = _matrix(520, 1000, 53, std=0.02)
+    w8, wt = acrl.fp8_quantize(w, block="tile"), acrl.fp8_quantize(w, block="tile", transpose=True)
+    n = api.fp8_linear_workspace_bytes(300, 520, 1000)
+    nb = api.fp8_linear_backward_workspace_bytes(300, 520, 1000)
+    want = acrl.fp8_linear(x, w8), *acrl.fp8_linear_backward(dy, x, wt), acrl.fp8_quantize(x).q.view(torch.uint8)
+    want = [t.clone() for t in want]
+    side = torch.cuda.Stream()
+    big = torch.randn(4096, 4096, device=DEV)
+    torch.cuda.synchronize()
+    for _ in range(20):                       # tens of milliseconds of the current stream
+        big = torch.tanh(big @ big)
+    for size in (n, nb, 300 * 520 * 2, 300 * 1000 * 2, 520 * 1000 * 4, 300 * 1008, 300 * 8):
+        for _ in range(3):
+            torch.empty(size, dtype=torch.uint8, device=DEV).fill_(255)   # freed at once, written when the stream gets there
+    got = acrl.fp8_linear(x, w8, stream=side), *acrl.fp8_linear_backward(dy, x, wt, stream=side), \
+        acrl.fp8_quantize(x, stream=side).q.view(torch.uint8)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
