@@ -31,10 +31,19 @@ bool few_rows(int64_t M, int64_t N, int64_t K);
 acrl_status matmul_few(const Matrix& a, const acrl_bf16* x, int64_t ldx, const Matrix& b, int64_t K, void* out, acrl_dtype out_dtype,
                        int64_t ldo, int32_t* flags, cudaStream_t s);
 
-// x by rows and the transpose of x by rows (acrl_fp8_quantize twice), x read once; checked arguments.
-acrl_status quantize_both(const acrl_bf16* x, int64_t R, int64_t C, int64_t ldx, acrl_fp8_format format, uint8_t* q, int64_t ldq,
-                          uint8_t* scale, int64_t lds, uint8_t* qt, int64_t ldqt, uint8_t* scale_t, int64_t ldst,
-                          int32_t* flags, cudaStream_t s);
+// Where a quantised matrix goes.
+struct Quantised {
+    uint8_t* q;
+    int64_t ldq;
+    uint8_t* scale;
+    int64_t lds;
+};
+
+// For a layer's backward: dy [M, N] by rows (`as`) and its transpose by rows (`turned`), dy read once, and the transpose of x
+// [M, K] by rows; checked arguments.
+acrl_status quantize_backward(const acrl_bf16* dy, int64_t M, int64_t N, int64_t lddy, acrl_fp8_format format, const Quantised& as,
+                              const Quantised& turned, const acrl_bf16* x, int64_t K, int64_t ldx, acrl_fp8_format x_format,
+                              const Quantised& x_turned, int32_t* flags, cudaStream_t s);
 
 namespace {
 

@@ -1148,12 +1148,9 @@ extern "C" acrl_status acrl_fp8_linear_backward(const acrl_bf16* dy, int64_t M, 
     if (N == 0) return product(a, w, 0, dx, dx_dtype, lddx, dev_flags, s);
     if (!dy || !aligned16(dy) || !workspace || !aligned16(workspace) || !operands_on_current_device({wt, base, dx, dw}))
         return ACRL_ERR_INVALID_ARG;
-    acrl_status st = quantize_both(dy, M, N, lddy, dy_format, base + parts.dy.at, parts.dy.ldq, const_cast<uint8_t*>(a.scale),
-                                   parts.dy.lds, base + parts.dyt.at, parts.dyt.ldq, const_cast<uint8_t*>(at.scale), parts.dyt.lds,
-                                   dev_flags, s);
-    if (st == ACRL_OK)
-        st = acrl_fp8_quantize(x, ACRL_BF16, M, K, ldx, x_format, ACRL_FP8_ROW, 1, base + parts.xt.at, parts.xt.ldq,
-                               const_cast<uint8_t*>(xt.scale), parts.xt.lds, dev_flags, stream);
+    auto into = [&](const Part& p, const Matrix& m) { return Quantised{base + p.at, p.ldq, const_cast<uint8_t*>(m.scale), p.lds}; };
+    acrl_status st = quantize_backward(dy, M, N, lddy, dy_format, into(parts.dy, a), into(parts.dyt, at), x, K, ldx, x_format,
+                                       into(parts.xt, xt), dev_flags, s);
     if (st == ACRL_OK) st = two_products({a, w, N, dx, dx_dtype, lddx}, {at, xt, M, dw, dw_dtype, lddw}, dev_flags, s);
     return st;
 }

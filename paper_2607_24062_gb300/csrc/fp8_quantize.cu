@@ -182,17 +182,20 @@ constexpr int kTileRows = MAKE == kTile ? 8 : 4;
 template <Make MAKE>
 constexpr int kTileThreads = 2048 / kTileRows<MAKE>;
 
-struct Quantised {
-    uint8_t* q;
-    int64_t ldq;
-    uint8_t* scale;
-    int64_t lds;
+template <typename T>
+struct Tiled {
+    const T* x;
+    int64_t R, C, ldx;
+    int col_blocks;
+    Quantised as, turned;
 };
 
 template <typename T, int FMT, Make MAKE>
-__global__ void __launch_bounds__(kTileThreads<MAKE>, MAKE == kTile ? 3 : 2)
-    quantize_tiles(const T* __restrict__ x, int64_t R, int64_t C, int64_t ldx, int col_blocks, Quantised as, Quantised turned,
-                   int32_t* flags) {
+__device__ __forceinline__ void quantize_tile(const Tiled<T>& job, int64_t block, int32_t* flags) {
+    const T* __restrict__ x = job.x;
+    const int64_t R = job.R, C = job.C, ldx = job.ldx;
+    const int col_blocks = job.col_blocks;
+    const Quantised &as = job.as, &turned = job.turned;
     constexpr int U = kTileRows<MAKE>, kThreads = kTileThreads<MAKE>;
     constexpr int kWarps = kThreads / 32, kKeys = Eight<T>::kKeys;
     constexpr bool kOne = MAKE == kTile || MAKE == kTileT;
@@ -201,7 +204,7 @@ __global__ void __launch_bounds__(kTileThreads<MAKE>, MAKE == kTile ? 3 : 2)
     __shared__ __align__(16) uint8_t turn[MAKE == kTile ? 16 : 128 * 128];
     const int lane = threadIdx.x & 31;
     const int g = threadIdx.x >> 4, cl = threadIdx.x & 15;        // rows U g .., columns 8 cl ..
-    const int64_t rb = blockIdx.x / col_blocks, cb = blockIdx.x - rb * col_blocks;
+    const int64_t rb = block / col_blocks, cb = block - rb * col_blocks;
     const int64_t r0 = rb * 128 + U * g, c0 = cb * 128 + 8 * cl;
     const int nc = int(min(int64_t(8), C - c0));
     grid_begin();
@@ -303,12 +306,37 @@ __global__ void __launch_bounds__(kTileThreads<MAKE>, MAKE == kTile ? 3 : 2)
     }
 }
 
+// (fp32 as it is: 64 registers of elements a thread, and two CTAs an SM have 128 KB of loads in flight)
+template <typename T, int FMT, Make MAKE>
+__global__ void __launch_bounds__(kTileThreads<MAKE>, MAKE == kTile && sizeof(T) == 2 ? 3 : 2)
+    quantize_tiles(const __grid_constant__ Tiled<T> job, int32_t* flags) {
+    quantize_tile<T, FMT, MAKE>(job, int64_t(blockIdx.x), flags);
+}
+
+// What a layer's backward needs: `dy` both ways, then `x` turned, in one launch (two: 2.5 us more on the GPU, 4 on the host).
+template <int FMT, int X_FMT>
+__global__ void __launch_bounds__(kTileThreads<kBoth>, 2)
+    quantize_backward_tiles(const __grid_constant__ Tiled<acrl_bf16> dy, const __grid_constant__ Tiled<acrl_bf16> x,
+                            int64_t dy_tiles, int32_t* flags) {
+    if (int64_t(blockIdx.x) < dy_tiles)
+        quantize_tile<acrl_bf16, FMT, kBoth>(dy, int64_t(blockIdx.x), flags);
+    else
+        quantize_tile<acrl_bf16, X_FMT, kRowT>(x, int64_t(blockIdx.x) - dy_tiles, flags);
+}
+
+template <typename T>
+Tiled<T> tiled(const T* x, int64_t R, int64_t C, int64_t ldx, const Quantised& as, const Quantised& turned) {
+    return Tiled<T>{x, R, C, ldx, int((C + 127) / 128), as, turned};
+}
+template <typename T>
+int64_t tiles_of(const Tiled<T>& t) { return (t.R + 127) / 128 * t.col_blocks; }
+
 template <typename T, int FMT, Make MAKE>
 acrl_status launch_tiles(const T* x, int64_t R, int64_t C, int64_t ldx, const Quantised& as, const Quantised& turned,
                          int32_t* flags, cudaStream_t s) {
-    const int64_t cb = (C + 127) / 128, grid = (R + 127) / 128 * cb;
-    if (grid > kMaxGrid) return ACRL_ERR_INVALID_ARG;
-    return launch(quantize_tiles<T, FMT, MAKE>, grid, kTileThreads<MAKE>, 0, 0, s, x, R, C, ldx, int(cb), as, turned, flags);
+    const Tiled<T> job = tiled(x, R, C, ldx, as, turned);
+    if (tiles_of(job) > kMaxGrid) return ACRL_ERR_INVALID_ARG;
+    return launch(quantize_tiles<T, FMT, MAKE>, tiles_of(job), kTileThreads<MAKE>, 0, 0, s, job, flags);
 }
 
 template <typename T, int FMT>
@@ -327,12 +355,16 @@ acrl_status launch_quantize(const T* x, int64_t R, int64_t C, int64_t ldx, bool 
 
 }  // namespace
 
-acrl_status quantize_both(const acrl_bf16* x, int64_t R, int64_t C, int64_t ldx, acrl_fp8_format format, uint8_t* q, int64_t ldq,
-                          uint8_t* scale, int64_t lds, uint8_t* qt, int64_t ldqt, uint8_t* scale_t, int64_t ldst,
-                          int32_t* flags, cudaStream_t s) {
-    const Quantised as{q, ldq, scale, lds}, turned{qt, ldqt, scale_t, ldst};
-    return format == ACRL_FP8_E4M3 ? launch_tiles<acrl_bf16, 0, kBoth>(x, R, C, ldx, as, turned, flags, s)
-                                   : launch_tiles<acrl_bf16, 1, kBoth>(x, R, C, ldx, as, turned, flags, s);
+acrl_status quantize_backward(const acrl_bf16* dy, int64_t M, int64_t N, int64_t lddy, acrl_fp8_format format, const Quantised& as,
+                              const Quantised& turned, const acrl_bf16* x, int64_t K, int64_t ldx, acrl_fp8_format x_format,
+                              const Quantised& x_turned, int32_t* flags, cudaStream_t s) {
+    const Tiled<acrl_bf16> a = tiled(dy, M, N, lddy, as, turned), b = tiled(x, M, K, ldx, x_turned, x_turned);
+    const int64_t tiles = tiles_of(a), grid = tiles + tiles_of(b);
+    if (grid > kMaxGrid) return ACRL_ERR_INVALID_ARG;
+    auto run = [&](auto* kernel) { return launch(kernel, grid, kTileThreads<kBoth>, 0, 0, s, a, b, tiles, flags); };
+    if (format == ACRL_FP8_E4M3)
+        return x_format == ACRL_FP8_E4M3 ? run(quantize_backward_tiles<0, 0>) : run(quantize_backward_tiles<0, 1>);
+    return x_format == ACRL_FP8_E4M3 ? run(quantize_backward_tiles<1, 0>) : run(quantize_backward_tiles<1, 1>);
 }
 
 }  // namespace acrl
