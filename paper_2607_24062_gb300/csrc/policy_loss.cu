@@ -82,15 +82,22 @@ __device__ __forceinline__ float exponent_beside(float mx, float U) {
     return fabsf(W - U) <= 16.f ? U : W;
 }
 
-// z - log(2^U s).  U log 2 in two parts, the first of 15 bits, so that z less it is exact for every bf16 z of ordinary size
-// and one rounding at the result's size is left.  Beyond, by differences of the logits, which are as coarse as units there.
-__device__ __forceinline__ float less_log(float z, float m, float U, float s) {
+// z - log(2^U s) in two parts.  U log 2 in two as well, the first of 15 bits, so that z less it is exact for every bf16 z of
+// ordinary size and one rounding, at the size of what is computed from the parts, is left: a log-prob's difference from another
+// is far smaller than either.  Beyond, by differences of the logits, which are as coarse as units there.
+struct LogShare {
+    float whole, rest;     // whole - rest
+    __device__ __forceinline__ float value() const { return whole - rest; }
+    __device__ __forceinline__ float less(float other) const { return (whole - other) - rest; }
+};
+__device__ __forceinline__ LogShare less_log(float z, float m, float U, float s) {
     constexpr float kHi = 22713.f / 32768.f, kLo = 1.42860682e-6f;   // log 2 = kHi + kLo
     const int bits = __float_as_int(s), e = (bits - 0x3f400000) >> 23;   // s = 2^e f, 3/4 <= f < 3/2
     const bool normal = s > 1e-37f && s < 3e38f;                         // else (0, infinite, NaN): its own logarithm
     const float f = normal ? __int_as_float(bits - e * (1 << 23)) : s, n = normal ? U + float(e) : U;
     const float l = kLn2 * log2f(f);
-    return fabsf(U) < 1e6f ? fmaf(-n, kHi, z) - fmaf(n, kLo, l) : (z - m) - (l + kLn2 * (n - U - fmaf(m, kLog2e, -U)));
+    if (fabsf(U) < 1e6f) return LogShare{fmaf(-n, kHi, z), fmaf(n, kLo, l)};
+    return LogShare{z - m, l + kLn2 * (n - U - fmaf(m, kLog2e, -U))};
 }
 
 // Two fp32 numbers in a register pair: sums, products and fused products of both in one instruction (issue bounds these
@@ -373,7 +380,8 @@ template <Kind KIND>
 __device__ __forceinline__ int row_scalars(const PolicyArgs& A, int64_t t, const State& row, int a, float za, float xa,
                                            float c0, float kc, float old, float ref, bool writes, RowGrad& g) {
     const bool sums = row.sz > 0.f && isfinite(row.sz) && isfinite(row.mz);
-    const float logp = less_log(za, row.mz, row.U, row.sz);
+    const LogShare share = less_log(za, row.mz, row.U, row.sz);
+    const float logp = share.value();
     float KL = 0.f, apart = 0.f, logq = 0.f;                                      // apart = lse_z - lse_x
     g.a = a;
     g.k = kc;
@@ -386,11 +394,11 @@ __device__ __forceinline__ int row_scalars(const PolicyArgs& A, int64_t t, const
         apart = fabsf(row.U) < 1e6f && fabsf(row.W) < 1e6f
                     ? fmaf(row.U - row.W, kLn2, ratio)
                     : (row.mz - row.mx) + (ratio - kLn2 * (fmaf(row.mz, kLog2e, -row.U) - fmaf(row.mx, kLog2e, -row.W)));
-        logq = less_log(xa, row.mx, row.W, row.sx);
+        logq = less_log(xa, row.mx, row.W, row.sx).value();
         KL = KIND == kExact ? row.cross / row.sz - apart : row.cross / row.sx + apart;
         g.W = row.W + log2f(row.sx);
     } else {
-        const float d = logp - ref;
+        const float d = share.less(ref);
         if (A.kl == ACRL_KL_K1) {
             KL = d;
             slope = 1.f;
@@ -403,7 +411,7 @@ __device__ __forceinline__ int row_scalars(const PolicyArgs& A, int64_t t, const
             slope = -e;
         }
     }
-    const float ratio = A.old_logp ? expf(logp - old) : 1.f;
+    const float ratio = A.old_logp ? expf(share.less(old)) : 1.f;
     float surrogate = 0.f;
     g.c = 0.f;
     if (c0 != 0.f) {
@@ -747,7 +755,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_kernel(const __g
         st = meet<kSampled, 32>(lane < kWarps ? get(sh.warps[lane]) : none);
     }
     if (tid != 0) return;
-    const float l = -less_log(0.f, st.mz, st.U, st.sz), lp = in ? less_log(za, st.mz, st.U, st.sz) : 0.f;
+    const float l = -less_log(0.f, st.mz, st.U, st.sz).value(), lp = in ? less_log(za, st.mz, st.U, st.sz).value() : 0.f;
     if (!in) raise_flag(A.flags, ACRL_FLAG_BAD_ID);
     const bool fine = isfinite(l) && isfinite(lp);
     if (!fine) raise_flag(A.flags, ACRL_FLAG_NONFINITE);
