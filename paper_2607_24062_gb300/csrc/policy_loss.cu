@@ -181,13 +181,14 @@ __device__ __forceinline__ void fold(State& st, const uint4 (&z)[N], const uint4
         }
     }
     const Two l2e = two(kLog2e, kLog2e), nU = two(-st.U, -st.U), nW = two(-st.W, -st.W), minus = two(-1.f, -1.f);
+    const Two low = two(kLog2eLow, kLog2eLow);
     Two sz = two(0.f, 0.f), sx = sz, cr = sz;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
         const uint32_t zw[4] = {z[k].x, z[k].y, z[k].z, z[k].w}, xw[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const Two a = widen(zw[j]), e = ex2_2(fma2(a, l2e, nU));
+            const Two a = widen(zw[j]), u = fma2(a, l2e, nU), e = ex2_2(KIND == kSampled ? fma2(a, low, u) : u);
             sz = add2(sz, e);
             if constexpr (KIND != kSampled) {
                 const Two b = widen(xw[j]), h = ex2_2(fma2(b, l2e, nW));
@@ -204,10 +205,13 @@ __device__ __forceinline__ void fold(State& st, const uint4 (&z)[N], const uint4
     }
 }
 
-// The quick way: sums against exponents that are fixed for the row, those of some of its columns.  Sums are as exact
-// against any exponent from which they neither overflow nor vanish; a row whose sums are not finite (a maximum that is
-// 2^127 times what the exponents stand for, an infinity, a column taken out on one side) is folded again the careful way.
+// The quick way: sums against exponents that are fixed for a warp's share of the row, those of some of its columns.  Sums are as
+// exact against any exponent from which they neither overflow nor vanish.  A warp that holds a lane's sum of kQuickMost or more
+// (columns 44 above those of the exponents, an infinity, a column taken out on one side) folds its share again the careful way.
+// The bound is for what comes after: 2^13 lanes of a cluster and factors of up to 2^32 between their exponents leave the row's
+// sum below 2^109; and a factor that is flushed to 0, below 2^-126, has taken less than 2^-49 from a sum that is 2^-16 or more.
 // Where the careful way is not needed both give the same cross sum's terms; the careful way costs nearly half as much again.
+constexpr float kQuickMost = 0x1p64f;
 template <Kind KIND>
 struct Quick {
     float mz, mx;
@@ -570,8 +574,8 @@ struct Cta {
         }
         __syncwarp();
         State st = q.state();
-        // no sum is finite in which one of these is not
-        careful = __any_sync(0xffffffffu, !isfinite(KIND == kSampled ? st.sz : st.cross + (st.sz + st.sx)));
+        const bool small = st.sz < kQuickMost && (KIND == kSampled || (st.sx < kQuickMost && fabsf(st.cross) < kQuickMost));
+        careful = __any_sync(0xffffffffu, !small);     // (a NaN is not below the bound)
         if (careful) {          // once more, from where the vectors are now
             st = empty_state();
             auto f = [&](const uint4& z, const uint4& x, int) {

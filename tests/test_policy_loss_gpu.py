@@ -284,3 +284,67 @@ def test_refusals():
                dict(grad=i["z"].float()), dict(logp=i["coef"][:1])):
         with pytest.raises(acrl.AcrlError):
             _run(i, **kw)
+
+
+def _heights(T, V, shape, seed, low=60, step=1):
+    """Logits of rows whose columns stand at one of two heights, the lower one `low` + `step` t below in row t: a head of the row
+    below the rest ("head"), blocks of 256 columns at either height by chance ("blocks"), or single columns above ("peaks")."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    ld, col = (V + 7) // 8 * 8, torch.arange(V, device=DEV)
+    if shape == "head":
+        down = (col < V // 4 + 1)[None].repeat(T, 1)
+    elif shape == "blocks":
+        down = (torch.rand((T, V // 256 + 1), generator=g, device=DEV) < 0.5).repeat_interleave(256, 1)[:, :V]
+        down[:, :256] = True
+    else:
+        down = torch.rand((T, V), generator=g, device=DEV) >= 4.0 / V
+    down[:, V - 1] = False
+    drop = low + step * torch.arange(T, device=DEV, dtype=torch.float32)
+    z = torch.zeros((T, ld), device=DEV)
+    z[:, :V] = 0.25 * torch.randn((T, V), generator=g, device=DEV) - down * drop[:, None]
+    return z.to(torch.bfloat16)
+
+
+# rows of one warp, of several, and of a cluster of two and of eight CTAs, with what fits in shared memory and more
+@pytest.mark.parametrize("kl", ["exact", "reverse", "k3", None])
+@pytest.mark.parametrize("shape", ["head", "blocks", "peaks"])
+@pytest.mark.parametrize("T,V,step", [(51, 1000, 1), (51, 4096, 1), (51, 20011, 1), (156, 20011, 0.3125), (17, 65544, 3),
+                                      (156, 65544, 0.3125), (160, 151936, 0.3125)])
+def test_columns_far_below_the_others(kl, shape, T, V, step):
+    """Columns that lie 60 to 110 below the row's largest, and where a warp meets them before those: every number of such a row
+    is an ordinary one."""
+    i = _inputs(T, V, 200 + V, kl)
+    i["z"] = _heights(T, V, shape, V, step=step)
+    i["mask"] = None
+    i["ids"] = torch.where(torch.arange(T, device=DEV) % 3 > 0, V - 1, i["ids"]).to(torch.int32)
+    lp = torch.log_softmax(i["z"][:, :V].double(), 1).gather(1, i["ids"].long()[:, None])[:, 0]
+    g = torch.Generator(device=DEV).manual_seed(1)
+    i["old"] = (lp + 0.3 * torch.randn(T, generator=g, device=DEV)).float()
+    if i["ref_logits"] is not None:     # near the policy's logits, or with heights of its own
+        x, other = i["z"].float(), _heights(T, V, shape, V + 1, step=step).float()
+        x[::2] = other[::2]
+        i["ref_logits"] = (x + 0.25 * torch.randn(x.shape, generator=g, device=DEV)).to(torch.bfloat16)
+    elif kl:
+        i["ref_logp"] = (lp + 0.3 * torch.randn(T, generator=g, device=DEV)).float()
+    flags = api.new_flags()
+    o = _run(i, flags=flags)
+    assert acrl.read_flags(flags) == 0
+    _check(i, o)
+
+
+@pytest.mark.parametrize("kl", ["exact", "reverse", "k2", None])
+@pytest.mark.parametrize("gap", [79.0, 81.0, 83.0, 85.0, 87.0, 95.0])
+def test_leading_columns_of_one_height(kl, gap):
+    """The first 256 of 4,096 columns at -gap, the others at 0: lse = log 3,840 to the last bits."""
+    i = _inputs(8, 4096, 3, kl)
+    i["z"][:, :256], i["z"][:, 256:] = -gap, 0.0
+    i["mask"] = None
+    i["ids"] = torch.full((8,), 4000, dtype=torch.int32, device=DEV)
+    i["old"] = None
+    if kl == "k2":
+        i["ref_logp"] = torch.full((8,), -8.0, device=DEV)
+    flags = api.new_flags()
+    o = _run(i, flags=flags)
+    assert acrl.read_flags(flags) == 0
+    assert bool(((o.logp.double() + math.log(3840.0)).abs() <= 4e-6).all())
+    _check(i, o)

@@ -236,3 +236,34 @@ def test_refusals():
     step = acrl.PreferenceStep(20, 64, 64, 4, 2)
     with pytest.raises(acrl.AcrlError):
         step.run(torch.zeros((19, 64), dtype=torch.bfloat16, device=DEV), None, None, None, b["rewards"], b["so"], b["go"])
+
+
+@pytest.mark.parametrize("V", [1000, 4096, 20011, 70001, 151936])
+@pytest.mark.parametrize("shape", ["head", "blocks", "peaks"])
+def test_log_probs_of_columns_far_below_the_others(V, shape):
+    """As test_log_probs_of_the_step, with columns 60 to 110 below the row's largest: a head of the row, blocks of 256 columns, or
+    all but a few."""
+    T = 51
+    g = torch.Generator(device=DEV).manual_seed(V)
+    ld = (V + 7) // 8 * 8
+    if shape == "head":
+        down = (torch.arange(V, device=DEV) < V // 4 + 1)[None].repeat(T, 1)
+    elif shape == "blocks":
+        down = (torch.rand((T, V // 256 + 1), generator=g, device=DEV) < 0.5).repeat_interleave(256, 1)[:, :V]
+        down[:, :256] = True
+    else:
+        down = torch.rand((T, V), generator=g, device=DEV) >= 4.0 / V
+    down[:, V - 1] = False
+    z = torch.zeros((T, ld), device=DEV)
+    z[:, :V] = 0.25 * torch.randn((T, V), generator=g, device=DEV) - down * (60.0 + torch.arange(T, device=DEV))[:, None]
+    z = z.to(torch.bfloat16)
+    ids = torch.randint(0, V, (T,), generator=g, device=DEV, dtype=torch.int32)
+    ids[::2] = V - 1
+    step = acrl.PreferenceStep(T, V, ld, 2, 1)
+    so, go = torch.tensor([0, 20, T], device=DEV), torch.tensor([0, 2], dtype=torch.int32, device=DEV)
+    step.run(z, ids, None, None, torch.tensor([1.0, 0.0], device=DEV), so, go)
+    assert acrl.read_flags(step.flags) == 0
+    lse = torch.logsumexp(z[:, :V].double(), 1)
+    lp = z[:, :V].gather(1, ids.long()[:, None])[:, 0].double() - lse
+    for got, want in ((step.lse, lse), (step.logp, lp)):
+        assert bool(((got - want).abs() <= 4e-6 + 2e-7 * want.abs()).all())
