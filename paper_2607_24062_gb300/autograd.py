@@ -66,7 +66,15 @@ def acrl_loss(step: AcrlStep, logits: torch.Tensor, ids, mask, logp_mu, rewards,
 class _PolicyLoss(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, ids, mask, coef, kw):
+        stream = kw.get("stream")
+        if stream is not None:    # the logits and the rest of the graph are the current stream's
+            here = torch.cuda.current_stream(stream.device)
+            stream.wait_stream(here)
         out = api.policy_loss_grad_logits(logits.detach(), ids, mask, coef, **kw)
+        if stream is not None:
+            here.wait_stream(stream)
+            for t in (out.grad, out.loss):    # of `stream`, and read here
+                t.record_stream(here)
         ctx.grad, ctx.shape = out.grad, logits.shape
         return out.loss.reshape(()).clone()
 
@@ -78,7 +86,8 @@ class _PolicyLoss(torch.autograd.Function):
 def policy_loss(logits: torch.Tensor, ids, mask, coef, **kw) -> torch.Tensor:
     """The scalar loss of policy_loss_grad_logits (same arguments; fp32, 0-d) with dL/dlogits attached for autograd.
     `logits` is bf16 [T, V] with a row stride that is a multiple of eight; outputs given by keyword (logp, kl_out,
-    token_loss) are filled."""
+    token_loss) are filled.  With `stream` the kernels run there, after what the current stream holds and before what it gets
+    next."""
     if kw.get("V") not in (None, logits.shape[1]):
         raise ValueError("logits: pass the view [T, V] itself")
     kw["V"] = logits.shape[1]

@@ -348,3 +348,35 @@ def test_leading_columns_of_one_height(kl, gap):
     assert acrl.read_flags(flags) == 0
     assert bool(((o.logp.double() + math.log(3840.0)).abs() <= 4e-6).all())
     _check(i, o)
+
+
+def test_autograd_node_on_another_stream():
+    """What a call on a busy stream writes is there when the node's own stream reads it, forwards and backwards."""
+    i = _inputs(40, 5000, 12)
+    want = _run(i)
+    side = torch.cuda.Stream()
+    big = torch.randn(4096, 4096, device=DEV)
+    grad, loss_of = torch.full_like(i["z"], 7.0), torch.full((1,), 7.0, device=DEV)
+    y = i["z"].clone().requires_grad_()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(20):                       # tens of milliseconds
+            big = torch.tanh(big @ big)
+    loss = acrl.policy_loss(y[:, :5000], i["ids"], i["mask"], i["coef"], old_logp=i["old"], kl="exact", kl_coef=i["kl_coef"],
+                            ref_logits=i["ref_logits"], stream=side, grad=grad, loss=loss_of)
+    loss.backward()
+    got = y.grad.clone()
+    torch.cuda.synchronize()
+    assert torch.equal(loss.detach().reshape(1), want.loss)
+    assert torch.equal(got[:, :5000], want.grad[:, :5000])
+    # and the other way round: logits that the current stream is still to write
+    z = i["z"].clone()
+    late = torch.full_like(z, 3.0)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        big = torch.tanh(big @ big)
+    late.copy_(z)
+    loss = acrl.policy_loss(late[:, :5000], i["ids"], i["mask"], i["coef"], old_logp=i["old"], kl="exact", kl_coef=i["kl_coef"],
+                            ref_logits=i["ref_logits"], stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(loss.reshape(1), want.loss)
