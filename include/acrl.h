@@ -700,7 +700,9 @@ typedef enum {
  * it.  A row whose log-prob, KL or ratio is not defined (a NaN; a +infinity; every
  * column or the sampled one at -infinity; a KL that is infinite) raises
  * NONFINITE; its logp and kl_out are NaN where they are undefined, and where coef
- * or kl_coef is not 0 its token_loss and gradient row are NaN.  A row with both
+ * or kl_coef is not 0 its token_loss and gradient row are NaN.  So is a row whose
+ * loss is beyond fp32: a ratio that overflows where nothing clips it (a negative
+ * coef without dual_clip), a coefficient that is no finite number.  A row with both
  * coefficients 0 has gradient and token_loss 0.
  */
 acrl_status acrl_policy_loss_grad_logits(const acrl_bf16* logits, int64_t T, int64_t V, int64_t ld,

@@ -429,7 +429,8 @@ __device__ __forceinline__ int row_scalars(const PolicyArgs& A, int64_t t, const
     const float loss = kc != 0.f ? fmaf(kc, KL, surrogate) : surrogate;
     const bool defined = isfinite(logp) && sums && (KIND == kSampled || isfinite(KL));
     const bool carries = c0 != 0.f || kc != 0.f;
-    const bool undefined = carries && (!defined || (c0 != 0.f && isnan(ratio)) || (kc != 0.f && !isfinite(KL)));
+    // a NaN ratio is lost in the clip; one that is infinite, or a coefficient that is no number, shows in what it makes
+    const bool undefined = carries && (!defined || (c0 != 0.f && isnan(ratio)) || !isfinite(loss) || !isfinite(g.c));
     if (writes) {
         const float nan = __int_as_float(0x7fc00000);
         A.logp[t] = defined ? logp : nan;

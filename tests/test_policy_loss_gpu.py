@@ -380,3 +380,29 @@ def test_autograd_node_on_another_stream():
                             ref_logits=i["ref_logits"], stream=side)
     torch.cuda.synchronize()
     assert torch.equal(loss.reshape(1), want.loss)
+
+
+def test_numbers_that_overflow():
+    """A ratio beyond fp32 that nothing clips, or a coefficient that is no number: the row is undefined and says so."""
+    T, V = 6, 300
+    z = (2 * torch.randn((T, 304), generator=torch.Generator(device=DEV).manual_seed(2), device=DEV)).to(torch.bfloat16)
+    ids = torch.full((T,), 9, dtype=torch.int32, device=DEV)
+    lp = torch.log_softmax(z[:, :V].double(), 1)[:, 9].float()
+    coef = torch.tensor([-0.5, 0.5, -0.5, -0.5, 0.0, -0.5], device=DEV)
+    old = lp - torch.tensor([100.0, 100.0, 1.0, 0.0, 100.0, math.inf], device=DEV)
+    for dual in (0.0, 3.0):
+        flags = api.new_flags()
+        o = acrl.policy_loss_grad_logits(z, ids, None, coef, V=V, old_logp=old, dual_clip=dual, flags=flags)
+        bad = [0, 5] if dual == 0.0 else []          # a dual clip bounds them; a positive coefficient's are bounded anyway
+        good = [t for t in range(T) if t not in bad]
+        assert acrl.read_flags(flags) == (acrl.FLAG_NONFINITE if bad else 0)
+        assert bool(o.grad[bad, :V].isnan().all()) and bool(o.token_loss[bad].isnan().all())
+        assert bool(o.grad[good, :V].isfinite().all()) and bool(o.token_loss[good].isfinite().all())
+        assert bool(o.logp.isfinite().all()) and bool(o.loss.isnan()) == bool(bad)
+    # coefficients that are no numbers
+    flags = api.new_flags()
+    o = acrl.policy_loss_grad_logits(z, ids, None, torch.tensor([math.nan, 1, math.inf, 1, 1, 1], device=DEV), V=V, kl="k1",
+                                     kl_coef=torch.tensor([0, math.nan, 0, 0, 0, 0], device=DEV), ref_logp=lp, flags=flags)
+    assert acrl.read_flags(flags) == acrl.FLAG_NONFINITE
+    assert bool(o.grad[:3, :V].isnan().all()) and bool(o.token_loss[:3].isnan().all())
+    assert bool(o.grad[3:, :V].isfinite().all()) and bool(o.token_loss[3:].isfinite().all())
