@@ -702,7 +702,9 @@ typedef enum {
  * NONFINITE; its logp and kl_out are NaN where they are undefined, and where coef
  * or kl_coef is not 0 its token_loss and gradient row are NaN.  So is a row whose
  * loss is beyond fp32: a ratio that overflows where nothing clips it (a negative
- * coef without dual_clip), a coefficient that is no finite number.  A row with both
+ * coef without dual_clip), a coefficient that is no finite number.  An estimate (K1
+ * to K3) that is infinite or NaN is one of the row's loss only where kl_coef is not 0;
+ * where it is 0, token_loss and gradient are the clipped loss's.  A row with both
  * coefficients 0 has gradient and token_loss 0.
  */
 acrl_status acrl_policy_loss_grad_logits(const acrl_bf16* logits, int64_t T, int64_t V, int64_t ld,

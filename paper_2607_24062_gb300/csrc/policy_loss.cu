@@ -427,16 +427,17 @@ __device__ __forceinline__ int row_scalars(const PolicyArgs& A, int64_t t, const
     }
     if (kc != 0.f && KIND == kSampled) g.c -= kc * slope;
     const float loss = kc != 0.f ? fmaf(kc, KL, surrogate) : surrogate;
-    const bool defined = isfinite(logp) && sums && (KIND == kSampled || isfinite(KL));
+    const bool defined = isfinite(logp) && sums, estimated = defined && isfinite(KL);   // the log-prob; the KL (0 if there is none)
     const bool carries = c0 != 0.f || kc != 0.f;
     // a NaN ratio is lost in the clip; one that is infinite, or a coefficient that is no number, shows in what it makes
-    const bool undefined = carries && (!defined || (c0 != 0.f && isnan(ratio)) || !isfinite(loss) || !isfinite(g.c));
+    const bool undefined = carries && (!(KIND == kSampled ? defined : estimated) || (c0 != 0.f && isnan(ratio)) || !isfinite(loss) ||
+                                       !isfinite(g.c));
     if (writes) {
         const float nan = __int_as_float(0x7fc00000);
         A.logp[t] = defined ? logp : nan;
-        if (A.kl_out) A.kl_out[t] = defined ? KL : nan;
+        if (A.kl_out) A.kl_out[t] = estimated ? KL : nan;
         A.token_loss[t] = undefined ? nan : loss;
-        if (!defined || undefined) raise_flag(A.flags, ACRL_FLAG_NONFINITE);
+        if (!estimated || undefined) raise_flag(A.flags, ACRL_FLAG_NONFINITE);
     }
     if (!carries || undefined) return undefined ? kFillNaN : kFillZero;
     g.target = g.c * expm1f(logp);

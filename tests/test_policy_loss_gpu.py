@@ -406,3 +406,39 @@ def test_numbers_that_overflow():
     assert acrl.read_flags(flags) == acrl.FLAG_NONFINITE
     assert bool(o.grad[:3, :V].isnan().all()) and bool(o.token_loss[:3].isnan().all())
     assert bool(o.grad[3:, :V].isfinite().all()) and bool(o.token_loss[3:].isfinite().all())
+
+
+def test_estimates_that_overflow():
+    """An infinite estimate of the KL is undefined as a figure, and in the loss where it has a factor there."""
+    T, V = 6, 300
+    z = (2 * torch.randn((T, 304), generator=torch.Generator(device=DEV).manual_seed(2), device=DEV)).to(torch.bfloat16)
+    ids = torch.full((T,), 9, dtype=torch.int32, device=DEV)
+    lp = torch.log_softmax(z[:, :V].double(), 1)[:, 9].float()
+    coef = torch.tensor([-0.5, 0.5, -0.5, -0.5, 0.0, -0.5], device=DEV)
+    ref = lp + torch.tensor([100.0, 1e30, 0.1, 0.0, 100.0, math.inf], device=DEV)
+    k = torch.tensor([0.1, 0.1, 0.1, 0.1, 0.0, 0.0], device=DEV)
+    for kl, undefined in (("k3", [0, 1, 4, 5]), ("k2", [1, 5])):
+        for kl_coef in (k, None):
+            flags = api.new_flags()
+            o = acrl.policy_loss_grad_logits(z, ids, None, coef, V=V, kl=kl, kl_coef=kl_coef, ref_logp=ref, flags=flags)
+            assert acrl.read_flags(flags) == acrl.FLAG_NONFINITE
+            assert o.kl.isnan().nonzero()[:, 0].tolist() == undefined and bool(o.logp.isfinite().all())
+            bad = [t for t in undefined if kl_coef is not None and float(k[t]) != 0]
+            good = [t for t in range(T) if t not in bad]
+            assert bool(o.grad[bad, :V].isnan().all()) and bool(o.token_loss[bad].isnan().all())
+            assert bool(o.grad[good, :V].isfinite().all()) and bool(o.token_loss[good].isfinite().all())
+
+
+@pytest.mark.parametrize("kl", ["exact", "reverse"])
+def test_log_prob_beside_an_infinite_kl(kl):
+    """Where only the KL is infinite the log-prob is a number, and is given."""
+    i = _inputs(4, 300, 8, kl)
+    i["mask"] = None
+    (i["ref_logits"] if kl == "exact" else i["z"])[1, 40] = -math.inf
+    i["ids"][:] = 17
+    flags = api.new_flags()
+    o = _run(i, flags=flags)
+    assert acrl.read_flags(flags) == acrl.FLAG_NONFINITE
+    assert o.kl.isnan().nonzero()[:, 0].tolist() == [1]
+    want = torch.log_softmax(i["z"][:, :300].double(), 1)[:, 17]
+    assert bool(((o.logp - want).abs() <= 4e-6 + 2e-7 * want.abs()).all())
