@@ -301,3 +301,38 @@ def test_what_a_call_allocates_belongs_to_its_stream():
         acrl.fp8_quantize(x, stream=side).q.view(torch.uint8)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+@pytest.mark.parametrize("M,N", [(1, 140), (1, 5000), (200, 140)])
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+def test_nan_blocks_of_one_row_and_of_many(M, N, fmt):
+    """As test_nan_blocks_reach_what_they_touch, on the one-row kernel and on pairs, quantised in the call and before."""
+    K, row = 1301, M // 2
+    x = _matrix(M, K, 12)
+    x[row, 700] = float("nan") if fmt == "e4m3" else float("-inf")
+    w = acrl.fp8_quantize(_matrix(N, K, 13), block="tile", fmt=fmt)
+    flags = api.new_flags()
+    outs = [acrl.fp8_linear(x, w, fmt=fmt, flags=flags)]
+    assert acrl.read_flags(flags) == acrl.FLAG_NONFINITE
+    outs.append(acrl.fp8_matmul(acrl.fp8_quantize(x, fmt=fmt), w))
+    for out in outs:
+        nan = out.isnan()
+        assert bool(nan[row].all()) and int(nan.sum()) == N
+    bad = _matrix(N, K, 13)
+    bad[130, 5] = float("inf")
+    flags = api.new_flags()
+    out = acrl.fp8_linear(_matrix(M, K, 12), acrl.fp8_quantize(bad, block="tile", fmt=fmt), fmt=fmt, flags=flags)
+    assert acrl.read_flags(flags) == 0                     # the activations are fine
+    assert bool(out[:, 128:256].isnan().all()) and not bool(out[:, :128].isnan().any()) and not bool(out[:, 256:].isnan().any())
+
+
+@pytest.mark.parametrize("fa,fb", [("e4m3", "e4m3"), ("e4m3", "e5m2"), ("e5m2", "e4m3"), ("e5m2", "e5m2")])
+@pytest.mark.parametrize("ba,bb", [("row", "row"), ("tile", "row"), ("row", "tile")])
+@pytest.mark.parametrize("N,K", [(1, 17), (203, 900), (130, 2051), (5001, 1337)])
+def test_one_row_formats_and_blocks(fa, fb, ba, bb, N, K):
+    x = _matrix(1, K, 3)
+    a, b = acrl.fp8_quantize(x, fmt=fa, block=ba), acrl.fp8_quantize(_matrix(N, K, 4), fmt=fb, block=bb)
+    for dtype in (torch.float32, torch.bfloat16):
+        out = acrl.fp8_matmul(a, b, out_dtype=dtype)
+        _check_product(out, a, b)
+        assert torch.equal(acrl.fp8_linear(x, b, fmt=fa, out_dtype=dtype), out)
