@@ -28,8 +28,8 @@ inline bool matrix_ok(const Matrix& m, int64_t K) {
 // kFewNot: these sizes are not its.
 constexpr acrl_status kFewNot = ACRL_ERR_NOT_IMPLEMENTED;
 bool few_rows(int64_t M, int64_t N, int64_t K);
-acrl_status matmul_few(const Matrix& a, const acrl_bf16* x, int64_t ldx, const Matrix& b, int64_t K, void* out, acrl_dtype out_dtype,
-                       int64_t ldo, int32_t* flags, cudaStream_t s);
+acrl_status matmul_few(const Matrix& a, const acrl_bf16* x, const Matrix& b, int64_t K, void* out, acrl_dtype out_dtype, int32_t* flags,
+                       cudaStream_t s);
 
 // Where a quantised matrix goes.
 struct Quantised {

@@ -23,10 +23,9 @@ constexpr int64_t kFewBytes = 16 << 20;
 int64_t few_cols(int64_t K) { return (K + 2 * kStep - 1) / (2 * kStep) * (2 * kStep); }
 
 struct FewArgs {
-    Matrix a, b;
-    const acrl_bf16* x;
-    int64_t ldx, ldo;
-    int K, cols;      // columns, and those that the steps cover
+    Matrix a, b;          // a: the one row
+    const acrl_bf16* x;   // the row as activations, or null
+    int K, cols;          // columns, and those that the steps cover
     void* out;
     int32_t* flags;
 };
@@ -78,11 +77,11 @@ __device__ __forceinline__ uint4 load16(const uint8_t* row, int c, int K) {
 // The row as fp32 values, zeros beyond K: sixteen lanes a block of 128 columns.
 template <int FMT>
 __device__ __forceinline__ void quantise_into(const FewArgs& A, float* xs) {
-    const int blocks = A.cols / 128, l = threadIdx.x & 15;
-    for (int u = threadIdx.x >> 4; u < int(A.a.rows) * blocks; u += kThreads / 16) {   // whole half-warps
-        const int m = u / blocks, c = (u - m * blocks) * 128 + l * 8;
+    const int l = threadIdx.x & 15;
+    for (int u = threadIdx.x >> 4; u < A.cols / 128; u += kThreads / 16) {   // whole half-warps
+        const int c = u * 128 + l * 8;
         float f[8];
-        load8<acrl_bf16>(A.x + m * A.ldx + min(c, A.K), max(0, A.K - c), f);
+        load8<acrl_bf16>(A.x + min(c, A.K), max(0, A.K - c), f);
         uint32_t top = max8(f);
         const uint32_t mask = 0xffffu << (threadIdx.x & 16);
 #pragma unroll
@@ -94,7 +93,7 @@ __device__ __forceinline__ void quantise_into(const FewArgs& A, float* xs) {
         float w[8];
         widen4<FMT>(q.x, w);
         widen4<FMT>(q.y, w + 4);
-        float4* to = reinterpret_cast<float4*>(xs + m * A.cols + c);
+        float4* to = reinterpret_cast<float4*>(xs + c);
         to[0] = make_float4(w[0] * by, w[1] * by, w[2] * by, w[3] * by);
         to[1] = make_float4(w[4] * by, w[5] * by, w[6] * by, w[7] * by);
     }
@@ -102,13 +101,11 @@ __device__ __forceinline__ void quantise_into(const FewArgs& A, float* xs) {
 
 template <int FMT>
 __device__ __forceinline__ void widen_into(const FewArgs& A, float* xs) {
-    const int pieces = A.cols / 16;
-    for (int u = threadIdx.x; u < int(A.a.rows) * pieces; u += kThreads) {
-        const int m = u / pieces, c = (u - m * pieces) * 16;
+    for (int c = threadIdx.x * 16; c < A.cols; c += kThreads * 16) {
         float w[16];
-        widen16<FMT>(load16(A.a.q + m * A.a.ld, c, A.K), w);
-        const float by = c < A.K ? factor_of(A.a.scale[(A.a.block == ACRL_FP8_TILE ? 0 : m) * A.a.lds + (c >> 7)]) : 0.f;
-        float4* to = reinterpret_cast<float4*>(xs + m * A.cols + c);
+        widen16<FMT>(load16(A.a.q, c, A.K), w);
+        const float by = c < A.K ? factor_of(A.a.scale[c >> 7]) : 0.f;
+        float4* to = reinterpret_cast<float4*>(xs + c);
 #pragma unroll
         for (int j = 0; j < 4; ++j) to[j] = make_float4(w[4 * j] * by, w[4 * j + 1] * by, w[4 * j + 2] * by, w[4 * j + 3] * by);
     }
@@ -201,16 +198,14 @@ acrl_status launch_few(const FewArgs& A, cudaStream_t s) {
 // (1 x 4,096 x 151,936: 100 us against 142).
 bool few_rows(int64_t M, int64_t N, int64_t K) { return M == 1 && K > 0 && N * K <= kFewBytes && few_cols(K) * 4 <= kMostBytes; }
 
-acrl_status matmul_few(const Matrix& a, const acrl_bf16* x, int64_t ldx, const Matrix& b, int64_t K, void* out, acrl_dtype out_dtype,
-                       int64_t ldo, int32_t* flags, cudaStream_t s) {
+acrl_status matmul_few(const Matrix& a, const acrl_bf16* x, const Matrix& b, int64_t K, void* out, acrl_dtype out_dtype, int32_t* flags,
+                       cudaStream_t s) {
     if (!few_rows(a.rows, b.rows, K)) return kFewNot;
     const int64_t cols = few_cols(K);
     FewArgs A = {};
     A.a = a;
     A.b = b;
     A.x = x;
-    A.ldx = ldx;
-    A.ldo = ldo;
     A.K = int(K);
     A.cols = int(cols);
     A.out = out;

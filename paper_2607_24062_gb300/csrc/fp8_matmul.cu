@@ -942,7 +942,7 @@ acrl_status product(const Matrix& a, const Matrix& b, int64_t K, void* out, acrl
                    ? ACRL_OK
                    : launch_status();
     }
-    const acrl_status few = matmul_few(a, nullptr, 0, b, K, out, out_dtype, ldo, flags, s);
+    const acrl_status few = matmul_few(a, nullptr, b, K, out, out_dtype, flags, s);
     if (few != kFewNot) return few;
     return out_dtype == ACRL_BF16 ? launch_matmul<acrl_bf16>(a, b, K, out, ldo, flags, s)
                                   : launch_matmul<float>(a, b, K, out, ldo, flags, s);
@@ -1079,7 +1079,7 @@ extern "C" acrl_status acrl_fp8_linear(const acrl_bf16* x, int64_t M, int64_t K,
     if (!out || !aligned16(out) || (K > 0 && (!x || !w || !w_scale || !aligned16(x) || !aligned16(w)))) return ACRL_ERR_INVALID_ARG;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     if (K > 0) {
-        const acrl_status few = matmul_few(a, x, ldx, b, K, out, out_dtype, ldo, dev_flags, s);
+        const acrl_status few = matmul_few(a, x, b, K, out, out_dtype, dev_flags, s);
         if (few != kFewNot) return few;
         if (!operands_on_current_device({w, q, out})) return ACRL_ERR_INVALID_ARG;
     }
