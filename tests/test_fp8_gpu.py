@@ -336,3 +336,35 @@ def test_one_row_formats_and_blocks(fa, fb, ba, bb, N, K):
         out = acrl.fp8_matmul(a, b, out_dtype=dtype)
         _check_product(out, a, b)
         assert torch.equal(acrl.fp8_linear(x, b, fmt=fa, out_dtype=dtype), out)
+
+
+@pytest.mark.parametrize("fa,fb", [("e4m3", "e4m3"), ("e5m2", "e4m3"), ("e4m3", "e5m2")])
+@pytest.mark.parametrize("M", [1, 2, 150])
+def test_scales_of_any_size(fa, fb, M):
+    """Factors near the ends of their range whose products are ordinary: a row as large as fp32 allows and a small matrix, and the
+    other way round."""
+    K, N = 700, 300
+    for up in (118, -118):
+        a, b = acrl.fp8_quantize(_matrix(M, K, 61), fmt=fa), acrl.fp8_quantize(_matrix(N, K, 62), fmt=fb, block="tile")
+        a = acrl.Fp8Tensor(a.q, (a.scale.int() + up).clamp(0, 254).to(torch.uint8))
+        b = acrl.Fp8Tensor(b.q, (b.scale.int() - up).clamp(0, 254).to(torch.uint8))
+        sa, sb = (torch.exp2(t.scale.double() - 127).cpu().numpy() for t in (a, b))
+        A = a.q.float().cpu().numpy().astype(np.float64) * np.repeat(sa, 128, 1)[:, :K]
+        B = b.q.float().cpu().numpy().astype(np.float64) * np.repeat(np.repeat(sb, 128, 1)[:, :K], 128, 0)[:N]
+        exact, off = A @ B.T, 2.0 ** -24 * np.sqrt(K) * (np.abs(A) @ np.abs(B).T)
+        assert np.abs(exact).max() < 1e30
+        out = acrl.fp8_matmul(a, b, out_dtype=torch.float32).double().cpu().numpy()
+        assert (np.abs(out - exact) <= off * (1 + 2.0 ** -20) + 2.0 ** -24 * np.abs(exact)).all()
+
+
+def test_one_row_of_activations_at_the_ends_of_their_range():
+    K, N = 700, 300
+    for size in (2.0 ** 120, 2.0 ** -120):
+        x = torch.zeros((2, 704), dtype=torch.bfloat16, device=DEV)
+        w = torch.zeros((N, 704), dtype=torch.bfloat16, device=DEV)
+        x[:, :K], w[:, :K] = _matrix(1, K, 63).double() * size, _matrix(N, K, 64).double() / size
+        w8 = acrl.fp8_quantize(w[:, :K], block="tile")
+        one = acrl.fp8_linear(x[:1, :K], w8, out_dtype=torch.float32)
+        two = acrl.fp8_linear(x[:, :K], w8, out_dtype=torch.float32)
+        assert bool(one.isfinite().all())
+        assert bool(((one[0] - two[0]).abs() <= 2.0 ** -18 * two.abs().max()).all())
