@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(kRowThreads)
     const T* xr = x + (in ? row : 0) * ldx;
     Eight<T> f[kRowUnroll];
     // whole units without a test between their loads, so that all of them are in flight together
-    if (in && (kb0 + kRowUnroll) * 128 <= C) {
+    if (in && kb0 + kRowUnroll <= C >> 7) {   // in blocks: their columns' number may pass 32 bits
 #pragma unroll
         for (int k = 0; k < kRowUnroll; ++k) f[k].load(xr + (kb0 + k) * 128 + l * 8, 8);
     } else {

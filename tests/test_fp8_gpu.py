@@ -368,3 +368,14 @@ def test_one_row_of_activations_at_the_ends_of_their_range():
         two = acrl.fp8_linear(x[:, :K], w8, out_dtype=torch.float32)
         assert bool(one.isfinite().all())
         assert bool(((one[0] - two[0]).abs() <= 2.0 ** -18 * two.abs().max()).all())
+
+
+def test_quantize_the_longest_rows():
+    """A row of as many columns as the call takes, the largest number of all just beyond them."""
+    C = 2 ** 31 - 1
+    x = torch.zeros((1, C + 1), dtype=torch.bfloat16, device=DEV)
+    x[0, C], x[0, C - 1], x[0, 5] = 1e30, 3.0, 5.0
+    t = acrl.fp8_quantize(x[:, :C])
+    assert float(t.q[0, C - 1].float()) == 384.0 and int(t.scale[0, -1]) == 120     # 3 = 384 2^-7
+    assert float(t.q[0, 5].float()) == 320.0 and int(t.scale[0, 0]) == 121          # 5 = 320 2^-6
+    assert bool((t.scale[0, 1:-1] == 127).all())
