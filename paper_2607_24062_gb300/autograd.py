@@ -25,6 +25,7 @@ from __future__ import annotations
 from typing import Callable
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import api
 from .pipeline import AcrlStep, PreferenceStep
@@ -135,6 +136,7 @@ class _Fp8Layer(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, w = ctx.saved_tensors
         dx, dw = api.fp8_linear_backward(_rows_of_eight(dy), x, api.fp8_quantize(w, block="tile", transpose=True),
@@ -144,5 +146,5 @@ class _Fp8Layer(torch.autograd.Function):
 
 def fp8_layer(x: torch.Tensor, weight: torch.Tensor, grad_fmt: str = "e4m3") -> torch.Tensor:
     """x [M, K] times the transpose of weight [N, K] (both bf16), computed on 8-bit matrices; the backward's two products
-    are on 8-bit matrices as well, the incoming gradient in `grad_fmt`."""
+    are on 8-bit matrices as well, the incoming gradient in `grad_fmt`.  They have no derivative of their own."""
     return _Fp8Layer.apply(x, weight, grad_fmt)

@@ -379,3 +379,13 @@ def test_quantize_the_longest_rows():
     assert float(t.q[0, C - 1].float()) == 384.0 and int(t.scale[0, -1]) == 120     # 3 = 384 2^-7
     assert float(t.q[0, 5].float()) == 320.0 and int(t.scale[0, 0]) == 121          # 5 = 320 2^-6
     assert bool((t.scale[0, 1:-1] == 127).all())
+
+
+def test_layer_has_no_second_derivative():
+    """Its backward's products have no backward: a graph of the gradients is refused, not left without their part."""
+    x = _matrix(9, 64, 8).contiguous().requires_grad_()
+    w = _matrix(40, 64, 10, std=0.02).contiguous().requires_grad_()
+    y = acrl.fp8_layer(x, w)
+    dx, = torch.autograd.grad(y.float().square().sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        dx.float().sum().backward()
