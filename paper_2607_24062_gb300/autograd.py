@@ -76,12 +76,14 @@ class _PolicyLoss(torch.autograd.Function):
             here.wait_stream(stream)
             for t in (out.grad, out.loss):    # of `stream`, and read here
                 t.record_stream(here)
-        ctx.grad, ctx.shape = out.grad, logits.shape
+        # the very tensor that the backward returns: a leaf takes a gradient that nobody else holds as its .grad, and what is
+        # done to that would be done to the next backward's too
+        ctx.grad = out.grad[: logits.shape[0], : logits.shape[1]]
         return out.loss.reshape(()).clone()
 
     @staticmethod
     def backward(ctx, grad_out):
-        return _scaled(ctx.grad[: ctx.shape[0], : ctx.shape[1]], grad_out), None, None, None, None
+        return _scaled(ctx.grad, grad_out), None, None, None, None
 
 
 def policy_loss(logits: torch.Tensor, ids, mask, coef, **kw) -> torch.Tensor:

@@ -442,3 +442,21 @@ def test_log_prob_beside_an_infinite_kl(kl):
     assert o.kl.isnan().nonzero()[:, 0].tolist() == [1]
     want = torch.log_softmax(i["z"][:, :300].double(), 1)[:, 17]
     assert bool(((o.logp - want).abs() <= 4e-6 + 2e-7 * want.abs()).all())
+
+
+def test_autograd_node_again_and_again():
+    """A graph that is kept gives the same gradient each time, whatever was done to the leaf's in between."""
+    i = _inputs(5, 80, 11)
+    y = i["z"].clone().requires_grad_()
+    loss = acrl.policy_loss(y, i["ids"], i["mask"], i["coef"], old_logp=i["old"], kl="exact", kl_coef=i["kl_coef"],
+                            ref_logits=i["ref_logits"])
+    loss.backward(retain_graph=True)
+    first = y.grad.clone()
+    y.grad.mul_(3.0)                # as a clipped gradient norm does
+    y.grad = None
+    loss.backward(retain_graph=True)
+    assert torch.equal(y.grad, first)
+    loss.backward()                 # and added up
+    assert torch.equal(y.grad, first + first)
+    loss_again = _run(dict(i, z=y.detach(), V=80)).grad
+    assert torch.equal(first, loss_again)
