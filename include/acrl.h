@@ -715,6 +715,15 @@ acrl_status acrl_policy_loss_grad_logits(const acrl_bf16* logits, int64_t T, int
                                          float* kl_out, float* token_loss, float* loss, int32_t* dev_flags,
                                          acrl_stream stream);
 
+/*
+ * acrl_token_logp -- lse and logp of acrl_token_stats on the same arguments (no
+ * entropy; dev_flags may be NULL), from sums without a bias: the log-probs of a
+ * response add up in a log ratio, here and on the policy's side (acrl_preference_step
+ * takes the same), and with them what their errors have in common.
+ */
+acrl_status acrl_token_logp(const acrl_bf16* logits, int64_t T, int64_t V, int64_t ld, const int32_t* ids,
+                            const uint8_t* mask, float* lse, float* logp, int32_t* dev_flags, acrl_stream stream);
+
 typedef enum {
     ACRL_PREF_SIGMOID = 0,  /* (1 - s) log(1 + e^-h) + s log(1 + e^h), s = label_smoothing */
     ACRL_PREF_HINGE = 1,    /* max(0, 1 - h)                                               */
@@ -754,7 +763,7 @@ acrl_status acrl_preference_loss(const float* logp, const float* ref_logp, const
  * log-probs of the rows, acrl_preference_loss on them, and acrl_loss_grad_logits
  * with its coef, which writes d loss / d logits.  Arguments, outputs and flags are
  * theirs (dev_flags is required); lse and logp, device float [T], are those of
- * acrl_token_stats, from sums without a bias that a response's tokens would add up.
+ * acrl_token_logp.
  *   workspace  device, 16-byte aligned, acrl_preference_step_workspace_bytes(T, S,
  *              Gn) bytes.
  */

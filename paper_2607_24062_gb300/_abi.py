@@ -109,6 +109,7 @@ SIGNATURES = {
                                          c_i64, c_i32, c_p, c_i32, c_i64, c_p, c_i32, c_i64, c_p, c_i64, c_p, c_p]),
     "acrl_policy_loss_grad_logits": (c_i32, [c_p, c_i64, c_i64, c_i64, c_p, c_p, c_p, c_p, c_f32, c_f32, c_f32, c_i32,
                                              c_p, c_p, c_i64, c_p, c_p, c_p, c_p, c_p, c_p, c_p, c_p]),
+    "acrl_token_logp": (c_i32, [c_p, c_i64, c_i64, c_i64, c_p, c_p, c_p, c_p, c_p, c_p]),
     "acrl_preference_workspace_bytes": (c_i64, [c_i32, c_i32]),
     "acrl_preference_loss": (c_i32, [c_p, c_p, c_p, c_i64, c_p, c_p, c_i32, c_p, c_i32, c_i32, c_f32, c_f32, c_f32, c_i32,
                                      c_p, c_p, c_p, c_p, c_i64, c_p, c_p]),

@@ -763,6 +763,21 @@ def policy_loss_grad_logits(logits, ids, mask, coef, *, V=None, old_logp=None, c
     return PolicyLoss(grad, logp, kl_out, token_loss, loss)
 
 
+def token_logp(logits, ids, mask=None, *, V=None, lse=None, logp=None, flags=None, stream=None):
+    """acrl_token_logp.  Returns (lse, logp) float32 [T]."""
+    T, ld = _rows(logits, "logits")
+    if stream is not None:
+        return _on_stream(token_logp, "acrl_token_logp", logits, stream, logits, ids, mask, V=V, lse=lse, logp=logp, flags=flags)
+    V = ld if V is None else V
+    _need(ids, torch.int32, T, "ids")
+    _opt(mask, torch.uint8, T, "mask")
+    lse, logp = (_vec(t, torch.float32, T, name, logits.device) for t, name in ((lse, "lse"), (logp, "logp")))
+    _opt(flags, torch.int32, 1, "flags")
+    _call("acrl_token_logp", (logits, ids, mask, lse, logp, flags), None, _ptr(logits), T, V, ld, _ptr(ids), _ptr(mask),
+          _ptr(lse), _ptr(logp), _ptr(flags))
+    return lse, logp
+
+
 @dataclass
 class Preference:
     loss: torch.Tensor     # float32 [1]
@@ -948,7 +963,7 @@ def check_flags(flags, stream=None) -> None:
 __all__ = ["Params", "AcrlError", "token_stats", "seq_discrepancy", "grpo_advantage", "controller_init",
            "controller_step", "importance_weights", "step", "loss_grad_logits", "reduce_loss", "scale_grad",
            "read_flags", "check_flags", "read_state", "Discrepancy",
-           "PolicyLoss", "policy_loss_grad_logits", "Preference", "preference_loss", "preference_workspace_bytes",
+           "PolicyLoss", "policy_loss_grad_logits", "token_logp", "Preference", "preference_loss", "preference_workspace_bytes",
            "preference_step", "preference_step_workspace_bytes",
            "Fp8Tensor", "fp8_quantize", "fp8_matmul", "fp8_linear", "fp8_linear_backward", "fp8_linear_workspace_bytes",
            "fp8_linear_backward_workspace_bytes",

@@ -31,7 +31,6 @@
 #include "acrl_device.cuh"
 #include "acrl_host.h"
 #include "mbarrier.cuh"
-#include "row_logp.h"
 #include "row_lse.cuh"
 
 namespace acrl {
@@ -851,12 +850,19 @@ acrl_status launch_policy(const PolicyArgs& A, cudaStream_t s) {
 
 }  // namespace
 
-acrl_status row_logp(const acrl_bf16* logits, int64_t T, int64_t V, int64_t ld, const int32_t* ids, const uint8_t* mask, float* lse,
-                     float* logp, int32_t* flags, cudaStream_t s) {
+}  // namespace acrl
+
+using namespace acrl;
+
+extern "C" acrl_status acrl_token_logp(const acrl_bf16* logits, int64_t T, int64_t V, int64_t ld, const int32_t* ids,
+                                       const uint8_t* mask, float* lse, float* logp, int32_t* dev_flags, acrl_stream stream) {
+    if (T < 0 || V < 1 || V > kMaxVocab || ld < V || (ld & 7) != 0) return ACRL_ERR_INVALID_ARG;
+    if (T > 0 && (!logits || !ids || !lse || !logp || !aligned16(logits))) return ACRL_ERR_INVALID_ARG;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     PolicyArgs A = {};
     A.V = int(V);
     A.ldz = ld;
-    A.flags = flags;
+    A.flags = dev_flags;
     for (int64_t t = 0; t < T; t += kMaxGrid) {
         A.z = logits + t * ld;
         A.ids = ids + t;
@@ -871,10 +877,6 @@ acrl_status row_logp(const acrl_bf16* logits, int64_t T, int64_t V, int64_t ld, 
     }
     return ACRL_OK;
 }
-
-}  // namespace acrl
-
-using namespace acrl;
 
 extern "C" acrl_status acrl_policy_loss_grad_logits(const acrl_bf16* logits, int64_t T, int64_t V, int64_t ld,
                                                     const int32_t* ids, const uint8_t* mask, const float* old_logp,

@@ -14,7 +14,6 @@
 
 #include "acrl_device.cuh"
 #include "acrl_host.h"
-#include "row_logp.h"
 
 namespace acrl {
 namespace {
@@ -311,7 +310,7 @@ extern "C" acrl_status acrl_preference_step(const acrl_bf16* logits, int64_t T, 
     if (!pairs_ok(logp, T, rewards, seq_offsets, S, group_offsets, Gn, form, beta, margin, label_smoothing, ratio, coef, loss))
         return ACRL_ERR_INVALID_ARG;
     if (T > 0) {
-        const acrl_status st = row_logp(logits, T, V, ld, ids, mask, lse, logp, dev_flags, reinterpret_cast<cudaStream_t>(stream));
+        const acrl_status st = acrl_token_logp(logits, T, V, ld, ids, mask, lse, logp, dev_flags, stream);
         if (st != ACRL_OK) return st;
     }
     acrl_status st = acrl_preference_loss(logp, ref_logp, mask, T, rewards, seq_offsets, S, group_offsets, Gn, form, beta, margin,

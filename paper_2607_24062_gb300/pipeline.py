@@ -262,12 +262,12 @@ class Fp8Head:
         return api.fp8_linear(hidden, self.weight, out=out, workspace=workspace, flags=flags, stream=stream)
 
     def logp(self, hidden, ids, mask=None, *, out=None, flags=None, stream=None):
-        """float32 [T] log-probs of the sampled tokens (0 where masked)."""
+        """float32 [T] log-probs of the sampled tokens (0 where masked), as a PreferenceStep makes the policy's."""
         if stream is not None:
             with torch.cuda.stream(stream):
                 return self.logp(hidden, ids, mask, out=out, flags=flags)
         z = self.logits(hidden, out=out, flags=flags)
-        return api.token_stats(z, ids, mask, V=z.shape[1], flags=flags)[1]
+        return api.token_logp(z, ids, mask, V=z.shape[1], flags=flags)[1]
 
 
 class HostPipeline:

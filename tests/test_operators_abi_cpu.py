@@ -110,3 +110,11 @@ def test_preference_step(L):
                 dict(n=n - 1), dict(ws=FAKE + 4), dict(z=FAKE + 2), dict(grad=FAKE + 8), dict(T=-1), dict(V=0), dict(ld=8),
                 dict(ld=20), dict(S=-1), dict(S=0), dict(Gn=0), dict(form=3), dict(beta=-1.0), dict(smooth=0.5)):
         assert _call(L.acrl_preference_step, ok, **bad) == E, bad
+
+
+def test_token_logp(L):
+    ok = dict(z=FAKE, T=9, V=16, ld=16, ids=FAKE, mask=None, lse=FAKE, logp=FAKE, flags=None, stream=None)
+    for bad in (dict(z=None), dict(ids=None), dict(lse=None), dict(logp=None), dict(z=FAKE + 2), dict(T=-1), dict(V=0), dict(ld=8),
+                dict(ld=20), dict(V=(1 << 30) + 8, ld=(1 << 30) + 8)):
+        assert _call(L.acrl_token_logp, ok, **bad) == E, bad
+    assert _call(L.acrl_token_logp, ok, T=0, z=None, ids=None) == OK

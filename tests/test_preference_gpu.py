@@ -267,3 +267,29 @@ def test_log_probs_of_columns_far_below_the_others(V, shape):
     lp = z[:, :V].gather(1, ids.long()[:, None])[:, 0].double() - lse
     for got, want in ((step.lse, lse), (step.logp, lp)):
         assert bool(((got - want).abs() <= 4e-6 + 2e-7 * want.abs()).all())
+
+
+def test_token_logp():
+    """The step's lse and log-probs by themselves, to the last bit, on any stream; nothing for no rows."""
+    T, V = 40, 5003
+    g = torch.Generator(device=DEV).manual_seed(6)
+    z = (2 * torch.randn((T, 5008), generator=g, device=DEV)).to(torch.bfloat16)
+    ids = torch.randint(0, V, (T,), generator=g, device=DEV, dtype=torch.int32)
+    mask = (torch.arange(T, device=DEV) % 4 > 0).to(torch.uint8)
+    step = acrl.PreferenceStep(T, V, 5008, 2, 1)
+    step.run(z, ids, mask, None, torch.tensor([1.0, 0.0], device=DEV), torch.tensor([0, 9, T], device=DEV),
+             torch.tensor([0, 2], dtype=torch.int32, device=DEV))
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for lse, logp in (api.token_logp(z, ids, mask, V=V), api.token_logp(z, ids, mask, V=V, stream=side)):
+        torch.cuda.synchronize()
+        assert torch.equal(lse, step.lse) and torch.equal(logp, step.logp)
+    assert [t.numel() for t in api.token_logp(z[:0], ids[:0], V=V)] == [0, 0]
+    flags = api.new_flags()
+    ids[3], z[5, 7] = V, math.nan
+    logp = api.token_logp(z, ids, mask, V=V, flags=flags)[1]
+    assert acrl.read_flags(flags) == acrl.FLAG_BAD_ID | acrl.FLAG_NONFINITE
+    assert float(logp[3]) == 0 and bool(logp[5].isnan())
+    for bad in (dict(ids=ids.long()), dict(ids=ids[:3]), dict(mask=mask.bool()), dict(logits=z.float()), dict(V=5009), dict(logp=ids)):
+        with pytest.raises(acrl.AcrlError):
+            api.token_logp(**{**dict(logits=z, ids=ids, mask=mask, V=V), **bad})
