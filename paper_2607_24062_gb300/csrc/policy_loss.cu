@@ -38,7 +38,9 @@ namespace {
 
 constexpr int kMaxCluster = 8;
 
-enum Kind { kSampled, kExact, kReverse };   // which sums a row needs
+enum Kind { kSampled, kExact, kReverse, kMean };   // which sums a row needs; kMean: the log-probs by themselves
+template <Kind KIND>
+constexpr bool kTwo = KIND == kExact || KIND == kReverse;   // two operands
 
 struct PolicyArgs {
     const acrl_bf16 *z, *x;
@@ -60,7 +62,7 @@ struct PolicyArgs {
 };
 
 // A row's (or part's) running state in base 2: maxima, exponents U = max log2 e as whole numbers, sums
-// against them, and the cross sum: exact  sum 2^(u - U) (z - x),  reverse  sum 2^(w - W) (x - z).
+// against them, and the cross sum: exact  sum 2^(u - U) (z - x),  reverse  sum 2^(w - W) (x - z),  mean  sum 2^(u - U) z.
 // `off` = sx - sz where U = W: KL of two close distributions needs the logarithm of the sums' ratio to better than the
 // sums' own roundings, and the difference, summed by itself from the lanes on, is rounded at its own size.
 struct State {
@@ -69,8 +71,13 @@ struct State {
 
 __device__ __forceinline__ State empty_state() { return State{-INFINITY, kLowestU, 0.f, -INFINITY, kLowestU, 0.f, 0.f, 0.f}; }
 
-// log2 e less its nearest fp32 number: left out, it would tilt every log-prob by 1.3e-8 of the logits' weighted mean, which
-// a sum over a response's tokens carries.  (With KL over the vocabulary nothing sums them, and p's and q's tilts cancel.)
+// log2 e less its nearest fp32 number: left out of the exponents, as here, it tilts lse by 1.3e-8 of the distribution's mean logit,
+// and every log-prob with it, which a sum over a response's tokens carries; so lse takes it afterwards.  (In the exponents it
+// would be lost to their rounding where a column lies far above those of U.)  The log-probs by themselves, bound by HBM, sum the
+// mean too.  A loss's sums leave no room for another product a column (2-8 % of the time): halfway between lse, which is the
+// mean and the entropy, and the sampled logit, which is the mean over tokens sampled from the row, is near enough, and for an
+// unlikely token the difference is below the rounding of its log-prob.  p's and q's tilts cancel in the KL.  (Mean error over rows
+// of 4,096 columns around 0 / 20, KL over the vocabulary: 9.4e-8 / 3.6e-7 before, 2e-8 / 3e-8 so.)
 constexpr float kLog2eLow = 1.92596303e-8f;
 
 // Whole numbers: sums are brought from one to another without a rounding.
@@ -97,6 +104,15 @@ __device__ __forceinline__ LogShare less_log(float z, float m, float U, float s)
     const float l = kLn2 * log2f(f);
     if (fabsf(U) < 1e6f) return LogShare{fmaf(-n, kHi, z), fmaf(n, kLo, l)};
     return LogShare{z - m, l + kLn2 * (n - U - fmaf(m, kLog2e, -U))};
+}
+
+// That of a row's own logits, with what the exponents lack; z: the sampled one's (0 with kMean: -lse).
+template <Kind KIND>
+__device__ __forceinline__ LogShare log_share(float z, const State& row) {
+    LogShare r = less_log(z, row.mz, row.U, row.sz);
+    const float lse = kLn2 * (row.U + log2f(row.sz)), mean = row.cross / row.sz;
+    r.rest = fmaf(kLog2eLow * kLn2, KIND != kMean ? 0.5f * (z + lse) : isfinite(mean) ? mean : lse, r.rest);
+    return r;
 }
 
 // Two fp32 numbers in a register pair: sums, products and fused products of both in one instruction (issue bounds these
@@ -166,9 +182,9 @@ __device__ __forceinline__ void fold(State& st, const uint4 (&z)[N], const uint4
     if (vm > st.mz) {
         const float f = raise_max(vm, st.mz, st.U);
         st.sz *= f;
-        if (KIND == kExact) st.cross *= f;
+        if (KIND != kReverse) st.cross *= f;
     }
-    if constexpr (KIND != kSampled) {
+    if constexpr (kTwo<KIND>) {
         uint32_t qm = max_pairs(x[0]);
 #pragma unroll
         for (int k = 1; k < N; ++k) qm = max_bf16x2(qm, max_pairs(x[k]));
@@ -180,16 +196,16 @@ __device__ __forceinline__ void fold(State& st, const uint4 (&z)[N], const uint4
         }
     }
     const Two l2e = two(kLog2e, kLog2e), nU = two(-st.U, -st.U), nW = two(-st.W, -st.W), minus = two(-1.f, -1.f);
-    const Two low = two(kLog2eLow, kLog2eLow);
     Two sz = two(0.f, 0.f), sx = sz, cr = sz;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
         const uint32_t zw[4] = {z[k].x, z[k].y, z[k].z, z[k].w}, xw[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const Two a = widen(zw[j]), u = fma2(a, l2e, nU), e = ex2_2(KIND == kSampled ? fma2(a, low, u) : u);
+            const Two a = widen(zw[j]), e = ex2_2(fma2(a, l2e, nU));
             sz = add2(sz, e);
-            if constexpr (KIND != kSampled) {
+            if constexpr (KIND == kMean) cr = fma2(e, where_weighted(e, a), cr);
+            if constexpr (kTwo<KIND>) {
                 const Two b = widen(xw[j]), h = ex2_2(fma2(b, l2e, nW));
                 sx = add2(sx, h);
                 const Two w = KIND == kExact ? e : h, d = KIND == kExact ? fma2(b, minus, a) : fma2(a, minus, b);
@@ -198,10 +214,8 @@ __device__ __forceinline__ void fold(State& st, const uint4 (&z)[N], const uint4
         }
     }
     st.sz += sum_of(sz);
-    if (KIND != kSampled) {
-        st.sx += sum_of(sx);
-        st.cross += sum_of(cr);
-    }
+    st.cross += sum_of(cr);
+    if (kTwo<KIND>) st.sx += sum_of(sx);
 }
 
 // The quick way: sums against exponents that are fixed for a warp's share of the row, those of some of its columns.  Sums are as
@@ -222,7 +236,7 @@ struct Quick {
         const float U = exponent_of(mz);
         nU = two(-U, -U);
         sz = sx = cr = two(0.f, 0.f);
-        if constexpr (KIND != kSampled) {
+        if constexpr (kTwo<KIND>) {
             mx = warp_max_of(max_pairs(x));
             const float W = exponent_beside(mx, U);
             nW = two(-W, -W);
@@ -235,15 +249,16 @@ struct Quick {
     }
     template <int N>
     __device__ __forceinline__ void fold(const uint4 (&z)[N], const uint4 (&x)[N]) {
-        const Two l2e = two(kLog2e, kLog2e), low = two(kLog2eLow, kLog2eLow), minus = two(-1.f, -1.f);
+        const Two l2e = two(kLog2e, kLog2e), minus = two(-1.f, -1.f);
 #pragma unroll
         for (int k = 0; k < N; ++k) {
             const uint32_t zw[4] = {z[k].x, z[k].y, z[k].z, z[k].w}, xw[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const Two a = widen(zw[j]), u = fma2(a, l2e, nU), e = ex2_2(KIND == kSampled ? fma2(a, low, u) : u);
+                const Two a = widen(zw[j]), e = ex2_2(fma2(a, l2e, nU));
                 sz = add2(sz, e);
-                if constexpr (KIND != kSampled) {
+                if constexpr (KIND == kMean) cr = fma2(e, a, cr);     // NaN beside a column at -infinity: log_share() looks
+                if constexpr (kTwo<KIND>) {
                     const Two b = widen(xw[j]), h = ex2_2(fma2(b, l2e, nW));
                     sx = add2(sx, h);
                     cr = KIND == kExact ? fma2(e, fma2(b, minus, a), cr) : fma2(h, fma2(a, minus, b), cr);
@@ -256,11 +271,11 @@ struct Quick {
         s.mz = mz;
         s.U = exponent_of(mz);
         s.sz = sum_of(sz);
-        if constexpr (KIND != kSampled) {
+        s.cross = sum_of(cr);
+        if constexpr (kTwo<KIND>) {
             s.mx = mx;
             s.W = exponent_beside(mx, s.U);
             s.sx = sum_of(sx);
-            s.cross = sum_of(cr);
             s.off = s.sx - s.sz;
         }
         return s;
@@ -275,9 +290,10 @@ __device__ __forceinline__ State bring(const State& s, float mz, float mx) {
     r.U = exponent_of(mz);
     const float f = ex2(s.U - r.U);
     r.sz = s.sz * f;
-    if constexpr (KIND == kSampled) {
+    if constexpr (!kTwo<KIND>) {
         r.mx = mx;
-        r.W = r.sx = r.cross = r.off = 0.f;
+        r.W = r.sx = r.off = 0.f;
+        r.cross = KIND == kMean ? s.cross * f : 0.f;
     } else {
         r.mx = mx;
         r.W = exponent_beside(mx, r.U);
@@ -296,15 +312,15 @@ __device__ __forceinline__ State meet(State s) {
 #pragma unroll
     for (int m = LANES / 2; m >= 1; m >>= 1) {
         mz = fmaxf(mz, __shfl_xor_sync(0xffffffffu, mz, m));
-        if (KIND != kSampled) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, m));
+        if (kTwo<KIND>) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, m));
     }
     s = bring<KIND>(s, mz, mx);
 #pragma unroll
     for (int m = LANES / 2; m >= 1; m >>= 1) {
         s.sz += __shfl_xor_sync(0xffffffffu, s.sz, m);
-        if (KIND != kSampled) {
+        if (KIND != kSampled) s.cross += __shfl_xor_sync(0xffffffffu, s.cross, m);
+        if (kTwo<KIND>) {
             s.sx += __shfl_xor_sync(0xffffffffu, s.sx, m);
-            s.cross += __shfl_xor_sync(0xffffffffu, s.cross, m);
             s.off += __shfl_xor_sync(0xffffffffu, s.off, m);
         }
     }
@@ -339,7 +355,7 @@ struct RowGrad {
 template <Kind KIND, bool SAFE>
 __device__ __forceinline__ Two grad_two(Two z, Two x, const RowGrad& g) {
     const Two l2e = two(kLog2e, kLog2e), p = ex2_2(fma2(z, l2e, two(-g.U, -g.U)));
-    if constexpr (KIND == kSampled) return mul2(p, two(g.c, g.c));
+    if constexpr (!kTwo<KIND>) return mul2(p, two(g.c, g.c));
     if constexpr (KIND == kReverse) {
         const Two q = ex2_2(fma2(x, l2e, two(-g.W, -g.W)));
         return fma2(p, two(g.c2, g.c2), mul2(q, two(-g.k, -g.k)));
@@ -383,7 +399,7 @@ template <Kind KIND>
 __device__ __forceinline__ int row_scalars(const PolicyArgs& A, int64_t t, const State& row, int a, float za, float xa,
                                            float c0, float kc, float old, float ref, bool writes, RowGrad& g) {
     const bool sums = row.sz > 0.f && isfinite(row.sz) && isfinite(row.mz);
-    const LogShare share = less_log(za, row.mz, row.U, row.sz);
+    const LogShare share = log_share<KIND>(za, row);
     const float logp = share.value();
     float KL = 0.f, apart = 0.f, logq = 0.f;                                      // apart = lse_z - lse_x
     g.a = a;
@@ -391,7 +407,7 @@ __device__ __forceinline__ int row_scalars(const PolicyArgs& A, int64_t t, const
     g.U = row.U + log2f(row.sz);
     g.W = 0.f;
     float slope = 0.f;                                                            // of the sampled estimators, in logp
-    if constexpr (KIND != kSampled) {
+    if constexpr (kTwo<KIND>) {
         const float off = isfinite(row.off) ? row.off : row.sx - row.sz;
         const float ratio = row.U == row.W && fabsf(off) < 0.5f * row.sx ? log1pf(-off / row.sx) : kLn2 * log2f(row.sz / row.sx);
         apart = fabsf(row.U) < 1e6f && fabsf(row.W) < 1e6f
@@ -424,12 +440,12 @@ __device__ __forceinline__ int row_scalars(const PolicyArgs& A, int64_t t, const
         surrogate = -c0 * capped;
         if (live) g.c = c0 * ratio;
     }
-    if (kc != 0.f && KIND == kSampled) g.c -= kc * slope;
+    if (kc != 0.f && !kTwo<KIND>) g.c -= kc * slope;
     const float loss = kc != 0.f ? fmaf(kc, KL, surrogate) : surrogate;
     const bool defined = isfinite(logp) && sums, estimated = defined && isfinite(KL);   // the log-prob; the KL (0 if there is none)
     const bool carries = c0 != 0.f || kc != 0.f;
     // a NaN ratio is lost in the clip; one that is infinite, or a coefficient that is no number, shows in what it makes
-    const bool undefined = carries && (!(KIND == kSampled ? defined : estimated) || (c0 != 0.f && isnan(ratio)) || !isfinite(loss) ||
+    const bool undefined = carries && (!(!kTwo<KIND> ? defined : estimated) || (c0 != 0.f && isnan(ratio)) || !isfinite(loss) ||
                                        !isfinite(g.c));
     if (writes) {
         const float nan = __int_as_float(0x7fc00000);
@@ -479,7 +495,7 @@ struct Shared {
 
 template <Kind KIND, int THREADS>
 struct Cta {
-    static constexpr int kOps = KIND == kSampled ? 1 : 2;
+    static constexpr int kOps = !kTwo<KIND> ? 1 : 2;
     static constexpr int kWide = 4 / kOps;             // vectors of each operand that a thread has in flight
     static constexpr int kStep = kWide * THREADS;      // vectors of a step of the CTA
     const PolicyArgs& A;
@@ -495,7 +511,7 @@ struct Cta {
         const uint32_t bytes = uint32_t(kept) * 16u;
         mbar_expect_tx(&sh.landed, kOps * bytes);
         bulk_in(const_cast<uint4*>(sz), reinterpret_cast<const uint4*>(A.z + t * A.ldz) + begin, bytes, &sh.landed, once);
-        if (KIND != kSampled)
+        if (kTwo<KIND>)
             bulk_in(const_cast<uint4*>(sx), reinterpret_cast<const uint4*>(A.x + t * A.ldx) + begin, bytes, &sh.landed, once);
     }
 
@@ -509,7 +525,7 @@ struct Cta {
 #pragma unroll
             for (int k = 0; k < kWide; ++k) {
                 z[k] = ld_policy(gz + v + k * THREADS, pol);
-                if constexpr (KIND != kSampled) x[k] = ld_policy(gx + v + k * THREADS, pol);
+                if constexpr (kTwo<KIND>) x[k] = ld_policy(gx + v + k * THREADS, pol);
                 else x[k] = z[k];
             }
 #pragma unroll
@@ -518,13 +534,13 @@ struct Cta {
         for (; v < n; v += THREADS) {
             const uint4 z = ld_policy(gz + v, pol);
             uint4 x = z;
-            if constexpr (KIND != kSampled) x = ld_policy(gx + v, pol);
+            if constexpr (kTwo<KIND>) x = ld_policy(gx + v, pol);
             f(z, x, v);
         }
     }
     __device__ __forceinline__ State fold_row(int64_t t, bool& careful) {
         const int tid = threadIdx.x;
-        const acrl_bf16 *zr = A.z + t * A.ldz, *xr = KIND == kSampled ? zr : A.x + t * A.ldx;
+        const acrl_bf16 *zr = A.z + t * A.ldz, *xr = !kTwo<KIND> ? zr : A.x + t * A.ldx;
         const uint4 *gz = reinterpret_cast<const uint4*>(zr) + begin, *gx = reinterpret_cast<const uint4*>(xr) + begin;
         // the columns beyond the whole vectors, one a thread: a vector whose other columns are both operands' lowest
         // number, which add nothing
@@ -533,7 +549,7 @@ struct Cta {
         uint4 oz = make_uint4(low, low, low, low), ox = oz;
         if (odd) {
             oz.x = 0xff7f0000u | zr[(A.V & ~7) + tid];
-            ox.x = KIND == kSampled ? oz.x : 0xff7f0000u | xr[(A.V & ~7) + tid];
+            ox.x = !kTwo<KIND> ? oz.x : 0xff7f0000u | xr[(A.V & ~7) + tid];
         }
         const uint64_t again = policy_evict_last();
         Quick<KIND> q;
@@ -546,7 +562,7 @@ struct Cta {
         if (kept + (tid & ~31) < n) {
             const int at = min(kept + tid, n - 1);
             const uint4 z = __ldg(gz + at);
-            first_of(z, KIND == kSampled ? z : __ldg(gx + at));
+            first_of(z, !kTwo<KIND> ? z : __ldg(gx + at));
             rest(gz, gx, again, [&](const uint4& z, const uint4& x, int) {
                 const uint4 a[1] = {z}, b[1] = {x};
                 q.fold(a, b);
@@ -575,7 +591,7 @@ struct Cta {
         }
         __syncwarp();
         State st = q.state();
-        const bool small = st.sz < kQuickMost && (KIND == kSampled || (st.sx < kQuickMost && fabsf(st.cross) < kQuickMost));
+        const bool small = st.sz < kQuickMost && (!kTwo<KIND> || (st.sx < kQuickMost && fabsf(st.cross) < kQuickMost));
         careful = __any_sync(0xffffffffu, !small);     // (a NaN is not below the bound)
         if (careful) {          // once more, from where the vectors are now
             st = empty_state();
@@ -605,7 +621,7 @@ struct Cta {
     }
     template <bool SAFE>
     __device__ __forceinline__ void write_rest(int64_t t, uint4* out, acrl_bf16* gr, const RowGrad& g, int rel0) const {
-        const acrl_bf16 *zr = A.z + t * A.ldz, *xr = KIND == kSampled ? zr : A.x + t * A.ldx;
+        const acrl_bf16 *zr = A.z + t * A.ldz, *xr = !kTwo<KIND> ? zr : A.x + t * A.ldx;
         const uint4 *gz = reinterpret_cast<const uint4*>(zr) + begin, *gx = reinterpret_cast<const uint4*>(xr) + begin;
         auto f = [&](const uint4& z, const uint4& x, int v) {
             st_stream(out + v, grad_vec8<KIND, SAFE>(z, x, g, rel0 - (v << 3)));
@@ -613,7 +629,7 @@ struct Cta {
         rest(gz, gx, policy_evict_first(), f);
         if (last && threadIdx.x < (A.V & 7)) {
             const int j = (A.V & ~7) + int(threadIdx.x);
-            const float z = bf16_to_float(zr[j]), x = KIND == kSampled ? 0.f : bf16_to_float(xr[j]);
+            const float z = bf16_to_float(zr[j]), x = !kTwo<KIND> ? 0.f : bf16_to_float(xr[j]);
             float v, none;
             split(grad_two<KIND, SAFE>(two(z, z), two(x, x), g), v, none);
             gr[j] = acrl_bf16(pack_bf16x2(j == g.a ? g.target : v, 0.f) & 0xffffu);
@@ -668,7 +684,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) policy_kernel(const __grid_co
         if (lane >= 2) {
             const float* p = lane == 2 ? A.coef : lane == 3 ? A.kl_coef : lane == 4 ? A.old_logp : A.ref_logp;
             if (p) mine = p[t];
-        } else if (lane == 0 || KIND != kSampled) {
+        } else if (lane == 0 || kTwo<KIND>) {
             mine = bf16_to_float(lane == 0 ? A.z[t * A.ldz + a] : A.x[t * A.ldx + a]);
         }
     }
@@ -740,7 +756,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_kernel(const __g
     __shared__ __align__(16) Shared<THREADS> sh;
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     const int64_t t = blockIdx.x;
-    Cta<kSampled, THREADS> cta{A, sh, nullptr, nullptr, 0, A.V >> 3, 0, true};
+    Cta<kMean, THREADS> cta{A, sh, nullptr, nullptr, 0, A.V >> 3, 0, true};
     grid_begin();
     const bool masked = A.mask && A.mask[t] == 0;
     if (masked) {
@@ -757,10 +773,10 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logp_kernel(const __g
         __syncthreads();
         if (wid != 0) return;
         const State none = empty_state();
-        st = meet<kSampled, 32>(lane < kWarps ? get(sh.warps[lane]) : none);
+        st = meet<kMean, 32>(lane < kWarps ? get(sh.warps[lane]) : none);
     }
     if (tid != 0) return;
-    const float l = -less_log(0.f, st.mz, st.U, st.sz).value(), lp = in ? less_log(za, st.mz, st.U, st.sz).value() : 0.f;
+    const float l = -log_share<kMean>(0.f, st).value(), lp = in ? log_share<kMean>(za, st).value() : 0.f;
     if (!in) raise_flag(A.flags, ACRL_FLAG_BAD_ID);
     const bool fine = isfinite(l) && isfinite(lp);
     if (!fine) raise_flag(A.flags, ACRL_FLAG_NONFINITE);
@@ -786,12 +802,12 @@ void stagger(PolicyArgs& A, int64_t bytes_moved, int per_sm) {
 
 template <Kind KIND, int THREADS, int PER_SM>
 acrl_status launch_rows(PolicyArgs A, int ctas, cudaStream_t s) {
-    constexpr int kVec = KIND == kSampled ? 16 : 32;       // bytes of a vector of all operands
+    constexpr int kVec = !kTwo<KIND> ? 16 : 32;       // bytes of a vector of all operands
     const int nvec = A.V >> 3, slice = (nvec + ctas - 1) / ctas;
     constexpr int room = kSmBytes / PER_SM - 1024 - int(sizeof(Shared<THREADS>));   // the system takes 1 KB of each CTA's
     // whole steps of the CTA, where not all of it
     A.keep = slice <= room / kVec ? slice : room / kVec / (2 * THREADS) * (2 * THREADS);
-    if (A.keep < slice && ctas == 1) stagger(A, int64_t(nvec) * (KIND == kSampled ? 32 : 48), PER_SM);
+    if (A.keep < slice && ctas == 1) stagger(A, int64_t(nvec) * (!kTwo<KIND> ? 32 : 48), PER_SM);
     auto* kernel = policy_kernel<KIND, THREADS, PER_SM>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, room) != cudaSuccess) return launch_status();
     const int64_t T = A.T, most = kMaxGrid / ctas;
@@ -820,7 +836,7 @@ acrl_status launch_rows(PolicyArgs A, int ctas, cudaStream_t s) {
 
 template <Kind KIND>
 acrl_status launch_policy(const PolicyArgs& A, cudaStream_t s) {
-    const int64_t bytes = int64_t(A.V >> 3) * (KIND == kSampled ? 16 : 32);    // of a row
+    const int64_t bytes = int64_t(A.V >> 3) * (!kTwo<KIND> ? 16 : 32);    // of a row
     // Few rows: several CTAs each, of 16 KB or more.  V = 151,936 over the vocabulary, 1 / 2 / 4 / 8 CTAs a row: 19 rows
     // 27.3 / 19.1 / 15.1 / 15.4 us, 76 rows 27.9 / 21.2 / 29.0 / 31.0, 152 rows 33.5 / 35.7 / 50.9 / 55.9.
     int ctas = 1;
@@ -844,7 +860,7 @@ acrl_status launch_policy(const PolicyArgs& A, cudaStream_t s) {
     if (slice <= 20 * 1024) return launch_rows<KIND, 64, 13>(A, ctas, s);
     if (slice <= 48 * 1024) return launch_rows<KIND, 128, 5>(A, ctas, s);
     if (slice <= 84 * 1024) return launch_rows<KIND, 256, 3>(A, ctas, s);
-    if (KIND == kSampled || slice <= 340 * 1024) return launch_rows<KIND, 512, 2>(A, ctas, s);
+    if (!kTwo<KIND> || slice <= 340 * 1024) return launch_rows<KIND, 512, 2>(A, ctas, s);
     return launch_rows<KIND, 1024, 1>(A, ctas, s);
 }
 

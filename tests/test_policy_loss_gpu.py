@@ -460,3 +460,22 @@ def test_autograd_node_again_and_again():
     assert torch.equal(y.grad, first + first)
     loss_again = _run(dict(i, z=y.detach(), V=80)).grad
     assert torch.equal(first, loss_again)
+
+
+@pytest.mark.parametrize("kl", ["exact", "reverse", "k3", None])
+@pytest.mark.parametrize("height", [0.0, 20.0, -20.0])
+def test_log_probs_add_up(kl, height):
+    """The log-probs' errors, below 4e-6 + 2e-7 |logp| each, have signs that mix: 6 standard deviations of a sum of 2,000 errors of
+    fp32's spacing at 16, wherever the logits stand.  (A common part of 1e-7 would make 2.0e-4.)"""
+    T, V = 2000, 4096
+    i = _inputs(T, V, 21, kl)
+    z = i["z"].float() + height
+    z[:, ::61] += 4.0
+    i["z"], i["mask"] = z.to(torch.bfloat16), None
+    lp = torch.log_softmax(i["z"].double(), 1).gather(1, i["ids"].long()[:, None])[:, 0]
+    i["old"] = lp.float()
+    if i["ref_logits"] is not None:
+        i["ref_logits"] = (i["z"].float() + 0.4 * torch.randn(z.shape, generator=torch.Generator(device=DEV).manual_seed(3), device=DEV)).to(torch.bfloat16)
+    error = _run(i).logp.double() - lp
+    assert bool((error.abs() <= 4e-6 + 2e-7 * lp.abs()).all())
+    assert abs(float(error.sum())) <= 6 * 1e-6 * math.sqrt(T) / 2
