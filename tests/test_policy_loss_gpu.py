@@ -479,3 +479,26 @@ def test_log_probs_add_up(kl, height):
     error = _run(i).logp.double() - lp
     assert bool((error.abs() <= 4e-6 + 2e-7 * lp.abs()).all())
     assert abs(float(error.sum())) <= 6 * 1e-6 * math.sqrt(T) / 2
+
+
+@pytest.mark.parametrize("kl", ["exact", "reverse", "k3", None])
+@pytest.mark.parametrize("T,V", [(2000, 4096), (1500, 32000), (300, 151936)])
+@pytest.mark.parametrize("rest", [0.1, 1e-2, 1e-3, 1e-5])
+def test_log_probs_of_likely_tokens(kl, T, V, rest):
+    """Rows whose sampled column has nearly all of the probability.  The log-probs' errors have a spread of up to 5e-7 (the largest
+    column's exponent, of up to 32, is rounded at 2^-24 of it: 1e-6 / sqrt(3) / 2 and the sums'), of which 6 standard deviations of
+    the mean are allowed; in common they have what the exponential's have (ex2.approx: 5e-8 on average) and the sums'
+    roundings, 1.5e-7 together."""
+    i = _inputs(T, V, 22, kl)
+    g = torch.Generator(device=DEV).manual_seed(7)
+    z = 2.5 * torch.randn((T, V), generator=g, device=DEV)
+    z[torch.arange(T), i["ids"].long()] = torch.logsumexp(z, 1) - math.log(rest) + torch.rand(T, generator=g, device=DEV)
+    i["z"], i["mask"] = z.to(torch.bfloat16), None
+    lp = torch.cat([torch.log_softmax(part.double(), 1).gather(1, ids.long()[:, None])[:, 0]
+                    for part, ids in zip(i["z"].split(100), i["ids"].split(100))])
+    i["old"] = lp.float()
+    if i["ref_logits"] is not None:
+        i["ref_logits"] = (i["z"].float() + 0.4 * torch.randn(z.shape, generator=g, device=DEV)).to(torch.bfloat16)
+    error = _run(i).logp.double() - lp
+    assert bool((error.abs() <= 4e-6 + 2e-7 * lp.abs()).all())
+    assert abs(float(error.mean())) <= 1.5e-7 + 6 * 5e-7 / math.sqrt(T)

@@ -293,3 +293,21 @@ def test_token_logp():
     for bad in (dict(ids=ids.long()), dict(ids=ids[:3]), dict(mask=mask.bool()), dict(logits=z.float()), dict(V=5009), dict(logp=ids)):
         with pytest.raises(acrl.AcrlError):
             api.token_logp(**{**dict(logits=z, ids=ids, mask=mask, V=V), **bad})
+
+
+@pytest.mark.parametrize("T,V", [(2000, 4096), (1500, 32000), (300, 151936)])
+@pytest.mark.parametrize("rest", [0.1, 1e-2, 1e-3, 1e-5])
+def test_log_probs_of_likely_tokens(T, V, rest):
+    """Rows whose sampled column has nearly all of the probability, as for the policy loss: a spread of up to 5e-7, and in common
+    the exponential's mean error (5e-8) and the sums' roundings, 1.5e-7 together."""
+    g = torch.Generator(device=DEV).manual_seed(8)
+    z = 2.5 * torch.randn((T, V), generator=g, device=DEV)
+    ids = torch.randint(0, V, (T,), generator=g, device=DEV, dtype=torch.int32)
+    z[torch.arange(T), ids.long()] = torch.logsumexp(z, 1) - math.log(rest) + torch.rand(T, generator=g, device=DEV)
+    z = z.to(torch.bfloat16)
+    lse = torch.cat([torch.logsumexp(part.double(), 1) for part in z.split(100)])
+    lp = z.gather(1, ids.long()[:, None])[:, 0].double() - lse
+    got = api.token_logp(z, ids)
+    for a, b in zip(got, (lse, lp)):
+        assert bool(((a - b).abs() <= 4e-6 + 2e-7 * b.abs()).all())
+    assert abs(float((got[1] - lp).mean())) <= 1.5e-7 + 6 * 5e-7 / math.sqrt(T)
