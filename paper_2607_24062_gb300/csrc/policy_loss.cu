@@ -225,7 +225,12 @@ __device__ __forceinline__ void fold(State& st, const uint4 (&z)[N], const uint4
 // sum below 2^109; and a factor that is flushed to 0, below 2^-126, has taken less than 2^-49 from a sum that is 2^-16 or more.
 // Where the careful way is not needed both give the same cross sum's terms; the careful way costs nearly half as much again.
 constexpr float kQuickMost = 0x1p64f;
-template <Kind KIND>
+// BY_VECTORS: a vector's columns are added up by themselves before they meet the lane's sum.  One by one beside a sum that holds a
+// column far above them, small ones are lost, all in one direction: rows of 151,936 whose likeliest token has 0.9 had log-probs
+// 5.7e-7 (256 threads) or 2.1e-7 (512) too high on average, 3e-8 and 6e-8 too low so.  In the statistics at no cost; from
+// log-probs with 256 threads or more (2,632 x 151,936 319 us against 324, but 146,000 x 2,048 in CTAs of 32 216 against 207, where
+// a lane adds up few columns); with KL over the vocabulary registers are short (2,632 x 151,936 485 against 475).
+template <Kind KIND, bool BY_VECTORS>
 struct Quick {
     float mz, mx;
     Two nU, nW, sz, sx, cr;
@@ -258,18 +263,15 @@ struct Quick {
             for (int j = 0; j < 4; ++j) {
                 const Two a = widen(zw[j]);
                 e[j] = ex2_2(fma2(a, l2e, nU));
+                if constexpr (!BY_VECTORS) sz = add2(sz, e[j]);
                 if constexpr (KIND == kMean) cr = fma2(e[j], a, cr);     // NaN beside a column at -infinity: log_share() looks
-                else sz = add2(sz, e[j]);
                 if constexpr (kTwo<KIND>) {
                     const Two b = widen(xw[j]), h = ex2_2(fma2(b, l2e, nW));
                     sx = add2(sx, h);
                     cr = KIND == kExact ? fma2(e[j], fma2(b, minus, a), cr) : fma2(h, fma2(a, minus, b), cr);
                 }
             }
-            // a vector's columns by themselves first: one by one beside a sum that holds a column far above them, small ones would
-            // be lost, and all in one direction (rows of 151,936 whose likeliest token has 0.9: log-probs 5.7e-7 too high on average,
-            // so 3e-8 too low; the same time)
-            if constexpr (KIND == kMean) sz = add2(sz, add2(add2(e[0], e[1]), add2(e[2], e[3])));
+            if constexpr (BY_VECTORS) sz = add2(sz, add2(add2(e[0], e[1]), add2(e[2], e[3])));
         }
     }
     __device__ __forceinline__ State state() const {
@@ -558,7 +560,7 @@ struct Cta {
             ox.x = !kTwo<KIND> ? oz.x : 0xff7f0000u | xr[(A.V & ~7) + tid];
         }
         const uint64_t again = policy_evict_last();
-        Quick<KIND> q;
+        Quick<KIND, KIND == kMean || (KIND == kSampled && THREADS >= 256)> q;
         bool started = false;
         auto first_of = [&](const uint4& z, const uint4& x) {
             if (!started) q.start(z, x);
