@@ -717,9 +717,9 @@ acrl_status acrl_policy_loss_grad_logits(const acrl_bf16* logits, int64_t T, int
 
 /*
  * acrl_token_logp -- lse and logp of acrl_token_stats on the same arguments (no
- * entropy; dev_flags may be NULL), from sums without a bias: the log-probs of a
- * response add up in a log ratio, here and on the policy's side (acrl_preference_step
- * takes the same), and with them what their errors have in common.
+ * entropy; dev_flags may be NULL), with less in common among the errors: the
+ * log-probs of a response add up in a log ratio, and with them what their errors have
+ * in common.  acrl_preference_step takes the same on the policy's side.
  */
 acrl_status acrl_token_logp(const acrl_bf16* logits, int64_t T, int64_t V, int64_t ld, const int32_t* ids,
                             const uint8_t* mask, float* lse, float* logp, int32_t* dev_flags, acrl_stream stream);
@@ -748,7 +748,8 @@ typedef enum {
  *   coef    device float [T] output;  loss  device float [1] output.
  *   workspace  device, 16-byte aligned, acrl_preference_workspace_bytes(S, Gn) bytes.
  * A D_i that is not finite, or a NaN reward, raises NONFINITE; the former makes the
- * loss and the coefficients of its prompt's pairs NaN.  Fixed order, fp64 sums.
+ * loss and the coefficients of its prompt's pairs NaN.  Fixed order; a thread's tokens
+ * in a compensated fp32 sum, what meets beyond it in fp64.
  */
 int64_t     acrl_preference_workspace_bytes(int32_t S, int32_t Gn);
 acrl_status acrl_preference_loss(const float* logp, const float* ref_logp, const uint8_t* mask, int64_t T,

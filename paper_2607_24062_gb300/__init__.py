@@ -19,7 +19,7 @@ from ._abi import (AGG_SEQ_MEAN_TOKEN_MEAN, AGG_TOKEN_MEAN, FLAG_BAD_ID, FLAG_BA
                    MODE_TIS, SINGLETON_MEAN0_STD1, SINGLETON_ZERO, Y_BATCH, Y_GROUP, Y_SEQUENCE, AcrlError, Params)
 from .api import (Fp8Tensor, controller_init, controller_step, fp8_linear, fp8_linear_backward,  # noqa: F401
                   fp8_matmul, fp8_quantize, grpo_advantage, loss_grad_logits, policy_loss_grad_logits, preference_loss,
-                  read_flags, read_state, reduce_loss, seq_discrepancy, token_stats)
+                  read_flags, read_state, reduce_loss, seq_discrepancy, token_logp, token_stats)
 from .pipeline import AcrlStep, Fp8Head, HostPipeline, PreferenceStep, Weights, importance_weights  # noqa: F401
 from .autograd import acrl_loss, fp8_layer, pairs_loss, policy_loss  # noqa: F401
 

@@ -1,7 +1,8 @@
-// The product of one row, a token, with an 8-bit matrix: every byte of the matrix is used once, so HBM bounds it, and
-// at the sizes of one layer the latency of a launch.  No tensor cores: their pipeline's start and end (tensor memory,
-// barriers, the split of the sum) and the launch that quantises the row take longer than a small product: 1,024 x 1,024 3.3 us
-// against 6.6, 4,096 x 4,096 9.3 against 9.1, and 16 against 25 as a call; from there on the tensor cores' way is faster (8,192 x
+// The product of one row, a token, with an 8-bit matrix: every byte of the matrix is used once, so HBM would bound it; at the
+// sizes of one layer the latency of a launch and of a warp's loads does (of 9.0 us at 4,096 x 4,096 some 6.4 bring 15.7 MB, 2.5 TB/s: a
+// lane has four loads of 16 bytes in flight, and 4,096 columns are four round trips one after another).  No tensor cores: their pipeline's start and end (tensor memory,
+// barriers, the split of the sum) and the launch that quantises the row take longer than a small product: 1,024 x 1,024 2.6 us
+// against 6.6, 4,096 x 4,096 9.0 against 9.1, and 16 against 25 as a call; from there on the tensor cores' way is faster (8,192 x
 // 4,096 14.7 against 11.5).  A warp takes kW rows of the matrix at a time: each lane loads 16 bytes of each,
 // 512 columns a step, two steps ahead, converts them to fp32 through half precision (exact for both formats) and multiplies
 // them with the row, whose 8-bit numbers lie in shared memory as fp32; the 16 products' sum takes both blocks' scales at once, as

@@ -64,8 +64,9 @@ __global__ void __launch_bounds__(kRespThreads)
         if (!ok) raise_flag(flags, ACRL_FLAG_BAD_OFFSETS);
         if (i == 0) *w.prompts = 0;
     }
-    // Differences and sums exactly, in two fp32 numbers a thread, then in fp64 (with rounded differences a sum near 0 had lost three
-    // digits; with fp64 a token, 2 a cycle and SM, the kernel took 14 us at 512 x 2,048).  Four tokens a thread in flight.
+    // Compensated sums: every difference and addition exactly, as a rounded number and what the rounding left, which is added up by
+    // itself (in fp32, its own roundings 2^-24 of what was left); then in fp64.  With rounded differences a sum near 0 had lost three
+    // digits; with fp64 a token, 2 a cycle and SM, the kernel took 14 us at 512 x 2,048.  Four tokens a thread in flight.
     float high = 0.f, low = 0.f;
     int n = 0;
     for (int64_t t0 = lo + threadIdx.x; t0 < hi; t0 += 4 * kRespThreads) {
