@@ -653,6 +653,94 @@ acrl_status acrl_fp8_linear_backward(const acrl_bf16* dy, int64_t M, int64_t N, 
                                      void* workspace, int64_t workspace_bytes, int32_t* dev_flags, acrl_stream stream);
 
 /* ------------------------------------------------------------------------
+ * A linear layer in bf16, the training engine's type (Sec. 5.1), its gradients,
+ * and the update of its weight.  Matrices are row-major, 16-byte aligned, with a
+ * row stride that is a multiple of 8 elements; sizes below 2^31 - 512.  x, w, dy,
+ * pre and the outputs are device memory of the current device, as for the LM
+ * head.  dev_flags may be NULL.  Waits are time-bounded (ACRL_FLAG_TIMEOUT: the
+ * outputs are invalid).  Nothing is written beyond an output's columns.
+ */
+typedef enum {
+    ACRL_ACT_NONE = 0,
+    ACRL_ACT_RELU = 1,        /* max(u, 0)                                                  */
+    ACRL_ACT_GELU = 2,        /* u Phi(u), Phi the normal distribution                      */
+    ACRL_ACT_GELU_TANH = 3,   /* u (1 + tanh(sqrt(2 / pi) (u + 0.044715 u^3))) / 2          */
+    ACRL_ACT_SILU = 4         /* u / (1 + e^-u)                                             */
+} acrl_activation;
+
+/*
+ * acrl_linear -- out = f(u) + residual, u = x W^T + bias: the product of bf16
+ * matrices on the tensor cores, summed in fp32, and what follows it in its
+ * epilogue, rounded once.
+ *   x     device bf16 [M, ldx], K columns;  w  device bf16 [N, ldw], K columns.
+ *   bias  device float or bf16 [N] (of its own alignment), or NULL.
+ *   residual  device bf16 or float [M, ldr], or NULL; it may be `out` itself, of
+ *         the same type and stride.
+ *   pre   device bf16 [M, ldp] or NULL: u, rounded, for acrl_linear_backward.
+ *   out   device bf16 or float [M, ldo].
+ *   workspace  device, 16-byte aligned, acrl_linear_workspace_bytes(M, N, K)
+ *         bytes (0, and NULL, where the sum is not split); calls that overlap need
+ *         one each.
+ * K = 0: u = bias.
+ */
+int64_t     acrl_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
+acrl_status acrl_linear(const acrl_bf16* x, int64_t M, int64_t K, int64_t ldx, const acrl_bf16* w, int64_t N, int64_t ldw,
+                        const void* bias, acrl_dtype bias_dtype, acrl_activation act, const void* residual,
+                        acrl_dtype residual_dtype, int64_t ldr, acrl_bf16* pre, int64_t ldp, void* out,
+                        acrl_dtype out_dtype, int64_t ldo, void* workspace, int64_t workspace_bytes, int32_t* dev_flags,
+                        acrl_stream stream);
+
+/*
+ * acrl_linear_backward -- the gradients of acrl_linear, with g = dy f'(u):
+ *     dx = g W,   dw = g^T x,   dbias = sum over the rows of g
+ * (that of the residual is dy itself).  f' is computed in fp32 from u as it was
+ * kept in bf16; the products take g rounded to bf16, the type of dy, and dbias adds
+ * g up in fp32 before that rounding.  f'(0) of RELU is 0.
+ *   dy    device bf16 [M, lddy], N columns;  x, w  as above.
+ *   pre   device bf16 [M, ldp]: u; NULL with ACRL_ACT_NONE.
+ *   dx    device bf16 or float [M, lddx], or NULL;  dw  device bf16 or float
+ *         [N, lddw], or NULL;  dbias  device float [N], or NULL.  What is NULL is not
+ *         computed.
+ *   workspace  device, 16-byte aligned, acrl_linear_backward_workspace_bytes(M,
+ *         N, K) bytes.
+ * Fixed order: equal inputs give equal outputs.
+ */
+int64_t     acrl_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K);
+acrl_status acrl_linear_backward(const acrl_bf16* dy, int64_t M, int64_t N, int64_t lddy, const acrl_bf16* x, int64_t K,
+                                 int64_t ldx, const acrl_bf16* w, int64_t ldw, acrl_activation act, const acrl_bf16* pre,
+                                 int64_t ldp, void* dx, acrl_dtype dx_dtype, int64_t lddx, void* dw, acrl_dtype dw_dtype,
+                                 int64_t lddw, float* dbias, void* workspace, int64_t workspace_bytes, int32_t* dev_flags,
+                                 acrl_stream stream);
+
+/*
+ * acrl_orthogonalize -- an update (a weight's gradient or its momentum) with its
+ * singular values brought near one by Newton-Schulz steps:
+ *     X_0 = G / (|G| + eps)   (|G| the Frobenius norm),
+ *     X_k = a_k X + b_k (X X^T) X + c_k (X X^T)^2 X,   X = X_(k-1),
+ *     out = scale X_steps,
+ * each singular value s of X going to a s + b s^3 + c s^5.  (Of a tall matrix
+ * the transpose is taken, and turned back; the result is the same.)  Every operand
+ * of a product is held as two bf16 numbers, to 2^-16 of it, and each product as three
+ * of theirs: in bf16 alone the roundings of a gradient's few strong directions would
+ * drown the weak ones, which the steps amplify by up to a^steps.
+ *   g     device bf16 or float: `batch` matrices of m x n, rows at a stride of ldg
+ *         (a multiple of 8 for bf16, 4 for float; 16-byte aligned), matrices at a
+ *         stride of g_stride elements (likewise).
+ *   coeffs  host float [3 steps]: a, b, c of each step.  1 <= steps <= 64.
+ *   eps >= 0.  A matrix of zeros gives zeros, eps = 0 included.
+ *   out   device bf16, rows at ldo, matrices at out_stride; it may be g.
+ *   workspace  device, 16-byte aligned, acrl_orthogonalize_workspace_bytes(batch,
+ *         m, n) bytes.
+ * A matrix with an infinity or a NaN is NaN throughout and raises NONFINITE; the
+ * others of the batch are not touched by it.
+ */
+int64_t     acrl_orthogonalize_workspace_bytes(int64_t batch, int64_t m, int64_t n);
+acrl_status acrl_orthogonalize(const void* g, acrl_dtype g_dtype, int64_t batch, int64_t m, int64_t n, int64_t ldg,
+                               int64_t g_stride, const float* coeffs, int32_t steps, float eps, float scale, acrl_bf16* out,
+                               int64_t ldo, int64_t out_stride, void* workspace, int64_t workspace_bytes,
+                               int32_t* dev_flags, acrl_stream stream);
+
+/* ------------------------------------------------------------------------
  * Losses with a reference policy.
  */
 

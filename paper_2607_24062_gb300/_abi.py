@@ -28,6 +28,7 @@ SINGLETON_MEAN0_STD1, SINGLETON_ZERO = 0, 1
 BF16, F32 = 0, 1
 FP8_E4M3, FP8_E5M2 = 0, 1
 FP8_ROW, FP8_TILE = 0, 1
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4
 KL_NONE, KL_K1, KL_K2, KL_K3, KL_EXACT, KL_REVERSE = 0, 1, 2, 3, 4, 5
 PREF_SIGMOID, PREF_HINGE, PREF_IPO = 0, 1, 2
 
@@ -107,6 +108,15 @@ SIGNATURES = {
     "acrl_fp8_linear_backward_workspace_bytes": (c_i64, [c_i64, c_i64, c_i64]),
     "acrl_fp8_linear_backward": (c_i32, [c_p, c_i64, c_i64, c_i64, c_i32, c_p, c_i64, c_i64, c_i32, c_p, c_i64, c_i32, c_p,
                                          c_i64, c_i32, c_p, c_i32, c_i64, c_p, c_i32, c_i64, c_p, c_i64, c_p, c_p]),
+    "acrl_linear_workspace_bytes": (c_i64, [c_i64, c_i64, c_i64]),
+    "acrl_linear": (c_i32, [c_p, c_i64, c_i64, c_i64, c_p, c_i64, c_i64, c_p, c_i32, c_i32, c_p, c_i32, c_i64, c_p, c_i64, c_p,
+                            c_i32, c_i64, c_p, c_i64, c_p, c_p]),
+    "acrl_linear_backward_workspace_bytes": (c_i64, [c_i64, c_i64, c_i64]),
+    "acrl_linear_backward": (c_i32, [c_p, c_i64, c_i64, c_i64, c_p, c_i64, c_i64, c_p, c_i64, c_i32, c_p, c_i64, c_p, c_i32,
+                                     c_i64, c_p, c_i32, c_i64, c_p, c_p, c_i64, c_p, c_p]),
+    "acrl_orthogonalize_workspace_bytes": (c_i64, [c_i64, c_i64, c_i64]),
+    "acrl_orthogonalize": (c_i32, [c_p, c_i32, c_i64, c_i64, c_i64, c_i64, c_i64, c_p, c_i32, c_f32, c_f32, c_p, c_i64, c_i64,
+                                   c_p, c_i64, c_p, c_p]),
     "acrl_policy_loss_grad_logits": (c_i32, [c_p, c_i64, c_i64, c_i64, c_p, c_p, c_p, c_p, c_f32, c_f32, c_f32, c_i32,
                                              c_p, c_p, c_i64, c_p, c_p, c_p, c_p, c_p, c_p, c_p, c_p]),
     "acrl_token_logp": (c_i32, [c_p, c_i64, c_i64, c_i64, c_p, c_p, c_p, c_p, c_p, c_p]),

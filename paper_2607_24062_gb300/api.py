@@ -685,6 +685,161 @@ def fp8_linear_backward(dy, x, weight_t: Fp8Tensor, *, fmt="e4m3", x_fmt="e4m3",
 
 
 # ---------------------------------------------------------------------------
+# a layer in bf16, its gradients and the update of its weight
+# ---------------------------------------------------------------------------
+
+_ACT = {None: _abi.ACT_NONE, "relu": _abi.ACT_RELU, "gelu": _abi.ACT_GELU, "gelu_tanh": _abi.ACT_GELU_TANH, "silu": _abi.ACT_SILU}
+
+
+def _act(act) -> int:
+    code = _ACT.get(act)
+    if code is None:
+        raise AcrlError(f"act: {act!r}, expected one of {list(_ACT)}")
+    return code
+
+
+def _given(t, M: int, N: int, dtypes, name: str):
+    """(`t`, its row stride) of a matrix [M, N] that the caller gives, None and 0 for None."""
+    if t is None:
+        return None, 0
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or t.dim() != 2 or not t.is_cuda or \
+            (N > 1 and t.stride(1) != 1) or tuple(t.shape) != (M, N):
+        raise AcrlError(f"{name}: expected a CUDA matrix of {(M, N)}, {' or '.join(str(d) for d in dtypes)}, with unit column stride")
+    return t, t.stride(0) if M > 1 and N > 0 else (N + 7) // 8 * 8
+
+
+def _workspace(workspace, n: int, dev):
+    if workspace is not None:
+        return _need(workspace, torch.uint8, n, "workspace")
+    return torch.empty(n, dtype=torch.uint8, device=dev) if n > 0 else None
+
+
+def linear_workspace_bytes(M: int, N: int, K: int) -> int:
+    """acrl_linear_workspace_bytes."""
+    return int(lib().acrl_linear_workspace_bytes(M, N, K))
+
+
+def linear(x, weight, bias=None, *, act=None, residual=None, pre_out=None, out_dtype=torch.bfloat16, out=None, workspace=None,
+           flags=None, stream=None):
+    """acrl_linear: act(x W^T + bias) + residual as `out_dtype` [M, N].  x bf16 [M, K], weight bf16 [N, K]; bias float32 or
+    bfloat16 [N]; `act` is None, "relu", "gelu", "gelu_tanh" or "silu"; residual bfloat16 or float32 [M, N] (`out` itself is
+    allowed); `pre_out` bf16 [M, N] takes x W^T + bias, for linear_backward."""
+    (M, K), (N, Kw) = _bf16_rows(x, "x"), _bf16_rows(weight, "weight")
+    if stream is not None:
+        return _on_stream(linear, "acrl_linear", x, stream, x, weight, bias, act=act, residual=residual, pre_out=pre_out,
+                          out_dtype=out_dtype, out=out, workspace=workspace, flags=flags)
+    if Kw != K:
+        raise AcrlError(f"x and weight disagree on K: {K} and {Kw}")
+    if out_dtype not in _OUT_DTYPE:
+        raise AcrlError(f"out_dtype: {out_dtype}, expected bfloat16 or float32")
+    if bias is not None and (not isinstance(bias, torch.Tensor) or bias.dtype not in _OUT_DTYPE or tuple(bias.shape) != (N,) or
+                             not bias.is_cuda or not bias.is_contiguous()):
+        raise AcrlError(f"bias: expected a contiguous float32 or bfloat16 CUDA vector of {N}")
+    code = _act(act)
+    residual, ldr = _given(residual, M, N, (torch.bfloat16, torch.float32), "residual")
+    pre_out, ldp = _given(pre_out, M, N, (torch.bfloat16,), "pre_out")
+    out, ldo = _product_out(out, M, N, out_dtype, x.device)
+    n = lib().acrl_linear_workspace_bytes(M, N, K)
+    workspace = _workspace(workspace, n, x.device)
+    if flags is not None:
+        _need(flags, torch.int32, 1, "flags")
+    _call("acrl_linear", (x, weight, bias, residual, pre_out, out, workspace, flags), None, x.data_ptr(), M, K, _ld(x),
+          weight.data_ptr(), N, _ld(weight), None if bias is None else bias.data_ptr(),
+          0 if bias is None else _OUT_DTYPE[bias.dtype], code, None if residual is None else residual.data_ptr(),
+          0 if residual is None else _OUT_DTYPE[residual.dtype], ldr, None if pre_out is None else pre_out.data_ptr(), ldp,
+          out.data_ptr(), _OUT_DTYPE[out.dtype], ldo, None if workspace is None else workspace.data_ptr(), n,
+          None if flags is None else flags.data_ptr())
+    return out
+
+
+def linear_backward_workspace_bytes(M: int, N: int, K: int) -> int:
+    """acrl_linear_backward_workspace_bytes."""
+    return int(lib().acrl_linear_backward_workspace_bytes(M, N, K))
+
+
+def linear_backward(dy, x, weight, *, act=None, pre=None, bias=False, need_dx=True, need_dw=True, dx_dtype=torch.bfloat16,
+                    dw_dtype=torch.float32, dx=None, dw=None, dbias=None, workspace=None, flags=None, stream=None):
+    """acrl_linear_backward, the gradients of linear: with g = dy act'(pre), dx = g W, dw = g^T x and, with `bias`,
+    dbias = sum of g over the rows.  dy bf16 [M, N], x bf16 [M, K], weight bf16 [N, K], `pre` the bf16 [M, N] that linear
+    wrote.  Returns (dx [M, K], dw [N, K], dbias float32 [N]), None where not asked for; the gradient of the residual is dy."""
+    (M, N), (Mx, K) = _bf16_rows(dy, "dy"), _bf16_rows(x, "x")
+    Nw, Kw = _bf16_rows(weight, "weight")
+    if stream is not None:
+        return _on_stream(linear_backward, "acrl_linear_backward", dy, stream, dy, x, weight, act=act, pre=pre, bias=bias,
+                          need_dx=need_dx, need_dw=need_dw, dx_dtype=dx_dtype, dw_dtype=dw_dtype, dx=dx, dw=dw, dbias=dbias,
+                          workspace=workspace, flags=flags)
+    if Mx != M or (Nw, Kw) != (N, K):
+        raise AcrlError(f"dy {(M, N)}, x {(Mx, K)} and weight {(Nw, Kw)} do not belong together")
+    if dx_dtype not in _OUT_DTYPE or dw_dtype not in _OUT_DTYPE:
+        raise AcrlError("dx_dtype, dw_dtype: expected bfloat16 or float32")
+    code = _act(act)
+    if (act is None) != (pre is None):
+        raise AcrlError(f"act={act!r} takes " + ("no pre" if act is None else "pre, the pre-activation that linear wrote"))
+    if (dx is not None and not need_dx) or (dw is not None and not need_dw) or (dbias is not None and not bias):
+        raise AcrlError("dx, dw, dbias: an output that is not asked for")
+    pre, ldp = _given(pre, M, N, (torch.bfloat16,), "pre")
+    dev = dy.device
+    dx, lddx = _product_out(dx, M, K, dx_dtype, dev) if need_dx else (None, 0)
+    dw, lddw = _product_out(dw, N, K, dw_dtype, dev) if need_dw else (None, 0)
+    dbias = _vec(dbias, torch.float32, N, "dbias", dev) if bias else None
+    n = lib().acrl_linear_backward_workspace_bytes(M, N, K)
+    workspace = _workspace(workspace, n, dev)
+    if flags is not None:
+        _need(flags, torch.int32, 1, "flags")
+    _call("acrl_linear_backward", (dy, x, weight, pre, dx, dw, dbias, workspace, flags), None, dy.data_ptr(), M, N, _ld(dy),
+          x.data_ptr(), K, _ld(x), weight.data_ptr(), _ld(weight), code, _ptr(pre), ldp, _ptr(dx),
+          0 if dx is None else _OUT_DTYPE[dx.dtype], lddx, _ptr(dw), 0 if dw is None else _OUT_DTYPE[dw.dtype], lddw, _ptr(dbias),
+          _ptr(workspace), n, _ptr(flags))
+    return dx, dw, dbias
+
+
+def orthogonalize_workspace_bytes(batch: int, m: int, n: int) -> int:
+    """acrl_orthogonalize_workspace_bytes."""
+    return int(lib().acrl_orthogonalize_workspace_bytes(batch, m, n))
+
+
+def _matrices(t, name: str):
+    """(batch, m, n, row stride, matrix stride) of one matrix or a batch of them, padded strides where a size is one."""
+    to = 8 if t.dtype == torch.bfloat16 else 4
+    B, (m, n) = (t.shape[0] if t.dim() == 3 else 1), t.shape[-2:]
+    if n > 1 and t.stride(-1) != 1:
+        raise AcrlError(f"{name}: expected unit column stride")
+    ld = t.stride(-2) if m > 1 and n > 0 else (n + to - 1) // to * to
+    return B, m, n, ld, t.stride(0) if t.dim() == 3 and B > 1 else m * ld
+
+
+def orthogonalize(g, *, steps=5, coeffs=(3.4445, -4.7750, 2.0315), eps=1e-7, scale=1.0, out=None, workspace=None, flags=None,
+                  stream=None):
+    """acrl_orthogonalize: an update, bf16 or float32 [m, n] or a batch [B, m, n] of them, with its singular values brought
+    near one by `steps` Newton-Schulz steps, times `scale`; bf16 of the same shape.  `coeffs` is (a, b, c), or one such triple
+    for each step.  `out` may be g."""
+    if not isinstance(g, torch.Tensor) or g.dtype not in _OUT_DTYPE or g.dim() not in (2, 3) or not g.is_cuda:
+        raise AcrlError("g: expected a bfloat16 or float32 CUDA matrix, or a batch of them")
+    if stream is not None:
+        return _on_stream(orthogonalize, "acrl_orthogonalize", g, stream, g, steps=steps, coeffs=coeffs, eps=eps, scale=scale,
+                          out=out, workspace=workspace, flags=flags)
+    B, m, n, ldg, stride = _matrices(g, "g")
+    coeffs = np.asarray(coeffs, dtype=np.float32)
+    if not isinstance(steps, int) or coeffs.shape not in ((3,), (steps, 3)):
+        raise AcrlError("coeffs: expected three numbers, or three for each of the steps")
+    flat = (coeffs if coeffs.ndim == 2 else np.tile(coeffs, max(steps, 1))).ravel().tolist()
+    if out is None:
+        ld = (n + 7) // 8 * 8
+        out = torch.empty_strided(g.shape, ((ld, 1) if g.dim() == 2 else (m * ld, ld, 1)), dtype=torch.bfloat16, device=g.device)
+    elif not isinstance(out, torch.Tensor) or out.dtype != torch.bfloat16 or out.shape != g.shape or not out.is_cuda:
+        raise AcrlError(f"out: expected a bfloat16 CUDA tensor of {tuple(g.shape)}")
+    _, _, _, ldo, out_stride = _matrices(out, "out")
+    nbytes = lib().acrl_orthogonalize_workspace_bytes(B, m, n)
+    workspace = _workspace(workspace, nbytes, g.device)
+    if flags is not None:
+        _need(flags, torch.int32, 1, "flags")
+    _call("acrl_orthogonalize", (g, out, workspace, flags), None, g.data_ptr(), _OUT_DTYPE[g.dtype], B, m, n, ldg, stride,
+          (ctypes.c_float * len(flat))(*flat), steps, eps, scale, out.data_ptr(), ldo, out_stride, _ptr(workspace), nbytes,
+          _ptr(flags))
+    return out
+
+
+# ---------------------------------------------------------------------------
 # losses with a reference policy
 # ---------------------------------------------------------------------------
 

@@ -17,7 +17,8 @@ step object runs again.
 The losses with a reference policy work alike: `policy_loss` (the clipped loss
 with a KL term) and `pairs_loss` (a PreferenceStep) write dL/dlogits in their
 forward.  `fp8_layer` is a linear layer on 8-bit matrices, whose backward makes
-both gradients on 8-bit matrices too.
+both gradients on 8-bit matrices too; `linear_layer` one in bf16 with bias,
+activation and residual.
 """
 
 from __future__ import annotations
@@ -150,3 +151,38 @@ def fp8_layer(x: torch.Tensor, weight: torch.Tensor, grad_fmt: str = "e4m3") -> 
     """x [M, K] times the transpose of weight [N, K] (both bf16), computed on 8-bit matrices; the backward's two products
     are on 8-bit matrices as well, the incoming gradient in `grad_fmt`.  They have no derivative of their own."""
     return _Fp8Layer.apply(x, weight, grad_fmt)
+
+
+class _LinearLayer(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, residual, act):
+        w, x = _rows_of_eight(weight.detach()), _rows_of_eight(x.detach())
+        pre = None
+        if act is not None and any(ctx.needs_input_grad[:3]):
+            pre = api._padded((x.shape[0], w.shape[0]), 8, torch.bfloat16, x.device)
+        r = None if residual is None else _rows_of_eight(residual.detach())
+        y = api.linear(x, w, None if bias is None else bias.detach().contiguous(), act=act, residual=r, pre_out=pre)
+        ctx.save_for_backward(x, w, pre)
+        ctx.act = act
+        ctx.bias_dtype = None if bias is None else bias.dtype
+        ctx.residual_dtype = None if residual is None else residual.dtype
+        return y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        x, w, pre = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        dx = dw = dbias = None
+        if any(need[:3]):
+            dx, dw, dbias = api.linear_backward(_rows_of_eight(dy), x, w, act=ctx.act, pre=pre, bias=need[2], need_dx=need[0],
+                                                need_dw=need[1], dw_dtype=torch.bfloat16)
+        return dx, dw, None if dbias is None else dbias.to(ctx.bias_dtype), dy.to(ctx.residual_dtype) if need[3] else None, None
+
+
+def linear_layer(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = None, act: str | None = None,
+                 residual: torch.Tensor | None = None) -> torch.Tensor:
+    """act(x W^T + bias) + residual for autograd: x [M, K] and weight [N, K] bf16, bias [N] and residual [M, N] bf16 or
+    float32; bf16 [M, N].  With an activation the pre-activation is kept in bf16 for the backward.  The gradients have no
+    derivative of their own."""
+    return _LinearLayer.apply(x, weight, bias, residual, act)
