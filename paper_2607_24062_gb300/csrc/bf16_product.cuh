@@ -1,0 +1,544 @@
+// The tensor-core product that the bf16 layer and the orthogonalised update share: sums of bf16 products
+//
+//     acc[i, j] = sum_k p[i, k] q[j, k]
+//
+// in fp32, handed to an epilogue of the caller's.  Either operand may lie with the sum's index along its rows ([rows, K]:
+// "K-major", a layer's forward) or along its columns ([K, rows]: its gradients, which contract over rows of what they
+// read); the copies then fetch 64 x 64 blocks and the MMA takes them transposed, so nothing is turned beforehand.
+//
+// One CTA per SM, warp-specialised: warp 0 issues the TMA loads of slabs of 64 along the sum (128-byte swizzle) into a ring
+// of stages; warp 1 issues tcgen05.mma, four of K = 16 a slab; warps 2-9 are the epilogue, which reads one of two
+// accumulators in tensor memory while the MMAs fill the other.  Persistent over the tiles.  Two ways:
+//
+// Pairs: two CTAs (cta_group::2) share a tile of 256 rows x up to 256 columns, each staging its 128 rows of p and half of q's.
+// Alone: a CTA has 128 rows of p and up to 128 columns.  For few rows of a layer's input, which then are the columns: p is
+//   the weight, so that no product is made and nothing is loaded for rows that are not there.
+//
+// A long sum over few tiles is split: the parts' accumulators go to a workspace in fp32, and the caller joins them in order.
+//
+// TERMS = 3: each operand is two bf16 matrices, p = p0 + p1, and acc takes p0 q0 + p0 q1 + p1 q0 (Dekker's split product
+// without its smallest term): four tiles in shared memory feed three MMAs.
+#pragma once
+
+#include <cuda.h>
+
+#include "acrl_device.cuh"
+#include "acrl_host.h"
+#include "mbarrier.cuh"
+#include "tcgen05.cuh"
+#include "tma_host.h"
+
+namespace acrl {
+namespace {
+
+constexpr int kRows = 128;           // rows of p per CTA and tile
+constexpr int kSlab = 64;            // of the sum: 128 bytes, one row of the 128-byte swizzle
+constexpr int kRowBytes = kSlab * 2;
+constexpr int kMaxStages = 12;
+constexpr int kDrain = 8;            // epilogue warps
+constexpr int kProductThreads = (2 + kDrain) * 32;
+constexpr uint32_t kTmemCols = 512;
+constexpr int kAccCols = 256;        // of each accumulator
+constexpr int kWarpStaging = 4096;   // bytes of an epilogue warp: a block of 32 x 32 in fp32, or two in bf16
+constexpr int kProductSmem = 227 * 1024;
+
+struct ProductBarriers {
+    uint64_t full[kMaxStages];    // the copies of a stage have landed (pair: the even CTA's counts both CTAs')
+    uint64_t empty[kMaxStages];   // the MMAs that read it are done
+    uint64_t tfull[2];            // an accumulator is complete
+    uint64_t tempty[2];           // the epilogue warps (pair: of both CTAs, on the even one) have read it
+    uint64_t mma_done;
+    uint32_t tmem_base;
+    int32_t abort;
+};
+constexpr int kRingBytes = (kProductSmem - 1024 - kDrain * kWarpStaging - int(sizeof(ProductBarriers))) / 1024 * 1024;
+
+struct Problem {
+    int rows, cols_all;      // of the result
+    int slabs;               // ceil(K / 64)
+    int batch;
+    int cols;                // of a tile: a multiple of 32 (pair; of 128 where q is not K-major) or of 16 (alone)
+    int p_tiles, q_tiles;
+    int parts, per;          // of the sum, and slabs of each
+    int lower;               // tiles that lie above the diagonal's are left out: the result is symmetric
+    int p_turned, q_turned;  // the operand lies with the sum along its columns
+    uint32_t idesc;
+    int tiles, units;        // tiles of one matrix and part; all
+};
+
+// What a CTA or pair works on at a time.
+struct Unit {
+    int tp, tq, z, part, lo, hi;
+};
+
+template <int NP, int TERMS, class Epi>
+struct ProductLaunch {
+    static constexpr int kMats = TERMS == 3 ? 2 : 1;
+    CUtensorMap p[NP][kMats], q[NP][kMats];
+    Problem pr[NP];
+    Epi epi[NP];
+    int stages, stage_bytes;
+    int32_t* flags;
+};
+
+// Tiles in bands of kBand row tiles, all column tiles of a band in turn, so that the tiles in flight share operands in L2.
+constexpr int kBand = 16;
+
+template <bool PAIR>
+__device__ __forceinline__ Unit unit_at(const Problem& pr, int u) {
+    Unit w;
+    const int t = u % pr.tiles, zp = u / pr.tiles;
+    w.part = zp % pr.parts;
+    w.z = zp / pr.parts;
+    w.lo = w.part * pr.per;
+    w.hi = min(pr.slabs, w.lo + pr.per);
+    if (pr.lower) {
+        // row tile i has min(q_tiles, (i + 1) r) column tiles, r of them as wide as a row tile is high: r i (i + 1) / 2 before it
+        const int r = 2 * kRows / pr.cols;
+        int i = int((sqrtf(8.f * float(t / r) + 1.f) - 1.f) * 0.5f);
+        while (r * i * (i + 1) / 2 > t) --i;
+        while (r * (i + 1) * (i + 2) / 2 <= t) ++i;
+        w.tp = i;
+        w.tq = t - r * i * (i + 1) / 2;
+    } else {
+        const int per_band = kBand * pr.q_tiles, band = t / per_band, k = t - band * per_band;
+        const int h = min(kBand, pr.p_tiles - band * kBand);
+        w.tp = band * kBand + k % h;
+        w.tq = k / h;
+    }
+    return w;
+}
+
+// The units that this CTA or pair takes, of all problems in turn.
+template <bool PAIR, int NP, class L>
+struct Units {
+    const L& l;
+    int u, step, which = 0;
+    __device__ Units(const L& launch) : l(launch) {
+        u = int(blockIdx.x) >> (PAIR ? 1 : 0);
+        step = int(gridDim.x) >> (PAIR ? 1 : 0);
+        turn();
+    }
+    __device__ __forceinline__ void turn() {
+        if (NP == 2 && which == 0 && u >= l.pr[0].units) {
+            which = 1;
+            u -= l.pr[0].units;
+        }
+    }
+    __device__ __forceinline__ bool more() const { return u < l.pr[NP == 2 ? which : 0].units; }
+    __device__ __forceinline__ void next() {
+        u += step;
+        turn();
+    }
+    __device__ __forceinline__ const Problem& problem() const { return l.pr[NP == 2 ? which : 0]; }
+    __device__ __forceinline__ Unit unit() const { return unit_at<PAIR>(problem(), u); }
+};
+
+// The descriptor of an operand's tile: rows of 128 bytes along the sum, or 64 x 64 blocks in which the sum runs from row to row:
+// 64 of the operand's rows are the 128 bytes, eight of the sum are 1,024, and the next 64 rows are a block further.
+__device__ __forceinline__ uint64_t tile_desc(uint32_t addr, int turned) {
+    return smem_desc(addr) | (turned ? uint64_t(kSlab * kRowBytes >> 4) << 16 : 0);
+}
+
+template <bool PAIR, int NP, int TERMS, class L>
+__device__ void produce_slabs(const L& l, uint8_t* ring, ProductBarriers* bars, uint32_t rank) {
+    constexpr int kMats = TERMS == 3 ? 2 : 1;
+    volatile int32_t* abort = &bars->abort;
+    int stage = 0;
+    uint32_t phase = 0;
+    long issued = 0;
+    for (Units<PAIR, NP, L> w(l); w.more(); w.next()) {
+        const Problem& pr = w.problem();
+        const Unit t = w.unit();
+        const CUtensorMap *tmP = l.p[NP == 2 ? w.which : 0], *tmQ = l.q[NP == 2 ? w.which : 0];
+        const int q_rows = PAIR ? pr.cols / 2 : pr.cols, q_bytes = q_rows * kRowBytes;
+        const int bytes = kMats * (kRows * kRowBytes + q_bytes);
+        const int p0 = (PAIR ? 2 * t.tp + int(rank) : t.tp) * kRows;
+        const int q0 = t.tq * pr.cols + (PAIR ? int(rank) * q_rows : 0);
+        for (int kb = t.lo; kb < t.hi; ++kb) {
+            if (!warp_wait(&bars->empty[stage], phase ^ 1u, abort)) {
+                give_up(abort, l.flags);
+                // the copies that were started land before the CTA can exit: the even CTA's barriers count both CTAs', the
+                // odd one gives its own time to land
+                if (!PAIR || rank == 0) {
+                    for (long j = issued - 1; j >= 0 && j >= issued - l.stages; --j)
+                        wait_phase(&bars->full[j % l.stages], uint32_t((j / l.stages) & 1), nullptr);
+                } else {
+                    const uint64_t t0 = global_ns();
+                    while (global_ns() - t0 < 100000ull) {
+                    }
+                }
+                return;
+            }
+            uint8_t* s = ring + stage * l.stage_bytes;
+            const uint32_t bar = PAIR ? peer_addr(&bars->full[stage], 0) : smem_u32(&bars->full[stage]);
+            if (elect_one()) {
+                if (!PAIR || rank == 0) mbar_expect_tx(&bars->full[stage], uint32_t((PAIR ? 2 : 1) * bytes));
+#pragma unroll
+                for (int i = 0; i < kMats; ++i) {
+                    uint8_t* to = s + i * kRows * kRowBytes;
+                    if (pr.p_turned) {
+                        tma_load_3d<PAIR>(to, &tmP[i], bar, p0, kb * kSlab, t.z);
+                        tma_load_3d<PAIR>(to + kSlab * kRowBytes, &tmP[i], bar, p0 + kSlab, kb * kSlab, t.z);
+                    } else {
+                        tma_load_3d<PAIR>(to, &tmP[i], bar, kb * kSlab, p0, t.z);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < kMats; ++i) {
+                    uint8_t* to = s + kMats * kRows * kRowBytes + i * q_bytes;
+                    if (pr.q_turned) {
+                        for (int j = 0; j < q_rows; j += kSlab)
+                            tma_load_3d<PAIR>(to + j * kRowBytes, &tmQ[i], bar, q0 + j, kb * kSlab, t.z);
+                    } else {
+                        tma_load_3d<PAIR>(to, &tmQ[i], bar, kb * kSlab, q0, t.z);
+                    }
+                }
+            }
+            ++issued;
+            if (++stage == l.stages) {
+                stage = 0;
+                phase ^= 1u;
+            }
+        }
+    }
+}
+
+template <bool PAIR>
+__device__ __forceinline__ void mma_bf16(uint32_t d, uint64_t pdesc, uint64_t qdesc, uint32_t idesc, uint32_t accumulate) {
+    if (PAIR)
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+            "l"(pdesc), "l"(qdesc), "r"(idesc), "r"(accumulate));
+    else
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+            "l"(pdesc), "l"(qdesc), "r"(idesc), "r"(accumulate));
+}
+
+template <bool PAIR, int NP, int TERMS, class L>
+__device__ void issue_products(const L& l, uint8_t* ring, ProductBarriers* bars, uint32_t tmem) {
+    constexpr int kMats = TERMS == 3 ? 2 : 1;
+    volatile int32_t* abort = &bars->abort;
+    const uint32_t units = uint32_t(l.stage_bytes) >> 4;   // of a stage, in descriptors
+    const uint32_t base = smem_u32(ring);
+    int stage = 0, acc = 0;
+    uint32_t phase = 0, aphase = 0;
+    bool ok = true;
+    for (Units<PAIR, NP, L> w(l); w.more() && ok; w.next()) {
+        const Problem& pr = w.problem();
+        const Unit t = w.unit();
+        const uint64_t pdesc0 = tile_desc(base, pr.p_turned), qdesc0 = tile_desc(base + kMats * kRows * kRowBytes, pr.q_turned);
+        // from one K = 16 to the next: 32 bytes of a row, or sixteen rows
+        const uint32_t pstep = pr.p_turned ? 16 * kRowBytes >> 4 : 2, qstep = pr.q_turned ? 16 * kRowBytes >> 4 : 2;
+        const uint32_t plow = kRows * kRowBytes >> 4, qlow = uint32_t((PAIR ? pr.cols / 2 : pr.cols) * kRowBytes) >> 4;
+        if (!warp_wait(&bars->tempty[acc], aphase ^ 1u, abort)) {
+            give_up(abort, l.flags);
+            break;
+        }
+        tc_fence_after();
+        const uint32_t d = tmem + uint32_t(acc * kAccCols);
+        for (int kb = t.lo; kb < t.hi; ++kb) {
+            ok = warp_wait(&bars->full[stage], phase, abort);
+            if (!ok) break;
+            tc_fence_after();
+            const uint64_t pd = pdesc0 + stage * units, qd = qdesc0 + stage * units;
+            const uint32_t more = kb > t.lo;
+            if (elect_one()) {
+#pragma unroll
+                for (int i = 0; i < TERMS; ++i) {
+                    const uint64_t a = pd + (i == 2 ? plow : 0u), b = qd + (i == 1 ? qlow : 0u);
+#pragma unroll
+                    for (uint32_t k = 0; k < kSlab / 16; ++k)
+                        mma_bf16<PAIR>(d, a + k * pstep, b + k * qstep, pr.idesc, i > 0 || k > 0 ? 1u : more);
+                }
+                commit<PAIR>(&bars->empty[stage]);
+            }
+            if (++stage == l.stages) {
+                stage = 0;
+                phase ^= 1u;
+            }
+        }
+        if (!ok) {
+            give_up(abort, l.flags);
+            break;
+        }
+        if (elect_one()) commit<PAIR>(&bars->tfull[acc]);
+        if (++acc == 2) {
+            acc = 0;
+            aphase ^= 1u;
+        }
+    }
+    // every MMA has finished before the CTA moves on
+    if (elect_one()) {
+        if (PAIR)
+            asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
+                             peer_addr(&bars->mma_done, 0))
+                         : "memory");
+        else
+            commit<false>(&bars->mma_done);
+    }
+    wait_phase(&bars->mma_done, 0, nullptr);
+    __syncwarp();
+}
+
+// An epilogue warp's way out: its block of shared memory, and stores of 32 x 32 values by TMA.
+struct WarpOut {
+    uint8_t* staging;
+    int lane;
+    int half = 0;
+    bool whole = false;   // the last store read the whole block
+
+    // Lane i has row row0 + i.  Not for a matrix that ends within these columns at no multiple of 16 bytes: a TMA store leaves
+    // columns out in pieces of that size and would write beyond it.
+    template <typename T>
+    __device__ __forceinline__ void store(const CUtensorMap* map, const float (&v)[32], int row0, int col0, int z) {
+        constexpr int kPieces = 32 * int(sizeof(T)) / 16;
+        // a block of bf16 alternates between the halves; one of fp32 takes both
+        uint8_t* block = staging;
+        if (sizeof(T) == 2) {
+            block += half * (kWarpStaging / 2);
+            half ^= 1;
+            if (lane == 0) {
+                if (whole) bulk_wait_read<0>();
+                else bulk_wait_read<1>();
+            }
+        } else {
+            if (lane == 0) bulk_wait_read<0>();
+        }
+        whole = sizeof(T) == 4;
+        __syncwarp();
+        // row `lane`, its 16-byte pieces permuted by the swizzle of the map: 64-byte rows in fours, 128-byte rows in eights
+        const uint32_t swz = kPieces == 4 ? uint32_t((lane >> 1) & 3) : uint32_t(lane & 7);
+        const uint32_t to = smem_u32(block) + uint32_t(lane * 32 * int(sizeof(T)));
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) {
+            uint4 x;
+            if constexpr (sizeof(T) == 2)
+                x = make_uint4(pack_bf16x2(v[8 * k], v[8 * k + 1]), pack_bf16x2(v[8 * k + 2], v[8 * k + 3]),
+                               pack_bf16x2(v[8 * k + 4], v[8 * k + 5]), pack_bf16x2(v[8 * k + 6], v[8 * k + 7]));
+            else
+                x = make_uint4(__float_as_uint(v[4 * k]), __float_as_uint(v[4 * k + 1]), __float_as_uint(v[4 * k + 2]),
+                               __float_as_uint(v[4 * k + 3]));
+            st_shared16(to + ((uint32_t(k) ^ swz) << 4), x);
+        }
+        fence_async_shared();
+        __syncwarp();
+        if (lane == 0) tma_store_3d(map, block, col0, row0, z);
+    }
+};
+
+template <bool PAIR, int NP, class L>
+__device__ void drain(const L& l, ProductBarriers* bars, uint32_t tmem, uint8_t* staging, uint32_t rank) {
+    volatile int32_t* abort = &bars->abort;
+    const int warp = int(threadIdx.x >> 5) - 2, lane = threadIdx.x & 31, quarter = (threadIdx.x >> 5) & 3;
+    WarpOut out{staging + warp * kWarpStaging, lane};
+    const uint32_t lanes = uint32_t(quarter * 32) << 16;
+    int acc = 0;
+    uint32_t phase = 0;
+    for (Units<PAIR, NP, L> w(l); w.more(); w.next()) {
+        const Problem& pr = w.problem();
+        const Unit t = w.unit();
+        const int row0 = (PAIR ? 2 * t.tp + int(rank) : t.tp) * kRows + quarter * 32;
+        if (!warp_wait(&bars->tfull[acc], phase, abort)) {
+            give_up(abort, l.flags);
+            break;
+        }
+        tc_fence_after();
+        bool told = false;
+#pragma unroll 1
+        for (int c = 32 * (warp >> 2); c < pr.cols; c += 64) {   // the two warps of a quarter take 32 columns in turn
+            uint32_t r[32];
+            __syncwarp();
+            tmem_ld32(tmem + uint32_t(acc * kAccCols + c) + lanes, r);
+            if (c + 64 >= pr.cols) {   // read out: the MMA warp may fill it again
+                told = true;
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (PAIR) remote_arrive(peer_addr(&bars->tempty[acc], 0));
+                    else mbar_arrive(&bars->tempty[acc]);
+                }
+            }
+            const int col0 = t.tq * pr.cols + c;
+            if (row0 < pr.rows && col0 < pr.cols_all)   // the same for the whole warp
+                l.epi[NP == 2 ? w.which : 0].chunk(pr, t, r, row0, col0, out);
+        }
+        if (!told) {   // a tile of one chunk has none for this warp
+            __syncwarp();
+            if (lane == 0) {
+                if (PAIR) remote_arrive(peer_addr(&bars->tempty[acc], 0));
+                else mbar_arrive(&bars->tempty[acc]);
+            }
+        }
+        __syncwarp();
+        if (++acc == 2) {
+            acc = 0;
+            phase ^= 1u;
+        }
+    }
+    if (lane == 0) bulk_wait_all();   // the blocks stay valid until every store has completed
+    __syncwarp();
+}
+
+template <bool PAIR, int NP, int TERMS, class Epi>
+__global__ void __launch_bounds__(kProductThreads, 1)
+    product_kernel(const __grid_constant__ ProductLaunch<NP, TERMS, Epi> l) {
+    using L = ProductLaunch<NP, TERMS, Epi>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t* staging = ring + kRingBytes;
+    ProductBarriers* bars = reinterpret_cast<ProductBarriers*>(staging + kDrain * kWarpStaging);
+    const int warp = threadIdx.x >> 5;
+    const uint32_t rank = PAIR ? cluster_rank() : 0;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kMaxStages; ++s) {
+            mbar_init(&bars->full[s], 1);
+            mbar_init(&bars->empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(&bars->tfull[b], 1);
+            mbar_init(&bars->tempty[b], (PAIR ? 2 : 1) * kDrain);
+        }
+        mbar_init(&bars->mma_done, 1);
+        bars->abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&l.p[0][0])) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&l.q[0][0])) : "memory");
+    }
+    grid_begin();
+    if (warp == 2) {
+        if (PAIR) {   // one warp of each CTA of the pair, together
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)),
+                         "r"(kTmemCols)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)),
+                         "r"(kTmemCols)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (PAIR) cluster_sync();   // the other's barriers are initialised, and it runs
+    tc_fence_after();
+    const uint32_t tmem = bars->tmem_base;
+    if (warp == 0) {
+        produce_slabs<PAIR, NP, TERMS, L>(l, ring, bars, rank);
+    } else if (warp == 1) {
+        if (rank == 0) issue_products<PAIR, NP, TERMS, L>(l, ring, bars, tmem);
+    } else {
+        drain<PAIR, NP, L>(l, bars, tmem, staging, rank);
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (PAIR) cluster_sync();   // no CTA frees its TMEM or leaves while the other may still touch it
+    if (warp == 2) {
+        tc_fence_after();
+        if (PAIR)
+            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+        else
+            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------------------------------------------
+
+// An operand of a product: [rows, K], or with `turned` [K, rows]; `count` of them `apart` elements from one another.
+struct Matrix {
+    const acrl_bf16* at;
+    int64_t rows, ld;
+    bool turned;
+    int64_t count, apart;
+};
+
+inline bool operand_map(CUtensorMap* map, const Matrix& m, int64_t K, int box_rows) {
+    return m.turned ? encode_map_3d(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, m.at, uint64_t(m.count), uint64_t(K), uint64_t(m.rows),
+                                    uint64_t(m.ld), uint64_t(m.apart), kSlab, kSlab, CU_TENSOR_MAP_SWIZZLE_128B)
+                    : encode_map_3d(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, m.at, uint64_t(m.count), uint64_t(m.rows), uint64_t(K),
+                                    uint64_t(m.ld), uint64_t(m.apart), uint32_t(box_rows), kSlab, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+// The map of a result that WarpOut::store writes.
+inline bool result_map(CUtensorMap* map, const void* at, bool f32, int64_t rows, int64_t cols, int64_t ld, int64_t count, int64_t apart) {
+    return encode_map_3d(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, f32 ? 4 : 2, at, uint64_t(count),
+                         uint64_t(rows), uint64_t(cols), uint64_t(ld), uint64_t(apart), 32, 32,
+                         f32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
+}
+
+// How a product is cut.
+struct Cut {
+    int cols, parts, per;
+};
+
+// tcgen05.mma kind::f16: D f32 (bits 4-5 = 1), A and B bf16 (bits 7-9, 10-12 = 1), A and B transposed (bits 15, 16),
+// N / 8 at bit 17, M / 16 at bit 24.
+inline Problem problem_of(bool pair, int64_t rows, int64_t cols_all, int64_t K, int64_t batch, bool p_turned, bool q_turned,
+                          bool lower, const Cut& cut) {
+    Problem pr = {};
+    const int high = pair ? 2 * kRows : kRows;
+    pr.rows = int(rows);
+    pr.cols_all = int(cols_all);
+    pr.slabs = int((K + kSlab - 1) / kSlab);
+    pr.batch = int(batch);
+    pr.cols = cut.cols;
+    pr.p_tiles = int((rows + high - 1) / high);
+    pr.q_tiles = int((cols_all + cut.cols - 1) / cut.cols);
+    pr.parts = cut.parts;
+    pr.per = cut.per;
+    pr.lower = lower;
+    pr.p_turned = p_turned;
+    pr.q_turned = q_turned;
+    pr.idesc = 1u << 4 | 1u << 7 | 1u << 10 | uint32_t(p_turned) << 15 | uint32_t(q_turned) << 16 |
+               uint32_t(cut.cols >> 3) << 17 | uint32_t(high >> 4) << 24;
+    if (lower) {
+        const int r = high / cut.cols, last = pr.p_tiles - 1;   // all row tiles but the last have r columns more than the one before
+        pr.tiles = r * last * (last + 1) / 2 + pr.q_tiles;
+    } else {
+        pr.tiles = pr.p_tiles * pr.q_tiles;
+    }
+    pr.units = pr.tiles * pr.parts * pr.batch;
+    return pr;
+}
+
+// Units beyond 32 bits are refused by the caller: rows / 128 x columns / 16 x parts x batch.
+inline bool units_fit(bool pair, int64_t rows, int64_t cols_all, int64_t batch, const Cut& cut) {
+    const int64_t high = pair ? 2 * kRows : kRows;
+    const double n = double((rows + high - 1) / high) * double((cols_all + cut.cols - 1) / cut.cols) * cut.parts * double(batch);
+    return n < 1e9;
+}
+
+template <bool PAIR, int NP, int TERMS, class Epi>
+acrl_status launch_product(ProductLaunch<NP, TERMS, Epi>& l, int32_t* flags, cudaStream_t s) {
+    constexpr int kMats = TERMS == 3 ? 2 : 1;
+    auto* kernel = product_kernel<PAIR, NP, TERMS, Epi>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem) != cudaSuccess) return launch_status();
+    l.stage_bytes = 0;
+    int64_t units = 0;
+    for (int i = 0; i < NP; ++i) {
+        const int bytes = kMats * (kRows + (PAIR ? l.pr[i].cols / 2 : l.pr[i].cols)) * kRowBytes;
+        l.stage_bytes = std::max(l.stage_bytes, bytes);
+        units += l.pr[i].units;
+    }
+    l.stages = std::min(kMaxStages, kRingBytes / l.stage_bytes);
+    l.flags = flags;
+    int64_t most;
+    if (PAIR) {
+        most = resident_clusters(reinterpret_cast<const void*>(kernel), kProductThreads, kProductSmem, 2);
+    } else {
+        int dev = 0, sms = 0;
+        if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+            return launch_status();
+        most = sms;
+    }
+    if (most < 1) return ACRL_ERR_CUDA;
+    return launch(kernel, std::min(units, most) * (PAIR ? 2 : 1), kProductThreads, kProductSmem, PAIR ? 2 : 0, s, l);
+}
+
+}  // namespace
+}  // namespace acrl

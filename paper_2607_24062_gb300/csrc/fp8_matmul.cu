@@ -146,37 +146,6 @@ __device__ __forceinline__ void mma_scaled(uint32_t d, uint64_t adesc, uint64_t 
             "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate));
 }
 
-// Arrive on this CTA's barrier, or on that of both CTAs of the pair, when this thread's MMAs so far have completed.
-template <bool PAIR>
-__device__ __forceinline__ void commit(uint64_t* bar) {
-    if constexpr (PAIR) {
-#pragma unroll
-        for (uint32_t r = 0; r < 2; ++r)
-            asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(peer_addr(bar, r))
-                         : "memory");
-    } else {
-        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
-                     : "memory");
-    }
-}
-
-// `bar`: a shared::cluster address.
-template <bool PAIR>
-__device__ __forceinline__ void tma_load(void* dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
-    if (PAIR)
-        asm volatile(
-            "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, "
-            "%3}], [%4];" ::"r"(smem_u32(dst)),
-            "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
-            : "memory");
-    else
-        asm volatile(
-            "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
-                smem_u32(dst)),
-            "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
-            : "memory");
-}
-
 // What a CTA works on.  Pairs take tiles in turn, all slabs of each; of two problems the first one's, and then consecutive tiles of
 // the second, as many as even out what the first left unequal (share_out): `more_first` for a pair that has one tile more of
 // the first, `most_else` or one more for the others.  Alone, a cluster of CTAs splits one tile's slabs.
@@ -233,19 +202,6 @@ __device__ __forceinline__ void tile_at(int t, const Problem& pr, int& tp, int& 
     const int h = min(kBand, pr.p_tiles - band * kBand);
     tp = band * kBand + r % h;
     tq = r / h;
-}
-
-// One lane of a warp that is together.
-__device__ __forceinline__ bool elect_one() {
-    uint32_t r;
-    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(r));
-    return r != 0;
-}
-
-// A whole warp waits; the common case, a phase that has completed, without a call.
-__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int32_t* abort) {
-    const bool ok = mbar_try_wait(bar, parity) || wait_phase(bar, parity, abort);
-    return __all_sync(0xffffffffu, ok);
 }
 
 // The producer's and the MMA warp's loops run in the whole warp, and one lane is elected for each batch of copies or MMAs:

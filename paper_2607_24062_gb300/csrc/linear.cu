@@ -1,45 +1,295 @@
 // acrl_linear and acrl_linear_backward: a bf16 layer with bias, activation and residual, and its gradients.
 #include <algorithm>
+#include <type_traits>
 
 #include "acrl_host.h"
 #include "activation.cuh"
-#include "simple_product.cuh"
-#include "tma_host.h"
+#include "bf16_product.cuh"
 
 namespace acrl {
 namespace {
 
 constexpr int64_t kMostSize = kMaxGrid - 512;
+constexpr int kPairs = 76;           // of SMs: what a cut is made for
+constexpr int64_t kAloneRows = 128;  // rows that become a CTA's columns
 
-struct Epilogue {
+template <typename F>
+__host__ __device__ __forceinline__ acrl_status by_act(int a, F f) {
+    switch (a) {
+        case ACRL_ACT_NONE: return f(std::integral_constant<int, ACRL_ACT_NONE>{});
+        case ACRL_ACT_RELU: return f(std::integral_constant<int, ACRL_ACT_RELU>{});
+        case ACRL_ACT_GELU: return f(std::integral_constant<int, ACRL_ACT_GELU>{});
+        case ACRL_ACT_GELU_TANH: return f(std::integral_constant<int, ACRL_ACT_GELU_TANH>{});
+        case ACRL_ACT_SILU: return f(std::integral_constant<int, ACRL_ACT_SILU>{});
+    }
+    return ACRL_ERR_INVALID_ARG;
+}
+
+// What follows the sum: out = f(sum + bias) + residual.
+struct Finish {
     const void *bias, *residual;
-    bool bias_f32, residual_f32, out_f32;
-    int64_t ldr, ldp, ldo;
-    acrl_bf16* pre;
     void* out;
+    acrl_bf16* pre;
+    int64_t ldr, ldp, ldo;
+    int act;
+    bool bias_f32, residual_f32, out_f32;
 };
 
-template <int ACT>
-__global__ void __launch_bounds__(256) product_kernel(View A, View B, int M, int N, int K, Epilogue e) {
-    grid_begin();
-    const int tiles = (N + 63) / 64, m0 = int(blockIdx.x) / tiles * 64, n0 = int(blockIdx.x) % tiles * 64;
-    simple_product(A, B, M, N, K, m0, n0, [&](int64_t m, int64_t n, float u) {
-        if (e.bias) u += load_float(e.bias, e.bias_f32, n);
-        if (e.pre) e.pre[m * e.ldp + n] = to_bf16(u);
-        u = act<ACT>(u);
-        if (e.residual) u += load_float(e.residual, e.residual_f32, m * e.ldr + n);
-        if (e.out_f32)
-            static_cast<float*>(e.out)[m * e.ldo + n] = u;
-        else
-            static_cast<acrl_bf16*>(e.out)[m * e.ldo + n] = to_bf16(u);
+__device__ __forceinline__ void store_float(void* p, bool f32, int64_t i, float v) {
+    if (f32)
+        static_cast<float*>(p)[i] = v;
+    else
+        static_cast<acrl_bf16*>(p)[i] = to_bf16(v);
+}
+
+template <int N>
+__device__ __forceinline__ void apply(int which, float (&v)[N]) {
+    by_act(which, [&](auto a) {
+        if constexpr (a != ACRL_ACT_NONE)
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[j] = act<a>(v[j]);
+        return ACRL_OK;
     });
 }
 
-template <int ACT>
-acrl_status product(const View& A, const View& B, int64_t M, int64_t N, int64_t K, const Epilogue& e, cudaStream_t s) {
-    const int64_t tiles = ((M + 63) / 64) * ((N + 63) / 64);
-    if (tiles > kMaxGrid) return ACRL_ERR_INVALID_ARG;
-    return launch(product_kernel<ACT>, tiles, 256, 0, 0, s, A, B, int(M), int(N), int(K), e);
+// N values of a row from column c on, as fp32; N a multiple of eight and c of four.
+template <int N>
+__device__ __forceinline__ void load_row(const void* p, bool f32, int64_t row, int c, int cols, float (&v)[N]) {
+    if (c + N > cols) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = c + j < cols ? load_float(p, f32, row + c + j) : 0.f;
+    } else if (f32) {
+        const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + row + c);
+#pragma unroll
+        for (int j = 0; j < N / 4; ++j) {
+            const float4 x = q[j];
+            v[4 * j] = x.x;
+            v[4 * j + 1] = x.y;
+            v[4 * j + 2] = x.z;
+            v[4 * j + 3] = x.w;
+        }
+    } else {
+        const uint2* q = reinterpret_cast<const uint2*>(static_cast<const acrl_bf16*>(p) + row + c);
+#pragma unroll
+        for (int j = 0; j < N / 4; ++j) {
+            const uint2 x = q[j];
+            v[4 * j] = bf16_lo(x.x);
+            v[4 * j + 1] = bf16_hi(x.x);
+            v[4 * j + 2] = bf16_lo(x.y);
+            v[4 * j + 3] = bf16_hi(x.y);
+        }
+    }
+}
+
+// A tile's accumulators on their way out.  Pair: a lane has a row of the result and 32 of its columns.  Alone: p is the
+// weight, a lane has a column of the result and 32 rows, and a warp's stores are of neighbours.
+template <bool PAIR>
+struct LinearEpilogue {
+    Finish f;
+    CUtensorMap out_map, pre_map;   // pair: of out (or of the parts), and of pre
+    float* parts;                   // where the sum is split: [part][row][ldparts]
+    int64_t ldparts, part_size;
+
+    __device__ __forceinline__ void chunk(const Problem& pr, const Unit& t, const uint32_t (&r)[32], int row0, int col0,
+                                          WarpOut& out) const {
+        float v[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
+        if constexpr (PAIR) {
+            if (parts) {
+                out.store<float>(&out_map, v, row0, col0, t.part);
+                return;
+            }
+            const int row = row0 + out.lane;
+            const bool ragged = col0 + 32 > pr.cols_all;
+            if (f.bias) {
+                const float b = col0 + out.lane < pr.cols_all ? load_float(f.bias, f.bias_f32, col0 + out.lane) : 0.f;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] += __shfl_sync(0xffffffffu, b, j);
+            }
+            if (f.pre) {
+                if (ragged && (pr.cols_all & 7)) {
+                    if (row < pr.rows)
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (col0 + j < pr.cols_all) f.pre[row * f.ldp + col0 + j] = to_bf16(v[j]);
+                } else {
+                    out.store<acrl_bf16>(&pre_map, v, row0, col0, 0);
+                }
+            }
+            apply(f.act, v);
+            if (f.residual && row < pr.rows) {
+                float add[32];
+                load_row(f.residual, f.residual_f32, row * f.ldr, col0, pr.cols_all, add);
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] += add[j];
+            }
+            if (ragged && (pr.cols_all & (f.out_f32 ? 3 : 7))) {
+                if (row < pr.rows)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (col0 + j < pr.cols_all) store_float(f.out, f.out_f32, row * f.ldo + col0 + j, v[j]);
+            } else if (f.out_f32) {
+                out.store<float>(&out_map, v, row0, col0, 0);
+            } else {
+                out.store<acrl_bf16>(&out_map, v, row0, col0, 0);
+            }
+        } else {
+            const int64_t n = row0 + out.lane;
+            if (n >= pr.rows) return;
+            const int rows = pr.cols_all - col0;   // of the result that this chunk has, of 32
+            if (parts) {
+                float* to = parts + t.part * part_size + col0 * ldparts + n;
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (j < rows) to[j * ldparts] = v[j];
+                return;
+            }
+            const float b = f.bias ? load_float(f.bias, f.bias_f32, n) : 0.f;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] += b;
+            if (f.pre)
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (j < rows) f.pre[(col0 + j) * f.ldp + n] = to_bf16(v[j]);
+            apply(f.act, v);
+            if (f.residual) {
+                float add[32];
+#pragma unroll
+                for (int j = 0; j < 32; ++j) add[j] = j < rows ? load_float(f.residual, f.residual_f32, (col0 + j) * f.ldr + n) : 0.f;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] += add[j];
+            }
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                if (j < rows) store_float(f.out, f.out_f32, (col0 + j) * f.ldo + n, v[j]);
+        }
+    }
+};
+
+// The parts of a split sum in their order, and what follows; no parts are the empty sum.  A thread has four columns of a row.
+__global__ void __launch_bounds__(256) join_kernel(Finish f, const float* parts, int count, int64_t ldparts, int64_t part_size, int M,
+                                                   int N) {
+    grid_begin();
+    const int64_t quads = (N + 3) / 4, i = int64_t(blockIdx.x) * 256 + threadIdx.x;
+    if (i >= quads * M) return;
+    const int64_t row = i / quads;
+    const int c = int(i - row * quads) * 4;
+    float v[4] = {};
+    for (int p = 0; p < count; ++p) {
+        const float4 x = *reinterpret_cast<const float4*>(parts + p * part_size + row * ldparts + c);
+        v[0] += x.x;
+        v[1] += x.y;
+        v[2] += x.z;
+        v[3] += x.w;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (f.bias && c + j < N) v[j] += load_float(f.bias, f.bias_f32, c + j);
+    auto store = [&](void* to, bool f32, int64_t ld) {
+        if (c + 4 > N) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (c + j < N) store_float(to, f32, row * ld + c + j, v[j]);
+        } else if (f32) {
+            *reinterpret_cast<float4*>(static_cast<float*>(to) + row * ld + c) = make_float4(v[0], v[1], v[2], v[3]);
+        } else {
+            *reinterpret_cast<uint2*>(static_cast<acrl_bf16*>(to) + row * ld + c) =
+                make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+        }
+    };
+    if (f.pre) store(f.pre, false, f.ldp);
+    apply(f.act, v);
+    if (f.residual) {
+        float add[4];
+        load_row(f.residual, f.residual_f32, row * f.ldr, c, N, add);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] += add[j];
+    }
+    store(f.out, f.out_f32, f.ldo);
+}
+
+// How a product of M x N results over K is made.
+struct Plan {
+    bool alone;
+    Cut cut;
+    int64_t cost, workspace;   // cycles by estimate; bytes
+    int64_t ldparts, part_size;
+};
+
+// The cut with the least estimated time: rounds of tiles x (slabs x a slab's cycles + a tile's), and the joining of parts.
+Plan plan_of(int64_t M, int64_t N, int64_t K, bool x_turned, bool w_turned) {
+    constexpr int64_t kTile = 2000, kJoin = 6000, kJoinBytes = 3000;   // cycles, cycles, bytes a cycle
+    const int64_t slabs = std::max<int64_t>(1, (K + kSlab - 1) / kSlab);
+    Plan best = {};
+    best.alone = M <= kAloneRows;
+    best.ldparts = (N + 7) / 8 * 8;
+    best.part_size = M * best.ldparts;
+    const int64_t rows = best.alone ? N : M, cols_all = best.alone ? M : N, high = best.alone ? kRows : 2 * kRows;
+    const int64_t lanes = best.alone ? 2 * kPairs : kPairs;
+    int widest = 256, step = 32, least = 64;   // columns of a tile
+    if (best.alone) widest = least = int(x_turned ? std::max<int64_t>(1, (M + 63) / 64) * 64 : std::max<int64_t>(1, (M + 15) / 16) * 16);   // of blocks of 64
+    else if (w_turned) step = least = 128;
+    for (int cols = widest; cols >= least; cols -= step) {
+        const int64_t tiles = (rows + high - 1) / high * ((cols_all + cols - 1) / cols);
+        // a slab: its MMAs, or its loads at 64 bytes a cycle
+        const int64_t slab = best.alone ? 2 * (kRows + cols) : std::max(2 * cols, 2 * (kRows + cols / 2));
+        for (int64_t parts = 1; parts <= 16 && parts <= slabs; ++parts) {
+            const int64_t per = (slabs + parts - 1) / parts;
+            if ((slabs + per - 1) / per != parts) continue;
+            const int64_t rounds = (tiles * parts + lanes - 1) / lanes;
+            const int64_t cost = rounds * (per * slab + kTile) + (parts > 1 ? kJoin + (parts + 1) * best.part_size * 4 / kJoinBytes : 0);
+            if (best.cost == 0 || cost < best.cost) {
+                best.cost = cost;
+                best.cut = Cut{cols, int(parts), int(per)};
+            }
+        }
+    }
+    best.workspace = best.cut.parts > 1 ? best.cut.parts * best.part_size * 4 : 0;
+    return best;
+}
+
+acrl_status join(const Finish& f, const float* parts, int count, const Plan& plan, int64_t M, int64_t N, cudaStream_t s) {
+    const int64_t threads = (N + 3) / 4 * M;
+    if ((threads + 255) / 256 > kMaxGrid) return ACRL_ERR_INVALID_ARG;
+    return launch(join_kernel, (threads + 255) / 256, 256, 0, 0, s, f, parts, count, plan.ldparts, plan.part_size, int(M), int(N));
+}
+
+// Fills one problem of a launch; x has the result's rows, w its columns.
+template <bool PAIR, int NP>
+bool describe(ProductLaunch<NP, 1, LinearEpilogue<PAIR>>& l, int at, const Plan& plan, const Matrix& x, const Matrix& w, int64_t K,
+              const Finish& f, float* parts) {
+    const Matrix &p = PAIR ? x : w, &q = PAIR ? w : x;
+    const int64_t M = x.rows, N = w.rows;
+    l.pr[at] = problem_of(PAIR, p.rows, q.rows, K, 1, p.turned, q.turned, false, plan.cut);
+    LinearEpilogue<PAIR>& e = l.epi[at];
+    e.f = f;
+    e.parts = plan.cut.parts > 1 ? parts : nullptr;
+    e.ldparts = plan.ldparts;
+    e.part_size = plan.part_size;
+    if (!operand_map(&l.p[at][0], p, K, kRows) || !operand_map(&l.q[at][0], q, K, PAIR ? plan.cut.cols / 2 : plan.cut.cols)) return false;
+    if (!PAIR) return true;
+    if (e.parts) return result_map(&e.out_map, parts, true, M, plan.ldparts, plan.ldparts, plan.cut.parts, plan.part_size);
+    return result_map(&e.out_map, f.out, f.out_f32, M, N, f.ldo, 1, M * f.ldo) &&
+           (!f.pre || result_map(&e.pre_map, f.pre, false, M, N, f.ldp, 1, M * f.ldp));
+}
+
+template <bool PAIR>
+acrl_status run_product(const Plan& plan, const Matrix& x, const Matrix& w, int64_t K, const Finish& f, float* parts, int32_t* flags,
+                        cudaStream_t s) {
+    ProductLaunch<1, 1, LinearEpilogue<PAIR>> l = {};
+    if (!describe<PAIR, 1>(l, 0, plan, x, w, K, f, parts)) return ACRL_ERR_CUDA;
+    const acrl_status st = launch_product<PAIR>(l, flags, s);
+    return st != ACRL_OK || plan.cut.parts == 1 ? st : join(f, parts, plan.cut.parts, plan, x.rows, w.rows, s);
+}
+
+// f(x w^T + ...): K > 0 columns, or an empty sum.
+acrl_status product(const Matrix& x, const Matrix& w, int64_t K, const Finish& f, void* workspace, int32_t* flags, cudaStream_t s) {
+    const Plan plan = plan_of(x.rows, w.rows, K, x.turned, w.turned);
+    if (K == 0) return join(f, nullptr, 0, plan, x.rows, w.rows, s);
+    if (!units_fit(!plan.alone, plan.alone ? w.rows : x.rows, plan.alone ? x.rows : w.rows, 1, plan.cut)) return ACRL_ERR_INVALID_ARG;
+    float* parts = static_cast<float*>(workspace);
+    return plan.alone ? run_product<false>(plan, x, w, K, f, parts, flags, s) : run_product<true>(plan, x, w, K, f, parts, flags, s);
 }
 
 // g = dy f'(u), rounded, and the columns' sums of the unrounded.
@@ -73,28 +323,17 @@ __global__ void __launch_bounds__(256) sums_kernel(const float* sums, int parts,
     dbias[n] = sum;
 }
 
-template <typename F>
-acrl_status by_act(acrl_activation a, F f) {
-    switch (a) {
-        case ACRL_ACT_NONE: return f(std::integral_constant<int, ACRL_ACT_NONE>{});
-        case ACRL_ACT_RELU: return f(std::integral_constant<int, ACRL_ACT_RELU>{});
-        case ACRL_ACT_GELU: return f(std::integral_constant<int, ACRL_ACT_GELU>{});
-        case ACRL_ACT_GELU_TANH: return f(std::integral_constant<int, ACRL_ACT_GELU_TANH>{});
-        case ACRL_ACT_SILU: return f(std::integral_constant<int, ACRL_ACT_SILU>{});
-    }
-    return ACRL_ERR_INVALID_ARG;
-}
-
 bool dtype_ok(acrl_dtype d) { return d == ACRL_BF16 || d == ACRL_F32; }
 bool matrix_ok(const void* p, int64_t cols, int64_t ld) { return p && aligned16(p) && ld >= cols && (ld & 7) == 0; }
 
+// The backward's workspace: g, the columns' sums of its parts, the parts of a product's split sum (of one after the other).
 struct BackwardParts {
-    int64_t ldg, g, sums, end;   // bytes
+    int64_t ldg, sums, parts, end;   // bytes
     BackwardParts(int64_t M, int64_t N, int64_t K) {
         ldg = (N + 7) / 8 * 8;
-        g = 0;
         sums = M * ldg * 2;
-        end = sums + (M + kSlopeRows - 1) / kSlopeRows * ldg * 4;
+        parts = sums + (M + kSlopeRows - 1) / kSlopeRows * ldg * 4;
+        end = parts + std::max(plan_of(M, K, N, false, true).workspace, plan_of(N, K, M, true, true).workspace);
     }
 };
 
@@ -103,7 +342,10 @@ struct BackwardParts {
 
 using namespace acrl;
 
-extern "C" int64_t acrl_linear_workspace_bytes(int64_t M, int64_t N, int64_t K) { return M < 0 || N < 0 || K < 0 ? -1 : 0; }
+extern "C" int64_t acrl_linear_workspace_bytes(int64_t M, int64_t N, int64_t K) {
+    if (M < 0 || N < 0 || K < 0) return -1;
+    return M == 0 || N == 0 || K == 0 || M > kMostSize || N > kMostSize || K > kMostSize ? 0 : plan_of(M, N, K, false, false).workspace;
+}
 
 extern "C" acrl_status acrl_linear(const acrl_bf16* x, int64_t M, int64_t K, int64_t ldx, const acrl_bf16* w, int64_t N, int64_t ldw,
                                    const void* bias, acrl_dtype bias_dtype, acrl_activation act, const void* residual,
@@ -120,15 +362,16 @@ extern "C" acrl_status acrl_linear(const acrl_bf16* x, int64_t M, int64_t K, int
         return ACRL_ERR_INVALID_ARG;
     if (K > 0 && (!matrix_ok(x, K, ldx) || !matrix_ok(w, K, ldw) || !operands_on_current_device({x, w, out})))
         return ACRL_ERR_INVALID_ARG;
-    const Epilogue e{bias, residual, bias_dtype == ACRL_F32, residual_dtype == ACRL_F32, out_dtype == ACRL_F32, ldr, ldp, ldo, pre,
-                     out};
-    return by_act(act, [&](auto a) {
-        return product<a>(View{x, false, ldx, 1}, View{w, false, ldw, 1}, M, N, K, e, reinterpret_cast<cudaStream_t>(stream));
-    });
+    const int64_t need = acrl_linear_workspace_bytes(M, N, K);
+    if (need > 0 && (!workspace || !aligned16(workspace) || !operands_on_current_device({workspace}))) return ACRL_ERR_INVALID_ARG;
+    const Finish f{bias, residual, out, pre, ldr, ldp, ldo, int(act), bias_dtype == ACRL_F32, residual_dtype == ACRL_F32,
+                   out_dtype == ACRL_F32};
+    return product(Matrix{x, M, ldx, false, 1, M * ldx}, Matrix{w, N, ldw, false, 1, N * ldw}, K, f, workspace, dev_flags,
+                   reinterpret_cast<cudaStream_t>(stream));
 }
 
 extern "C" int64_t acrl_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-    return M < 0 || N < 0 || K < 0 ? -1 : BackwardParts(M, N, K).end;
+    return M < 0 || N < 0 || K < 0 ? -1 : M > kMostSize || N > kMostSize || K > kMostSize ? 0 : BackwardParts(M, N, K).end;
 }
 
 extern "C" acrl_status acrl_linear_backward(const acrl_bf16* dy, int64_t M, int64_t N, int64_t lddy, const acrl_bf16* x, int64_t K,
@@ -157,7 +400,7 @@ extern "C" acrl_status acrl_linear_backward(const acrl_bf16* dy, int64_t M, int6
     int64_t ldg = lddy;
     acrl_status st = ACRL_OK;
     if (has_g && (act != ACRL_ACT_NONE || dbias)) {
-        acrl_bf16* to = act == ACRL_ACT_NONE || !(has_dx || has_dw) ? nullptr : reinterpret_cast<acrl_bf16*>(base + parts.g);
+        acrl_bf16* to = act == ACRL_ACT_NONE || !(has_dx || has_dw) ? nullptr : reinterpret_cast<acrl_bf16*>(base);
         float* sums = dbias ? reinterpret_cast<float*>(base + parts.sums) : nullptr;
         const int64_t rows = (M + kSlopeRows - 1) / kSlopeRows, tiles = (N + 255) / 256;
         if (rows * tiles > kMaxGrid) return ACRL_ERR_INVALID_ARG;
@@ -174,15 +417,23 @@ extern "C" acrl_status acrl_linear_backward(const acrl_bf16* dy, int64_t M, int6
     } else if (dbias && N > 0) {
         if (cudaMemsetAsync(dbias, 0, size_t(N) * 4, s) != cudaSuccess) return launch_status();
     }
-    // without rows, or without columns of dy, the sums are empty: K = 0 below
+    // without rows, or without columns of dy, the sums are empty
     if (has_dx) {
-        const Epilogue e{nullptr, nullptr, false, false, dx_dtype == ACRL_F32, 0, 0, lddx, nullptr, dx};
-        st = product<ACRL_ACT_NONE>(View{g, false, ldg, 1}, View{w, false, 1, ldw}, M, K, has_g ? N : 0, e, s);
+        Finish f = {};
+        f.out = dx;
+        f.ldo = lddx;
+        f.out_f32 = dx_dtype == ACRL_F32;
+        st = product(Matrix{g, M, ldg, false, 1, M * ldg}, Matrix{w, K, ldw, true, 1, N * ldw}, has_g ? N : 0, f, base + parts.parts,
+                     dev_flags, s);
         if (st != ACRL_OK) return st;
     }
     if (has_dw) {
-        const Epilogue e{nullptr, nullptr, false, false, dw_dtype == ACRL_F32, 0, 0, lddw, nullptr, dw};
-        st = product<ACRL_ACT_NONE>(View{g, false, 1, ldg}, View{x, false, 1, ldx}, N, K, has_g ? M : 0, e, s);
+        Finish f = {};
+        f.out = dw;
+        f.ldo = lddw;
+        f.out_f32 = dw_dtype == ACRL_F32;
+        st = product(Matrix{g, N, ldg, true, 1, M * ldg}, Matrix{x, K, ldx, true, 1, M * ldx}, has_g ? M : 0, f, base + parts.parts,
+                     dev_flags, s);
     }
     return st;
 }
