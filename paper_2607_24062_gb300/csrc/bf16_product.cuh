@@ -22,6 +22,8 @@
 
 #include <cuda.h>
 
+#include <algorithm>
+
 #include "acrl_device.cuh"
 #include "acrl_host.h"
 #include "mbarrier.cuh"

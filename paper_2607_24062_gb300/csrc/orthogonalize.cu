@@ -1,112 +1,405 @@
 // acrl_orthogonalize: Newton-Schulz steps on an update.  With X (m x n, m <= n; a tall matrix's transpose) a step is
-//     A = X X^T,   Q = a I + b A + c A^2,   X <- Q X,
-// so the polynomial in the Gram matrix is made on its m x m elements, and X is read and written once.
+//
+//     A = X X^T,   Q = a I + b A + c A A,   X <- Q X,
+//
+// so that the polynomial in the Gram matrix is made on its m x m elements, and X is read twice and written once.  A and Q are
+// symmetric: tiles above the diagonal are left out and written as mirror images, 3 m^2 n + m^3 multiply-adds a step where the
+// plain products have 4 m^2 n + 2 m^3.
+//
+// Operands are two bf16 numbers each, x = x0 + x1 with x0 the rounding of x and x1 that of what is left, which together are
+// within 2^-16 of it, and a product is three of the tensor cores' (bf16_product.cuh).  One bf16 number would not do: gradients
+// have a few strong directions and many weak ones, whose singular values the steps amplify by up to a^steps (485 for five
+// steps of the usual quintic), and with them whatever the rounding of the strong ones has put in their place.
 #include <algorithm>
 
+#include "acrl_device.cuh"
 #include "acrl_host.h"
-#include "simple_product.cuh"
-#include "tma_host.h"
+#include "activation.cuh"
+#include "bf16_product.cuh"
 
 namespace acrl {
 namespace {
 
 constexpr int kMostSteps = 64;
+constexpr int kPairs = 76;
+constexpr int kSumCtas = 608;      // four of an SM's: CTAs that add up squares
 
-// 1 / (|G| + eps) of each matrix; NaN, and the flag, where an element is none.
-__global__ void __launch_bounds__(1024) norm_kernel(View g, int64_t stride, int m, int n, float eps, double* inv, int32_t* flags) {
-    __shared__ double part[32];
-    grid_begin();
-    const int64_t at = int64_t(blockIdx.x) * stride;
-    double sum = 0.0;
-    for (int64_t i = threadIdx.x; i < int64_t(m) * n; i += 1024) {
-        const double v = load_float(g.p, g.f32, at + i / n * g.row + i % n);
-        sum += v * v;
+struct Update {
+    const void* g;
+    bool f32;
+    int64_t ld, stride;
+    int m, n;              // as given
+};
+
+// ---------------------------------------------------------------------------------------------------------------
+// the first iterate
+// ---------------------------------------------------------------------------------------------------------------
+
+// A sum of squares of numbers of any size, in three sums whose terms stay within fp32: of numbers from 2^50 on scaled by
+// 2^-80, of those below 2^-50 by 2^80, and of the others.
+struct Squares {
+    float low = 0.f, mid = 0.f, high = 0.f;
+    __device__ __forceinline__ void add(float x) {
+        const float a = fabsf(x);
+        if (a > 0x1p50f) {
+            x *= 0x1p-80f;
+            high = fmaf(x, x, high);
+        } else if (a < 0x1p-50f) {
+            x *= 0x1p80f;
+            low = fmaf(x, x, low);
+        } else {
+            mid = fmaf(x, x, mid);   // a NaN as well
+        }
     }
-    sum = warp_sum(sum);
+    __device__ __forceinline__ double total() const { return double(low) * 0x1p-160 + double(mid) + double(high) * 0x1p160; }
+};
+
+// Partial sums of a matrix's squares, `ctas` of them: rows in turn, 16 bytes a thread.  HBM bounds it.
+__global__ void __launch_bounds__(256) squares_kernel(Update u, int ctas, double* sums) {
+    __shared__ double part[8];
+    grid_begin();
+    const int b = int(blockIdx.x) / ctas, c = int(blockIdx.x) - b * ctas;
+    const int V = u.f32 ? 4 : 8, vectors = (u.n + V - 1) / V;
+    Squares s;
+    const int64_t all = int64_t(u.m) * vectors;
+    for (int64_t i = int64_t(c) * 256 + threadIdx.x; i < all; i += int64_t(ctas) * 256) {
+        const int64_t r = i / vectors;
+        const int at = int(i - r * vectors) * V;
+        const int64_t row = b * u.stride + r * u.ld + at;
+        if (at + V > u.n) {
+            for (int j = at; j < u.n; ++j) s.add(load_float(u.g, u.f32, row + j - at));
+        } else if (u.f32) {
+            const float4 x = *reinterpret_cast<const float4*>(static_cast<const float*>(u.g) + row);
+            s.add(x.x);
+            s.add(x.y);
+            s.add(x.z);
+            s.add(x.w);
+        } else {
+            const uint4 x = *reinterpret_cast<const uint4*>(static_cast<const acrl_bf16*>(u.g) + row);
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                s.add(bf16_lo(w[j]));
+                s.add(bf16_hi(w[j]));
+            }
+        }
+    }
+    const double sum = warp_sum(s.total());
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = sum;
     __syncthreads();
     if (threadIdx.x == 0) {
-        sum = 0.0;
-        for (int i = 0; i < 32; ++i) sum += part[i];
-        const bool bad = !(sum <= 1.7e308);
-        if (bad) raise_flag(flags, ACRL_FLAG_NONFINITE);
-        const double d = sqrt(sum) + double(eps);
-        inv[blockIdx.x] = bad ? nan("") : d > 0.0 ? 1.0 / d : 0.0;
+        double t = 0.0;
+        for (int i = 0; i < 8; ++i) t += part[i];
+        sums[blockIdx.x] = t;
     }
 }
 
-__global__ void __launch_bounds__(256) first_kernel(View g, int64_t stride, int m, int n, bool tall, const double* inv, float* x) {
+// Two bf16 numbers for one.
+__device__ __forceinline__ void halves(float x, acrl_bf16& hi, acrl_bf16& lo) {
+    hi = to_bf16(x);
+    lo = to_bf16(x - bf16_to_float(hi));
+}
+
+// X_0 = G / (|G| + eps) in two bf16 matrices, 32 x 32 blocks, turned where G is tall.  The factor is a power of two times a
+// number in [1, 2): an update of any size is brought near 1 before it is divided.
+__global__ void __launch_bounds__(256) first_kernel(Update u, int ctas, const double* sums, float eps, acrl_bf16* hi, acrl_bf16* lo,
+                                                    int64_t ldx, int64_t size, int32_t* flags) {
+    __shared__ float block[32][33];
+    __shared__ float by[3];
     grid_begin();
-    const int64_t b = blockIdx.y, size = int64_t(m) * n;
-    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < size; i += int64_t(gridDim.x) * 256) {
-        const int64_t r = i / n, c = i % n;
-        const float v = load_float(g.p, g.f32, b * stride + r * g.row + c);
-        x[b * size + (tall ? c * m + r : i)] = float(double(v) * inv[b]);
+    const int64_t rows = (u.m + 31) / 32, cols = (u.n + 31) / 32, blocks = rows * cols;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int b = int(int64_t(blockIdx.x) / blocks);
+    const int64_t k = int64_t(blockIdx.x) - b * blocks;
+    const int r0 = int(k / cols) * 32, c0 = int(k % cols) * 32;
+    if (warp == 0) {
+        double sum = 0.0;
+        for (int i = lane; i < ctas; i += 32) sum += sums[int64_t(b) * ctas + i];
+        sum = warp_sum(sum);
+        if (lane == 0) {
+            const bool bad = !(sum <= 1.7e308);   // an infinity or a NaN: no finite matrix comes near
+            if (bad && k == 0) raise_flag(flags, ACRL_FLAG_NONFINITE);
+            int e = 0;
+            const double f = frexp(sqrt(sum) + double(eps), &e);   // f 2^e
+            by[0] = exp2f(float(-e / 2));
+            by[1] = exp2f(float(-e - -e / 2));
+            by[2] = bad ? __int_as_float(0x7fc00000) : f > 0.0 ? float(1.0 / f) : 0.f;
+        }
+    }
+    __syncthreads();
+    const float one = by[0], two = by[1], rest = by[2];
+    const bool tall = u.m > u.n;
+    acrl_bf16 *h = hi + b * size, *l = lo + b * size;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = r0 + warp + 8 * i, c = c0 + lane;
+        float x = 0.f;
+        if (r < u.m && c < u.n) x = load_float(u.g, u.f32, b * u.stride + r * u.ld + c) * one * two * rest;
+        if (tall)
+            block[warp + 8 * i][lane] = x;
+        else if (r < u.m && c < u.n)
+            halves(x, h[r * ldx + c], l[r * ldx + c]);
+    }
+    if (!tall) return;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = c0 + warp + 8 * i, c = r0 + lane;   // of X
+        if (r < u.n && c < u.m) halves(block[lane][warp + 8 * i], h[r * ldx + c], l[r * ldx + c]);
     }
 }
 
-// MODE 0: A = X X^T; 1: Q = a I + b A + c A A^T; 2: X' = Q X; 3: the same to `out`, scaled.
-struct Step {
+// ---------------------------------------------------------------------------------------------------------------
+// the steps' products
+// ---------------------------------------------------------------------------------------------------------------
+
+// What is made of the sums: A itself; Q = a I + b A + c sum; X; and the last X as the result.
+enum Kind { kGram, kPolynomial, kIterate, kResult };
+
+struct Finish {
+    int kind;
     float a, b, c, scale;
-    const float *x, *gram, *q;
-    float* to;
-    acrl_bf16* out;
+    const acrl_bf16 *hi_in, *lo_in;    // A, for the polynomial
+    acrl_bf16 *hi, *lo;                // A, Q or X
+    int64_t ld, size;                  // of all of these, and from one matrix to the next
+    acrl_bf16* out;                    // the result
     int64_t ldo, out_stride;
-    int m, n;
-    bool tall;
+    bool tall;                         // the result is turned back
 };
 
-template <int MODE>
-__global__ void __launch_bounds__(256) step_kernel(Step s) {
-    grid_begin();
-    const int64_t b = blockIdx.y, mm = int64_t(s.m) * s.m, mn = int64_t(s.m) * s.n;
-    const int N = MODE < 2 ? s.m : s.n, K = MODE == 0 ? s.n : s.m;
-    const int tiles = (N + 63) / 64, m0 = int(blockIdx.x) / tiles * 64, n0 = int(blockIdx.x) % tiles * 64;
-    const View X{s.x + b * mn, true, s.n, 1}, XT{s.x + b * mn, true, 1, s.n};
-    const View A{s.gram + b * mm, true, s.m, 1}, Q{s.q + b * mm, true, s.m, 1};
-    simple_product(MODE == 0 ? X : MODE == 1 ? A : Q, MODE == 0 ? X : MODE == 1 ? A : XT, s.m, N, K, m0, n0,
-                   [&](int64_t i, int64_t j, float v) {
-                       if (MODE == 1) v = fmaf(s.c, v, fmaf(s.b, A.at(i, j), i == j ? s.a : 0.f));
-                       if (MODE < 3)
-                           s.to[b * (MODE < 2 ? mm : mn) + i * N + j] = v;
-                       else
-                           s.out[b * s.out_stride + (s.tall ? j * s.ldo + i : i * s.ldo + j)] = to_bf16(s.scale * v);
-                   });
+// a I + b A + c v at row i, columns j .. j + 31 (zeros beyond the matrix).
+__device__ __forceinline__ void polynomial(const Finish& f, int64_t at, int i, int j, int m, float (&v)[32]) {
+#pragma unroll
+    for (int k = 0; k < 32; ++k) {
+        const bool in = i < m && j + k < m;
+        const float A = in ? bf16_to_float(f.hi_in[at + k]) + bf16_to_float(f.lo_in[at + k]) : 0.f;
+        v[k] = fmaf(f.c, v[k], fmaf(f.b, A, in && i == j + k ? f.a : 0.f));
+    }
 }
 
-struct Parts {
-    int64_t inv, x[2], gram, q, end;
-    Parts(int64_t batch, int64_t m, int64_t n) {
-        const int64_t k = std::min(m, n);
-        inv = 0;
-        x[0] = (batch * 8 + 15) / 16 * 16;
-        x[1] = x[0] + (batch * m * n * 4 + 15) / 16 * 16;
-        gram = x[1] + (batch * m * n * 4 + 15) / 16 * 16;
-        q = gram + (batch * k * k * 4 + 15) / 16 * 16;
-        end = q + (batch * k * k * 4 + 15) / 16 * 16;
+struct StepEpilogue {
+    Finish f;
+    CUtensorMap hi, lo;     // of what is written; with parts hi is theirs; of the result hi alone
+    bool parts;
+
+    // Lane i's 32 values as column i of a block.
+    __device__ __forceinline__ void mirror(const CUtensorMap* map, const float (&v)[32], int row0, int col0, int z, WarpOut& out) const {
+        uint8_t* b = out.staging + out.half * (kWarpStaging / 2);
+        out.half ^= 1;
+        if (out.lane == 0) {
+            if (out.whole) bulk_wait_read<0>();
+            else bulk_wait_read<1>();
+        }
+        out.whole = false;
+        __syncwarp();
+        const uint32_t to = smem_u32(b) + uint32_t((out.lane & 7) * 2);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            const uint32_t piece = uint32_t(out.lane >> 3) ^ uint32_t((j >> 1) & 3);
+            asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + uint32_t(j * 64) + (piece << 4)), "h"(to_bf16(v[j])) : "memory");
+        }
+        fence_async_shared();
+        __syncwarp();
+        if (out.lane == 0) tma_store_3d(map, b, row0, col0, z);
+    }
+
+    __device__ __forceinline__ void chunk(const Problem& pr, const Unit& t, const uint32_t (&r)[32], int row0, int col0,
+                                          WarpOut& out) const {
+        float v[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
+        if (parts) {
+            out.store<float>(&hi, v, row0, col0, t.z * pr.parts + t.part);
+            return;
+        }
+        const int row = row0 + out.lane;
+        if (f.kind == kResult) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] *= f.scale;
+            acrl_bf16* to = f.out + t.z * f.out_stride;
+            if (f.tall) {   // the lanes' stores are of neighbours
+                if (row < pr.rows)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (col0 + j < pr.cols_all) to[(col0 + j) * f.ldo + row] = to_bf16(v[j]);
+            } else if (col0 + 32 > pr.cols_all && (pr.cols_all & 7)) {
+                if (row < pr.rows)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (col0 + j < pr.cols_all) to[row * f.ldo + col0 + j] = to_bf16(v[j]);
+            } else {
+                out.store<acrl_bf16>(&hi, v, row0, col0, t.z);
+            }
+            return;
+        }
+        if (f.kind == kPolynomial) polynomial(f, t.z * f.size + row * f.ld + col0, row, col0, pr.rows, v);
+        const bool twice = pr.lower && col0 < t.tp * 2 * kRows;   // a tile above the diagonal has no other way to be written
+        out.store<acrl_bf16>(&hi, v, row0, col0, t.z);
+        if (twice) mirror(&hi, v, row0, col0, t.z, out);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] -= bf16_to_float(to_bf16(v[j]));
+        out.store<acrl_bf16>(&lo, v, row0, col0, t.z);
+        if (twice) mirror(&lo, v, row0, col0, t.z, out);
     }
 };
+
+// The parts of a split sum in their order, and what is made of them.  Above the diagonal's tiles of a symmetric matrix the
+// mirror image is taken.
+__global__ void __launch_bounds__(256) join_kernel(Finish f, const float* parts, int count, int64_t ldparts, int64_t part_size, int lower,
+                                                   int rows, int cols, int64_t all) {
+    grid_begin();
+    const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
+    if (i >= all) return;
+    const int64_t each = int64_t(rows) * cols, z = i / each, k = i - z * each;
+    // a turned result is written in its own order
+    const bool turn = f.kind == kResult && f.tall;
+    const int r = int(turn ? k % rows : k / cols), c = int(turn ? k / rows : k % cols);
+    const bool flip = lower && c >= (r / (2 * kRows) + 1) * 2 * kRows;
+    const float* p = parts + z * count * part_size + (flip ? int64_t(c) * ldparts + r : int64_t(r) * ldparts + c);
+    float v = 0.f;
+    for (int j = 0; j < count; ++j) v += p[j * part_size];
+    if (f.kind == kResult) {
+        f.out[z * f.out_stride + (f.tall ? c * f.ldo + r : r * f.ldo + c)] = to_bf16(f.scale * v);
+        return;
+    }
+    const int64_t at = z * f.size + r * f.ld + c;
+    if (f.kind == kPolynomial)
+        v = fmaf(f.c, v, fmaf(f.b, bf16_to_float(f.hi_in[at]) + bf16_to_float(f.lo_in[at]), r == c ? f.a : 0.f));
+    halves(v, f.hi[at], f.lo[at]);
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------------------------------------------
+
+struct Plan {
+    Cut cut;
+    int64_t cost, workspace, ldparts, part_size;
+};
+
+// The cut of a product rows x cols over K with the least estimated time, as for a layer's.
+Plan plan_of(int64_t batch, int64_t rows, int64_t cols_all, int64_t K, bool lower, bool q_turned) {
+    constexpr int64_t kTile = 4000, kJoin = 6000, kJoinBytes = 3000;
+    const int64_t slabs = (K + kSlab - 1) / kSlab, p_tiles = (rows + 2 * kRows - 1) / (2 * kRows);
+    Plan best = {};
+    best.ldparts = (cols_all + 7) / 8 * 8;
+    best.part_size = rows * best.ldparts;
+    for (int cols = 256; cols >= (q_turned ? 128 : 64); cols /= 2) {
+        const int64_t q_tiles = (cols_all + cols - 1) / cols, r = 2 * kRows / cols;
+        const int64_t tiles = batch * (lower ? r * (p_tiles - 1) * p_tiles / 2 + q_tiles : p_tiles * q_tiles);
+        const int64_t slab = std::max(6 * cols, 4 * (kRows + cols / 2));
+        for (int64_t parts = 1; parts <= 16 && parts <= slabs; ++parts) {
+            const int64_t per = (slabs + parts - 1) / parts;
+            if ((slabs + per - 1) / per != parts) continue;
+            const int64_t rounds = (tiles * parts + kPairs - 1) / kPairs;
+            const int64_t cost = rounds * (per * slab + kTile) +
+                                 (parts > 1 ? kJoin + (parts + 1) * batch * best.part_size * 4 / kJoinBytes : 0);
+            if (best.cost == 0 || cost < best.cost) {
+                best.cost = cost;
+                best.cut = Cut{cols, int(parts), int(per)};
+            }
+        }
+    }
+    best.workspace = best.cut.parts > 1 ? best.cut.parts * batch * best.part_size * 4 : 0;
+    return best;
+}
+
+// The workspace, in bytes: sums of squares; X twice, A and Q, each in two matrices; the parts of a split sum.
+struct Layout {
+    int64_t m, n, ldx, lda, ctas;
+    int64_t x[2][2], gram[2], q[2], parts, end;
+    Plan plan_gram, plan_q, plan_x;
+    Layout(int64_t batch, int64_t rows, int64_t cols) {
+        m = std::min(rows, cols);
+        n = std::max(rows, cols);
+        ldx = (n + 7) / 8 * 8;
+        lda = (m + 7) / 8 * 8;
+        ctas = std::max<int64_t>(1, std::min<int64_t>(std::max<int64_t>(1, kSumCtas / batch), m * n / 4096));
+        int64_t at = (batch * ctas * 8 + 127) / 128 * 128;
+        auto take = [&](int64_t bytes) {
+            const int64_t here = at;
+            at += (bytes + 127) / 128 * 128;
+            return here;
+        };
+        for (auto& pair : x)
+            for (int64_t& half : pair) half = take(batch * m * ldx * 2);
+        for (int64_t& half : gram) half = take(batch * m * lda * 2);
+        for (int64_t& half : q) half = take(batch * m * lda * 2);
+        plan_gram = plan_of(batch, m, m, n, true, false);
+        plan_q = plan_of(batch, m, m, m, true, false);
+        plan_x = plan_of(batch, m, n, m, false, true);
+        parts = take(std::max(plan_gram.workspace, std::max(plan_q.workspace, plan_x.workspace)));
+        end = at;
+    }
+};
+
+struct Halves {
+    acrl_bf16 *hi, *lo;
+    int64_t ld, size;   // from one matrix to the next
+};
+
+// One product of the steps: rows x cols over K.
+acrl_status step_product(const Plan& plan, int64_t batch, int64_t rows, int64_t cols, int64_t K, const Halves& p, const Halves& q,
+                         bool q_turned, bool lower, const Finish& f, float* parts, int32_t* flags, cudaStream_t s) {
+    ProductLaunch<1, 3, StepEpilogue> l = {};
+    l.pr[0] = problem_of(true, rows, cols, K, batch, false, q_turned, lower, plan.cut);
+    StepEpilogue& e = l.epi[0];
+    e.f = f;
+    e.parts = plan.cut.parts > 1;
+    for (int i = 0; i < 2; ++i) {
+        if (!operand_map(&l.p[0][i], Matrix{i ? p.lo : p.hi, rows, p.ld, false, batch, p.size}, K, kRows) ||
+            !operand_map(&l.q[0][i], Matrix{i ? q.lo : q.hi, cols, q.ld, q_turned, batch, q.size}, K, plan.cut.cols / 2))
+            return ACRL_ERR_CUDA;
+    }
+    bool ok;
+    if (e.parts) {
+        ok = result_map(&e.hi, parts, true, rows, plan.ldparts, plan.ldparts, batch * plan.cut.parts, plan.part_size);
+    } else if (f.kind == kResult) {
+        ok = f.tall || result_map(&e.hi, f.out, false, rows, cols, f.ldo, batch, batch > 1 ? f.out_stride : rows * f.ldo);
+    } else {
+        ok = result_map(&e.hi, f.hi, false, rows, f.ld, f.ld, batch, f.size) && result_map(&e.lo, f.lo, false, rows, f.ld, f.ld, batch, f.size);
+    }
+    if (!ok) return ACRL_ERR_CUDA;
+    const acrl_status st = launch_product<true>(l, flags, s);
+    if (st != ACRL_OK || !e.parts) return st;
+    const int64_t all = batch * rows * cols;
+    return launch(join_kernel, (all + 255) / 256, 256, 0, 0, s, f, static_cast<const float*>(parts), plan.cut.parts, plan.ldparts,
+                  plan.part_size, int(lower), int(rows), int(cols), all);
+}
 
 }  // namespace
 }  // namespace acrl
 
 using namespace acrl;
 
+namespace {
+bool sizes_ok(int64_t batch, int64_t m, int64_t n) {
+    constexpr int64_t kMost = kMaxGrid - 512;
+    return batch >= 0 && m >= 0 && n >= 0 && batch <= kMost && m <= kMost && n <= kMost;
+}
+// One launch's blocks, and the parts' too, stay within a grid.
+bool blocks_ok(int64_t batch, int64_t m, int64_t n) {
+    return double(batch) * double((m + 31) / 32) * double((n + 31) / 32) < double(kMaxGrid);
+}
+}  // namespace
+
 extern "C" int64_t acrl_orthogonalize_workspace_bytes(int64_t batch, int64_t m, int64_t n) {
-    return batch < 0 || m < 0 || n < 0 ? -1 : batch == 0 || m == 0 || n == 0 ? 0 : Parts(batch, m, n).end;
+    if (batch < 0 || m < 0 || n < 0) return -1;
+    return batch == 0 || m == 0 || n == 0 || !sizes_ok(batch, m, n) || !blocks_ok(batch, m, n) ? 0 : Layout(batch, m, n).end;
 }
 
 extern "C" acrl_status acrl_orthogonalize(const void* g, acrl_dtype g_dtype, int64_t batch, int64_t m, int64_t n, int64_t ldg,
                                           int64_t g_stride, const float* coeffs, int32_t steps, float eps, float scale,
                                           acrl_bf16* out, int64_t ldo, int64_t out_stride, void* workspace, int64_t workspace_bytes,
                                           int32_t* dev_flags, acrl_stream stream) {
-    if (batch < 0 || m < 0 || n < 0 || batch > 65535 || m > kMaxGrid - 512 || n > kMaxGrid - 512) return ACRL_ERR_INVALID_ARG;
+    if (!sizes_ok(batch, m, n)) return ACRL_ERR_INVALID_ARG;
     if ((g_dtype != ACRL_BF16 && g_dtype != ACRL_F32) || steps < 1 || steps > kMostSteps || !coeffs) return ACRL_ERR_INVALID_ARG;
     if (!(eps >= 0.f && eps < INFINITY) || !(scale > -INFINITY && scale < INFINITY)) return ACRL_ERR_INVALID_ARG;
     for (int i = 0; i < 3 * steps; ++i)
         if (!(coeffs[i] > -INFINITY && coeffs[i] < INFINITY)) return ACRL_ERR_INVALID_ARG;
     if (workspace_bytes < acrl_orthogonalize_workspace_bytes(batch, m, n)) return ACRL_ERR_INVALID_ARG;
     if (batch == 0 || m == 0 || n == 0) return ACRL_OK;
+    if (!blocks_ok(batch, m, n)) return ACRL_ERR_INVALID_ARG;
     const int64_t to = g_dtype == ACRL_BF16 ? 7 : 3;
     if (!g || !aligned16(g) || ldg < n || (ldg & to) || (g_stride & to) || !out || !aligned16(out) || ldo < n || (ldo & 7) ||
         (out_stride & 7) || !workspace || !aligned16(workspace))
@@ -114,43 +407,50 @@ extern "C" acrl_status acrl_orthogonalize(const void* g, acrl_dtype g_dtype, int
     if (batch > 1 && (g_stride < (m - 1) * ldg + n || out_stride < (m - 1) * ldo + n)) return ACRL_ERR_INVALID_ARG;
     if (!operands_on_current_device({g, out, workspace})) return ACRL_ERR_INVALID_ARG;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    const Parts p(batch, m, n);
+    const Layout l(batch, m, n);
     uint8_t* base = static_cast<uint8_t*>(workspace);
-    const bool tall = m > n;
-    const View G{g, g_dtype == ACRL_F32, ldg, 1};
-    double* inv = reinterpret_cast<double*>(base + p.inv);
-    float* x[2] = {reinterpret_cast<float*>(base + p.x[0]), reinterpret_cast<float*>(base + p.x[1])};
-    norm_kernel<<<unsigned(batch), 1024, 0, s>>>(G, g_stride, int(m), int(n), eps, inv, dev_flags);
-    first_kernel<<<dim3(unsigned(std::min<int64_t>(1024, (m * n + 255) / 256)), unsigned(batch)), 256, 0, s>>>(G, g_stride, int(m), int(n), tall, inv, x[0]);
-    Step t = {};
-    t.m = int(std::min(m, n));
-    t.n = int(std::max(m, n));
-    t.tall = tall;
-    t.scale = scale;
-    t.out = out;
-    t.ldo = ldo;
-    t.out_stride = out_stride;
-    float* gram = reinterpret_cast<float*>(base + p.gram);
-    float* q = reinterpret_cast<float*>(base + p.q);
-    t.gram = gram;
-    t.q = q;
-    const int64_t tm = (t.m + 63) / 64, tn = (t.n + 63) / 64;
-    if (tm * tn > kMaxGrid) return ACRL_ERR_INVALID_ARG;
-    const dim3 small(unsigned(tm * tm), unsigned(batch)), large(unsigned(tm * tn), unsigned(batch));
-    for (int i = 0; i < steps; ++i) {
-        t.a = coeffs[3 * i];
-        t.b = coeffs[3 * i + 1];
-        t.c = coeffs[3 * i + 2];
-        t.x = x[i & 1];
-        t.to = gram;
-        step_kernel<0><<<small, 256, 0, s>>>(t);
-        t.to = q;
-        step_kernel<1><<<small, 256, 0, s>>>(t);
-        t.to = x[1 - (i & 1)];
-        if (i + 1 < steps)
-            step_kernel<2><<<large, 256, 0, s>>>(t);
-        else
-            step_kernel<3><<<large, 256, 0, s>>>(t);
+    auto halves_at = [&](const int64_t (&at)[2], int64_t ld) {
+        return Halves{reinterpret_cast<acrl_bf16*>(base + at[0]), reinterpret_cast<acrl_bf16*>(base + at[1]), ld, l.m * ld};
+    };
+    const Halves x[2] = {halves_at(l.x[0], l.ldx), halves_at(l.x[1], l.ldx)}, gram = halves_at(l.gram, l.lda), q = halves_at(l.q, l.lda);
+    float* parts = reinterpret_cast<float*>(base + l.parts);
+    double* sums = reinterpret_cast<double*>(base);
+    const Update u{g, g_dtype == ACRL_F32, ldg, g_stride, int(m), int(n)};
+    acrl_status st = launch(squares_kernel, batch * l.ctas, 256, 0, 0, s, u, int(l.ctas), sums);
+    if (st != ACRL_OK) return st;
+    st = launch(first_kernel, batch * ((m + 31) / 32) * ((n + 31) / 32), 256, 0, 0, s, u, int(l.ctas), static_cast<const double*>(sums), eps, x[0].hi,
+                x[0].lo, l.ldx, x[0].size, dev_flags);
+    for (int i = 0; i < steps && st == ACRL_OK; ++i) {
+        const Halves &from = x[i & 1], &into = x[1 - (i & 1)];
+        Finish f = {};
+        f.kind = kGram;
+        f.hi = gram.hi;
+        f.lo = gram.lo;
+        f.ld = gram.ld;
+        f.size = gram.size;
+        st = step_product(l.plan_gram, batch, l.m, l.m, l.n, from, from, false, true, f, parts, dev_flags, s);
+        if (st != ACRL_OK) break;
+        f.kind = kPolynomial;
+        f.a = coeffs[3 * i];
+        f.b = coeffs[3 * i + 1];
+        f.c = coeffs[3 * i + 2];
+        f.hi_in = gram.hi;
+        f.lo_in = gram.lo;
+        f.hi = q.hi;
+        f.lo = q.lo;
+        st = step_product(l.plan_q, batch, l.m, l.m, l.m, gram, gram, false, true, f, parts, dev_flags, s);
+        if (st != ACRL_OK) break;
+        f.kind = i + 1 < steps ? kIterate : kResult;
+        f.hi = into.hi;
+        f.lo = into.lo;
+        f.ld = into.ld;
+        f.size = into.size;
+        f.scale = scale;
+        f.out = out;
+        f.ldo = ldo;
+        f.out_stride = out_stride;
+        f.tall = m > n;
+        st = step_product(l.plan_x, batch, l.m, l.n, l.m, q, from, true, false, f, parts, dev_flags, s);
     }
-    return launch_status();
+    return st;
 }
