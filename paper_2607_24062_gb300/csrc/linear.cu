@@ -1,85 +1,15 @@
 // acrl_linear and acrl_linear_backward: a bf16 layer with bias, activation and residual, and its gradients.
 #include <algorithm>
-#include <type_traits>
 
 #include "acrl_host.h"
-#include "activation.cuh"
 #include "bf16_product.cuh"
+#include "linear.cuh"
 
 namespace acrl {
 namespace {
 
-constexpr int64_t kMostSize = kMaxGrid - 512;
 constexpr int kPairs = 76;           // of SMs: what a cut is made for
 constexpr int64_t kAloneRows = 128;  // rows that become a CTA's columns
-
-template <typename F>
-__host__ __device__ __forceinline__ acrl_status by_act(int a, F f) {
-    switch (a) {
-        case ACRL_ACT_NONE: return f(std::integral_constant<int, ACRL_ACT_NONE>{});
-        case ACRL_ACT_RELU: return f(std::integral_constant<int, ACRL_ACT_RELU>{});
-        case ACRL_ACT_GELU: return f(std::integral_constant<int, ACRL_ACT_GELU>{});
-        case ACRL_ACT_GELU_TANH: return f(std::integral_constant<int, ACRL_ACT_GELU_TANH>{});
-        case ACRL_ACT_SILU: return f(std::integral_constant<int, ACRL_ACT_SILU>{});
-    }
-    return ACRL_ERR_INVALID_ARG;
-}
-
-// What follows the sum: out = f(sum + bias) + residual.
-struct Finish {
-    const void *bias, *residual;
-    void* out;
-    acrl_bf16* pre;
-    int64_t ldr, ldp, ldo;
-    int act;
-    bool bias_f32, residual_f32, out_f32;
-};
-
-__device__ __forceinline__ void store_float(void* p, bool f32, int64_t i, float v) {
-    if (f32)
-        static_cast<float*>(p)[i] = v;
-    else
-        static_cast<acrl_bf16*>(p)[i] = to_bf16(v);
-}
-
-template <int N>
-__device__ __forceinline__ void apply(int which, float (&v)[N]) {
-    by_act(which, [&](auto a) {
-        if constexpr (a != ACRL_ACT_NONE)
-#pragma unroll
-            for (int j = 0; j < N; ++j) v[j] = act<a>(v[j]);
-        return ACRL_OK;
-    });
-}
-
-// N values of a row from column c on, as fp32; N a multiple of eight and c of four.
-template <int N>
-__device__ __forceinline__ void load_row(const void* p, bool f32, int64_t row, int c, int cols, float (&v)[N]) {
-    if (c + N > cols) {
-#pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = c + j < cols ? load_float(p, f32, row + c + j) : 0.f;
-    } else if (f32) {
-        const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + row + c);
-#pragma unroll
-        for (int j = 0; j < N / 4; ++j) {
-            const float4 x = q[j];
-            v[4 * j] = x.x;
-            v[4 * j + 1] = x.y;
-            v[4 * j + 2] = x.z;
-            v[4 * j + 3] = x.w;
-        }
-    } else {
-        const uint2* q = reinterpret_cast<const uint2*>(static_cast<const acrl_bf16*>(p) + row + c);
-#pragma unroll
-        for (int j = 0; j < N / 4; ++j) {
-            const uint2 x = q[j];
-            v[4 * j] = bf16_lo(x.x);
-            v[4 * j + 1] = bf16_hi(x.x);
-            v[4 * j + 2] = bf16_lo(x.y);
-            v[4 * j + 3] = bf16_hi(x.y);
-        }
-    }
-}
 
 // A tile's accumulators on their way out.  Pair: a lane has a row of the result and 32 of its columns.  Alone: p is the
 // weight, a lane has a column of the result and 32 rows, and a warp's stores are of neighbours.
@@ -292,34 +222,98 @@ acrl_status product(const Matrix& x, const Matrix& w, int64_t K, const Finish& f
     return plan.alone ? run_product<false>(plan, x, w, K, f, parts, flags, s) : run_product<true>(plan, x, w, K, f, parts, flags, s);
 }
 
-// g = dy f'(u), rounded, and the columns' sums of the unrounded.
-constexpr int kSlopeRows = 256;   // of a CTA
+// g = dy f'(u), rounded, and the columns' sums of the unrounded.  A lane has eight columns, a warp 256, and the eight warps of a
+// CTA take its rows in turn, four at a time in flight; their sums meet in shared memory.  HBM bounds it, 6 bytes an element
+// (2 without an activation).
+constexpr int kSlopeCols = 256, kSlopeAhead = 4;
+
+// Rows of a CTA: as many as still make a few CTAs for each SM.
+int64_t slope_rows(int64_t M, int64_t N) { return (M + 127) / 128 * ((N + kSlopeCols - 1) / kSlopeCols) >= 1024 ? 128 : 32; }
 
 template <int ACT>
 __global__ void __launch_bounds__(256) slope_kernel(const acrl_bf16* dy, int64_t lddy, const acrl_bf16* pre, int64_t ldp, int M,
-                                                    int N, acrl_bf16* g, int64_t ldg, float* sums) {
+                                                    int N, int rows, acrl_bf16* g, int64_t ldg, float* sums, int64_t ldsums) {
+    __shared__ float part[8][kSlopeCols];
     grid_begin();
-    const int tiles = (N + 255) / 256, n = int(blockIdx.x) % tiles * 256 + threadIdx.x, part = int(blockIdx.x) / tiles;
-    const int m0 = part * kSlopeRows;
-    if (n >= N) return;
-    float sum = 0.f;
-    for (int64_t m = m0; m < min(M, m0 + kSlopeRows); ++m) {
-        float v = bf16_to_float(dy[m * lddy + n]);
-        if (ACT != ACRL_ACT_NONE) {
-            v = __fmul_rn(v, act_slope<ACT>(bf16_to_float(pre[m * ldp + n])));   // the same with and without g: no fma into the sum
-            if (g) g[m * ldg + n] = to_bf16(v);
+    const int tiles = (N + kSlopeCols - 1) / kSlopeCols, at = int(blockIdx.x) / tiles;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int c = int(int64_t(blockIdx.x) - int64_t(at) * tiles) * kSlopeCols + lane * 8;
+    const int64_t m0 = int64_t(at) * rows, end = min(int64_t(M), m0 + rows);
+    const bool whole = c + 8 <= N;
+    float sum[8] = {};
+    // g's eight values of a row; beyond the matrix there are zeros in dy, and nothing is stored
+    auto row = [&](int64_t m, const uint4& d, const uint4& u) {
+        const uint32_t dw[4] = {d.x, d.y, d.z, d.w}, uw[4] = {u.x, u.y, u.z, u.w};
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[2 * j] = bf16_lo(dw[j]);
+            v[2 * j + 1] = bf16_hi(dw[j]);
+            if (ACT != ACRL_ACT_NONE) {   // the same with and without g: no fma into the sum
+                v[2 * j] = __fmul_rn(v[2 * j], act_slope<ACT>(bf16_lo(uw[j])));
+                v[2 * j + 1] = __fmul_rn(v[2 * j + 1], act_slope<ACT>(bf16_hi(uw[j])));
+            }
         }
-        sum += v;
+        if (ACT != ACRL_ACT_NONE && g) {
+            acrl_bf16* to = g + m * ldg + c;
+            if (whole) {
+                *reinterpret_cast<uint4*>(to) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
+                                                           pack_bf16x2(v[6], v[7]));
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (c + j < N) to[j] = to_bf16(v[j]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] += v[j];
+    };
+    auto load = [&](const acrl_bf16* p) {
+        if (whole) return *reinterpret_cast<const uint4*>(p);
+        uint32_t w[4] = {};
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (c + j < N) w[j >> 1] |= uint32_t(p[j]) << (j & 1) * 16;
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    };
+    if (c < N) {
+        for (int64_t m = m0 + warp; m < end; m += 8 * kSlopeAhead) {
+            uint4 d[kSlopeAhead], u[kSlopeAhead] = {};
+#pragma unroll
+            for (int i = 0; i < kSlopeAhead; ++i)
+                if (m + 8 * i < end) {
+                    d[i] = load(dy + (m + 8 * i) * lddy + c);
+                    if (ACT != ACRL_ACT_NONE) u[i] = load(pre + (m + 8 * i) * ldp + c);
+                }
+#pragma unroll
+            for (int i = 0; i < kSlopeAhead; ++i)
+                if (m + 8 * i < end) row(m + 8 * i, d[i], u[i]);
+        }
     }
-    if (sums) sums[int64_t(part) * N + n] = sum;
+    if (!sums) return;   // the same for the CTA
+#pragma unroll
+    for (int j = 0; j < 8; ++j) part[warp][lane * 8 + j] = sum[j];
+    __syncthreads();
+    float total = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) total += part[w][threadIdx.x];
+    sums[at * ldsums + (int64_t(blockIdx.x) - int64_t(at) * tiles) * kSlopeCols + threadIdx.x] = total;
 }
 
-__global__ void __launch_bounds__(256) sums_kernel(const float* sums, int parts, int N, float* dbias) {
+// The sums of the parts, 32 columns a CTA: each of eight warps adds up every eighth part, then the eight meet.
+__global__ void __launch_bounds__(256) sums_kernel(const float* sums, int64_t ldsums, int parts, int N, float* dbias) {
+    __shared__ float part[8][32];
     grid_begin();
-    const int n = int(blockIdx.x) * 256 + threadIdx.x;
-    if (n >= N) return;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = int(blockIdx.x) * 32 + lane;   // ldsums is a multiple of 256
     float sum = 0.f;
-    for (int p = 0; p < parts; ++p) sum += sums[int64_t(p) * N + n];
+#pragma unroll 4
+    for (int p = warp; p < parts; p += 8) sum += sums[p * ldsums + n];
+    part[warp][lane] = sum;
+    __syncthreads();
+    if (warp != 0 || n >= N) return;
+    sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) sum += part[w][lane];
     dbias[n] = sum;
 }
 
@@ -328,11 +322,15 @@ bool matrix_ok(const void* p, int64_t cols, int64_t ld) { return p && aligned16(
 
 // The backward's workspace: g, the columns' sums of its parts, the parts of a product's split sum (of one after the other).
 struct BackwardParts {
-    int64_t ldg, sums, parts, end;   // bytes
+    int64_t ldg, rows, count, ldsums;   // of a part of the sums, and how many there are
+    int64_t sums, parts, end;           // bytes
     BackwardParts(int64_t M, int64_t N, int64_t K) {
         ldg = (N + 7) / 8 * 8;
         sums = M * ldg * 2;
-        parts = sums + (M + kSlopeRows - 1) / kSlopeRows * ldg * 4;
+        rows = slope_rows(M, N);
+        count = (M + rows - 1) / rows;
+        ldsums = (N + kSlopeCols - 1) / kSlopeCols * kSlopeCols;
+        parts = sums + count * ldsums * 4;
         end = parts + std::max(plan_of(M, K, N, false, true).workspace, plan_of(N, K, M, true, true).workspace);
     }
 };
@@ -344,7 +342,8 @@ using namespace acrl;
 
 extern "C" int64_t acrl_linear_workspace_bytes(int64_t M, int64_t N, int64_t K) {
     if (M < 0 || N < 0 || K < 0) return -1;
-    return M == 0 || N == 0 || K == 0 || M > kMostSize || N > kMostSize || K > kMostSize ? 0 : plan_of(M, N, K, false, false).workspace;
+    return M == 0 || N == 0 || K == 0 || M > kMostSize || N > kMostSize || K > kMostSize || linear_few_rows(M, N, K) ? 0
+                                                                                                              : plan_of(M, N, K, false, false).workspace;
 }
 
 extern "C" acrl_status acrl_linear(const acrl_bf16* x, int64_t M, int64_t K, int64_t ldx, const acrl_bf16* w, int64_t N, int64_t ldw,
@@ -366,6 +365,7 @@ extern "C" acrl_status acrl_linear(const acrl_bf16* x, int64_t M, int64_t K, int
     if (need > 0 && (!workspace || !aligned16(workspace) || !operands_on_current_device({workspace}))) return ACRL_ERR_INVALID_ARG;
     const Finish f{bias, residual, out, pre, ldr, ldp, ldo, int(act), bias_dtype == ACRL_F32, residual_dtype == ACRL_F32,
                    out_dtype == ACRL_F32};
+    if (linear_few_rows(M, N, K)) return linear_few(x, M, K, ldx, w, N, ldw, f, reinterpret_cast<cudaStream_t>(stream));
     return product(Matrix{x, M, ldx, false, 1, M * ldx}, Matrix{w, N, ldw, false, 1, N * ldw}, K, f, workspace, dev_flags,
                    reinterpret_cast<cudaStream_t>(stream));
 }
@@ -402,17 +402,20 @@ extern "C" acrl_status acrl_linear_backward(const acrl_bf16* dy, int64_t M, int6
     if (has_g && (act != ACRL_ACT_NONE || dbias)) {
         acrl_bf16* to = act == ACRL_ACT_NONE || !(has_dx || has_dw) ? nullptr : reinterpret_cast<acrl_bf16*>(base);
         float* sums = dbias ? reinterpret_cast<float*>(base + parts.sums) : nullptr;
-        const int64_t rows = (M + kSlopeRows - 1) / kSlopeRows, tiles = (N + 255) / 256;
-        if (rows * tiles > kMaxGrid) return ACRL_ERR_INVALID_ARG;
+        const int64_t tiles = (N + kSlopeCols - 1) / kSlopeCols;
+        if (parts.count * tiles > kMaxGrid) return ACRL_ERR_INVALID_ARG;
         st = by_act(act, [&](auto a) {
-            return launch(slope_kernel<a>, rows * tiles, 256, 0, 0, s, dy, lddy, pre, ldp, int(M), int(N), to, parts.ldg, sums);
+            return launch(slope_kernel<a>, parts.count * tiles, 256, 0, 0, s, dy, lddy, pre, ldp, int(M), int(N), int(parts.rows), to,
+                          parts.ldg, sums, parts.ldsums);
         });
         if (st != ACRL_OK) return st;
         if (to) {
             g = to;
             ldg = parts.ldg;
         }
-        if (dbias) st = launch(sums_kernel, tiles, 256, 0, 0, s, static_cast<const float*>(sums), int(rows), int(N), dbias);
+        if (dbias)
+            st = launch(sums_kernel, (N + 31) / 32, 256, 0, 0, s, static_cast<const float*>(sums), parts.ldsums, int(parts.count), int(N),
+                        dbias);
         if (st != ACRL_OK) return st;
     } else if (dbias && N > 0) {
         if (cudaMemsetAsync(dbias, 0, size_t(N) * 4, s) != cudaSuccess) return launch_status();

@@ -1,0 +1,113 @@
+// A layer of up to 16 rows, single tokens first of all: every byte of the weight is used once, and HBM bounds it.  Neither
+// tensor memory nor a ring of copies: their start and end, and the join of a split sum, take longer than the weight of a layer.
+// A CTA has 16 rows of the weight; its eight warps take turns along the sum, 128 columns each, and their sums meet in shared
+// memory.  The products are mma.sync m16n8k16, the weight's rows the 16 and those of x the eight: the pipes of tcgen05 would
+// wait for the same bytes.  A lane loads 16 bytes of a weight's row, eight neighbours of the sum, where the instruction's
+// layout has four pairs: which eight of a slab's 32 columns a lane holds does not matter as long as both operands agree.
+#include "linear.cuh"
+
+namespace acrl {
+namespace {
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kW = 16;          // rows of the weight, of a CTA
+constexpr int kAhead = 4;       // slabs of 32 columns in flight
+constexpr int kTurn = 32 * kAhead;
+
+struct FewArgs {
+    const acrl_bf16 *x, *w;
+    int64_t ldx, ldw;
+    int M, N, K;
+    Finish f;
+};
+
+// Eight numbers of a row from column k on, zeros beyond its end.
+__device__ __forceinline__ uint4 load8(const acrl_bf16* row, int k, int K) {
+    uint32_t v[4] = {};
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (k + j < K) v[j >> 1] |= uint32_t(row[k + j]) << (j & 1) * 16;
+    return make_uint4(v[0], v[1], v[2], v[3]);
+}
+
+__device__ __forceinline__ void mma_16x8(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// T: eights of x's rows.
+template <int T>
+__global__ void __launch_bounds__(kThreads, T == 1 ? 3 : 2) few_kernel(const __grid_constant__ FewArgs A) {
+    __shared__ float red[kWarps][8 * T][kW + 1];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    const int n0 = int(blockIdx.x) * kW, K = A.K;
+    grid_begin();
+    const acrl_bf16* w0 = A.w + int64_t(min(n0 + g, A.N - 1)) * A.ldw;
+    const acrl_bf16* w1 = A.w + int64_t(min(n0 + g + 8, A.N - 1)) * A.ldw;
+    float c[T][4] = {};
+    for (int k0 = warp * kTurn; k0 < K; k0 += kWarps * kTurn) {
+        uint4 a[kAhead], b[kAhead], x[T][kAhead];
+        if (k0 + kTurn <= K) {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                a[i] = ld_stream(reinterpret_cast<const uint4*>(w0 + k0 + 32 * i + 8 * t));
+                b[i] = ld_stream(reinterpret_cast<const uint4*>(w1 + k0 + 32 * i + 8 * t));
+            }
+#pragma unroll
+            for (int r = 0; r < T; ++r)
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i)
+                    x[r][i] = 8 * r + g < A.M ? __ldg(reinterpret_cast<const uint4*>(A.x + (8 * r + g) * A.ldx + k0 + 32 * i + 8 * t))
+                                              : make_uint4(0u, 0u, 0u, 0u);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int k = k0 + 32 * i + 8 * t;
+                a[i] = load8(w0, k, K);
+                b[i] = load8(w1, k, K);
+#pragma unroll
+                for (int r = 0; r < T; ++r) x[r][i] = load8(A.x + (8 * r + g) * A.ldx, k, 8 * r + g < A.M ? K : 0);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+            for (int r = 0; r < T; ++r) {
+                mma_16x8(c[r], a[i].x, b[i].x, a[i].y, b[i].y, x[r][i].x, x[r][i].y);
+                mma_16x8(c[r], a[i].z, b[i].z, a[i].w, b[i].w, x[r][i].z, x[r][i].w);
+            }
+    }
+#pragma unroll
+    for (int r = 0; r < T; ++r) {
+        red[warp][8 * r + 2 * t][g] = c[r][0];
+        red[warp][8 * r + 2 * t + 1][g] = c[r][1];
+        red[warp][8 * r + 2 * t][g + 8] = c[r][2];
+        red[warp][8 * r + 2 * t + 1][g + 8] = c[r][3];
+    }
+    __syncthreads();
+    const int m = threadIdx.x / kW;
+    const int64_t n = n0 + (threadIdx.x & (kW - 1));
+    if (m >= A.M || n >= A.N) return;
+    float v[1] = {};
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) v[0] += red[i][m][n - n0];
+    const Finish& f = A.f;
+    if (f.bias) v[0] += load_float(f.bias, f.bias_f32, n);
+    if (f.pre) f.pre[m * f.ldp + n] = to_bf16(v[0]);
+    apply(f.act, v);
+    if (f.residual) v[0] += load_float(f.residual, f.residual_f32, m * f.ldr + n);
+    store_float(f.out, f.out_f32, m * f.ldo + n, v[0]);
+}
+
+}  // namespace
+
+bool linear_few_rows(int64_t M, int64_t N, int64_t K) { return M > 0 && M <= 16 && N > 0 && K > 0; }
+
+acrl_status linear_few(const acrl_bf16* x, int64_t M, int64_t K, int64_t ldx, const acrl_bf16* w, int64_t N, int64_t ldw, const Finish& f,
+                       cudaStream_t s) {
+    const FewArgs A{x, w, ldx, ldw, int(M), int(N), int(K), f};
+    return launch(M <= 8 ? few_kernel<1> : few_kernel<2>, (N + kW - 1) / kW, kThreads, 0, 0, s, A);
+}
+
+}  // namespace acrl
