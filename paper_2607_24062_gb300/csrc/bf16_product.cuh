@@ -7,7 +7,7 @@
 // read); the copies then fetch 64 x 64 blocks and the MMA takes them transposed, so nothing is turned beforehand.
 //
 // One CTA per SM, warp-specialised: warp 0 issues the TMA loads of slabs of 64 along the sum (128-byte swizzle) into a ring
-// of stages; warp 1 issues tcgen05.mma, four of K = 16 a slab; warps 2-9 are the epilogue, which reads one of two
+// of stages; warp 1 issues tcgen05.mma, four of K = 16 a slab; warps 4-11 are the epilogue, which reads one of two
 // accumulators in tensor memory while the MMAs fill the other.  Persistent over the tiles.  Two ways:
 //
 // Pairs: two CTAs (cta_group::2) share a tile of 256 rows x up to 256 columns, each staging its 128 rows of p and half of q's.
@@ -15,6 +15,11 @@
 //   the weight, so that no product is made and nothing is loaded for rows that are not there.
 //
 // A long sum over few tiles is split: the parts' accumulators go to a workspace in fp32, and the caller joins them in order.
+//
+// The tensor cores cut partial sums off where they should round them: an error toward zero that grows with the length of a run
+// (relative to the result's norm, of normal numbers: 0.7e-6 for a sum of 1,027, 1.7e-6 for 2,507).  bf16 hides it; for an fp32
+// result the sum is taken in runs of kRun slabs, whose accumulators the epilogue's warps add up in registers, rounding, while
+// the MMAs fill the next (LONG).
 //
 // TERMS = 3: each operand is two bf16 matrices, p = p0 + p1, and acc takes p0 q0 + p0 q1 + p1 q0 (Dekker's split product
 // without its smallest term): four tiles in shared memory feed three MMAs.
@@ -38,11 +43,16 @@ constexpr int kSlab = 64;            // of the sum: 128 bytes, one row of the 12
 constexpr int kRowBytes = kSlab * 2;
 constexpr int kMaxStages = 12;
 constexpr int kDrain = 8;            // epilogue warps
-constexpr int kProductThreads = (2 + kDrain) * 32;
+constexpr int kProductThreads = (4 + kDrain) * 32;
 constexpr uint32_t kTmemCols = 512;
 constexpr int kAccCols = 256;        // of each accumulator
 constexpr int kWarpStaging = 4096;   // bytes of an epilogue warp: a block of 32 x 32 in fp32, or two in bf16
 constexpr int kProductSmem = 227 * 1024;
+constexpr int kRun = 8;              // slabs of a run
+// Registers of a thread in the kernel with runs: 384 threads at launch with kLaunchRegs each, of which the first warpgroup
+// gives to the other two, that hold up to 128 sums.
+constexpr int kLaunchRegs = 168, kFewRegs = 56, kManyRegs = 224;
+static_assert(kFewRegs + 2 * kManyRegs <= 3 * kLaunchRegs && kProductThreads == 384, "what a launch has");
 
 struct ProductBarriers {
     uint64_t full[kMaxStages];    // the copies of a stage have landed (pair: the even CTA's counts both CTAs')
@@ -62,6 +72,7 @@ struct Problem {
     int cols;                // of a tile: a multiple of 32 (pair; of 128 where q is not K-major) or of 16 (alone)
     int p_tiles, q_tiles;
     int parts, per;          // of the sum, and slabs of each
+    int run;                 // slabs that one accumulator takes
     int lower;               // tiles that lie above the diagonal's are left out: the result is symmetric
     int p_turned, q_turned;  // the operand lies with the sum along its columns
     uint32_t idesc;
@@ -234,42 +245,41 @@ __device__ void issue_products(const L& l, uint8_t* ring, ProductBarriers* bars,
         // from one K = 16 to the next: 32 bytes of a row, or sixteen rows
         const uint32_t pstep = pr.p_turned ? 16 * kRowBytes >> 4 : 2, qstep = pr.q_turned ? 16 * kRowBytes >> 4 : 2;
         const uint32_t plow = kRows * kRowBytes >> 4, qlow = uint32_t((PAIR ? pr.cols / 2 : pr.cols) * kRowBytes) >> 4;
-        if (!warp_wait(&bars->tempty[acc], aphase ^ 1u, abort)) {
-            give_up(abort, l.flags);
-            break;
-        }
-        tc_fence_after();
-        const uint32_t d = tmem + uint32_t(acc * kAccCols);
-        for (int kb = t.lo; kb < t.hi; ++kb) {
-            ok = warp_wait(&bars->full[stage], phase, abort);
+        for (int run = t.lo; run < t.hi && ok; run += pr.run) {
+            ok = warp_wait(&bars->tempty[acc], aphase ^ 1u, abort);
             if (!ok) break;
             tc_fence_after();
-            const uint64_t pd = pdesc0 + stage * units, qd = qdesc0 + stage * units;
-            const uint32_t more = kb > t.lo;
-            if (elect_one()) {
+            const uint32_t d = tmem + uint32_t(acc * kAccCols);
+            const int end = min(t.hi, run + pr.run);
+            for (int kb = run; kb < end; ++kb) {
+                ok = warp_wait(&bars->full[stage], phase, abort);
+                if (!ok) break;
+                tc_fence_after();
+                const uint64_t pd = pdesc0 + stage * units, qd = qdesc0 + stage * units;
+                const uint32_t more = kb > run;
+                if (elect_one()) {
 #pragma unroll
-                for (int i = 0; i < TERMS; ++i) {
-                    const uint64_t a = pd + (i == 2 ? plow : 0u), b = qd + (i == 1 ? qlow : 0u);
+                    for (int i = 0; i < TERMS; ++i) {
+                        const uint64_t a = pd + (i == 2 ? plow : 0u), b = qd + (i == 1 ? qlow : 0u);
 #pragma unroll
-                    for (uint32_t k = 0; k < kSlab / 16; ++k)
-                        mma_bf16<PAIR>(d, a + k * pstep, b + k * qstep, pr.idesc, i > 0 || k > 0 ? 1u : more);
+                        for (uint32_t k = 0; k < kSlab / 16; ++k)
+                            mma_bf16<PAIR>(d, a + k * pstep, b + k * qstep, pr.idesc, i > 0 || k > 0 ? 1u : more);
+                    }
+                    commit<PAIR>(&bars->empty[stage]);
                 }
-                commit<PAIR>(&bars->empty[stage]);
+                if (++stage == l.stages) {
+                    stage = 0;
+                    phase ^= 1u;
+                }
             }
-            if (++stage == l.stages) {
-                stage = 0;
-                phase ^= 1u;
+            if (!ok) break;
+            if (elect_one()) commit<PAIR>(&bars->tfull[acc]);
+            if (++acc == 2) {
+                acc = 0;
+                aphase ^= 1u;
             }
         }
-        if (!ok) {
-            give_up(abort, l.flags);
-            break;
-        }
-        if (elect_one()) commit<PAIR>(&bars->tfull[acc]);
-        if (++acc == 2) {
-            acc = 0;
-            aphase ^= 1u;
-        }
+        if (!ok) give_up(abort, l.flags);
     }
     // every MMA has finished before the CTA moves on
     if (elect_one()) {
@@ -330,60 +340,99 @@ struct WarpOut {
     }
 };
 
-template <bool PAIR, int NP, class L>
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&v)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
+        "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+        "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]), "f"(v[10]),
+        "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]), "f"(v[16]), "f"(v[17]), "f"(v[18]), "f"(v[19]), "f"(v[20]),
+        "f"(v[21]), "f"(v[22]), "f"(v[23]), "f"(v[24]), "f"(v[25]), "f"(v[26]), "f"(v[27]), "f"(v[28]), "f"(v[29]), "f"(v[30]),
+        "f"(v[31])
+        : "memory");
+}
+
+template <bool PAIR, bool LONG, int NP, class L>
 __device__ void drain(const L& l, ProductBarriers* bars, uint32_t tmem, uint8_t* staging, uint32_t rank) {
     volatile int32_t* abort = &bars->abort;
-    const int warp = int(threadIdx.x >> 5) - 2, lane = threadIdx.x & 31, quarter = (threadIdx.x >> 5) & 3;
+    const int warp = int(threadIdx.x >> 5) - 4, lane = threadIdx.x & 31, quarter = (threadIdx.x >> 5) & 3;
     WarpOut out{staging + warp * kWarpStaging, lane};
     const uint32_t lanes = uint32_t(quarter * 32) << 16;
+    const int first = 32 * (warp >> 2);   // the two warps of a quarter take 32 columns in turn
     int acc = 0;
     uint32_t phase = 0;
-    for (Units<PAIR, NP, L> w(l); w.more(); w.next()) {
-        const Problem& pr = w.problem();
-        const Unit t = w.unit();
-        const int row0 = (PAIR ? 2 * t.tp + int(rank) : t.tp) * kRows + quarter * 32;
-        if (!warp_wait(&bars->tfull[acc], phase, abort)) {
-            give_up(abort, l.flags);
-            break;
-        }
-        tc_fence_after();
-        bool told = false;
-#pragma unroll 1
-        for (int c = 32 * (warp >> 2); c < pr.cols; c += 64) {   // the two warps of a quarter take 32 columns in turn
-            uint32_t r[32];
-            __syncwarp();
-            tmem_ld32(tmem + uint32_t(acc * kAccCols + c) + lanes, r);
-            if (c + 64 >= pr.cols) {   // read out: the MMA warp may fill it again
-                told = true;
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) {
-                    if (PAIR) remote_arrive(peer_addr(&bars->tempty[acc], 0));
-                    else mbar_arrive(&bars->tempty[acc]);
-                }
-            }
-            const int col0 = t.tq * pr.cols + c;
-            if (row0 < pr.rows && col0 < pr.cols_all)   // the same for the whole warp
-                l.epi[NP == 2 ? w.which : 0].chunk(pr, t, r, row0, col0, out);
-        }
-        if (!told) {   // a tile of one chunk has none for this warp
-            __syncwarp();
-            if (lane == 0) {
-                if (PAIR) remote_arrive(peer_addr(&bars->tempty[acc], 0));
-                else mbar_arrive(&bars->tempty[acc]);
-            }
-        }
+    auto release = [&] {   // the accumulator is read out: the MMA warp may fill it again
+        tc_fence_before();
         __syncwarp();
+        if (lane == 0) {
+            if (PAIR) remote_arrive(peer_addr(&bars->tempty[acc], 0));
+            else mbar_arrive(&bars->tempty[acc]);
+        }
+    };
+    auto turn = [&] {
         if (++acc == 2) {
             acc = 0;
             phase ^= 1u;
         }
+    };
+    bool ok = true;
+    for (Units<PAIR, NP, L> w(l); w.more(); w.next()) {
+        const Problem& pr = w.problem();
+        const Unit t = w.unit();
+        const int row0 = (PAIR ? 2 * t.tp + int(rank) : t.tp) * kRows + quarter * 32;
+        if constexpr (LONG) {
+            constexpr int kMost = PAIR ? 4 : 2;   // chunks of a warp
+            float sum[kMost][32] = {};
+            const int runs = (t.hi - t.lo + pr.run - 1) / pr.run;
+            for (int i = 0; i < runs && ok; ++i) {
+                ok = __all_sync(0xffffffffu, wait_phase_inline(&bars->tfull[acc], phase, abort));   // a call would spill the sums
+                if (!ok) break;
+                tc_fence_after();
+                if (runs == 1) break;
+                const bool last = i + 1 == runs;
+#pragma unroll
+                for (int k = 0; k < kMost; ++k) {
+                    const uint32_t at = tmem + uint32_t(acc * kAccCols + first + 64 * k) + lanes;   // beyond the tile's columns, too
+                    uint32_t r[32];
+                    tmem_ld32(at, r);
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) sum[k][j] += __uint_as_float(r[j]);
+                }
+                if (last) {   // what follows reads the whole sum as it would read one run's
+#pragma unroll
+                    for (int k = 0; k < kMost; ++k) tmem_st32(tmem + uint32_t(acc * kAccCols + first + 64 * k) + lanes, sum[k]);
+                    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                } else {
+                    release();
+                    turn();
+                }
+            }
+        } else {
+            ok = warp_wait(&bars->tfull[acc], phase, abort);
+            tc_fence_after();
+        }
+        if (!ok) {
+            give_up(abort, l.flags);
+            break;
+        }
+        if (first >= pr.cols) release();   // a tile of 32 columns has none for this warp
+#pragma unroll 1
+        for (int c = first; c < pr.cols; c += 64) {
+            uint32_t r[32];
+            __syncwarp();
+            tmem_ld32(tmem + uint32_t(acc * kAccCols + c) + lanes, r);
+            if (c + 64 >= pr.cols) release();
+            const int col0 = t.tq * pr.cols + c;
+            if (row0 < pr.rows && col0 < pr.cols_all)   // the same for the whole warp
+                l.epi[NP == 2 ? w.which : 0].chunk(pr, t, r, row0, col0, out);
+        }
+        __syncwarp();
+        turn();
     }
     if (lane == 0) bulk_wait_all();   // the blocks stay valid until every store has completed
     __syncwarp();
 }
 
-template <bool PAIR, int NP, int TERMS, class Epi>
+template <bool PAIR, bool LONG, int NP, int TERMS, class Epi>
 __global__ void __launch_bounds__(kProductThreads, 1)
     product_kernel(const __grid_constant__ ProductLaunch<NP, TERMS, Epi> l) {
     using L = ProductLaunch<NP, TERMS, Epi>;
@@ -427,12 +476,13 @@ __global__ void __launch_bounds__(kProductThreads, 1)
     if (PAIR) cluster_sync();   // the other's barriers are initialised, and it runs
     tc_fence_after();
     const uint32_t tmem = bars->tmem_base;
-    if (warp == 0) {
-        produce_slabs<PAIR, NP, TERMS, L>(l, ring, bars, rank);
-    } else if (warp == 1) {
-        if (rank == 0) issue_products<PAIR, NP, TERMS, L>(l, ring, bars, tmem);
+    if (warp < 4) {
+        if constexpr (LONG) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegs));
+        if (warp == 0) produce_slabs<PAIR, NP, TERMS, L>(l, ring, bars, rank);
+        if (warp == 1 && rank == 0) issue_products<PAIR, NP, TERMS, L>(l, ring, bars, tmem);
     } else {
-        drain<PAIR, NP, L>(l, bars, tmem, staging, rank);
+        if constexpr (LONG) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegs));
+        drain<PAIR, LONG, NP, L>(l, bars, tmem, staging, rank);
     }
     __syncwarp();
     tc_fence_before();
@@ -481,7 +531,7 @@ struct Cut {
 // tcgen05.mma kind::f16: D f32 (bits 4-5 = 1), A and B bf16 (bits 7-9, 10-12 = 1), A and B transposed (bits 15, 16),
 // N / 8 at bit 17, M / 16 at bit 24.
 inline Problem problem_of(bool pair, int64_t rows, int64_t cols_all, int64_t K, int64_t batch, bool p_turned, bool q_turned,
-                          bool lower, const Cut& cut) {
+                          bool lower, bool runs, const Cut& cut) {
     Problem pr = {};
     const int high = pair ? 2 * kRows : kRows;
     pr.rows = int(rows);
@@ -493,6 +543,7 @@ inline Problem problem_of(bool pair, int64_t rows, int64_t cols_all, int64_t K, 
     pr.q_tiles = int((cols_all + cut.cols - 1) / cut.cols);
     pr.parts = cut.parts;
     pr.per = cut.per;
+    pr.run = runs ? kRun : pr.slabs;
     pr.lower = lower;
     pr.p_turned = p_turned;
     pr.q_turned = q_turned;
@@ -515,11 +566,32 @@ inline bool units_fit(bool pair, int64_t rows, int64_t cols_all, int64_t batch, 
     return n < 1e9;
 }
 
-template <bool PAIR, int NP, int TERMS, class Epi>
+// Allows the kernel its shared memory; the pairs, or CTAs alone, that can be resident at once: kept for the device that the
+// calling thread used last.
+template <bool PAIR, bool LONG, int NP, int TERMS, class Epi>
+int64_t resident_products() {
+    static thread_local int known = -1;
+    static thread_local int64_t most = 0;
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return 0;
+    }
+    if (dev == known) return most;
+    auto* kernel = product_kernel<PAIR, LONG, NP, TERMS, Epi>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return 0;
+    }
+    most = PAIR ? resident_clusters(reinterpret_cast<const void*>(kernel), kProductThreads, kProductSmem, 2) : sms;
+    if (most > 0) known = dev;
+    return most;
+}
+
+template <bool PAIR, bool LONG, int NP, int TERMS, class Epi>
 acrl_status launch_product(ProductLaunch<NP, TERMS, Epi>& l, int32_t* flags, cudaStream_t s) {
     constexpr int kMats = TERMS == 3 ? 2 : 1;
-    auto* kernel = product_kernel<PAIR, NP, TERMS, Epi>;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem) != cudaSuccess) return launch_status();
     l.stage_bytes = 0;
     int64_t units = 0;
     for (int i = 0; i < NP; ++i) {
@@ -529,17 +601,10 @@ acrl_status launch_product(ProductLaunch<NP, TERMS, Epi>& l, int32_t* flags, cud
     }
     l.stages = std::min(kMaxStages, kRingBytes / l.stage_bytes);
     l.flags = flags;
-    int64_t most;
-    if (PAIR) {
-        most = resident_clusters(reinterpret_cast<const void*>(kernel), kProductThreads, kProductSmem, 2);
-    } else {
-        int dev = 0, sms = 0;
-        if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-            return launch_status();
-        most = sms;
-    }
+    const int64_t most = resident_products<PAIR, LONG, NP, TERMS, Epi>();
     if (most < 1) return ACRL_ERR_CUDA;
-    return launch(kernel, std::min(units, most) * (PAIR ? 2 : 1), kProductThreads, kProductSmem, PAIR ? 2 : 0, s, l);
+    return launch(product_kernel<PAIR, LONG, NP, TERMS, Epi>, std::min(units, most) * (PAIR ? 2 : 1), kProductThreads, kProductSmem,
+                  PAIR ? 2 : 0, s, l);
 }
 
 }  // namespace

@@ -147,36 +147,99 @@ struct Plan {
     int64_t ldparts, part_size;
 };
 
+constexpr int64_t kTile = 2000, kJoin = 6000, kJoinBytes = 3000;   // a tile's and a join's cycles, and its bytes a cycle
+constexpr int kPartChoices[] = {1, 2, 3, 4, 6, 8, 12, 16};
+
+int64_t slabs_of(int64_t K) { return std::max<int64_t>(1, (K + kSlab - 1) / kSlab); }
+// A pair's slab: its MMAs, or its loads at 64 bytes a cycle.
+int64_t pair_slab(int cols) { return std::max(2 * cols, 2 * (kRows + cols / 2)); }
+int64_t pair_tiles(int64_t M, int64_t N, int cols) { return (M + 2 * kRows - 1) / (2 * kRows) * ((N + cols - 1) / cols); }
+
+// Parts of equal length, none of them empty: false where `parts` is no such number.
+bool part_length(int64_t slabs, int64_t parts, int64_t& per) {
+    if (parts > slabs) return false;
+    per = (slabs + parts - 1) / parts;
+    return (slabs + per - 1) / per == parts;
+}
+
+void set_cut(Plan& plan, int64_t M, int64_t N, const Cut& cut) {
+    plan.cut = cut;
+    plan.ldparts = (N + 7) / 8 * 8;
+    plan.part_size = M * plan.ldparts;
+    plan.workspace = cut.parts > 1 ? cut.parts * plan.part_size * 4 : 0;
+}
+
 // The cut with the least estimated time: rounds of tiles x (slabs x a slab's cycles + a tile's), and the joining of parts.
 Plan plan_of(int64_t M, int64_t N, int64_t K, bool x_turned, bool w_turned) {
-    constexpr int64_t kTile = 2000, kJoin = 6000, kJoinBytes = 3000;   // cycles, cycles, bytes a cycle
-    const int64_t slabs = std::max<int64_t>(1, (K + kSlab - 1) / kSlab);
+    const int64_t slabs = slabs_of(K);
     Plan best = {};
     best.alone = M <= kAloneRows;
-    best.ldparts = (N + 7) / 8 * 8;
-    best.part_size = M * best.ldparts;
-    const int64_t rows = best.alone ? N : M, cols_all = best.alone ? M : N, high = best.alone ? kRows : 2 * kRows;
     const int64_t lanes = best.alone ? 2 * kPairs : kPairs;
     int widest = 256, step = 32, least = 64;   // columns of a tile
-    if (best.alone) widest = least = int(x_turned ? std::max<int64_t>(1, (M + 63) / 64) * 64 : std::max<int64_t>(1, (M + 15) / 16) * 16);   // of blocks of 64
-    else if (w_turned) step = least = 128;
+    if (best.alone) widest = least = int(x_turned ? std::max<int64_t>(1, (M + 63) / 64) * 64 : std::max<int64_t>(1, (M + 15) / 16) * 16);
+    else if (w_turned) step = least = 128;     // blocks of 64 a CTA
+    Cut cut = {};
     for (int cols = widest; cols >= least; cols -= step) {
-        const int64_t tiles = (rows + high - 1) / high * ((cols_all + cols - 1) / cols);
-        // a slab: its MMAs, or its loads at 64 bytes a cycle
-        const int64_t slab = best.alone ? 2 * (kRows + cols) : std::max(2 * cols, 2 * (kRows + cols / 2));
-        for (int64_t parts = 1; parts <= 16 && parts <= slabs; ++parts) {
-            const int64_t per = (slabs + parts - 1) / parts;
-            if ((slabs + per - 1) / per != parts) continue;
+        const int64_t tiles = best.alone ? (N + kRows - 1) / kRows : pair_tiles(M, N, cols);
+        const int64_t slab = best.alone ? 2 * (kRows + cols) : pair_slab(cols);
+        for (int64_t parts : kPartChoices) {
+            int64_t per;
+            if (parts > 1 && tiles * (parts - 1) >= 2 * lanes) break;   // there are tiles enough
+            if (!part_length(slabs, parts, per)) continue;
             const int64_t rounds = (tiles * parts + lanes - 1) / lanes;
-            const int64_t cost = rounds * (per * slab + kTile) + (parts > 1 ? kJoin + (parts + 1) * best.part_size * 4 / kJoinBytes : 0);
+            const int64_t cost = rounds * (per * slab + kTile) + (parts > 1 ? kJoin + (parts + 1) * M * N * 4 / kJoinBytes : 0);
             if (best.cost == 0 || cost < best.cost) {
                 best.cost = cost;
-                best.cut = Cut{cols, int(parts), int(per)};
+                cut = Cut{cols, int(parts), int(per)};
             }
         }
     }
-    best.workspace = best.cut.parts > 1 ? best.cut.parts * best.part_size * 4 : 0;
+    set_cut(best, M, N, cut);
     return best;
+}
+
+// Both products of a backward pass in one launch: the tiles of dw continue where those of dx end, so that a part-filled last
+// round of one is filled by the other.
+struct BackwardPlan {
+    Plan dx, dw;
+    bool together;
+};
+
+BackwardPlan plan_backward(int64_t M, int64_t N, int64_t K) {
+    BackwardPlan b = {plan_of(M, K, N, false, true), plan_of(N, K, M, true, true), false};
+    if (b.dx.alone || b.dw.alone || M == 0 || N == 0 || K == 0) return b;
+    const int64_t s0 = slabs_of(N), s1 = slabs_of(M);
+    int64_t least = 0;
+    Cut cut0 = {}, cut1 = {};
+    for (int cols = 256; cols >= 128; cols -= 128) {
+        const int64_t t0 = pair_tiles(M, K, cols), t1 = pair_tiles(N, K, cols), slab = pair_slab(cols);
+        for (int64_t p0 : kPartChoices) {
+            int64_t per0;
+            if (p0 > 8 || (p0 > 1 && t0 * p0 + t1 > 4 * kPairs)) break;
+            if (!part_length(s0, p0, per0)) continue;
+            const int64_t n0 = t0 * p0, c0 = per0 * slab + kTile, full = n0 % kPairs, each = n0 / kPairs;
+            for (int64_t p1 : kPartChoices) {
+                int64_t per1;
+                if (p1 > 8 || (p1 > 1 && t0 + t1 * p1 > 4 * kPairs)) break;
+                if (!part_length(s1, p1, per1)) continue;
+                const int64_t n1 = t1 * p1, c1 = per1 * slab + kTile, rest = std::max<int64_t>(0, n1 - (kPairs - full));
+                // pairs that have one tile more of the first, and those that have not
+                int64_t cost = each * c0 + (n1 + kPairs - 1) / kPairs * c1;
+                if (full > 0) cost = std::max(cost, (each + 1) * c0 + (rest + kPairs - 1) / kPairs * c1);
+                if (p0 > 1) cost += kJoin + (p0 + 1) * M * K * 4 / kJoinBytes;
+                if (p1 > 1) cost += kJoin + (p1 + 1) * N * K * 4 / kJoinBytes;
+                if (least == 0 || cost < least) {
+                    least = cost;
+                    cut0 = Cut{cols, int(p0), int(per0)};
+                    cut1 = Cut{cols, int(p1), int(per1)};
+                }
+            }
+        }
+    }
+    b.together = true;
+    set_cut(b.dx, M, K, cut0);
+    set_cut(b.dw, N, K, cut1);
+    return b;
 }
 
 acrl_status join(const Finish& f, const float* parts, int count, const Plan& plan, int64_t M, int64_t N, cudaStream_t s) {
@@ -185,41 +248,64 @@ acrl_status join(const Finish& f, const float* parts, int count, const Plan& pla
     return launch(join_kernel, (threads + 255) / 256, 256, 0, 0, s, f, parts, count, plan.ldparts, plan.part_size, int(M), int(N));
 }
 
-// Fills one problem of a launch; x has the result's rows, w its columns.
+// One product: x has the result's rows, w its columns.
+struct Product {
+    const Plan& plan;
+    Matrix x, w;
+    int64_t K;
+    const Finish& f;
+    float* parts;
+};
+
+// An fp32 result of more than one run.
+bool has_runs(const Product& p) { return p.f.out_f32 && p.plan.cut.per > kRun; }
+
 template <bool PAIR, int NP>
-bool describe(ProductLaunch<NP, 1, LinearEpilogue<PAIR>>& l, int at, const Plan& plan, const Matrix& x, const Matrix& w, int64_t K,
-              const Finish& f, float* parts) {
-    const Matrix &p = PAIR ? x : w, &q = PAIR ? w : x;
-    const int64_t M = x.rows, N = w.rows;
-    l.pr[at] = problem_of(PAIR, p.rows, q.rows, K, 1, p.turned, q.turned, false, plan.cut);
+bool describe(ProductLaunch<NP, 1, LinearEpilogue<PAIR>>& l, int at, const Product& d) {
+    const Matrix &p = PAIR ? d.x : d.w, &q = PAIR ? d.w : d.x;
+    const Plan& plan = d.plan;
+    const Finish& f = d.f;
+    const int64_t M = d.x.rows, N = d.w.rows;
+    l.pr[at] = problem_of(PAIR, p.rows, q.rows, d.K, 1, p.turned, q.turned, false, has_runs(d), plan.cut);
     LinearEpilogue<PAIR>& e = l.epi[at];
     e.f = f;
-    e.parts = plan.cut.parts > 1 ? parts : nullptr;
+    e.parts = plan.cut.parts > 1 ? d.parts : nullptr;
     e.ldparts = plan.ldparts;
     e.part_size = plan.part_size;
-    if (!operand_map(&l.p[at][0], p, K, kRows) || !operand_map(&l.q[at][0], q, K, PAIR ? plan.cut.cols / 2 : plan.cut.cols)) return false;
+    if (!operand_map(&l.p[at][0], p, d.K, kRows) || !operand_map(&l.q[at][0], q, d.K, PAIR ? plan.cut.cols / 2 : plan.cut.cols)) return false;
     if (!PAIR) return true;
-    if (e.parts) return result_map(&e.out_map, parts, true, M, plan.ldparts, plan.ldparts, plan.cut.parts, plan.part_size);
+    if (e.parts) return result_map(&e.out_map, d.parts, true, M, plan.ldparts, plan.ldparts, plan.cut.parts, plan.part_size);
     return result_map(&e.out_map, f.out, f.out_f32, M, N, f.ldo, 1, M * f.ldo) &&
            (!f.pre || result_map(&e.pre_map, f.pre, false, M, N, f.ldp, 1, M * f.ldp));
 }
 
-template <bool PAIR>
-acrl_status run_product(const Plan& plan, const Matrix& x, const Matrix& w, int64_t K, const Finish& f, float* parts, int32_t* flags,
-                        cudaStream_t s) {
-    ProductLaunch<1, 1, LinearEpilogue<PAIR>> l = {};
-    if (!describe<PAIR, 1>(l, 0, plan, x, w, K, f, parts)) return ACRL_ERR_CUDA;
-    const acrl_status st = launch_product<PAIR>(l, flags, s);
-    return st != ACRL_OK || plan.cut.parts == 1 ? st : join(f, parts, plan.cut.parts, plan, x.rows, w.rows, s);
+acrl_status join_parts(const Product& d, cudaStream_t s) {
+    return d.plan.cut.parts == 1 ? ACRL_OK : join(d.f, d.parts, d.plan.cut.parts, d.plan, d.x.rows, d.w.rows, s);
+}
+
+template <bool PAIR, int NP>
+acrl_status run_products(const Product (&d)[NP], int32_t* flags, cudaStream_t s) {
+    ProductLaunch<NP, 1, LinearEpilogue<PAIR>> l = {};
+    bool runs = false;
+    for (int i = 0; i < NP; ++i) {
+        if (!describe<PAIR, NP>(l, i, d[i])) return ACRL_ERR_CUDA;
+        runs = runs || has_runs(d[i]);
+    }
+    acrl_status st = runs ? launch_product<PAIR, true>(l, flags, s) : launch_product<PAIR, false>(l, flags, s);
+    for (int i = 0; i < NP && st == ACRL_OK; ++i) st = join_parts(d[i], s);
+    return st;
+}
+
+bool product_fits(const Product& d) {
+    return units_fit(!d.plan.alone, d.plan.alone ? d.w.rows : d.x.rows, d.plan.alone ? d.x.rows : d.w.rows, 1, d.plan.cut);
 }
 
 // f(x w^T + ...): K > 0 columns, or an empty sum.
-acrl_status product(const Matrix& x, const Matrix& w, int64_t K, const Finish& f, void* workspace, int32_t* flags, cudaStream_t s) {
-    const Plan plan = plan_of(x.rows, w.rows, K, x.turned, w.turned);
-    if (K == 0) return join(f, nullptr, 0, plan, x.rows, w.rows, s);
-    if (!units_fit(!plan.alone, plan.alone ? w.rows : x.rows, plan.alone ? x.rows : w.rows, 1, plan.cut)) return ACRL_ERR_INVALID_ARG;
-    float* parts = static_cast<float*>(workspace);
-    return plan.alone ? run_product<false>(plan, x, w, K, f, parts, flags, s) : run_product<true>(plan, x, w, K, f, parts, flags, s);
+acrl_status product(const Product& d, int32_t* flags, cudaStream_t s) {
+    if (d.K == 0) return join(d.f, nullptr, 0, d.plan, d.x.rows, d.w.rows, s);
+    if (!product_fits(d)) return ACRL_ERR_INVALID_ARG;
+    const Product one[1] = {d};
+    return d.plan.alone ? run_products<false, 1>(one, flags, s) : run_products<true, 1>(one, flags, s);
 }
 
 // g = dy f'(u), rounded, and the columns' sums of the unrounded.  A lane has eight columns, a warp 256, and the eight warps of a
@@ -320,18 +406,20 @@ __global__ void __launch_bounds__(256) sums_kernel(const float* sums, int64_t ld
 bool dtype_ok(acrl_dtype d) { return d == ACRL_BF16 || d == ACRL_F32; }
 bool matrix_ok(const void* p, int64_t cols, int64_t ld) { return p && aligned16(p) && ld >= cols && (ld & 7) == 0; }
 
-// The backward's workspace: g, the columns' sums of its parts, the parts of a product's split sum (of one after the other).
+// The backward's workspace: g, the columns' sums of its parts, the parts of the products' split sums.
 struct BackwardParts {
-    int64_t ldg, rows, count, ldsums;   // of a part of the sums, and how many there are
-    int64_t sums, parts, end;           // bytes
-    BackwardParts(int64_t M, int64_t N, int64_t K) {
+    BackwardPlan plan;
+    int64_t ldg, rows, count, ldsums;   // of a part of the columns' sums, and how many there are
+    int64_t sums, dx, dw, end;          // bytes
+    BackwardParts(int64_t M, int64_t N, int64_t K) : plan(plan_backward(M, N, K)) {
         ldg = (N + 7) / 8 * 8;
         sums = M * ldg * 2;
         rows = slope_rows(M, N);
         count = (M + rows - 1) / rows;
         ldsums = (N + kSlopeCols - 1) / kSlopeCols * kSlopeCols;
-        parts = sums + count * ldsums * 4;
-        end = parts + std::max(plan_of(M, K, N, false, true).workspace, plan_of(N, K, M, true, true).workspace);
+        dx = sums + count * ldsums * 4;
+        dw = dx + plan.dx.workspace;
+        end = dw + plan.dw.workspace;
     }
 };
 
@@ -366,8 +454,9 @@ extern "C" acrl_status acrl_linear(const acrl_bf16* x, int64_t M, int64_t K, int
     const Finish f{bias, residual, out, pre, ldr, ldp, ldo, int(act), bias_dtype == ACRL_F32, residual_dtype == ACRL_F32,
                    out_dtype == ACRL_F32};
     if (linear_few_rows(M, N, K)) return linear_few(x, M, K, ldx, w, N, ldw, f, reinterpret_cast<cudaStream_t>(stream));
-    return product(Matrix{x, M, ldx, false, 1, M * ldx}, Matrix{w, N, ldw, false, 1, N * ldw}, K, f, workspace, dev_flags,
-                   reinterpret_cast<cudaStream_t>(stream));
+    const Plan plan = plan_of(M, N, K, false, false);
+    return product({plan, Matrix{x, M, ldx, false, 1, M * ldx}, Matrix{w, N, ldw, false, 1, N * ldw}, K, f, static_cast<float*>(workspace)},
+                   dev_flags, reinterpret_cast<cudaStream_t>(stream));
 }
 
 extern "C" int64_t acrl_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K) {
@@ -421,22 +510,22 @@ extern "C" acrl_status acrl_linear_backward(const acrl_bf16* dy, int64_t M, int6
         if (cudaMemsetAsync(dbias, 0, size_t(N) * 4, s) != cudaSuccess) return launch_status();
     }
     // without rows, or without columns of dy, the sums are empty
-    if (has_dx) {
-        Finish f = {};
-        f.out = dx;
-        f.ldo = lddx;
-        f.out_f32 = dx_dtype == ACRL_F32;
-        st = product(Matrix{g, M, ldg, false, 1, M * ldg}, Matrix{w, K, ldw, true, 1, N * ldw}, has_g ? N : 0, f, base + parts.parts,
-                     dev_flags, s);
-        if (st != ACRL_OK) return st;
+    Finish fx = {}, fw = {};
+    fx.out = dx;
+    fx.ldo = lddx;
+    fx.out_f32 = dx_dtype == ACRL_F32;
+    fw.out = dw;
+    fw.ldo = lddw;
+    fw.out_f32 = dw_dtype == ACRL_F32;
+    const Product both[2] = {{parts.plan.dx, Matrix{g, M, ldg, false, 1, M * ldg}, Matrix{w, K, ldw, true, 1, N * ldw}, has_g ? N : 0, fx,
+                              reinterpret_cast<float*>(base + parts.dx)},
+                             {parts.plan.dw, Matrix{g, N, ldg, true, 1, M * ldg}, Matrix{x, K, ldx, true, 1, M * ldx}, has_g ? M : 0, fw,
+                              reinterpret_cast<float*>(base + parts.dw)}};
+    if (has_dx && has_dw && has_g && parts.plan.together) {
+        if (!product_fits(both[0]) || !product_fits(both[1])) return ACRL_ERR_INVALID_ARG;
+        return run_products<true, 2>(both, dev_flags, s);
     }
-    if (has_dw) {
-        Finish f = {};
-        f.out = dw;
-        f.ldo = lddw;
-        f.out_f32 = dw_dtype == ACRL_F32;
-        st = product(Matrix{g, N, ldg, true, 1, M * ldg}, Matrix{x, K, ldx, true, 1, M * ldx}, has_g ? M : 0, f, base + parts.parts,
-                     dev_flags, s);
-    }
+    if (has_dx) st = product(both[0], dev_flags, s);
+    if (has_dw && st == ACRL_OK) st = product(both[1], dev_flags, s);
     return st;
 }

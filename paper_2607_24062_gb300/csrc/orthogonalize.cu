@@ -385,7 +385,7 @@ struct Halves {
 acrl_status step_product(const Plan& plan, int64_t batch, int64_t rows, int64_t cols, int64_t K, const Halves& p, const Halves& q,
                          bool q_turned, bool lower, const Finish& f, float* parts, int32_t* flags, cudaStream_t s) {
     ProductLaunch<1, 3, StepEpilogue> l = {};
-    l.pr[0] = problem_of(true, rows, cols, K, batch, false, q_turned, lower, plan.cut);
+    l.pr[0] = problem_of(true, rows, cols, K, batch, false, q_turned, lower, false, plan.cut);
     StepEpilogue& e = l.epi[0];
     e.f = f;
     e.parts = plan.cut.parts > 1;
@@ -403,7 +403,7 @@ acrl_status step_product(const Plan& plan, int64_t batch, int64_t rows, int64_t 
         ok = result_map(&e.hi, f.hi, false, rows, f.ld, f.ld, batch, f.size) && result_map(&e.lo, f.lo, false, rows, f.ld, f.ld, batch, f.size);
     }
     if (!ok) return ACRL_ERR_CUDA;
-    const acrl_status st = launch_product<true>(l, flags, s);
+    const acrl_status st = launch_product<true, false>(l, flags, s);
     if (st != ACRL_OK || !e.parts) return st;
     return launch(join_kernel, batch * ((rows + 31) / 32) * ((cols + 31) / 32), 256, 0, 0, s, f, static_cast<const float*>(parts),
                   plan.cut.parts, plan.ldparts, plan.part_size, int(lower), int(rows), int(cols));

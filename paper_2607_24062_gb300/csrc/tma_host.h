@@ -4,21 +4,32 @@
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
+#include <atomic>
 #include <initializer_list>
 
 #include "acrl_host.h"
 
 namespace acrl {
 
+// The driver's function, looked up once.
+inline PFN_cuTensorMapEncodeTiled_v12000 map_encoder() {
+    static std::atomic<void*> known{nullptr};
+    void* fn = known.load(std::memory_order_relaxed);
+    if (fn == nullptr) {
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess)
+            return nullptr;
+        known.store(fn, std::memory_order_relaxed);
+    }
+    return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
+}
+
 // A two-dimensional map of rows of `cols` elements of `bytes` bytes at a stride of ld elements.
 inline bool encode_map(CUtensorMap* map, CUtensorMapDataType type, uint32_t bytes, const void* ptr, uint64_t rows,
                        uint64_t cols, uint64_t ld, uint32_t box_rows, uint32_t box_cols, CUtensorMapSwizzle swizzle) {
-    void* fn = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q) != cudaSuccess ||
-        q != cudaDriverEntryPointSuccess || fn == nullptr)
-        return false;
-    auto encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
+    const PFN_cuTensorMapEncodeTiled_v12000 encode = map_encoder();
+    if (encode == nullptr) return false;
     const cuuint64_t dims[2] = {cols, rows};
     const cuuint64_t strides[1] = {ld * bytes};
     const cuuint32_t box[2] = {box_cols, box_rows};
@@ -32,12 +43,8 @@ inline bool encode_map(CUtensorMap* map, CUtensorMapDataType type, uint32_t byte
 inline bool encode_map_3d(CUtensorMap* map, CUtensorMapDataType type, uint32_t bytes, const void* ptr, uint64_t count, uint64_t rows,
                           uint64_t cols, uint64_t ld, uint64_t apart, uint32_t box_rows, uint32_t box_cols,
                           CUtensorMapSwizzle swizzle) {
-    void* fn = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q) != cudaSuccess ||
-        q != cudaDriverEntryPointSuccess || fn == nullptr)
-        return false;
-    auto encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
+    const PFN_cuTensorMapEncodeTiled_v12000 encode = map_encoder();
+    if (encode == nullptr) return false;
     const cuuint64_t dims[3] = {cols, rows, count};
     const cuuint64_t strides[2] = {ld * bytes, apart * bytes};
     const cuuint32_t box[3] = {box_cols, box_rows, 1};
