@@ -46,7 +46,7 @@ constexpr int kDrain = 8;            // epilogue warps
 constexpr int kProductThreads = (4 + kDrain) * 32;
 constexpr uint32_t kTmemCols = 512;
 constexpr int kAccCols = 256;        // of each accumulator
-constexpr int kWarpStaging = 4096;   // bytes of an epilogue warp: a block of 32 x 32 in fp32, or two in bf16
+constexpr int kWarpStaging = 4096;   // bytes of an epilogue warp: a block of 32 x 32 in fp32
 constexpr int kProductSmem = 227 * 1024;
 constexpr int kRun = 8;              // slabs of a run
 // Registers of a thread in the kernel with runs: 384 threads at launch with kLaunchRegs each, of which the first warpgroup
@@ -294,35 +294,56 @@ __device__ void issue_products(const L& l, uint8_t* ring, ProductBarriers* bars,
     __syncwarp();
 }
 
-// An epilogue warp's way out: its block of shared memory, and stores of 32 x 32 values by TMA.
+// An epilogue warp's way out: through its block of shared memory, so that neighbouring lanes store neighbouring pieces of 16
+// bytes, four or eight to a row.  (TMA stores of the blocks took longer: a copy keeps its block for about 1,000 cycles, and the
+// next 32 columns waited for it.  256 x 256 x 256, alone: 4.3 us, now 3.3.)
 struct WarpOut {
     uint8_t* staging;
     int lane;
-    int half = 0;
-    bool whole = false;   // the last store read the whole block
 
-    // Lane i has row row0 + i.  Not for a matrix that ends within these columns at no multiple of 16 bytes: a TMA store leaves
-    // columns out in pieces of that size and would write beyond it.
+    // What was staged, 32 rows of T at `at` and on, to rows row0 .. and columns col0 .. of a matrix of rows x cols at a stride
+    // of ld.  Every lane of the warp.
     template <typename T>
-    __device__ __forceinline__ void store(const CUtensorMap* map, const float (&v)[32], int row0, int col0, int z) {
-        constexpr int kPieces = 32 * int(sizeof(T)) / 16;
-        // a block of bf16 alternates between the halves; one of fp32 takes both
-        uint8_t* block = staging;
-        if (sizeof(T) == 2) {
-            block += half * (kWarpStaging / 2);
-            half ^= 1;
-            if (lane == 0) {
-                if (whole) bulk_wait_read<0>();
-                else bulk_wait_read<1>();
-            }
-        } else {
-            if (lane == 0) bulk_wait_read<0>();
-        }
-        whole = sizeof(T) == 4;
+    __device__ __forceinline__ void send(T* to, int64_t ld, int rows, int cols, int row0, int col0) const {
+        constexpr int kPieces = 32 * int(sizeof(T)) / 16, kEach = 16 / int(sizeof(T)), kRowsAtOnce = 32 / kPieces;
+        const uint32_t base = smem_u32(staging);
         __syncwarp();
-        // row `lane`, its 16-byte pieces permuted by the swizzle of the map: 64-byte rows in fours, 128-byte rows in eights
+        const int piece = lane & (kPieces - 1), c = col0 + piece * kEach, r0 = lane / kPieces;
+        uint32_t v[kPieces][4];
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int r = i * kRowsAtOnce + r0;
+            const uint32_t swz = kPieces == 4 ? uint32_t((r >> 1) & 3) : uint32_t(r & 7);
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(v[i][0]), "=r"(v[i][1]), "=r"(v[i][2]), "=r"(v[i][3])
+                         : "r"(base + uint32_t(r * 32 * int(sizeof(T))) + ((uint32_t(piece) ^ swz) << 4)));
+        }
+        T* p = to + (row0 + r0) * ld + c;
+        const int64_t step = kRowsAtOnce * ld;
+        if (c + kEach <= cols) {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i)
+                if (row0 + r0 + i * kRowsAtOnce < rows)
+                    *reinterpret_cast<uint4*>(p + i * step) = make_uint4(v[i][0], v[i][1], v[i][2], v[i][3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+                for (int k = 0; k < kEach; ++k)
+                    if (c + k < cols && row0 + r0 + i * kRowsAtOnce < rows) {
+                        if constexpr (sizeof(T) == 2) p[i * step + k] = T(v[i][k >> 1] >> (k & 1) * 16);
+                        else p[i * step + k] = __uint_as_float(v[i][k]);
+                    }
+        }
+        __syncwarp();   // the block may be written again
+    }
+
+    // Lane i has row row0 + i and its columns col0 .. col0 + 31; ld is a multiple of a piece.
+    template <typename T>
+    __device__ __forceinline__ void store(T* to, int64_t ld, int rows, int cols, const float (&v)[32], int row0, int col0) const {
+        constexpr int kPieces = 32 * int(sizeof(T)) / 16;
         const uint32_t swz = kPieces == 4 ? uint32_t((lane >> 1) & 3) : uint32_t(lane & 7);
-        const uint32_t to = smem_u32(block) + uint32_t(lane * 32 * int(sizeof(T)));
+        const uint32_t at = smem_u32(staging) + uint32_t(lane * 32 * int(sizeof(T)));
 #pragma unroll
         for (int k = 0; k < kPieces; ++k) {
             uint4 x;
@@ -332,11 +353,23 @@ struct WarpOut {
             else
                 x = make_uint4(__float_as_uint(v[4 * k]), __float_as_uint(v[4 * k + 1]), __float_as_uint(v[4 * k + 2]),
                                __float_as_uint(v[4 * k + 3]));
-            st_shared16(to + ((uint32_t(k) ^ swz) << 4), x);
+            st_shared16(at + ((uint32_t(k) ^ swz) << 4), x);
         }
-        fence_async_shared();
-        __syncwarp();
-        if (lane == 0) tma_store_3d(map, block, col0, row0, z);
+        send(to, ld, rows, cols, row0, col0);
+    }
+
+    // The same values turned, rounded to bf16: lane i has column col0 + i and its rows row0 .. row0 + 31.
+    __device__ __forceinline__ void store_turned(acrl_bf16* to, int64_t ld, int rows, int cols, const float (&v)[32], int row0,
+                                                 int col0) const {
+        const uint32_t at = smem_u32(staging) + uint32_t((lane & 7) * 2);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            const uint32_t piece = uint32_t(lane >> 3) ^ uint32_t((j >> 1) & 3);
+            asm volatile("st.shared.u16 [%0], %1;" ::"r"(at + uint32_t(j * 64) + (piece << 4)),
+                         "h"(acrl_bf16(pack_bf16x2(v[j], 0.f) & 0xffffu))
+                         : "memory");
+        }
+        send(to, ld, rows, cols, row0, col0);
     }
 };
 
@@ -355,17 +388,21 @@ template <bool PAIR, bool LONG, int NP, class L>
 __device__ void drain(const L& l, ProductBarriers* bars, uint32_t tmem, uint8_t* staging, uint32_t rank) {
     volatile int32_t* abort = &bars->abort;
     const int warp = int(threadIdx.x >> 5) - 4, lane = threadIdx.x & 31, quarter = (threadIdx.x >> 5) & 3;
-    WarpOut out{staging + warp * kWarpStaging, lane};
+    const WarpOut out{staging + warp * kWarpStaging, lane};
     const uint32_t lanes = uint32_t(quarter * 32) << 16;
     const int first = 32 * (warp >> 2);   // the two warps of a quarter take 32 columns in turn
     int acc = 0;
     uint32_t phase = 0;
-    auto release = [&] {   // the accumulator is read out: the MMA warp may fill it again
+    // The accumulator is read out: the MMA warp may fill it again.  The fence orders the reads of tensor memory; the arrival has
+    // nothing else to release, and one that releases to the whole cluster waits for the stores under way, 1,000 cycles.
+    auto release = [&] {
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
-            if (PAIR) remote_arrive(peer_addr(&bars->tempty[acc], 0));
-            else mbar_arrive(&bars->tempty[acc]);
+            if (PAIR)
+                asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(peer_addr(&bars->tempty[acc], 0)) : "memory");
+            else
+                mbar_arrive(&bars->tempty[acc]);
         }
     };
     auto turn = [&] {
@@ -374,12 +411,17 @@ __device__ void drain(const L& l, ProductBarriers* bars, uint32_t tmem, uint8_t*
             phase ^= 1u;
         }
     };
-    bool ok = true;
-    for (Units<PAIR, NP, L> w(l); w.more(); w.next()) {
+    // The first unit's first columns are gone through twice, before its products are there with a matrix of no rows and no
+    // columns, which loads and stores nothing: what follows a sum is then in the instruction cache when it is waited for (from
+    // there its 1,100 cycles were mostly misses; a layer of 256 x 256 x 256 3.9 us, now 3.4).
+    bool ok = true, dry = true;
+    Units<PAIR, NP, L> w(l);
+    while (w.more()) {
         const Problem& pr = w.problem();
         const Unit t = w.unit();
         const int row0 = (PAIR ? 2 * t.tp + int(rank) : t.tp) * kRows + quarter * 32;
-        if constexpr (LONG) {
+        if (dry) {
+        } else if constexpr (LONG) {
             constexpr int kMost = PAIR ? 4 : 2;   // chunks of a warp
             float sum[kMost][32] = {};
             const int runs = (t.hi - t.lo + pr.run - 1) / pr.run;
@@ -414,22 +456,26 @@ __device__ void drain(const L& l, ProductBarriers* bars, uint32_t tmem, uint8_t*
             give_up(abort, l.flags);
             break;
         }
-        if (first >= pr.cols) release();   // a tile of 32 columns has none for this warp
+        if (!dry && first >= pr.cols) release();   // a tile of 32 columns has none for this warp
 #pragma unroll 1
         for (int c = first; c < pr.cols; c += 64) {
             uint32_t r[32];
             __syncwarp();
             tmem_ld32(tmem + uint32_t(acc * kAccCols + c) + lanes, r);
-            if (c + 64 >= pr.cols) release();
+            if (!dry && c + 64 >= pr.cols) release();
             const int col0 = t.tq * pr.cols + c;
             if (row0 < pr.rows && col0 < pr.cols_all)   // the same for the whole warp
-                l.epi[NP == 2 ? w.which : 0].chunk(pr, t, r, row0, col0, out);
+                l.epi[NP == 2 ? w.which : 0].chunk(pr, t, r, row0, col0, dry ? 0 : pr.rows, dry ? 0 : pr.cols_all, out);
+            if (dry) break;
+        }
+        if (dry) {
+            dry = false;
+            continue;
         }
         __syncwarp();
         turn();
+        w.next();
     }
-    if (lane == 0) bulk_wait_all();   // the blocks stay valid until every store has completed
-    __syncwarp();
 }
 
 template <bool PAIR, bool LONG, int NP, int TERMS, class Epi>
@@ -457,7 +503,8 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&l.p[0][0])) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&l.q[0][0])) : "memory");
     }
-    grid_begin();
+    // Before the grid's wait, while the launch before this one ends: nothing here touches memory, and with all of an SM's shared
+    // memory a CTA shares its tensor memory with no other.
     if (warp == 2) {
         if (PAIR) {   // one warp of each CTA of the pair, together
             asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)),
@@ -476,6 +523,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
     if (PAIR) cluster_sync();   // the other's barriers are initialised, and it runs
     tc_fence_after();
     const uint32_t tmem = bars->tmem_base;
+    grid_begin();
     if (warp < 4) {
         if constexpr (LONG) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegs));
         if (warp == 0) produce_slabs<PAIR, NP, TERMS, L>(l, ring, bars, rank);
@@ -514,13 +562,6 @@ inline bool operand_map(CUtensorMap* map, const Matrix& m, int64_t K, int box_ro
                                     uint64_t(m.ld), uint64_t(m.apart), kSlab, kSlab, CU_TENSOR_MAP_SWIZZLE_128B)
                     : encode_map_3d(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, m.at, uint64_t(m.count), uint64_t(m.rows), uint64_t(K),
                                     uint64_t(m.ld), uint64_t(m.apart), uint32_t(box_rows), kSlab, CU_TENSOR_MAP_SWIZZLE_128B);
-}
-
-// The map of a result that WarpOut::store writes.
-inline bool result_map(CUtensorMap* map, const void* at, bool f32, int64_t rows, int64_t cols, int64_t ld, int64_t count, int64_t apart) {
-    return encode_map_3d(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, f32 ? 4 : 2, at, uint64_t(count),
-                         uint64_t(rows), uint64_t(cols), uint64_t(ld), uint64_t(apart), 32, 32,
-                         f32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
 }
 
 // How a product is cut.

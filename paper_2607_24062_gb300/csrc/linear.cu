@@ -16,63 +16,46 @@ constexpr int64_t kAloneRows = 128;  // rows that become a CTA's columns
 template <bool PAIR>
 struct LinearEpilogue {
     Finish f;
-    CUtensorMap out_map, pre_map;   // pair: of out (or of the parts), and of pre
     float* parts;                   // where the sum is split: [part][row][ldparts]
     int64_t ldparts, part_size;
 
-    __device__ __forceinline__ void chunk(const Problem& pr, const Unit& t, const uint32_t (&r)[32], int row0, int col0,
-                                          WarpOut& out) const {
+    __device__ __forceinline__ void chunk(const Problem& pr, const Unit& t, const uint32_t (&r)[32], int row0, int col0, int rows,
+                                          int cols, const WarpOut& out) const {
         float v[32];
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
         if constexpr (PAIR) {
             if (parts) {
-                out.store<float>(&out_map, v, row0, col0, t.part);
+                out.store(parts + t.part * part_size, ldparts, rows, cols, v, row0, col0);
                 return;
             }
             const int row = row0 + out.lane;
-            const bool ragged = col0 + 32 > pr.cols_all;
             if (f.bias) {
-                const float b = col0 + out.lane < pr.cols_all ? load_float(f.bias, f.bias_f32, col0 + out.lane) : 0.f;
+                const float b = col0 + out.lane < cols ? load_float(f.bias, f.bias_f32, col0 + out.lane) : 0.f;
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[j] += __shfl_sync(0xffffffffu, b, j);
             }
-            if (f.pre) {
-                if (ragged && (pr.cols_all & 7)) {
-                    if (row < pr.rows)
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (col0 + j < pr.cols_all) f.pre[row * f.ldp + col0 + j] = to_bf16(v[j]);
-                } else {
-                    out.store<acrl_bf16>(&pre_map, v, row0, col0, 0);
-                }
-            }
+            if (f.pre) out.store(f.pre, f.ldp, rows, cols, v, row0, col0);
             apply(f.act, v);
-            if (f.residual && row < pr.rows) {
+            if (f.residual && row < rows) {
                 float add[32];
-                load_row(f.residual, f.residual_f32, row * f.ldr, col0, pr.cols_all, add);
+                load_row(f.residual, f.residual_f32, row * f.ldr, col0, cols, add);
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[j] += add[j];
             }
-            if (ragged && (pr.cols_all & (f.out_f32 ? 3 : 7))) {
-                if (row < pr.rows)
-#pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (col0 + j < pr.cols_all) store_float(f.out, f.out_f32, row * f.ldo + col0 + j, v[j]);
-            } else if (f.out_f32) {
-                out.store<float>(&out_map, v, row0, col0, 0);
-            } else {
-                out.store<acrl_bf16>(&out_map, v, row0, col0, 0);
-            }
+            if (f.out_f32)
+                out.store(static_cast<float*>(f.out), f.ldo, rows, cols, v, row0, col0);
+            else
+                out.store(static_cast<acrl_bf16*>(f.out), f.ldo, rows, cols, v, row0, col0);
         } else {
             const int64_t n = row0 + out.lane;
-            if (n >= pr.rows) return;
-            const int rows = pr.cols_all - col0;   // of the result that this chunk has, of 32
+            if (n >= rows) return;
+            const int count = cols - col0;   // of the result's rows that this chunk has, of 32
             if (parts) {
                 float* to = parts + t.part * part_size + col0 * ldparts + n;
 #pragma unroll
                 for (int j = 0; j < 32; ++j)
-                    if (j < rows) to[j * ldparts] = v[j];
+                    if (j < count) to[j * ldparts] = v[j];
                 return;
             }
             const float b = f.bias ? load_float(f.bias, f.bias_f32, n) : 0.f;
@@ -81,18 +64,18 @@ struct LinearEpilogue {
             if (f.pre)
 #pragma unroll
                 for (int j = 0; j < 32; ++j)
-                    if (j < rows) f.pre[(col0 + j) * f.ldp + n] = to_bf16(v[j]);
+                    if (j < count) f.pre[(col0 + j) * f.ldp + n] = to_bf16(v[j]);
             apply(f.act, v);
             if (f.residual) {
                 float add[32];
 #pragma unroll
-                for (int j = 0; j < 32; ++j) add[j] = j < rows ? load_float(f.residual, f.residual_f32, (col0 + j) * f.ldr + n) : 0.f;
+                for (int j = 0; j < 32; ++j) add[j] = j < count ? load_float(f.residual, f.residual_f32, (col0 + j) * f.ldr + n) : 0.f;
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[j] += add[j];
             }
 #pragma unroll
             for (int j = 0; j < 32; ++j)
-                if (j < rows) store_float(f.out, f.out_f32, (col0 + j) * f.ldo + n, v[j]);
+                if (j < count) store_float(f.out, f.out_f32, (col0 + j) * f.ldo + n, v[j]);
         }
     }
 };
@@ -264,19 +247,13 @@ template <bool PAIR, int NP>
 bool describe(ProductLaunch<NP, 1, LinearEpilogue<PAIR>>& l, int at, const Product& d) {
     const Matrix &p = PAIR ? d.x : d.w, &q = PAIR ? d.w : d.x;
     const Plan& plan = d.plan;
-    const Finish& f = d.f;
-    const int64_t M = d.x.rows, N = d.w.rows;
     l.pr[at] = problem_of(PAIR, p.rows, q.rows, d.K, 1, p.turned, q.turned, false, has_runs(d), plan.cut);
     LinearEpilogue<PAIR>& e = l.epi[at];
-    e.f = f;
+    e.f = d.f;
     e.parts = plan.cut.parts > 1 ? d.parts : nullptr;
     e.ldparts = plan.ldparts;
     e.part_size = plan.part_size;
-    if (!operand_map(&l.p[at][0], p, d.K, kRows) || !operand_map(&l.q[at][0], q, d.K, PAIR ? plan.cut.cols / 2 : plan.cut.cols)) return false;
-    if (!PAIR) return true;
-    if (e.parts) return result_map(&e.out_map, d.parts, true, M, plan.ldparts, plan.ldparts, plan.cut.parts, plan.part_size);
-    return result_map(&e.out_map, f.out, f.out_f32, M, N, f.ldo, 1, M * f.ldo) &&
-           (!f.pre || result_map(&e.pre_map, f.pre, false, M, N, f.ldp, 1, M * f.ldp));
+    return operand_map(&l.p[at][0], p, d.K, kRows) && operand_map(&l.q[at][0], q, d.K, PAIR ? plan.cut.cols / 2 : plan.cut.cols);
 }
 
 acrl_status join_parts(const Product& d, cudaStream_t s) {

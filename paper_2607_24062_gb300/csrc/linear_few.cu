@@ -70,13 +70,18 @@ __global__ void __launch_bounds__(kThreads, T == 1 ? 3 : 2) few_kernel(const __g
                 for (int r = 0; r < T; ++r) x[r][i] = load8(A.x + (8 * r + g) * A.ldx, k, 8 * r + g < A.M ? K : 0);
             }
         }
+        // each turn's products in a sum of their own: the tensor cores cut partial sums off, an error that grows with their number
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i)
+        for (int r = 0; r < T; ++r) {
+            float d[4] = {};
 #pragma unroll
-            for (int r = 0; r < T; ++r) {
-                mma_16x8(c[r], a[i].x, b[i].x, a[i].y, b[i].y, x[r][i].x, x[r][i].y);
-                mma_16x8(c[r], a[i].z, b[i].z, a[i].w, b[i].w, x[r][i].z, x[r][i].w);
+            for (int i = 0; i < kAhead; ++i) {
+                mma_16x8(d, a[i].x, b[i].x, a[i].y, b[i].y, x[r][i].x, x[r][i].y);
+                mma_16x8(d, a[i].z, b[i].z, a[i].w, b[i].w, x[r][i].z, x[r][i].w);
             }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) c[r][j] += d[j];
+        }
     }
 #pragma unroll
     for (int r = 0; r < T; ++r) {

@@ -175,8 +175,7 @@ __device__ __forceinline__ void add_halves(uint2 h, uint2 l, float (&A)[4]) {
     A[3] = bf16_hi(h.y) + bf16_hi(l.y);
 }
 
-// a I + b A + c v at row i, columns j .. j + 31, all of them below ld or left out of the result (zeros beyond the matrix).  A
-// row's 64 bytes of each half come in 16-byte loads: one by one they took three times as long as the product (24 x 1,024 x
+// a I + b A + c v at row i, columns j .. j + 31; what is beyond the matrix is left out of the result.  A row's 64 bytes of each half come in 16-byte loads: one by one they took three times as long as the product (24 x 1,024 x
 // 1,024: 220 us a step against 66 for A itself).
 __device__ __forceinline__ void polynomial(const Finish& f, int64_t at, int i, int j, int m, float (&v)[32]) {
 #pragma unroll
@@ -196,67 +195,37 @@ __device__ __forceinline__ void polynomial(const Finish& f, int64_t at, int i, i
 
 struct StepEpilogue {
     Finish f;
-    CUtensorMap hi, lo;     // of what is written; with parts hi is theirs; of the result hi alone
-    bool parts;
+    float* parts;                  // where the sum is split: [matrix][part][row][ldparts]
+    int64_t ldparts, part_size;
 
-    // Lane i's 32 values as column i of a block.
-    __device__ __forceinline__ void mirror(const CUtensorMap* map, const float (&v)[32], int row0, int col0, int z, WarpOut& out) const {
-        uint8_t* b = out.staging + out.half * (kWarpStaging / 2);
-        out.half ^= 1;
-        if (out.lane == 0) {
-            if (out.whole) bulk_wait_read<0>();
-            else bulk_wait_read<1>();
-        }
-        out.whole = false;
-        __syncwarp();
-        const uint32_t to = smem_u32(b) + uint32_t((out.lane & 7) * 2);
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            const uint32_t piece = uint32_t(out.lane >> 3) ^ uint32_t((j >> 1) & 3);
-            asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + uint32_t(j * 64) + (piece << 4)), "h"(to_bf16(v[j])) : "memory");
-        }
-        fence_async_shared();
-        __syncwarp();
-        if (out.lane == 0) tma_store_3d(map, b, row0, col0, z);
-    }
-
-    __device__ __forceinline__ void chunk(const Problem& pr, const Unit& t, const uint32_t (&r)[32], int row0, int col0,
-                                          WarpOut& out) const {
+    __device__ __forceinline__ void chunk(const Problem& pr, const Unit& t, const uint32_t (&r)[32], int row0, int col0, int rows,
+                                          int cols, const WarpOut& out) const {
         float v[32];
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
         if (parts) {
-            out.store<float>(&hi, v, row0, col0, t.z * pr.parts + t.part);
+            out.store(parts + (int64_t(t.z) * pr.parts + t.part) * part_size, ldparts, rows, cols, v, row0, col0);
             return;
         }
-        const int row = row0 + out.lane;
         if (f.kind == kResult) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] *= f.scale;
             acrl_bf16* to = f.out + t.z * f.out_stride;
-            if (f.tall) {   // the lanes' stores are of neighbours
-                if (row < pr.rows)
-#pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (col0 + j < pr.cols_all) to[(col0 + j) * f.ldo + row] = to_bf16(v[j]);
-            } else if (col0 + 32 > pr.cols_all && (pr.cols_all & 7)) {
-                if (row < pr.rows)
-#pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (col0 + j < pr.cols_all) to[row * f.ldo + col0 + j] = to_bf16(v[j]);
-            } else {
-                out.store<acrl_bf16>(&hi, v, row0, col0, t.z);
-            }
+            if (f.tall) out.store_turned(to, f.ldo, cols, rows, v, col0, row0);
+            else out.store(to, f.ldo, rows, cols, v, row0, col0);
             return;
         }
-        if (f.kind == kPolynomial) polynomial(f, t.z * f.size + row * f.ld + col0, row, col0, pr.rows, v);
+        const int row = row0 + out.lane;
+        if (f.kind == kPolynomial) polynomial(f, t.z * f.size + row * f.ld + col0, row, col0, rows, v);
         const bool twice = pr.lower && col0 < t.tp * 2 * kRows;   // a tile above the diagonal has no other way to be written
-        out.store<acrl_bf16>(&hi, v, row0, col0, t.z);
-        if (twice) mirror(&hi, v, row0, col0, t.z, out);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] -= bf16_to_float(to_bf16(v[j]));
-        out.store<acrl_bf16>(&lo, v, row0, col0, t.z);
-        if (twice) mirror(&lo, v, row0, col0, t.z, out);
+        for (int half = 0; half < 2; ++half) {
+            acrl_bf16* to = (half ? f.lo : f.hi) + t.z * f.size;
+            out.store(to, f.ld, rows, cols, v, row0, col0);
+            if (twice) out.store_turned(to, f.ld, cols, rows, v, col0, row0);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] -= bf16_to_float(to_bf16(v[j]));   // what is left for the other
+        }
     }
 };
 
@@ -388,21 +357,14 @@ acrl_status step_product(const Plan& plan, int64_t batch, int64_t rows, int64_t 
     l.pr[0] = problem_of(true, rows, cols, K, batch, false, q_turned, lower, false, plan.cut);
     StepEpilogue& e = l.epi[0];
     e.f = f;
-    e.parts = plan.cut.parts > 1;
+    e.parts = plan.cut.parts > 1 ? parts : nullptr;
+    e.ldparts = plan.ldparts;
+    e.part_size = plan.part_size;
     for (int i = 0; i < 2; ++i) {
         if (!operand_map(&l.p[0][i], Matrix{i ? p.lo : p.hi, rows, p.ld, false, batch, p.size}, K, kRows) ||
             !operand_map(&l.q[0][i], Matrix{i ? q.lo : q.hi, cols, q.ld, q_turned, batch, q.size}, K, plan.cut.cols / 2))
             return ACRL_ERR_CUDA;
     }
-    bool ok;
-    if (e.parts) {
-        ok = result_map(&e.hi, parts, true, rows, plan.ldparts, plan.ldparts, batch * plan.cut.parts, plan.part_size);
-    } else if (f.kind == kResult) {
-        ok = f.tall || result_map(&e.hi, f.out, false, rows, cols, f.ldo, batch, batch > 1 ? f.out_stride : rows * f.ldo);
-    } else {
-        ok = result_map(&e.hi, f.hi, false, rows, f.ld, f.ld, batch, f.size) && result_map(&e.lo, f.lo, false, rows, f.ld, f.ld, batch, f.size);
-    }
-    if (!ok) return ACRL_ERR_CUDA;
     const acrl_status st = launch_product<true, false>(l, flags, s);
     if (st != ACRL_OK || !e.parts) return st;
     return launch(join_kernel, batch * ((rows + 31) / 32) * ((cols + 31) / 32), 256, 0, 0, s, f, static_cast<const float*>(parts),
