@@ -698,14 +698,27 @@ def _act(act) -> int:
     return code
 
 
+def _operand(t, name: str):
+    """(rows, columns, row stride) of a 2-D bf16 CUDA tensor; these calls are short, and each look at a tensor costs."""
+    if isinstance(t, torch.Tensor) and t.dtype is torch.bfloat16 and t.is_cuda:
+        shape = t.shape
+        if len(shape) == 2:
+            R, C = shape
+            ld, cs = t.stride()
+            if cs == 1 or C <= 1:
+                return R, C, ld if R > 1 and C > 0 else (C + 7) // 8 * 8
+    raise AcrlError(f"{name}: expected a 2-D bfloat16 CUDA tensor with unit column stride")
+
+
+_BF16_ONLY, _BF16_F32 = (torch.bfloat16,), (torch.bfloat16, torch.float32)
+
+
 def _given(t, M: int, N: int, dtypes, name: str):
-    """(`t`, its row stride) of a matrix [M, N] that the caller gives, None and 0 for None."""
-    if t is None:
-        return None, 0
+    """The row stride of a matrix [M, N] that the caller gives."""
     if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or t.dim() != 2 or not t.is_cuda or \
-            (N > 1 and t.stride(1) != 1) or tuple(t.shape) != (M, N):
+            (N > 1 and t.stride(1) != 1) or t.shape[0] != M or t.shape[1] != N:
         raise AcrlError(f"{name}: expected a CUDA matrix of {(M, N)}, {' or '.join(str(d) for d in dtypes)}, with unit column stride")
-    return t, t.stride(0) if M > 1 and N > 0 else (N + 7) // 8 * 8
+    return t.stride(0) if M > 1 and N > 0 else (N + 7) // 8 * 8
 
 
 def _workspace(workspace, n: int, dev):
@@ -724,7 +737,8 @@ def linear(x, weight, bias=None, *, act=None, residual=None, pre_out=None, out_d
     """acrl_linear: act(x W^T + bias) + residual as `out_dtype` [M, N].  x bf16 [M, K], weight bf16 [N, K]; bias float32 or
     bfloat16 [N]; `act` is None, "relu", "gelu", "gelu_tanh" or "silu"; residual bfloat16 or float32 [M, N] (`out` itself is
     allowed); `pre_out` bf16 [M, N] takes x W^T + bias, for linear_backward."""
-    (M, K), (N, Kw) = _bf16_rows(x, "x"), _bf16_rows(weight, "weight")
+    M, K, ldx = _operand(x, "x")
+    N, Kw, ldw = _operand(weight, "weight")
     if stream is not None:
         return _on_stream(linear, "acrl_linear", x, stream, x, weight, bias, act=act, residual=residual, pre_out=pre_out,
                           out_dtype=out_dtype, out=out, workspace=workspace, flags=flags)
@@ -732,23 +746,29 @@ def linear(x, weight, bias=None, *, act=None, residual=None, pre_out=None, out_d
         raise AcrlError(f"x and weight disagree on K: {K} and {Kw}")
     if out_dtype not in _OUT_DTYPE:
         raise AcrlError(f"out_dtype: {out_dtype}, expected bfloat16 or float32")
-    if bias is not None and (not isinstance(bias, torch.Tensor) or bias.dtype not in _OUT_DTYPE or tuple(bias.shape) != (N,) or
-                             not bias.is_cuda or not bias.is_contiguous()):
-        raise AcrlError(f"bias: expected a contiguous float32 or bfloat16 CUDA vector of {N}")
     code = _act(act)
-    residual, ldr = _given(residual, M, N, (torch.bfloat16, torch.float32), "residual")
-    pre_out, ldp = _given(pre_out, M, N, (torch.bfloat16,), "pre_out")
+    pb = pr = pp = None
+    tb = tr = ldr = ldp = 0
+    if bias is not None:
+        if not isinstance(bias, torch.Tensor) or bias.dtype not in _OUT_DTYPE or tuple(bias.shape) != (N,) or \
+                not bias.is_cuda or not bias.is_contiguous():
+            raise AcrlError(f"bias: expected a contiguous float32 or bfloat16 CUDA vector of {N}")
+        pb, tb = bias.data_ptr(), _OUT_DTYPE[bias.dtype]
+    if residual is not None:
+        ldr = _given(residual, M, N, _BF16_F32, "residual")
+        pr, tr = residual.data_ptr(), _OUT_DTYPE[residual.dtype]
+    if pre_out is not None:
+        ldp = _given(pre_out, M, N, _BF16_ONLY, "pre_out")
+        pp = pre_out.data_ptr()
     out, ldo = _product_out(out, M, N, out_dtype, x.device)
     n = lib().acrl_linear_workspace_bytes(M, N, K)
-    workspace = _workspace(workspace, n, x.device)
+    if n > 0 or workspace is not None:
+        workspace = _workspace(workspace, n, x.device)
     if flags is not None:
         _need(flags, torch.int32, 1, "flags")
-    _call("acrl_linear", (x, weight, bias, residual, pre_out, out, workspace, flags), None, x.data_ptr(), M, K, _ld(x),
-          weight.data_ptr(), N, _ld(weight), None if bias is None else bias.data_ptr(),
-          0 if bias is None else _OUT_DTYPE[bias.dtype], code, None if residual is None else residual.data_ptr(),
-          0 if residual is None else _OUT_DTYPE[residual.dtype], ldr, None if pre_out is None else pre_out.data_ptr(), ldp,
-          out.data_ptr(), _OUT_DTYPE[out.dtype], ldo, None if workspace is None else workspace.data_ptr(), n,
-          None if flags is None else flags.data_ptr())
+    _call("acrl_linear", (x, weight, bias, residual, pre_out, out, workspace, flags), None, x.data_ptr(), M, K, ldx,
+          weight.data_ptr(), N, ldw, pb, tb, code, pr, tr, ldr, pp, ldp, out.data_ptr(), _OUT_DTYPE[out.dtype], ldo,
+          None if workspace is None else workspace.data_ptr(), n, None if flags is None else flags.data_ptr())
     return out
 
 
@@ -762,13 +782,14 @@ def linear_backward(dy, x, weight, *, act=None, pre=None, bias=False, need_dx=Tr
     """acrl_linear_backward, the gradients of linear: with g = dy act'(pre), dx = g W, dw = g^T x and, with `bias`,
     dbias = sum of g over the rows.  dy bf16 [M, N], x bf16 [M, K], weight bf16 [N, K], `pre` the bf16 [M, N] that linear
     wrote.  Returns (dx [M, K], dw [N, K], dbias float32 [N]), None where not asked for; the gradient of the residual is dy."""
-    (M, N), (Mx, K) = _bf16_rows(dy, "dy"), _bf16_rows(x, "x")
-    Nw, Kw = _bf16_rows(weight, "weight")
+    M, N, lddy = _operand(dy, "dy")
+    Mx, K, ldx = _operand(x, "x")
+    Nw, Kw, ldw = _operand(weight, "weight")
     if stream is not None:
         return _on_stream(linear_backward, "acrl_linear_backward", dy, stream, dy, x, weight, act=act, pre=pre, bias=bias,
                           need_dx=need_dx, need_dw=need_dw, dx_dtype=dx_dtype, dw_dtype=dw_dtype, dx=dx, dw=dw, dbias=dbias,
                           workspace=workspace, flags=flags)
-    if Mx != M or (Nw, Kw) != (N, K):
+    if Mx != M or Nw != N or Kw != K:
         raise AcrlError(f"dy {(M, N)}, x {(Mx, K)} and weight {(Nw, Kw)} do not belong together")
     if dx_dtype not in _OUT_DTYPE or dw_dtype not in _OUT_DTYPE:
         raise AcrlError("dx_dtype, dw_dtype: expected bfloat16 or float32")
@@ -777,19 +798,26 @@ def linear_backward(dy, x, weight, *, act=None, pre=None, bias=False, need_dx=Tr
         raise AcrlError(f"act={act!r} takes " + ("no pre" if act is None else "pre, the pre-activation that linear wrote"))
     if (dx is not None and not need_dx) or (dw is not None and not need_dw) or (dbias is not None and not bias):
         raise AcrlError("dx, dw, dbias: an output that is not asked for")
-    pre, ldp = _given(pre, M, N, (torch.bfloat16,), "pre")
+    ldp = 0 if pre is None else _given(pre, M, N, _BF16_ONLY, "pre")
     dev = dy.device
-    dx, lddx = _product_out(dx, M, K, dx_dtype, dev) if need_dx else (None, 0)
-    dw, lddw = _product_out(dw, N, K, dw_dtype, dev) if need_dw else (None, 0)
-    dbias = _vec(dbias, torch.float32, N, "dbias", dev) if bias else None
+    px = pw = pb = None
+    tx = tw = lddx = lddw = 0
+    if need_dx:
+        dx, lddx = _product_out(dx, M, K, dx_dtype, dev)
+        px, tx = dx.data_ptr(), _OUT_DTYPE[dx.dtype]
+    if need_dw:
+        dw, lddw = _product_out(dw, N, K, dw_dtype, dev)
+        pw, tw = dw.data_ptr(), _OUT_DTYPE[dw.dtype]
+    if bias:
+        dbias = _vec(dbias, torch.float32, N, "dbias", dev)
+        pb = dbias.data_ptr()
     n = lib().acrl_linear_backward_workspace_bytes(M, N, K)
     workspace = _workspace(workspace, n, dev)
     if flags is not None:
         _need(flags, torch.int32, 1, "flags")
-    _call("acrl_linear_backward", (dy, x, weight, pre, dx, dw, dbias, workspace, flags), None, dy.data_ptr(), M, N, _ld(dy),
-          x.data_ptr(), K, _ld(x), weight.data_ptr(), _ld(weight), code, _ptr(pre), ldp, _ptr(dx),
-          0 if dx is None else _OUT_DTYPE[dx.dtype], lddx, _ptr(dw), 0 if dw is None else _OUT_DTYPE[dw.dtype], lddw, _ptr(dbias),
-          _ptr(workspace), n, _ptr(flags))
+    _call("acrl_linear_backward", (dy, x, weight, pre, dx, dw, dbias, workspace, flags), None, dy.data_ptr(), M, N, lddy,
+          x.data_ptr(), K, ldx, weight.data_ptr(), ldw, code, _ptr(pre), ldp, px, tx, lddx, pw, tw, lddw, pb, _ptr(workspace), n,
+          _ptr(flags))
     return dx, dw, dbias
 
 
@@ -808,6 +836,17 @@ def _matrices(t, name: str):
     return B, m, n, ld, t.stride(0) if t.dim() == 3 and B > 1 else m * ld
 
 
+def _step_coeffs(coeffs, steps) -> list[float]:
+    """Three numbers for each step, from one triple or from as many as there are steps."""
+    try:
+        c = np.asarray(coeffs, dtype=np.float32)
+        if isinstance(steps, int) and steps >= 1 and c.shape in ((3,), (steps, 3)):
+            return np.broadcast_to(c, (steps, 3)).ravel().tolist()
+    except (TypeError, ValueError):
+        pass
+    raise AcrlError("steps, coeffs: expected a number of steps, and three numbers, or three for each of them")
+
+
 def orthogonalize(g, *, steps=5, coeffs=(3.4445, -4.7750, 2.0315), eps=1e-7, scale=1.0, out=None, workspace=None, flags=None,
                   stream=None):
     """acrl_orthogonalize: an update, bf16 or float32 [m, n] or a batch [B, m, n] of them, with its singular values brought
@@ -819,10 +858,7 @@ def orthogonalize(g, *, steps=5, coeffs=(3.4445, -4.7750, 2.0315), eps=1e-7, sca
         return _on_stream(orthogonalize, "acrl_orthogonalize", g, stream, g, steps=steps, coeffs=coeffs, eps=eps, scale=scale,
                           out=out, workspace=workspace, flags=flags)
     B, m, n, ldg, stride = _matrices(g, "g")
-    coeffs = np.asarray(coeffs, dtype=np.float32)
-    if not isinstance(steps, int) or coeffs.shape not in ((3,), (steps, 3)):
-        raise AcrlError("coeffs: expected three numbers, or three for each of the steps")
-    flat = (coeffs if coeffs.ndim == 2 else np.tile(coeffs, max(steps, 1))).ravel().tolist()
+    flat = _step_coeffs(coeffs, steps)
     if out is None:
         ld = (n + 7) // 8 * 8
         out = torch.empty_strided(g.shape, ((ld, 1) if g.dim() == 2 else (m * ld, ld, 1)), dtype=torch.bfloat16, device=g.device)
