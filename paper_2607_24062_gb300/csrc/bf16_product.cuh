@@ -14,7 +14,10 @@
 // Alone: a CTA has 128 rows of p and up to 128 columns.  For few rows of a layer's input, which then are the columns: p is
 //   the weight, so that no product is made and nothing is loaded for rows that are not there.
 //
-// A long sum over few tiles is split: the parts' accumulators go to a workspace in fp32, and the caller joins them in order.
+// Where tiles are few their sums are split: the parts' accumulators go to a workspace in fp32, and the caller joins them in
+// order.  (Splitting only the tiles of a part-filled last round, so that it fills up, gained less than its join takes: 24 x
+// 1,024 x 1,024 in three rounds and a sixth 61 us and 9 for the join, in four 66; at the power cap a round that leaves SMs idle
+// runs at a higher clock anyway.)
 //
 // The tensor cores cut partial sums off where they should round them: an error toward zero that grows with the length of a run
 // (relative to the result's norm, of normal numbers: 0.7e-6 for a sum of 1,027, 1.7e-6 for 2,507).  bf16 hides it; for an fp32
@@ -71,17 +74,24 @@ struct Problem {
     int batch;
     int cols;                // of a tile: a multiple of 32 (pair; of 128 where q is not K-major) or of 16 (alone)
     int p_tiles, q_tiles;
-    int parts, per;          // of the sum, and slabs of each
+    int parts, per;          // of the sum, of so many slabs
     int run;                 // slabs that one accumulator takes
     int lower;               // tiles that lie above the diagonal's are left out: the result is symmetric
     int p_turned, q_turned;  // the operand lies with the sum along its columns
     uint32_t idesc;
-    int tiles, units;        // tiles of one matrix and part; all
+    int tiles, units;        // tiles of one matrix; parts of all
+    int pair;
+
+    __host__ __device__ int high() const { return pair ? 2 * kRows : kRows; }
+    // The result's rows and columns of a tile: alone, the rows of q are the result's.
+    __host__ __device__ int tile_rows() const { return pair ? 2 * kRows : cols; }
+    __host__ __device__ int tile_cols() const { return pair ? cols : kRows; }
 };
 
 // What a CTA or pair works on at a time.
 struct Unit {
     int tp, tq, z, part, lo, hi;
+    int all;   // the tile among all matrices'
 };
 
 template <int NP, int TERMS, class Epi>
@@ -97,14 +107,12 @@ struct ProductLaunch {
 // Tiles in bands of kBand row tiles, all column tiles of a band in turn, so that the tiles in flight share operands in L2.
 constexpr int kBand = 16;
 
-template <bool PAIR>
-__device__ __forceinline__ Unit unit_at(const Problem& pr, int u) {
+// Tile `all` of all matrices'.
+__device__ __forceinline__ Unit tile_at(const Problem& pr, int all) {
     Unit w;
-    const int t = u % pr.tiles, zp = u / pr.tiles;
-    w.part = zp % pr.parts;
-    w.z = zp / pr.parts;
-    w.lo = w.part * pr.per;
-    w.hi = min(pr.slabs, w.lo + pr.per);
+    w.all = all;
+    w.z = all / pr.tiles;
+    const int t = all - w.z * pr.tiles;
     if (pr.lower) {
         // row tile i has min(q_tiles, (i + 1) r) column tiles, r of them as wide as a row tile is high: r i (i + 1) / 2 before it
         const int r = 2 * kRows / pr.cols;
@@ -119,6 +127,14 @@ __device__ __forceinline__ Unit unit_at(const Problem& pr, int u) {
         w.tp = band * kBand + k % h;
         w.tq = k / h;
     }
+    return w;
+}
+
+__device__ __forceinline__ Unit unit_at(const Problem& pr, int u) {
+    Unit w = tile_at(pr, u / pr.parts);
+    w.part = u - w.all * pr.parts;
+    w.lo = w.part * pr.per;
+    w.hi = min(pr.slabs, w.lo + pr.per);
     return w;
 }
 
@@ -144,7 +160,7 @@ struct Units {
         turn();
     }
     __device__ __forceinline__ const Problem& problem() const { return l.pr[NP == 2 ? which : 0]; }
-    __device__ __forceinline__ Unit unit() const { return unit_at<PAIR>(problem(), u); }
+    __device__ __forceinline__ Unit unit() const { return unit_at(problem(), u); }
 };
 
 // The descriptor of an operand's tile: rows of 128 bytes along the sum, or 64 x 64 blocks in which the sum runs from row to row:
@@ -564,48 +580,140 @@ inline bool operand_map(CUtensorMap* map, const Matrix& m, int64_t K, int box_ro
                                     uint64_t(m.ld), uint64_t(m.apart), uint32_t(box_rows), kSlab, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-// How a product is cut.
+// How a product is cut: columns of a tile, tiles of all matrices, and the sum's parts of `per` slabs.
 struct Cut {
-    int cols, parts, per;
+    int cols;
+    int64_t tiles;
+    int parts, per;
+
+    int64_t units() const { return tiles * parts; }
 };
+
+// What is cut.  cols from `widest` down to `least` in steps of `step`, or halves for 0.
+struct Shape {
+    bool pair;
+    int64_t rows, cols_all, K, batch;
+    bool lower;
+    int terms, widest, least, step;
+
+    int64_t slabs() const { return std::max<int64_t>(1, (K + kSlab - 1) / kSlab); }
+    int high() const { return pair ? 2 * kRows : kRows; }
+    int64_t lanes() const { return pair ? 76 : 152; }   // what a GPU of 152 SMs runs at once
+    int64_t tiles(int cols) const {
+        const int64_t p = (rows + high() - 1) / high(), q = (cols_all + cols - 1) / cols, r = high() / cols;
+        // of a symmetric matrix, each row tile but the last has r columns more than the one before
+        return batch * (lower && p > 0 ? r * (p - 1) * p / 2 + q : p * q);
+    }
+    // Cycles of a slab: the MMAs, or the copies at 52 bytes a cycle of an SM.
+    int64_t slab(int cols) const {
+        const int64_t mats = terms == 3 ? 2 : 1, mine = pair ? cols / 2 : cols;
+        return std::max<int64_t>(terms * (pair ? 2 : 4) * int64_t(cols), mats * (kRows + mine) * kRowBytes / 52);
+    }
+    int64_t tile_bytes(int cols) const { return int64_t(high()) * cols * 4; }
+    int next(int cols) const { return step > 0 ? cols - step : cols / 2; }
+};
+
+constexpr int64_t kTileCycles = 500;                             // of a tile in a run of them
+constexpr int64_t kJoinCycles = 5000, kJoinBytes = 3000;         // of a join's launch; bytes a cycle
+constexpr int kPartChoices[] = {2, 3, 4, 5, 6, 8, 10, 12, 16};
+
+// Parts of equal length, none of them empty: false where `parts` is no such number.
+inline bool part_length(int64_t slabs, int64_t parts, int64_t& per) {
+    if (parts > slabs) return false;
+    per = (slabs + parts - 1) / parts;
+    return (slabs + per - 1) / per == parts;
+}
+
+inline int64_t join_cycles(const Shape& s, const Cut& c) {
+    return c.parts == 1 ? 0 : kJoinCycles + c.tiles * (c.parts + 1) * s.tile_bytes(c.cols) / kJoinBytes;
+}
+inline int64_t unit_cycles(const Shape& s, const Cut& c) { return c.per * s.slab(c.cols) + kTileCycles; }
+
+// consider(cut) for the whole sums of tiles of `cols` columns and, where there are no more than `few` tiles, for parts of them.
+template <typename F>
+void each_cut(const Shape& s, int cols, int64_t few, F consider) {
+    const int64_t tiles = s.tiles(cols), slabs = s.slabs();
+    consider(Cut{cols, tiles, 1, int(slabs)});
+    for (int64_t parts : kPartChoices) {
+        int64_t per;
+        if (tiles > few || tiles * (parts - 1) >= 2 * s.lanes()) break;
+        if (part_length(slabs, parts, per)) consider(Cut{cols, tiles, int(parts), int(per)});
+    }
+}
+
+// The cut with the least estimated time: rounds of units, and the joining of parts.
+inline Cut best_cut(const Shape& s) {
+    const int64_t lanes = s.lanes();
+    Cut best = {};
+    int64_t least = -1;
+    for (int cols = s.widest; cols >= s.least; cols = s.next(cols))
+        each_cut(s, cols, 2 * lanes, [&](const Cut& c) {
+            const int64_t cost = (c.units() + lanes - 1) / lanes * unit_cycles(s, c) + join_cycles(s, c);
+            if (least >= 0 && cost >= least) return;
+            least = cost;
+            best = c;
+        });
+    return best;
+}
+
+// Two products in one launch, the second's units after the first's: the cycles of the busiest lane, whose units are every
+// lanes-th.
+inline int64_t two_cycles(const Shape& s0, const Cut& c0, const Shape& s1, const Cut& c1) {
+    const int64_t lanes = s0.lanes(), a = c0.units(), b = a + c1.units();
+    auto upto = [&](int64_t x, int64_t lane) { return x > lane ? (x - lane + lanes - 1) / lanes : 0; };
+    int64_t most = 0;
+    for (int64_t lane : {int64_t(0), a % lanes, b % lanes}) {   // where the counts change
+        const int64_t n = upto(a, lane);
+        most = std::max(most, n * unit_cycles(s0, c0) + (upto(b, lane) - n) * unit_cycles(s1, c1));
+    }
+    return most + join_cycles(s0, c0) + join_cycles(s1, c1);
+}
+
+// Cuts both for one launch.
+inline void best_cuts(const Shape& s0, const Shape& s1, Cut& best0, Cut& best1) {
+    int64_t least = -1;
+    for (int cols = s0.widest; cols >= s0.least; cols = s0.next(cols))
+        each_cut(s0, cols, s0.lanes(), [&](const Cut& c0) {
+            each_cut(s1, cols, s0.lanes(), [&](const Cut& c1) {
+                const int64_t cost = two_cycles(s0, c0, s1, c1);
+                if (least >= 0 && cost >= least) return;
+                least = cost;
+                best0 = c0;
+                best1 = c1;
+            });
+        });
+}
+
+// The parts' workspace: [tile][part][row of the tile][column of it].
+inline int64_t parts_bytes(const Shape& s, const Cut& c) { return c.parts == 1 ? 0 : c.units() * s.tile_bytes(c.cols); }
 
 // tcgen05.mma kind::f16: D f32 (bits 4-5 = 1), A and B bf16 (bits 7-9, 10-12 = 1), A and B transposed (bits 15, 16),
 // N / 8 at bit 17, M / 16 at bit 24.
-inline Problem problem_of(bool pair, int64_t rows, int64_t cols_all, int64_t K, int64_t batch, bool p_turned, bool q_turned,
-                          bool lower, bool runs, const Cut& cut) {
+inline Problem problem_of(const Shape& s, const Cut& cut, bool p_turned, bool q_turned, bool runs) {
     Problem pr = {};
-    const int high = pair ? 2 * kRows : kRows;
-    pr.rows = int(rows);
-    pr.cols_all = int(cols_all);
-    pr.slabs = int((K + kSlab - 1) / kSlab);
-    pr.batch = int(batch);
+    pr.rows = int(s.rows);
+    pr.cols_all = int(s.cols_all);
+    pr.slabs = int(s.slabs());
+    pr.batch = int(s.batch);
     pr.cols = cut.cols;
-    pr.p_tiles = int((rows + high - 1) / high);
-    pr.q_tiles = int((cols_all + cut.cols - 1) / cut.cols);
+    pr.pair = s.pair;
+    pr.p_tiles = int((s.rows + s.high() - 1) / s.high());
+    pr.q_tiles = int((s.cols_all + cut.cols - 1) / cut.cols);
     pr.parts = cut.parts;
     pr.per = cut.per;
     pr.run = runs ? kRun : pr.slabs;
-    pr.lower = lower;
+    pr.lower = s.lower;
     pr.p_turned = p_turned;
     pr.q_turned = q_turned;
     pr.idesc = 1u << 4 | 1u << 7 | 1u << 10 | uint32_t(p_turned) << 15 | uint32_t(q_turned) << 16 |
-               uint32_t(cut.cols >> 3) << 17 | uint32_t(high >> 4) << 24;
-    if (lower) {
-        const int r = high / cut.cols, last = pr.p_tiles - 1;   // all row tiles but the last have r columns more than the one before
-        pr.tiles = r * last * (last + 1) / 2 + pr.q_tiles;
-    } else {
-        pr.tiles = pr.p_tiles * pr.q_tiles;
-    }
-    pr.units = pr.tiles * pr.parts * pr.batch;
+               uint32_t(cut.cols >> 3) << 17 | uint32_t(s.high() >> 4) << 24;
+    pr.tiles = int(cut.tiles / std::max<int64_t>(1, s.batch));
+    pr.units = int(cut.units());
     return pr;
 }
 
-// Units beyond 32 bits are refused by the caller: rows / 128 x columns / 16 x parts x batch.
-inline bool units_fit(bool pair, int64_t rows, int64_t cols_all, int64_t batch, const Cut& cut) {
-    const int64_t high = pair ? 2 * kRows : kRows;
-    const double n = double((rows + high - 1) / high) * double((cols_all + cut.cols - 1) / cut.cols) * cut.parts * double(batch);
-    return n < 1e9;
-}
+// More units than an int counts are refused by the caller.
+inline bool units_fit(const Cut& cut) { return cut.tiles < (1 << 30) && cut.units() < (1 << 30); }
 
 // Allows the kernel its shared memory; the pairs, or CTAs alone, that can be resident at once: kept for the device that the
 // calling thread used last.

@@ -8,7 +8,6 @@
 namespace acrl {
 namespace {
 
-constexpr int kPairs = 76;           // of SMs: what a cut is made for
 constexpr int64_t kAloneRows = 128;  // rows that become a CTA's columns
 
 // A tile's accumulators on their way out.  Pair: a lane has a row of the result and 32 of its columns.  Alone: p is the
@@ -16,8 +15,7 @@ constexpr int64_t kAloneRows = 128;  // rows that become a CTA's columns
 template <bool PAIR>
 struct LinearEpilogue {
     Finish f;
-    float* parts;                   // where the sum is split: [part][row][ldparts]
-    int64_t ldparts, part_size;
+    float* parts;                   // of the tiles
 
     __device__ __forceinline__ void chunk(const Problem& pr, const Unit& t, const uint32_t (&r)[32], int row0, int col0, int rows,
                                           int cols, const WarpOut& out) const {
@@ -25,8 +23,10 @@ struct LinearEpilogue {
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
         if constexpr (PAIR) {
-            if (parts) {
-                out.store(parts + t.part * part_size, ldparts, rows, cols, v, row0, col0);
+            if (pr.parts > 1) {
+                const int high = pr.tile_rows(), wide = pr.tile_cols();
+                out.store(parts + (int64_t(t.all) * pr.parts + t.part) * high * wide, wide, rows > 0 ? high : 0, wide, v,
+                          row0 - t.tp * high, col0 - t.tq * wide);
                 return;
             }
             const int row = row0 + out.lane;
@@ -51,11 +51,11 @@ struct LinearEpilogue {
             const int64_t n = row0 + out.lane;
             if (n >= rows) return;
             const int count = cols - col0;   // of the result's rows that this chunk has, of 32
-            if (parts) {
-                float* to = parts + t.part * part_size + col0 * ldparts + n;
+            if (pr.parts > 1) {
+                float* to = parts + ((int64_t(t.all) * pr.parts + t.part) * pr.cols + col0 - t.tq * pr.cols) * kRows + n - t.tp * kRows;
 #pragma unroll
                 for (int j = 0; j < 32; ++j)
-                    if (j < count) to[j * ldparts] = v[j];
+                    if (j < count) to[j * kRows] = v[j];
                 return;
             }
             const float b = f.bias ? load_float(f.bias, f.bias_f32, n) : 0.f;
@@ -80,155 +80,109 @@ struct LinearEpilogue {
     }
 };
 
-// The parts of a split sum in their order, and what follows; no parts are the empty sum.  A thread has four columns of a row.
-__global__ void __launch_bounds__(256) join_kernel(Finish f, const float* parts, int count, int64_t ldparts, int64_t part_size, int M,
-                                                   int N) {
+// The parts of the tiles in their order, and what follows; without parts the sum is empty.  A CTA has kJoinRows rows of a
+// tile, a thread four columns of some.
+constexpr int kJoinRows = 16;
+
+__global__ void __launch_bounds__(256) join_kernel(Finish f, const float* parts, Problem pr, int M, int N) {
     grid_begin();
-    const int64_t quads = (N + 3) / 4, i = int64_t(blockIdx.x) * 256 + threadIdx.x;
-    if (i >= quads * M) return;
-    const int64_t row = i / quads;
-    const int c = int(i - row * quads) * 4;
-    float v[4] = {};
-    for (int p = 0; p < count; ++p) {
-        const float4 x = *reinterpret_cast<const float4*>(parts + p * part_size + row * ldparts + c);
-        v[0] += x.x;
-        v[1] += x.y;
-        v[2] += x.z;
-        v[3] += x.w;
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (f.bias && c + j < N) v[j] += load_float(f.bias, f.bias_f32, c + j);
-    auto store = [&](void* to, bool f32, int64_t ld) {
-        if (c + 4 > N) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (c + j < N) store_float(to, f32, row * ld + c + j, v[j]);
-        } else if (f32) {
-            *reinterpret_cast<float4*>(static_cast<float*>(to) + row * ld + c) = make_float4(v[0], v[1], v[2], v[3]);
-        } else {
-            *reinterpret_cast<uint2*>(static_cast<acrl_bf16*>(to) + row * ld + c) =
-                make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+    const int high = pr.tile_rows(), wide = pr.tile_cols(), strips = (high + kJoinRows - 1) / kJoinRows;
+    const int tile = int(blockIdx.x) / strips, strip = int(blockIdx.x) - tile * strips;
+    const Unit t = tile_at(pr, tile);
+    const int r0 = (pr.pair ? t.tp : t.tq) * high, c0 = (pr.pair ? t.tq : t.tp) * wide, quads = wide / 4;
+    for (int i = threadIdx.x; i < kJoinRows * quads; i += 256) {
+        const int r = strip * kJoinRows + i / quads, at = i % quads * 4, c = c0 + at;
+        const int64_t row = r0 + r;
+        if (r >= high || row >= M || c >= N) continue;
+        float v[4] = {};
+        const float* p = parts + (int64_t(tile) * pr.parts * high + r) * wide + at;
+        for (int k = 0; k < pr.parts; ++k) {
+            const float4 x = *reinterpret_cast<const float4*>(p + int64_t(k) * high * wide);
+            v[0] += x.x;
+            v[1] += x.y;
+            v[2] += x.z;
+            v[3] += x.w;
         }
-    };
-    if (f.pre) store(f.pre, false, f.ldp);
-    apply(f.act, v);
-    if (f.residual) {
-        float add[4];
-        load_row(f.residual, f.residual_f32, row * f.ldr, c, N, add);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] += add[j];
+        for (int j = 0; j < 4; ++j)
+            if (f.bias && c + j < N) v[j] += load_float(f.bias, f.bias_f32, c + j);
+        auto store = [&](void* to, bool f32, int64_t ld) {
+            if (c + 4 > N) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (c + j < N) store_float(to, f32, row * ld + c + j, v[j]);
+            } else if (f32) {
+                *reinterpret_cast<float4*>(static_cast<float*>(to) + row * ld + c) = make_float4(v[0], v[1], v[2], v[3]);
+            } else {
+                *reinterpret_cast<uint2*>(static_cast<acrl_bf16*>(to) + row * ld + c) =
+                    make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+            }
+        };
+        if (f.pre) store(f.pre, false, f.ldp);
+        apply(f.act, v);
+        if (f.residual) {
+            float add[4];
+            load_row(f.residual, f.residual_f32, row * f.ldr, c, N, add);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] += add[j];
+        }
+        store(f.out, f.out_f32, f.ldo);
     }
-    store(f.out, f.out_f32, f.ldo);
 }
 
-// How a product of M x N results over K is made.
+// How a product of M x N results over K is made: x has the rows, w the columns, either turned.
 struct Plan {
-    bool alone;
+    Shape shape;
     Cut cut;
-    int64_t cost, workspace;   // cycles by estimate; bytes
-    int64_t ldparts, part_size;
+    int64_t workspace;
 };
 
-constexpr int64_t kTile = 2000, kJoin = 6000, kJoinBytes = 3000;   // a tile's and a join's cycles, and its bytes a cycle
-constexpr int kPartChoices[] = {1, 2, 3, 4, 6, 8, 12, 16};
-
-int64_t slabs_of(int64_t K) { return std::max<int64_t>(1, (K + kSlab - 1) / kSlab); }
-// A pair's slab: its MMAs, or its loads at 64 bytes a cycle.
-int64_t pair_slab(int cols) { return std::max(2 * cols, 2 * (kRows + cols / 2)); }
-int64_t pair_tiles(int64_t M, int64_t N, int cols) { return (M + 2 * kRows - 1) / (2 * kRows) * ((N + cols - 1) / cols); }
-
-// Parts of equal length, none of them empty: false where `parts` is no such number.
-bool part_length(int64_t slabs, int64_t parts, int64_t& per) {
-    if (parts > slabs) return false;
-    per = (slabs + parts - 1) / parts;
-    return (slabs + per - 1) / per == parts;
+Shape shape_of(int64_t M, int64_t N, int64_t K, bool x_turned, bool w_turned) {
+    if (M > kAloneRows) return Shape{true, M, N, K, 1, false, 1, 256, w_turned ? 128 : 64, w_turned ? 128 : 32};   // blocks of 64 a CTA
+    const int64_t to = x_turned ? 64 : 16;
+    const int cols = int(std::max<int64_t>(1, (M + to - 1) / to) * to);
+    return Shape{false, N, M, K, 1, false, 1, cols, cols, cols};
 }
 
-void set_cut(Plan& plan, int64_t M, int64_t N, const Cut& cut) {
-    plan.cut = cut;
-    plan.ldparts = (N + 7) / 8 * 8;
-    plan.part_size = M * plan.ldparts;
-    plan.workspace = cut.parts > 1 ? cut.parts * plan.part_size * 4 : 0;
-}
+Plan plan_of(const Shape& s, const Cut& cut) { return Plan{s, cut, parts_bytes(s, cut)}; }
 
-// The cut with the least estimated time: rounds of tiles x (slabs x a slab's cycles + a tile's), and the joining of parts.
 Plan plan_of(int64_t M, int64_t N, int64_t K, bool x_turned, bool w_turned) {
-    const int64_t slabs = slabs_of(K);
-    Plan best = {};
-    best.alone = M <= kAloneRows;
-    const int64_t lanes = best.alone ? 2 * kPairs : kPairs;
-    int widest = 256, step = 32, least = 64;   // columns of a tile
-    if (best.alone) widest = least = int(x_turned ? std::max<int64_t>(1, (M + 63) / 64) * 64 : std::max<int64_t>(1, (M + 15) / 16) * 16);
-    else if (w_turned) step = least = 128;     // blocks of 64 a CTA
-    Cut cut = {};
-    for (int cols = widest; cols >= least; cols -= step) {
-        const int64_t tiles = best.alone ? (N + kRows - 1) / kRows : pair_tiles(M, N, cols);
-        const int64_t slab = best.alone ? 2 * (kRows + cols) : pair_slab(cols);
-        for (int64_t parts : kPartChoices) {
-            int64_t per;
-            if (parts > 1 && tiles * (parts - 1) >= 2 * lanes) break;   // there are tiles enough
-            if (!part_length(slabs, parts, per)) continue;
-            const int64_t rounds = (tiles * parts + lanes - 1) / lanes;
-            const int64_t cost = rounds * (per * slab + kTile) + (parts > 1 ? kJoin + (parts + 1) * M * N * 4 / kJoinBytes : 0);
-            if (best.cost == 0 || cost < best.cost) {
-                best.cost = cost;
-                cut = Cut{cols, int(parts), int(per)};
-            }
-        }
-    }
-    set_cut(best, M, N, cut);
-    return best;
+    const Shape s = shape_of(M, N, K, x_turned, w_turned);
+    return plan_of(s, best_cut(s));
 }
 
-// Both products of a backward pass in one launch: the tiles of dw continue where those of dx end, so that a part-filled last
-// round of one is filled by the other.
+// Both products of a backward pass, in one launch where both are made by pairs.
 struct BackwardPlan {
     Plan dx, dw;
     bool together;
 };
 
 BackwardPlan plan_backward(int64_t M, int64_t N, int64_t K) {
-    BackwardPlan b = {plan_of(M, K, N, false, true), plan_of(N, K, M, true, true), false};
-    if (b.dx.alone || b.dw.alone || M == 0 || N == 0 || K == 0) return b;
-    const int64_t s0 = slabs_of(N), s1 = slabs_of(M);
-    int64_t least = 0;
-    Cut cut0 = {}, cut1 = {};
-    for (int cols = 256; cols >= 128; cols -= 128) {
-        const int64_t t0 = pair_tiles(M, K, cols), t1 = pair_tiles(N, K, cols), slab = pair_slab(cols);
-        for (int64_t p0 : kPartChoices) {
-            int64_t per0;
-            if (p0 > 8 || (p0 > 1 && t0 * p0 + t1 > 4 * kPairs)) break;
-            if (!part_length(s0, p0, per0)) continue;
-            const int64_t n0 = t0 * p0, c0 = per0 * slab + kTile, full = n0 % kPairs, each = n0 / kPairs;
-            for (int64_t p1 : kPartChoices) {
-                int64_t per1;
-                if (p1 > 8 || (p1 > 1 && t0 + t1 * p1 > 4 * kPairs)) break;
-                if (!part_length(s1, p1, per1)) continue;
-                const int64_t n1 = t1 * p1, c1 = per1 * slab + kTile, rest = std::max<int64_t>(0, n1 - (kPairs - full));
-                // pairs that have one tile more of the first, and those that have not
-                int64_t cost = each * c0 + (n1 + kPairs - 1) / kPairs * c1;
-                if (full > 0) cost = std::max(cost, (each + 1) * c0 + (rest + kPairs - 1) / kPairs * c1);
-                if (p0 > 1) cost += kJoin + (p0 + 1) * M * K * 4 / kJoinBytes;
-                if (p1 > 1) cost += kJoin + (p1 + 1) * N * K * 4 / kJoinBytes;
-                if (least == 0 || cost < least) {
-                    least = cost;
-                    cut0 = Cut{cols, int(p0), int(per0)};
-                    cut1 = Cut{cols, int(p1), int(per1)};
-                }
-            }
-        }
-    }
-    b.together = true;
-    set_cut(b.dx, M, K, cut0);
-    set_cut(b.dw, N, K, cut1);
-    return b;
+    const Shape sx = shape_of(M, K, N, false, true), sw = shape_of(N, K, M, true, true);
+    if (!sx.pair || !sw.pair || K == 0) return BackwardPlan{plan_of(sx, best_cut(sx)), plan_of(sw, best_cut(sw)), false};
+    Cut cx = {}, cw = {};
+    best_cuts(sx, sw, cx, cw);
+    return BackwardPlan{plan_of(sx, cx), plan_of(sw, cw), true};
 }
 
-acrl_status join(const Finish& f, const float* parts, int count, const Plan& plan, int64_t M, int64_t N, cudaStream_t s) {
-    const int64_t threads = (N + 3) / 4 * M;
-    if ((threads + 255) / 256 > kMaxGrid) return ACRL_ERR_INVALID_ARG;
-    return launch(join_kernel, (threads + 255) / 256, 256, 0, 0, s, f, parts, count, plan.ldparts, plan.part_size, int(M), int(N));
+// Plans of the sizes that the calling thread asked for last: a call asks twice, for its workspace and for its launches.
+template <typename P, typename F>
+P planned(int64_t M, int64_t N, int64_t K, F make) {
+    struct Known {
+        int64_t M, N, K;
+        P plan;
+    };
+    static thread_local Known known[4] = {{-1, -1, -1, P{}}, {-1, -1, -1, P{}}, {-1, -1, -1, P{}}, {-1, -1, -1, P{}}};
+    static thread_local int turn = 0;
+    for (const Known& k : known)
+        if (k.M == M && k.N == N && k.K == K) return k.plan;
+    turn = (turn + 1) % 4;
+    known[turn] = Known{M, N, K, make()};
+    return known[turn].plan;
+}
+
+Plan plan_linear(int64_t M, int64_t N, int64_t K) {
+    return planned<Plan>(M, N, K, [&] { return plan_of(M, N, K, false, false); });
 }
 
 // One product: x has the result's rows, w its columns.
@@ -241,23 +195,22 @@ struct Product {
 };
 
 // An fp32 result of more than one run.
-bool has_runs(const Product& p) { return p.f.out_f32 && p.plan.cut.per > kRun; }
+bool has_runs(const Product& p) { return p.f.out_f32 && p.plan.shape.slabs() > kRun; }
 
 template <bool PAIR, int NP>
 bool describe(ProductLaunch<NP, 1, LinearEpilogue<PAIR>>& l, int at, const Product& d) {
     const Matrix &p = PAIR ? d.x : d.w, &q = PAIR ? d.w : d.x;
-    const Plan& plan = d.plan;
-    l.pr[at] = problem_of(PAIR, p.rows, q.rows, d.K, 1, p.turned, q.turned, false, has_runs(d), plan.cut);
-    LinearEpilogue<PAIR>& e = l.epi[at];
-    e.f = d.f;
-    e.parts = plan.cut.parts > 1 ? d.parts : nullptr;
-    e.ldparts = plan.ldparts;
-    e.part_size = plan.part_size;
-    return operand_map(&l.p[at][0], p, d.K, kRows) && operand_map(&l.q[at][0], q, d.K, PAIR ? plan.cut.cols / 2 : plan.cut.cols);
+    const Cut& cut = d.plan.cut;
+    l.pr[at] = problem_of(d.plan.shape, cut, p.turned, q.turned, has_runs(d));
+    l.epi[at].f = d.f;
+    l.epi[at].parts = d.parts;
+    return operand_map(&l.p[at][0], p, d.K, kRows) && operand_map(&l.q[at][0], q, d.K, PAIR ? cut.cols / 2 : cut.cols);
 }
 
-acrl_status join_parts(const Product& d, cudaStream_t s) {
-    return d.plan.cut.parts == 1 ? ACRL_OK : join(d.f, d.parts, d.plan.cut.parts, d.plan, d.x.rows, d.w.rows, s);
+acrl_status join(const Problem& pr, const Product& d, cudaStream_t s) {
+    const int64_t ctas = d.plan.cut.tiles * ((pr.tile_rows() + kJoinRows - 1) / kJoinRows);
+    if (ctas > kMaxGrid) return ACRL_ERR_INVALID_ARG;
+    return launch(join_kernel, ctas, 256, 0, 0, s, d.f, static_cast<const float*>(d.parts), pr, int(d.x.rows), int(d.w.rows));
 }
 
 template <bool PAIR, int NP>
@@ -265,24 +218,27 @@ acrl_status run_products(const Product (&d)[NP], int32_t* flags, cudaStream_t s)
     ProductLaunch<NP, 1, LinearEpilogue<PAIR>> l = {};
     bool runs = false;
     for (int i = 0; i < NP; ++i) {
+        if (!units_fit(d[i].plan.cut)) return ACRL_ERR_INVALID_ARG;
         if (!describe<PAIR, NP>(l, i, d[i])) return ACRL_ERR_CUDA;
         runs = runs || has_runs(d[i]);
     }
     acrl_status st = runs ? launch_product<PAIR, true>(l, flags, s) : launch_product<PAIR, false>(l, flags, s);
-    for (int i = 0; i < NP && st == ACRL_OK; ++i) st = join_parts(d[i], s);
+    for (int i = 0; i < NP && st == ACRL_OK; ++i)
+        if (d[i].plan.cut.parts > 1) st = join(l.pr[i], d[i], s);
     return st;
-}
-
-bool product_fits(const Product& d) {
-    return units_fit(!d.plan.alone, d.plan.alone ? d.w.rows : d.x.rows, d.plan.alone ? d.x.rows : d.w.rows, 1, d.plan.cut);
 }
 
 // f(x w^T + ...): K > 0 columns, or an empty sum.
 acrl_status product(const Product& d, int32_t* flags, cudaStream_t s) {
-    if (d.K == 0) return join(d.f, nullptr, 0, d.plan, d.x.rows, d.w.rows, s);
-    if (!product_fits(d)) return ACRL_ERR_INVALID_ARG;
+    if (d.K == 0) {
+        const Cut& c = d.plan.cut;
+        if (!units_fit(c)) return ACRL_ERR_INVALID_ARG;
+        Problem pr = problem_of(d.plan.shape, c, d.x.turned, d.w.turned, false);
+        pr.parts = 0;
+        return join(pr, d, s);
+    }
     const Product one[1] = {d};
-    return d.plan.alone ? run_products<false, 1>(one, flags, s) : run_products<true, 1>(one, flags, s);
+    return d.plan.shape.pair ? run_products<true, 1>(one, flags, s) : run_products<false, 1>(one, flags, s);
 }
 
 // g = dy f'(u), rounded, and the columns' sums of the unrounded.  A lane has eight columns, a warp 256, and the eight warps of a
@@ -388,7 +344,8 @@ struct BackwardParts {
     BackwardPlan plan;
     int64_t ldg, rows, count, ldsums;   // of a part of the columns' sums, and how many there are
     int64_t sums, dx, dw, end;          // bytes
-    BackwardParts(int64_t M, int64_t N, int64_t K) : plan(plan_backward(M, N, K)) {
+    BackwardParts(int64_t M, int64_t N, int64_t K)
+        : plan(planned<BackwardPlan>(M, N, K, [&] { return plan_backward(M, N, K); })) {
         ldg = (N + 7) / 8 * 8;
         sums = M * ldg * 2;
         rows = slope_rows(M, N);
@@ -408,7 +365,7 @@ using namespace acrl;
 extern "C" int64_t acrl_linear_workspace_bytes(int64_t M, int64_t N, int64_t K) {
     if (M < 0 || N < 0 || K < 0) return -1;
     return M == 0 || N == 0 || K == 0 || M > kMostSize || N > kMostSize || K > kMostSize || linear_few_rows(M, N, K) ? 0
-                                                                                                              : plan_of(M, N, K, false, false).workspace;
+                                                                                                              : plan_linear(M, N, K).workspace;
 }
 
 extern "C" acrl_status acrl_linear(const acrl_bf16* x, int64_t M, int64_t K, int64_t ldx, const acrl_bf16* w, int64_t N, int64_t ldw,
@@ -431,7 +388,7 @@ extern "C" acrl_status acrl_linear(const acrl_bf16* x, int64_t M, int64_t K, int
     const Finish f{bias, residual, out, pre, ldr, ldp, ldo, int(act), bias_dtype == ACRL_F32, residual_dtype == ACRL_F32,
                    out_dtype == ACRL_F32};
     if (linear_few_rows(M, N, K)) return linear_few(x, M, K, ldx, w, N, ldw, f, reinterpret_cast<cudaStream_t>(stream));
-    const Plan plan = plan_of(M, N, K, false, false);
+    const Plan plan = plan_linear(M, N, K);
     return product({plan, Matrix{x, M, ldx, false, 1, M * ldx}, Matrix{w, N, ldw, false, 1, N * ldw}, K, f, static_cast<float*>(workspace)},
                    dev_flags, reinterpret_cast<cudaStream_t>(stream));
 }
@@ -498,10 +455,7 @@ extern "C" acrl_status acrl_linear_backward(const acrl_bf16* dy, int64_t M, int6
                               reinterpret_cast<float*>(base + parts.dx)},
                              {parts.plan.dw, Matrix{g, N, ldg, true, 1, M * ldg}, Matrix{x, K, ldx, true, 1, M * ldx}, has_g ? M : 0, fw,
                               reinterpret_cast<float*>(base + parts.dw)}};
-    if (has_dx && has_dw && has_g && parts.plan.together) {
-        if (!product_fits(both[0]) || !product_fits(both[1])) return ACRL_ERR_INVALID_ARG;
-        return run_products<true, 2>(both, dev_flags, s);
-    }
+    if (has_dx && has_dw && has_g && parts.plan.together) return run_products<true, 2>(both, dev_flags, s);
     if (has_dx) st = product(both[0], dev_flags, s);
     if (has_dw && st == ACRL_OK) st = product(both[1], dev_flags, s);
     return st;

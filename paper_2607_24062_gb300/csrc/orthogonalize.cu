@@ -21,7 +21,6 @@ namespace acrl {
 namespace {
 
 constexpr int kMostSteps = 64;
-constexpr int kPairs = 76;
 constexpr int kSumCtas = 608;      // four of an SM's: CTAs that add up squares
 
 struct Update {
@@ -54,38 +53,59 @@ struct Squares {
     __device__ __forceinline__ double total() const { return double(low) * 0x1p-160 + double(mid) + double(high) * 0x1p160; }
 };
 
-// Partial sums of a matrix's squares, `ctas` of them: rows in turn, 16 bytes a thread.  HBM bounds it.
+// A matrix's rows are gone through in pieces of kPiece columns, a warp a piece; `ctas` CTAs a matrix take them in turn.
+constexpr int kPiece = 1024, kVec = 8, kTurns = kPiece / (32 * kVec);
+
+struct Pieces {
+    int per_row, all, at, step;
+    __device__ Pieces(const Update& u, int cta, int ctas) {
+        per_row = (u.n + kPiece - 1) / kPiece;
+        all = u.m * per_row;
+        at = cta * 8 + int(threadIdx.x >> 5);
+        step = ctas * 8;
+    }
+};
+
+// Eight of a row's numbers from column c on, zeros beyond its end.
+__device__ __forceinline__ void load8(const Update& u, int64_t row, int c, float (&v)[8]) {
+    if (c + 8 > u.n) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = c + j < u.n ? load_float(u.g, u.f32, row + c + j) : 0.f;
+    } else if (u.f32) {
+        const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(u.g) + row + c);
+        const float4 a = p[0], b = p[1];
+        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    } else {
+        const uint4 x = *reinterpret_cast<const uint4*>(static_cast<const acrl_bf16*>(u.g) + row + c);
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[2 * j] = bf16_lo(w[j]);
+            v[2 * j + 1] = bf16_hi(w[j]);
+        }
+    }
+}
+
+// Partial sums of a matrix's squares, `ctas` of them.  HBM bounds it.
 __global__ void __launch_bounds__(256) squares_kernel(Update u, int ctas, double* sums) {
     __shared__ double part[8];
     grid_begin();
-    const int b = int(blockIdx.x) / ctas, c = int(blockIdx.x) - b * ctas;
-    const int V = u.f32 ? 4 : 8, vectors = (u.n + V - 1) / V;
+    const int b = int(blockIdx.x) / ctas, lane = threadIdx.x & 31;
     Squares s;
-    const int64_t all = int64_t(u.m) * vectors;
-    for (int64_t i = int64_t(c) * 256 + threadIdx.x; i < all; i += int64_t(ctas) * 256) {
-        const int64_t r = i / vectors;
-        const int at = int(i - r * vectors) * V;
-        const int64_t row = b * u.stride + r * u.ld + at;
-        if (at + V > u.n) {
-            for (int j = at; j < u.n; ++j) s.add(load_float(u.g, u.f32, row + j - at));
-        } else if (u.f32) {
-            const float4 x = *reinterpret_cast<const float4*>(static_cast<const float*>(u.g) + row);
-            s.add(x.x);
-            s.add(x.y);
-            s.add(x.z);
-            s.add(x.w);
-        } else {
-            const uint4 x = *reinterpret_cast<const uint4*>(static_cast<const acrl_bf16*>(u.g) + row);
-            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    Pieces p(u, int(blockIdx.x) - b * ctas, ctas);
+    for (; p.at < p.all; p.at += p.step) {
+        const int r = p.at / p.per_row, c = (p.at - r * p.per_row) * kPiece + lane * kVec;
+        const int64_t row = b * u.stride + r * u.ld;
+        float v[kTurns][8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                s.add(bf16_lo(w[j]));
-                s.add(bf16_hi(w[j]));
-            }
-        }
+        for (int i = 0; i < kTurns; ++i) load8(u, row, min(c + i * 32 * kVec, u.n), v[i]);
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s.add(v[i][j]);
     }
     const double sum = warp_sum(s.total());
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = sum;
+    if (lane == 0) part[threadIdx.x >> 5] = sum;
     __syncthreads();
     if (threadIdx.x == 0) {
         double t = 0.0;
@@ -100,25 +120,34 @@ __device__ __forceinline__ void halves(float x, acrl_bf16& hi, acrl_bf16& lo) {
     lo = to_bf16(x - bf16_to_float(hi));
 }
 
-// X_0 = G / (|G| + eps) in two bf16 matrices, 32 x 32 blocks, turned where G is tall.  The factor is a power of two times a
-// number in [1, 2): an update of any size is brought near 1 before it is divided.
+// Eight of them, from a column that is a multiple of eight.
+__device__ __forceinline__ void halves8(const float (&v)[8], acrl_bf16* hi, acrl_bf16* lo) {
+    uint32_t h[4], l[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        h[j] = pack_bf16x2(v[2 * j], v[2 * j + 1]);
+        l[j] = pack_bf16x2(v[2 * j] - bf16_lo(h[j]), v[2 * j + 1] - bf16_hi(h[j]));
+    }
+    *reinterpret_cast<uint4*>(hi) = make_uint4(h[0], h[1], h[2], h[3]);
+    *reinterpret_cast<uint4*>(lo) = make_uint4(l[0], l[1], l[2], l[3]);
+}
+
+// X_0 = G / (|G| + eps) in two bf16 matrices, turned where G is tall, in blocks of 64 x 64 through shared memory.  The factor is
+// a power of two times a number in [1, 2): an update of any size is brought near 1 before it is divided.  `ctas` CTAs a matrix
+// (each adds up the squares for itself; a CTA for each block of 32 x 32 took 95 us for 24 x 1,024 x 1,024, these 24).
 __global__ void __launch_bounds__(256) first_kernel(Update u, int ctas, const double* sums, float eps, acrl_bf16* hi, acrl_bf16* lo,
                                                     int64_t ldx, int64_t size, int32_t* flags) {
-    __shared__ float block[32][33];
+    __shared__ float block[64][65];
     __shared__ float by[3];
     grid_begin();
-    const int64_t rows = (u.m + 31) / 32, cols = (u.n + 31) / 32, blocks = rows * cols;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int b = int(int64_t(blockIdx.x) / blocks);
-    const int64_t k = int64_t(blockIdx.x) - b * blocks;
-    const int r0 = int(k / cols) * 32, c0 = int(k % cols) * 32;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, b = int(blockIdx.x) / ctas, cta = int(blockIdx.x) - b * ctas;
     if (warp == 0) {
         double sum = 0.0;
         for (int i = lane; i < ctas; i += 32) sum += sums[int64_t(b) * ctas + i];
         sum = warp_sum(sum);
         if (lane == 0) {
             const bool bad = !(sum <= 1.7e308);   // an infinity or a NaN: no finite matrix comes near
-            if (bad && k == 0) raise_flag(flags, ACRL_FLAG_NONFINITE);
+            if (bad && cta == 0) raise_flag(flags, ACRL_FLAG_NONFINITE);
             int e = 0;
             const double f = frexp(sqrt(sum) + double(eps), &e);   // f 2^e
             by[0] = exp2f(float(-e / 2));
@@ -128,24 +157,46 @@ __global__ void __launch_bounds__(256) first_kernel(Update u, int ctas, const do
     }
     __syncthreads();
     const float one = by[0], two = by[1], rest = by[2];
-    const bool tall = u.m > u.n;
     acrl_bf16 *h = hi + b * size, *l = lo + b * size;
+    if (u.m <= u.n) {
+        Pieces p(u, cta, ctas);
+        for (; p.at < p.all; p.at += p.step) {
+            const int r = p.at / p.per_row, c = (p.at - r * p.per_row) * kPiece + lane * kVec;
+            float v[kTurns][8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = r0 + warp + 8 * i, c = c0 + lane;
-        float x = 0.f;
-        if (r < u.m && c < u.n) x = load_float(u.g, u.f32, b * u.stride + r * u.ld + c) * one * two * rest;
-        if (tall)
-            block[warp + 8 * i][lane] = x;
-        else if (r < u.m && c < u.n)
-            halves(x, h[r * ldx + c], l[r * ldx + c]);
+            for (int i = 0; i < kTurns; ++i) load8(u, b * u.stride + r * u.ld, min(c + i * 32 * kVec, u.n), v[i]);
+#pragma unroll
+            for (int i = 0; i < kTurns; ++i) {
+                const int at = c + i * 32 * kVec;
+                if (at >= u.n) break;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[i][j] = v[i][j] * one * two * rest;
+                halves8(v[i], h + r * ldx + at, l + r * ldx + at);   // the last ones' zeros are within ldx
+            }
+        }
+        return;
     }
-    if (!tall) return;
-    __syncthreads();
+    const int cols = (u.n + 63) / 64, blocks = (u.m + 63) / 64 * cols, k = int(threadIdx.x & 7) * 8, row = int(threadIdx.x >> 3);
+    for (int at = cta; at < blocks; at += ctas) {
+        const int r0 = at / cols * 64, c0 = at % cols * 64;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = c0 + warp + 8 * i, c = r0 + lane;   // of X
-        if (r < u.n && c < u.m) halves(block[lane][warp + 8 * i], h[r * ldx + c], l[r * ldx + c]);
+        for (int i = 0; i < 64; i += 32) {
+            float v[8] = {};
+            const int r = r0 + row + i;
+            if (r < u.m && c0 + k < u.n) load8(u, b * u.stride + r * u.ld, c0 + k, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) block[row + i][k + j] = v[j] * one * two * rest;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 64; i += 32) {
+            const int r = c0 + row + i, c = r0 + k;   // of X
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = block[k + j][row + i];
+            if (r < u.n && c < u.m) halves8(v, h + r * ldx + c, l + r * ldx + c);
+        }
+        __syncthreads();
     }
 }
 
@@ -195,16 +246,17 @@ __device__ __forceinline__ void polynomial(const Finish& f, int64_t at, int i, i
 
 struct StepEpilogue {
     Finish f;
-    float* parts;                  // where the sum is split: [matrix][part][row][ldparts]
-    int64_t ldparts, part_size;
+    float* parts;                  // of the tiles
 
     __device__ __forceinline__ void chunk(const Problem& pr, const Unit& t, const uint32_t (&r)[32], int row0, int col0, int rows,
                                           int cols, const WarpOut& out) const {
         float v[32];
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
-        if (parts) {
-            out.store(parts + (int64_t(t.z) * pr.parts + t.part) * part_size, ldparts, rows, cols, v, row0, col0);
+        if (pr.parts > 1) {
+            const int high = 2 * kRows, wide = pr.cols;
+            out.store(parts + (int64_t(t.all) * pr.parts + t.part) * high * wide, wide, rows > 0 ? high : 0, wide, v, row0 - t.tp * high,
+                      col0 - t.tq * wide);
             return;
         }
         if (f.kind == kResult) {
@@ -229,27 +281,25 @@ struct StepEpilogue {
     }
 };
 
-// The parts of a split sum in their order, and what is made of them, a block of 32 x 32 a CTA; of a symmetric matrix those
-// that were computed, and their mirror images.
-__global__ void __launch_bounds__(256) join_kernel(Finish f, const float* parts, int count, int64_t ldparts, int64_t part_size, int lower,
-                                                   int rows, int cols) {
+// The parts of the tiles in their order, and what is made of them, a block of 32 x 32 a CTA; of a symmetric matrix the
+// mirror image as well.
+__global__ void __launch_bounds__(256) join_kernel(Finish f, const float* parts, Problem pr) {
     __shared__ float block[32][33];
     grid_begin();
-    const int64_t across = (cols + 31) / 32, blocks = (rows + 31) / 32 * across, z = int64_t(blockIdx.x) / blocks;
-    const int64_t k = int64_t(blockIdx.x) - z * blocks;
-    const int r0 = int(k / across) * 32, c0 = int(k % across) * 32, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int tile = r0 / (2 * kRows) * 2 * kRows;   // the first row, and column, of the diagonal's tile
-    if (lower && c0 >= tile + 2 * kRows) return;
-    const bool turn = f.kind == kResult && f.tall, twice = lower && c0 < tile;
+    const int across = pr.cols / 32, blocks = 2 * kRows / 32 * across, tile = int(blockIdx.x) / blocks, k = int(blockIdx.x) - tile * blocks;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rows = pr.rows, cols = pr.cols_all;
+    const Unit t = tile_at(pr, tile);
+    const int64_t z = t.z;
+    const int rt = k / across * 32, ct = k % across * 32, r0 = t.tp * 2 * kRows + rt, c0 = t.tq * pr.cols + ct;   // in the tile, in all
+    if (r0 >= rows || c0 >= cols) return;
+    const bool turn = f.kind == kResult && f.tall, twice = pr.lower && c0 < t.tp * 2 * kRows;
     float v[4] = {};
     const int c = c0 + lane;
-    for (int j = 0; j < count; ++j) {
-        const float* p = parts + (z * count + j) * part_size + c;
+    const int64_t size = int64_t(2 * kRows) * pr.cols;
+    const float* p = parts + tile * pr.parts * size + (rt + warp) * pr.cols + ct + lane;
+    for (int j = 0; j < pr.parts; ++j) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = r0 + warp + 8 * i;
-            if (r < rows && c < cols) v[i] += p[r * ldparts];
-        }
+        for (int i = 0; i < 4; ++i) v[i] += p[j * size + 8 * i * pr.cols];
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -285,35 +335,15 @@ __global__ void __launch_bounds__(256) join_kernel(Finish f, const float* parts,
 // ---------------------------------------------------------------------------------------------------------------
 
 struct Plan {
+    Shape shape;
     Cut cut;
-    int64_t cost, workspace, ldparts, part_size;
+    int64_t workspace;
 };
 
-// The cut of a product rows x cols over K with the least estimated time, as for a layer's.
-Plan plan_of(int64_t batch, int64_t rows, int64_t cols_all, int64_t K, bool lower, bool q_turned) {
-    constexpr int64_t kTile = 4000, kJoin = 6000, kJoinBytes = 3000;
-    const int64_t slabs = (K + kSlab - 1) / kSlab, p_tiles = (rows + 2 * kRows - 1) / (2 * kRows);
-    Plan best = {};
-    best.ldparts = (cols_all + 7) / 8 * 8;
-    best.part_size = rows * best.ldparts;
-    for (int cols = 256; cols >= (q_turned ? 128 : 64); cols /= 2) {
-        const int64_t q_tiles = (cols_all + cols - 1) / cols, r = 2 * kRows / cols;
-        const int64_t tiles = batch * (lower ? r * (p_tiles - 1) * p_tiles / 2 + q_tiles : p_tiles * q_tiles);
-        const int64_t slab = std::max(6 * cols, 4 * (kRows + cols / 2));
-        for (int64_t parts = 1; parts <= 16 && parts <= slabs; ++parts) {
-            const int64_t per = (slabs + parts - 1) / parts;
-            if ((slabs + per - 1) / per != parts) continue;
-            const int64_t rounds = (tiles * parts + kPairs - 1) / kPairs;
-            const int64_t cost = rounds * (per * slab + kTile) +
-                                 (parts > 1 ? kJoin + (parts + 1) * batch * best.part_size * 4 / kJoinBytes : 0);
-            if (best.cost == 0 || cost < best.cost) {
-                best.cost = cost;
-                best.cut = Cut{cols, int(parts), int(per)};
-            }
-        }
-    }
-    best.workspace = best.cut.parts > 1 ? best.cut.parts * batch * best.part_size * 4 : 0;
-    return best;
+Plan plan_of(int64_t batch, int64_t rows, int64_t cols, int64_t K, bool lower, bool q_turned) {
+    const Shape s{true, rows, cols, K, batch, lower, 3, 256, q_turned ? 128 : 64, 0};
+    const Cut cut = best_cut(s);
+    return Plan{s, cut, parts_bytes(s, cut)};
 }
 
 // The workspace, in bytes: sums of squares; X twice, A and Q, each in two matrices; the parts of a split sum.
@@ -350,25 +380,22 @@ struct Halves {
     int64_t ld, size;   // from one matrix to the next
 };
 
-// One product of the steps: rows x cols over K.
-acrl_status step_product(const Plan& plan, int64_t batch, int64_t rows, int64_t cols, int64_t K, const Halves& p, const Halves& q,
-                         bool q_turned, bool lower, const Finish& f, float* parts, int32_t* flags, cudaStream_t s) {
+// One product of the steps.
+acrl_status step_product(const Plan& plan, const Halves& p, const Halves& q, bool q_turned, const Finish& f, float* parts, int32_t* flags,
+                         cudaStream_t s) {
+    const Shape& sh = plan.shape;
     ProductLaunch<1, 3, StepEpilogue> l = {};
-    l.pr[0] = problem_of(true, rows, cols, K, batch, false, q_turned, lower, false, plan.cut);
-    StepEpilogue& e = l.epi[0];
-    e.f = f;
-    e.parts = plan.cut.parts > 1 ? parts : nullptr;
-    e.ldparts = plan.ldparts;
-    e.part_size = plan.part_size;
+    l.pr[0] = problem_of(sh, plan.cut, false, q_turned, false);
+    l.epi[0].f = f;
+    l.epi[0].parts = parts;
     for (int i = 0; i < 2; ++i) {
-        if (!operand_map(&l.p[0][i], Matrix{i ? p.lo : p.hi, rows, p.ld, false, batch, p.size}, K, kRows) ||
-            !operand_map(&l.q[0][i], Matrix{i ? q.lo : q.hi, cols, q.ld, q_turned, batch, q.size}, K, plan.cut.cols / 2))
+        if (!operand_map(&l.p[0][i], Matrix{i ? p.lo : p.hi, sh.rows, p.ld, false, sh.batch, p.size}, sh.K, kRows) ||
+            !operand_map(&l.q[0][i], Matrix{i ? q.lo : q.hi, sh.cols_all, q.ld, q_turned, sh.batch, q.size}, sh.K, plan.cut.cols / 2))
             return ACRL_ERR_CUDA;
     }
     const acrl_status st = launch_product<true, false>(l, flags, s);
-    if (st != ACRL_OK || !e.parts) return st;
-    return launch(join_kernel, batch * ((rows + 31) / 32) * ((cols + 31) / 32), 256, 0, 0, s, f, static_cast<const float*>(parts),
-                  plan.cut.parts, plan.ldparts, plan.part_size, int(lower), int(rows), int(cols));
+    if (st != ACRL_OK || plan.cut.parts == 1) return st;
+    return launch(join_kernel, plan.cut.tiles * (2 * kRows / 32) * (plan.cut.cols / 32), 256, 0, 0, s, f, static_cast<const float*>(parts), l.pr[0]);
 }
 
 }  // namespace
@@ -381,9 +408,9 @@ bool sizes_ok(int64_t batch, int64_t m, int64_t n) {
     constexpr int64_t kMost = kMaxGrid - 512;
     return batch >= 0 && m >= 0 && n >= 0 && batch <= kMost && m <= kMost && n <= kMost;
 }
-// One launch's blocks, and the parts' too, stay within a grid.
+// Tiles, pieces and blocks of a launch are counted in 32 bits.
 bool blocks_ok(int64_t batch, int64_t m, int64_t n) {
-    return double(batch) * double((m + 31) / 32) * double((n + 31) / 32) < double(kMaxGrid);
+    return double(batch) * double((m + 31) / 32) * double((n + 31) / 32) < double(1 << 30);
 }
 }  // namespace
 
@@ -422,7 +449,7 @@ extern "C" acrl_status acrl_orthogonalize(const void* g, acrl_dtype g_dtype, int
     const Update u{g, g_dtype == ACRL_F32, ldg, g_stride, int(m), int(n)};
     acrl_status st = launch(squares_kernel, batch * l.ctas, 256, 0, 0, s, u, int(l.ctas), sums);
     if (st != ACRL_OK) return st;
-    st = launch(first_kernel, batch * ((m + 31) / 32) * ((n + 31) / 32), 256, 0, 0, s, u, int(l.ctas), static_cast<const double*>(sums), eps, x[0].hi,
+    st = launch(first_kernel, batch * l.ctas, 256, 0, 0, s, u, int(l.ctas), static_cast<const double*>(sums), eps, x[0].hi,
                 x[0].lo, l.ldx, x[0].size, dev_flags);
     for (int i = 0; i < steps && st == ACRL_OK; ++i) {
         const Halves &from = x[i & 1], &into = x[1 - (i & 1)];
@@ -432,7 +459,7 @@ extern "C" acrl_status acrl_orthogonalize(const void* g, acrl_dtype g_dtype, int
         f.lo = gram.lo;
         f.ld = gram.ld;
         f.size = gram.size;
-        st = step_product(l.plan_gram, batch, l.m, l.m, l.n, from, from, false, true, f, parts, dev_flags, s);
+        st = step_product(l.plan_gram, from, from, false, f, parts, dev_flags, s);
         if (st != ACRL_OK) break;
         f.kind = kPolynomial;
         f.a = coeffs[3 * i];
@@ -442,7 +469,7 @@ extern "C" acrl_status acrl_orthogonalize(const void* g, acrl_dtype g_dtype, int
         f.lo_in = gram.lo;
         f.hi = q.hi;
         f.lo = q.lo;
-        st = step_product(l.plan_q, batch, l.m, l.m, l.m, gram, gram, false, true, f, parts, dev_flags, s);
+        st = step_product(l.plan_q, gram, gram, false, f, parts, dev_flags, s);
         if (st != ACRL_OK) break;
         f.kind = i + 1 < steps ? kIterate : kResult;
         f.hi = into.hi;
@@ -454,7 +481,7 @@ extern "C" acrl_status acrl_orthogonalize(const void* g, acrl_dtype g_dtype, int
         f.ldo = ldo;
         f.out_stride = out_stride;
         f.tall = m > n;
-        st = step_product(l.plan_x, batch, l.m, l.n, l.m, q, from, true, false, f, parts, dev_flags, s);
+        st = step_product(l.plan_x, q, from, true, f, parts, dev_flags, s);
     }
     return st;
 }
