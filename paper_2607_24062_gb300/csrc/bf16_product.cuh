@@ -52,10 +52,6 @@ constexpr int kAccCols = 256;        // of each accumulator
 constexpr int kWarpStaging = 4096;   // bytes of an epilogue warp: a block of 32 x 32 in fp32
 constexpr int kProductSmem = 227 * 1024;
 constexpr int kRun = 8;              // slabs of a run
-// Registers of a thread in the kernel with runs: 384 threads at launch with kLaunchRegs each, of which the first warpgroup
-// gives to the other two, that hold up to 128 sums.
-constexpr int kLaunchRegs = 168, kFewRegs = 56, kManyRegs = 224;
-static_assert(kFewRegs + 2 * kManyRegs <= 3 * kLaunchRegs && kProductThreads == 384, "what a launch has");
 
 struct ProductBarriers {
     uint64_t full[kMaxStages];    // the copies of a stage have landed (pair: the even CTA's counts both CTAs')
@@ -169,48 +165,65 @@ __device__ __forceinline__ uint64_t tile_desc(uint32_t addr, int turned) {
     return smem_desc(addr) | (turned ? uint64_t(kSlab * kRowBytes >> 4) << 16 : 0);
 }
 
-template <bool PAIR, int NP, int TERMS, class L>
-__device__ void produce_slabs(const L& l, uint8_t* ring, ProductBarriers* bars, uint32_t rank) {
-    constexpr int kMats = TERMS == 3 ? 2 : 1;
-    volatile int32_t* abort = &bars->abort;
+// What the roles have in common: the ring of stages, its barriers, and how they give up.
+struct Ring {
+    uint8_t* at;
+    ProductBarriers* bars;
+    int stages, stage_bytes;
+    uint32_t rank;
+    int32_t* flags;
+};
+
+// The producer warp's loops, and the MMA warp's, run in the whole warp, and one lane is elected for each batch of copies or
+// MMAs.  Each role goes through the units that it is given; false: it has given up.
+template <bool PAIR, int TERMS>
+struct Producer {
+    static constexpr int kMats = TERMS == 3 ? 2 : 1;
+    const Ring& ring;
     int stage = 0;
     uint32_t phase = 0;
     long issued = 0;
-    for (Units<PAIR, NP, L> w(l); w.more(); w.next()) {
-        const Problem& pr = w.problem();
-        const Unit t = w.unit();
-        const CUtensorMap *tmP = l.p[NP == 2 ? w.which : 0], *tmQ = l.q[NP == 2 ? w.which : 0];
+
+    // The copies that were started land before the CTA can exit: the even CTA's barriers count both CTAs', the odd one gives its
+    // own time to land.
+    __device__ void land() {
+        ProductBarriers* bars = ring.bars;
+        if (!PAIR || ring.rank == 0) {
+            for (long j = issued - 1; j >= 0 && j >= issued - ring.stages; --j)
+                wait_phase(&bars->full[j % ring.stages], uint32_t((j / ring.stages) & 1), nullptr);
+        } else {
+            const uint64_t t0 = global_ns();
+            while (global_ns() - t0 < 100000ull) {
+            }
+        }
+    }
+
+    // p and q: the maps of the operands' matrices.
+    __device__ __forceinline__ bool unit(const Problem& pr, const Unit& t, const CUtensorMap* p, const CUtensorMap* q) {
+        ProductBarriers* bars = ring.bars;
+        volatile int32_t* abort = &bars->abort;
         const int q_rows = PAIR ? pr.cols / 2 : pr.cols, q_bytes = q_rows * kRowBytes;
         const int bytes = kMats * (kRows * kRowBytes + q_bytes);
-        const int p0 = (PAIR ? 2 * t.tp + int(rank) : t.tp) * kRows;
-        const int q0 = t.tq * pr.cols + (PAIR ? int(rank) * q_rows : 0);
+        const int p0 = (PAIR ? 2 * t.tp + int(ring.rank) : t.tp) * kRows;
+        const int q0 = t.tq * pr.cols + (PAIR ? int(ring.rank) * q_rows : 0);
         for (int kb = t.lo; kb < t.hi; ++kb) {
             if (!warp_wait(&bars->empty[stage], phase ^ 1u, abort)) {
-                give_up(abort, l.flags);
-                // the copies that were started land before the CTA can exit: the even CTA's barriers count both CTAs', the
-                // odd one gives its own time to land
-                if (!PAIR || rank == 0) {
-                    for (long j = issued - 1; j >= 0 && j >= issued - l.stages; --j)
-                        wait_phase(&bars->full[j % l.stages], uint32_t((j / l.stages) & 1), nullptr);
-                } else {
-                    const uint64_t t0 = global_ns();
-                    while (global_ns() - t0 < 100000ull) {
-                    }
-                }
-                return;
+                give_up(abort, ring.flags);
+                land();
+                return false;
             }
-            uint8_t* s = ring + stage * l.stage_bytes;
+            uint8_t* s = ring.at + stage * ring.stage_bytes;
             const uint32_t bar = PAIR ? peer_addr(&bars->full[stage], 0) : smem_u32(&bars->full[stage]);
             if (elect_one()) {
-                if (!PAIR || rank == 0) mbar_expect_tx(&bars->full[stage], uint32_t((PAIR ? 2 : 1) * bytes));
+                if (!PAIR || ring.rank == 0) mbar_expect_tx(&bars->full[stage], uint32_t((PAIR ? 2 : 1) * bytes));
 #pragma unroll
                 for (int i = 0; i < kMats; ++i) {
                     uint8_t* to = s + i * kRows * kRowBytes;
                     if (pr.p_turned) {
-                        tma_load_3d<PAIR>(to, &tmP[i], bar, p0, kb * kSlab, t.z);
-                        tma_load_3d<PAIR>(to + kSlab * kRowBytes, &tmP[i], bar, p0 + kSlab, kb * kSlab, t.z);
+                        tma_load_3d<PAIR>(to, &p[i], bar, p0, kb * kSlab, t.z);
+                        tma_load_3d<PAIR>(to + kSlab * kRowBytes, &p[i], bar, p0 + kSlab, kb * kSlab, t.z);
                     } else {
-                        tma_load_3d<PAIR>(to, &tmP[i], bar, kb * kSlab, p0, t.z);
+                        tma_load_3d<PAIR>(to, &p[i], bar, kb * kSlab, p0, t.z);
                     }
                 }
 #pragma unroll
@@ -218,20 +231,21 @@ __device__ void produce_slabs(const L& l, uint8_t* ring, ProductBarriers* bars, 
                     uint8_t* to = s + kMats * kRows * kRowBytes + i * q_bytes;
                     if (pr.q_turned) {
                         for (int j = 0; j < q_rows; j += kSlab)
-                            tma_load_3d<PAIR>(to + j * kRowBytes, &tmQ[i], bar, q0 + j, kb * kSlab, t.z);
+                            tma_load_3d<PAIR>(to + j * kRowBytes, &q[i], bar, q0 + j, kb * kSlab, t.z);
                     } else {
-                        tma_load_3d<PAIR>(to, &tmQ[i], bar, kb * kSlab, q0, t.z);
+                        tma_load_3d<PAIR>(to, &q[i], bar, kb * kSlab, q0, t.z);
                     }
                 }
             }
             ++issued;
-            if (++stage == l.stages) {
+            if (++stage == ring.stages) {
                 stage = 0;
                 phase ^= 1u;
             }
         }
+        return true;
     }
-}
+};
 
 template <bool PAIR>
 __device__ __forceinline__ void mma_bf16(uint32_t d, uint64_t pdesc, uint64_t qdesc, uint32_t idesc, uint32_t accumulate) {
@@ -245,31 +259,35 @@ __device__ __forceinline__ void mma_bf16(uint32_t d, uint64_t pdesc, uint64_t qd
             "l"(pdesc), "l"(qdesc), "r"(idesc), "r"(accumulate));
 }
 
-template <bool PAIR, int NP, int TERMS, class L>
-__device__ void issue_products(const L& l, uint8_t* ring, ProductBarriers* bars, uint32_t tmem) {
-    constexpr int kMats = TERMS == 3 ? 2 : 1;
-    volatile int32_t* abort = &bars->abort;
-    const uint32_t units = uint32_t(l.stage_bytes) >> 4;   // of a stage, in descriptors
-    const uint32_t base = smem_u32(ring);
+template <bool PAIR, int TERMS>
+struct Multiplier {
+    static constexpr int kMats = TERMS == 3 ? 2 : 1;
+    const Ring& ring;
+    uint32_t tmem;
     int stage = 0, acc = 0;
     uint32_t phase = 0, aphase = 0;
-    bool ok = true;
-    for (Units<PAIR, NP, L> w(l); w.more() && ok; w.next()) {
-        const Problem& pr = w.problem();
-        const Unit t = w.unit();
+
+    __device__ __forceinline__ bool unit(const Problem& pr, const Unit& t) {
+        ProductBarriers* bars = ring.bars;
+        volatile int32_t* abort = &bars->abort;
+        const uint32_t base = smem_u32(ring.at), units = uint32_t(ring.stage_bytes) >> 4;   // of a stage, in descriptors
         const uint64_t pdesc0 = tile_desc(base, pr.p_turned), qdesc0 = tile_desc(base + kMats * kRows * kRowBytes, pr.q_turned);
         // from one K = 16 to the next: 32 bytes of a row, or sixteen rows
         const uint32_t pstep = pr.p_turned ? 16 * kRowBytes >> 4 : 2, qstep = pr.q_turned ? 16 * kRowBytes >> 4 : 2;
         const uint32_t plow = kRows * kRowBytes >> 4, qlow = uint32_t((PAIR ? pr.cols / 2 : pr.cols) * kRowBytes) >> 4;
-        for (int run = t.lo; run < t.hi && ok; run += pr.run) {
-            ok = warp_wait(&bars->tempty[acc], aphase ^ 1u, abort);
-            if (!ok) break;
+        for (int run = t.lo; run < t.hi; run += pr.run) {
+            if (!warp_wait(&bars->tempty[acc], aphase ^ 1u, abort)) {
+                give_up(abort, ring.flags);
+                return false;
+            }
             tc_fence_after();
             const uint32_t d = tmem + uint32_t(acc * kAccCols);
             const int end = min(t.hi, run + pr.run);
             for (int kb = run; kb < end; ++kb) {
-                ok = warp_wait(&bars->full[stage], phase, abort);
-                if (!ok) break;
+                if (!warp_wait(&bars->full[stage], phase, abort)) {
+                    give_up(abort, ring.flags);
+                    return false;
+                }
                 tc_fence_after();
                 const uint64_t pd = pdesc0 + stage * units, qd = qdesc0 + stage * units;
                 const uint32_t more = kb > run;
@@ -283,32 +301,34 @@ __device__ void issue_products(const L& l, uint8_t* ring, ProductBarriers* bars,
                     }
                     commit<PAIR>(&bars->empty[stage]);
                 }
-                if (++stage == l.stages) {
+                if (++stage == ring.stages) {
                     stage = 0;
                     phase ^= 1u;
                 }
             }
-            if (!ok) break;
             if (elect_one()) commit<PAIR>(&bars->tfull[acc]);
             if (++acc == 2) {
                 acc = 0;
                 aphase ^= 1u;
             }
         }
-        if (!ok) give_up(abort, l.flags);
+        return true;
     }
-    // every MMA has finished before the CTA moves on
-    if (elect_one()) {
-        if (PAIR)
-            asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
-                             peer_addr(&bars->mma_done, 0))
-                         : "memory");
-        else
-            commit<false>(&bars->mma_done);
+
+    // Every MMA has finished before the CTA moves on.
+    __device__ void finish() {
+        if (elect_one()) {
+            if (PAIR)
+                asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
+                                 peer_addr(&ring.bars->mma_done, 0))
+                             : "memory");
+            else
+                commit<false>(&ring.bars->mma_done);
+        }
+        wait_phase(&ring.bars->mma_done, 0, nullptr);
+        __syncwarp();
     }
-    wait_phase(&bars->mma_done, 0, nullptr);
-    __syncwarp();
-}
+};
 
 // An epilogue warp's way out: through its block of shared memory, so that neighbouring lanes store neighbouring pieces of 16
 // bytes, four or eight to a row.  (TMA stores of the blocks took longer: a copy keeps its block for about 1,000 cycles, and the
@@ -389,121 +409,146 @@ struct WarpOut {
     }
 };
 
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&v)[32]) {
+// Sixteen columns of a warp's 32 lanes, added to v.
+__device__ __forceinline__ void tmem_add16(uint32_t taddr, float* v) {
+    uint32_t r[16];
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
-        "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+#pragma unroll
+    for (int j = 0; j < 16; ++j) v[j] += __uint_as_float(r[j]);
+}
+
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const float* v) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
         "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]), "f"(v[10]),
-        "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]), "f"(v[16]), "f"(v[17]), "f"(v[18]), "f"(v[19]), "f"(v[20]),
-        "f"(v[21]), "f"(v[22]), "f"(v[23]), "f"(v[24]), "f"(v[25]), "f"(v[26]), "f"(v[27]), "f"(v[28]), "f"(v[29]), "f"(v[30]),
-        "f"(v[31])
+        "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15])
         : "memory");
 }
 
-template <bool PAIR, bool LONG, int NP, class L>
-__device__ void drain(const L& l, ProductBarriers* bars, uint32_t tmem, uint8_t* staging, uint32_t rank) {
-    volatile int32_t* abort = &bars->abort;
-    const int warp = int(threadIdx.x >> 5) - 4, lane = threadIdx.x & 31, quarter = (threadIdx.x >> 5) & 3;
-    const WarpOut out{staging + warp * kWarpStaging, lane};
-    const uint32_t lanes = uint32_t(quarter * 32) << 16;
-    const int first = 32 * (warp >> 2);   // the two warps of a quarter take 32 columns in turn
+template <bool PAIR, bool LONG>
+struct Drain {
+    const Ring& ring;
+    uint32_t tmem;
+    WarpOut out;
+    int lane, quarter, first;   // the two warps of a quarter take 32 columns in turn
     int acc = 0;
     uint32_t phase = 0;
+    // The first unit's first columns are gone through twice, before its products are there with a matrix of no rows and no
+    // columns, which loads and stores nothing: what follows a sum is then in the instruction cache when it is waited for (from
+    // there its 1,100 cycles were mostly misses; a layer of 256 x 256 x 256 3.9 us, now 3.4).
+    bool dry = true;
+
+    __device__ Drain(const Ring& r, uint32_t t, uint8_t* staging) : ring(r), tmem(t) {
+        const int warp = int(threadIdx.x >> 5) - 4;
+        lane = threadIdx.x & 31;
+        quarter = warp & 3;
+        first = 32 * (warp >> 2);
+        out = WarpOut{staging + warp * kWarpStaging, lane};
+    }
+
     // The accumulator is read out: the MMA warp may fill it again.  The fence orders the reads of tensor memory; the arrival has
     // nothing else to release, and one that releases to the whole cluster waits for the stores under way, 1,000 cycles.
-    auto release = [&] {
+    __device__ __forceinline__ void release() {
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
             if (PAIR)
-                asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(peer_addr(&bars->tempty[acc], 0)) : "memory");
+                asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(peer_addr(&ring.bars->tempty[acc], 0)) : "memory");
             else
-                mbar_arrive(&bars->tempty[acc]);
+                mbar_arrive(&ring.bars->tempty[acc]);
         }
-    };
-    auto turn = [&] {
+    }
+    __device__ __forceinline__ void turn() {
         if (++acc == 2) {
             acc = 0;
             phase ^= 1u;
         }
-    };
-    // The first unit's first columns are gone through twice, before its products are there with a matrix of no rows and no
-    // columns, which loads and stores nothing: what follows a sum is then in the instruction cache when it is waited for (from
-    // there its 1,100 cycles were mostly misses; a layer of 256 x 256 x 256 3.9 us, now 3.4).
-    bool ok = true, dry = true;
-    Units<PAIR, NP, L> w(l);
-    while (w.more()) {
-        const Problem& pr = w.problem();
-        const Unit t = w.unit();
-        const int row0 = (PAIR ? 2 * t.tp + int(rank) : t.tp) * kRows + quarter * 32;
-        if (dry) {
-        } else if constexpr (LONG) {
-            constexpr int kMost = PAIR ? 4 : 2;   // chunks of a warp
-            float sum[kMost][32] = {};
-            const int runs = (t.hi - t.lo + pr.run - 1) / pr.run;
-            for (int i = 0; i < runs && ok; ++i) {
-                ok = __all_sync(0xffffffffu, wait_phase_inline(&bars->tfull[acc], phase, abort));   // a call would spill the sums
-                if (!ok) break;
-                tc_fence_after();
-                if (runs == 1) break;
-                const bool last = i + 1 == runs;
-#pragma unroll
-                for (int k = 0; k < kMost; ++k) {
-                    const uint32_t at = tmem + uint32_t(acc * kAccCols + first + 64 * k) + lanes;   // beyond the tile's columns, too
-                    uint32_t r[32];
-                    tmem_ld32(at, r);
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) sum[k][j] += __uint_as_float(r[j]);
-                }
-                if (last) {   // what follows reads the whole sum as it would read one run's
-#pragma unroll
-                    for (int k = 0; k < kMost; ++k) tmem_st32(tmem + uint32_t(acc * kAccCols + first + 64 * k) + lanes, sum[k]);
-                    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-                } else {
-                    release();
-                    turn();
-                }
-            }
-        } else {
-            ok = warp_wait(&bars->tfull[acc], phase, abort);
-            tc_fence_after();
-        }
-        if (!ok) {
-            give_up(abort, l.flags);
-            break;
-        }
-        if (!dry && first >= pr.cols) release();   // a tile of 32 columns has none for this warp
-#pragma unroll 1
-        for (int c = first; c < pr.cols; c += 64) {
-            uint32_t r[32];
-            __syncwarp();
-            tmem_ld32(tmem + uint32_t(acc * kAccCols + c) + lanes, r);
-            if (!dry && c + 64 >= pr.cols) release();
-            const int col0 = t.tq * pr.cols + c;
-            if (row0 < pr.rows && col0 < pr.cols_all)   // the same for the whole warp
-                l.epi[NP == 2 ? w.which : 0].chunk(pr, t, r, row0, col0, dry ? 0 : pr.rows, dry ? 0 : pr.cols_all, out);
-            if (dry) break;
-        }
-        if (dry) {
-            dry = false;
-            continue;
-        }
-        __syncwarp();
-        turn();
-        w.next();
     }
-}
 
-template <bool PAIR, bool LONG, int NP, int TERMS, class Epi>
-__global__ void __launch_bounds__(kProductThreads, 1)
-    product_kernel(const __grid_constant__ ProductLaunch<NP, TERMS, Epi> l) {
-    using L = ProductLaunch<NP, TERMS, Epi>;
-    extern __shared__ uint8_t smem_raw[];
-    uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    // The sums of a unit, once their accumulator holds them whole.
+    __device__ __forceinline__ bool ready(const Problem& pr, const Unit& t) {
+        volatile int32_t* abort = &ring.bars->abort;
+        if constexpr (!LONG) {
+            const bool ok = warp_wait(&ring.bars->tfull[acc], phase, abort);
+            tc_fence_after();
+            return ok;
+        }
+        constexpr int kMost = PAIR ? 4 : 2;   // chunks of a warp
+        const uint32_t lanes = uint32_t(quarter * 32) << 16;
+        float sum[kMost * 32] = {};
+        const int runs = (t.hi - t.lo + pr.run - 1) / pr.run;
+        bool ok = true;
+        for (int i = 0; i < runs && ok; ++i) {
+            // a call would spill the sums
+            ok = __all_sync(0xffffffffu, wait_phase_inline(&ring.bars->tfull[acc], phase, abort));
+            if (!ok) break;
+            tc_fence_after();
+            if (runs == 1) break;
+            const bool last = i + 1 == runs;
+            const uint32_t at = tmem + uint32_t(acc * kAccCols + first) + lanes;   // beyond the tile's columns, too
+#pragma unroll
+            for (int k = 0; k < 2 * kMost; ++k) tmem_add16(at + 64 * (k >> 1) + 16 * (k & 1), sum + 16 * k);
+            if (last) {   // what follows reads the whole sum as it would read one run's
+#pragma unroll
+                for (int k = 0; k < 2 * kMost; ++k) tmem_st16(at + 64 * (k >> 1) + 16 * (k & 1), sum + 16 * k);
+                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+            } else {
+                release();
+                turn();
+            }
+        }
+        return ok;
+    }
+
+    template <class Epi>
+    __device__ __forceinline__ bool unit(const Problem& pr, const Unit& t, const Epi& epi) {
+        const int row0 = (PAIR ? 2 * t.tp + int(ring.rank) : t.tp) * kRows + quarter * 32;
+#pragma unroll 1
+        for (int pass = dry ? 0 : 1; pass < 2; ++pass) {
+            const bool live = pass == 1;
+            if (live && !ready(pr, t)) {
+                give_up(&ring.bars->abort, ring.flags);
+                return false;
+            }
+            if (live && first >= pr.cols) release();   // a tile of 32 columns has none for this warp
+#pragma unroll 1
+            for (int c = first; c < pr.cols; c += 64) {
+                uint32_t r[32];
+                __syncwarp();
+                tmem_ld32(tmem + uint32_t(acc * kAccCols + c) + (uint32_t(quarter * 32) << 16), r);
+                if (live && c + 64 >= pr.cols) release();
+                const int col0 = t.tq * pr.cols + c;
+                if (row0 < pr.rows && col0 < pr.cols_all)   // the same for the whole warp
+                    epi.chunk(pr, t, r, row0, col0, live ? pr.rows : 0, live ? pr.cols_all : 0, out);
+                if (!live) break;
+            }
+            __syncwarp();
+        }
+        dry = false;
+        turn();
+        return true;
+    }
+};
+
+// What a kernel of products does before its roles begin, and after they have ended.
+struct Begun {
+    Ring ring;
+    uint8_t* staging;
+    uint32_t tmem;
+};
+
+template <bool PAIR>
+__device__ __forceinline__ Begun begin_products(uint8_t* smem, int stages, int stage_bytes, const CUtensorMap* p, const CUtensorMap* q,
+                                                int32_t* flags) {
+    uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem) + 1023) & ~uintptr_t(1023));
     uint8_t* staging = ring + kRingBytes;
     ProductBarriers* bars = reinterpret_cast<ProductBarriers*>(staging + kDrain * kWarpStaging);
-    const int warp = threadIdx.x >> 5;
-    const uint32_t rank = PAIR ? cluster_rank() : 0;
     if (threadIdx.x == 0) {
         for (int s = 0; s < kMaxStages; ++s) {
             mbar_init(&bars->full[s], 1);
@@ -516,12 +561,12 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         mbar_init(&bars->mma_done, 1);
         bars->abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&l.p[0][0])) : "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&l.q[0][0])) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(p)) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(q)) : "memory");
     }
     // Before the grid's wait, while the launch before this one ends: nothing here touches memory, and with all of an SM's shared
     // memory a CTA shares its tensor memory with no other.
-    if (warp == 2) {
+    if (threadIdx.x >> 5 == 2) {
         if (PAIR) {   // one warp of each CTA of the pair, together
             asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)),
                          "r"(kTmemCols)
@@ -538,27 +583,51 @@ __global__ void __launch_bounds__(kProductThreads, 1)
     __syncthreads();
     if (PAIR) cluster_sync();   // the other's barriers are initialised, and it runs
     tc_fence_after();
-    const uint32_t tmem = bars->tmem_base;
+    const Begun b{Ring{ring, bars, stages, stage_bytes, PAIR ? cluster_rank() : 0u, flags}, staging, bars->tmem_base};
     grid_begin();
-    if (warp < 4) {
-        if constexpr (LONG) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegs));
-        if (warp == 0) produce_slabs<PAIR, NP, TERMS, L>(l, ring, bars, rank);
-        if (warp == 1 && rank == 0) issue_products<PAIR, NP, TERMS, L>(l, ring, bars, tmem);
-    } else {
-        if constexpr (LONG) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegs));
-        drain<PAIR, LONG, NP, L>(l, bars, tmem, staging, rank);
-    }
+    return b;
+}
+
+template <bool PAIR>
+__device__ __forceinline__ void end_products(uint32_t tmem) {
     __syncwarp();
     tc_fence_before();
     __syncthreads();
     if (PAIR) cluster_sync();   // no CTA frees its TMEM or leaves while the other may still touch it
-    if (warp == 2) {
+    if (threadIdx.x >> 5 == 2) {
         tc_fence_after();
         if (PAIR)
             asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
         else
             asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
     }
+}
+
+template <bool PAIR, bool LONG, int NP, int TERMS, class Epi>
+__global__ void __launch_bounds__(kProductThreads, 1)
+    product_kernel(const __grid_constant__ ProductLaunch<NP, TERMS, Epi> l) {
+    using L = ProductLaunch<NP, TERMS, Epi>;
+    extern __shared__ uint8_t smem_raw[];
+    const Begun b = begin_products<PAIR>(smem_raw, l.stages, l.stage_bytes, &l.p[0][0], &l.q[0][0], l.flags);
+    const int warp = threadIdx.x >> 5;
+    if (warp < 4) {
+        if (warp == 0) {
+            Producer<PAIR, TERMS> role{b.ring};
+            for (Units<PAIR, NP, L> w(l); w.more(); w.next())
+                if (!role.unit(w.problem(), w.unit(), l.p[NP == 2 ? w.which : 0], l.q[NP == 2 ? w.which : 0])) break;
+        }
+        if (warp == 1 && b.ring.rank == 0) {
+            Multiplier<PAIR, TERMS> role{b.ring, b.tmem};
+            for (Units<PAIR, NP, L> w(l); w.more(); w.next())
+                if (!role.unit(w.problem(), w.unit())) break;
+            role.finish();
+        }
+    } else {
+        Drain<PAIR, LONG> role(b.ring, b.tmem, b.staging);
+        for (Units<PAIR, NP, L> w(l); w.more(); w.next())
+            if (!role.unit(w.problem(), w.unit(), l.epi[NP == 2 ? w.which : 0])) break;
+    }
+    end_products<PAIR>(b.tmem);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
