@@ -25,7 +25,8 @@
 // the MMAs fill the next (LONG).
 //
 // TERMS = 3: each operand is two bf16 matrices, p = p0 + p1, and acc takes p0 q0 + p0 q1 + p1 q0 (Dekker's split product
-// without its smallest term): four tiles in shared memory feed three MMAs.
+// without its smallest term): four tiles in shared memory feed three MMAs.  One copy brings both halves of an operand: a copy
+// takes 75 ns to issue, and of a short sum the first four slabs' sixteen took longer than its MMAs.
 #pragma once
 
 #include <cuda.h>
@@ -59,6 +60,8 @@ struct ProductBarriers {
     uint64_t tfull[2];            // an accumulator is complete
     uint64_t tempty[2];           // the epilogue warps (pair: of both CTAs, on the even one) have read it
     uint64_t mma_done;
+    uint64_t written;             // the epilogue warps have written what they had of a product
+    uint64_t passed;              // and so have all CTAs' of the grid
     uint32_t tmem_base;
     int32_t abort;
 };
@@ -92,8 +95,7 @@ struct Unit {
 
 template <int NP, int TERMS, class Epi>
 struct ProductLaunch {
-    static constexpr int kMats = TERMS == 3 ? 2 : 1;
-    CUtensorMap p[NP][kMats], q[NP][kMats];
+    CUtensorMap p[NP], q[NP];
     Problem pr[NP];
     Epi epi[NP];
     int stages, stage_bytes;
@@ -160,9 +162,11 @@ struct Units {
 };
 
 // The descriptor of an operand's tile: rows of 128 bytes along the sum, or 64 x 64 blocks in which the sum runs from row to row:
-// 64 of the operand's rows are the 128 bytes, eight of the sum are 1,024, and the next 64 rows are a block further.
+// 64 of the operand's rows are the 128 bytes, eight of the sum are 1,024, and the next 64 rows are a block further (two
+// blocks, where each half has its own).
+template <int MATS>
 __device__ __forceinline__ uint64_t tile_desc(uint32_t addr, int turned) {
-    return smem_desc(addr) | (turned ? uint64_t(kSlab * kRowBytes >> 4) << 16 : 0);
+    return smem_desc(addr) | (turned ? uint64_t(MATS * kSlab * kRowBytes >> 4) << 16 : 0);
 }
 
 // What the roles have in common: the ring of stages, its barriers, and how they give up.
@@ -198,7 +202,7 @@ struct Producer {
         }
     }
 
-    // p and q: the maps of the operands' matrices.
+    // p and q: the operands' maps.
     __device__ __forceinline__ bool unit(const Problem& pr, const Unit& t, const CUtensorMap* p, const CUtensorMap* q) {
         ProductBarriers* bars = ring.bars;
         volatile int32_t* abort = &bars->abort;
@@ -206,6 +210,7 @@ struct Producer {
         const int bytes = kMats * (kRows * kRowBytes + q_bytes);
         const int p0 = (PAIR ? 2 * t.tp + int(ring.rank) : t.tp) * kRows;
         const int q0 = t.tq * pr.cols + (PAIR ? int(ring.rank) * q_rows : 0);
+        const bool p_turned = pr.p_turned, q_turned = pr.q_turned;
         for (int kb = t.lo; kb < t.hi; ++kb) {
             if (!warp_wait(&bars->empty[stage], phase ^ 1u, abort)) {
                 give_up(abort, ring.flags);
@@ -216,26 +221,17 @@ struct Producer {
             const uint32_t bar = PAIR ? peer_addr(&bars->full[stage], 0) : smem_u32(&bars->full[stage]);
             if (elect_one()) {
                 if (!PAIR || ring.rank == 0) mbar_expect_tx(&bars->full[stage], uint32_t((PAIR ? 2 : 1) * bytes));
-#pragma unroll
-                for (int i = 0; i < kMats; ++i) {
-                    uint8_t* to = s + i * kRows * kRowBytes;
-                    if (pr.p_turned) {
-                        tma_load_3d<PAIR>(to, &p[i], bar, p0, kb * kSlab, t.z);
-                        tma_load_3d<PAIR>(to + kSlab * kRowBytes, &p[i], bar, p0 + kSlab, kb * kSlab, t.z);
-                    } else {
-                        tma_load_3d<PAIR>(to, &p[i], bar, kb * kSlab, p0, t.z);
+                // 64 x 64 blocks of a turned operand, rows of the other kind
+                auto copy = [&](uint8_t* to, const CUtensorMap* map, bool turned, int row, int rows) {
+                    for (int j = 0; j < (turned ? rows : 1); j += kSlab) {
+                        uint8_t* at = to + kMats * j * kRowBytes;
+                        const int x = turned ? row + j : kb * kSlab, y = turned ? kb * kSlab : row;
+                        if constexpr (kMats == 2) tma_load_4d<PAIR>(at, map, bar, x, y, t.z);
+                        else tma_load_3d<PAIR>(at, map, bar, x, y, t.z);
                     }
-                }
-#pragma unroll
-                for (int i = 0; i < kMats; ++i) {
-                    uint8_t* to = s + kMats * kRows * kRowBytes + i * q_bytes;
-                    if (pr.q_turned) {
-                        for (int j = 0; j < q_rows; j += kSlab)
-                            tma_load_3d<PAIR>(to + j * kRowBytes, &q[i], bar, q0 + j, kb * kSlab, t.z);
-                    } else {
-                        tma_load_3d<PAIR>(to, &q[i], bar, kb * kSlab, q0, t.z);
-                    }
-                }
+                };
+                copy(s, p, p_turned, p0, kRows);
+                copy(s + kMats * kRows * kRowBytes, q, q_turned, q0, q_rows);
             }
             ++issued;
             if (++stage == ring.stages) {
@@ -271,10 +267,13 @@ struct Multiplier {
         ProductBarriers* bars = ring.bars;
         volatile int32_t* abort = &bars->abort;
         const uint32_t base = smem_u32(ring.at), units = uint32_t(ring.stage_bytes) >> 4;   // of a stage, in descriptors
-        const uint64_t pdesc0 = tile_desc(base, pr.p_turned), qdesc0 = tile_desc(base + kMats * kRows * kRowBytes, pr.q_turned);
+        const uint64_t pdesc0 = tile_desc<kMats>(base, pr.p_turned);
+        const uint64_t qdesc0 = tile_desc<kMats>(base + kMats * kRows * kRowBytes, pr.q_turned);
         // from one K = 16 to the next: 32 bytes of a row, or sixteen rows
         const uint32_t pstep = pr.p_turned ? 16 * kRowBytes >> 4 : 2, qstep = pr.q_turned ? 16 * kRowBytes >> 4 : 2;
-        const uint32_t plow = kRows * kRowBytes >> 4, qlow = uint32_t((PAIR ? pr.cols / 2 : pr.cols) * kRowBytes) >> 4;
+        // from a half to the other
+        const uint32_t plow = uint32_t((pr.p_turned ? kSlab : kRows) * kRowBytes) >> 4;
+        const uint32_t qlow = uint32_t((pr.q_turned ? kSlab : PAIR ? pr.cols / 2 : pr.cols) * kRowBytes) >> 4;
         for (int run = t.lo; run < t.hi; run += pr.run) {
             if (!warp_wait(&bars->tempty[acc], aphase ^ 1u, abort)) {
                 give_up(abort, ring.flags);
@@ -330,6 +329,10 @@ struct Multiplier {
     }
 };
 
+__device__ __forceinline__ void ld_shared16(uint32_t addr, uint32_t (&v)[4]) {
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(addr));
+}
+
 // An epilogue warp's way out: through its block of shared memory, so that neighbouring lanes store neighbouring pieces of 16
 // bytes, four or eight to a row.  (TMA stores of the blocks took longer: a copy keeps its block for about 1,000 cycles, and the
 // next 32 columns waited for it.  256 x 256 x 256, alone: 4.3 us, now 3.3.)
@@ -350,9 +353,7 @@ struct WarpOut {
         for (int i = 0; i < kPieces; ++i) {
             const int r = i * kRowsAtOnce + r0;
             const uint32_t swz = kPieces == 4 ? uint32_t((r >> 1) & 3) : uint32_t(r & 7);
-            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                         : "=r"(v[i][0]), "=r"(v[i][1]), "=r"(v[i][2]), "=r"(v[i][3])
-                         : "r"(base + uint32_t(r * 32 * int(sizeof(T))) + ((uint32_t(piece) ^ swz) << 4)));
+            ld_shared16(base + uint32_t(r * 32 * int(sizeof(T))) + ((uint32_t(piece) ^ swz) << 4), v[i]);
         }
         T* p = to + (row0 + r0) * ld + c;
         const int64_t step = kRowsAtOnce * ld;
@@ -392,6 +393,80 @@ struct WarpOut {
             st_shared16(at + ((uint32_t(k) ^ swz) << 4), x);
         }
         send(to, ld, rows, cols, row0, col0);
+    }
+
+    // The values as two bf16 numbers each, h their roundings and l those of what is left, to two matrices; as store, or turned:
+    // lane i has column col0 + i and its rows row0 .. row0 + 31.  Both go through shared memory at once, turned ones as words of
+    // both halves: one after the other, with 16-bit words, a tile of 256 x 256 and its mirror image took 9 us.
+    __device__ __forceinline__ void store_halves(acrl_bf16* hi, acrl_bf16* lo, int64_t ld, int rows, int cols, const uint32_t (&h)[16],
+                                                 const uint32_t (&l)[16], int row0, int col0) const {
+        const uint32_t base = smem_u32(staging), swz = uint32_t((lane >> 1) & 3), at = base + uint32_t(lane * 64);
+        constexpr uint32_t kHalf = kWarpStaging / 2;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t to = at + ((uint32_t(k) ^ swz) << 4);
+            st_shared16(to, make_uint4(h[4 * k], h[4 * k + 1], h[4 * k + 2], h[4 * k + 3]));
+            st_shared16(to + kHalf, make_uint4(l[4 * k], l[4 * k + 1], l[4 * k + 2], l[4 * k + 3]));
+        }
+        __syncwarp();
+        const int piece = lane & 3, c = col0 + 8 * piece, r0 = lane >> 2;
+        uint32_t v[8][4];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = (i & 3) * 8 + r0;
+            ld_shared16(base + (i >> 2) * kHalf + uint32_t(r * 64) + ((uint32_t(piece) ^ uint32_t((r >> 1) & 3)) << 4), v[i]);
+        }
+        const int64_t to = (row0 + r0) * ld + c;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            acrl_bf16* p = (i < 4 ? hi : lo) + to + (i & 3) * 8 * ld;
+            if (row0 + r0 + (i & 3) * 8 >= rows) continue;
+            if (c + 8 <= cols) {
+                *reinterpret_cast<uint4*>(p) = make_uint4(v[i][0], v[i][1], v[i][2], v[i][3]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (c + k < cols) p[k] = acrl_bf16(v[i][k >> 1] >> (k & 1) * 16);
+            }
+        }
+        __syncwarp();
+    }
+
+    __device__ __forceinline__ void store_halves_turned(acrl_bf16* hi, acrl_bf16* lo, int64_t ld, int rows, int cols, const uint32_t (&h)[16],
+                                                        const uint32_t (&l)[16], int row0, int col0) const {
+        const uint32_t base = smem_u32(staging), at = base + uint32_t((lane & 3) * 4);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            const uint32_t word = __byte_perm(h[j >> 1], l[j >> 1], j & 1 ? 0x7632 : 0x5410);
+            asm volatile("st.shared.u32 [%0], %1;" ::"r"(at + uint32_t(j * 128) + ((uint32_t(lane >> 2) ^ uint32_t(j & 7)) << 4)), "r"(word)
+                         : "memory");
+        }
+        __syncwarp();
+        const int piece = lane & 7, c = col0 + 4 * piece, r0 = lane >> 3;
+        uint32_t v[8][4];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = i * 4 + r0;
+            ld_shared16(base + uint32_t(r * 128) + ((uint32_t(piece) ^ uint32_t(r & 7)) << 4), v[i]);
+        }
+        const int64_t to = (row0 + r0) * ld + c;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (row0 + r0 + i * 4 >= rows) continue;
+            acrl_bf16 *p = hi + to + i * 4 * ld, *q = lo + to + i * 4 * ld;
+            if (c + 4 <= cols) {
+                *reinterpret_cast<uint2*>(p) = make_uint2(__byte_perm(v[i][0], v[i][1], 0x5410), __byte_perm(v[i][2], v[i][3], 0x5410));
+                *reinterpret_cast<uint2*>(q) = make_uint2(__byte_perm(v[i][0], v[i][1], 0x7632), __byte_perm(v[i][2], v[i][3], 0x7632));
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (c + k < cols) {
+                        p[k] = acrl_bf16(v[i][k]);
+                        q[k] = acrl_bf16(v[i][k] >> 16);
+                    }
+            }
+        }
+        __syncwarp();
     }
 
     // The same values turned, rounded to bf16: lane i has column col0 + i and its rows row0 .. row0 + 31.
@@ -559,6 +634,8 @@ __device__ __forceinline__ Begun begin_products(uint8_t* smem, int stages, int s
             mbar_init(&bars->tempty[b], (PAIR ? 2 : 1) * kDrain);
         }
         mbar_init(&bars->mma_done, 1);
+        mbar_init(&bars->written, kDrain);
+        mbar_init(&bars->passed, 1);
         bars->abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(p)) : "memory");
@@ -608,13 +685,13 @@ __global__ void __launch_bounds__(kProductThreads, 1)
     product_kernel(const __grid_constant__ ProductLaunch<NP, TERMS, Epi> l) {
     using L = ProductLaunch<NP, TERMS, Epi>;
     extern __shared__ uint8_t smem_raw[];
-    const Begun b = begin_products<PAIR>(smem_raw, l.stages, l.stage_bytes, &l.p[0][0], &l.q[0][0], l.flags);
+    const Begun b = begin_products<PAIR>(smem_raw, l.stages, l.stage_bytes, &l.p[0], &l.q[0], l.flags);
     const int warp = threadIdx.x >> 5;
     if (warp < 4) {
         if (warp == 0) {
             Producer<PAIR, TERMS> role{b.ring};
             for (Units<PAIR, NP, L> w(l); w.more(); w.next())
-                if (!role.unit(w.problem(), w.unit(), l.p[NP == 2 ? w.which : 0], l.q[NP == 2 ? w.which : 0])) break;
+                if (!role.unit(w.problem(), w.unit(), &l.p[NP == 2 ? w.which : 0], &l.q[NP == 2 ? w.which : 0])) break;
         }
         if (warp == 1 && b.ring.rank == 0) {
             Multiplier<PAIR, TERMS> role{b.ring, b.tmem};
@@ -634,19 +711,19 @@ __global__ void __launch_bounds__(kProductThreads, 1)
 // host
 // ---------------------------------------------------------------------------------------------------------------
 
-// An operand of a product: [rows, K], or with `turned` [K, rows]; `count` of them `apart` elements from one another.
+// An operand of a product: [rows, K], or with `turned` [K, rows]; `count` of them `apart` elements from one another, and with
+// `halves` > 0 two such lots, that many from one another.
 struct Matrix {
     const acrl_bf16* at;
     int64_t rows, ld;
     bool turned;
-    int64_t count, apart;
+    int64_t count, apart, halves;
 };
 
 inline bool operand_map(CUtensorMap* map, const Matrix& m, int64_t K, int box_rows) {
-    return m.turned ? encode_map_3d(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, m.at, uint64_t(m.count), uint64_t(K), uint64_t(m.rows),
-                                    uint64_t(m.ld), uint64_t(m.apart), kSlab, kSlab, CU_TENSOR_MAP_SWIZZLE_128B)
-                    : encode_map_3d(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, m.at, uint64_t(m.count), uint64_t(m.rows), uint64_t(K),
-                                    uint64_t(m.ld), uint64_t(m.apart), uint32_t(box_rows), kSlab, CU_TENSOR_MAP_SWIZZLE_128B);
+    return encode_map_3d(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, m.at, uint64_t(m.count), uint64_t(m.turned ? K : m.rows),
+                         uint64_t(m.turned ? m.rows : K), uint64_t(m.ld), uint64_t(m.apart), uint64_t(m.halves),
+                         uint32_t(m.turned ? kSlab : box_rows), kSlab, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 // How a product is cut: columns of a tile, tiles of all matrices, and the sum's parts of `per` slabs.

@@ -204,7 +204,7 @@ bool describe(ProductLaunch<NP, 1, LinearEpilogue<PAIR>>& l, int at, const Produ
     l.pr[at] = problem_of(d.plan.shape, cut, p.turned, q.turned, has_runs(d));
     l.epi[at].f = d.f;
     l.epi[at].parts = d.parts;
-    return operand_map(&l.p[at][0], p, d.K, kRows) && operand_map(&l.q[at][0], q, d.K, PAIR ? cut.cols / 2 : cut.cols);
+    return operand_map(&l.p[at], p, d.K, kRows) && operand_map(&l.q[at], q, d.K, PAIR ? cut.cols / 2 : cut.cols);
 }
 
 acrl_status join(const Problem& pr, const Product& d, cudaStream_t s) {
@@ -389,7 +389,7 @@ extern "C" acrl_status acrl_linear(const acrl_bf16* x, int64_t M, int64_t K, int
                    out_dtype == ACRL_F32};
     if (linear_few_rows(M, N, K)) return linear_few(x, M, K, ldx, w, N, ldw, f, reinterpret_cast<cudaStream_t>(stream));
     const Plan plan = plan_linear(M, N, K);
-    return product({plan, Matrix{x, M, ldx, false, 1, M * ldx}, Matrix{w, N, ldw, false, 1, N * ldw}, K, f, static_cast<float*>(workspace)},
+    return product({plan, Matrix{x, M, ldx, false, 1, M * ldx, 0}, Matrix{w, N, ldw, false, 1, N * ldw, 0}, K, f, static_cast<float*>(workspace)},
                    dev_flags, reinterpret_cast<cudaStream_t>(stream));
 }
 
@@ -451,9 +451,9 @@ extern "C" acrl_status acrl_linear_backward(const acrl_bf16* dy, int64_t M, int6
     fw.out = dw;
     fw.ldo = lddw;
     fw.out_f32 = dw_dtype == ACRL_F32;
-    const Product both[2] = {{parts.plan.dx, Matrix{g, M, ldg, false, 1, M * ldg}, Matrix{w, K, ldw, true, 1, N * ldw}, has_g ? N : 0, fx,
+    const Product both[2] = {{parts.plan.dx, Matrix{g, M, ldg, false, 1, M * ldg, 0}, Matrix{w, K, ldw, true, 1, N * ldw, 0}, has_g ? N : 0, fx,
                               reinterpret_cast<float*>(base + parts.dx)},
-                             {parts.plan.dw, Matrix{g, N, ldg, true, 1, M * ldg}, Matrix{x, K, ldx, true, 1, M * ldx}, has_g ? M : 0, fw,
+                             {parts.plan.dw, Matrix{g, N, ldg, true, 1, M * ldg, 0}, Matrix{x, K, ldx, true, 1, M * ldx, 0}, has_g ? M : 0, fw,
                               reinterpret_cast<float*>(base + parts.dw)}};
     if (has_dx && has_dw && has_g && parts.plan.together) return run_products<true, 2>(both, dev_flags, s);
     if (has_dx) st = product(both[0], dev_flags, s);

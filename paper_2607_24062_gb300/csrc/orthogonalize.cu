@@ -6,6 +6,10 @@
 // symmetric: tiles above the diagonal are left out and written as mirror images, 3 m^2 n + m^3 multiply-adds a step where the
 // plain products have 4 m^2 n + 2 m^3.
 //
+// All steps are one cooperative launch: CTA pairs, one CTA an SM, go through the products of all steps, and wait for one
+// another between them on a counter in the workspace (each wait is bounded in time).  Launched one by one, each product of a
+// small matrix spent more on its launch, on tensor memory and on first copies than on its sums.
+//
 // Operands are two bf16 numbers each, x = x0 + x1 with x0 the rounding of x and x1 that of what is left, which together are
 // within 2^-16 of it, and a product is three of the tensor cores' (bf16_product.cuh).  One bf16 number would not do: gradients
 // have a few strong directions and many weak ones, whose singular values the steps amplify by up to a^steps (485 for five
@@ -86,10 +90,11 @@ __device__ __forceinline__ void load8(const Update& u, int64_t row, int c, float
     }
 }
 
-// Partial sums of a matrix's squares, `ctas` of them.  HBM bounds it.
-__global__ void __launch_bounds__(256) squares_kernel(Update u, int ctas, double* sums) {
+// Partial sums of a matrix's squares, `ctas` of them.  HBM bounds it.  It also clears the counter of the steps' waits.
+__global__ void __launch_bounds__(256) squares_kernel(Update u, int ctas, double* sums, unsigned* arrived) {
     __shared__ double part[8];
     grid_begin();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *arrived = 0;
     const int b = int(blockIdx.x) / ctas, lane = threadIdx.x & 31;
     Squares s;
     Pieces p(u, int(blockIdx.x) - b * ctas, ctas);
@@ -114,13 +119,7 @@ __global__ void __launch_bounds__(256) squares_kernel(Update u, int ctas, double
     }
 }
 
-// Two bf16 numbers for one.
-__device__ __forceinline__ void halves(float x, acrl_bf16& hi, acrl_bf16& lo) {
-    hi = to_bf16(x);
-    lo = to_bf16(x - bf16_to_float(hi));
-}
-
-// Eight of them, from a column that is a multiple of eight.
+// Two bf16 numbers for each of eight, from a column that is a multiple of eight.
 __device__ __forceinline__ void halves8(const float (&v)[8], acrl_bf16* hi, acrl_bf16* lo) {
     uint32_t h[4], l[4];
 #pragma unroll
@@ -218,35 +217,66 @@ struct Finish {
     bool tall;                         // the result is turned back
 };
 
-// Four of A's numbers from their halves.
-__device__ __forceinline__ void add_halves(uint2 h, uint2 l, float (&A)[4]) {
-    A[0] = bf16_lo(h.x) + bf16_lo(l.x);
-    A[1] = bf16_hi(h.x) + bf16_hi(l.x);
-    A[2] = bf16_lo(h.y) + bf16_lo(l.y);
-    A[3] = bf16_hi(h.y) + bf16_hi(l.y);
-}
-
-// a I + b A + c v at row i, columns j .. j + 31; what is beyond the matrix is left out of the result.  A row's 64 bytes of each half come in 16-byte loads: one by one they took three times as long as the product (24 x 1,024 x
-// 1,024: 220 us a step against 66 for A itself).
-__device__ __forceinline__ void polynomial(const Finish& f, int64_t at, int i, int j, int m, float (&v)[32]) {
+// a I + b A + c v at row i, columns j .. j + 31; what is beyond the matrix is left out of the result.  A row's 64 bytes of each
+// half come in 16-byte loads, all of them in flight together: no test is around a load, and those beyond the matrix are of its
+// first row or column (one after the other they took 1.1 us of a tile's 2.6).
+__device__ __forceinline__ void polynomial(const Finish& f, int z, int i, int j, int m, float (&v)[32]) {
+    if (m == 0) return;
+    const int64_t row = z * f.size + min(i, m - 1) * f.ld;
+    uint4 h[4], l[4];
 #pragma unroll
-    for (int k = 0; k < 32; k += 8) {
-        uint4 h = make_uint4(0u, 0u, 0u, 0u), l = h;
-        if (i < m && j + k < f.ld) {   // ld is a multiple of eight
-            h = *reinterpret_cast<const uint4*>(f.hi_in + at + k);
-            l = *reinterpret_cast<const uint4*>(f.lo_in + at + k);
+    for (int k = 0; k < 4; ++k) {
+        const int64_t at = row + (j + 8 * k < f.ld ? j + 8 * k : 0);   // ld is a multiple of eight
+        h[k] = *reinterpret_cast<const uint4*>(f.hi_in + at);
+        l[k] = *reinterpret_cast<const uint4*>(f.lo_in + at);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t hw[4] = {h[k].x, h[k].y, h[k].z, h[k].w}, lw[4] = {l[k].x, l[k].y, l[k].z, l[k].w};
+#pragma unroll
+        for (int n = 0; n < 8; ++n) {
+            const float A = n & 1 ? bf16_hi(hw[n >> 1]) + bf16_hi(lw[n >> 1]) : bf16_lo(hw[n >> 1]) + bf16_lo(lw[n >> 1]);
+            v[8 * k + n] = fmaf(f.c, v[8 * k + n], fmaf(f.b, A, i == j + 8 * k + n ? f.a : 0.f));
         }
-        float A[8];
-        add_halves(make_uint2(h.x, h.y), make_uint2(l.x, l.y), *reinterpret_cast<float (*)[4]>(A));
-        add_halves(make_uint2(h.z, h.w), make_uint2(l.z, l.w), *reinterpret_cast<float (*)[4]>(A + 4));
-#pragma unroll
-        for (int n = 0; n < 8; ++n) v[k + n] = fmaf(f.c, v[k + n], fmaf(f.b, A[n], i < m && i == j + k + n ? f.a : 0.f));
     }
 }
 
 struct StepEpilogue {
     Finish f;
-    float* parts;                  // of the tiles
+    float* parts;   // of the tiles
+
+    // Whole sums of 32 x 32: a lane has a row, or with `turned` a column.
+    __device__ __forceinline__ void finish(const Problem& pr, const Unit& t, float (&v)[32], int row0, int col0, int rows, int cols,
+                                           bool turned, const WarpOut& out) const {
+        if (f.kind == kResult) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] *= f.scale;
+            acrl_bf16* to = f.out + t.z * f.out_stride;
+            // of the matrix, or of its transpose
+            const int R = f.tall ? cols : rows, C = f.tall ? rows : cols, r = f.tall ? col0 : row0, c = f.tall ? row0 : col0;
+            if (turned != f.tall) out.store_turned(to, f.ldo, R, C, v, r, c);
+            else out.store(to, f.ldo, R, C, v, r, c);
+            return;
+        }
+        if (f.kind == kPolynomial)   // A is symmetric: its column is its row
+            polynomial(f, t.z, (turned ? col0 : row0) + out.lane, turned ? row0 : col0, rows, v);
+        uint32_t h[16], l[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            h[j] = pack_bf16x2(v[2 * j], v[2 * j + 1]);
+            l[j] = pack_bf16x2(v[2 * j] - bf16_lo(h[j]), v[2 * j + 1] - bf16_hi(h[j]));
+        }
+        acrl_bf16 *hi = f.hi + t.z * f.size, *lo = f.lo + t.z * f.size;
+        const bool twice = pr.lower && col0 < t.tp * 2 * kRows;   // a tile above the diagonal has no other way to be written
+        if (!turned || twice) {
+            const bool other = turned;   // the lane's values, as a row of the transpose
+            out.store_halves(hi, lo, f.ld, other ? cols : rows, other ? rows : cols, h, l, other ? col0 : row0, other ? row0 : col0);
+        }
+        if (turned || twice) {
+            const bool other = !turned;
+            out.store_halves_turned(hi, lo, f.ld, other ? cols : rows, other ? rows : cols, h, l, other ? col0 : row0, other ? row0 : col0);
+        }
+    }
 
     __device__ __forceinline__ void chunk(const Problem& pr, const Unit& t, const uint32_t (&r)[32], int row0, int col0, int rows,
                                           int cols, const WarpOut& out) const {
@@ -259,75 +289,160 @@ struct StepEpilogue {
                       col0 - t.tq * wide);
             return;
         }
-        if (f.kind == kResult) {
+        finish(pr, t, v, row0, col0, rows, cols, false, out);
+    }
+
+    // The parts of the tiles in their order, and what is made of them: block after block of 32 x 32, a warp each.  A lane has a
+    // column of the block, so that a row of it is one load.
+    __device__ void join(const Problem& pr, int warp, int warps, const WarpOut& out) const {
+        const int across = pr.cols / 32, each = 2 * kRows / 32 * across, tiles = pr.tiles * pr.batch;
+        const int64_t size = int64_t(2 * kRows) * pr.cols;
+        for (int64_t k = warp; k < int64_t(tiles) * each; k += warps) {
+            const Unit t = tile_at(pr, int(k / each));
+            const int in = int(k - int64_t(t.all) * each), r = in / across * 32, c = in % across * 32;   // in the tile
+            const int row0 = t.tp * 2 * kRows + r, col0 = t.tq * pr.cols + c;
+            if (row0 >= pr.rows || col0 >= pr.cols_all) continue;
+            float v[32] = {};
+            const float* p = parts + t.all * pr.parts * size + int64_t(r) * pr.cols + c + out.lane;
+            for (int j = 0; j < pr.parts; ++j)
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] *= f.scale;
-            acrl_bf16* to = f.out + t.z * f.out_stride;
-            if (f.tall) out.store_turned(to, f.ldo, cols, rows, v, col0, row0);
-            else out.store(to, f.ldo, rows, cols, v, row0, col0);
-            return;
-        }
-        const int row = row0 + out.lane;
-        if (f.kind == kPolynomial) polynomial(f, t.z * f.size + row * f.ld + col0, row, col0, rows, v);
-        const bool twice = pr.lower && col0 < t.tp * 2 * kRows;   // a tile above the diagonal has no other way to be written
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            acrl_bf16* to = (half ? f.lo : f.hi) + t.z * f.size;
-            out.store(to, f.ld, rows, cols, v, row0, col0);
-            if (twice) out.store_turned(to, f.ld, cols, rows, v, col0, row0);
-#pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] -= bf16_to_float(to_bf16(v[j]));   // what is left for the other
+                for (int i = 0; i < 32; ++i) v[i] += p[j * size + i * pr.cols];
+            finish(pr, t, v, row0, col0, pr.rows, pr.cols_all, true, out);
         }
     }
 };
 
-// The parts of the tiles in their order, and what is made of them, a block of 32 x 32 a CTA; of a symmetric matrix the
-// mirror image as well.
-__global__ void __launch_bounds__(256) join_kernel(Finish f, const float* parts, Problem pr) {
-    __shared__ float block[32][33];
-    grid_begin();
-    const int across = pr.cols / 32, blocks = 2 * kRows / 32 * across, tile = int(blockIdx.x) / blocks, k = int(blockIdx.x) - tile * blocks;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rows = pr.rows, cols = pr.cols_all;
-    const Unit t = tile_at(pr, tile);
-    const int64_t z = t.z;
-    const int rt = k / across * 32, ct = k % across * 32, r0 = t.tp * 2 * kRows + rt, c0 = t.tq * pr.cols + ct;   // in the tile, in all
-    if (r0 >= rows || c0 >= cols) return;
-    const bool turn = f.kind == kResult && f.tall, twice = pr.lower && c0 < t.tp * 2 * kRows;
-    float v[4] = {};
-    const int c = c0 + lane;
-    const int64_t size = int64_t(2 * kRows) * pr.cols;
-    const float* p = parts + tile * pr.parts * size + (rt + warp) * pr.cols + ct + lane;
-    for (int j = 0; j < pr.parts; ++j) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] += p[j * size + 8 * i * pr.cols];
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = r0 + warp + 8 * i;
-        const bool in = r < rows && c < cols;
-        const int64_t at = z * f.size + r * f.ld + c;
-        if (f.kind == kResult) {
-            v[i] *= f.scale;
-            if (in && !turn) f.out[z * f.out_stride + r * f.ldo + c] = to_bf16(v[i]);
-        } else {
-            if (f.kind == kPolynomial && in)
-                v[i] = fmaf(f.c, v[i], fmaf(f.b, bf16_to_float(f.hi_in[at]) + bf16_to_float(f.lo_in[at]), r == c ? f.a : 0.f));
-            if (in) halves(v[i], f.hi[at], f.lo[at]);
+// The products of a step: A = X X^T, Q from A A, Q X.
+enum { kProducts = 3 };
+
+struct StepsLaunch {
+    // of X (each of two buffers), A and Q: 128 rows as p, half a tile's columns as q, blocks turned
+    CUtensorMap x_p[2], x_q[2], x_turned[2], a_p, a_q, q_p;
+    Problem pr[kProducts];
+    Finish f[kProducts + 1];          // of A, Q, X in the first buffer, X in the second
+    float coeffs[3 * kMostSteps];
+    int steps;
+    float* parts;
+    unsigned* arrived;                // CTAs, of all waits so far
+    int stages, stage_bytes;
+    int32_t* flags;
+};
+
+// The grid's barriers between the products, and between a split sum's parts and their join.  The epilogue warps come to the
+// CTA's barrier `written`; a warp of its own then tells the grid, waits until every CTA has told it as often, and lets the CTA go
+// on at `passed`.  One thread a CTA looks at the counter: nine warps of each did at first, and 20 barriers took 68 us more than
+// as many launches (2,051 x 1,000).
+// A warp that goes on reads what all the others wrote; and it comes to no barrier before it has passed the one before, or its
+// arrival would be counted for another's.
+__device__ __forceinline__ void come(ProductBarriers* bars) {
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(&bars->written);
+}
+__device__ __forceinline__ bool pass(ProductBarriers* bars, unsigned count) {   // barrier number `count`, from 1 on
+    return warp_wait(&bars->passed, (count - 1) & 1u, &bars->abort);
+}
+
+// One thread's part of barriers 1 to `count`.
+__device__ bool keep_barriers(ProductBarriers* bars, unsigned* arrived, unsigned count) {
+    volatile int32_t* abort = &bars->abort;
+    for (unsigned k = 1; k <= count; ++k) {
+        if (!wait_phase(&bars->written, (k - 1) & 1u, abort)) return false;
+        __threadfence();
+        asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(arrived) : "memory");
+        const unsigned want = k * gridDim.x;
+        uint64_t t0 = 0;
+        for (uint32_t i = 0;; ++i) {
+            unsigned n;
+            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(n) : "l"(arrived) : "memory");
+            if (int(n - want) >= 0) break;
+            if ((i & 63u) == 63u) {
+                if (t0 == 0) t0 = global_ns();
+                if (*abort || global_ns() - t0 > kWaitNs) return false;
+            }
         }
-        block[warp + 8 * i][lane] = v[i];
+        mbar_arrive(&bars->passed);
     }
-    if (!turn && !twice) return;   // the same for the CTA
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = c0 + warp + 8 * i, d = r0 + lane;   // of the turned block
-        if (r >= cols || d >= rows) continue;
-        const float x = block[lane][warp + 8 * i];
-        if (turn)
-            f.out[z * f.out_stride + r * f.ldo + d] = to_bf16(x);
-        else
-            halves(x, f.hi[z * f.size + r * f.ld + d], f.lo[z * f.size + r * f.ld + d]);
+    return true;
+}
+
+__global__ void __launch_bounds__(kProductThreads, 1) steps_kernel(const __grid_constant__ StepsLaunch l) {
+    extern __shared__ uint8_t smem_raw[];
+    const Begun b = begin_products<true>(smem_raw, l.stages, l.stage_bytes, &l.x_p[0], &l.x_q[0], l.flags);
+    const int warp = threadIdx.x >> 5, pair = int(blockIdx.x >> 1), pairs = int(gridDim.x >> 1), last = kProducts * l.steps - 1;
+    ProductBarriers* bars = b.ring.bars;
+    volatile int32_t* abort = &bars->abort;
+    if (warp == 0) {
+        Producer<true, 3> role{b.ring};
+        unsigned barrier = 0;
+        bool ok = true;
+        for (int k = 0; k <= last && ok; ++k) {
+            const int kind = k % kProducts, x = (k / kProducts) & 1;
+            const Problem pr = l.pr[kind];
+            const CUtensorMap* p = kind == 0 ? &l.x_p[x] : kind == 1 ? &l.a_p : &l.q_p;
+            const CUtensorMap* q = kind == 0 ? &l.x_q[x] : kind == 1 ? &l.a_q : &l.x_turned[x];
+            Unit unit = unit_at(pr, pair);   // before the wait
+            if (k > 0 && !pass(bars, barrier)) {
+                give_up(abort, l.flags);
+                role.land();
+                break;
+            }
+            asm volatile("fence.proxy.async;" ::: "memory");   // copies read what others' stores have written
+            for (int u = pair; u < pr.units && ok; u += pairs) {
+                ok = role.unit(pr, unit, p, q);
+                unit = unit_at(pr, u + pairs);
+            }
+            if (ok && pr.parts > 1) {
+                ok = pass(bars, ++barrier);   // every phase of a barrier is waited for
+                if (!ok) {
+                    give_up(abort, l.flags);
+                    role.land();
+                }
+            }
+            ++barrier;
+        }
+    } else if (warp == 1 && b.ring.rank == 0) {
+        Multiplier<true, 3> role{b.ring, b.tmem};
+        bool ok = true;
+        for (int k = 0; k <= last && ok; ++k) {
+            const Problem pr = l.pr[k % kProducts];
+            for (int u = pair; u < pr.units && ok; u += pairs) ok = role.unit(pr, unit_at(pr, u));
+        }
+        role.finish();
+    } else if (warp == 2) {
+        unsigned count = 0;
+        for (int k = 0; k <= last; ++k) count += (l.pr[k % kProducts].parts > 1 ? 1 : 0) + (k < last ? 1 : 0);
+        if ((threadIdx.x & 31) == 0 && !keep_barriers(bars, l.arrived, count)) give_up(abort, l.flags);
+    } else if (warp >= 4) {
+        Drain<true, false> role(b.ring, b.tmem, b.staging);
+        unsigned barrier = 0;
+        bool ok = true;
+#pragma unroll 1
+        for (int k = 0; k <= last && ok; ++k) {
+            const int kind = k % kProducts, step = k / kProducts;
+            const Problem pr = l.pr[kind];
+            StepEpilogue e{l.f[kind < 2 ? kind : 2 + (1 - (step & 1))], l.parts};
+            if (kind == 1) {
+                e.f.a = l.coeffs[3 * step];
+                e.f.b = l.coeffs[3 * step + 1];
+                e.f.c = l.coeffs[3 * step + 2];
+            }
+            if (k == last) e.f.kind = kResult;
+            ok = k == 0 || pass(bars, barrier);
+#pragma unroll 1
+            for (int u = pair; u < pr.units && ok; u += pairs) ok = role.unit(pr, unit_at(pr, u), e);
+            if (ok && pr.parts > 1) {
+                come(bars);
+                ok = pass(bars, ++barrier);
+                if (ok) e.join(pr, int(blockIdx.x) * kDrain + warp - 4, int(gridDim.x) * kDrain, role.out);
+            }
+            if (ok && k < last) {
+                come(bars);
+                ++barrier;
+            }
+        }
+        if (!ok) give_up(abort, l.flags);
     }
+    end_products<true>(b.tmem);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -349,7 +464,7 @@ Plan plan_of(int64_t batch, int64_t rows, int64_t cols, int64_t K, bool lower, b
 // The workspace, in bytes: sums of squares; X twice, A and Q, each in two matrices; the parts of a split sum.
 struct Layout {
     int64_t m, n, ldx, lda, ctas;
-    int64_t x[2][2], gram[2], q[2], parts, end;
+    int64_t arrived, x[2], gram, q, parts, end;
     Plan plan_gram, plan_q, plan_x;
     Layout(int64_t batch, int64_t rows, int64_t cols) {
         m = std::min(rows, cols);
@@ -363,10 +478,10 @@ struct Layout {
             at += (bytes + 127) / 128 * 128;
             return here;
         };
-        for (auto& pair : x)
-            for (int64_t& half : pair) half = take(batch * m * ldx * 2);
-        for (int64_t& half : gram) half = take(batch * m * lda * 2);
-        for (int64_t& half : q) half = take(batch * m * lda * 2);
+        arrived = take(sizeof(unsigned));
+        for (int64_t& one : x) one = take(batch * m * ldx * 4);   // a half after the other
+        gram = take(batch * m * lda * 4);
+        q = take(batch * m * lda * 4);
         plan_gram = plan_of(batch, m, m, n, true, false);
         plan_q = plan_of(batch, m, m, m, true, false);
         plan_x = plan_of(batch, m, n, m, false, true);
@@ -380,22 +495,41 @@ struct Halves {
     int64_t ld, size;   // from one matrix to the next
 };
 
-// One product of the steps.
-acrl_status step_product(const Plan& plan, const Halves& p, const Halves& q, bool q_turned, const Finish& f, float* parts, int32_t* flags,
-                         cudaStream_t s) {
-    const Shape& sh = plan.shape;
-    ProductLaunch<1, 3, StepEpilogue> l = {};
-    l.pr[0] = problem_of(sh, plan.cut, false, q_turned, false);
-    l.epi[0].f = f;
-    l.epi[0].parts = parts;
-    for (int i = 0; i < 2; ++i) {
-        if (!operand_map(&l.p[0][i], Matrix{i ? p.lo : p.hi, sh.rows, p.ld, false, sh.batch, p.size}, sh.K, kRows) ||
-            !operand_map(&l.q[0][i], Matrix{i ? q.lo : q.hi, sh.cols_all, q.ld, q_turned, sh.batch, q.size}, sh.K, plan.cut.cols / 2))
-            return ACRL_ERR_CUDA;
+// All pairs are resident at once, or the launch is refused: cooperative.  The most that are, of the calling thread's last device.
+int64_t resident_pairs() {
+    static thread_local int known = -1;
+    static thread_local int64_t most = 0;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return 0;
     }
-    const acrl_status st = launch_product<true, false>(l, flags, s);
-    if (st != ACRL_OK || plan.cut.parts == 1) return st;
-    return launch(join_kernel, plan.cut.tiles * (2 * kRows / 32) * (plan.cut.cols / 32), 256, 0, 0, s, f, static_cast<const float*>(parts), l.pr[0]);
+    if (dev == known) return most;
+    if (cudaFuncSetAttribute(steps_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return 0;
+    }
+    most = resident_clusters(reinterpret_cast<const void*>(steps_kernel), kProductThreads, kProductSmem, 2);
+    if (most > 0) known = dev;
+    return most;
+}
+
+acrl_status launch_steps(const StepsLaunch& l, int64_t pairs, cudaStream_t s) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(2 * pairs), 1, 1);
+    cfg.blockDim = dim3(kProductThreads, 1, 1);
+    cfg.dynamicSmemBytes = kProductSmem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeCooperative;
+    attr[0].val.cooperative = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 2;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    (void)cudaLaunchKernelEx(&cfg, steps_kernel, l);
+    return launch_status();
 }
 
 }  // namespace
@@ -440,48 +574,64 @@ extern "C" acrl_status acrl_orthogonalize(const void* g, acrl_dtype g_dtype, int
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     const Layout l(batch, m, n);
     uint8_t* base = static_cast<uint8_t*>(workspace);
-    auto halves_at = [&](const int64_t (&at)[2], int64_t ld) {
-        return Halves{reinterpret_cast<acrl_bf16*>(base + at[0]), reinterpret_cast<acrl_bf16*>(base + at[1]), ld, l.m * ld};
+    auto halves_at = [&](int64_t at, int64_t ld) {
+        acrl_bf16* hi = reinterpret_cast<acrl_bf16*>(base + at);
+        return Halves{hi, hi + batch * l.m * ld, ld, l.m * ld};
     };
     const Halves x[2] = {halves_at(l.x[0], l.ldx), halves_at(l.x[1], l.ldx)}, gram = halves_at(l.gram, l.lda), q = halves_at(l.q, l.lda);
-    float* parts = reinterpret_cast<float*>(base + l.parts);
     double* sums = reinterpret_cast<double*>(base);
-    const Update u{g, g_dtype == ACRL_F32, ldg, g_stride, int(m), int(n)};
-    acrl_status st = launch(squares_kernel, batch * l.ctas, 256, 0, 0, s, u, int(l.ctas), sums);
-    if (st != ACRL_OK) return st;
-    st = launch(first_kernel, batch * l.ctas, 256, 0, 0, s, u, int(l.ctas), static_cast<const double*>(sums), eps, x[0].hi,
-                x[0].lo, l.ldx, x[0].size, dev_flags);
-    for (int i = 0; i < steps && st == ACRL_OK; ++i) {
-        const Halves &from = x[i & 1], &into = x[1 - (i & 1)];
-        Finish f = {};
-        f.kind = kGram;
-        f.hi = gram.hi;
-        f.lo = gram.lo;
-        f.ld = gram.ld;
-        f.size = gram.size;
-        st = step_product(l.plan_gram, from, from, false, f, parts, dev_flags, s);
-        if (st != ACRL_OK) break;
-        f.kind = kPolynomial;
-        f.a = coeffs[3 * i];
-        f.b = coeffs[3 * i + 1];
-        f.c = coeffs[3 * i + 2];
+    StepsLaunch t = {};
+    t.steps = steps;
+    t.parts = reinterpret_cast<float*>(base + l.parts);
+    t.arrived = reinterpret_cast<unsigned*>(base + l.arrived);
+    t.flags = dev_flags;
+    std::copy(coeffs, coeffs + 3 * steps, t.coeffs);
+    const Plan* plans[kProducts] = {&l.plan_gram, &l.plan_q, &l.plan_x};
+    int64_t units = 0;
+    for (int k = 0; k < kProducts; ++k) {
+        const Plan& p = *plans[k];
+        t.pr[k] = problem_of(p.shape, p.cut, false, k == 2, false);
+        t.stage_bytes = std::max(t.stage_bytes, 2 * (kRows + p.cut.cols / 2) * kRowBytes);
+        units = std::max(units, p.cut.units());
+    }
+    t.stages = std::min(kMaxStages, kRingBytes / t.stage_bytes);
+    bool ok = true;
+    auto map = [&](CUtensorMap& to, const Halves& h, int64_t rows, bool turned, int64_t K, int box) {
+        ok = ok && operand_map(&to, Matrix{h.hi, rows, h.ld, turned, batch, h.size, batch * h.size}, K, box);
+    };
+    for (int b = 0; b < 2; ++b) {
+        map(t.x_p[b], x[b], l.m, false, l.n, kRows);
+        map(t.x_q[b], x[b], l.m, false, l.n, l.plan_gram.cut.cols / 2);
+        map(t.x_turned[b], x[b], l.n, true, l.m, kSlab);
+    }
+    map(t.a_p, gram, l.m, false, l.m, kRows);
+    map(t.a_q, gram, l.m, false, l.m, l.plan_q.cut.cols / 2);
+    map(t.q_p, q, l.m, false, l.m, kRows);
+    if (!ok) return ACRL_ERR_CUDA;
+    auto finish = [&](Finish& f, Kind kind, const Halves& to) {
+        f.kind = kind;
+        f.hi = to.hi;
+        f.lo = to.lo;
+        f.ld = to.ld;
+        f.size = to.size;
         f.hi_in = gram.hi;
         f.lo_in = gram.lo;
-        f.hi = q.hi;
-        f.lo = q.lo;
-        st = step_product(l.plan_q, gram, gram, false, f, parts, dev_flags, s);
-        if (st != ACRL_OK) break;
-        f.kind = i + 1 < steps ? kIterate : kResult;
-        f.hi = into.hi;
-        f.lo = into.lo;
-        f.ld = into.ld;
-        f.size = into.size;
         f.scale = scale;
         f.out = out;
         f.ldo = ldo;
         f.out_stride = out_stride;
         f.tall = m > n;
-        st = step_product(l.plan_x, q, from, true, f, parts, dev_flags, s);
-    }
-    return st;
+    };
+    finish(t.f[0], kGram, gram);
+    finish(t.f[1], kPolynomial, q);
+    finish(t.f[2], kIterate, x[0]);
+    finish(t.f[3], kIterate, x[1]);
+    const int64_t most = resident_pairs();
+    if (most < 1) return ACRL_ERR_CUDA;
+    const Update u{g, g_dtype == ACRL_F32, ldg, g_stride, int(m), int(n)};
+    acrl_status st = launch(squares_kernel, batch * l.ctas, 256, 0, 0, s, u, int(l.ctas), sums, t.arrived);
+    if (st == ACRL_OK)
+        st = launch(first_kernel, batch * l.ctas, 256, 0, 0, s, u, int(l.ctas), static_cast<const double*>(sums), eps, x[0].hi, x[0].lo, l.ldx,
+                    x[0].size, dev_flags);
+    return st != ACRL_OK ? st : launch_steps(t, std::min(units, most), s);
 }

@@ -111,6 +111,23 @@ __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, u
             : "memory");
 }
 
+// And of a four-dimensional one, from its first matrix on in the last dimension.
+template <bool PAIR>
+__device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
+    if (PAIR)
+        asm volatile(
+            "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, "
+            "%3, %4, %6}], [%5];" ::"r"(smem_u32(dst)),
+            "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar), "r"(0)
+            : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %6}], [%5];" ::"r"(
+                smem_u32(dst)),
+            "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar), "r"(0)
+            : "memory");
+}
+
 // One lane of a warp that is together.
 __device__ __forceinline__ bool elect_one() {
     uint32_t r;

@@ -39,18 +39,19 @@ inline bool encode_map(CUtensorMap* map, CUtensorMapDataType type, uint32_t byte
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The same of `count` matrices at a stride of `apart` elements: the coordinates are column, row, matrix.
+// The same of `count` matrices at a stride of `apart` elements: the coordinates are column, row, matrix.  With `halves` > 0
+// there are two such lots, so many elements from one another, and a box has as much of each: column, row, matrix, 0.
 inline bool encode_map_3d(CUtensorMap* map, CUtensorMapDataType type, uint32_t bytes, const void* ptr, uint64_t count, uint64_t rows,
-                          uint64_t cols, uint64_t ld, uint64_t apart, uint32_t box_rows, uint32_t box_cols,
+                          uint64_t cols, uint64_t ld, uint64_t apart, uint64_t halves, uint32_t box_rows, uint32_t box_cols,
                           CUtensorMapSwizzle swizzle) {
     const PFN_cuTensorMapEncodeTiled_v12000 encode = map_encoder();
     if (encode == nullptr) return false;
-    const cuuint64_t dims[3] = {cols, rows, count};
-    const cuuint64_t strides[2] = {ld * bytes, apart * bytes};
-    const cuuint32_t box[3] = {box_cols, box_rows, 1};
-    const cuuint32_t estr[3] = {1, 1, 1};
-    return encode(map, type, 3, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
-                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const cuuint64_t dims[4] = {cols, rows, count, 2};
+    const cuuint64_t strides[3] = {ld * bytes, apart * bytes, halves * bytes};
+    const cuuint32_t box[4] = {box_cols, box_rows, 1, 2};
+    const cuuint32_t estr[4] = {1, 1, 1, 1};
+    return encode(map, type, halves > 0 ? 4 : 3, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // True when every pointer is device memory of the current device: not managed
