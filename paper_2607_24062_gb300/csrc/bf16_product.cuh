@@ -60,8 +60,10 @@ struct ProductBarriers {
     uint64_t tfull[2];            // an accumulator is complete
     uint64_t tempty[2];           // the epilogue warps (pair: of both CTAs, on the even one) have read it
     uint64_t mma_done;
-    uint64_t written;             // the epilogue warps have written what they had of a product
-    uint64_t passed;              // and so have all CTAs' of the grid
+    // for kernels whose CTAs wait for one another:
+    uint64_t written[2];          // the epilogue warps have written a unit, by its accumulator
+    uint64_t passed;              // all CTAs have written their parts of sums
+    uint64_t joined;              // the epilogue warps have joined theirs
     uint32_t tmem_base;
     int32_t abort;
 };
@@ -75,7 +77,7 @@ struct Problem {
     int p_tiles, q_tiles;
     int parts, per;          // of the sum, of so many slabs
     int run;                 // slabs that one accumulator takes
-    int lower;               // tiles that lie above the diagonal's are left out: the result is symmetric
+    int lower;               // p and q are the same, the result symmetric: tiles above the diagonal's are left out
     int p_turned, q_turned;  // the operand lies with the sum along its columns
     uint32_t idesc;
     int tiles, units;        // tiles of one matrix; parts of all
@@ -101,6 +103,12 @@ struct ProductLaunch {
     int stages, stage_bytes;
     int32_t* flags;
 };
+
+// A tile of 256 x 256 on a symmetric result's diagonal: a CTA's rows of p are its share of q as well, and are loaded once (10 %
+// of all loads where there are four tiles to a side; of L2's bandwidth, which bounds 24 x 1,024 x 1,024).
+__device__ __forceinline__ bool on_diagonal(const Problem& pr, const Unit& t) {
+    return pr.lower && pr.cols == 2 * kRows && t.tp == t.tq;
+}
 
 // Tiles in bands of kBand row tiles, all column tiles of a band in turn, so that the tiles in flight share operands in L2.
 constexpr int kBand = 16;
@@ -207,7 +215,8 @@ struct Producer {
         ProductBarriers* bars = ring.bars;
         volatile int32_t* abort = &bars->abort;
         const int q_rows = PAIR ? pr.cols / 2 : pr.cols, q_bytes = q_rows * kRowBytes;
-        const int bytes = kMats * (kRows * kRowBytes + q_bytes);
+        const bool once = PAIR && on_diagonal(pr, t);
+        const int bytes = kMats * (kRows * kRowBytes + (once ? 0 : q_bytes));
         const int p0 = (PAIR ? 2 * t.tp + int(ring.rank) : t.tp) * kRows;
         const int q0 = t.tq * pr.cols + (PAIR ? int(ring.rank) * q_rows : 0);
         const bool p_turned = pr.p_turned, q_turned = pr.q_turned;
@@ -231,7 +240,7 @@ struct Producer {
                     }
                 };
                 copy(s, p, p_turned, p0, kRows);
-                copy(s + kMats * kRows * kRowBytes, q, q_turned, q0, q_rows);
+                if (!once) copy(s + kMats * kRows * kRowBytes, q, q_turned, q0, q_rows);
             }
             ++issued;
             if (++stage == ring.stages) {
@@ -268,7 +277,7 @@ struct Multiplier {
         volatile int32_t* abort = &bars->abort;
         const uint32_t base = smem_u32(ring.at), units = uint32_t(ring.stage_bytes) >> 4;   // of a stage, in descriptors
         const uint64_t pdesc0 = tile_desc<kMats>(base, pr.p_turned);
-        const uint64_t qdesc0 = tile_desc<kMats>(base + kMats * kRows * kRowBytes, pr.q_turned);
+        const uint64_t qdesc0 = PAIR && on_diagonal(pr, t) ? pdesc0 : tile_desc<kMats>(base + kMats * kRows * kRowBytes, pr.q_turned);
         // from one K = 16 to the next: 32 bytes of a row, or sixteen rows
         const uint32_t pstep = pr.p_turned ? 16 * kRowBytes >> 4 : 2, qstep = pr.q_turned ? 16 * kRowBytes >> 4 : 2;
         // from a half to the other
@@ -634,8 +643,9 @@ __device__ __forceinline__ Begun begin_products(uint8_t* smem, int stages, int s
             mbar_init(&bars->tempty[b], (PAIR ? 2 : 1) * kDrain);
         }
         mbar_init(&bars->mma_done, 1);
-        mbar_init(&bars->written, kDrain);
+        for (int b = 0; b < 2; ++b) mbar_init(&bars->written[b], kDrain);
         mbar_init(&bars->passed, 1);
+        mbar_init(&bars->joined, kDrain);
         bars->abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(p)) : "memory");

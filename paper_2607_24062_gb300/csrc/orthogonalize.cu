@@ -6,9 +6,11 @@
 // symmetric: tiles above the diagonal are left out and written as mirror images, 3 m^2 n + m^3 multiply-adds a step where the
 // plain products have 4 m^2 n + 2 m^3.
 //
-// All steps are one cooperative launch: CTA pairs, one CTA an SM, go through the products of all steps, and wait for one
-// another between them on a counter in the workspace (each wait is bounded in time).  Launched one by one, each product of a
-// small matrix spent more on its launch, on tensor memory and on first copies than on its sums.
+// All steps are one cooperative launch: CTA pairs, one CTA an SM, go through the tiles of all products of all steps, in one
+// order, every pairs-th.  A tile of a product waits until its matrix's product before is written: a counter for each matrix says
+// how far it is (each wait is bounded in time).  So the matrices of a batch run into one another, and neither a part-filled round
+// nor the last tiles' stores hold up the next product: 24 x 1,024 x 1,024, launched product by product, 1,290 us; with a barrier of
+// the grid between them 1,274.
 //
 // Operands are two bf16 numbers each, x = x0 + x1 with x0 the rounding of x and x1 that of what is left, which together are
 // within 2^-16 of it, and a product is three of the tensor cores' (bf16_product.cuh).  One bf16 number would not do: gradients
@@ -90,12 +92,12 @@ __device__ __forceinline__ void load8(const Update& u, int64_t row, int c, float
     }
 }
 
-// Partial sums of a matrix's squares, `ctas` of them.  HBM bounds it.  It also clears the counter of the steps' waits.
-__global__ void __launch_bounds__(256) squares_kernel(Update u, int ctas, double* sums, unsigned* arrived) {
+// Partial sums of a matrix's squares, `ctas` of them.  HBM bounds it.  It also clears the matrix's counter.
+__global__ void __launch_bounds__(256) squares_kernel(Update u, int ctas, double* sums, unsigned* done) {
     __shared__ double part[8];
     grid_begin();
-    if (blockIdx.x == 0 && threadIdx.x == 0) *arrived = 0;
     const int b = int(blockIdx.x) / ctas, lane = threadIdx.x & 31;
+    if (int(blockIdx.x) == b * ctas && threadIdx.x == 0) done[b] = 0;
     Squares s;
     Pieces p(u, int(blockIdx.x) - b * ctas, ctas);
     for (; p.at < p.all; p.at += p.step) {
@@ -227,8 +229,8 @@ __device__ __forceinline__ void polynomial(const Finish& f, int z, int i, int j,
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const int64_t at = row + (j + 8 * k < f.ld ? j + 8 * k : 0);   // ld is a multiple of eight
-        h[k] = *reinterpret_cast<const uint4*>(f.hi_in + at);
-        l[k] = *reinterpret_cast<const uint4*>(f.lo_in + at);
+        h[k] = __ldcg(reinterpret_cast<const uint4*>(f.hi_in + at));
+        l[k] = __ldcg(reinterpret_cast<const uint4*>(f.lo_in + at));
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -306,7 +308,7 @@ struct StepEpilogue {
             const float* p = parts + t.all * pr.parts * size + int64_t(r) * pr.cols + c + out.lane;
             for (int j = 0; j < pr.parts; ++j)
 #pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] += p[j * size + i * pr.cols];
+                for (int i = 0; i < 32; ++i) v[i] += __ldcg(p + j * size + i * pr.cols);
             finish(pr, t, v, row0, col0, pr.rows, pr.cols_all, true, out);
         }
     }
@@ -323,44 +325,73 @@ struct StepsLaunch {
     float coeffs[3 * kMostSteps];
     int steps;
     float* parts;
-    unsigned* arrived;                // CTAs, of all waits so far
+    unsigned* done;                   // CTAs' units written so far, of each matrix; with parts, of all
+    int each;                         // a counter for each matrix
     int stages, stage_bytes;
     int32_t* flags;
 };
 
-// The grid's barriers between the products, and between a split sum's parts and their join.  The epilogue warps come to the
-// CTA's barrier `written`; a warp of its own then tells the grid, waits until every CTA has told it as often, and lets the CTA go
-// on at `passed`.  One thread a CTA looks at the counter: nine warps of each did at first, and 20 barriers took 68 us more than
-// as many launches (2,051 x 1,000).
-// A warp that goes on reads what all the others wrote; and it comes to no barrier before it has passed the one before, or its
-// arrival would be counted for another's.
-__device__ __forceinline__ void come(ProductBarriers* bars) {
-    __syncwarp();
-    if ((threadIdx.x & 31) == 0) mbar_arrive(&bars->written);
-}
-__device__ __forceinline__ bool pass(ProductBarriers* bars, unsigned count) {   // barrier number `count`, from 1 on
-    return warp_wait(&bars->passed, (count - 1) & 1u, &bars->abort);
+// Where a role is among the products: their units in order, every pairs-th.
+struct Place {
+    const StepsLaunch& l;
+    int k = 0, pair, pairs, last;
+    int offset = 0;          // units of the products before, modulo the pairs
+    unsigned before = 0;     // of a counter: what the products before add up to
+    __device__ explicit Place(const StepsLaunch& launch) : l(launch) {
+        pair = int(blockIdx.x >> 1);
+        pairs = int(gridDim.x >> 1);
+        last = kProducts * l.steps - 1;
+    }
+    __device__ __forceinline__ bool more() const { return k <= last; }
+    __device__ __forceinline__ int kind() const { return k % kProducts; }
+    __device__ __forceinline__ int step() const { return k / kProducts; }
+    __device__ __forceinline__ int first() const { return pair >= offset ? pair - offset : pair - offset + pairs; }
+    // This product's units add up to this much: two CTAs each.
+    __device__ __forceinline__ unsigned units(const Problem& pr) const { return 2u * unsigned(l.each ? pr.tiles : pr.units); }
+    __device__ __forceinline__ void next(const Problem& pr) {
+        before += units(pr) + (pr.parts > 1 ? gridDim.x : 0u);
+        offset = (offset + pr.units) % pairs;
+        ++k;
+    }
+};
+
+// Until `counter` has come to `want`: what was written before it did is visible then.  False after the time limit, or once the
+// CTA has given up.
+__device__ __forceinline__ bool wait_done(const unsigned* counter, unsigned want, volatile int32_t* abort) {
+    uint64_t t0 = 0;
+    for (uint32_t i = 0;; ++i) {
+        unsigned n;
+        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(n) : "l"(counter) : "memory");
+        if (int(n - want) >= 0) return true;
+        if ((i & 63u) == 63u) {
+            if (t0 == 0) t0 = global_ns();
+            if (*abort || global_ns() - t0 > kWaitNs) return false;
+        }
+    }
 }
 
-// One thread's part of barriers 1 to `count`.
-__device__ bool keep_barriers(ProductBarriers* bars, unsigned* arrived, unsigned count) {
+// One thread tells the matrices' counters what the CTA has written.  Where sums are split it also waits for everyone's parts, lets
+// the epilogue warps join them, and tells of that.
+__device__ bool keep_counters(const StepsLaunch& l, ProductBarriers* bars) {
     volatile int32_t* abort = &bars->abort;
-    for (unsigned k = 1; k <= count; ++k) {
-        if (!wait_phase(&bars->written, (k - 1) & 1u, abort)) return false;
+    auto tell = [&](unsigned* counter) {
         __threadfence();
-        asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(arrived) : "memory");
-        const unsigned want = k * gridDim.x;
-        uint64_t t0 = 0;
-        for (uint32_t i = 0;; ++i) {
-            unsigned n;
-            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(n) : "l"(arrived) : "memory");
-            if (int(n - want) >= 0) break;
-            if ((i & 63u) == 63u) {
-                if (t0 == 0) t0 = global_ns();
-                if (*abort || global_ns() - t0 > kWaitNs) return false;
-            }
+        asm volatile("red.relaxed.gpu.global.add.u32 [%0], 1;" ::"l"(counter) : "memory");
+    };
+    unsigned n = 0, joins = 0;
+    for (Place at(l); at.more();) {
+        const Problem pr = l.pr[at.kind()];
+        for (int u = at.first(); u < pr.units; u += at.pairs, ++n) {
+            if (!wait_phase(&bars->written[n & 1u], (n >> 1) & 1u, abort)) return false;
+            tell(l.done + (l.each ? u / pr.tiles : 0));
         }
-        mbar_arrive(&bars->passed);
+        if (pr.parts > 1) {
+            if (!wait_done(l.done, at.before + at.units(pr), abort)) return false;
+            mbar_arrive(&bars->passed);
+            if (!wait_phase(&bars->joined, joins++ & 1u, abort)) return false;
+            tell(l.done);
+        }
+        at.next(pr);
     }
     return true;
 }
@@ -368,79 +399,84 @@ __device__ bool keep_barriers(ProductBarriers* bars, unsigned* arrived, unsigned
 __global__ void __launch_bounds__(kProductThreads, 1) steps_kernel(const __grid_constant__ StepsLaunch l) {
     extern __shared__ uint8_t smem_raw[];
     const Begun b = begin_products<true>(smem_raw, l.stages, l.stage_bytes, &l.x_p[0], &l.x_q[0], l.flags);
-    const int warp = threadIdx.x >> 5, pair = int(blockIdx.x >> 1), pairs = int(gridDim.x >> 1), last = kProducts * l.steps - 1;
+    const int warp = threadIdx.x >> 5;
     ProductBarriers* bars = b.ring.bars;
     volatile int32_t* abort = &bars->abort;
+    bool ok = true;
     if (warp == 0) {
         Producer<true, 3> role{b.ring};
-        unsigned barrier = 0;
-        bool ok = true;
-        for (int k = 0; k <= last && ok; ++k) {
-            const int kind = k % kProducts, x = (k / kProducts) & 1;
-            const Problem pr = l.pr[kind];
+        for (Place at(l); at.more() && ok;) {
+            const Problem pr = l.pr[at.kind()];
+            const int kind = at.kind(), x = at.step() & 1;
             const CUtensorMap* p = kind == 0 ? &l.x_p[x] : kind == 1 ? &l.a_p : &l.q_p;
             const CUtensorMap* q = kind == 0 ? &l.x_q[x] : kind == 1 ? &l.a_q : &l.x_turned[x];
-            Unit unit = unit_at(pr, pair);   // before the wait
-            if (k > 0 && !pass(bars, barrier)) {
-                give_up(abort, l.flags);
-                role.land();
-                break;
-            }
-            asm volatile("fence.proxy.async;" ::: "memory");   // copies read what others' stores have written
-            for (int u = pair; u < pr.units && ok; u += pairs) {
-                ok = role.unit(pr, unit, p, q);
-                unit = unit_at(pr, u + pairs);
-            }
-            if (ok && pr.parts > 1) {
-                ok = pass(bars, ++barrier);   // every phase of a barrier is waited for
-                if (!ok) {
-                    give_up(abort, l.flags);
-                    role.land();
+            int known = -1;   // the matrix whose product before is written
+            for (int u = at.first(); u < pr.units && ok; u += at.pairs) {
+                const Unit t = unit_at(pr, u);
+                const int z = l.each ? t.z : 0;
+                if (z != known) {
+                    known = z;
+                    ok = __all_sync(0xffffffffu, (threadIdx.x & 31) != 0 || wait_done(l.done + z, at.before, abort));
+                    if (!ok) {
+                        give_up(abort, l.flags);
+                        role.land();
+                        break;
+                    }
+                    asm volatile("fence.proxy.async;" ::: "memory");   // copies read what others' stores have written
                 }
+                ok = role.unit(pr, t, p, q);
             }
-            ++barrier;
+            at.next(pr);
         }
     } else if (warp == 1 && b.ring.rank == 0) {
         Multiplier<true, 3> role{b.ring, b.tmem};
-        bool ok = true;
-        for (int k = 0; k <= last && ok; ++k) {
-            const Problem pr = l.pr[k % kProducts];
-            for (int u = pair; u < pr.units && ok; u += pairs) ok = role.unit(pr, unit_at(pr, u));
+        for (Place at(l); at.more() && ok;) {
+            const Problem pr = l.pr[at.kind()];
+            for (int u = at.first(); u < pr.units && ok; u += at.pairs) ok = role.unit(pr, unit_at(pr, u));
+            at.next(pr);
         }
         role.finish();
     } else if (warp == 2) {
-        unsigned count = 0;
-        for (int k = 0; k <= last; ++k) count += (l.pr[k % kProducts].parts > 1 ? 1 : 0) + (k < last ? 1 : 0);
-        if ((threadIdx.x & 31) == 0 && !keep_barriers(bars, l.arrived, count)) give_up(abort, l.flags);
+        if ((threadIdx.x & 31) == 0 && !keep_counters(l, bars)) give_up(abort, l.flags);
     } else if (warp >= 4) {
         Drain<true, false> role(b.ring, b.tmem, b.staging);
-        unsigned barrier = 0;
-        bool ok = true;
+        unsigned n = 0, joins = 0;
+        auto come = [&](uint64_t* bar) {
+            __syncwarp();
+            if (role.lane == 0) mbar_arrive(bar);
+        };
+        // A warp that has read out an accumulator may still be storing when another is two units on, and comes to the same barrier.
+        auto come_in_turn = [&] {
+            uint64_t* bar = &bars->written[n & 1u];
+            if (n >= 2 && !warp_wait(bar, ((n - 2) >> 1) & 1u, abort)) return false;
+            come(bar);
+            ++n;
+            return true;
+        };
 #pragma unroll 1
-        for (int k = 0; k <= last && ok; ++k) {
-            const int kind = k % kProducts, step = k / kProducts;
-            const Problem pr = l.pr[kind];
-            StepEpilogue e{l.f[kind < 2 ? kind : 2 + (1 - (step & 1))], l.parts};
-            if (kind == 1) {
-                e.f.a = l.coeffs[3 * step];
-                e.f.b = l.coeffs[3 * step + 1];
-                e.f.c = l.coeffs[3 * step + 2];
+        for (Place at(l); at.more() && ok;) {
+            const Problem pr = l.pr[at.kind()];
+            StepEpilogue e{l.f[at.kind() < 2 ? at.kind() : 2 + (1 - (at.step() & 1))], l.parts};
+            if (at.kind() == 1) {
+                e.f.a = l.coeffs[3 * at.step()];
+                e.f.b = l.coeffs[3 * at.step() + 1];
+                e.f.c = l.coeffs[3 * at.step() + 2];
             }
-            if (k == last) e.f.kind = kResult;
-            ok = k == 0 || pass(bars, barrier);
+            if (at.k == at.last) e.f.kind = kResult;
 #pragma unroll 1
-            for (int u = pair; u < pr.units && ok; u += pairs) ok = role.unit(pr, unit_at(pr, u), e);
-            if (ok && pr.parts > 1) {
-                come(bars);
-                ok = pass(bars, ++barrier);
-                if (ok) e.join(pr, int(blockIdx.x) * kDrain + warp - 4, int(gridDim.x) * kDrain, role.out);
+            for (int u = at.first(); u < pr.units && ok; u += at.pairs) {
+                ok = role.unit(pr, unit_at(pr, u), e) && come_in_turn();
             }
-            if (ok && k < last) {
-                come(bars);
-                ++barrier;
+            if (pr.parts > 1 && ok) {
+                ok = warp_wait(&bars->passed, joins++ & 1u, abort);
+                if (!ok) give_up(abort, l.flags);
+                else {
+                    e.join(pr, int(blockIdx.x) * kDrain + warp - 4, int(gridDim.x) * kDrain, role.out);
+                    come(&bars->joined);
+                }
             }
+            at.next(pr);
         }
-        if (!ok) give_up(abort, l.flags);
     }
     end_products<true>(b.tmem);
 }
@@ -464,7 +500,7 @@ Plan plan_of(int64_t batch, int64_t rows, int64_t cols, int64_t K, bool lower, b
 // The workspace, in bytes: sums of squares; X twice, A and Q, each in two matrices; the parts of a split sum.
 struct Layout {
     int64_t m, n, ldx, lda, ctas;
-    int64_t arrived, x[2], gram, q, parts, end;
+    int64_t done, x[2], gram, q, parts, end;
     Plan plan_gram, plan_q, plan_x;
     Layout(int64_t batch, int64_t rows, int64_t cols) {
         m = std::min(rows, cols);
@@ -478,7 +514,7 @@ struct Layout {
             at += (bytes + 127) / 128 * 128;
             return here;
         };
-        arrived = take(sizeof(unsigned));
+        done = take(batch * 4);
         for (int64_t& one : x) one = take(batch * m * ldx * 4);   // a half after the other
         gram = take(batch * m * lda * 4);
         q = take(batch * m * lda * 4);
@@ -583,7 +619,8 @@ extern "C" acrl_status acrl_orthogonalize(const void* g, acrl_dtype g_dtype, int
     StepsLaunch t = {};
     t.steps = steps;
     t.parts = reinterpret_cast<float*>(base + l.parts);
-    t.arrived = reinterpret_cast<unsigned*>(base + l.arrived);
+    t.done = reinterpret_cast<unsigned*>(base + l.done);
+    t.each = 1;
     t.flags = dev_flags;
     std::copy(coeffs, coeffs + 3 * steps, t.coeffs);
     const Plan* plans[kProducts] = {&l.plan_gram, &l.plan_q, &l.plan_x};
@@ -593,6 +630,7 @@ extern "C" acrl_status acrl_orthogonalize(const void* g, acrl_dtype g_dtype, int
         t.pr[k] = problem_of(p.shape, p.cut, false, k == 2, false);
         t.stage_bytes = std::max(t.stage_bytes, 2 * (kRows + p.cut.cols / 2) * kRowBytes);
         units = std::max(units, p.cut.units());
+        if (p.cut.parts > 1) t.each = 0;   // parts are of all matrices at once
     }
     t.stages = std::min(kMaxStages, kRingBytes / t.stage_bytes);
     bool ok = true;
@@ -629,7 +667,7 @@ extern "C" acrl_status acrl_orthogonalize(const void* g, acrl_dtype g_dtype, int
     const int64_t most = resident_pairs();
     if (most < 1) return ACRL_ERR_CUDA;
     const Update u{g, g_dtype == ACRL_F32, ldg, g_stride, int(m), int(n)};
-    acrl_status st = launch(squares_kernel, batch * l.ctas, 256, 0, 0, s, u, int(l.ctas), sums, t.arrived);
+    acrl_status st = launch(squares_kernel, batch * l.ctas, 256, 0, 0, s, u, int(l.ctas), sums, t.done);
     if (st == ACRL_OK)
         st = launch(first_kernel, batch * l.ctas, 256, 0, 0, s, u, int(l.ctas), static_cast<const double*>(sums), eps, x[0].hi, x[0].lo, l.ldx,
                     x[0].size, dev_flags);
