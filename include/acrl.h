@@ -723,12 +723,12 @@ acrl_status acrl_linear_backward(const acrl_bf16* dy, int64_t M, int64_t N, int6
  * of a product is held as two bf16 numbers, to 2^-16 of it, and each product as three
  * of theirs: in bf16 alone the roundings of a gradient's few strong directions would
  * drown the weak ones, which the steps amplify by up to a^steps.
- *   g     device bf16 or float: `batch` matrices of m x n, rows at a stride of ldg
- *         (a multiple of 8 for bf16, 4 for float; 16-byte aligned), matrices at a
- *         stride of g_stride elements (likewise).
+ *   g     device bf16 or float: `batch` matrices of m x n, rows at a stride of ldg,
+ *         matrices at a stride of g_stride elements; of any alignment of its type
+ *         (16 bytes, and strides that keep them, are read fastest).
  *   coeffs  host float [3 steps]: a, b, c of each step.  1 <= steps <= 64.
  *   eps >= 0.  A matrix of zeros gives zeros, eps = 0 included.
- *   out   device bf16, rows at ldo, matrices at out_stride; it may be g.
+ *   out   device bf16, rows at ldo, matrices at out_stride, likewise; it may be g.
  *   workspace  device, 16-byte aligned, acrl_orthogonalize_workspace_bytes(batch,
  *         m, n) bytes.
  * A matrix with an infinity or a NaN is NaN throughout and raises NONFINITE; the

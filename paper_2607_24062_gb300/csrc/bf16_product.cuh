@@ -349,10 +349,10 @@ struct WarpOut {
     uint8_t* staging;
     int lane;
 
-    // What was staged, 32 rows of T at `at` and on, to rows row0 .. and columns col0 .. of a matrix of rows x cols at a stride
-    // of ld.  Every lane of the warp.
+    // What was staged, 32 rows of T, to rows row0 .. and columns col0 .. of a matrix of rows x cols at a stride of ld.  Every lane
+    // of the warp.  `wide`: the pieces start on 16 bytes.
     template <typename T>
-    __device__ __forceinline__ void send(T* to, int64_t ld, int rows, int cols, int row0, int col0) const {
+    __device__ __forceinline__ void send(T* to, int64_t ld, int rows, int cols, int row0, int col0, bool wide) const {
         constexpr int kPieces = 32 * int(sizeof(T)) / 16, kEach = 16 / int(sizeof(T)), kRowsAtOnce = 32 / kPieces;
         const uint32_t base = smem_u32(staging);
         __syncwarp();
@@ -366,7 +366,7 @@ struct WarpOut {
         }
         T* p = to + (row0 + r0) * ld + c;
         const int64_t step = kRowsAtOnce * ld;
-        if (c + kEach <= cols) {
+        if (c + kEach <= cols && wide) {
 #pragma unroll
             for (int i = 0; i < kPieces; ++i)
                 if (row0 + r0 + i * kRowsAtOnce < rows)
@@ -384,9 +384,10 @@ struct WarpOut {
         __syncwarp();   // the block may be written again
     }
 
-    // Lane i has row row0 + i and its columns col0 .. col0 + 31; ld is a multiple of a piece.
+    // Lane i has row row0 + i and its columns col0 .. col0 + 31.
     template <typename T>
-    __device__ __forceinline__ void store(T* to, int64_t ld, int rows, int cols, const float (&v)[32], int row0, int col0) const {
+    __device__ __forceinline__ void store(T* to, int64_t ld, int rows, int cols, const float (&v)[32], int row0, int col0,
+                                          bool wide = true) const {
         constexpr int kPieces = 32 * int(sizeof(T)) / 16;
         const uint32_t swz = kPieces == 4 ? uint32_t((lane >> 1) & 3) : uint32_t(lane & 7);
         const uint32_t at = smem_u32(staging) + uint32_t(lane * 32 * int(sizeof(T)));
@@ -401,7 +402,7 @@ struct WarpOut {
                                __float_as_uint(v[4 * k + 3]));
             st_shared16(at + ((uint32_t(k) ^ swz) << 4), x);
         }
-        send(to, ld, rows, cols, row0, col0);
+        send(to, ld, rows, cols, row0, col0, wide);
     }
 
     // The values as two bf16 numbers each, h their roundings and l those of what is left, to two matrices; as store, or turned:
@@ -480,7 +481,7 @@ struct WarpOut {
 
     // The same values turned, rounded to bf16: lane i has column col0 + i and its rows row0 .. row0 + 31.
     __device__ __forceinline__ void store_turned(acrl_bf16* to, int64_t ld, int rows, int cols, const float (&v)[32], int row0,
-                                                 int col0) const {
+                                                 int col0, bool wide) const {
         const uint32_t at = smem_u32(staging) + uint32_t((lane & 7) * 2);
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
@@ -489,7 +490,7 @@ struct WarpOut {
                          "h"(acrl_bf16(pack_bf16x2(v[j], 0.f) & 0xffffu))
                          : "memory");
         }
-        send(to, ld, rows, cols, row0, col0);
+        send(to, ld, rows, cols, row0, col0, wide);
     }
 };
 

@@ -31,7 +31,7 @@ constexpr int kSumCtas = 608;      // four of an SM's: CTAs that add up squares
 
 struct Update {
     const void* g;
-    bool f32;
+    bool f32, wide;        // wide: every eighth of a row's numbers starts on 16 bytes
     int64_t ld, stride;
     int m, n;              // as given
 };
@@ -74,7 +74,7 @@ struct Pieces {
 
 // Eight of a row's numbers from column c on, zeros beyond its end.
 __device__ __forceinline__ void load8(const Update& u, int64_t row, int c, float (&v)[8]) {
-    if (c + 8 > u.n) {
+    if (c + 8 > u.n || !u.wide) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = c + j < u.n ? load_float(u.g, u.f32, row + c + j) : 0.f;
     } else if (u.f32) {
@@ -216,7 +216,7 @@ struct Finish {
     int64_t ld, size;                  // of all of these, and from one matrix to the next
     acrl_bf16* out;                    // the result
     int64_t ldo, out_stride;
-    bool tall;                         // the result is turned back
+    bool tall, wide;                   // the result is turned back; every eighth of its numbers starts on 16 bytes
 };
 
 // a I + b A + c v at row i, columns j .. j + 31; what is beyond the matrix is left out of the result.  A row's 64 bytes of each
@@ -256,8 +256,8 @@ struct StepEpilogue {
             acrl_bf16* to = f.out + t.z * f.out_stride;
             // of the matrix, or of its transpose
             const int R = f.tall ? cols : rows, C = f.tall ? rows : cols, r = f.tall ? col0 : row0, c = f.tall ? row0 : col0;
-            if (turned != f.tall) out.store_turned(to, f.ldo, R, C, v, r, c);
-            else out.store(to, f.ldo, R, C, v, r, c);
+            if (turned != f.tall) out.store_turned(to, f.ldo, R, C, v, r, c, f.wide);
+            else out.store(to, f.ldo, R, C, v, r, c, f.wide);
             return;
         }
         if (f.kind == kPolynomial)   // A is symmetric: its column is its row
@@ -601,9 +601,8 @@ extern "C" acrl_status acrl_orthogonalize(const void* g, acrl_dtype g_dtype, int
     if (workspace_bytes < acrl_orthogonalize_workspace_bytes(batch, m, n)) return ACRL_ERR_INVALID_ARG;
     if (batch == 0 || m == 0 || n == 0) return ACRL_OK;
     if (!blocks_ok(batch, m, n)) return ACRL_ERR_INVALID_ARG;
-    const int64_t to = g_dtype == ACRL_BF16 ? 7 : 3;
-    if (!g || !aligned16(g) || ldg < n || (ldg & to) || (g_stride & to) || !out || !aligned16(out) || ldo < n || (ldo & 7) ||
-        (out_stride & 7) || !workspace || !aligned16(workspace))
+    if (!g || (reinterpret_cast<uintptr_t>(g) & (g_dtype == ACRL_BF16 ? 1 : 3)) || ldg < n || !out ||
+        (reinterpret_cast<uintptr_t>(out) & 1) || ldo < n || !workspace || !aligned16(workspace))
         return ACRL_ERR_INVALID_ARG;
     if (batch > 1 && (g_stride < (m - 1) * ldg + n || out_stride < (m - 1) * ldo + n)) return ACRL_ERR_INVALID_ARG;
     if (!operands_on_current_device({g, out, workspace})) return ACRL_ERR_INVALID_ARG;
@@ -659,6 +658,7 @@ extern "C" acrl_status acrl_orthogonalize(const void* g, acrl_dtype g_dtype, int
         f.ldo = ldo;
         f.out_stride = out_stride;
         f.tall = m > n;
+        f.wide = aligned16(out) && (ldo & 7) == 0 && (batch == 1 || (out_stride & 7) == 0);
     };
     finish(t.f[0], kGram, gram);
     finish(t.f[1], kPolynomial, q);
@@ -666,7 +666,9 @@ extern "C" acrl_status acrl_orthogonalize(const void* g, acrl_dtype g_dtype, int
     finish(t.f[3], kIterate, x[1]);
     const int64_t most = resident_pairs();
     if (most < 1) return ACRL_ERR_CUDA;
-    const Update u{g, g_dtype == ACRL_F32, ldg, g_stride, int(m), int(n)};
+    const int64_t to = g_dtype == ACRL_BF16 ? 7 : 3;
+    const bool wide = aligned16(g) && (ldg & to) == 0 && (batch == 1 || (g_stride & to) == 0);
+    const Update u{g, g_dtype == ACRL_F32, wide, ldg, g_stride, int(m), int(n)};
     acrl_status st = launch(squares_kernel, batch * l.ctas, 256, 0, 0, s, u, int(l.ctas), sums, t.done);
     if (st == ACRL_OK)
         st = launch(first_kernel, batch * l.ctas, 256, 0, 0, s, u, int(l.ctas), static_cast<const double*>(sums), eps, x[0].hi, x[0].lo, l.ldx,

@@ -77,9 +77,8 @@ def test_orthogonalize(L):
     ok = dict(g=FAKE, t=1, B=2, m=24, n=40, ldg=40, gs=24 * 40, c=of(*[3.4445, -4.775, 2.0315] * 5), steps=5, eps=1e-7, scale=1.0,
               out=FAKE, ldo=40, os=24 * 40, ws=FAKE, bytes=n, flags=None, stream=None)
     for bad in ({}, dict(g=None), dict(out=None), dict(ws=None), dict(c=None), dict(t=2), dict(B=-1), dict(m=-1), dict(n=-1),
-                dict(m=1 << 31), dict(n=1 << 31), dict(ldg=36), dict(ldg=42), dict(t=0, ldg=44), dict(gs=24 * 40 - 4),
-                dict(gs=24 * 40 + 2), dict(ldo=32), dict(ldo=44), dict(os=24 * 40 - 8), dict(os=24 * 40 + 4), dict(g=FAKE + 4),
-                dict(out=FAKE + 8), dict(ws=FAKE + 8), dict(bytes=n - 1), dict(steps=0), dict(steps=65), dict(eps=-1.0),
+                dict(m=1 << 31), dict(n=1 << 31), dict(ldg=36), dict(gs=24 * 40 - 4), dict(ldo=32), dict(os=24 * 40 - 8),
+                dict(g=FAKE + 2), dict(t=0, g=FAKE + 1), dict(out=FAKE + 1), dict(ws=FAKE + 8), dict(bytes=n - 1), dict(steps=0), dict(steps=65), dict(eps=-1.0),
                 dict(eps=float("inf")), dict(scale=float("nan")), dict(c=of(*[3.4445, -4.775, float("inf")] * 5))):
         assert _call(L.acrl_orthogonalize, ok, **bad) == E, bad
     for none in (dict(B=0), dict(m=0), dict(n=0)):
