@@ -8,6 +8,7 @@ library's kernels."""
 from __future__ import annotations
 
 import ctypes
+import functools
 from dataclasses import dataclass
 
 import numpy as np
@@ -721,6 +722,20 @@ def _given(t, M: int, N: int, dtypes, name: str):
     return t.stride(0) if M > 1 and N > 0 else (N + 7) // 8 * 8
 
 
+def _result(out, M: int, N: int, dtype, dev):
+    """_product_out, a new matrix without the view that cuts its padding off: the last row ends with its columns."""
+    if out is not None:
+        return _product_out(out, M, N, dtype, dev)
+    ld = (N + 7) // 8 * 8
+    return torch.empty_strided((M, N), (ld, 1), dtype=dtype, device=dev), ld
+
+
+@functools.lru_cache(maxsize=256)
+def _size_of(name: str, *sizes: int) -> int:
+    """What a *_workspace_bytes entry point says, by its sizes alone."""
+    return int(getattr(lib(), name)(*sizes))
+
+
 def _workspace(workspace, n: int, dev):
     if workspace is not None:
         return _need(workspace, torch.uint8, n, "workspace")
@@ -760,8 +775,8 @@ def linear(x, weight, bias=None, *, act=None, residual=None, pre_out=None, out_d
     if pre_out is not None:
         ldp = _given(pre_out, M, N, _BF16_ONLY, "pre_out")
         pp = pre_out.data_ptr()
-    out, ldo = _product_out(out, M, N, out_dtype, x.device)
-    n = lib().acrl_linear_workspace_bytes(M, N, K)
+    out, ldo = _result(out, M, N, out_dtype, x.device)
+    n = _size_of("acrl_linear_workspace_bytes", M, N, K)
     if n > 0 or workspace is not None:
         workspace = _workspace(workspace, n, x.device)
     if flags is not None:
@@ -803,15 +818,15 @@ def linear_backward(dy, x, weight, *, act=None, pre=None, bias=False, need_dx=Tr
     px = pw = pb = None
     tx = tw = lddx = lddw = 0
     if need_dx:
-        dx, lddx = _product_out(dx, M, K, dx_dtype, dev)
+        dx, lddx = _result(dx, M, K, dx_dtype, dev)
         px, tx = dx.data_ptr(), _OUT_DTYPE[dx.dtype]
     if need_dw:
-        dw, lddw = _product_out(dw, N, K, dw_dtype, dev)
+        dw, lddw = _result(dw, N, K, dw_dtype, dev)
         pw, tw = dw.data_ptr(), _OUT_DTYPE[dw.dtype]
     if bias:
         dbias = _vec(dbias, torch.float32, N, "dbias", dev)
         pb = dbias.data_ptr()
-    n = lib().acrl_linear_backward_workspace_bytes(M, N, K)
+    n = _size_of("acrl_linear_backward_workspace_bytes", M, N, K)
     workspace = _workspace(workspace, n, dev)
     if flags is not None:
         _need(flags, torch.int32, 1, "flags")
@@ -865,7 +880,7 @@ def orthogonalize(g, *, steps=5, coeffs=(3.4445, -4.7750, 2.0315), eps=1e-7, sca
     elif not isinstance(out, torch.Tensor) or out.dtype != torch.bfloat16 or out.shape != g.shape or not out.is_cuda:
         raise AcrlError(f"out: expected a bfloat16 CUDA tensor of {tuple(g.shape)}")
     _, _, _, ldo, out_stride = _matrices(out, "out")
-    nbytes = lib().acrl_orthogonalize_workspace_bytes(B, m, n)
+    nbytes = _size_of("acrl_orthogonalize_workspace_bytes", B, m, n)
     workspace = _workspace(workspace, nbytes, g.device)
     if flags is not None:
         _need(flags, torch.int32, 1, "flags")

@@ -15,7 +15,8 @@
 //   the weight, so that no product is made and nothing is loaded for rows that are not there.
 //
 // Where tiles are few their sums are split: the parts' accumulators go to a workspace in fp32, and the caller joins them in
-// order.  (Splitting only the tiles of a part-filled last round, so that it fills up, gained less than its join takes: 24 x
+// order.  (Joining them in a cluster through distributed shared memory instead saved a launch, but clusters of four CTAs that
+// each take an SM do not all find a place at once: 48 x 16,384 x 4,096 33.4 us against 30.3.  Splitting only the tiles of a part-filled last round, so that it fills up, gained less than its join takes: 24 x
 // 1,024 x 1,024 in three rounds and a sixth 61 us and 9 for the join, in four 66; at the power cap a round that leaves SMs idle
 // runs at a higher clock anyway.)
 //
@@ -95,11 +96,36 @@ struct Unit {
     int all;   // the tile among all matrices'
 };
 
+// Sums over rows of a matrix's columns, from sums of parts of them ([part][ldparts]), which a warp that is idle otherwise adds up
+// beside the products.  The parts go to eight sums in turn, and those are added up in order.
+struct ColumnSums {
+    const float* parts;
+    int64_t ldparts;   // a multiple of 32
+    int count, cols;
+    float* out;        // or null
+
+    __device__ __forceinline__ void run(int warp, int warps) const {
+        for (int c = warp * 32 + int(threadIdx.x & 31); c < cols; c += warps * 32) {
+            float sum[8] = {};
+            for (int p = 0; p < count; p += 8) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (p + k < count) sum[k] += parts[(p + k) * ldparts + c];
+            }
+            float total = 0.f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) total += sum[k];
+            out[c] = total;
+        }
+    }
+};
+
 template <int NP, int TERMS, class Epi>
 struct ProductLaunch {
     CUtensorMap p[NP], q[NP];
     Problem pr[NP];
     Epi epi[NP];
+    ColumnSums sums;
     int stages, stage_bytes;
     int32_t* flags;
 };
@@ -710,6 +736,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                 if (!role.unit(w.problem(), w.unit())) break;
             role.finish();
         }
+        if (warp == 3 && l.sums.out) l.sums.run(int(blockIdx.x), int(gridDim.x));
     } else {
         Drain<PAIR, LONG> role(b.ring, b.tmem, b.staging);
         for (Units<PAIR, NP, L> w(l); w.more(); w.next())

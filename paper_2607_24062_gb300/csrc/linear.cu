@@ -214,8 +214,9 @@ acrl_status join(const Problem& pr, const Product& d, cudaStream_t s) {
 }
 
 template <bool PAIR, int NP>
-acrl_status run_products(const Product (&d)[NP], int32_t* flags, cudaStream_t s) {
+acrl_status run_products(const Product (&d)[NP], const ColumnSums& sums, int32_t* flags, cudaStream_t s) {
     ProductLaunch<NP, 1, LinearEpilogue<PAIR>> l = {};
+    l.sums = sums;
     bool runs = false;
     for (int i = 0; i < NP; ++i) {
         if (!units_fit(d[i].plan.cut)) return ACRL_ERR_INVALID_ARG;
@@ -229,8 +230,8 @@ acrl_status run_products(const Product (&d)[NP], int32_t* flags, cudaStream_t s)
 }
 
 // f(x w^T + ...): K > 0 columns, or an empty sum.
-acrl_status product(const Product& d, int32_t* flags, cudaStream_t s) {
-    if (d.K == 0) {
+acrl_status product(const Product& d, const ColumnSums& sums, int32_t* flags, cudaStream_t s) {
+    if (d.K == 0) {   // of no rows, or of no columns: there are no columns' sums to join beside it
         const Cut& c = d.plan.cut;
         if (!units_fit(c)) return ACRL_ERR_INVALID_ARG;
         Problem pr = problem_of(d.plan.shape, c, d.x.turned, d.w.turned, false);
@@ -238,7 +239,7 @@ acrl_status product(const Product& d, int32_t* flags, cudaStream_t s) {
         return join(pr, d, s);
     }
     const Product one[1] = {d};
-    return d.plan.shape.pair ? run_products<true, 1>(one, flags, s) : run_products<false, 1>(one, flags, s);
+    return d.plan.shape.pair ? run_products<true, 1>(one, sums, flags, s) : run_products<false, 1>(one, sums, flags, s);
 }
 
 // g = dy f'(u), rounded, and the columns' sums of the unrounded.  A lane has eight columns, a warp 256, and the eight warps of a
@@ -319,21 +320,10 @@ __global__ void __launch_bounds__(256) slope_kernel(const acrl_bf16* dy, int64_t
     sums[at * ldsums + (int64_t(blockIdx.x) - int64_t(at) * tiles) * kSlopeCols + threadIdx.x] = total;
 }
 
-// The sums of the parts, 32 columns a CTA: each of eight warps adds up every eighth part, then the eight meet.
-__global__ void __launch_bounds__(256) sums_kernel(const float* sums, int64_t ldsums, int parts, int N, float* dbias) {
-    __shared__ float part[8][32];
+// The columns' sums where no product is made beside.
+__global__ void __launch_bounds__(32) sums_kernel(ColumnSums sums) {
     grid_begin();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = int(blockIdx.x) * 32 + lane;   // ldsums is a multiple of 256
-    float sum = 0.f;
-#pragma unroll 4
-    for (int p = warp; p < parts; p += 8) sum += sums[p * ldsums + n];
-    part[warp][lane] = sum;
-    __syncthreads();
-    if (warp != 0 || n >= N) return;
-    sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) sum += part[w][lane];
-    dbias[n] = sum;
+    sums.run(int(blockIdx.x), int(gridDim.x));
 }
 
 bool dtype_ok(acrl_dtype d) { return d == ACRL_BF16 || d == ACRL_F32; }
@@ -390,7 +380,7 @@ extern "C" acrl_status acrl_linear(const acrl_bf16* x, int64_t M, int64_t K, int
     if (linear_few_rows(M, N, K)) return linear_few(x, M, K, ldx, w, N, ldw, f, reinterpret_cast<cudaStream_t>(stream));
     const Plan plan = plan_linear(M, N, K);
     return product({plan, Matrix{x, M, ldx, false, 1, M * ldx, 0}, Matrix{w, N, ldw, false, 1, N * ldw, 0}, K, f, static_cast<float*>(workspace)},
-                   dev_flags, reinterpret_cast<cudaStream_t>(stream));
+                   ColumnSums{}, dev_flags, reinterpret_cast<cudaStream_t>(stream));
 }
 
 extern "C" int64_t acrl_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K) {
@@ -422,6 +412,7 @@ extern "C" acrl_status acrl_linear_backward(const acrl_bf16* dy, int64_t M, int6
     const acrl_bf16* g = dy;
     int64_t ldg = lddy;
     acrl_status st = ACRL_OK;
+    ColumnSums columns = {};
     if (has_g && (act != ACRL_ACT_NONE || dbias)) {
         acrl_bf16* to = act == ACRL_ACT_NONE || !(has_dx || has_dw) ? nullptr : reinterpret_cast<acrl_bf16*>(base);
         float* sums = dbias ? reinterpret_cast<float*>(base + parts.sums) : nullptr;
@@ -436,10 +427,8 @@ extern "C" acrl_status acrl_linear_backward(const acrl_bf16* dy, int64_t M, int6
             g = to;
             ldg = parts.ldg;
         }
-        if (dbias)
-            st = launch(sums_kernel, (N + 31) / 32, 256, 0, 0, s, static_cast<const float*>(sums), parts.ldsums, int(parts.count), int(N),
-                        dbias);
-        if (st != ACRL_OK) return st;
+        if (dbias) columns = ColumnSums{sums, parts.ldsums, int(parts.count), int(N), dbias};
+        if (dbias && !has_dx && !has_dw) return launch(sums_kernel, std::min<int64_t>((N + 31) / 32, 4096), 32, 0, 0, s, columns);
     } else if (dbias && N > 0) {
         if (cudaMemsetAsync(dbias, 0, size_t(N) * 4, s) != cudaSuccess) return launch_status();
     }
@@ -455,8 +444,8 @@ extern "C" acrl_status acrl_linear_backward(const acrl_bf16* dy, int64_t M, int6
                               reinterpret_cast<float*>(base + parts.dx)},
                              {parts.plan.dw, Matrix{g, N, ldg, true, 1, M * ldg, 0}, Matrix{x, K, ldx, true, 1, M * ldx, 0}, has_g ? M : 0, fw,
                               reinterpret_cast<float*>(base + parts.dw)}};
-    if (has_dx && has_dw && has_g && parts.plan.together) return run_products<true, 2>(both, dev_flags, s);
-    if (has_dx) st = product(both[0], dev_flags, s);
-    if (has_dw && st == ACRL_OK) st = product(both[1], dev_flags, s);
+    if (has_dx && has_dw && has_g && parts.plan.together) return run_products<true, 2>(both, columns, dev_flags, s);
+    if (has_dx) st = product(both[0], columns, dev_flags, s);
+    if (has_dw && st == ACRL_OK) st = product(both[1], has_dx ? ColumnSums{} : columns, dev_flags, s);
     return st;
 }
