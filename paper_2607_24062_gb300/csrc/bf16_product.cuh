@@ -23,7 +23,7 @@
 // The tensor cores cut partial sums off where they should round them: an error toward zero that grows with the length of a run
 // (relative to the result's norm, of normal numbers: 0.7e-6 for a sum of 1,027, 1.7e-6 for 2,507).  bf16 hides it; for an fp32
 // result the sum is taken in runs of kRun slabs, whose accumulators the epilogue's warps add up in registers, rounding, while
-// the MMAs fill the next (LONG).
+// the MMAs fill the next (LONG).  No accumulator takes more than kLongest slabs, whatever the result's type.
 //
 // TERMS = 3: each operand is two bf16 matrices, p = p0 + p1, and acc takes p0 q0 + p0 q1 + p1 q0 (Dekker's split product
 // without its smallest term): four tiles in shared memory feed three MMAs.  One copy brings both halves of an operand: a copy
@@ -54,6 +54,7 @@ constexpr int kAccCols = 256;        // of each accumulator
 constexpr int kWarpStaging = 4096;   // bytes of an epilogue warp: a block of 32 x 32 in fp32
 constexpr int kProductSmem = 227 * 1024;
 constexpr int kRun = 8;              // slabs of a run
+constexpr int kLongest = 512;        // slabs of a run of any result: 32,768 columns
 
 struct ProductBarriers {
     uint64_t full[kMaxStages];    // the copies of a stage have landed (pair: the even CTA's counts both CTAs')
@@ -817,11 +818,13 @@ inline int64_t unit_cycles(const Shape& s, const Cut& c) { return c.per * s.slab
 template <typename F>
 void each_cut(const Shape& s, int cols, int64_t few, F consider) {
     const int64_t tiles = s.tiles(cols), slabs = s.slabs();
-    consider(Cut{cols, tiles, 1, int(slabs)});
+    // products of two halves each have no runs: a very long sum is split wherever it is
+    const int64_t least = s.terms == 3 ? (slabs + kLongest - 1) / kLongest : 1, longest = (slabs + least - 1) / least;
+    consider(Cut{cols, tiles, int((slabs + longest - 1) / longest), int(longest)});
     for (int64_t parts : kPartChoices) {
         int64_t per;
         if (tiles > few || tiles * (parts - 1) >= 2 * s.lanes()) break;
-        if (part_length(slabs, parts, per)) consider(Cut{cols, tiles, int(parts), int(per)});
+        if (parts > least && part_length(slabs, parts, per)) consider(Cut{cols, tiles, int(parts), int(per)});
     }
 }
 

@@ -194,8 +194,8 @@ struct Product {
     float* parts;
 };
 
-// An fp32 result of more than one run.
-bool has_runs(const Product& p) { return p.f.out_f32 && p.plan.shape.slabs() > kRun; }
+// An fp32 result of more than one run, and any of a very long sum.
+bool has_runs(const Product& p) { return p.plan.shape.slabs() > (p.f.out_f32 ? kRun : kLongest); }
 
 template <bool PAIR, int NP>
 bool describe(ProductLaunch<NP, 1, LinearEpilogue<PAIR>>& l, int at, const Product& d) {

@@ -9,7 +9,7 @@
 
 namespace acrl {
 
-constexpr int64_t kMostSize = kMaxGrid - 512;   // rows and columns
+constexpr int64_t kMostSize = kMaxGrid - 8192;   // rows and columns: what a loop or a tile goes beyond them stays an int
 
 // What follows the sum: out = f(sum + bias) + residual.
 struct Finish {

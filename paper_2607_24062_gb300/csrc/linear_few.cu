@@ -42,9 +42,15 @@ __global__ void __launch_bounds__(kThreads, T == 1 ? 3 : 2) few_kernel(const __g
     __shared__ float red[kWarps][8 * T][kW + 1];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int n0 = int(blockIdx.x) * kW, K = A.K;
-    grid_begin();
     const acrl_bf16* w0 = A.w + int64_t(min(n0 + g, A.N - 1)) * A.ldw;
     const acrl_bf16* w1 = A.w + int64_t(min(n0 + g + 8, A.N - 1)) * A.ldw;
+    // The weight's first columns on their way to L2 before the launch before this one has ended.  (L2 is where all writes go: what
+    // that launch still writes of them is what the loads will find.)
+    if (warp * kTurn < K) {
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(w0 + min(warp * kTurn + 32 * t, K - 1)));
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(w1 + min(warp * kTurn + 32 * t, K - 1)));
+    }
+    grid_begin();
     float c[T][4] = {};
     for (int k0 = warp * kTurn; k0 < K; k0 += kWarps * kTurn) {
         uint4 a[kAhead], b[kAhead], x[T][kAhead];

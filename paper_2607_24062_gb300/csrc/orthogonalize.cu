@@ -575,7 +575,7 @@ using namespace acrl;
 
 namespace {
 bool sizes_ok(int64_t batch, int64_t m, int64_t n) {
-    constexpr int64_t kMost = kMaxGrid - 512;
+    constexpr int64_t kMost = kMaxGrid - 8192;   // what a loop or a tile goes beyond them stays an int
     return batch >= 0 && m >= 0 && n >= 0 && batch <= kMost && m <= kMost && n <= kMost;
 }
 // Tiles, pieces and blocks of a launch are counted in 32 bits.

@@ -327,6 +327,31 @@ def test_more_than_two_to_the_31_elements():
     assert bool((db.double() == float(x[:, 0].double().sum())).all())             # below 2^24
 
 
+@pytest.mark.parametrize("M,K", [(1, 2 ** 31 - 8200), (17, 2 ** 28 + 8)])
+def test_the_longest_sums(M, K):
+    """A few terms at both ends and in the middle of rows as long as the call takes; fewer rows of it where 17 would not fit."""
+    x, w = torch.zeros((M, K), dtype=BF, device=DEV), torch.zeros((3, K), dtype=BF, device=DEV)
+    for i, k in enumerate((0, 5000, K // 2, K - 1)):
+        x[:, k], w[1, k] = i + 1.0, 2.0 ** i
+    y = acrl.linear(x, w, out_dtype=F32)
+    assert bool((y[:, 1] == 1 + 4 + 12 + 32).all()) and not bool(y[:, 0].any()) and not bool(y[:, 2].any())
+
+
+@pytest.mark.parametrize("M", [5, 60, 300])
+def test_long_sums_of_one_sign(M):
+    """Terms that are all alike add up without a drift: every partial sum is rounded, or short enough.  (Cut off after its 24
+    bits at each step of sixteen terms, a sum of 2^17 ones and a bit would lose up to 2^13 times 2^-24 of it.)"""
+    K = 2 ** 17
+    x, w = torch.full((M, K), 1.0 + 2.0 ** -7, dtype=BF, device=DEV), torch.full((70, K), 1.0 - 2.0 ** -8, dtype=BF, device=DEV)
+    exact = K * (1.0 + 2.0 ** -7) * (1.0 - 2.0 ** -8)
+    y = acrl.linear(x, w, out_dtype=F32).double()
+    # runs of 512 terms at most are exact to 2^-23 of themselves a step (32 steps), and at most 256 of them, or 1,024, add up
+    assert bool(((y - exact).abs() <= exact * (2.0 ** -23 * 32 + 2.0 ** -24 * 1024)).all())
+    # the same in bf16, of runs of 32,768: 2,048 steps
+    y = acrl.linear(x, w).double()
+    assert bool(((y - exact).abs() <= exact * (2.0 ** -8 + 2.0 ** -23 * 2048)).all())
+
+
 def test_refusals():
     x, w = _matrix(8, 64, 1), _matrix(16, 64, 2)
     dy = _matrix(8, 16, 3)

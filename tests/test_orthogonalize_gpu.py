@@ -131,6 +131,13 @@ def test_updates_of_any_size(size, eps):
     _check(acrl.orthogonalize(g, eps=eps), g, eps=eps)
 
 
+def test_very_long_rows():
+    """The Gram matrix of rows of a million columns: its sums are split, however many tiles there are."""
+    for m, n in ((40, 2 ** 20 + 24), (2 ** 17 + 40, 300)):
+        g = _update((m, n), 17, BF)
+        _check(acrl.orthogonalize(g), g)
+
+
 def test_zeros_infinities_and_nan():
     for m, n in ((40, 72), (300, 130)):
         g = _update((5, m, n), 11)
