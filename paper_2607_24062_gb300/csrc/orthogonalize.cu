@@ -384,6 +384,7 @@ __device__ bool keep_counters(const StepsLaunch& l, ProductBarriers* bars) {
         for (int u = at.first(); u < pr.units; u += at.pairs, ++n) {
             if (!wait_phase(&bars->written[n & 1u], (n >> 1) & 1u, abort)) return false;
             tell(l.done + (l.each ? u / pr.tiles : 0));
+            mbar_arrive(&bars->told[n & 1u]);
         }
         if (pr.parts > 1) {
             if (!wait_done(l.done, at.before + at.units(pr), abort)) return false;
@@ -445,11 +446,12 @@ __global__ void __launch_bounds__(kProductThreads, 1) steps_kernel(const __grid_
             __syncwarp();
             if (role.lane == 0) mbar_arrive(bar);
         };
-        // A warp that has read out an accumulator may still be storing when another is two units on, and comes to the same barrier.
+        // Not before the unit two before, which had the same barrier, has been told of: a warp that has read out an accumulator may
+        // still be storing when another is two units on, and the teller may be as far behind, to whom a barrier that has been
+        // passed twice looks as if it had not been at all.
         auto come_in_turn = [&] {
-            uint64_t* bar = &bars->written[n & 1u];
-            if (n >= 2 && !warp_wait(bar, ((n - 2) >> 1) & 1u, abort)) return false;
-            come(bar);
+            if (n >= 2 && !warp_wait(&bars->told[n & 1u], ((n - 2) >> 1) & 1u, abort)) return false;
+            come(&bars->written[n & 1u]);
             ++n;
             return true;
         };

@@ -83,6 +83,24 @@ def test_batches(B, m, n, dtype):
     _check(acrl.orthogonalize(g[B - 1]), g[B - 1])
 
 
+@pytest.mark.parametrize("B,m,n", [(30, 512, 512), (12, 512, 700), (9, 700, 512), (24, 1024, 1024)])
+def test_more_matrices_than_pairs_of_processors(B, m, n):
+    """Where the steps of many matrices overlap, and their products have tiles of 256 x 256 on the diagonal: the same every time,
+    and each matrix as by itself."""
+    g = _update((B, m, n), 9)
+    flags = api.new_flags()
+    out = acrl.orthogonalize(g, flags=flags)
+    for _ in range(20):
+        assert torch.equal(acrl.orthogonalize(g, flags=flags), out)
+    assert acrl.read_flags(flags) == 0
+    for z in (0, B // 2, B - 1):
+        _check(out[z], g[z])
+    x = out.float()
+    x = x if m <= n else x.mT
+    gram = x @ x.mT
+    assert float((gram - torch.diag_embed(gram.diagonal(dim1=1, dim2=2))).abs().max()) < 1.0 and bool(torch.isfinite(out).all())
+
+
 def _aligned(t, gap=0):
     to = torch.full((*t.shape[:-1], (t.shape[-1] + 7) // 8 * 8 + gap), float("nan"), dtype=t.dtype, device=DEV)[..., : t.shape[-1]]
     return to.copy_(t)
