@@ -1,9 +1,12 @@
-// A layer of up to 16 rows, single tokens first of all: every byte of the weight is used once, and HBM bounds it.  Neither
-// tensor memory nor a ring of copies: their start and end, and the join of a split sum, take longer than the weight of a layer.
+// A layer of up to 16 rows, single tokens first of all, and a small layer of up to 64: every byte of the weight is used once,
+// and HBM bounds it.  Neither tensor memory nor a ring of copies: their start and end, and the join of a split sum, take longer
+// than the weight of a layer.
 // A CTA has 16 rows of the weight; its eight warps take turns along the sum, 128 columns each, and their sums meet in shared
 // memory.  The products are mma.sync m16n8k16, the weight's rows the 16 and those of x the eight: the pipes of tcgen05 would
 // wait for the same bytes.  A lane loads 16 bytes of a weight's row, eight neighbours of the sum, where the instruction's
 // layout has four pairs: which eight of a slab's 32 columns a lane holds does not matter as long as both operands agree.
+#include <algorithm>
+
 #include "linear.cuh"
 
 namespace acrl {
@@ -30,6 +33,22 @@ __device__ __forceinline__ uint4 load8(const acrl_bf16* row, int k, int K) {
     return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
+// Eight numbers, or zeros, without a branch around the load; of the weight, which is read once, past L1.
+template <bool ONCE>
+__device__ __forceinline__ uint4 eight(const acrl_bf16* p, bool there) {
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (ONCE)
+        asm volatile(
+            "{\n .reg .pred q;\n setp.ne.b32 q, %5, 0;\n @q ld.global.nc.L1::no_allocate.L2::256B.v4.u32 {%0, %1, %2, %3}, [%4];\n}"
+            : "+r"(v.x), "+r"(v.y), "+r"(v.z), "+r"(v.w)
+            : "l"(p), "r"(uint32_t(there)));
+    else
+        asm volatile("{\n .reg .pred q;\n setp.ne.b32 q, %5, 0;\n @q ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];\n}"
+                     : "+r"(v.x), "+r"(v.y), "+r"(v.z), "+r"(v.w)
+                     : "l"(p), "r"(uint32_t(there)));
+    return v;
+}
+
 __device__ __forceinline__ void mma_16x8(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
@@ -38,7 +57,7 @@ __device__ __forceinline__ void mma_16x8(float (&c)[4], uint32_t a0, uint32_t a1
 
 // T: eights of x's rows.
 template <int T>
-__global__ void __launch_bounds__(kThreads, T == 1 ? 3 : 2) few_kernel(const __grid_constant__ FewArgs A) {
+__global__ void __launch_bounds__(kThreads, T == 1 ? 3 : T <= 4 ? 2 : 1) few_kernel(const __grid_constant__ FewArgs A) {
     __shared__ float red[kWarps][8 * T][kW + 1];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int n0 = int(blockIdx.x) * kW, K = A.K;
@@ -52,30 +71,36 @@ __global__ void __launch_bounds__(kThreads, T == 1 ? 3 : 2) few_kernel(const __g
     }
     grid_begin();
     float c[T][4] = {};
-    for (int k0 = warp * kTurn; k0 < K; k0 += kWarps * kTurn) {
+    const int whole = K & ~7;
+    for (int k0 = warp * kTurn; k0 < whole; k0 += kWarps * kTurn) {
         uint4 a[kAhead], b[kAhead], x[T][kAhead];
-        if (k0 + kTurn <= K) {
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                a[i] = ld_stream(reinterpret_cast<const uint4*>(w0 + k0 + 32 * i + 8 * t));
-                b[i] = ld_stream(reinterpret_cast<const uint4*>(w1 + k0 + 32 * i + 8 * t));
+        // With eight rows of x three CTAs are resident and a thread has 80 registers: predicates for the loads would not fit (1 x
+        // 16,384 x 4,096 26.4 us against 22.5), and the sum's end is gone through slab by slab instead.
+        if (T == 1 && k0 + kTurn > whole) {
+#pragma unroll 1
+            for (int k = k0 + 8 * t; k < k0 + 8 * t + kTurn && k - 8 * t < whole; k += 32) {
+                const uint4 a = eight<true>(w0 + k, k < whole), b = eight<true>(w1 + k, k < whole);
+                const uint4 x = eight<false>(A.x + g * A.ldx + k, g < A.M && k < whole);
+                mma_16x8(c[0], a.x, b.x, a.y, b.y, x.x, x.y);
+                mma_16x8(c[0], a.z, b.z, a.w, b.w, x.z, x.w);
             }
+            break;
+        }
 #pragma unroll
-            for (int r = 0; r < T; ++r)
+        for (int i = 0; i < kAhead; ++i) {
+            const int k = k0 + 32 * i + 8 * t;
+            a[i] = T == 1 ? ld_stream(reinterpret_cast<const uint4*>(w0 + k)) : eight<true>(w0 + k, k < whole);
+            b[i] = T == 1 ? ld_stream(reinterpret_cast<const uint4*>(w1 + k)) : eight<true>(w1 + k, k < whole);
+        }
 #pragma unroll
-                for (int i = 0; i < kAhead; ++i)
-                    x[r][i] = 8 * r + g < A.M ? __ldg(reinterpret_cast<const uint4*>(A.x + (8 * r + g) * A.ldx + k0 + 32 * i + 8 * t))
-                                              : make_uint4(0u, 0u, 0u, 0u);
-        } else {
+        for (int r = 0; r < T; ++r)
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
                 const int k = k0 + 32 * i + 8 * t;
-                a[i] = load8(w0, k, K);
-                b[i] = load8(w1, k, K);
-#pragma unroll
-                for (int r = 0; r < T; ++r) x[r][i] = load8(A.x + (8 * r + g) * A.ldx, k, 8 * r + g < A.M ? K : 0);
+                const acrl_bf16* p = A.x + (8 * r + g) * A.ldx + k;
+                if (T == 1) x[r][i] = g < A.M ? __ldg(reinterpret_cast<const uint4*>(p)) : make_uint4(0u, 0u, 0u, 0u);
+                else x[r][i] = eight<false>(p, 8 * r + g < A.M && k < whole);
             }
-        }
         // each turn's products in a sum of their own: the tensor cores cut partial sums off, an error that grows with their number
 #pragma unroll
         for (int r = 0; r < T; ++r) {
@@ -89,6 +114,15 @@ __global__ void __launch_bounds__(kThreads, T == 1 ? 3 : 2) few_kernel(const __g
             for (int j = 0; j < 4; ++j) c[r][j] += d[j];
         }
     }
+    if (warp == kWarps - 1 && whole < K) {   // fewer than eight columns: the first of a row's lanes has them
+        const uint4 a = load8(w0, whole, t == 0 ? K : 0), b = load8(w1, whole, t == 0 ? K : 0);
+#pragma unroll
+        for (int r = 0; r < T; ++r) {
+            const uint4 x = load8(A.x + (8 * r + g) * A.ldx, whole, t == 0 && 8 * r + g < A.M ? K : 0);
+            mma_16x8(c[r], a.x, b.x, a.y, b.y, x.x, x.y);
+            mma_16x8(c[r], a.z, b.z, a.w, b.w, x.z, x.w);
+        }
+    }
 #pragma unroll
     for (int r = 0; r < T; ++r) {
         red[warp][8 * r + 2 * t][g] = c[r][0];
@@ -97,28 +131,48 @@ __global__ void __launch_bounds__(kThreads, T == 1 ? 3 : 2) few_kernel(const __g
         red[warp][8 * r + 2 * t + 1][g + 8] = c[r][3];
     }
     __syncthreads();
-    const int m = threadIdx.x / kW;
     const int64_t n = n0 + (threadIdx.x & (kW - 1));
-    if (m >= A.M || n >= A.N) return;
-    float v[1] = {};
-#pragma unroll
-    for (int i = 0; i < kWarps; ++i) v[0] += red[i][m][n - n0];
     const Finish& f = A.f;
-    if (f.bias) v[0] += load_float(f.bias, f.bias_f32, n);
-    if (f.pre) f.pre[m * f.ldp + n] = to_bf16(v[0]);
-    apply(f.act, v);
-    if (f.residual) v[0] += load_float(f.residual, f.residual_f32, m * f.ldr + n);
-    store_float(f.out, f.out_f32, m * f.ldo + n, v[0]);
+#pragma unroll 1
+    for (int m = threadIdx.x / kW; m < A.M && n < A.N; m += kThreads / kW) {
+        float v[1] = {};
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) v[0] += red[i][m][n - n0];
+        if (f.bias) v[0] += load_float(f.bias, f.bias_f32, n);
+        if (f.pre) f.pre[m * f.ldp + n] = to_bf16(v[0]);
+        apply(f.act, v);
+        if (f.residual) v[0] += load_float(f.residual, f.residual_f32, m * f.ldr + n);
+        store_float(f.out, f.out_f32, m * f.ldo + n, v[0]);
+        if (T <= 2) break;
+    }
 }
+
+// Eights of x's rows that a CTA goes through.
+int eights(int64_t M) { return M <= 32 ? int((M + 7) / 8) : M <= 48 ? 6 : 8; }
 
 }  // namespace
 
-bool linear_few_rows(int64_t M, int64_t N, int64_t K) { return M > 0 && M <= 16 && N > 0 && K > 0; }
+// Above 16 rows the CTAs' loads of x count: with those of their 16 rows of the weight they come from L2 at some 80 bytes a
+// nanosecond of an SM, 70 where one CTA is resident.  Tensor memory's way reads x for 128 rows of the weight at once and HBM
+// bounds it, 5.9 TB/s, but it takes 3.5 us more to begin, to end and to join parts.  Measured, us here and there: 32 x 2,048 x
+// 2,048 4.7 and 8.8, 64 x 2,048 x 2,048 6.7 and 9.7, 32 x 4,096 x 4,096 11.1 and 12.3, 48 x 4,096 x 4,096 17 and 13, 20 x 16,384 x
+// 4,096 31 and 26.
+bool linear_few_rows(int64_t M, int64_t N, int64_t K) {
+    if (M <= 0 || M > 64 || N <= 0 || K <= 0) return false;
+    if (M <= 16) return true;
+    const int64_t ctas = (N + kW - 1) / kW;
+    const int T = eights(M);
+    const double rounds = T <= 4 ? std::max(1.0, ctas / 152.0) : double((ctas + 151) / 152);
+    return rounds * double(kW + 8 * T) * 2.0 * double(K) / (T <= 4 ? 80.0 : 70.0) < 3500.0 + 2.0 * double(N) * double(K) / 5900.0;
+}
 
 acrl_status linear_few(const acrl_bf16* x, int64_t M, int64_t K, int64_t ldx, const acrl_bf16* w, int64_t N, int64_t ldw, const Finish& f,
                        cudaStream_t s) {
     const FewArgs A{x, w, ldx, ldw, int(M), int(N), int(K), f};
-    return launch(M <= 8 ? few_kernel<1> : few_kernel<2>, (N + kW - 1) / kW, kThreads, 0, 0, s, A);
+    const int T = eights(M);
+    return launch(T == 1 ? few_kernel<1> : T == 2 ? few_kernel<2> : T == 3 ? few_kernel<3> : T == 4 ? few_kernel<4> : T == 6 ? few_kernel<6>
+                                                                                                                             : few_kernel<8>,
+                  (N + kW - 1) / kW, kThreads, 0, 0, s, A);
 }
 
 }  // namespace acrl

@@ -85,6 +85,32 @@ def test_linear(M, N, K, dtype):
     _check_linear(x, w, None, None, None, acrl.linear(x, w, out_dtype=dtype))
 
 
+@pytest.mark.parametrize("M,N,K", [(17, 33, 7), (24, 2051, 1030), (31, 520, 2051), (47, 1000, 1003), (60, 70, 9), (64, 2048, 2048), (64, 264, 520),
+                                   (20, 16384, 1027), (48, 4100, 4104), (65, 264, 520), (100, 1000, 520), (128, 515, 513)])
+def test_a_few_dozen_rows(M, N, K):
+    """What one kernel does in registers and the other in tensor memory, by size, with everything that follows the sum."""
+    x, w = _matrix(M, K, 1, gap=8), _matrix(N, K, 2, std=K ** -0.5, gap=16)
+    b, r = torch.randn(N, device=DEV), _matrix(M, N, 5, gap=8)
+    pre = torch.full((M + 1, (N + 7) // 8 * 8 + 8), 7.0, dtype=BF, device=DEV)
+    y = torch.full((M + 1, (N + 7) // 8 * 8 + 8), 7.0, dtype=F32, device=DEV)
+    got = acrl.linear(x, w, b, act="silu", residual=r, pre_out=pre[:M, :N], out=y[:M, :N])
+    _check_linear(x, w, b, "silu", r, got, pre[:M, :N])
+    for t in (y, pre):
+        assert bool((t[M:] == 7.0).all()) and bool((t[:, N:] == 7.0).all())
+
+
+@pytest.mark.parametrize("M,N,K", [(3, 40, 264), (8, 130, 1003), (20, 40, 264), (30, 40, 1003), (64, 40, 268)])
+def test_infinities_stay_in_their_row_and_column(M, N, K):
+    """An infinity anywhere in a row, its first numbers included, makes its own results infinite or NaN and no others."""
+    for k in (0, K - 1, K // 2):
+        x, w = _matrix(M, K, 3), _matrix(N, K, 4)
+        x[M // 2, k] = float("inf")
+        w[N // 3, k] = float("-inf")
+        y = acrl.linear(x, w, out_dtype=F32)
+        want = x.float() @ w.float().t()
+        assert torch.equal(torch.isnan(y), torch.isnan(want)) and torch.equal(torch.isinf(y), torch.isinf(want))
+
+
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("bias,residual,out,keep", [(F32, BF, BF, True), (BF, F32, F32, False), (F32, None, F32, True),
                                                     (None, BF, F32, False), (BF, BF, BF, True), (None, F32, BF, True)])
