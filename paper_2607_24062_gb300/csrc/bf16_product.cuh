@@ -11,14 +11,14 @@
 // accumulators in tensor memory while the MMAs fill the other.  Persistent over the tiles.  Two ways:
 //
 // Pairs: two CTAs (cta_group::2) share a tile of 256 rows x up to 256 columns, each staging its 128 rows of p and half of q's.
-// Alone: a CTA has 128 rows of p and up to 128 columns.  For few rows of a layer's input, which then are the columns: p is
+// Alone: a CTA has 128 rows of p or fewer and up to 128 columns.  For few rows of a layer's input, which then are the columns: p is
 //   the weight, so that no product is made and nothing is loaded for rows that are not there.
 //
 // Where tiles are few their sums are split: the parts' accumulators go to a workspace in fp32, and the caller joins them in
 // order.  (Joining them in a cluster through distributed shared memory instead saved a launch, but clusters of four CTAs that
-// each take an SM do not all find a place at once: 48 x 16,384 x 4,096 33.4 us against 30.3.  Splitting only the tiles of a part-filled last round, so that it fills up, gained less than its join takes: 24 x
-// 1,024 x 1,024 in three rounds and a sixth 61 us and 9 for the join, in four 66; at the power cap a round that leaves SMs idle
-// runs at a higher clock anyway.)
+// each take an SM do not all find a place at once: 48 x 16,384 x 4,096 33.4 us against 30.3.  Splitting only the tiles of a
+// part-filled last round, so that it fills up, gained less than its join takes: 24 x 1,024 x 1,024 in three rounds and a sixth
+// 61 us and 9 for the join, in four 66; at the power cap a round that leaves SMs idle runs at a higher clock anyway.)
 //
 // The tensor cores cut partial sums off where they should round them: an error toward zero that grows with the length of a run
 // (relative to the result's norm, of normal numbers: 0.7e-6 for a sum of 1,027, 1.7e-6 for 2,507).  bf16 hides it; for an fp32
@@ -77,6 +77,7 @@ struct Problem {
     int slabs;               // ceil(K / 64)
     int batch;
     int cols;                // of a tile: a multiple of 32 (pair; of 128 where q is not K-major) or of 16 (alone)
+    int high;                // rows of a tile of p: both CTAs' 256, or alone 128 or fewer, a multiple of eight
     int p_tiles, q_tiles;
     int parts, per;          // of the sum, of so many slabs
     int run;                 // slabs that one accumulator takes
@@ -86,10 +87,9 @@ struct Problem {
     int tiles, units;        // tiles of one matrix; parts of all
     int pair;
 
-    __host__ __device__ int high() const { return pair ? 2 * kRows : kRows; }
     // The result's rows and columns of a tile: alone, the rows of q are the result's.
-    __host__ __device__ int tile_rows() const { return pair ? 2 * kRows : cols; }
-    __host__ __device__ int tile_cols() const { return pair ? cols : kRows; }
+    __host__ __device__ int tile_rows() const { return pair ? high : cols; }
+    __host__ __device__ int tile_cols() const { return pair ? cols : high; }
 };
 
 // What a CTA or pair works on at a time.
@@ -244,8 +244,8 @@ struct Producer {
         volatile int32_t* abort = &bars->abort;
         const int q_rows = PAIR ? pr.cols / 2 : pr.cols, q_bytes = q_rows * kRowBytes;
         const bool once = PAIR && on_diagonal(pr, t);
-        const int bytes = kMats * (kRows * kRowBytes + (once ? 0 : q_bytes));
-        const int p0 = (PAIR ? 2 * t.tp + int(ring.rank) : t.tp) * kRows;
+        const int bytes = kMats * ((PAIR ? kRows : pr.high) * kRowBytes + (once ? 0 : q_bytes));
+        const int p0 = PAIR ? (2 * t.tp + int(ring.rank)) * kRows : t.tp * pr.high;
         const int q0 = t.tq * pr.cols + (PAIR ? int(ring.rank) * q_rows : 0);
         const bool p_turned = pr.p_turned, q_turned = pr.q_turned;
         for (int kb = t.lo; kb < t.hi; ++kb) {
@@ -621,7 +621,8 @@ struct Drain {
 
     template <class Epi>
     __device__ __forceinline__ bool unit(const Problem& pr, const Unit& t, const Epi& epi) {
-        const int row0 = (PAIR ? 2 * t.tp + int(ring.rank) : t.tp) * kRows + quarter * 32;
+        const int row0 = (PAIR ? (2 * t.tp + int(ring.rank)) * kRows : t.tp * pr.high) + quarter * 32;
+        const int rows = PAIR ? pr.rows : min(pr.rows, (t.tp + 1) * pr.high);
 #pragma unroll 1
         for (int pass = dry ? 0 : 1; pass < 2; ++pass) {
             const bool live = pass == 1;
@@ -637,8 +638,8 @@ struct Drain {
                 tmem_ld32(tmem + uint32_t(acc * kAccCols + c) + (uint32_t(quarter * 32) << 16), r);
                 if (live && c + 64 >= pr.cols) release();
                 const int col0 = t.tq * pr.cols + c;
-                if (row0 < pr.rows && col0 < pr.cols_all)   // the same for the whole warp
-                    epi.chunk(pr, t, r, row0, col0, live ? pr.rows : 0, live ? pr.cols_all : 0, out);
+                if (row0 < rows && col0 < pr.cols_all)   // the same for the whole warp
+                    epi.chunk(pr, t, r, row0, col0, live ? rows : 0, live ? pr.cols_all : 0, out);
                 if (!live) break;
             }
             __syncwarp();
@@ -784,21 +785,23 @@ struct Shape {
     int64_t rows, cols_all, K, batch;
     bool lower;
     int terms, widest, least, step;
+    int high;   // rows of a tile
 
     int64_t slabs() const { return std::max<int64_t>(1, (K + kSlab - 1) / kSlab); }
-    int high() const { return pair ? 2 * kRows : kRows; }
     int64_t lanes() const { return pair ? 76 : 152; }   // what a GPU of 152 SMs runs at once
     int64_t tiles(int cols) const {
-        const int64_t p = (rows + high() - 1) / high(), q = (cols_all + cols - 1) / cols, r = high() / cols;
+        const int64_t p = (rows + high - 1) / high, q = (cols_all + cols - 1) / cols, r = high / cols;
         // of a symmetric matrix, each row tile but the last has r columns more than the one before
         return batch * (lower && p > 0 ? r * (p - 1) * p / 2 + q : p * q);
     }
-    // Cycles of a slab: the MMAs, or the copies at 52 bytes a cycle of an SM.
+    // Cycles of a slab: the MMAs, or the copies at 52 bytes a cycle of an SM; alone, where they come from HBM, no less than 3,800
+    // a turn of the ring (48 x 4,096 x 4,096 whole: 64 slabs 16 us, whether the tiles have 64 or 128 rows of p).
     int64_t slab(int cols) const {
-        const int64_t mats = terms == 3 ? 2 : 1, mine = pair ? cols / 2 : cols;
-        return std::max<int64_t>(terms * (pair ? 2 : 4) * int64_t(cols), mats * (kRows + mine) * kRowBytes / 52);
+        const int64_t mats = terms == 3 ? 2 : 1, mine = pair ? cols / 2 : cols, bytes = mats * (kRows + mine) * kRowBytes;
+        const int64_t work = std::max<int64_t>(terms * (pair ? 2 : 4) * int64_t(cols), bytes / 52);
+        return pair ? work : std::max(work, 3800 / std::min<int64_t>(kMaxStages, kRingBytes / bytes));
     }
-    int64_t tile_bytes(int cols) const { return int64_t(high()) * cols * 4; }
+    int64_t tile_bytes(int cols) const { return int64_t(high) * cols * 4; }
     int next(int cols) const { return step > 0 ? cols - step : cols / 2; }
 };
 
@@ -817,6 +820,15 @@ inline int64_t join_cycles(const Shape& s, const Cut& c) {
     return c.parts == 1 ? 0 : kJoinCycles + c.tiles * (c.parts + 1) * s.tile_bytes(c.cols) / kJoinBytes;
 }
 inline int64_t unit_cycles(const Shape& s, const Cut& c) { return c.per * s.slab(c.cols) + kTileCycles; }
+
+// Rounds of units, the last of them part-filled, and the joining of parts.  Alone, HBM bounds a round that is full.
+constexpr int64_t kHbmBytes = 3100;   // a cycle
+inline int64_t cut_cycles(const Shape& s, const Cut& c) {
+    const int64_t lanes = s.lanes(), units = c.units(), unit = unit_cycles(s, c);
+    const int64_t bytes = s.pair ? 0 : int64_t(c.per) * s.high * kRowBytes;
+    auto round = [&](int64_t n) { return std::max(unit, n * bytes / kHbmBytes); };
+    return units / lanes * round(lanes) + (units % lanes > 0 ? round(units % lanes) : 0) + join_cycles(s, c);
+}
 
 // consider(cut) for the whole sums of tiles of `cols` columns and, where there are no more than `few` tiles, for parts of them.
 template <typename F>
@@ -839,7 +851,7 @@ inline Cut best_cut(const Shape& s) {
     int64_t least = -1;
     for (int cols = s.widest; cols >= s.least; cols = s.next(cols))
         each_cut(s, cols, 2 * lanes, [&](const Cut& c) {
-            const int64_t cost = (c.units() + lanes - 1) / lanes * unit_cycles(s, c) + join_cycles(s, c);
+            const int64_t cost = cut_cycles(s, c);
             if (least >= 0 && cost >= least) return;
             least = cost;
             best = c;
@@ -888,7 +900,8 @@ inline Problem problem_of(const Shape& s, const Cut& cut, bool p_turned, bool q_
     pr.batch = int(s.batch);
     pr.cols = cut.cols;
     pr.pair = s.pair;
-    pr.p_tiles = int((s.rows + s.high() - 1) / s.high());
+    pr.high = s.high;
+    pr.p_tiles = int((s.rows + s.high - 1) / s.high);
     pr.q_tiles = int((s.cols_all + cut.cols - 1) / cut.cols);
     pr.parts = cut.parts;
     pr.per = cut.per;
@@ -897,7 +910,7 @@ inline Problem problem_of(const Shape& s, const Cut& cut, bool p_turned, bool q_
     pr.p_turned = p_turned;
     pr.q_turned = q_turned;
     pr.idesc = 1u << 4 | 1u << 7 | 1u << 10 | uint32_t(p_turned) << 15 | uint32_t(q_turned) << 16 |
-               uint32_t(cut.cols >> 3) << 17 | uint32_t(s.high() >> 4) << 24;
+               uint32_t(cut.cols >> 3) << 17 | uint32_t((s.pair ? 2 * kRows : kRows) >> 4) << 24;
     pr.tiles = int(cut.tiles / std::max<int64_t>(1, s.batch));
     pr.units = int(cut.units());
     return pr;

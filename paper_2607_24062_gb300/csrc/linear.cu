@@ -52,10 +52,10 @@ struct LinearEpilogue {
             if (n >= rows) return;
             const int count = cols - col0;   // of the result's rows that this chunk has, of 32
             if (pr.parts > 1) {
-                float* to = parts + ((int64_t(t.all) * pr.parts + t.part) * pr.cols + col0 - t.tq * pr.cols) * kRows + n - t.tp * kRows;
+                float* to = parts + ((int64_t(t.all) * pr.parts + t.part) * pr.cols + col0 - t.tq * pr.cols) * pr.high + n - t.tp * pr.high;
 #pragma unroll
                 for (int j = 0; j < 32; ++j)
-                    if (j < count) to[j * kRows] = v[j];
+                    if (j < count) to[j * pr.high] = v[j];
                 return;
             }
             const float b = f.bias ? load_float(f.bias, f.bias_f32, n) : 0.f;
@@ -138,17 +138,35 @@ struct Plan {
 };
 
 Shape shape_of(int64_t M, int64_t N, int64_t K, bool x_turned, bool w_turned) {
-    if (M > kAloneRows) return Shape{true, M, N, K, 1, false, 1, 256, w_turned ? 128 : 64, w_turned ? 128 : 32};   // blocks of 64 a CTA
+    if (M > kAloneRows)   // blocks of 64 a CTA
+        return Shape{true, M, N, K, 1, false, 1, 256, w_turned ? 128 : 64, w_turned ? 128 : 32, 2 * kRows};
     const int64_t to = x_turned ? 64 : 16;
     const int cols = int(std::max<int64_t>(1, (M + to - 1) / to) * to);
-    return Shape{false, N, M, K, 1, false, 1, cols, cols, cols};
+    return Shape{false, N, M, K, 1, false, 1, cols, cols, cols, kRows};
 }
 
 Plan plan_of(const Shape& s, const Cut& cut) { return Plan{s, cut, parts_bytes(s, cut)}; }
 
+// Alone, the tiles of whole sums have fewer than 128 rows of p where the last round is fuller then, which HBM bounds like the
+// others (the MMAs are of 128 all the same).  Measured, us with 128 and with these: 48 x 40,960 x 4,096 67.5 and 59.6, 100 x
+// 28,672 x 4,096 55.6 and 47.6, 48 x 20,000 x 1,024 14.4 and 13.4; where nothing is gained, as with 16,384 columns, 128 stay.
+Plan plan_of(Shape s, bool any_high) {
+    Plan best = plan_of(s, best_cut(s));
+    if (s.pair || !any_high || best.cut.parts > 1) return best;
+    int64_t least = cut_cycles(s, best.cut);
+    for (s.high = kRows - 8; s.high >= kRows / 2; s.high -= 8) {
+        Cut c = best.cut;
+        c.tiles = s.tiles(c.cols);
+        const int64_t cost = cut_cycles(s, c);
+        if (cost >= least) continue;
+        least = cost;
+        best = plan_of(s, c);
+    }
+    return best;
+}
+
 Plan plan_of(int64_t M, int64_t N, int64_t K, bool x_turned, bool w_turned) {
-    const Shape s = shape_of(M, N, K, x_turned, w_turned);
-    return plan_of(s, best_cut(s));
+    return plan_of(shape_of(M, N, K, x_turned, w_turned), !w_turned);
 }
 
 // Both products of a backward pass, in one launch where both are made by pairs.
@@ -159,7 +177,7 @@ struct BackwardPlan {
 
 BackwardPlan plan_backward(int64_t M, int64_t N, int64_t K) {
     const Shape sx = shape_of(M, K, N, false, true), sw = shape_of(N, K, M, true, true);
-    if (!sx.pair || !sw.pair || K == 0) return BackwardPlan{plan_of(sx, best_cut(sx)), plan_of(sw, best_cut(sw)), false};
+    if (!sx.pair || !sw.pair || K == 0) return BackwardPlan{plan_of(sx, false), plan_of(sw, false), false};
     Cut cx = {}, cw = {};
     best_cuts(sx, sw, cx, cw);
     return BackwardPlan{plan_of(sx, cx), plan_of(sw, cw), true};
@@ -204,7 +222,7 @@ bool describe(ProductLaunch<NP, 1, LinearEpilogue<PAIR>>& l, int at, const Produ
     l.pr[at] = problem_of(d.plan.shape, cut, p.turned, q.turned, has_runs(d));
     l.epi[at].f = d.f;
     l.epi[at].parts = d.parts;
-    return operand_map(&l.p[at], p, d.K, kRows) && operand_map(&l.q[at], q, d.K, PAIR ? cut.cols / 2 : cut.cols);
+    return operand_map(&l.p[at], p, d.K, PAIR ? kRows : d.plan.shape.high) && operand_map(&l.q[at], q, d.K, PAIR ? cut.cols / 2 : cut.cols);
 }
 
 acrl_status join(const Problem& pr, const Product& d, cudaStream_t s) {

@@ -153,17 +153,20 @@ int eights(int64_t M) { return M <= 32 ? int((M + 7) / 8) : M <= 48 ? 6 : 8; }
 }  // namespace
 
 // Above 16 rows the CTAs' loads of x count: with those of their 16 rows of the weight they come from L2 at some 80 bytes a
-// nanosecond of an SM, 70 where one CTA is resident.  Tensor memory's way reads x for 128 rows of the weight at once and HBM
-// bounds it, 5.9 TB/s, but it takes 3.5 us more to begin, to end and to join parts.  Measured, us here and there: 32 x 2,048 x
+// nanosecond of an SM and 0.4 us a CTA, or, where one CTA is resident, 70 and 1.2 us for each after the first.  Tensor memory's
+// way reads x for 128 rows of the weight at once and HBM bounds it, 5.9 TB/s, but it takes 3.5 us more to begin, to end and to
+// join parts.  Measured, us here and there: 32 x 2,048 x
 // 2,048 4.7 and 8.8, 64 x 2,048 x 2,048 6.7 and 9.7, 32 x 4,096 x 4,096 11.1 and 12.3, 48 x 4,096 x 4,096 17 and 13, 20 x 16,384 x
-// 4,096 31 and 26.
+// 4,096 31 and 26, 48 x 12,290 x 200 11.6 and 6.3.
 bool linear_few_rows(int64_t M, int64_t N, int64_t K) {
     if (M <= 0 || M > 64 || N <= 0 || K <= 0) return false;
     if (M <= 16) return true;
     const int64_t ctas = (N + kW - 1) / kW;
     const int T = eights(M);
-    const double rounds = T <= 4 ? std::max(1.0, ctas / 152.0) : double((ctas + 151) / 152);
-    return rounds * double(kW + 8 * T) * 2.0 * double(K) / (T <= 4 ? 80.0 : 70.0) < 3500.0 + 2.0 * double(N) * double(K) / 5900.0;
+    const double bytes = double(kW + 8 * T) * 2.0 * double(K), there = 3500.0 + 2.0 * double(N) * double(K) / 5900.0;
+    if (T <= 4) return std::max(1.0, ctas / 152.0) * (bytes / 80.0 + 400.0) < there;
+    const double rounds = double((ctas + 151) / 152);
+    return rounds * bytes / 70.0 + (rounds - 1.0) * 1200.0 < there;
 }
 
 acrl_status linear_few(const acrl_bf16* x, int64_t M, int64_t K, int64_t ldx, const acrl_bf16* w, int64_t N, int64_t ldw, const Finish& f,

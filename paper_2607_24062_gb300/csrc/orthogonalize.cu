@@ -494,7 +494,7 @@ struct Plan {
 };
 
 Plan plan_of(int64_t batch, int64_t rows, int64_t cols, int64_t K, bool lower, bool q_turned) {
-    const Shape s{true, rows, cols, K, batch, lower, 3, 256, q_turned ? 128 : 64, 0};
+    const Shape s{true, rows, cols, K, batch, lower, 3, 256, q_turned ? 128 : 64, 0, 2 * kRows};
     const Cut cut = best_cut(s);
     return Plan{s, cut, parts_bytes(s, cut)};
 }

@@ -86,7 +86,8 @@ def test_linear(M, N, K, dtype):
 
 
 @pytest.mark.parametrize("M,N,K", [(17, 33, 7), (24, 2051, 1030), (31, 520, 2051), (47, 1000, 1003), (60, 70, 9), (64, 2048, 2048), (64, 264, 520),
-                                   (20, 16384, 1027), (48, 4100, 4104), (65, 264, 520), (100, 1000, 520), (128, 515, 513)])
+                                   (20, 16384, 1027), (48, 4100, 4104), (65, 264, 520), (100, 1000, 520), (128, 515, 513),
+                                   (70, 20003, 1032), (128, 23000, 1500), (40, 12290, 200)])
 def test_a_few_dozen_rows(M, N, K):
     """What one kernel does in registers and the other in tensor memory, by size, with everything that follows the sum."""
     x, w = _matrix(M, K, 1, gap=8), _matrix(N, K, 2, std=K ** -0.5, gap=16)
