@@ -184,5 +184,7 @@ def linear_layer(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | Non
                  residual: torch.Tensor | None = None) -> torch.Tensor:
     """act(x W^T + bias) + residual for autograd: x [M, K] and weight [N, K] bf16, bias [N] and residual [M, N] bf16 or
     float32; bf16 [M, N].  With an activation the pre-activation is kept in bf16 for the backward.  The gradients have no
-    derivative of their own."""
+    derivative of their own.  To capture a backward into a graph, run it once before on another stream, and
+    keep no eager result of the same leaves alive meanwhile: torch would join that result's stream to the capture, and end the
+    process."""
     return _LinearLayer.apply(x, weight, bias, residual, act)

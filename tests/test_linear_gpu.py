@@ -338,6 +338,31 @@ def test_captured_and_replayed():
     assert all(_same(w, o) for w, o in zip(want, outs))
 
 
+def test_layer_captured_with_its_backward():
+    """A forward and its backward in one graph, replayed on other values, gives what the same calls give eagerly."""
+    M, N, K = 70, 264, 136
+    x, w = _matrix(M, K, 1).requires_grad_(), _matrix(N, K, 2, std=0.1).requires_grad_()
+    b, r = torch.randn(N, device=DEV).requires_grad_(), _matrix(M, N, 3).requires_grad_()
+    dy = _matrix(M, N, 4)
+    run = lambda: torch.autograd.grad(acrl.linear_layer(x, w, b, "gelu", r), (x, w, b, r), dy)   # noqa: E731
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.current_stream().wait_stream(side)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = run()
+    for seed in (5, 6):
+        with torch.no_grad():
+            x.copy_(_matrix(M, K, seed))
+            w.copy_(_matrix(N, K, seed + 2, std=0.1))
+            dy.copy_(_matrix(M, N, seed + 4))
+        g.replay()
+        torch.cuda.synchronize()
+        assert _same(run(), got)
+
+
 def test_more_than_two_to_the_31_elements():
     """An output whose offsets pass 32 bits, of rows that hold one value each."""
     M, N, K = 70000, 32768, 8
