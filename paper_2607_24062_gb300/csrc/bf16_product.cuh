@@ -77,7 +77,6 @@ struct Problem {
     int slabs;               // ceil(K / 64)
     int batch;
     int cols;                // of a tile: a multiple of 32 (pair; of 128 where q is not K-major) or of 16 (alone)
-    int high;                // rows of a tile of p: both CTAs' 256, or alone 128 or fewer, a multiple of eight
     int p_tiles, q_tiles;
     int parts, per;          // of the sum, of so many slabs
     int run;                 // slabs that one accumulator takes
@@ -86,9 +85,10 @@ struct Problem {
     uint32_t idesc;
     int tiles, units;        // tiles of one matrix; parts of all
     int pair;
+    int high;                // rows of a tile of p: both CTAs' 256, or alone 128 or fewer, a multiple of eight
 
     // The result's rows and columns of a tile: alone, the rows of q are the result's.
-    __host__ __device__ int tile_rows() const { return pair ? high : cols; }
+    __host__ __device__ int tile_rows() const { return pair ? 2 * kRows : cols; }
     __host__ __device__ int tile_cols() const { return pair ? cols : high; }
 };
 
@@ -522,18 +522,17 @@ struct WarpOut {
     }
 };
 
-// Sixteen columns of a warp's 32 lanes, added to v.
-__device__ __forceinline__ void tmem_add16(uint32_t taddr, float* v) {
-    uint32_t r[16];
+// Eight columns of a warp's 32 lanes, added to v.  (Sixteen at a time would not fit beside a long sum.)
+__device__ __forceinline__ void tmem_add8(uint32_t taddr, float* v) {
+    uint32_t r[8];
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
+        "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n"
         "tcgen05.wait::ld.sync.aligned;"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
         : "r"(taddr)
         : "memory");
 #pragma unroll
-    for (int j = 0; j < 16; ++j) v[j] += __uint_as_float(r[j]);
+    for (int j = 0; j < 8; ++j) v[j] += __uint_as_float(r[j]);
 }
 
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const float* v) {
@@ -606,7 +605,7 @@ struct Drain {
             const bool last = i + 1 == runs;
             const uint32_t at = tmem + uint32_t(acc * kAccCols + first) + lanes;   // beyond the tile's columns, too
 #pragma unroll
-            for (int k = 0; k < 2 * kMost; ++k) tmem_add16(at + 64 * (k >> 1) + 16 * (k & 1), sum + 16 * k);
+            for (int k = 0; k < 4 * kMost; ++k) tmem_add8(at + 64 * (k >> 2) + 8 * (k & 3), sum + 8 * k);
             if (last) {   // what follows reads the whole sum as it would read one run's
 #pragma unroll
                 for (int k = 0; k < 2 * kMost; ++k) tmem_st16(at + 64 * (k >> 1) + 16 * (k & 1), sum + 16 * k);
@@ -619,10 +618,10 @@ struct Drain {
         return ok;
     }
 
+    // The unit numbered u.
     template <class Epi>
-    __device__ __forceinline__ bool unit(const Problem& pr, const Unit& t, const Epi& epi) {
-        const int row0 = (PAIR ? (2 * t.tp + int(ring.rank)) * kRows : t.tp * pr.high) + quarter * 32;
-        const int rows = PAIR ? pr.rows : min(pr.rows, (t.tp + 1) * pr.high);
+    __device__ __forceinline__ bool unit(const Problem& pr, int u, const Epi& epi) {
+        Unit t = unit_at(pr, u);
 #pragma unroll 1
         for (int pass = dry ? 0 : 1; pass < 2; ++pass) {
             const bool live = pass == 1;
@@ -630,6 +629,12 @@ struct Drain {
                 give_up(&ring.bars->abort, ring.flags);
                 return false;
             }
+            if constexpr (LONG) {   // worked out again: kept beside a long sum it would take registers that the sum needs
+                asm volatile("" : "+r"(u));
+                t = unit_at(pr, u);
+            }
+            const int row0 = (PAIR ? (2 * t.tp + int(ring.rank)) * kRows : t.tp * pr.high) + quarter * 32;
+            const int rows = PAIR ? pr.rows : min(pr.rows, (t.tp + 1) * pr.high);   // of the result, as far as the tile goes
             if (live && first >= pr.cols) release();   // a tile of 32 columns has none for this warp
 #pragma unroll 1
             for (int c = first; c < pr.cols; c += 64) {
@@ -746,7 +751,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
     } else {
         Drain<PAIR, LONG> role(b.ring, b.tmem, b.staging);
         for (Units<PAIR, NP, L> w(l); w.more(); w.next())
-            if (!role.unit(w.problem(), w.unit(), l.epi[NP == 2 ? w.which : 0])) break;
+            if (!role.unit(w.problem(), w.u, l.epi[NP == 2 ? w.which : 0])) break;
     }
     end_products<PAIR>(b.tmem);
 }

@@ -467,7 +467,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) steps_kernel(const __grid_
             if (at.k == at.last) e.f.kind = kResult;
 #pragma unroll 1
             for (int u = at.first(); u < pr.units && ok; u += at.pairs) {
-                ok = role.unit(pr, unit_at(pr, u), e) && come_in_turn();
+                ok = role.unit(pr, u, e) && come_in_turn();
             }
             if (pr.parts > 1 && ok) {
                 ok = warp_wait(&bars->passed, joins++ & 1u, abort);
