@@ -62,11 +62,6 @@ struct ProductBarriers {
     uint64_t tfull[2];            // an accumulator is complete
     uint64_t tempty[2];           // the epilogue warps (pair: of both CTAs, on the even one) have read it
     uint64_t mma_done;
-    // for kernels whose CTAs wait for one another:
-    uint64_t written[2];          // the epilogue warps have written a unit, by its accumulator
-    uint64_t told[2];             // and the grid has been told
-    uint64_t passed;              // all CTAs have written their parts of sums
-    uint64_t joined;              // the epilogue warps have joined theirs
     uint32_t tmem_base;
     int32_t abort;
 };
@@ -678,12 +673,6 @@ __device__ __forceinline__ Begun begin_products(uint8_t* smem, int stages, int s
             mbar_init(&bars->tempty[b], (PAIR ? 2 : 1) * kDrain);
         }
         mbar_init(&bars->mma_done, 1);
-        for (int b = 0; b < 2; ++b) {
-            mbar_init(&bars->written[b], kDrain);
-            mbar_init(&bars->told[b], 1);
-        }
-        mbar_init(&bars->passed, 1);
-        mbar_init(&bars->joined, kDrain);
         bars->abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(p)) : "memory");

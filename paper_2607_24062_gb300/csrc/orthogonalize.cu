@@ -325,7 +325,7 @@ struct StepsLaunch {
     float coeffs[3 * kMostSteps];
     int steps;
     float* parts;
-    unsigned* done;                   // CTAs' units written so far, of each matrix; with parts, of all
+    unsigned* done;                   // warps' shares of units written so far, of each matrix; with parts, of all
     int each;                         // a counter for each matrix
     int stages, stage_bytes;
     int32_t* flags;
@@ -346,10 +346,12 @@ struct Place {
     __device__ __forceinline__ int kind() const { return k % kProducts; }
     __device__ __forceinline__ int step() const { return k / kProducts; }
     __device__ __forceinline__ int first() const { return pair >= offset ? pair - offset : pair - offset + pairs; }
-    // This product's units add up to this much: two CTAs each.
-    __device__ __forceinline__ unsigned units(const Problem& pr) const { return 2u * unsigned(l.each ? pr.tiles : pr.units); }
+    // This product's units add up to this much: the epilogue warps of two CTAs each.
+    __device__ __forceinline__ unsigned units(const Problem& pr) const {
+        return 2u * unsigned(kDrain) * unsigned(l.each ? pr.tiles : pr.units);
+    }
     __device__ __forceinline__ void next(const Problem& pr) {
-        before += units(pr) + (pr.parts > 1 ? gridDim.x : 0u);
+        before += units(pr) + (pr.parts > 1 ? gridDim.x * unsigned(kDrain) : 0u);
         offset = (offset + pr.units) % pairs;
         ++k;
     }
@@ -370,31 +372,16 @@ __device__ __forceinline__ bool wait_done(const unsigned* counter, unsigned want
     }
 }
 
-// One thread tells the matrices' counters what the CTA has written.  Where sums are split it also waits for everyone's parts, lets
-// the epilogue warps join them, and tells of that.
-__device__ bool keep_counters(const StepsLaunch& l, ProductBarriers* bars) {
-    volatile int32_t* abort = &bars->abort;
-    auto tell = [&](unsigned* counter) {
-        __threadfence();
-        asm volatile("red.relaxed.gpu.global.add.u32 [%0], 1;" ::"l"(counter) : "memory");
-    };
-    unsigned n = 0, joins = 0;
-    for (Place at(l); at.more();) {
-        const Problem pr = l.pr[at.kind()];
-        for (int u = at.first(); u < pr.units; u += at.pairs, ++n) {
-            if (!wait_phase(&bars->written[n & 1u], (n >> 1) & 1u, abort)) return false;
-            tell(l.done + (l.each ? u / pr.tiles : 0));
-            mbar_arrive(&bars->told[n & 1u]);
-        }
-        if (pr.parts > 1) {
-            if (!wait_done(l.done, at.before + at.units(pr), abort)) return false;
-            mbar_arrive(&bars->passed);
-            if (!wait_phase(&bars->joined, joins++ & 1u, abort)) return false;
-            tell(l.done);
-        }
-        at.next(pr);
-    }
-    return true;
+// Whether all of the CTA's epilogue threads say so.  All of them come, whatever they say, and what they have written before is
+// visible to all of them.
+__device__ __forceinline__ bool epilogue_vote(bool ok) {
+    int all;
+    __syncwarp();
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.b32 p, %1, 0;\n bar.red.and.pred q, 1, %2, p;\n selp.b32 %0, 1, 0, q;\n}"
+                 : "=r"(all)
+                 : "r"(int(ok)), "n"(32 * kDrain)
+                 : "memory");
+    return all != 0;
 }
 
 __global__ void __launch_bounds__(kProductThreads, 1) steps_kernel(const __grid_constant__ StepsLaunch l) {
@@ -437,24 +424,19 @@ __global__ void __launch_bounds__(kProductThreads, 1) steps_kernel(const __grid_
             at.next(pr);
         }
         role.finish();
-    } else if (warp == 2) {
-        if ((threadIdx.x & 31) == 0 && !keep_counters(l, bars)) give_up(abort, l.flags);
     } else if (warp >= 4) {
         Drain<true, false> role(b.ring, b.tmem, b.staging);
-        unsigned n = 0, joins = 0;
-        auto come = [&](uint64_t* bar) {
+        // What the warp, or after a vote the CTA's epilogue, has written is visible to those who find it counted.  Every warp for
+        // itself, 256 x 256 takes 100 us, through a warp of the CTA that has waited for all 104; on the one counter that split sums
+        // have, 2,051 x 1,000 takes 258 so, and 242 with a vote.
+        auto tell = [&](unsigned* counter, unsigned shares) {
             __syncwarp();
-            if (role.lane == 0) mbar_arrive(bar);
+            if (role.lane == 0) {
+                __threadfence();
+                asm volatile("red.relaxed.gpu.global.add.u32 [%0], %1;" ::"l"(counter), "r"(shares) : "memory");
+            }
         };
-        // Not before the unit two before, which had the same barrier, has been told of: a warp that has read out an accumulator may
-        // still be storing when another is two units on, and the teller may be as far behind, to whom a barrier that has been
-        // passed twice looks as if it had not been at all.
-        auto come_in_turn = [&] {
-            if (n >= 2 && !warp_wait(&bars->told[n & 1u], ((n - 2) >> 1) & 1u, abort)) return false;
-            come(&bars->written[n & 1u]);
-            ++n;
-            return true;
-        };
+        const bool first = warp == 4;
 #pragma unroll 1
         for (Place at(l); at.more() && ok;) {
             const Problem pr = l.pr[at.kind()];
@@ -467,14 +449,21 @@ __global__ void __launch_bounds__(kProductThreads, 1) steps_kernel(const __grid_
             if (at.k == at.last) e.f.kind = kResult;
 #pragma unroll 1
             for (int u = at.first(); u < pr.units && ok; u += at.pairs) {
-                ok = role.unit(pr, u, e) && come_in_turn();
+                ok = role.unit(pr, u, e);
+                if (l.each) {
+                    if (ok) tell(l.done + u / pr.tiles, 1);
+                } else {
+                    ok = epilogue_vote(ok);
+                    if (ok && first) tell(l.done, kDrain);
+                }
             }
             if (pr.parts > 1 && ok) {
-                ok = warp_wait(&bars->passed, joins++ & 1u, abort);
+                ok = epilogue_vote(!first || role.lane != 0 || wait_done(l.done, at.before + at.units(pr), abort));
                 if (!ok) give_up(abort, l.flags);
                 else {
                     e.join(pr, int(blockIdx.x) * kDrain + warp - 4, int(gridDim.x) * kDrain, role.out);
-                    come(&bars->joined);
+                    epilogue_vote(true);
+                    if (first) tell(l.done, kDrain);
                 }
             }
             at.next(pr);
