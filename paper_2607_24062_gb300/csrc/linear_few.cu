@@ -1,4 +1,4 @@
-// A layer of up to 16 rows, single tokens first of all, and a small layer of up to 64: every byte of the weight is used once,
+// A layer of up to 16 rows, single tokens first of all, and a small layer of up to 256: every byte of the weight is used once,
 // and HBM bounds it.  Neither tensor memory nor a ring of copies: their start and end, and the join of a split sum, take longer
 // than the weight of a layer.
 // A CTA has 16 rows of the weight; its eight warps take turns along the sum, 128 columns each, and their sums meet in shared
@@ -21,6 +21,7 @@ struct FewArgs {
     const acrl_bf16 *x, *w;
     int64_t ldx, ldw;
     int M, N, K;
+    int ctas;   // of a block
     Finish f;
 };
 
@@ -55,12 +56,14 @@ __device__ __forceinline__ void mma_16x8(float (&c)[4], uint32_t a0, uint32_t a1
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// T: eights of x's rows.
-template <int T>
-__global__ void __launch_bounds__(kThreads, T == 1 ? 3 : T <= 4 ? 2 : 1) few_kernel(const __grid_constant__ FewArgs A) {
+// T: eights of x's rows, of all or of each of the BLOCKS that they are cut into.
+template <int T, bool BLOCKS>
+__global__ void __launch_bounds__(kThreads, T == 1 ? 3 : 2) few_kernel(const __grid_constant__ FewArgs A) {
     __shared__ float red[kWarps][8 * T][kW + 1];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const int n0 = int(blockIdx.x) * kW, K = A.K;
+    const int block = BLOCKS ? int(blockIdx.x) / A.ctas : 0;
+    const int n0 = (int(blockIdx.x) - block * A.ctas) * kW, m0 = block * 8 * T, M = BLOCKS ? min(A.M - m0, 8 * T) : A.M, K = A.K;
+    const acrl_bf16* X = A.x + m0 * A.ldx;
     const acrl_bf16* w0 = A.w + int64_t(min(n0 + g, A.N - 1)) * A.ldw;
     const acrl_bf16* w1 = A.w + int64_t(min(n0 + g + 8, A.N - 1)) * A.ldw;
     // The weight's first columns on their way to L2 before the launch before this one has ended.  (L2 is where all writes go: what
@@ -80,7 +83,7 @@ __global__ void __launch_bounds__(kThreads, T == 1 ? 3 : T <= 4 ? 2 : 1) few_ker
 #pragma unroll 1
             for (int k = k0 + 8 * t; k < k0 + 8 * t + kTurn && k - 8 * t < whole; k += 32) {
                 const uint4 a = eight<true>(w0 + k, k < whole), b = eight<true>(w1 + k, k < whole);
-                const uint4 x = eight<false>(A.x + g * A.ldx + k, g < A.M && k < whole);
+                const uint4 x = eight<false>(X + g * A.ldx + k, g < M && k < whole);
                 mma_16x8(c[0], a.x, b.x, a.y, b.y, x.x, x.y);
                 mma_16x8(c[0], a.z, b.z, a.w, b.w, x.z, x.w);
             }
@@ -97,9 +100,9 @@ __global__ void __launch_bounds__(kThreads, T == 1 ? 3 : T <= 4 ? 2 : 1) few_ker
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
                 const int k = k0 + 32 * i + 8 * t;
-                const acrl_bf16* p = A.x + (8 * r + g) * A.ldx + k;
-                if (T == 1) x[r][i] = g < A.M ? __ldg(reinterpret_cast<const uint4*>(p)) : make_uint4(0u, 0u, 0u, 0u);
-                else x[r][i] = eight<false>(p, 8 * r + g < A.M && k < whole);
+                const acrl_bf16* p = X + (8 * r + g) * A.ldx + k;
+                if (T == 1) x[r][i] = g < M ? __ldg(reinterpret_cast<const uint4*>(p)) : make_uint4(0u, 0u, 0u, 0u);
+                else x[r][i] = eight<false>(p, 8 * r + g < M && k < whole);
             }
         // each turn's products in a sum of their own: the tensor cores cut partial sums off, an error that grows with their number
 #pragma unroll
@@ -118,7 +121,7 @@ __global__ void __launch_bounds__(kThreads, T == 1 ? 3 : T <= 4 ? 2 : 1) few_ker
         const uint4 a = load8(w0, whole, t == 0 ? K : 0), b = load8(w1, whole, t == 0 ? K : 0);
 #pragma unroll
         for (int r = 0; r < T; ++r) {
-            const uint4 x = load8(A.x + (8 * r + g) * A.ldx, whole, t == 0 && 8 * r + g < A.M ? K : 0);
+            const uint4 x = load8(X + (8 * r + g) * A.ldx, whole, t == 0 && 8 * r + g < M ? K : 0);
             mma_16x8(c[r], a.x, b.x, a.y, b.y, x.x, x.y);
             mma_16x8(c[r], a.z, b.z, a.w, b.w, x.z, x.w);
         }
@@ -134,10 +137,11 @@ __global__ void __launch_bounds__(kThreads, T == 1 ? 3 : T <= 4 ? 2 : 1) few_ker
     const int64_t n = n0 + (threadIdx.x & (kW - 1));
     const Finish& f = A.f;
 #pragma unroll 1
-    for (int m = threadIdx.x / kW; m < A.M && n < A.N; m += kThreads / kW) {
+    for (int i = threadIdx.x / kW; i < M && n < A.N; i += kThreads / kW) {
+        const int64_t m = m0 + i;
         float v[1] = {};
 #pragma unroll
-        for (int i = 0; i < kWarps; ++i) v[0] += red[i][m][n - n0];
+        for (int j = 0; j < kWarps; ++j) v[0] += red[j][i][n - n0];
         if (f.bias) v[0] += load_float(f.bias, f.bias_f32, n);
         if (f.pre) f.pre[m * f.ldp + n] = to_bf16(v[0]);
         apply(f.act, v);
@@ -147,35 +151,31 @@ __global__ void __launch_bounds__(kThreads, T == 1 ? 3 : T <= 4 ? 2 : 1) few_ker
     }
 }
 
-// Eights of x's rows that a CTA goes through.
-int eights(int64_t M) { return M <= 32 ? int((M + 7) / 8) : M <= 48 ? 6 : 8; }
+constexpr int kMostFew = 256, kBlock = 32;   // rows of x, and of a block of them
 
 }  // namespace
 
 // Above 16 rows the CTAs' loads of x count: with those of their 16 rows of the weight they come from L2 at some 80 bytes a
-// nanosecond of an SM and 0.4 us a CTA, or, where one CTA is resident, 70 and 1.2 us for each after the first.  Tensor memory's
-// way reads x for 128 rows of the weight at once and HBM bounds it, 5.9 TB/s, but it takes 3.5 us more to begin, to end and to
-// join parts.  Measured, us here and there: 32 x 2,048 x
-// 2,048 4.7 and 8.8, 64 x 2,048 x 2,048 6.7 and 9.7, 32 x 4,096 x 4,096 11.1 and 12.3, 48 x 4,096 x 4,096 17 and 13, 20 x 16,384 x
-// 4,096 31 and 26, 48 x 12,290 x 200 11.6 and 6.3.
+// nanosecond of an SM, and a CTA has 0.4 us more.  Tensor memory's way reads x for 128 rows of the weight at once and HBM bounds
+// it, 5.9 TB/s, but it takes 3.5 us more to begin and to end, and of up to 128 rows 2 more where its tiles are so few that their
+// sums are split.  Measured, us here and there: 32 x 2,048 x 2,048 4.7 and 8.8, 64 x 2,048 x 2,048 6.3 and 9.7, 100 x 1,000 x 1,000
+// 4.5 and 8.2, 256 x 768 x 768 5.8 and 6.6, 128 x 4,096 x 512 6.9 and 10.1, 32 x 4,096 x 4,096 11.1 and 12.3; 48 x 4,096 x 4,096 18 and
+// 13, 64 x 1,024 x 5,120 9.8 and 8.4, 256 x 1,000 x 1,000 8.2 and 7.7.
 bool linear_few_rows(int64_t M, int64_t N, int64_t K) {
-    if (M <= 0 || M > 64 || N <= 0 || K <= 0) return false;
+    if (M <= 0 || M > kMostFew || N <= 0 || K <= 0) return false;
     if (M <= 16) return true;
-    const int64_t ctas = (N + kW - 1) / kW;
-    const int T = eights(M);
-    const double bytes = double(kW + 8 * T) * 2.0 * double(K), there = 3500.0 + 2.0 * double(N) * double(K) / 5900.0;
-    if (T <= 4) return std::max(1.0, ctas / 152.0) * (bytes / 80.0 + 400.0) < there;
-    const double rounds = double((ctas + 151) / 152);
-    return rounds * bytes / 70.0 + (rounds - 1.0) * 1200.0 < there;
+    const int64_t blocks = (M + kBlock - 1) / kBlock, T = blocks > 1 ? kBlock / 8 : (M + 7) / 8;
+    const double cta = double(kW + 8 * T) * 2.0 * double(K) / 80.0 + 400.0;
+    const double split = M <= 128 && (N + 127) / 128 * 4 <= 152 ? 2000.0 : 0.0;
+    return std::max(1.0, double(blocks * ((N + kW - 1) / kW)) / 152.0) * cta < 3500.0 + split + 2.0 * double(N) * double(K) / 5900.0;
 }
 
 acrl_status linear_few(const acrl_bf16* x, int64_t M, int64_t K, int64_t ldx, const acrl_bf16* w, int64_t N, int64_t ldw, const Finish& f,
                        cudaStream_t s) {
-    const FewArgs A{x, w, ldx, ldw, int(M), int(N), int(K), f};
-    const int T = eights(M);
-    return launch(T == 1 ? few_kernel<1> : T == 2 ? few_kernel<2> : T == 3 ? few_kernel<3> : T == 4 ? few_kernel<4> : T == 6 ? few_kernel<6>
-                                                                                                                             : few_kernel<8>,
-                  (N + kW - 1) / kW, kThreads, 0, 0, s, A);
+    const int64_t blocks = (M + kBlock - 1) / kBlock, ctas = (N + kW - 1) / kW, T = blocks > 1 ? kBlock / 8 : (M + 7) / 8;
+    const FewArgs A{x, w, ldx, ldw, int(M), int(N), int(K), int(ctas), f};
+    return launch(blocks > 1 ? few_kernel<4, true> : T == 1 ? few_kernel<1, false> : T == 2 ? few_kernel<2, false> :
+                  T == 3 ? few_kernel<3, false> : few_kernel<4, false>, blocks * ctas, kThreads, 0, 0, s, A);
 }
 
 }  // namespace acrl

@@ -87,8 +87,9 @@ def test_linear(M, N, K, dtype):
 
 @pytest.mark.parametrize("M,N,K", [(17, 33, 7), (24, 2051, 1030), (31, 520, 2051), (47, 1000, 1003), (60, 70, 9), (64, 2048, 2048), (64, 264, 520),
                                    (20, 16384, 1027), (48, 4100, 4104), (65, 264, 520), (100, 1000, 520), (128, 515, 513),
-                                   (70, 20003, 1032), (128, 23000, 1500), (40, 12290, 200)])
-def test_a_few_dozen_rows(M, N, K):
+                                   (70, 20003, 1032), (128, 23000, 1500), (40, 12290, 200), (100, 6000, 515), (128, 8200, 40),
+                                   (65, 131, 9000), (129, 264, 520), (200, 700, 77), (256, 768, 768), (255, 37, 1003)])
+def test_up_to_256_rows(M, N, K):
     """What one kernel does in registers and the other in tensor memory, by size, with everything that follows the sum."""
     x, w = _matrix(M, K, 1, gap=8), _matrix(N, K, 2, std=K ** -0.5, gap=16)
     b, r = torch.randn(N, device=DEV), _matrix(M, N, 5, gap=8)
