@@ -218,6 +218,38 @@ def test_streams_graphs_and_repetition():
     assert all(torch.equal(a, b) for a, b in zip(want, outs))
 
 
+def test_two_at_once_that_each_fill_the_gpu():
+    """On two streams, eagerly and from graphs, beside layers on a third: the CTAs of a call wait for one another, never for those
+    of another call."""
+    sets = [_update((30, 512, 512), 1), _update((16, 1024, 512), 2, BF)]
+    x, w = (torch.randn(n, 2048, device=DEV).to(BF) for n in (1024, 4096))
+    flags = [api.new_flags() for _ in sets]
+    want = [acrl.orthogonalize(t).clone() for t in sets]
+    y = acrl.linear(x, w).clone()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(5):
+        got.append([acrl.orthogonalize(t, flags=f, stream=s) for t, f, s in zip(sets, flags, streams)])
+        got[-1].append(acrl.linear(x, w, stream=streams[2]))
+    torch.cuda.synchronize()
+    assert [acrl.read_flags(f) for f in flags] == [0, 0]
+    assert all(torch.equal(a, b) for g in got for a, b in zip(want + [y], g))
+    graphs, outs = [], []
+    for t, f in zip(sets, flags):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append(acrl.orthogonalize(t, flags=f))
+        graphs.append(graph)
+    for _ in range(5):
+        for graph, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                graph.replay()
+    torch.cuda.synchronize()
+    assert [acrl.read_flags(f) for f in flags] == [0, 0]
+    assert all(torch.equal(a, b) for a, b in zip(want, outs))
+
+
 def test_nothing_and_refusals():
     g = _update((40, 72), 1)
     assert acrl.orthogonalize(g[:0]).shape == (0, 72) and acrl.orthogonalize(g[:, :0]).shape == (40, 0)
