@@ -789,11 +789,12 @@ struct Shape {
         return batch * (lower && p > 0 ? r * (p - 1) * p / 2 + q : p * q);
     }
     // Cycles of a slab: the MMAs, or the copies at 52 bytes a cycle of an SM; alone, where they come from HBM, no less than 3,800
-    // a turn of the ring (48 x 4,096 x 4,096 whole: 64 slabs 16 us, whether the tiles have 64 or 128 rows of p).
+    // a turn of the ring (48 x 4,096 x 4,096 whole: 64 slabs 16 us, whether the tiles have 64 or 128 rows of p), and of pairs, whose
+    // rings are deeper, no less than 450.
     int64_t slab(int cols) const {
         const int64_t mats = terms == 3 ? 2 : 1, mine = pair ? cols / 2 : cols, bytes = mats * (kRows + mine) * kRowBytes;
         const int64_t work = std::max<int64_t>(terms * (pair ? 2 : 4) * int64_t(cols), bytes / 52);
-        return pair ? work : std::max(work, 3800 / std::min<int64_t>(kMaxStages, kRingBytes / bytes));
+        return pair ? std::max<int64_t>(work, 450) : std::max(work, 3800 / std::min<int64_t>(kMaxStages, kRingBytes / bytes));
     }
     int64_t tile_bytes(int cols) const { return int64_t(high) * cols * 4; }
     int next(int cols) const { return step > 0 ? cols - step : cols / 2; }
@@ -801,6 +802,9 @@ struct Shape {
 
 constexpr int64_t kTileCycles = 500;                             // of a tile in a run of them
 constexpr int64_t kJoinCycles = 5000, kJoinBytes = 3000;         // of a join's launch; bytes a cycle
+constexpr int64_t kPartCycles = 1500;                            // of a part of pairs' sums: a join reads one after another
+// (with 450 cycles a slab and these: 768 x 4,096 x 1,024 18.4 -> 15.0 us, 2,048 x 8,192 x 256 20.5 -> 16.9, 200 x 4,096 x 4,096 18.5 ->
+// 17.2; 256 x 2,048 x 2,048 11.3 -> 11.9)
 constexpr int kPartChoices[] = {2, 3, 4, 5, 6, 8, 10, 12, 16};
 
 // Parts of equal length, none of them empty: false where `parts` is no such number.
@@ -811,7 +815,8 @@ inline bool part_length(int64_t slabs, int64_t parts, int64_t& per) {
 }
 
 inline int64_t join_cycles(const Shape& s, const Cut& c) {
-    return c.parts == 1 ? 0 : kJoinCycles + c.tiles * (c.parts + 1) * s.tile_bytes(c.cols) / kJoinBytes;
+    return c.parts == 1 ? 0 : kJoinCycles + (s.pair && s.terms == 1 ? c.parts * kPartCycles : 0) +
+                                  c.tiles * (c.parts + 1) * s.tile_bytes(c.cols) / kJoinBytes;
 }
 inline int64_t unit_cycles(const Shape& s, const Cut& c) { return c.per * s.slab(c.cols) + kTileCycles; }
 
