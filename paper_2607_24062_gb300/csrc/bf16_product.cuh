@@ -102,7 +102,8 @@ struct ColumnSums {
     float* out;        // or null
 
     __device__ __forceinline__ void run(int warp, int warps) const {
-        for (int c = warp * 32 + int(threadIdx.x & 31); c < cols; c += warps * 32) {
+        const int64_t step = int64_t(warps) * 32;   // as wide as a grid of its own: an int would pass 2^31 beside the most columns
+        for (int64_t c = int64_t(warp) * 32 + int(threadIdx.x & 31); c < cols; c += step) {
             float sum[8] = {};
             for (int p = 0; p < count; p += 8) {
 #pragma unroll
