@@ -345,6 +345,7 @@ __global__ void __launch_bounds__(32) sums_kernel(ColumnSums sums) {
 }
 
 bool dtype_ok(acrl_dtype d) { return d == ACRL_BF16 || d == ACRL_F32; }
+bool on_its_type(const void* p, bool f32) { return (reinterpret_cast<uintptr_t>(p) & (f32 ? 3 : 1)) == 0; }
 bool matrix_ok(const void* p, int64_t cols, int64_t ld) { return p && aligned16(p) && ld >= cols && (ld & 7) == 0; }
 
 // The backward's workspace: g, the columns' sums of its parts, the parts of the products' split sums.
@@ -389,10 +390,13 @@ extern "C" acrl_status acrl_linear(const acrl_bf16* x, int64_t M, int64_t K, int
     if (M == 0 || N == 0) return ACRL_OK;
     if (!matrix_ok(out, N, ldo) || (residual && !matrix_ok(residual, N, ldr)) || (pre && !matrix_ok(pre, N, ldp)))
         return ACRL_ERR_INVALID_ARG;
-    if (K > 0 && (!matrix_ok(x, K, ldx) || !matrix_ok(w, K, ldw) || !operands_on_current_device({x, w, out})))
-        return ACRL_ERR_INVALID_ARG;
+    if (K > 0 && (!matrix_ok(x, K, ldx) || !matrix_ok(w, K, ldw))) return ACRL_ERR_INVALID_ARG;
+    if (bias && !on_its_type(bias, bias_dtype == ACRL_F32)) return ACRL_ERR_INVALID_ARG;
     const int64_t need = acrl_linear_workspace_bytes(M, N, K);
-    if (need > 0 && (!workspace || !aligned16(workspace) || !operands_on_current_device({workspace}))) return ACRL_ERR_INVALID_ARG;
+    if (need > 0 && (!workspace || !aligned16(workspace))) return ACRL_ERR_INVALID_ARG;
+    auto used = [](bool is, const void* p) { return is ? p : nullptr; };
+    if (!operands_on_current_device({out, used(K > 0, x), used(K > 0, w), used(need > 0, workspace), bias, residual, pre}, true))
+        return ACRL_ERR_INVALID_ARG;
     const Finish f{bias, residual, out, pre, ldr, ldp, ldo, int(act), bias_dtype == ACRL_F32, residual_dtype == ACRL_F32,
                    out_dtype == ACRL_F32};
     if (linear_few_rows(M, N, K)) return linear_few(x, M, K, ldx, w, N, ldw, f, reinterpret_cast<cudaStream_t>(stream));
@@ -421,9 +425,11 @@ extern "C" acrl_status acrl_linear_backward(const acrl_bf16* dy, int64_t M, int6
     if (act == ACRL_ACT_NONE && pre) return ACRL_ERR_INVALID_ARG;
     if (has_g && ((has_dx && !matrix_ok(w, K, ldw)) || (has_dw && !matrix_ok(x, K, ldx)))) return ACRL_ERR_INVALID_ARG;
     if (!has_dx && !has_dw && !(dbias && N > 0)) return ACRL_OK;
-    if (has_g && parts.end > 0 && (!workspace || !aligned16(workspace))) return ACRL_ERR_INVALID_ARG;
-    if (has_g && !operands_on_current_device({dy, workspace})) return ACRL_ERR_INVALID_ARG;
-    if ((has_dx && has_g && !operands_on_current_device({w, dx})) || (has_dw && has_g && !operands_on_current_device({x, dw})))
+    if (has_g && (!workspace || !aligned16(workspace))) return ACRL_ERR_INVALID_ARG;
+    if (dbias && !on_its_type(dbias, true)) return ACRL_ERR_INVALID_ARG;
+    auto used = [](bool is, const void* p) { return is ? p : nullptr; };
+    if (!operands_on_current_device({used(has_g, dy), used(has_g, workspace), used(has_g, pre), used(has_dx, dx), used(has_dw, dw),
+                                     used(has_g && has_dx, w), used(has_g && has_dw, x), used(N > 0, dbias)}, true))
         return ACRL_ERR_INVALID_ARG;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     uint8_t* base = static_cast<uint8_t*>(workspace);

@@ -58,14 +58,15 @@ inline bool encode_map_3d(CUtensorMap* map, CUtensorMapDataType type, uint32_t b
 // memory, not host memory and not a peer GPU's memory.  The GEMM's tensor maps
 // are encoded over these pointers, and its TMA copies must stay within this
 // GPU's own memory.  A failed query counts as "no" and leaves no error behind
-// for a later launch check.
-inline bool operands_on_current_device(std::initializer_list<const void*> ptrs) {
+// for a later launch check.  With null_ok, null ones are not asked about.
+inline bool operands_on_current_device(std::initializer_list<const void*> ptrs, bool null_ok = false) {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) {
         (void)cudaGetLastError();
         return false;
     }
     for (const void* p : ptrs) {
+        if (null_ok && p == nullptr) continue;
         cudaPointerAttributes a{};
         if (cudaPointerGetAttributes(&a, p) != cudaSuccess) {
             (void)cudaGetLastError();
