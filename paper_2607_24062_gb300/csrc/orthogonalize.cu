@@ -410,6 +410,8 @@ __global__ void __launch_bounds__(kProductThreads, 1) steps_kernel(const __grid_
                         role.land();
                         break;
                     }
+                    // One lane has waited and whichever is elected copies: the vote orders no memory, this does.
+                    __syncwarp();
                     asm volatile("fence.proxy.async;" ::: "memory");   // copies read what others' stores have written
                 }
                 ok = role.unit(pr, t, p, q);

@@ -21,3 +21,14 @@ def test_aligned_cluster_barriers_follow_a_warp_sync():
             before = text[:m.start()].rstrip()
             assert re.search(r"__syncwarp\(\);\s*asm volatile\(\s*\"$", before), (path, before[-120:])
     assert found >= 1
+
+
+def test_copies_of_what_others_wrote_follow_a_warp_sync():
+    """One lane waits for other CTAs' stores to global memory, and whichever lane is elected issues the copies that read them. A
+    vote alone orders no memory between the two; __syncwarp does, and the proxy fence comes after it."""
+    found = 0
+    for path, text in _sources().items():
+        for m in re.finditer(r"asm volatile\(\"fence\.proxy\.async;\"", text):
+            found += 1
+            assert re.search(r"__syncwarp\(\);\s*$", text[:m.start()]), (path, text[m.start() - 160: m.start()])
+    assert found >= 1
