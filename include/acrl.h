@@ -655,9 +655,10 @@ acrl_status acrl_fp8_linear_backward(const acrl_bf16* dy, int64_t M, int64_t N, 
 /* ------------------------------------------------------------------------
  * A linear layer in bf16, the training engine's type (Sec. 5.1), its gradients,
  * and the update of its weight.  Matrices are row-major, 16-byte aligned, with a
- * row stride that is a multiple of 8 elements; sizes below 2^31 - 8,192.  Every
- * operand, output and workspace that a call uses is device memory of the current
- * device, as for the LM head; another place is refused.  dev_flags may be NULL.  Waits are time-bounded (ACRL_FLAG_TIMEOUT: the
+ * row stride that is a multiple of 8 elements; sizes below 2^31 - 8,192, the product
+ * of two of them below 2^48.  Every operand, output and workspace that a call uses
+ * is device memory of the current device, as for the LM head; another place is
+ * refused.  dev_flags may be NULL.  Waits are time-bounded (ACRL_FLAG_TIMEOUT: the
  * outputs are invalid).  Nothing is written beyond an output's columns.
  */
 typedef enum {

@@ -348,6 +348,12 @@ bool dtype_ok(acrl_dtype d) { return d == ACRL_BF16 || d == ACRL_F32; }
 bool on_its_type(const void* p, bool f32) { return (reinterpret_cast<uintptr_t>(p) & (f32 ? 3 : 1)) == 0; }
 bool matrix_ok(const void* p, int64_t cols, int64_t ld) { return p && aligned16(p) && ld >= cols && (ld & 7) == 0; }
 
+// A call's sizes; of a matrix of more than 2^48 numbers, which no GPU holds, the bytes of the workspace could leave 64 bits.
+bool sizes_ok(int64_t M, int64_t N, int64_t K) {
+    auto fits = [](int64_t a, int64_t b) { return double(a) * double(b) < 281474976710656.0; };
+    return M >= 0 && N >= 0 && K >= 0 && M <= kMostSize && N <= kMostSize && K <= kMostSize && fits(M, N) && fits(M, K) && fits(N, K);
+}
+
 // The backward's workspace: g, the columns' sums of its parts, the parts of the products' split sums.
 struct BackwardParts {
     BackwardPlan plan;
@@ -373,8 +379,7 @@ using namespace acrl;
 
 extern "C" int64_t acrl_linear_workspace_bytes(int64_t M, int64_t N, int64_t K) {
     if (M < 0 || N < 0 || K < 0) return -1;
-    return M == 0 || N == 0 || K == 0 || M > kMostSize || N > kMostSize || K > kMostSize || linear_few_rows(M, N, K) ? 0
-                                                                                                              : plan_linear(M, N, K).workspace;
+    return M == 0 || N == 0 || K == 0 || !sizes_ok(M, N, K) || linear_few_rows(M, N, K) ? 0 : plan_linear(M, N, K).workspace;
 }
 
 extern "C" acrl_status acrl_linear(const acrl_bf16* x, int64_t M, int64_t K, int64_t ldx, const acrl_bf16* w, int64_t N, int64_t ldw,
@@ -382,7 +387,7 @@ extern "C" acrl_status acrl_linear(const acrl_bf16* x, int64_t M, int64_t K, int
                                    acrl_dtype residual_dtype, int64_t ldr, acrl_bf16* pre, int64_t ldp, void* out,
                                    acrl_dtype out_dtype, int64_t ldo, void* workspace, int64_t workspace_bytes, int32_t* dev_flags,
                                    acrl_stream stream) {
-    if (M < 0 || N < 0 || K < 0 || M > kMostSize || N > kMostSize || K > kMostSize) return ACRL_ERR_INVALID_ARG;
+    if (!sizes_ok(M, N, K)) return ACRL_ERR_INVALID_ARG;
     if (act < ACRL_ACT_NONE || act > ACRL_ACT_SILU || !dtype_ok(out_dtype) || (bias && !dtype_ok(bias_dtype)) ||
         (residual && !dtype_ok(residual_dtype)))
         return ACRL_ERR_INVALID_ARG;
@@ -406,7 +411,7 @@ extern "C" acrl_status acrl_linear(const acrl_bf16* x, int64_t M, int64_t K, int
 }
 
 extern "C" int64_t acrl_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-    return M < 0 || N < 0 || K < 0 ? -1 : M > kMostSize || N > kMostSize || K > kMostSize ? 0 : BackwardParts(M, N, K).end;
+    return M < 0 || N < 0 || K < 0 ? -1 : sizes_ok(M, N, K) ? BackwardParts(M, N, K).end : 0;
 }
 
 extern "C" acrl_status acrl_linear_backward(const acrl_bf16* dy, int64_t M, int64_t N, int64_t lddy, const acrl_bf16* x, int64_t K,
@@ -414,7 +419,7 @@ extern "C" acrl_status acrl_linear_backward(const acrl_bf16* dy, int64_t M, int6
                                             const acrl_bf16* pre, int64_t ldp, void* dx, acrl_dtype dx_dtype, int64_t lddx, void* dw,
                                             acrl_dtype dw_dtype, int64_t lddw, float* dbias, void* workspace,
                                             int64_t workspace_bytes, int32_t* dev_flags, acrl_stream stream) {
-    if (M < 0 || N < 0 || K < 0 || M > kMostSize || N > kMostSize || K > kMostSize) return ACRL_ERR_INVALID_ARG;
+    if (!sizes_ok(M, N, K)) return ACRL_ERR_INVALID_ARG;
     if (act < ACRL_ACT_NONE || act > ACRL_ACT_SILU || (dx && !dtype_ok(dx_dtype)) || (dw && !dtype_ok(dw_dtype)))
         return ACRL_ERR_INVALID_ARG;
     const BackwardParts parts(M, N, K);

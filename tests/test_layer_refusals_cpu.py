@@ -38,3 +38,25 @@ def test_outputs_of_empty_sums_are_looked_at(L):
     assert _call(L.acrl_linear_backward, back, dw=FAKE) == E
     assert _call(L.acrl_linear_backward, back, db=FAKE) == E
     assert _call(L.acrl_linear_backward, back, M=5, N=0, lddy=0, ldx=40, dx=FAKE, lddx=40) == E
+
+
+MOST = 2 ** 31 - 8193
+
+
+def test_sizes_of_matrices_that_no_gpu_holds(L):
+    """The workspace of the largest sizes is counted within 64 bits, or the sizes are refused: never a number below zero."""
+    for M in (1, 5, 300, 2 ** 17, 2 ** 24, MOST):
+        for N in (1, 40, 2 ** 17, 2 ** 24, 2 ** 31 - 8200, MOST):
+            for K in (0, 1, 40, 2 ** 17, 2 ** 24, MOST):
+                held = max(M * N, M * K, N * K) < 2 ** 48
+                n = L.acrl_linear_backward_workspace_bytes(M, N, K)
+                assert (n >= M * N * 2 and n < 2 ** 60) if held else n == 0
+                assert 0 <= L.acrl_linear_workspace_bytes(M, N, K) < 2 ** 60
+    # nothing is asked for, so that the sizes alone are refused
+    back = dict(dy=FAKE, M=5, N=24, lddy=2 ** 31, x=None, K=40, ldx=0, w=None, ldw=0, act=0, pre=None, ldp=0, dx=None, tx=0, lddx=0,
+                dw=None, tw=1, lddw=0, db=None, ws=None, n=2 ** 62, flags=None, stream=None)
+    for fine in (dict(), dict(M=MOST), dict(N=MOST), dict(K=MOST), dict(M=2 ** 24, N=2 ** 24 - 1)):
+        assert _call(L.acrl_linear_backward, back, **fine) == OK, fine
+    for bad in (dict(M=MOST, N=MOST), dict(M=MOST, K=MOST), dict(N=MOST, K=MOST), dict(M=2 ** 24, N=2 ** 24), dict(M=MOST + 1),
+                dict(N=MOST + 1), dict(K=MOST + 1)):
+        assert _call(L.acrl_linear_backward, back, **bad) == E, bad
