@@ -676,7 +676,7 @@ typedef enum {
  *   x     device bf16 [M, ldx], K columns;  w  device bf16 [N, ldw], K columns.
  *   bias  device float or bf16 [N] (of its own alignment), or NULL.
  *   residual  device bf16 or float [M, ldr], or NULL; it may be `out` itself, of
- *         the same type and stride.
+ *         the same type and stride (others are refused).
  *   pre   device bf16 [M, ldp] or NULL: u, rounded, for acrl_linear_backward.
  *   out   device bf16 or float [M, ldo].
  *   workspace  device, 16-byte aligned, acrl_linear_workspace_bytes(M, N, K)

@@ -396,6 +396,8 @@ extern "C" acrl_status acrl_linear(const acrl_bf16* x, int64_t M, int64_t K, int
     if (!matrix_ok(out, N, ldo) || (residual && !matrix_ok(residual, N, ldr)) || (pre && !matrix_ok(pre, N, ldp)))
         return ACRL_ERR_INVALID_ARG;
     if (K > 0 && (!matrix_ok(x, K, ldx) || !matrix_ok(w, K, ldw))) return ACRL_ERR_INVALID_ARG;
+    // each lane adds what it has read before it stores, if the two are the same matrix
+    if (residual == out && (residual_dtype != out_dtype || (M > 1 && ldr != ldo))) return ACRL_ERR_INVALID_ARG;
     if (bias && !on_its_type(bias, bias_dtype == ACRL_F32)) return ACRL_ERR_INVALID_ARG;
     const int64_t need = acrl_linear_workspace_bytes(M, N, K);
     if (need > 0 && (!workspace || !aligned16(workspace))) return ACRL_ERR_INVALID_ARG;

@@ -79,3 +79,15 @@ def test_gradients_operands_elsewhere_are_refused(M, N, K):
     for name in used:
         assert _entry("acrl_linear_backward", ok, **{name: base}) == _abi.ERR_INVALID_ARG, name
     assert _entry("acrl_linear_backward", ok, db=at["db"] + 2) == _abi.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("M,N,K", [(5, 24, 40), (300, 264, 520)])
+def test_a_residual_in_place_of_another_type_or_stride_is_refused(M, N, K):
+    x, w, out = _filled(M, K), _filled(N, K), _filled(M, 2 * N, dtype=F32)
+    ok = dict(x=x.data_ptr(), M=M, K=K, ldx=K, w=w.data_ptr(), N=N, ldw=K, bias=None, tb=0, act=0, r=out.data_ptr(), tr=1, ldr=N, pre=None,
+              ldp=0, out=out.data_ptr(), to=1, ldo=N, ws=None, n=api.linear_workspace_bytes(M, N, K), flags=None, stream=None)
+    assert ok["n"] == 0
+    assert _entry("acrl_linear", ok) == _abi.OK and bool((out.view(-1)[: M * N] == K + 1).all())
+    assert _entry("acrl_linear", ok, M=1, ldr=N + 8) == _abi.OK          # of one row no stride is used
+    for bad in (dict(tr=0), dict(to=0), dict(ldr=N + 8), dict(ldo=N + 8)):
+        assert _entry("acrl_linear", ok, **bad) == _abi.ERR_INVALID_ARG, bad
