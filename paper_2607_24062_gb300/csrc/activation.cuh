@@ -20,23 +20,75 @@ __device__ __forceinline__ float fast_recip(float x) {
 // 1 / (1 + e^-x).
 __device__ __forceinline__ float logistic(float x) { return fast_recip(1.f + ex2(-kLog2e * x)); }
 
-// Phi(u), and e^(-u^2 / 2) beside it: erfc by Abramowitz and Stegun's formula 7.1.26 (absolute error 1.5e-7), which takes one
-// exponential and one reciprocal.  CUDA's normcdff, more exact in the tail than a rounding to bf16 shows, cost a product of
-// 4,096 x 16,384 x 4,096 with its pre-activation 80 us of 380.
-__device__ __forceinline__ float normal_cdf(float u, float& bell) {
-    const float t = fast_recip(fmaf(0.3275911f * 0.70710678f, fabsf(u), 1.f));
-    bell = ex2(-0.5f * kLog2e * u * u);
-    const float tail = 0.5f * bell * t *
-                       fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-    return u < 0.f ? tail : 1.f - tail;
+// Two fp32 numbers in the pipe's packed instructions, which round as the single ones do.
+using Two = unsigned long long;
+__device__ __forceinline__ Two two(float a, float b) {
+    Two v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
+    return v;
+}
+__device__ __forceinline__ Two both(float c) { return two(c, c); }
+__device__ __forceinline__ void part(Two v, float (&u)[2]) { asm("mov.b64 {%0, %1}, %2;" : "=f"(u[0]), "=f"(u[1]) : "l"(v)); }
+__device__ __forceinline__ Two mul2(Two a, Two b) {
+    Two v;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+    return v;
+}
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+    Two v;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
+    return v;
+}
+
+// Phi(-|u|) of two numbers, and e^(-u^2 / 2) beside it.  With x = |u| and t = 1 / (1 + 0.31 x), e^(x^2 / 2) Phi(-x) is t times a
+// polynomial in t of degree seven, fitted by linear programming for the least relative error from x = 0 to 15.5: 1.7e-7, and
+// 4.6e-7 as evaluated in fp32.  So the tail keeps its digits as far down as fp32 goes: gelu(-10) to 2^-17 of itself, by the square's
+// rounding in the exponent.  (Abramowitz and Stegun's 7.1.26, fitted for its absolute error, was off by 1.6e-3 at -5 and 2e-2 at
+// -10.)  The exponential is a square, so that it does not vanish before its product with u does.  One exponential and one
+// reciprocal each, the rest in packed instructions: 4,096 x 16,384 x 1,024 89.6 us, of which the product alone takes 79.4; with single
+// ones 104, with 7.1.26 in single ones 96.
+__device__ __forceinline__ void normal_tail(const float (&u)[2], Two& tail, Two& bell) {
+    const Two v = two(u[0], u[1]);
+    const Two t = two(fast_recip(fmaf(0.31f, fabsf(u[0]), 1.f)), fast_recip(fmaf(0.31f, fabsf(u[1]), 1.f)));
+    float e[2];
+    part(mul2(mul2(v, both(-0.25f * kLog2e)), v), e);
+    const Two root = two(ex2(e[0]), ex2(e[1]));
+    bell = mul2(root, root);
+    constexpr float c[] = {0.0359040648f, -0.141878068f, 0.15556632f, -0.0153910015f, 0.11038553f, 0.107681662f, 0.124075733f, 0.123655833f};
+    Two p = both(c[0]);
+#pragma unroll
+    for (int k = 1; k < 8; ++k) p = fma2(p, t, both(c[k]));
+    tail = mul2(mul2(bell, t), p);
+}
+
+// u Phi(u): u less, or beyond 0 nothing but, its part of the tail.  (100 keeps infinity from the tail's zero.)
+__device__ __forceinline__ void gelu(float (&u)[2]) {
+    Two tail, bell;
+    normal_tail(u, tail, bell);
+    float t[2];
+    part(tail, t);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) u[j] = fmaf(-fabsf(fminf(u[j], 100.f)), t[j], fmaxf(u[j], 0.f));
+}
+
+// Phi(u) + u phi(u).
+__device__ __forceinline__ void gelu_slope(float (&u)[2]) {
+    Two tail, bell;
+    normal_tail(u, tail, bell);
+    float p[2];
+    part(tail, p);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) p[j] = u[j] < 0.f ? p[j] : 1.f - p[j];
+    part(fma2(mul2(two(u[0], u[1]), both(kNormal)), bell, two(p[0], p[1])), u);
 }
 
 template <int ACT>
 __device__ __forceinline__ float act(float u) {
     if (ACT == ACRL_ACT_RELU) return u > 0.f || u != u ? u : 0.f;
     if (ACT == ACRL_ACT_GELU) {
-        float bell;
-        return u * normal_cdf(u, bell);
+        float v[2] = {u, 0.f};
+        gelu(v);
+        return v[0];
     }
     if (ACT == ACRL_ACT_GELU_TANH) return u * logistic(kTanhK * fmaf(kTanhC * u * u, u, u));
     if (ACT == ACRL_ACT_SILU) return u * logistic(u);
@@ -44,13 +96,8 @@ __device__ __forceinline__ float act(float u) {
 }
 
 template <int ACT>
-__device__ __forceinline__ float act_slope(float u) {
+__device__ __forceinline__ float act_slope(float u) {   // not GELU's: gelu_slope
     if (ACT == ACRL_ACT_RELU) return u > 0.f ? 1.f : u != u ? u : 0.f;
-    if (ACT == ACRL_ACT_GELU) {
-        float bell;
-        const float p = normal_cdf(u, bell);
-        return fmaf(u * kNormal, bell, p);
-    }
     if (ACT == ACRL_ACT_GELU_TANH) {
         // beyond 30 the logistic function is 0 or 1, and u^2 could leave fp32's range
         const float v = u > 30.f ? 30.f : u < -30.f ? -30.f : u, v2 = v * v;
@@ -62,6 +109,27 @@ __device__ __forceinline__ float act_slope(float u) {
         return p == 0.f ? 0.f : p * fmaf(u, 1.f - p, 1.f);
     }
     return 1.f;
+}
+
+// f and f' of two numbers.
+template <int ACT>
+__device__ __forceinline__ void act2(float (&u)[2]) {
+    if (ACT == ACRL_ACT_GELU) {
+        gelu(u);
+    } else {
+        u[0] = act<ACT>(u[0]);
+        u[1] = act<ACT>(u[1]);
+    }
+}
+
+template <int ACT>
+__device__ __forceinline__ void act_slope2(float (&u)[2]) {
+    if (ACT == ACRL_ACT_GELU) {
+        gelu_slope(u);
+    } else {
+        u[0] = act_slope<ACT>(u[0]);
+        u[1] = act_slope<ACT>(u[1]);
+    }
 }
 
 __device__ __forceinline__ float load_float(const void* p, bool f32, int64_t i) {

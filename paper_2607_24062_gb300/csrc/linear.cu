@@ -288,8 +288,10 @@ __global__ void __launch_bounds__(256) slope_kernel(const acrl_bf16* dy, int64_t
             v[2 * j] = bf16_lo(dw[j]);
             v[2 * j + 1] = bf16_hi(dw[j]);
             if (ACT != ACRL_ACT_NONE) {   // the same with and without g: no fma into the sum
-                v[2 * j] = __fmul_rn(v[2 * j], act_slope<ACT>(bf16_lo(uw[j])));
-                v[2 * j + 1] = __fmul_rn(v[2 * j + 1], act_slope<ACT>(bf16_hi(uw[j])));
+                float u[2] = {bf16_lo(uw[j]), bf16_hi(uw[j])};
+                act_slope2<ACT>(u);
+                v[2 * j] = __fmul_rn(v[2 * j], u[0]);
+                v[2 * j + 1] = __fmul_rn(v[2 * j + 1], u[1]);
             }
         }
         if (ACT != ACRL_ACT_NONE && g) {

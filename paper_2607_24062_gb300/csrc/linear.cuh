@@ -50,9 +50,17 @@ __device__ __forceinline__ void store_float(void* p, bool f32, int64_t i, float 
 template <int N>
 __device__ __forceinline__ void apply(int which, float (&v)[N]) {
     by_act(which, [&](auto a) {
-        if constexpr (a != ACRL_ACT_NONE)
+        if constexpr (a != ACRL_ACT_NONE && N == 1) {
+            v[0] = act<a>(v[0]);
+        } else if constexpr (a != ACRL_ACT_NONE) {
 #pragma unroll
-            for (int j = 0; j < N; ++j) v[j] = act<a>(v[j]);
+            for (int j = 0; j < N; j += 2) {
+                float u[2] = {v[j], v[j + 1]};
+                act2<a>(u);
+                v[j] = u[0];
+                v[j + 1] = u[1];
+            }
+        }
         return ACRL_OK;
     });
 }

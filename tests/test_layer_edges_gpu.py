@@ -1,5 +1,7 @@
 """The bf16 layer, its gradients and the update at the edges of what their entry points accept."""
 
+import math
+
 import pytest
 import torch
 
@@ -91,3 +93,76 @@ def test_a_residual_in_place_of_another_type_or_stride_is_refused(M, N, K):
     assert _entry("acrl_linear", ok, M=1, ldr=N + 8) == _abi.OK          # of one row no stride is used
     for bad in (dict(tr=0), dict(to=0), dict(ldr=N + 8), dict(ldo=N + 8)):
         assert _entry("acrl_linear", ok, **bad) == _abi.ERR_INVALID_ARG, bad
+
+
+def _unit(n):
+    """n roundings to 24 bits, of half a step each."""
+    return n * 2.0 ** -24
+
+
+def _tail(act, u):
+    """In 64 bits: f and f', and how far fp32 may be off, each a sum of relative errors times the terms that they are errors of.
+    Of 2^-24 each: an exponent z (a product of a few roundings, 2.5 for gelu's u^2 / 2 with its constant, 5 for the tanh form's)
+    comes back as that many times |z|; an exponential and its square 10; a reciprocal and what it is of 5; gelu's polynomial 8 and
+    the reciprocal in it again 5; the products a few.  Results below fp32's normal numbers to a few of its least steps."""
+    u = u.double()
+    if act == "gelu":
+        p, q, bell = torch.erfc(-u / 2 ** 0.5) / 2, torch.erfc(u / 2 ** 0.5) / 2, torch.exp(-u * u / 2) / (2 * math.pi) ** 0.5
+        each, slope = _unit(32) + _unit(2.5) * u * u / 2, p + u * bell
+        # beyond 0 Phi is 1 less its tail
+        off_p = each * torch.where(u < 0, p, q) + _unit(2) * p
+        off_f, off_s = u.abs() * off_p + _unit(2) * (u * p).abs(), off_p + (each + _unit(4)) * u.abs() * bell
+    else:
+        if act == "silu":
+            z, dz, n = u, torch.ones_like(u), 1
+        else:
+            k = (8 / math.pi) ** 0.5
+            z, dz, n = k * (u + 0.044715 * u ** 3), k * (1 + 3 * 0.044715 * u * u), 5
+        p, q = torch.sigmoid(z), torch.sigmoid(-z)
+        each = _unit(16) + _unit(n) * z.abs()
+        slope = p + u * p * q * dz
+        off_p = each * p * torch.where(z < 0, torch.ones_like(z), q) + _unit(6) * p
+        off_f = u.abs() * off_p + _unit(2) * (u * p).abs()
+        off_s = off_p + (2 * each + _unit(12)) * u.abs() * p * q * dz.abs()
+    least = 2.0 ** -149 * 4
+    return u * p, slope, off_f + least * (4 + u.abs()), off_s + least * (4 + u.abs() ** 3)
+
+
+def _within(got, exact, off, what):
+    """Rounding is monotone: `got` lies between the roundings of the ends of exact +- off."""
+    lo, hi = (exact - off).to(got.dtype), (exact + off).to(got.dtype)
+    bad = ~((got >= lo) & (got <= hi))
+    assert not bool(bad.any()), (what, int(bad.sum()), bad.nonzero()[:4].tolist(), got[bad][:4].tolist(), exact[bad][:4].tolist())
+
+
+@pytest.mark.parametrize("act,least", [("gelu", -14.5)])
+@pytest.mark.parametrize("M", [2, 40, 300])
+def test_activations_keep_their_digits_in_the_tail(act, least, M):
+    """f with an error relative to itself, as far down as fp32 goes, in each of the layer's kernels: u is the bias, of an empty
+    row's sum and of one of zeros."""
+    N = 16384
+    u = torch.cat([torch.linspace(least, 0, N // 2), torch.linspace(0, -least, N // 4), -torch.logspace(-30, 1, N // 8),
+                   torch.logspace(-30, 1, N // 8)]).to(DEV)
+    y, _, off, _ = _tail(act, u)
+    for K in (0, 8, 520):
+        x, w = torch.zeros((M, K), dtype=BF, device=DEV), torch.zeros((N, K), dtype=BF, device=DEV)
+        for dtype in (F32, BF):
+            out = acrl.linear(x, w, u, act=act, out_dtype=dtype)
+            assert bool((out == out[:1]).all())
+            _within(out[0], y, off, (K, dtype))
+
+
+@pytest.mark.parametrize("act,least", [("gelu", -14.5)])
+def test_slopes_keep_their_digits_in_the_tail(act, least):
+    """f' likewise: by dbias in fp32, and rounded to bf16 on its way through a product with the identity."""
+    u = torch.cat([torch.linspace(least, -least, 3900), torch.logspace(-30, 1, 98), -torch.logspace(-30, 1, 98)]).to(DEV).to(BF)
+    _, slope, _, off = _tail(act, u)
+    N = len(u)
+    one = torch.ones((1, N), dtype=BF, device=DEV)
+    none = torch.empty((N, 0), dtype=BF, device=DEV)
+    _, _, db = acrl.linear_backward(one, none[:1], none, act=act, pre=u[None], bias=True, need_dx=False, need_dw=False)
+    _within(db, slope, off, "dbias")
+    rows, eye = u.view(-1, 64), torch.eye(64, device=DEV).to(BF)
+    dx, _, _ = acrl.linear_backward(torch.ones_like(rows), torch.zeros_like(rows), eye, act=act, pre=rows, dx_dtype=F32, need_dw=False)
+    normal = slope.view(-1, 64).abs() >= 2.0 ** -120       # the tensor cores' products of smaller numbers are not at issue
+    _within(dx.to(BF)[normal], slope.view(-1, 64)[normal], off.view(-1, 64)[normal], "dx")
