@@ -667,7 +667,7 @@ typedef enum {
     ACRL_ACT_GELU = 2,        /* u Phi(u), Phi the normal distribution                      */
     ACRL_ACT_GELU_TANH = 3,   /* u (1 + tanh(sqrt(2 / pi) (u + 0.044715 u^3))) / 2          */
     ACRL_ACT_SILU = 4         /* u / (1 + e^-u)                                             */
-} acrl_activation;
+} acrl_activation;   /* in fp32, f and f' to some 2^-20 of themselves and their exponent's rounding, in the tails as well */
 
 /*
  * acrl_linear -- out = f(u) + residual, u = x W^T + bias: the product of bf16

@@ -17,9 +17,6 @@ __device__ __forceinline__ float fast_recip(float x) {
     return y;
 }
 
-// 1 / (1 + e^-x).
-__device__ __forceinline__ float logistic(float x) { return fast_recip(1.f + ex2(-kLog2e * x)); }
-
 // Two fp32 numbers in the pipe's packed instructions, which round as the single ones do.
 using Two = unsigned long long;
 __device__ __forceinline__ Two two(float a, float b) {
@@ -38,6 +35,20 @@ __device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
     Two v;
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
     return v;
+}
+
+// The logistic function of two numbers, p = 1 / (1 + e^-z), and q = 1 - p.  The exponential is the square of its root, taken down
+// by 2^-32 before: 2^-64 + 2^-64 e^-z stays a normal number down to z = -131, where p is zero in fp32, and p and q keep their
+// digits where they are small (1 / (1 + e^-z) as it stands is zero below -87.3, where silu is still -1e-36).  Below -131 q is no
+// number.
+__device__ __forceinline__ void logistic(Two z, Two& p, Two& q) {
+    float a[2], d[2];
+    part(mul2(z, both(-0.5f * kLog2e)), a);
+    const Two root = mul2(two(ex2(a[0]), ex2(a[1])), both(0x1p-32f));
+    part(fma2(root, root, both(0x1p-64f)), d);
+    const Two r = two(fast_recip(d[0]), fast_recip(d[1]));
+    p = mul2(r, both(0x1p-64f));
+    q = mul2(mul2(root, root), r);
 }
 
 // Phi(-|u|) of two numbers, and e^(-u^2 / 2) beside it.  With x = |u| and t = 1 / (1 + 0.31 x), e^(x^2 / 2) Phi(-x) is t times a
@@ -82,54 +93,60 @@ __device__ __forceinline__ void gelu_slope(float (&u)[2]) {
     part(fma2(mul2(two(u[0], u[1]), both(kNormal)), bell, two(p[0], p[1])), u);
 }
 
-template <int ACT>
-__device__ __forceinline__ float act(float u) {
-    if (ACT == ACRL_ACT_RELU) return u > 0.f || u != u ? u : 0.f;
-    if (ACT == ACRL_ACT_GELU) {
-        float v[2] = {u, 0.f};
-        gelu(v);
-        return v[0];
-    }
-    if (ACT == ACRL_ACT_GELU_TANH) return u * logistic(kTanhK * fmaf(kTanhC * u * u, u, u));
-    if (ACT == ACRL_ACT_SILU) return u * logistic(u);
+__device__ __forceinline__ float relu(float u) { return u > 0.f || u != u ? u : 0.f; }
+__device__ __forceinline__ float step(float u) { return u > 0.f ? 1.f : u != u ? u : 0.f; }
+
+// u at least `least` and, with BOTH, at most -least; a NaN stays one.
+template <bool BOTH>
+__device__ __forceinline__ float within(float u, float least) {
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(u) : "f"(least));
+    if (BOTH) asm("min.NaN.f32 %0, %0, %1;" : "+f"(u) : "f"(-least));
     return u;
 }
 
-template <int ACT>
-__device__ __forceinline__ float act_slope(float u) {   // not GELU's: gelu_slope
-    if (ACT == ACRL_ACT_RELU) return u > 0.f ? 1.f : u != u ? u : 0.f;
-    if (ACT == ACRL_ACT_GELU_TANH) {
-        // beyond 30 the logistic function is 0 or 1, and u^2 could leave fp32's range
-        const float v = u > 30.f ? 30.f : u < -30.f ? -30.f : u, v2 = v * v;
-        const float p = logistic(kTanhK * fmaf(kTanhC * v2, v, v));
-        return fmaf(v * p * (1.f - p), kTanhK * fmaf(3.f * kTanhC, v2, 1.f), p);
-    }
-    if (ACT == ACRL_ACT_SILU) {
-        const float p = logistic(u);
-        return p == 0.f ? 0.f : p * fmaf(u, 1.f - p, 1.f);
-    }
-    return 1.f;
-}
-
-// f and f' of two numbers.
+// f of two numbers.
 template <int ACT>
 __device__ __forceinline__ void act2(float (&u)[2]) {
-    if (ACT == ACRL_ACT_GELU) {
-        gelu(u);
-    } else {
-        u[0] = act<ACT>(u[0]);
-        u[1] = act<ACT>(u[1]);
+    if (ACT == ACRL_ACT_RELU) {
+        u[0] = relu(u[0]);
+        u[1] = relu(u[1]);
+    }
+    if (ACT == ACRL_ACT_GELU) gelu(u);
+    if (ACT == ACRL_ACT_GELU_TANH || ACT == ACRL_ACT_SILU) {
+        const Two v = two(u[0], u[1]);
+        Two p, q;
+        logistic(ACT == ACRL_ACT_SILU ? v : mul2(fma2(mul2(mul2(v, v), both(kTanhC)), v, v), both(kTanhK)), p, q);
+        part(mul2(v, p), u);
+    }
+}
+
+// f' of two numbers.  Of the logistic function's, numbers so small that p is zero are taken to ones where q is a number.
+template <int ACT>
+__device__ __forceinline__ void act_slope2(float (&u)[2]) {
+    if (ACT == ACRL_ACT_RELU) {
+        u[0] = step(u[0]);
+        u[1] = step(u[1]);
+    }
+    if (ACT == ACRL_ACT_GELU) gelu_slope(u);
+    if (ACT == ACRL_ACT_GELU_TANH) {   // beyond 11.5 p is 0 or 1, and u^2 could leave fp32's range
+        const Two v = two(within<true>(u[0], -11.5f), within<true>(u[1], -11.5f)), square = mul2(v, v);
+        Two p, q;
+        logistic(mul2(fma2(mul2(square, both(kTanhC)), v, v), both(kTanhK)), p, q);
+        part(fma2(mul2(v, mul2(p, q)), fma2(square, both(3.f * kTanhC * kTanhK), both(kTanhK)), p), u);
+    }
+    if (ACT == ACRL_ACT_SILU) {   // p (1 + u (1 - p))
+        const Two v = two(within<false>(u[0], -130.f), within<false>(u[1], -130.f));
+        Two p, q;
+        logistic(v, p, q);
+        part(mul2(p, fma2(v, q, both(1.f))), u);
     }
 }
 
 template <int ACT>
-__device__ __forceinline__ void act_slope2(float (&u)[2]) {
-    if (ACT == ACRL_ACT_GELU) {
-        gelu_slope(u);
-    } else {
-        u[0] = act_slope<ACT>(u[0]);
-        u[1] = act_slope<ACT>(u[1]);
-    }
+__device__ __forceinline__ float act(float u) {
+    float v[2] = {u, 0.f};
+    act2<ACT>(v);
+    return v[0];
 }
 
 __device__ __forceinline__ float load_float(const void* p, bool f32, int64_t i) {

@@ -102,9 +102,10 @@ def _unit(n):
 
 def _tail(act, u):
     """In 64 bits: f and f', and how far fp32 may be off, each a sum of relative errors times the terms that they are errors of.
-    Of 2^-24 each: an exponent z (a product of a few roundings, 2.5 for gelu's u^2 / 2 with its constant, 5 for the tanh form's)
-    comes back as that many times |z|; an exponential and its square 10; a reciprocal and what it is of 5; gelu's polynomial 8 and
-    the reciprocal in it again 5; the products a few.  Results below fp32's normal numbers to a few of its least steps."""
+    Of 2^-24 each: an exponent z, a product of a few roundings (2.5 for gelu's u^2 / 2 with its constant, 5 for the tanh form's,
+    1.25 for silu's with its constant), comes back as that many times |z|; an exponential and its square 10; a reciprocal and what
+    it is of 5; gelu's polynomial 8 and the reciprocal in it again 5; the products a few.  Results below fp32's normal numbers to a
+    few of its least steps."""
     u = u.double()
     if act == "gelu":
         p, q, bell = torch.erfc(-u / 2 ** 0.5) / 2, torch.erfc(u / 2 ** 0.5) / 2, torch.exp(-u * u / 2) / (2 * math.pi) ** 0.5
@@ -114,7 +115,7 @@ def _tail(act, u):
         off_f, off_s = u.abs() * off_p + _unit(2) * (u * p).abs(), off_p + (each + _unit(4)) * u.abs() * bell
     else:
         if act == "silu":
-            z, dz, n = u, torch.ones_like(u), 1
+            z, dz, n = u, torch.ones_like(u), 1.25
         else:
             k = (8 / math.pi) ** 0.5
             z, dz, n = k * (u + 0.044715 * u ** 3), k * (1 + 3 * 0.044715 * u * u), 5
@@ -135,7 +136,7 @@ def _within(got, exact, off, what):
     assert not bool(bad.any()), (what, int(bad.sum()), bad.nonzero()[:4].tolist(), got[bad][:4].tolist(), exact[bad][:4].tolist())
 
 
-@pytest.mark.parametrize("act,least", [("gelu", -14.5)])
+@pytest.mark.parametrize("act,least", [("gelu", -14.5), ("gelu_tanh", -10.5), ("silu", -110.0)])
 @pytest.mark.parametrize("M", [2, 40, 300])
 def test_activations_keep_their_digits_in_the_tail(act, least, M):
     """f with an error relative to itself, as far down as fp32 goes, in each of the layer's kernels: u is the bias, of an empty
@@ -152,7 +153,7 @@ def test_activations_keep_their_digits_in_the_tail(act, least, M):
             _within(out[0], y, off, (K, dtype))
 
 
-@pytest.mark.parametrize("act,least", [("gelu", -14.5)])
+@pytest.mark.parametrize("act,least", [("gelu", -14.5), ("gelu_tanh", -10.5), ("silu", -110.0)])
 def test_slopes_keep_their_digits_in_the_tail(act, least):
     """f' likewise: by dbias in fp32, and rounded to bf16 on its way through a product with the identity."""
     u = torch.cat([torch.linspace(least, -least, 3900), torch.logspace(-30, 1, 98), -torch.logspace(-30, 1, 98)]).to(DEV).to(BF)
@@ -166,3 +167,19 @@ def test_slopes_keep_their_digits_in_the_tail(act, least):
     dx, _, _ = acrl.linear_backward(torch.ones_like(rows), torch.zeros_like(rows), eye, act=act, pre=rows, dx_dtype=F32, need_dw=False)
     normal = slope.view(-1, 64).abs() >= 2.0 ** -120       # the tensor cores' products of smaller numbers are not at issue
     _within(dx.to(BF)[normal], slope.view(-1, 64)[normal], off.view(-1, 64)[normal], "dx")
+
+
+@pytest.mark.parametrize("act", ["relu", "gelu", "gelu_tanh", "silu"])
+def test_activations_of_the_largest_numbers(act):
+    """f and f' where an exponential over- or underflows, and of NaN."""
+    inf, nan = float("inf"), float("nan")
+    u = torch.tensor([-3e38, -1e30, -1e4, -300.0, 300.0, 1e4, 1e30, 3e38, inf, nan], device=DEV)
+    for M in (1, 300):
+        for dtype in (F32, BF):
+            y = acrl.linear(torch.zeros((M, 8), dtype=BF, device=DEV), torch.zeros((len(u), 8), dtype=BF, device=DEV), u, act=act, out_dtype=dtype)
+            assert bool((y[:, :4] == 0).all()) and torch.equal(y[:, 4:9], u[4:9].to(dtype).expand(M, 5)) and bool(y[:, 9].isnan().all())
+    u[8] = 200.0    # f' at infinity is not a limit that the formulas take
+    pre = u.to(BF)[None]
+    none = torch.empty((len(u), 0), dtype=BF, device=DEV)
+    slope = acrl.linear_backward(torch.ones_like(pre), none[:1], none, act=act, pre=pre, bias=True, need_dx=False, need_dw=False)[2]
+    assert slope[:9].tolist() == [0.0] * 4 + [1.0] * 5 and bool(slope[9].isnan())
