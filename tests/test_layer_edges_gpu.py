@@ -1,5 +1,6 @@
 """The bf16 layer, its gradients and the update at the edges of what their entry points accept."""
 
+import ctypes
 import math
 
 import pytest
@@ -81,6 +82,68 @@ def test_gradients_operands_elsewhere_are_refused(M, N, K):
     for name in used:
         assert _entry("acrl_linear_backward", ok, **{name: base}) == _abi.ERR_INVALID_ARG, name
     assert _entry("acrl_linear_backward", ok, db=at["db"] + 2) == _abi.ERR_INVALID_ARG
+
+
+ROOM = 1 << 16    # elements of each buffer below: more than any stride that is refused would reach
+
+
+def _refused(name, ok, bad):
+    """`ok` is accepted, and with each of the changes refused."""
+    assert _entry(name, ok) == _abi.OK
+    for changed in bad:
+        assert _entry(name, ok, **changed) == _abi.ERR_INVALID_ARG, changed
+    assert _entry(name, ok) == _abi.OK
+
+
+@pytest.mark.parametrize("M", [5, 300])
+def test_strides_and_alignments_that_are_refused(M):
+    N, K = 24, 40
+    b = {k: torch.ones(ROOM, dtype=F32, device=DEV) for k in ("x", "w", "bias", "r", "pre", "out", "dy", "dx", "dw", "db")}
+    p = {k: t.data_ptr() for k, t in b.items()}
+    n = api.linear_workspace_bytes(M, N, K)
+    assert n == 0
+    ok = dict(x=p["x"], M=M, K=K, ldx=40, w=p["w"], N=N, ldw=48, bias=p["bias"] + 2, tb=0, act=2, r=p["r"], tr=1, ldr=24, pre=p["pre"], ldp=24,
+              out=p["out"], to=0, ldo=24, ws=None, n=0, flags=None, stream=None)
+    _refused("acrl_linear", ok, [dict(x=None), dict(w=None), dict(out=None), dict(ldx=32), dict(ldx=44), dict(ldw=36), dict(ldw=32), dict(ldo=16),
+                                 dict(ldo=28), dict(ldr=20), dict(ldr=16), dict(ldp=20), dict(ldp=16), dict(x=p["x"] + 8), dict(w=p["w"] + 2),
+                                 dict(out=p["out"] + 8), dict(r=p["r"] + 4), dict(pre=p["pre"] + 2), dict(act=5), dict(to=2), dict(tb=2),
+                                 dict(tr=2), dict(n=-1)])
+    n = api.linear_backward_workspace_bytes(M, N, K)
+    ws = torch.empty(n + 16, dtype=torch.uint8, device=DEV)
+    ok = dict(dy=p["dy"], M=M, N=N, lddy=24, x=p["x"], K=K, ldx=40, w=p["w"], ldw=40, act=1, pre=p["pre"], ldp=24, dx=p["dx"], tx=0, lddx=40,
+              dw=p["dw"], tw=1, lddw=40, db=p["db"], ws=ws.data_ptr(), n=n, flags=None, stream=None)
+    _refused("acrl_linear_backward", ok, [dict(dy=None), dict(x=None), dict(w=None), dict(pre=None), dict(ws=None), dict(n=n - 1), dict(lddy=20),
+                                          dict(ldx=36), dict(ldw=32), dict(ldp=28), dict(lddx=32), dict(lddw=44), dict(act=5), dict(act=0),
+                                          dict(tx=2), dict(tw=-1), dict(dy=p["dy"] + 2), dict(x=p["x"] + 8), dict(w=p["w"] + 4),
+                                          dict(pre=p["pre"] + 8), dict(dx=p["dx"] + 4), dict(dw=p["dw"] + 2), dict(ws=ws.data_ptr() + 8)])
+
+
+@pytest.mark.parametrize("M,N,K", [(48, 1024, 16384), (129, 256, 8192)])
+def test_a_split_sums_workspace(M, N, K):
+    x, w, out = _filled(M, K), _filled(N, K), _filled(M, N, dtype=F32)
+    n = api.linear_workspace_bytes(M, N, K)
+    assert n > 0
+    ws = torch.full((n + 64,), 255, dtype=torch.uint8, device=DEV)
+    ok = dict(x=x.data_ptr(), M=M, K=K, ldx=K, w=w.data_ptr(), N=N, ldw=K, bias=None, tb=0, act=0, r=None, tr=0, ldr=0, pre=None, ldp=0,
+              out=out.data_ptr(), to=1, ldo=N, ws=ws.data_ptr(), n=n, flags=None, stream=None)
+    _refused("acrl_linear", ok, [dict(n=n - 1), dict(n=0, ws=None), dict(ws=None), dict(ws=ws.data_ptr() + 8), dict(n=-1)])
+    assert bool((out == K).all()) and bool((ws[n:] == 255).all())
+
+
+def test_updates_that_are_refused():
+    B, m, n = 2, 24, 40
+    g, out = (torch.ones(ROOM, dtype=t, device=DEV) for t in (F32, BF))
+    size = api.orthogonalize_workspace_bytes(B, m, n)
+    ws = torch.empty(size + 16, dtype=torch.uint8, device=DEV)
+    c = (ctypes.c_float * 15)(*[3.4445, -4.775, 2.0315] * 5)
+    ok = dict(g=g.data_ptr(), t=1, B=B, m=m, n=n, ldg=40, gs=24 * 40, c=c, steps=5, eps=1e-7, scale=1.0, out=out.data_ptr(), ldo=40,
+              os=24 * 40, ws=ws.data_ptr(), bytes=size, flags=None, stream=None)
+    host = torch.zeros(ROOM)
+    base = host.data_ptr() + 15 & ~15
+    _refused("acrl_orthogonalize", ok, [dict(g=None), dict(out=None), dict(ws=None), dict(c=None), dict(t=2), dict(ldg=36), dict(gs=24 * 40 - 1),
+                                        dict(ldo=32), dict(os=24 * 40 - 1), dict(g=g.data_ptr() + 2), dict(t=0, g=g.data_ptr() + 1),
+                                        dict(out=out.data_ptr() + 1), dict(ws=ws.data_ptr() + 8), dict(bytes=size - 1), dict(steps=0),
+                                        dict(steps=65), dict(eps=-1.0), dict(scale=float("nan")), dict(g=base), dict(out=base), dict(ws=base)])
 
 
 @pytest.mark.parametrize("M,N,K", [(5, 24, 40), (300, 264, 520)])
