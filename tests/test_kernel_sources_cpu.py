@@ -23,12 +23,15 @@ def test_aligned_cluster_barriers_follow_a_warp_sync():
     assert found >= 1
 
 
-def test_copies_of_what_others_wrote_follow_a_warp_sync():
-    """One lane waits for other CTAs' stores to global memory, and whichever lane is elected issues the copies that read them. A
-    vote alone orders no memory between the two; __syncwarp does, and the proxy fence comes after it."""
+def test_copies_of_what_others_wrote_follow_a_wait_of_every_lane():
+    """Whichever lane is elected issues the copies that read other CTAs' stores to global memory. If one lane alone has waited for
+    them, a vote does not order its acquire before the others' copies: every lane waits, or __syncwarp comes before the proxy
+    fence."""
     found = 0
     for path, text in _sources().items():
         for m in re.finditer(r"asm volatile\(\"fence\.proxy\.async;\"", text):
             found += 1
-            assert re.search(r"__syncwarp\(\);\s*$", text[:m.start()]), (path, text[m.start() - 160: m.start()])
+            before = text[:m.start()]
+            wait = before[before.rindex("wait_done(") - 40:]
+            assert re.search(r"__all_sync\(0xffffffffu, $", wait[:40]) or re.search(r"__syncwarp\(\);\s*$", before), (path, wait)
     assert found >= 1
