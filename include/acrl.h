@@ -659,7 +659,8 @@ acrl_status acrl_fp8_linear_backward(const acrl_bf16* dy, int64_t M, int64_t N, 
  * of two of them below 2^48.  Every operand, output and workspace that a call uses
  * is device memory of the current device, as for the LM head; another place is
  * refused.  dev_flags may be NULL.  Waits are time-bounded (ACRL_FLAG_TIMEOUT: the
- * outputs are invalid).  Nothing is written beyond an output's columns.
+ * outputs are invalid).  Nothing is written beyond an output's columns.  No output
+ * overlaps an operand or another output, but where that is said.
  */
 typedef enum {
     ACRL_ACT_NONE = 0,

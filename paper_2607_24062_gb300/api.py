@@ -796,7 +796,8 @@ def linear_backward(dy, x, weight, *, act=None, pre=None, bias=False, need_dx=Tr
                     dw_dtype=torch.float32, dx=None, dw=None, dbias=None, workspace=None, flags=None, stream=None):
     """acrl_linear_backward, the gradients of linear: with g = dy act'(pre), dx = g W, dw = g^T x and, with `bias`,
     dbias = sum of g over the rows.  dy bf16 [M, N], x bf16 [M, K], weight bf16 [N, K], `pre` the bf16 [M, N] that linear
-    wrote.  Returns (dx [M, K], dw [N, K], dbias float32 [N]), None where not asked for; the gradient of the residual is dy."""
+    wrote.  Returns (dx [M, K], dw [N, K], dbias float32 [N]), None where not asked for; the gradient of the residual is dy.  After
+    an activation g is rounded to bf16 for both products, whatever type dx and dw have."""
     M, N, lddy = _operand(dy, "dy")
     Mx, K, ldx = _operand(x, "x")
     Nw, Kw, ldw = _operand(weight, "weight")

@@ -11,6 +11,7 @@ namespace acrl {
 
 constexpr int64_t kMaxGrid = 2147483647LL;     // gridDim.x limit
 constexpr int64_t kMaxVocab = 1LL << 30;       // keeps vector indices in int range
+constexpr int64_t kMostSize = kMaxGrid - 8192; // a layer's or an update's rows and columns: a tile or a turn beyond them stays an int
 constexpr int64_t kWarpRowMaxV = 16384;        // rows up to this many columns use one warp each
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }

@@ -783,7 +783,7 @@ struct Shape {
     int high;   // rows of a tile
 
     int64_t slabs() const { return std::max<int64_t>(1, (K + kSlab - 1) / kSlab); }
-    int64_t lanes() const { return pair ? 76 : 152; }   // what a GPU of 152 SMs runs at once
+    int64_t lanes() const { return pair ? 76 : 152; }   // what a GPU of 152 SMs runs at once (another one is served, by these estimates)
     int64_t tiles(int cols) const {
         const int64_t p = (rows + high - 1) / high, q = (cols_all + cols - 1) / cols, r = high / cols;
         // of a symmetric matrix, each row tile but the last has r columns more than the one before

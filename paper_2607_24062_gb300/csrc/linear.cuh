@@ -9,8 +9,6 @@
 
 namespace acrl {
 
-constexpr int64_t kMostSize = kMaxGrid - 8192;   // rows and columns: what a loop or a tile goes beyond them stays an int
-
 // What follows the sum: out = f(sum + bias) + residual.
 struct Finish {
     const void *bias, *residual;
@@ -65,7 +63,7 @@ __device__ __forceinline__ void apply(int which, float (&v)[N]) {
     });
 }
 
-// N values of a row from column c on, as fp32; N a multiple of eight and c of four.
+// N values of a row from column c on, as fp32; N and c multiples of four.
 template <int N>
 __device__ __forceinline__ void load_row(const void* p, bool f32, int64_t row, int c, int cols, float (&v)[N]) {
     if (c + N > cols) {

@@ -1,5 +1,5 @@
-// A layer of up to 16 rows, single tokens first of all, and a small layer of up to 256: every byte of the weight is used once,
-// and HBM bounds it.  Neither tensor memory nor a ring of copies: their start and end, and the join of a split sum, take longer
+// A layer of up to 16 rows, single tokens first of all, and a small layer of up to 256.  Up to 32 rows every byte of the weight is
+// read once, and HBM bounds it; each further block of 32 reads the weight again, from L2.  Neither tensor memory nor a ring of copies: their start and end, and the join of a split sum, take longer
 // than the weight of a layer.
 // A CTA has 16 rows of the weight; its eight warps take turns along the sum, 128 columns each, and their sums meet in shared
 // memory.  The products are mma.sync m16n8k16, the weight's rows the 16 and those of x the eight: the pipes of tcgen05 would
@@ -34,7 +34,7 @@ __device__ __forceinline__ uint4 load8(const acrl_bf16* row, int k, int K) {
     return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
-// Eight numbers, or zeros, without a branch around the load; of the weight, which is read once, past L1.
+// Eight numbers, or zeros, without a branch around the load; of the weight, which a CTA reads once, past L1.
 template <bool ONCE>
 __device__ __forceinline__ uint4 eight(const acrl_bf16* p, bool there) {
     uint4 v = make_uint4(0u, 0u, 0u, 0u);

@@ -10,7 +10,7 @@
 // order, every pairs-th.  A tile of a product waits until its matrix's product before is written: a counter for each matrix says
 // how far it is (each wait is bounded in time).  So the matrices of a batch run into one another, and neither a part-filled round
 // nor the last tiles' stores hold up the next product: 24 x 1,024 x 1,024, launched product by product, 1,290 us; with a barrier of
-// the grid between them 1,274; as it is 1,163-1,190.
+// the grid between them 1,274; as it is 1,150-1,220, by the GPU.
 //
 // Operands are two bf16 numbers each, x = x0 + x1 with x0 the rounding of x and x1 that of what is left, which together are
 // within 2^-16 of it, and a product is three of the tensor cores' (bf16_product.cuh).  One bf16 number would not do: gradients
@@ -429,8 +429,8 @@ __global__ void __launch_bounds__(kProductThreads, 1) steps_kernel(const __grid_
     } else if (warp >= 4) {
         Drain<true, false> role(b.ring, b.tmem, b.staging);
         // What the warp, or after a vote the CTA's epilogue, has written is visible to those who find it counted.  Every warp for
-        // itself, 256 x 256 takes 100 us, through a warp of the CTA that has waited for all 104; on the one counter that split sums
-        // have, 2,051 x 1,000 takes 258 so, and 242 with a vote.
+        // itself, 256 x 256 took 100 us, through a warp of the CTA that has waited for all 104; on the one counter that split sums
+        // have, 2,051 x 1,000 took 258 so, and 242 with a vote.
         auto tell = [&](unsigned* counter, unsigned shares) {
             __syncwarp();
             if (role.lane == 0) {
@@ -568,8 +568,7 @@ using namespace acrl;
 
 namespace {
 bool sizes_ok(int64_t batch, int64_t m, int64_t n) {
-    constexpr int64_t kMost = kMaxGrid - 8192;   // what a loop or a tile goes beyond them stays an int
-    return batch >= 0 && m >= 0 && n >= 0 && batch <= kMost && m <= kMost && n <= kMost;
+    return batch >= 0 && m >= 0 && n >= 0 && batch <= kMostSize && m <= kMostSize && n <= kMostSize;
 }
 // Tiles, pieces and blocks of a launch are counted in 32 bits.
 bool blocks_ok(int64_t batch, int64_t m, int64_t n) {
